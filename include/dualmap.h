@@ -431,6 +431,191 @@ typedef enum {
 } dm_policy;
 dm_status dm_set_policy(dm_ctx* ctx, int policy);
 
+/* ---------------------------------------------------------------------------
+ * KV pages and attention over them: what an instance does with the blocks
+ * that the router counts.  A page holds one KV block (block_size tokens, the
+ * context's B) of every KV head; sequences list their pages in tables, and a
+ * prefix that several sequences share is one set of pages in all their
+ * tables.  The calls below do not wait for the device.  Malformed tables,
+ * page ids out of range and full outputs are found on the device and reported
+ * by dm_sync; no call reads or writes outside the arrays it was given.
+ * ------------------------------------------------------------------------- */
+
+typedef enum { DM_BF16 = 0, DM_F16 = 1 } dm_dtype;
+
+/* A store of pages: keys at k and values at v, each [layers][n_pages]
+ * [kv_heads][B][head_dim] elements of dtype with layer_stride elements from a
+ * layer to the next; 16-byte aligned, head_dim 64, 128 or 256, layer_stride a
+ * multiple of 8 and at least n_pages * kv_heads * B * head_dim, n_pages <
+ * 2^31. */
+typedef struct {
+    void* k;
+    void* v;
+    int64_t layer_stride;
+    uint32_t layers;
+    uint32_t n_pages;
+    uint32_t kv_heads;
+    uint32_t head_dim;
+    uint32_t dtype;    /* dm_dtype  */
+    uint32_t reserved; /* must be 0 */
+} dm_kv_pages;
+
+/* Page tables of n sequences (device arrays): sequence s holds pages
+ * page[off[s]] .. page[off[s+1] - 1] in order, of which the first
+ * ceil(len[s] / B) hold its len[s] < 2^31 tokens.  0 <= off[s] <= off[s+1] <=
+ * entries. */
+typedef struct {
+    const int64_t* off;  /* [n + 1]   */
+    const int32_t* page; /* [entries] */
+    const int64_t* len;  /* [n]       */
+    uint64_t n;
+    uint64_t entries;
+} dm_page_tables;
+
+/* Outputs of the calls that change tables (device arrays; none may overlap an
+ * input).  move_src/move_dst: pages whose data has to move, for
+ * dm_pages_copy, *moves of them.  live is dm_pages_compact's alone; off, len
+ * and cap are dm_pages_fork's. */
+typedef struct {
+    int64_t* off;      /* [m + 1]               */
+    int32_t* page;     /* [cap]                 */
+    int64_t* len;      /* [m]                   */
+    uint64_t cap;
+    int32_t* ref;      /* [n_pages]             */
+    int32_t* move_src; /* [move_cap]            */
+    int32_t* move_dst; /* [move_cap]            */
+    uint64_t move_cap;
+    int64_t* moves;    /* [1]                   */
+    int64_t* live;     /* [1] pages with ref > 0 */
+} dm_pages_out;
+
+/* The tables of the next step.  Sequence j of the result (j < m) holds the
+ * first keep[j] tokens of sequence src[j] (0 <= keep[j] <= its length; src is
+ * not read where keep[j] = 0) and room for grow[j] >= 0 more.  A sequence
+ * continued by several is forked, one continued by none is freed, a new one
+ * starts from the leading pages of a cached prefix (keep a multiple of B, e.g.
+ * B times the matched blocks that dm_route_batch reports) or from nothing.
+ * ref[p] (device int32 [n_pages]) counts the table entries that hold page p,
+ * and any other holder (a cached prefix without a sequence holds its pages by
+ * one more), so it is at least the number of entries; 0: free.  Pages are shared, not copied, with one exception: where
+ * sequence j is going to write into the last page that it keeps (keep[j] not a
+ * multiple of B, grow[j] > 0) and something else holds that page as well, j
+ * gets a page of its own and the pair joins the moves, in order of j; of
+ * several writers that alone hold a page, the first keeps it.  New pages are
+ * those with ref 0 on entry, lowest first, in the order of the result's
+ * entries; pages that the call frees are free for the next one.  out->ref gets
+ * the result's counts.  Nothing but *moves = 0 is written, and dm_sync
+ * reports it, if the tables or arguments are malformed, a table entry's page
+ * has no reference or a count is negative (DM_EINVAL), or free pages, cap or
+ * move_cap do not suffice (DM_EFULL).  n, m < 2^31; lengths stay below 2^31. */
+dm_status dm_pages_fork(dm_ctx* ctx, const dm_page_tables* in, const int32_t* ref,
+                        uint32_t n_pages, const int32_t* src, const int64_t* keep,
+                        const int64_t* grow, uint64_t m, const dm_pages_out* out);
+
+/* Live pages (ref > 0) moved together: with L of them, the k-th free page
+ * below L takes the k-th live page from L on, so that pages L and up are free.
+ * out->page gets the tables' entries after the moves (entries as in->entries;
+ * those outside every table are not written; off and len stay as they are),
+ * out->ref the counts, *live = L, and the moves their list.  Nothing but *moves
+ * = 0 is written if a table is malformed or holds a page without a reference
+ * or a count is negative (DM_EINVAL), or move_cap does not suffice (DM_EFULL).
+ * in->len is not read. */
+dm_status dm_pages_compact(dm_ctx* ctx, const dm_page_tables* in, const int32_t* ref,
+                           uint32_t n_pages, const dm_pages_out* out);
+
+/* Copies pages: for i < min(*count, cap), page src[i]'s keys and values to
+ * page dst[i], in every layer (src, dst: device int32 [cap]; count: device
+ * int64 [1]; *count > cap reports DM_EFULL).  Destinations must be distinct and
+ * none a source.  A pair with a page outside [0, n_pages) is left out and
+ * reported (DM_EINVAL). */
+dm_status dm_pages_copy(dm_ctx* ctx, const dm_kv_pages* kv, const int32_t* src,
+                        const int32_t* dst, const int64_t* count, uint64_t cap);
+
+/* New tokens of a batch: sequence s of the tables (lengths with the new tokens
+ * counted) has new tokens [q_off[s], q_off[s+1]) of the batch's q_tokens
+ * (q_off: device int64 [n + 1], 0 <= q_off[s] <= q_off[s+1] <= q_tokens <
+ * 2^31), the i-th at position len[s] - (q_off[s+1] - q_off[s]) + i of the
+ * sequence.  Tokens at negative positions (a place of a fixed batch with
+ * length 0) belong to no sequence.
+ * group_off (device int64 [groups + 1], group_off[0] = 0, non-decreasing, the
+ * last n; NULL with groups = 0: none) cuts the sequences into runs that may
+ * share a prefix; which pages a run's tables have in common is found on the
+ * device. */
+typedef struct {
+    dm_page_tables tables;
+    const int64_t* q_off;
+    uint64_t q_tokens;
+    const int64_t* group_off;
+    uint64_t groups;
+} dm_token_batch;
+
+/* Inputs and parameters of dm_kv_append.  q, k, v: the projections of the new
+ * tokens, token t's heads at q + t * q_stride (k, v alike; strides in
+ * elements, multiples of 8, at least heads * head_dim; heads contiguous).
+ * q_norm, k_norm: weights [head_dim], or NULL for no norm.  cos, sin: the
+ * rotation's tables [max_pos][rot_dim / 2], or NULL with rot_dim = 0; rot_dim a
+ * multiple of 16, at most head_dim.  interleaved: pairs are elements (2i, 2i +
+ * 1), else (i, i + rot_dim / 2). */
+typedef struct {
+    const void* q;
+    const void* k;
+    const void* v;
+    int64_t q_stride, k_stride, v_stride;
+    void* q_out;            /* [q_tokens] rows of q_heads * head_dim, q_out_stride apart */
+    int64_t q_out_stride;   /* q_out may be q, with its stride                           */
+    const void* q_norm;
+    const void* k_norm;
+    const float* cos;
+    const float* sin;
+    uint64_t max_pos;
+    uint32_t q_heads;
+    uint32_t rot_dim;
+    uint32_t interleaved;
+    float eps;
+} dm_append_args;
+
+/* Queries and keys of new tokens normed over each head, x / sqrt(mean(x^2) +
+ * eps) * weight, rotated by their positions, (a, b) -> (a cos - b sin, b cos +
+ * a sin), all in 32 bits, and rounded once: queries go to q_out, keys and the
+ * values as they are to their places in layer's pages.  Several tokens must
+ * not have one place (pages shared by sequences are not written: dm_pages_fork
+ * has seen to that).  A token at a negative position gets a q_out row of zeros
+ * and writes no page.  A token whose position is max_pos or past its table's
+ * pages, or whose page is out of range, is treated so too, and reported
+ * (DM_EINVAL).  Pointers 16-byte aligned. */
+dm_status dm_kv_append(dm_ctx* ctx, const dm_kv_pages* kv, uint32_t layer,
+                       const dm_token_batch* batch, const dm_append_args* args);
+
+/* Attention of a batch's new tokens over the pages: query head x reads KV head
+ * x / (q_heads / kv_heads), a token sees its own and the earlier positions of
+ * its sequence, out = sum_j w_j v_j / sum_j w_j with w_j = exp(scale q.k_j),
+ * lse = log sum_j w_j.  A token that sees nothing gets zeros and lse
+ * = -infinity.  Keys and values that a token does not see have no part in its
+ * result, whatever they hold.  Weights are kept in 32 bits and multiplied with
+ * the values in dtype; sums, maxima and results of parts are in 32 bits.
+ *
+ * dm_attn_plan looks at the batch's tables and cuts the work into items: the
+ * prefix pages that a run's sequences have in common are read once for all
+ * its queries, long rows are cut where there are few.  The plan (device, 16-byte
+ * aligned, dm_attn_plan_bytes(n, groups) bytes, the caller's) holds for this
+ * batch's tables, q_off and groups, for any layer and any number of dm_attn
+ * calls; it keeps no address.  dm_attn takes the same batch, kv (k, v and
+ * layers aside) and q_heads; q: token t's heads at q + t * q_stride, out
+ * alike (strides in elements, multiples of 8), lse NULL or float [q_tokens]
+ * [q_heads].  scale > 0.  q_heads a multiple of kv_heads. Rows past
+ * q_off[n] are not written.  A sequence whose table is malformed counts as
+ * length 0; one with a page out of range gets no defined result; both are
+ * reported (DM_EINVAL), and so is a plan of another batch (nothing written).
+ * dm_attn's work area is the context's: its size goes by q_tokens, q_heads and
+ * head_dim (it grows, synchronising once, only when a call needs more than
+ * any before it). */
+uint64_t dm_attn_plan_bytes(uint64_t n, uint64_t groups);
+dm_status dm_attn_plan(dm_ctx* ctx, const dm_token_batch* batch, const dm_kv_pages* kv,
+                       uint32_t q_heads, void* plan, uint64_t plan_bytes);
+dm_status dm_attn(dm_ctx* ctx, const dm_token_batch* batch, const dm_kv_pages* kv,
+                  uint32_t q_heads, const void* plan, uint32_t layer, const void* q,
+                  int64_t q_stride, float scale, void* out, int64_t out_stride, float* lse);
+
 /* Wait for all work on the context's stream (and, with pipelining, on its
  * work, selection and epilogue streams); return and clear the first
  * device-side error since the last dm_sync. */

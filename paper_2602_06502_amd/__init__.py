@@ -30,7 +30,8 @@ EXPORTS = ("dm_create", "dm_destroy", "dm_build_rings", "dm_ring_export", "dm_in
            "dm_kv_save", "dm_queue_append", "dm_queue_migrate", "dm_queue_drain", "dm_queue_reprobe",
            "dm_set_pipelining", "dm_set_policy", "dm_keylen_enable",
            "dm_keylen_window",
-           "dm_keylen_export", "dm_sync", "dm_last_error")
+           "dm_keylen_export", "dm_pages_fork", "dm_pages_compact", "dm_pages_copy", "dm_kv_append",
+           "dm_attn_plan_bytes", "dm_attn_plan", "dm_attn", "dm_sync", "dm_last_error")
 
 
 class DMError(RuntimeError):
@@ -70,6 +71,37 @@ class dm_migrations(C.Structure):
                 ("benefit_us", C.c_void_p), ("ttft_to_us", C.c_void_p), ("count", C.c_void_p)]
 
 
+class dm_kv_pages(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("layer_stride", C.c_int64),
+                ("layers", C.c_uint32), ("n_pages", C.c_uint32), ("kv_heads", C.c_uint32),
+                ("head_dim", C.c_uint32), ("dtype", C.c_uint32), ("reserved", C.c_uint32)]
+
+
+class dm_page_tables(C.Structure):
+    _fields_ = [("off", C.c_void_p), ("page", C.c_void_p), ("len", C.c_void_p), ("n", C.c_uint64),
+                ("entries", C.c_uint64)]
+
+
+class dm_pages_out(C.Structure):
+    _fields_ = [("off", C.c_void_p), ("page", C.c_void_p), ("len", C.c_void_p), ("cap", C.c_uint64),
+                ("ref", C.c_void_p), ("move_src", C.c_void_p), ("move_dst", C.c_void_p),
+                ("move_cap", C.c_uint64), ("moves", C.c_void_p), ("live", C.c_void_p)]
+
+
+class dm_token_batch(C.Structure):
+    _fields_ = [("tables", dm_page_tables), ("q_off", C.c_void_p), ("q_tokens", C.c_uint64),
+                ("group_off", C.c_void_p), ("groups", C.c_uint64)]
+
+
+class dm_append_args(C.Structure):
+    _fields_ = [("q", C.c_void_p), ("k", C.c_void_p), ("v", C.c_void_p), ("q_stride", C.c_int64),
+                ("k_stride", C.c_int64), ("v_stride", C.c_int64), ("q_out", C.c_void_p),
+                ("q_out_stride", C.c_int64), ("q_norm", C.c_void_p), ("k_norm", C.c_void_p),
+                ("cos", C.c_void_p), ("sin", C.c_void_p), ("max_pos", C.c_uint64),
+                ("q_heads", C.c_uint32), ("rot_dim", C.c_uint32), ("interleaved", C.c_uint32),
+                ("eps", C.c_float)]
+
+
 _lib = None
 
 
@@ -107,6 +139,13 @@ def load_library(path: str = LIB_PATH):
         "dm_keylen_enable": (i32, [P, u64, u64]),
         "dm_keylen_window": (i32, [P]),
         "dm_keylen_export": (i32, [P, P, u64, P]),
+        "dm_pages_fork": (i32, [P, P, P, u32, P, P, P, u64, P]),
+        "dm_pages_compact": (i32, [P, P, P, u32, P]),
+        "dm_pages_copy": (i32, [P, P, P, P, P, u64]),
+        "dm_kv_append": (i32, [P, P, u32, P, P]),
+        "dm_attn_plan_bytes": (u64, [u64, u64]),
+        "dm_attn_plan": (i32, [P, P, P, u32, P, u64]),
+        "dm_attn": (i32, [P, P, P, u32, P, u32, P, C.c_int64, C.c_float, P, C.c_int64, P]),
         "dm_sync": (i32, [P]),
         "dm_last_error": (C.c_char_p, [P]),
     }
@@ -143,6 +182,37 @@ def make_config(cfg: Dict) -> dm_config:
 
 def _ptr(t) -> Optional[int]:
     return None if t is None else t.data_ptr()
+
+
+class KVPages:
+    """A store of KV pages (see dm_kv_pages): keys and values, torch tensors
+    [layers, pages, kv_heads, block, head_dim] of one shape, bfloat16 or
+    float16, each layer contiguous."""
+
+    def __init__(self, k, v):
+        import torch
+        types = {torch.bfloat16: 0, torch.float16: 1}
+        if k.dim() != 5 or k.shape != v.shape or k.dtype != v.dtype or k.dtype not in types \
+                or k.device != v.device:
+            raise ValueError("k and v must be bfloat16 or float16 tensors of one shape "
+                             "[layers, pages, kv_heads, block, head_dim] on one device")
+        if k.shape[0] < 1 or k.shape[1] < 1 or k.stride() != v.stride() or not k[0].is_contiguous():
+            raise ValueError("k and v need a layer and a page, the same strides and contiguous layers")
+        self.k, self.v = k, v
+        self.layers, self.pages, self.kv_heads, self.block, self.head_dim = k.shape
+        self.dtype, self.device = k.dtype, k.device
+        stride = k.stride(0) if self.layers > 1 else k[0].numel()
+        self.struct = dm_kv_pages(k.data_ptr(), v.data_ptr(), stride, self.layers, self.pages,
+                                  self.kv_heads, self.head_dim, types[k.dtype], 0)
+        self._ref = C.byref(self.struct)
+
+
+class AttnPlan:
+    """A plan of DualMap.attn_plan: the batch that it was made for."""
+
+    def __init__(self, batch, kv, q_heads, buf, keep):
+        self.batch, self.kv, self.q_heads, self.buf = batch, kv, q_heads, buf
+        self._keep = keep  # the batch's tensors
 
 
 class DualMap:
@@ -457,3 +527,168 @@ class DualMap:
                                       _ptr(out["old"]), _ptr(out["new"]), _ptr(out["moved"]),
                                       _ptr(out["violations"])), "dm_scale")
         return out
+
+    # -- KV pages and attention over them: tables are tuples (off, page, len)
+    # of device tensors (int64 [n + 1], int32, int64 [n])
+    def _tables(self, tables):
+        t = self.torch
+        off, page, length = tables
+        off = self._dev(off, t.int64, "off")
+        page = self._dev(page, t.int32, "page")
+        length = self._dev(length, t.int64, "len")
+        if off.numel() != length.numel() + 1:
+            raise ValueError("off needs one entry more than len")
+        return dm_page_tables(off.data_ptr(), page.data_ptr(), length.data_ptr(), length.numel(),
+                              page.numel())
+
+    def _kv(self, kv):
+        if kv.device != self.device or kv.block != self.block:
+            raise ValueError("pages must be on %s and hold %d tokens" % (self.device, self.block))
+        return kv
+
+    def _pages_out(self, out, n_pages, m=None):
+        t = self.torch
+        o = {k: self._dev(out[k], t.int32, k) for k in ("page", "ref", "move_src", "move_dst")}
+        o.update({k: self._dev(out[k], t.int64, k)
+                  for k in (("moves", "off", "len") if m is not None else ("moves", "live"))})
+        if o["ref"].numel() != n_pages or o["moves"].numel() != 1 \
+                or o["move_src"].numel() != o["move_dst"].numel() \
+                or (m is not None and (o["off"].numel() != m + 1 or o["len"].numel() != m)) \
+                or (m is None and o["live"].numel() != 1):
+            raise ValueError("an output has the wrong size")
+        return dm_pages_out(_ptr(o.get("off")), o["page"].data_ptr(), _ptr(o.get("len")),
+                            o["page"].numel(), o["ref"].data_ptr(), o["move_src"].data_ptr(),
+                            o["move_dst"].data_ptr(), o["move_src"].numel(), o["moves"].data_ptr(),
+                            _ptr(o.get("live")))
+
+    def alloc_pages_out(self, n_pages: int, m: int, cap: int) -> Dict:
+        """Outputs of pages_fork_into for m sequences and cap entries (and, with cap the
+        tables' entries, of pages_compact_into)."""
+        t = self.torch
+        moves = max(m, n_pages // 2 + 1)
+        return dict(off=self._empty(m + 1, t.int64), page=self._empty(cap, t.int32),
+                    len=self._empty(m, t.int64), ref=self._empty(n_pages, t.int32),
+                    move_src=self._empty(moves, t.int32), move_dst=self._empty(moves, t.int32),
+                    moves=self._empty(1, t.int64), live=self._empty(1, t.int64))
+
+    def pages_fork_into(self, tables, ref, src, keep, grow, out: Dict) -> None:
+        """The tables of the next step (see dm_pages_fork) into preallocated
+        outputs: sequence j holds the first keep[j] tokens of src[j] and room
+        for grow[j] more.  out["move_src"], out["move_dst"] and out["moves"]
+        are pages_copy's list."""
+        t = self.torch
+        tb = self._tables(tables)
+        ref = self._dev(ref, t.int32, "ref")
+        src = self._dev(src, t.int32, "src")
+        keep = self._dev(keep, t.int64, "keep")
+        grow = self._dev(grow, t.int64, "grow")
+        m = src.numel()
+        if keep.numel() != m or grow.numel() != m:
+            raise ValueError("src, keep and grow must have one length")
+        o = self._pages_out(out, ref.numel(), m)
+        self._check(self.lib.dm_pages_fork(self._h, C.byref(tb), ref.data_ptr(), ref.numel(),
+                                           src.data_ptr(), keep.data_ptr(), grow.data_ptr(), m,
+                                           C.byref(o)), "dm_pages_fork")
+
+    def pages_fork(self, tables, ref, src, keep, grow, cap: int) -> Dict:
+        """pages_fork_into with outputs of its own (cap entries); page is cut
+        to the entries there are, which waits for the device."""
+        out = self.alloc_pages_out(ref.numel(), src.numel(), cap)
+        self.pages_fork_into(tables, ref, src, keep, grow, out)
+        self.sync()
+        out["page"] = out["page"][:int(out["off"][-1].item())]
+        return out
+
+    def pages_compact_into(self, tables, ref, out: Dict) -> None:
+        """Live pages moved together (see dm_pages_compact): out["page"], out["ref"],
+        out["live"] and the list of moves for pages_copy."""
+        tb = self._tables(tables)
+        ref = self._dev(ref, self.torch.int32, "ref")
+        o = self._pages_out(out, ref.numel())
+        if o.cap < tb.entries:
+            raise ValueError("page needs room for the tables' entries")
+        self._check(self.lib.dm_pages_compact(self._h, C.byref(tb), ref.data_ptr(), ref.numel(),
+                                              C.byref(o)), "dm_pages_compact")
+
+    def pages_copy(self, kv: KVPages, moves: Dict) -> None:
+        """Page data moved by a list of pages_fork or pages_compact (see dm_pages_copy)."""
+        t = self.torch
+        self._kv(kv)
+        src = self._dev(moves["move_src"], t.int32, "move_src")
+        dst = self._dev(moves["move_dst"], t.int32, "move_dst")
+        count = self._dev(moves["moves"], t.int64, "moves")
+        if src.numel() != dst.numel() or count.numel() != 1:
+            raise ValueError("move_src and move_dst must have one length, moves one entry")
+        self._check(self.lib.dm_pages_copy(self._h, kv._ref, src.data_ptr(), dst.data_ptr(),
+                                           count.data_ptr(), src.numel()), "dm_pages_copy")
+
+    def _batch(self, tables, q_off, q_tokens, groups=None):
+        t = self.torch
+        tb = self._tables(tables)
+        q_off = self._dev(q_off, t.int64, "q_off")
+        if q_off.numel() != tb.n + 1:
+            raise ValueError("q_off needs one entry more than len")
+        g = None if groups is None else self._dev(groups, t.int64, "groups")
+        return dm_token_batch(tb, q_off.data_ptr(), q_tokens, _ptr(g),
+                              0 if g is None else g.numel() - 1)
+
+    def _rows(self, x, name, heads, dim, tokens, dtype):
+        """Row stride of [tokens, heads, dim] with contiguous heads."""
+        if x.device != self.device or x.dtype != dtype or tuple(x.shape) != (tokens, heads, dim):
+            raise ValueError(f"{name} must be a {dtype} tensor {(tokens, heads, dim)} on {self.device}")
+        if x.numel() and (x.stride(2) != 1 or (heads > 1 and x.stride(1) != dim)):
+            raise ValueError(f"{name}'s heads must be contiguous")
+        return x.stride(0) if tokens > 1 else heads * dim
+
+    def kv_append(self, kv: KVPages, layer: int, tables, q_off, q, k, v, q_out, q_norm=None,
+                  k_norm=None, eps: float = 1e-6, cos=None, sin=None, interleaved: bool = False) -> None:
+        """New tokens' queries and keys normed per head and rotated, keys and
+        values written to layer's pages (see dm_kv_append).  q, q_out: [tokens,
+        q_heads, head_dim]; k, v: [tokens, kv_heads, head_dim]; cos, sin: float32
+        [positions, rot_dim / 2]."""
+        t = self.torch
+        self._kv(kv)
+        T, D = q.shape[0], kv.head_dim
+        b = self._batch(tables, q_off, T)
+        strides = [self._rows(x, n, h, D, T, kv.dtype)
+                   for x, n, h in ((q, "q", q.shape[1]), (k, "k", kv.kv_heads), (v, "v", kv.kv_heads),
+                                   (q_out, "q_out", q.shape[1]))]
+        for w, n in ((q_norm, "q_norm"), (k_norm, "k_norm")):
+            if w is not None and self._dev(w, kv.dtype, n).numel() != D:
+                raise ValueError(f"{n} needs head_dim weights")
+        rot = 0
+        if cos is not None or sin is not None:
+            cos, sin = self._dev(cos, t.float32, "cos"), self._dev(sin, t.float32, "sin")
+            if cos.dim() != 2 or cos.shape != sin.shape:
+                raise ValueError("cos and sin must be [positions, rot_dim / 2]")
+            rot = 2 * cos.shape[1]
+        a = dm_append_args(q.data_ptr(), k.data_ptr(), v.data_ptr(), strides[0], strides[1], strides[2],
+                           q_out.data_ptr(), strides[3], _ptr(q_norm), _ptr(k_norm),
+                           _ptr(cos) if rot else None, _ptr(sin) if rot else None,
+                           cos.shape[0] if rot else 0, q.shape[1], rot, 1 if interleaved else 0, eps)
+        self._check(self.lib.dm_kv_append(self._h, kv._ref, layer, C.byref(b), C.byref(a)),
+                    "dm_kv_append")
+
+    def attn_plan(self, kv: KVPages, tables, q_off, q_tokens: int, q_heads: int, groups=None) -> AttnPlan:
+        """The work of attn for a batch (see dm_attn_plan), once for all layers.
+        groups: int64 [runs + 1], the runs of sequences that may share a prefix."""
+        self._kv(kv)
+        b = self._batch(tables, q_off, q_tokens, groups)
+        need = self.lib.dm_attn_plan_bytes(b.tables.n, b.groups)
+        buf = self._empty(need, self.torch.uint8)
+        self._check(self.lib.dm_attn_plan(self._h, C.byref(b), kv._ref, q_heads, buf.data_ptr(), need),
+                    "dm_attn_plan")
+        return AttnPlan(b, kv, q_heads, buf, (tables, q_off, groups))
+
+    def attn(self, plan: AttnPlan, layer: int, q, scale: float, out, lse=None) -> None:
+        """Attention of a batch's new tokens over layer's pages (see dm_attn): q
+        and out [tokens, q_heads, head_dim], lse float32 [tokens, q_heads]."""
+        kv, b = plan.kv, plan.batch
+        T, D = b.q_tokens, kv.head_dim
+        qs = self._rows(q, "q", plan.q_heads, D, T, kv.dtype)
+        os_ = self._rows(out, "out", plan.q_heads, D, T, kv.dtype)
+        if lse is not None and tuple(self._dev(lse, self.torch.float32, "lse").shape) != (T, plan.q_heads):
+            raise ValueError("lse must be [tokens, q_heads]")
+        self._check(self.lib.dm_attn(self._h, C.byref(b), kv._ref, plan.q_heads, plan.buf.data_ptr(),
+                                     layer, q.data_ptr(), qs, scale, out.data_ptr(), os_, _ptr(lse)),
+                    "dm_attn")

@@ -789,6 +789,241 @@ dm_status dm_set_pipelining(dm_ctx* c, int on)
     return DM_OK;
 }
 
+// KV pages and attention over them: host checks (dm_pages.hip, dm_append.hip,
+// dm_attn.hip).
+static bool aligned16(const void* p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0; }
+
+static dm_status tables_check(dm_ctx* c, const dm_page_tables* t, bool len, const std::string& what)
+{
+    if (!t || (t->n && (!t->off || (len && !t->len))) || (t->entries && !t->page))
+        return fail(c, DM_EINVAL, what + ": null table");
+    if (!aligned(t->off) || !aligned(t->page) || (len && !aligned(t->len)))
+        return fail(c, DM_EINVAL, what + ": misaligned table");
+    if (t->n >= (1ull << 31) || t->entries >= (1ull << 40))
+        return fail(c, DM_EINVAL, what + ": too many sequences or entries");
+    return DM_OK;
+}
+
+static dm_status kv_pages_check(dm_ctx* c, const dm_kv_pages* kv, uint32_t layer, bool data,
+                                const std::string& what)
+{
+    if (!kv || (data && (!kv->k || !kv->v)))
+        return fail(c, DM_EINVAL, what + ": null pages");
+    if (kv->reserved || (kv->dtype != DM_BF16 && kv->dtype != DM_F16) ||
+        (kv->head_dim != 64 && kv->head_dim != 128 && kv->head_dim != 256) || kv->kv_heads < 1 ||
+        kv->kv_heads > 4096 || kv->n_pages >= (1u << 31))
+        return fail(c, DM_EINVAL, what + ": unsupported pages (bf16 or f16, head_dim 64, 128 or 256, "
+                                         "1 to 4096 KV heads, n_pages < 2^31)");
+    if (!data)
+        return DM_OK;
+    const uint64_t size = (uint64_t)kv->n_pages * kv->kv_heads * c->cfg.block_size * kv->head_dim;
+    if (kv->layers < 1 || kv->layers > 65536 || kv->layer_stride < 0 || kv->layer_stride % 8 ||
+        (uint64_t)kv->layer_stride < size || (uint64_t)kv->layer_stride >= (1ull << 46))
+        return fail(c, DM_EINVAL, what + ": layers or layer_stride");
+    if (!aligned16(kv->k) || !aligned16(kv->v))
+        return fail(c, DM_EINVAL, what + ": pages must be 16-byte aligned");
+    if (layer >= kv->layers)
+        return fail(c, DM_EINVAL, what + ": layer out of range");
+    return DM_OK;
+}
+
+static dm_status token_batch_check(dm_ctx* c, const dm_token_batch* b, const std::string& what)
+{
+    if (!b)
+        return fail(c, DM_EINVAL, what + ": null batch");
+    if (dm_status s = tables_check(c, &b->tables, true, what); s != DM_OK)
+        return s;
+    if ((b->tables.n && !b->q_off) || (b->groups != 0) != (b->group_off != nullptr))
+        return fail(c, DM_EINVAL, what + ": null q_off, or group_off without groups or the reverse");
+    if (!aligned(b->q_off) || !aligned(b->group_off))
+        return fail(c, DM_EINVAL, what + ": misaligned q_off or group_off");
+    if (b->q_tokens >= (1ull << 31) || b->groups > b->tables.n)
+        return fail(c, DM_EINVAL, what + ": q_tokens >= 2^31 or more groups than sequences");
+    return DM_OK;
+}
+
+// rows of heads * dim elements, `stride` apart
+static bool rows_ok(const void* p, int64_t stride, uint64_t heads, uint32_t dim)
+{
+    return p && aligned16(p) && stride % 8 == 0 && stride >= 0 && (uint64_t)stride >= heads * dim &&
+           stride < (1ll << 31);
+}
+
+static dm_status pages_out_check(dm_ctx* c, const dm_pages_out* o, const std::string& what)
+{
+    if (!o || !o->ref || !o->moves || (o->cap && !o->page) ||
+        (o->move_cap && (!o->move_src || !o->move_dst)))
+        return fail(c, DM_EINVAL, what + ": null output");
+    if (!aligned(o->off) || !aligned(o->page) || !aligned(o->len) || !aligned(o->ref) ||
+        !aligned(o->move_src) || !aligned(o->move_dst) || !aligned(o->moves) || !aligned(o->live))
+        return fail(c, DM_EINVAL, what + ": misaligned output");
+    return DM_OK;
+}
+
+dm_status dm_pages_fork(dm_ctx* c, const dm_page_tables* in, const int32_t* ref, uint32_t n_pages,
+                        const int32_t* src, const int64_t* keep, const int64_t* grow, uint64_t m,
+                        const dm_pages_out* out)
+{
+    if (!c)
+        return DM_EINVAL;
+    if (dm_status s = tables_check(c, in, true, "dm_pages_fork"); s != DM_OK)
+        return s;
+    if (dm_status s = pages_out_check(c, out, "dm_pages_fork"); s != DM_OK)
+        return s;
+    if (!ref || !out->off || (m && (!src || !keep || !grow || !out->len)))
+        return fail(c, DM_EINVAL, "dm_pages_fork: null argument");
+    if (!aligned(ref) || !aligned(src) || !aligned(keep) || !aligned(grow))
+        return fail(c, DM_EINVAL, "dm_pages_fork: misaligned pointer");
+    if (m >= (1ull << 31) || n_pages < 1 || n_pages >= (1u << 31))
+        return fail(c, DM_EINVAL, "dm_pages_fork: m or n_pages out of range");
+    DeviceGuard g(c->device);
+    hipError_t e = join_selection(c);
+    if (e == hipSuccess)
+        e = pages_fork(c, *in, ref, n_pages, src, keep, grow, m, *out);
+    return e == hipSuccess ? DM_OK : hip_fail(c, e, "dm_pages_fork");
+}
+
+dm_status dm_pages_compact(dm_ctx* c, const dm_page_tables* in, const int32_t* ref,
+                           uint32_t n_pages, const dm_pages_out* out)
+{
+    if (!c)
+        return DM_EINVAL;
+    if (dm_status s = tables_check(c, in, false, "dm_pages_compact"); s != DM_OK)
+        return s;
+    if (dm_status s = pages_out_check(c, out, "dm_pages_compact"); s != DM_OK)
+        return s;
+    if (!ref || !out->live || (in->entries && !out->page))
+        return fail(c, DM_EINVAL, "dm_pages_compact: null argument");
+    if (!aligned(ref))
+        return fail(c, DM_EINVAL, "dm_pages_compact: misaligned pointer");
+    if (n_pages < 1 || n_pages >= (1u << 31))
+        return fail(c, DM_EINVAL, "dm_pages_compact: n_pages out of range");
+    DeviceGuard g(c->device);
+    hipError_t e = join_selection(c);
+    if (e == hipSuccess)
+        e = pages_compact(c, *in, ref, n_pages, *out);
+    return e == hipSuccess ? DM_OK : hip_fail(c, e, "dm_pages_compact");
+}
+
+dm_status dm_pages_copy(dm_ctx* c, const dm_kv_pages* kv, const int32_t* src, const int32_t* dst,
+                        const int64_t* count, uint64_t cap)
+{
+    if (!c)
+        return DM_EINVAL;
+    if (dm_status s = kv_pages_check(c, kv, 0, true, "dm_pages_copy"); s != DM_OK)
+        return s;
+    if (!count || (cap && (!src || !dst)))
+        return fail(c, DM_EINVAL, "dm_pages_copy: null argument");
+    if (!aligned(src) || !aligned(dst) || !aligned(count))
+        return fail(c, DM_EINVAL, "dm_pages_copy: misaligned pointer");
+    if (cap >= (1ull << 31))
+        return fail(c, DM_EINVAL, "dm_pages_copy: too many pairs");
+    DeviceGuard g(c->device);
+    hipError_t e = join_selection(c);
+    if (e == hipSuccess)
+        e = pages_copy(c, *kv, src, dst, count, cap);
+    return e == hipSuccess ? DM_OK : hip_fail(c, e, "dm_pages_copy");
+}
+
+dm_status dm_kv_append(dm_ctx* c, const dm_kv_pages* kv, uint32_t layer,
+                       const dm_token_batch* batch, const dm_append_args* a)
+{
+    if (!c)
+        return DM_EINVAL;
+    if (dm_status s = kv_pages_check(c, kv, layer, true, "dm_kv_append"); s != DM_OK)
+        return s;
+    if (dm_status s = token_batch_check(c, batch, "dm_kv_append"); s != DM_OK)
+        return s;
+    if (!a)
+        return fail(c, DM_EINVAL, "dm_kv_append: null arguments");
+    if (a->q_heads < 1 || a->q_heads > 65536)
+        return fail(c, DM_EINVAL, "dm_kv_append: q_heads out of range");
+    if (a->rot_dim % 16 || a->rot_dim > kv->head_dim || (a->rot_dim && (!a->cos || !a->sin)) ||
+        a->max_pos > (1ull << 40))
+        return fail(c, DM_EINVAL, "dm_kv_append: rot_dim must be a multiple of 16, at most head_dim, "
+                                  "and have its tables");
+    if (!aligned16(a->q_norm) || !aligned16(a->k_norm) || !aligned16(a->cos) || !aligned16(a->sin))
+        return fail(c, DM_EINVAL, "dm_kv_append: weights and tables must be 16-byte aligned");
+    if (!(a->eps >= 0))
+        return fail(c, DM_EINVAL, "dm_kv_append: eps must not be negative");
+    if (batch->tables.n == 0 || batch->q_tokens == 0)
+        return DM_OK;
+    if (!rows_ok(a->q, a->q_stride, a->q_heads, kv->head_dim) ||
+        !rows_ok(a->k, a->k_stride, kv->kv_heads, kv->head_dim) ||
+        !rows_ok(a->v, a->v_stride, kv->kv_heads, kv->head_dim) ||
+        !rows_ok(a->q_out, a->q_out_stride, a->q_heads, kv->head_dim))
+        return fail(c, DM_EINVAL, "dm_kv_append: rows must be 16-byte aligned, their strides multiples "
+                                  "of 8 and at least heads * head_dim");
+    DeviceGuard g(c->device);
+    hipError_t e = join_selection(c);
+    if (e == hipSuccess)
+        e = kv_append(c, *kv, layer, *batch, *a);
+    return e == hipSuccess ? DM_OK : hip_fail(c, e, "dm_kv_append");
+}
+
+static dm_status heads_check(dm_ctx* c, const dm_kv_pages* kv, uint32_t q_heads, const std::string& what)
+{
+    if (q_heads < 1 || q_heads > 65536 || q_heads % kv->kv_heads)
+        return fail(c, DM_EINVAL, what + ": q_heads must be a multiple of kv_heads");
+    return DM_OK;
+}
+
+uint64_t dm_attn_plan_bytes(uint64_t n, uint64_t groups)
+{
+    return n < (1ull << 31) && groups <= n ? attn_plan_bytes(n, groups) : 0;
+}
+
+dm_status dm_attn_plan(dm_ctx* c, const dm_token_batch* batch, const dm_kv_pages* kv,
+                       uint32_t q_heads, void* plan, uint64_t plan_bytes)
+{
+    if (!c)
+        return DM_EINVAL;
+    if (dm_status s = kv_pages_check(c, kv, 0, false, "dm_attn_plan"); s != DM_OK)
+        return s;
+    if (dm_status s = token_batch_check(c, batch, "dm_attn_plan"); s != DM_OK)
+        return s;
+    if (dm_status s = heads_check(c, kv, q_heads, "dm_attn_plan"); s != DM_OK)
+        return s;
+    if (!plan || !aligned16(plan) || plan_bytes < attn_plan_bytes(batch->tables.n, batch->groups))
+        return fail(c, DM_EINVAL, "dm_attn_plan: plan is null, misaligned or smaller than "
+                                  "dm_attn_plan_bytes");
+    DeviceGuard g(c->device);
+    hipError_t e = join_selection(c);
+    if (e == hipSuccess)
+        e = attn_plan(c, *batch, *kv, q_heads, plan);
+    return e == hipSuccess ? DM_OK : hip_fail(c, e, "dm_attn_plan");
+}
+
+dm_status dm_attn(dm_ctx* c, const dm_token_batch* batch, const dm_kv_pages* kv, uint32_t q_heads,
+                  const void* plan, uint32_t layer, const void* q, int64_t q_stride, float scale,
+                  void* out, int64_t out_stride, float* lse)
+{
+    if (!c)
+        return DM_EINVAL;
+    if (dm_status s = kv_pages_check(c, kv, layer, true, "dm_attn"); s != DM_OK)
+        return s;
+    if (dm_status s = token_batch_check(c, batch, "dm_attn"); s != DM_OK)
+        return s;
+    if (dm_status s = heads_check(c, kv, q_heads, "dm_attn"); s != DM_OK)
+        return s;
+    if (!plan || !aligned16(plan) || !aligned(lse))
+        return fail(c, DM_EINVAL, "dm_attn: null plan or misaligned pointer");
+    if (!(scale > 0) || scale > 1e30f)
+        return fail(c, DM_EINVAL, "dm_attn: scale must be positive and finite");
+    if (batch->tables.n == 0 || batch->q_tokens == 0)
+        return DM_OK;
+    if (!rows_ok(q, q_stride, q_heads, kv->head_dim) || !rows_ok(out, out_stride, q_heads, kv->head_dim))
+        return fail(c, DM_EINVAL, "dm_attn: rows must be 16-byte aligned, their strides multiples of 8 "
+                                  "and at least heads * head_dim");
+    if (batch->q_tokens * q_heads >= (1ull << 31))
+        return fail(c, DM_EINVAL, "dm_attn: q_tokens * q_heads must be below 2^31");
+    DeviceGuard g(c->device);
+    hipError_t e = join_selection(c);
+    if (e == hipSuccess)
+        e = attn(c, *batch, *kv, q_heads, plan, layer, q, q_stride, scale, out, out_stride, lse);
+    return e == hipSuccess ? DM_OK : hip_fail(c, e, "dm_attn");
+}
+
 dm_status dm_sync(dm_ctx* c)
 {
     if (!c)
@@ -808,8 +1043,8 @@ dm_status dm_sync(dm_ctx* c)
         if (e != hipSuccess)
             return hip_fail(c, e, "dm_sync");
         if (st & kErrInval)
-            return fail(c, DM_EINVAL, "device: malformed input (offsets or queue records)");
-        return fail(c, DM_EFULL, "device: index table full or migration list over capacity");
+            return fail(c, DM_EINVAL, "device: malformed input (offsets, queue records or page tables)");
+        return fail(c, DM_EFULL, "device: index table full, migration list over capacity, or too few pages or room for tables");
     }
     return DM_OK;
 }

@@ -13,13 +13,14 @@
 namespace dm {
 
 constexpr int kWave = 64;
-constexpr int kScratchSlots = 10;  // context work buffers, one per use
+constexpr int kScratchSlots = 11;  // context work buffers, one per use
 // Scratch slots.  Routing uses starts, probe, select, keys, sort, scan and
 // members;
 // a rebalancing pass reuses probe, rebalance and select (it runs after the
 // batches before it have finished).
 constexpr int kSlotStarts = 0, kSlotProbe = 1, kSlotRebalance = 2, kSlotSelect = 3, kSlotKeys = 4,
-              kSlotRing = 5, kSlotSort = 6, kSlotScan = 7, kSlotPurge = 8, kSlotMembers = 9;
+              kSlotRing = 5, kSlotSort = 6, kSlotScan = 7, kSlotPurge = 8, kSlotMembers = 9,
+              kSlotPages = 10;  // page tables' counts; attention's parts
 constexpr uint32_t kMaxSlots = 4096;
 constexpr uint64_t kEmpty = 0;      // index slot never used
 constexpr uint64_t kTomb = 1;       // index slot erased
@@ -435,6 +436,24 @@ hipError_t route(dm_ctx* c, const int32_t* tokens, uint64_t n_tokens, const int6
 hipError_t queue_ends(dm_ctx* c, const int64_t* qoff, int64_t* first, int64_t* last);
 hipError_t rebalance(dm_ctx* c, const dm_queues* q, int64_t* loads_out, const dm_migrations* out,
                      uint64_t cap, uint64_t Q);
+
+// dm_pages.hip, dm_append.hip, dm_attn.hip: KV pages and attention over them,
+// asynchronous on c->stream; arguments checked by the entry points (dm_api.hip).
+hipError_t pages_fork(dm_ctx* c, const dm_page_tables& in, const int32_t* ref, uint32_t n_pages,
+                      const int32_t* src, const int64_t* keep, const int64_t* grow, uint64_t m,
+                      const dm_pages_out& out);
+hipError_t pages_compact(dm_ctx* c, const dm_page_tables& in, const int32_t* ref,
+                         uint32_t n_pages, const dm_pages_out& out);
+hipError_t pages_copy(dm_ctx* c, const dm_kv_pages& kv, const int32_t* src, const int32_t* dst,
+                      const int64_t* count, uint64_t cap);
+hipError_t kv_append(dm_ctx* c, const dm_kv_pages& kv, uint32_t layer, const dm_token_batch& b,
+                     const dm_append_args& a);
+uint64_t attn_plan_bytes(uint64_t n, uint64_t groups);
+hipError_t attn_plan(dm_ctx* c, const dm_token_batch& b, const dm_kv_pages& kv, uint32_t q_heads,
+                     void* plan);
+hipError_t attn(dm_ctx* c, const dm_token_batch& b, const dm_kv_pages& kv, uint32_t q_heads,
+                const void* plan, uint32_t layer, const void* q, int64_t q_stride, float scale,
+                void* out, int64_t out_stride, float* lse);
 
 }  // namespace dm
 
