@@ -14,6 +14,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+import struct
 from typing import Dict, Optional, Sequence
 
 _PKG = os.path.dirname(os.path.abspath(__file__))
@@ -184,6 +185,14 @@ def _ptr(t) -> Optional[int]:
     return None if t is None else t.data_ptr()
 
 
+# dm_page_tables, dm_token_batch, dm_pages_out and dm_append_args as bytes: a decode step makes these calls for every
+# layer, and packing takes a fraction of the time of filling a ctypes structure
+_PACK_TABLES = struct.Struct("=5Q").pack
+_PACK_BATCH = struct.Struct("=9Q").pack
+_PACK_OUT = struct.Struct("=10Q").pack
+_PACK_APPEND = struct.Struct("=3Q3qQq5Q3If").pack
+
+
 class KVPages:
     """A store of KV pages (see dm_kv_pages): keys and values, torch tensors
     [layers, pages, kv_heads, block, head_dim] of one shape, bfloat16 or
@@ -200,7 +209,7 @@ class KVPages:
             raise ValueError("k and v need a layer and a page, the same strides and contiguous layers")
         self.k, self.v = k, v
         self.layers, self.pages, self.kv_heads, self.block, self.head_dim = k.shape
-        self.dtype, self.device = k.dtype, k.device
+        self.dtype, self.index = k.dtype, k.get_device()
         stride = k.stride(0) if self.layers > 1 else k[0].numel()
         self.struct = dm_kv_pages(k.data_ptr(), v.data_ptr(), stride, self.layers, self.pages,
                                   self.kv_heads, self.head_dim, types[k.dtype], 0)
@@ -210,8 +219,8 @@ class KVPages:
 class AttnPlan:
     """A plan of DualMap.attn_plan: the batch that it was made for."""
 
-    def __init__(self, batch, kv, q_heads, buf, keep):
-        self.batch, self.kv, self.q_heads, self.buf = batch, kv, q_heads, buf
+    def __init__(self, batch, q_tokens, kv, q_heads, buf, keep):
+        self.batch, self.q_tokens, self.kv, self.q_heads, self.buf = batch, q_tokens, kv, q_heads, buf
         self._keep = keep  # the batch's tensors
 
 
@@ -224,6 +233,7 @@ class DualMap:
         self.lib = load_library()
         self.device = torch.device("cuda", torch.cuda.current_device() if device is None
                                    else torch.device(device).index or 0)
+        self._index = self.device.index
         self.cfg = dict(cfg)
         self.max_slots = cfg["max_slots"]
         self.block = cfg["block"]
@@ -253,9 +263,11 @@ class DualMap:
             raise DMError(st, f"{what}: {self.lib.dm_last_error(self._h).decode()}")
 
     def _dev(self, t, dtype, name):
-        torch = self.torch
-        if not isinstance(t, torch.Tensor) or t.device != self.device or t.dtype != dtype \
-                or not t.is_contiguous():
+        try:
+            ok = t.dtype is dtype and t.get_device() == self._index and t.is_contiguous()
+        except AttributeError:  # no tensor
+            ok = False
+        if not ok:
             raise ValueError(f"{name} must be a contiguous {dtype} tensor on {self.device}")
         return t
 
@@ -531,35 +543,42 @@ class DualMap:
     # -- KV pages and attention over them: tables are tuples (off, page, len)
     # of device tensors (int64 [n + 1], int32, int64 [n])
     def _tables(self, tables):
+        """dm_page_tables' fields."""
         t = self.torch
         off, page, length = tables
-        off = self._dev(off, t.int64, "off")
-        page = self._dev(page, t.int32, "page")
-        length = self._dev(length, t.int64, "len")
-        if off.numel() != length.numel() + 1:
+        self._dev(off, t.int64, "off")
+        self._dev(page, t.int32, "page")
+        self._dev(length, t.int64, "len")
+        n = length.numel()
+        if off.numel() != n + 1:
             raise ValueError("off needs one entry more than len")
-        return dm_page_tables(off.data_ptr(), page.data_ptr(), length.data_ptr(), length.numel(),
-                              page.numel())
+        return off.data_ptr(), page.data_ptr(), length.data_ptr(), n, page.numel()
 
     def _kv(self, kv):
-        if kv.device != self.device or kv.block != self.block:
+        if kv.index != self._index or kv.block != self.block:
             raise ValueError("pages must be on %s and hold %d tokens" % (self.device, self.block))
         return kv
 
     def _pages_out(self, out, n_pages, m=None):
-        t = self.torch
-        o = {k: self._dev(out[k], t.int32, k) for k in ("page", "ref", "move_src", "move_dst")}
-        o.update({k: self._dev(out[k], t.int64, k)
-                  for k in (("moves", "off", "len") if m is not None else ("moves", "live"))})
-        if o["ref"].numel() != n_pages or o["moves"].numel() != 1 \
-                or o["move_src"].numel() != o["move_dst"].numel() \
-                or (m is not None and (o["off"].numel() != m + 1 or o["len"].numel() != m)) \
-                or (m is None and o["live"].numel() != 1):
+        dev, i32, i64 = self._dev, self.torch.int32, self.torch.int64
+        page, ref = dev(out["page"], i32, "page"), dev(out["ref"], i32, "ref")
+        src, dst = dev(out["move_src"], i32, "move_src"), dev(out["move_dst"], i32, "move_dst")
+        moves = dev(out["moves"], i64, "moves")
+        off = length = live = 0
+        cap, room = page.numel(), src.numel()
+        ok = ref.numel() == n_pages and moves.numel() == 1 and dst.numel() == room
+        if m is not None:
+            off, length = dev(out["off"], i64, "off"), dev(out["len"], i64, "len")
+            ok = ok and off.numel() == m + 1 and length.numel() == m
+            off, length = off.data_ptr(), length.data_ptr()
+        else:
+            live = dev(out["live"], i64, "live")
+            ok = ok and live.numel() == 1
+            live = live.data_ptr()
+        if not ok:
             raise ValueError("an output has the wrong size")
-        return dm_pages_out(_ptr(o.get("off")), o["page"].data_ptr(), _ptr(o.get("len")),
-                            o["page"].numel(), o["ref"].data_ptr(), o["move_src"].data_ptr(),
-                            o["move_dst"].data_ptr(), o["move_src"].numel(), o["moves"].data_ptr(),
-                            _ptr(o.get("live")))
+        return _PACK_OUT(off, page.data_ptr(), length, cap, ref.data_ptr(), src.data_ptr(),
+                         dst.data_ptr(), room, moves.data_ptr(), live), cap
 
     def alloc_pages_out(self, n_pages: int, m: int, cap: int) -> Dict:
         """Outputs of pages_fork_into for m sequences and cap entries (and, with cap the
@@ -585,10 +604,10 @@ class DualMap:
         m = src.numel()
         if keep.numel() != m or grow.numel() != m:
             raise ValueError("src, keep and grow must have one length")
-        o = self._pages_out(out, ref.numel(), m)
-        self._check(self.lib.dm_pages_fork(self._h, C.byref(tb), ref.data_ptr(), ref.numel(),
-                                           src.data_ptr(), keep.data_ptr(), grow.data_ptr(), m,
-                                           C.byref(o)), "dm_pages_fork")
+        o, _ = self._pages_out(out, ref.numel(), m)
+        self._check(self.lib.dm_pages_fork(self._h, _PACK_TABLES(*tb), ref.data_ptr(), ref.numel(),
+                                           src.data_ptr(), keep.data_ptr(), grow.data_ptr(), m, o),
+                    "dm_pages_fork")
 
     def pages_fork(self, tables, ref, src, keep, grow, cap: int) -> Dict:
         """pages_fork_into with outputs of its own (cap entries); page is cut
@@ -604,11 +623,11 @@ class DualMap:
         out["live"] and the list of moves for pages_copy."""
         tb = self._tables(tables)
         ref = self._dev(ref, self.torch.int32, "ref")
-        o = self._pages_out(out, ref.numel())
-        if o.cap < tb.entries:
+        o, cap = self._pages_out(out, ref.numel())
+        if cap < tb[4]:
             raise ValueError("page needs room for the tables' entries")
-        self._check(self.lib.dm_pages_compact(self._h, C.byref(tb), ref.data_ptr(), ref.numel(),
-                                              C.byref(o)), "dm_pages_compact")
+        self._check(self.lib.dm_pages_compact(self._h, _PACK_TABLES(*tb), ref.data_ptr(), ref.numel(), o),
+                    "dm_pages_compact")
 
     def pages_copy(self, kv: KVPages, moves: Dict) -> None:
         """Page data moved by a list of pages_fork or pages_compact (see dm_pages_copy)."""
@@ -623,22 +642,24 @@ class DualMap:
                                            count.data_ptr(), src.numel()), "dm_pages_copy")
 
     def _batch(self, tables, q_off, q_tokens, groups=None):
-        t = self.torch
+        """dm_token_batch's fields."""
+        i64 = self.torch.int64
         tb = self._tables(tables)
-        q_off = self._dev(q_off, t.int64, "q_off")
-        if q_off.numel() != tb.n + 1:
+        if self._dev(q_off, i64, "q_off").numel() != tb[3] + 1:
             raise ValueError("q_off needs one entry more than len")
-        g = None if groups is None else self._dev(groups, t.int64, "groups")
-        return dm_token_batch(tb, q_off.data_ptr(), q_tokens, _ptr(g),
-                              0 if g is None else g.numel() - 1)
+        if groups is None:
+            return tb + (q_off.data_ptr(), q_tokens, 0, 0)
+        self._dev(groups, i64, "groups")
+        return tb + (q_off.data_ptr(), q_tokens, groups.data_ptr(), groups.numel() - 1)
 
     def _rows(self, x, name, heads, dim, tokens, dtype):
-        """Row stride of [tokens, heads, dim] with contiguous heads."""
-        if x.device != self.device or x.dtype != dtype or tuple(x.shape) != (tokens, heads, dim):
+        """Address and row stride of [tokens, heads, dim] with contiguous heads."""
+        if x.dtype is not dtype or x.shape != (tokens, heads, dim) or x.get_device() != self._index:
             raise ValueError(f"{name} must be a {dtype} tensor {(tokens, heads, dim)} on {self.device}")
-        if x.numel() and (x.stride(2) != 1 or (heads > 1 and x.stride(1) != dim)):
+        a, b, c = x.stride()
+        if tokens and (c != 1 or (heads > 1 and b != dim)):
             raise ValueError(f"{name}'s heads must be contiguous")
-        return x.stride(0) if tokens > 1 else heads * dim
+        return x.data_ptr(), a if tokens > 1 else heads * dim
 
     def kv_append(self, kv: KVPages, layer: int, tables, q_off, q, k, v, q_out, q_norm=None,
                   k_norm=None, eps: float = 1e-6, cos=None, sin=None, interleaved: bool = False) -> None:
@@ -646,49 +667,54 @@ class DualMap:
         values written to layer's pages (see dm_kv_append).  q, q_out: [tokens,
         q_heads, head_dim]; k, v: [tokens, kv_heads, head_dim]; cos, sin: float32
         [positions, rot_dim / 2]."""
-        t = self.torch
         self._kv(kv)
-        T, D = q.shape[0], kv.head_dim
+        T, D, dt = q.shape[0], kv.head_dim, kv.dtype
+        heads = q.shape[1]
         b = self._batch(tables, q_off, T)
-        strides = [self._rows(x, n, h, D, T, kv.dtype)
-                   for x, n, h in ((q, "q", q.shape[1]), (k, "k", kv.kv_heads), (v, "v", kv.kv_heads),
-                                   (q_out, "q_out", q.shape[1]))]
-        for w, n in ((q_norm, "q_norm"), (k_norm, "k_norm")):
-            if w is not None and self._dev(w, kv.dtype, n).numel() != D:
-                raise ValueError(f"{n} needs head_dim weights")
-        rot = 0
+        qp, qs = self._rows(q, "q", heads, D, T, dt)
+        kp, ks = self._rows(k, "k", kv.kv_heads, D, T, dt)
+        vp, vs = self._rows(v, "v", kv.kv_heads, D, T, dt)
+        op, os_ = self._rows(q_out, "q_out", heads, D, T, dt)
+        wq = wk = cp = sp = rot = rows = 0
+        if q_norm is not None:
+            wq = self._dev(q_norm, dt, "q_norm").data_ptr()
+        if k_norm is not None:
+            wk = self._dev(k_norm, dt, "k_norm").data_ptr()
+        if (wq and q_norm.numel() != D) or (wk and k_norm.numel() != D):
+            raise ValueError("q_norm and k_norm need head_dim weights")
         if cos is not None or sin is not None:
-            cos, sin = self._dev(cos, t.float32, "cos"), self._dev(sin, t.float32, "sin")
+            f32 = self.torch.float32
+            cp, sp = self._dev(cos, f32, "cos").data_ptr(), self._dev(sin, f32, "sin").data_ptr()
             if cos.dim() != 2 or cos.shape != sin.shape:
                 raise ValueError("cos and sin must be [positions, rot_dim / 2]")
-            rot = 2 * cos.shape[1]
-        a = dm_append_args(q.data_ptr(), k.data_ptr(), v.data_ptr(), strides[0], strides[1], strides[2],
-                           q_out.data_ptr(), strides[3], _ptr(q_norm), _ptr(k_norm),
-                           _ptr(cos) if rot else None, _ptr(sin) if rot else None,
-                           cos.shape[0] if rot else 0, q.shape[1], rot, 1 if interleaved else 0, eps)
-        self._check(self.lib.dm_kv_append(self._h, kv._ref, layer, C.byref(b), C.byref(a)),
-                    "dm_kv_append")
+            rows, rot = cos.shape
+            rot *= 2
+        a = _PACK_APPEND(qp, kp, vp, qs, ks, vs, op, os_, wq, wk, cp, sp, rows, heads, rot,
+                         1 if interleaved else 0, eps)
+        self._check(self.lib.dm_kv_append(self._h, kv._ref, layer, _PACK_BATCH(*b), a), "dm_kv_append")
 
     def attn_plan(self, kv: KVPages, tables, q_off, q_tokens: int, q_heads: int, groups=None) -> AttnPlan:
         """The work of attn for a batch (see dm_attn_plan), once for all layers.
         groups: int64 [runs + 1], the runs of sequences that may share a prefix."""
         self._kv(kv)
         b = self._batch(tables, q_off, q_tokens, groups)
-        need = self.lib.dm_attn_plan_bytes(b.tables.n, b.groups)
-        buf = self._empty(need, self.torch.uint8)
-        self._check(self.lib.dm_attn_plan(self._h, C.byref(b), kv._ref, q_heads, buf.data_ptr(), need),
+        need = self.lib.dm_attn_plan_bytes(b[3], b[8])
+        buf = self.torch.empty(need, dtype=self.torch.uint8, device=self.device)
+        batch = _PACK_BATCH(*b)
+        self._check(self.lib.dm_attn_plan(self._h, batch, kv._ref, q_heads, buf.data_ptr(), need),
                     "dm_attn_plan")
-        return AttnPlan(b, kv, q_heads, buf, (tables, q_off, groups))
+        return AttnPlan(batch, q_tokens, kv, q_heads, buf, (tables, q_off, groups))
 
     def attn(self, plan: AttnPlan, layer: int, q, scale: float, out, lse=None) -> None:
         """Attention of a batch's new tokens over layer's pages (see dm_attn): q
         and out [tokens, q_heads, head_dim], lse float32 [tokens, q_heads]."""
-        kv, b = plan.kv, plan.batch
-        T, D = b.q_tokens, kv.head_dim
-        qs = self._rows(q, "q", plan.q_heads, D, T, kv.dtype)
-        os_ = self._rows(out, "out", plan.q_heads, D, T, kv.dtype)
-        if lse is not None and tuple(self._dev(lse, self.torch.float32, "lse").shape) != (T, plan.q_heads):
-            raise ValueError("lse must be [tokens, q_heads]")
-        self._check(self.lib.dm_attn(self._h, C.byref(b), kv._ref, plan.q_heads, plan.buf.data_ptr(),
-                                     layer, q.data_ptr(), qs, scale, out.data_ptr(), os_, _ptr(lse)),
-                    "dm_attn")
+        kv, T, heads = plan.kv, plan.q_tokens, plan.q_heads
+        qp, qs = self._rows(q, "q", heads, kv.head_dim, T, kv.dtype)
+        op, os_ = self._rows(out, "out", heads, kv.head_dim, T, kv.dtype)
+        lp = None
+        if lse is not None:
+            lp = self._dev(lse, self.torch.float32, "lse").data_ptr()
+            if lse.shape != (T, heads):
+                raise ValueError("lse must be [tokens, q_heads]")
+        self._check(self.lib.dm_attn(self._h, plan.batch, kv._ref, heads, plan.buf.data_ptr(), layer, qp,
+                                     qs, scale, op, os_, lp), "dm_attn")

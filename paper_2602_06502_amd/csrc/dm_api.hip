@@ -264,7 +264,7 @@ dm_status dm_create(const dm_config* cfg, void* hip_stream, dm_ctx** out)
     if (e == hipSuccess)
         e = hipMemsetAsync(c->d_tables, 0, table_slots * sizeof(uint64_t), c->stream);
     if (e == hipSuccess) e = hipMemsetAsync(c->d_counts, 0, 2 * S * sizeof(uint64_t), c->stream);
-    if (e == hipSuccess) e = hipMemsetAsync(c->d_status, 0, sizeof(uint32_t), c->stream);
+    if (e == hipSuccess) e = hipMemsetAsync(c->d_status, 0, 256, c->stream);
     if (e == hipSuccess) e = hipMemsetAsync(c->d_next_live, 0, S * sizeof(uint32_t), c->stream);
     if (e == hipSuccess) e = hipStreamSynchronize(c->stream);
     // the static work area of allocation-free routing on this device; if it

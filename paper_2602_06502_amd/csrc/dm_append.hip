@@ -1,10 +1,15 @@
 // New tokens of a batch: queries and keys normed over each head and rotated
 // by their positions in one pass, keys and values written to their pages.
 //
-// Bound by HBM: every element is read once and written once (16 bytes a lane),
-// everything between stays in registers.  A head is D / 8 neighbouring lanes, so
-// its mean square is a few lane exchanges and the partner of a rotated pair is
-// in the lane itself or D_rot / 16 lanes on.
+// Bound by HBM: every element is read once and written once, everything between
+// stays in registers.  A head is D / 8 neighbouring lanes of eight elements, 16
+// bytes: its mean square is a few register exchanges between neighbouring lanes,
+// and the other half of its rotated pairs is in the lane itself or D_rot / 16
+// lanes on, from where the lane gets it as it was read.  (Two runs of four
+// elements a lane, so that every pair is in one lane, need no exchange, but
+// accesses of 8 bytes: 167 us instead of 117 for 18,700 tokens of 48 heads.)  A
+// token's steps wait for one another (its sequence, page, rotation), so its
+// rows, which do not depend on them, are all read first.
 #include "dm_internal.h"
 #include "dm_pages.h"
 
@@ -28,63 +33,69 @@ struct AppendIn {
     TokenBatch b;
 };
 
-// Eight neighbouring elements of a head, d0 the first one's place: normed
-// (weight w, if any) and rotated.  cs, sn: the lane's cosines and sines.
-template <int D, bool INTERLEAVED>
-__device__ __forceinline__ void norm_rotate(float (&x)[8], const float* w, float eps, uint32_t rot,
-                                            uint32_t d0, const float (&cs)[8], const float (&sn)[8])
+template <int CTRL>
+__device__ __forceinline__ float dpp_add(float x)
 {
-    if (w) {
-        float ss = 0;
-#pragma unroll
-        for (int i = 0; i < 8; i++)
-            ss += x[i] * x[i];
-#pragma unroll
-        for (int o = 1; o < D / 8; o *= 2)
-            ss += __shfl_xor(ss, o);
-        const float r = rsqrtf(ss * (1.0f / D) + eps);
-#pragma unroll
-        for (int i = 0; i < 8; i++)
-            x[i] = x[i] * r * w[i];
-    }
-    if (!rot)
-        return;
-    if (INTERLEAVED) {
-        if (d0 < rot) {
-#pragma unroll
-            for (int i = 0; i < 8; i += 2) {
-                const float a = x[i], b = x[i + 1];
-                x[i] = a * cs[i / 2] - b * sn[i / 2];
-                x[i + 1] = b * cs[i / 2] + a * sn[i / 2];
-            }
-        }
-    } else {
-        const bool low = d0 < rot / 2;
-        const int from = lane_id() + (low ? (int)(rot / 16) : -(int)(rot / 16));
-#pragma unroll
-        for (int i = 0; i < 8; i++) {
-            // every lane takes part; those past the rotated part keep their own
-            const float y = __shfl(x[i], d0 < rot ? from : lane_id());
-            if (d0 < rot)
-                x[i] = x[i] * cs[i] + (low ? -y : y) * sn[i];
-        }
-    }
+    return x + __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), CTRL,
+                                                                     0xF, 0xF, true));
 }
 
-// A workgroup for a token; its waves take 512 / D heads at a time.
-template <typename T, int D, bool INTERLEAVED>
-__global__ __launch_bounds__(kThreads) void append_kernel(AppendIn a, uint32_t* status)
+// Sum over a head's D / 8 lanes, in each of them.
+template <int D>
+__device__ __forceinline__ float head_sum(float x)
 {
-    constexpr int kLanes = D / 8, kHeads = kWave / kLanes;
-    const uint32_t li = threadIdx.x % kLanes, hi = threadIdx.x / kLanes;  // lane of a head, head
-    const uint32_t d0 = li * 8;
-    float wq[8], wk[8];
-    if (a.q_norm)
-        load8<T>(a.q_norm + d0, wq);
-    if (a.k_norm)
-        load8<T>(a.k_norm + d0, wk);
-    const uint32_t heads = a.q_heads + 2 * a.kv_heads;
+    x = dpp_add<0xB1>(x);   // neighbours
+    x = dpp_add<0x4E>(x);   // pairs
+    x = dpp_add<0x141>(x);  // fours, mirrored within eight lanes
+    if (D >= 128)
+        x = dpp_add<0x140>(x);  // eights, mirrored within sixteen
+    if (D >= 256)
+        x += __shfl_xor(x, 16);
+    return x;
+}
+
+// row[i] * r * w[i].
+template <typename T>
+__device__ __forceinline__ void scaled(const typename Vec8<T>::type& row, float r,
+                                       const typename Vec8<T>::type& w, float (&x)[8])
+{
+#pragma unroll
+    for (int i = 0; i < 8; i++)
+        x[i] = (float)row[i] * r * (float)w[i];
+}
+
+// A workgroup for a token; a wave takes 512 / D heads at a time, all queries,
+// keys or values, kAhead times read before the first is worked on.
+constexpr int kAhead = 3;
+
+template <typename T, int D, bool INTERLEAVED>
+__global__ __launch_bounds__(kThreads, 6) void append_kernel(AppendIn a, uint32_t* status)
+{
+    using V = typename Vec8<T>::type;
+    constexpr uint32_t kLanes = D / 8, kHeads = kWave / kLanes, kWaves = kThreads / kWave;
+    const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+    const uint32_t li = threadIdx.x % kLanes, hi = lane_id() / kLanes;  // lane of a head, head
+    const uint32_t d0 = li * 8, half = a.rot / 2;
+    const bool turns = d0 < a.rot, low = d0 < half;
+    // where the other half of the lane's pairs is
+    const int other = (int)lane_id() + (INTERLEAVED || !turns ? 0 : low ? (int)(half / 8) : -(int)(half / 8));
+    const uint32_t e0 = INTERLEAVED || !turns ? d0 : low ? d0 + half : d0 - half;
+    const uint32_t gq = (a.q_heads + kHeads - 1) / kHeads, gk = (a.kv_heads + kHeads - 1) / kHeads;
+    const uint32_t groups = gq + 2 * gk;
     for (uint32_t t = blockIdx.x; t < a.b.q_tokens; t += gridDim.x) {
+        V rows[kAhead];
+        auto fetch = [&](uint32_t g) -> V {
+            const bool is_q = g < gq, is_v = g >= gq + gk;
+            const uint32_t h = (g - (is_q ? 0 : is_v ? gq + gk : gq)) * kHeads + hi;
+            const uint32_t n = is_q ? a.q_heads : a.kv_heads;
+            const uint16_t* from = is_q   ? a.q + t * a.q_stride
+                                   : is_v ? a.v + t * a.v_stride
+                                          : a.k + t * a.k_stride;
+            return *reinterpret_cast<const V*>(from + (uint64_t)(h < n ? h : n - 1) * D + d0);
+        };
+#pragma unroll
+        for (int i = 0; i < kAhead; i++)
+            rows[i] = fetch(wave + i * kWaves);
         const uint32_t s = sequence_of(a.b, t);
         const SeqView sv = sequence_view(a.b, s);
         if (sv.bad && threadIdx.x == 0)
@@ -93,71 +104,91 @@ __global__ __launch_bounds__(kThreads) void append_kernel(AppendIn a, uint32_t* 
             continue;  // a token of no sequence: its row is not written
         const int64_t pos = sv.pos0 + (t - sv.tok0);
         int64_t place = -1;  // the token's row of the pages, for KV head 0
-        bool bad = sv.bad;
-        if (!bad && pos >= 0) {
-            const uint32_t p = (uint32_t)a.b.page[sv.off + (pos >> a.b.shift)];
-            bad = p >= a.n_pages || (a.rot && (uint64_t)pos >= a.max_pos);
-            if (!bad)
-                place = ((int64_t)p * a.kv_heads << a.b.shift) + (pos & ((1 << a.b.shift) - 1));
-        }
-        if (bad && !sv.bad && threadIdx.x == 0)
-            atomicOr(status, kErrInval);
         float cs[8], sn[8];
-        if (place >= 0 && a.rot && d0 < a.rot) {
-            const uint32_t half = a.rot / 2;
-            const uint64_t at = (uint64_t)pos * half +
-                                (INTERLEAVED ? d0 / 2 : d0 < half ? d0 : d0 - half);
 #pragma unroll
-            for (int i = 0; i < (INTERLEAVED ? 4 : 8); i += 4) {
-                const float4 c4 = *reinterpret_cast<const float4*>(a.cos + at + i);
-                const float4 s4 = *reinterpret_cast<const float4*>(a.sin + at + i);
-                cs[i] = c4.x, cs[i + 1] = c4.y, cs[i + 2] = c4.z, cs[i + 3] = c4.w;
-                sn[i] = s4.x, sn[i + 1] = s4.y, sn[i + 2] = s4.z, sn[i + 3] = s4.w;
-            }
-        }
-        // whole waves go through the loop: lanes of a wave exchange values
-        for (uint32_t h0 = hi / kHeads * kHeads; h0 < heads; h0 += kThreads / kLanes) {
-            const uint32_t h = h0 + hi % kHeads;
-            const bool is_q = h < a.q_heads, is_k = !is_q && h < a.q_heads + a.kv_heads;
-            const uint32_t hk = is_q ? h : is_k ? h - a.q_heads : h - a.q_heads - a.kv_heads;
-            float x[8] = {};
-            if (h < heads && place >= 0) {
-                const uint16_t* from = is_q   ? a.q + t * a.q_stride
-                                       : is_k ? a.k + t * a.k_stride
-                                              : a.v + t * a.v_stride;
-                if (!is_q && !is_k) {
-                    *reinterpret_cast<v4u32*>(a.v_pages + (place + ((int64_t)hk << a.b.shift)) * D + d0) =
-                        *reinterpret_cast<const v4u32*>(from + (uint64_t)hk * D + d0);
-                } else {
-                    load8<T>(from + (uint64_t)hk * D + d0, x);
+        for (int i = 0; i < 8; i++)
+            cs[i] = 1, sn[i] = 0;
+        if (!sv.bad && pos >= 0) {
+            const uint32_t p = (uint32_t)a.b.page[sv.off + (pos >> a.b.shift)];
+            const bool past = a.rot && (uint64_t)pos >= a.max_pos;
+            if (!past && turns) {
+                const uint64_t at = (uint64_t)pos * half + (INTERLEAVED ? d0 / 2 : low ? d0 : d0 - half);
+#pragma unroll
+                for (int i = 0; i < (INTERLEAVED ? 4 : 8); i += 4) {
+                    const float4 c4 = *reinterpret_cast<const float4*>(a.cos + at + i);
+                    const float4 s4 = *reinterpret_cast<const float4*>(a.sin + at + i);
+                    cs[i] = c4.x, cs[i + 1] = c4.y, cs[i + 2] = c4.z, cs[i + 3] = c4.w;
+                    sn[i] = s4.x, sn[i + 1] = s4.y, sn[i + 2] = s4.z, sn[i + 3] = s4.w;
                 }
-            }
-            float w[8];
-#pragma unroll
-            for (int i = 0; i < 8; i++)
-                w[i] = is_q ? (a.q_norm ? wq[i] : 1.0f) : (a.k_norm ? wk[i] : 1.0f);
-            // the branch is uniform: with one norm alone the other heads' mean
-            // square is taken and not used
-            if (a.q_norm || a.k_norm) {
-                float y[8];
-#pragma unroll
-                for (int i = 0; i < 8; i++)
-                    y[i] = x[i];
-                norm_rotate<D, INTERLEAVED>(y, w, a.eps, 0, d0, cs, sn);
-                if (is_q ? a.q_norm != nullptr : a.k_norm != nullptr)
+                if (!INTERLEAVED && low)
 #pragma unroll
                     for (int i = 0; i < 8; i++)
-                        x[i] = y[i];
+                        sn[i] = -sn[i];
             }
-            if (place >= 0)
-                norm_rotate<D, INTERLEAVED>(x, nullptr, 0.0f, a.rot, d0, cs, sn);
-            if (h >= heads)
-                continue;
-            if (is_q)
-                store8<T>(a.q_out + t * a.q_out_stride + (uint64_t)hk * D + d0, x);
-            else if (is_k && place >= 0)
-                store8<T>(a.k_pages + (place + ((int64_t)hk << a.b.shift)) * D + d0, x);
+            if (p < a.n_pages && !past)
+                place = ((int64_t)p * a.kv_heads << a.b.shift) + (pos & ((1 << a.b.shift) - 1));
+            else if (threadIdx.x == 0)
+                atomicOr(status, kErrInval);
         }
+        // whole waves go through this: lanes of a wave exchange values
+        auto work = [&](uint32_t g, const V& row) {
+            const bool is_q = g < gq, is_v = g >= gq + gk;
+            const uint32_t h = (g - (is_q ? 0 : is_v ? gq + gk : gq)) * kHeads + hi;
+            const uint32_t n = is_q ? a.q_heads : a.kv_heads;
+            if (place < 0 && !is_q)
+                return;
+            uint16_t* to = is_q ? a.q_out + t * a.q_out_stride + (uint64_t)h * D + d0
+                                : (is_v ? a.v_pages : a.k_pages) +
+                                      (place + ((int64_t)h << a.b.shift)) * D + d0;
+            if (is_v || place < 0) {
+                const V zero = {};
+                if (h < n)
+                    *reinterpret_cast<V*>(to) = is_v ? row : zero;
+                return;
+            }
+            // the norm's weights of the lane's elements and of their partners
+            const uint16_t* w = is_q ? a.q_norm : a.k_norm;
+            V w0 = {1, 1, 1, 1, 1, 1, 1, 1}, w1 = w0;
+            float r = 1.0f;
+            if (w) {
+                w0 = *reinterpret_cast<const V*>(w + d0);
+                w1 = *reinterpret_cast<const V*>(w + e0);
+                float ss = 0;
+#pragma unroll
+                for (int i = 0; i < 8; i++)
+                    ss += (float)row[i] * (float)row[i];
+                r = rsqrtf(head_sum<D>(ss) * (1.0f / D) + a.eps);
+            }
+            float x[8];
+            scaled<T>(row, r, w0, x);
+            if (INTERLEAVED) {
+#pragma unroll
+                for (int i = 0; i < 8; i += 2) {
+                    const float u = x[i], v = x[i + 1];
+                    x[i] = u * cs[i / 2] - v * sn[i / 2];
+                    x[i + 1] = v * cs[i / 2] + u * sn[i / 2];
+                }
+            } else if (a.rot) {
+                const v4u32 mine = __builtin_bit_cast(v4u32, row);
+                v4u32 far;
+#pragma unroll
+                for (int i = 0; i < 4; i++)
+                    far[i] = __shfl(mine[i], other);
+                float y[8];
+                scaled<T>(__builtin_bit_cast(V, far), r, w1, y);
+#pragma unroll
+                for (int i = 0; i < 8; i++)
+                    x[i] = turns ? x[i] * cs[i] + y[i] * sn[i] : x[i];
+            }
+            if (h < n)
+                store8<T>(to, x);
+        };
+#pragma unroll
+        for (int i = 0; i < kAhead; i++)
+            if (wave + i * kWaves < groups)
+                work(wave + i * kWaves, rows[i]);
+        for (uint32_t g = wave + kAhead * kWaves; g < groups; g += kWaves)
+            work(g, fetch(g));
     }
 }
 

@@ -33,6 +33,7 @@ constexpr int kThreads = 256, kWaves = 4;
 constexpr uint32_t kNarrow = 32, kWide = 128;  // rows of a tile
 constexpr uint32_t kNarrowKeys = 32, kWideKeys = 64;
 constexpr uint32_t kChunk = 128;               // chunks are multiples of this many keys
+constexpr uint32_t kLeastChunk = 128;          // and no shorter than this
 constexpr int kPlanThreads = 1024;
 constexpr uint64_t kPartRows = 1ull << 20;     // rows of parts kept beyond those of cut items
 
@@ -67,7 +68,7 @@ struct PlanView {
     uint32_t* limit;   // [n] pages that s has in common with its run's first, at most
     uint32_t* run;     // [n] its run
     uint32_t* shared;  // [groups] pages shared
-    unsigned long long* gain;  // [groups] tiles of its sequences, each on its own
+    uint32_t* gain;    // [groups] tiles of its sequences, each on its own
 };
 
 __host__ __device__ inline uint64_t up16(uint64_t x) { return (x + 15) & ~15ull; }
@@ -86,7 +87,7 @@ __host__ __device__ inline PlanView plan_view(void* p, uint64_t n, uint64_t grou
     b += up16(4 * n);
     v.shared = reinterpret_cast<uint32_t*>(b);
     b += up16(4 * groups);
-    v.gain = reinterpret_cast<unsigned long long*>(b);
+    v.gain = reinterpret_cast<uint32_t*>(b);
     return v;
 }
 
@@ -109,46 +110,6 @@ __device__ __forceinline__ bool run_ok(const TokenBatch& b, uint32_t g)
     return g0 >= 0 && g1 >= g0 && g1 <= (int64_t)b.n;
 }
 
-// A workgroup for a sequence: how many leading pages it could share with its
-// run's first one.  A shared prefix ends before the first new token of every
-// sequence that has any.
-__global__ __launch_bounds__(kThreads) void attn_common_kernel(TokenBatch b, PlanView pv)
-{
-    __shared__ uint32_t least;
-    for (uint32_t s = blockIdx.x; s < b.n; s += gridDim.x) {
-        const uint32_t g = wave_find(b.group_off, b.groups, 1, (int64_t)s);
-        const SeqView v = sequence_view(b, s);
-        const bool mine = run_ok(b, g) && b.group_off[g] <= (int64_t)s && (int64_t)s < b.group_off[g + 1];
-        uint32_t limit = 0;
-        if (mine && (v.ntok == 0 || (!v.bad && v.len == 0))) {
-            limit = 0xFFFFFFFFu;  // no rows that see a key: no say
-        } else if (mine && !v.bad && v.pos0 > 0) {
-            const SeqView f = sequence_view(b, (uint32_t)b.group_off[g]);
-            int64_t m = v.pos0 >> b.shift;
-            const int64_t have = f.bad ? 0 : b.off[b.group_off[g] + 1] - f.off;
-            if (have < m)
-                m = have;
-            limit = (uint32_t)m;
-            __syncthreads();
-            if (threadIdx.x == 0)
-                least = limit;
-            __syncthreads();
-            uint32_t differ = limit;
-            for (uint32_t i = threadIdx.x; i < limit && i < differ; i += kThreads)
-                if (b.page[v.off + i] != b.page[f.off + i])
-                    differ = i;
-            if (differ < limit)
-                atomicMin(&least, differ);
-            __syncthreads();
-            limit = least;
-        }
-        if (threadIdx.x == 0) {
-            pv.limit[s] = limit;
-            pv.run[s] = mine ? g : 0xFFFFFFFFu;
-        }
-    }
-}
-
 __device__ __forceinline__ uint64_t block_sum64(uint64_t v, uint64_t* lds)
 {
     const uint64_t s = wave_sum_u64(v);
@@ -157,7 +118,7 @@ __device__ __forceinline__ uint64_t block_sum64(uint64_t v, uint64_t* lds)
         lds[threadIdx.x / kWave] = s;
     __syncthreads();
     uint64_t t = 0;
-    for (uint32_t w = 0; w < blockDim.x / kWave; w++)
+    for (uint32_t w = 0; w < kPlanThreads / kWave; w++)
         t += lds[w];
     return t;
 }
@@ -167,134 +128,220 @@ struct PlanIn {
     uint32_t q_heads, kv_heads, ratio;
     uint64_t target;     // items wanted
     uint64_t part_rows;  // rows of parts there is room for
+    uint32_t* arrived;   // workgroups that are done with their sequences; zero between calls
 };
 
-// One workgroup: which runs share their prefixes, the chunk, and the units'
-// items.
+// Words that workgroups on other dies write or read within the launch.
+__device__ __forceinline__ void agent_store(uint32_t* p, uint32_t x)
+{
+    __hip_atomic_store(p, x, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ uint32_t agent_load(const uint32_t* p)
+{
+    return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+
+constexpr uint32_t kNoSay = 0xFFFFFFFFu;
+constexpr uint32_t kLdsRuns = 1024;
+
+// How many leading pages sequence s could share with its run's first one, by
+// the whole workgroup (kNoSay: it has no row that sees a key).  A shared prefix
+// ends before the first new token of every sequence that has any.
+__device__ void common_pages(const PlanIn& a, const PlanView& pv, uint32_t s, uint32_t* least)
+{
+    const TokenBatch& b = a.b;
+    const uint32_t g = wave_find(b.group_off, b.groups, 1, (int64_t)s);
+    const int64_t g0 = b.group_off[g];
+    const bool mine = run_ok(b, g) && g0 <= (int64_t)s && (int64_t)s < b.group_off[g + 1];
+    const SeqView v = sequence_view(b, s);
+    uint32_t limit = 0;
+    if (mine && (v.ntok == 0 || (!v.bad && v.len == 0))) {
+        limit = kNoSay;
+    } else if (mine && !v.bad && v.pos0 > 0) {
+        const SeqView f = sequence_view(b, (uint32_t)g0);
+        int64_t m = v.pos0 >> b.shift;
+        const int64_t have = f.bad ? 0 : b.off[g0 + 1] - f.off;
+        if (have < m)
+            m = have;
+        limit = (uint32_t)m;
+        __syncthreads();
+        if (threadIdx.x == 0)
+            *least = limit;
+        __syncthreads();
+        for (uint32_t i = threadIdx.x; i < limit; i += kPlanThreads)
+            if (b.page[v.off + i] != b.page[f.off + i]) {
+                atomicMin(least, i);
+                break;
+            }
+        __syncthreads();
+        limit = *least;
+    }
+    if (threadIdx.x == 0) {
+        agent_store(&pv.limit[s], limit);
+        agent_store(&pv.run[s], mine ? g : kNoSay);
+    }
+}
+
+// The units of run g over its shared pages, and of sequence s.
+__device__ __forceinline__ Unit run_unit(const PlanIn& a, uint32_t g, uint32_t pages)
+{
+    Unit u{};
+    if (pages == 0)
+        return u;
+    const int64_t s0 = a.b.group_off[g], s1 = a.b.group_off[g + 1];
+    u.tok0 = (uint32_t)a.b.q_off[s0];
+    u.ntok = (uint32_t)a.b.q_off[s1] - u.tok0;
+    u.key1 = pages << a.b.shift;
+    u.off = a.b.off[s0];
+    u.table = pages;
+    u.flags = kUnitParts | (tile_rows((uint64_t)u.ntok * a.ratio) == kWide ? kUnitWide : 0);
+    return u;
+}
+
+__device__ __forceinline__ Unit sequence_unit(const PlanIn& a, const SeqView& v, uint32_t pages)
+{
+    Unit u{};
+    u.tok0 = v.tok0;
+    u.ntok = v.ntok;
+    u.key0 = v.len ? pages << a.b.shift : 0;
+    u.key1 = (uint32_t)v.len;
+    u.off = v.off;
+    u.table = (uint32_t)((v.len + (1ll << a.b.shift) - 1) >> a.b.shift);
+    u.pos0 = (int32_t)v.pos0;
+    u.flags = kUnitCausal | (pages ? kUnitParts : 0) |
+              (tile_rows((uint64_t)u.ntok * a.ratio) == kWide ? kUnitWide : 0);
+    return u;
+}
+
+// Is a pass of its own over `pages` common pages worth it for run g?  Where the
+// run's rows together make clearly fewer tiles, over more than a chunk of keys.
+__device__ __forceinline__ bool worth_sharing(const PlanIn& a, uint32_t g, uint32_t pages, uint64_t gain)
+{
+    if (pages == 0 || pages == kNoSay || !run_ok(a.b, g) || ((uint64_t)pages << a.b.shift) < kChunk)
+        return false;
+    const int64_t t0 = a.b.q_off[a.b.group_off[g]], t1 = a.b.q_off[a.b.group_off[g + 1]];
+    return t0 >= 0 && t1 >= t0 && t1 <= (int64_t)a.b.q_tokens &&
+           2 * gain >= 3 * weight_of((uint64_t)(t1 - t0) * a.ratio);
+}
+
+// Which runs share their prefixes, the chunk, and the units' items.  With
+// runs, a workgroup for a sequence first, and the last one to finish goes on
+// alone (a launch less; 10 us with two launches and every step through memory, at
+// 256 sequences).  A thread keeps its unit in registers from step to step;
+// beyond 1024 units the others are made again for each step.
 __global__ __launch_bounds__(kPlanThreads) void attn_plan_kernel(PlanIn a, PlanView pv, uint32_t* status)
 {
     __shared__ uint64_t lds[2 * kPlanThreads / kWave];
-    __shared__ uint32_t most;
+    __shared__ uint32_t run_pages[kLdsRuns], run_gain[kLdsRuns];
+    __shared__ uint32_t most, least;
     const TokenBatch& b = a.b;
-    const uint32_t units = b.groups + b.n;
-    bool bad = false;
+    const uint32_t units = b.groups + b.n, tid = threadIdx.x;
     if (b.groups) {
-        for (uint32_t g = threadIdx.x; g < b.groups; g += kPlanThreads) {
-            pv.shared[g] = 0xFFFFFFFFu;
-            pv.gain[g] = 0;
+        for (uint32_t s = blockIdx.x; s < b.n; s += gridDim.x)
+            common_pages(a, pv, s, &least);
+        // thread 0 wrote the workgroup's words: its fence alone orders them (one by
+        // every wave of 256 workgroups took 60 us)
+        if (tid == 0) {
+            __builtin_amdgcn_fence(__ATOMIC_RELEASE, "agent");
+            least = atomicAdd(a.arrived, 1u);
+        }
+        __syncthreads();
+        if (least != gridDim.x - 1)
+            return;
+        if (tid == 0)
+            agent_store(a.arrived, 0);
+        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "agent");
+    }
+    uint32_t* pages = b.groups <= kLdsRuns ? run_pages : pv.shared;
+    uint32_t* gain = b.groups <= kLdsRuns ? run_gain : pv.gain;
+    bool bad = false;
+    auto settle = [&] {
+        if (b.groups > kLdsRuns)
+            __threadfence();
+        __syncthreads();
+    };
+    if (b.groups) {
+        for (uint32_t g = tid; g < b.groups; g += kPlanThreads) {
+            pages[g] = kNoSay;
+            gain[g] = 0;
             bad |= !run_ok(b, g) || (g == 0 && b.group_off[0] != 0) ||
                    (g + 1 == b.groups && b.group_off[b.groups] != (int64_t)b.n);
         }
-        __threadfence();
-        __syncthreads();
-        for (uint32_t s = threadIdx.x; s < b.n; s += kPlanThreads) {
-            const uint32_t g = pv.run[s];
+        settle();
+        for (uint32_t s = tid; s < b.n; s += kPlanThreads) {
+            const uint32_t g = agent_load(&pv.run[s]), limit = agent_load(&pv.limit[s]);
+            const SeqView v = sequence_view(b, s);
             if (g >= b.groups)
                 continue;
-            const SeqView v = sequence_view(b, s);
-            atomicMin(&pv.shared[g], pv.limit[s]);
+            atomicMin(&pages[g], limit);
             if (v.len)
-                atomicAdd(&pv.gain[g], (unsigned long long)weight_of((uint64_t)v.ntok * a.ratio));
+                atomicAdd(&gain[g], (uint32_t)weight_of((uint64_t)v.ntok * a.ratio));
         }
-        __threadfence();
-        __syncthreads();
+        settle();
+        for (uint32_t g = tid; g < b.groups; g += kPlanThreads)
+            pages[g] = worth_sharing(a, g, pages[g], gain[g]) ? pages[g] : 0;
+        settle();
     }
     // 0: as wanted; 1: without sharing and without cuts, if the parts of the
     // first try have no room
     for (int attempt = 0; attempt < 2; attempt++) {
-        // units, their cost with it
-        uint64_t cost = 0;
-        for (uint32_t g = threadIdx.x; g < b.groups; g += kPlanThreads) {
-            Unit u{};
-            uint32_t pages = __hip_atomic_load(&pv.shared[g], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-            if (pages == 0xFFFFFFFFu || attempt || !run_ok(b, g))
-                pages = 0;
-            const int64_t s0 = b.group_off[g], s1 = b.group_off[g + 1];
-            if (pages) {
-                const int64_t t0 = b.q_off[s0], t1 = b.q_off[s1];
-                // worth a pass of its own where the run's rows together make
-                // clearly fewer tiles, over more than a chunk of keys
-                const uint64_t gain = __hip_atomic_load(&pv.gain[g], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-                const bool in_order = t0 >= 0 && t1 >= t0 && t1 <= (int64_t)b.q_tokens;
-                if (!in_order || ((uint64_t)pages << b.shift) < kChunk ||
-                    2 * gain < 3 * weight_of((uint64_t)(t1 - t0) * a.ratio)) {
-                    pages = 0;
-                } else {
-                    u.tok0 = (uint32_t)t0;
-                    u.ntok = (uint32_t)(t1 - t0);
-                    u.key1 = pages << b.shift;
-                    u.off = b.off[s0];
-                    u.table = pages;
-                    u.flags = kUnitParts;
-                    if (tile_rows((uint64_t)u.ntok * a.ratio) == kWide)
-                        u.flags |= kUnitWide;
-                    cost += weight_of((uint64_t)u.ntok * a.ratio) * u.key1;
-                }
-            }
-            pv.shared[g] = pages;
-            pv.unit[g] = u;
-        }
-        __threadfence();
-        __syncthreads();
-        for (uint32_t s = threadIdx.x; s < b.n; s += kPlanThreads) {
-            Unit u{};
+        auto make = [&](uint32_t i) -> Unit {
+            if (i < b.groups)
+                return run_unit(a, i, attempt ? 0 : pages[i]);
+            const uint32_t s = i - b.groups, g = b.groups ? agent_load(&pv.run[s]) : kNoSay;
             const SeqView v = sequence_view(b, s);
             bad |= v.bad;
-            const uint32_t g = b.groups ? pv.run[s] : 0xFFFFFFFFu;
-            const uint32_t pages = g < b.groups ? pv.shared[g] : 0;
-            u.tok0 = v.tok0;
-            u.ntok = v.ntok;
-            u.key0 = v.len ? pages << b.shift : 0;
-            u.key1 = (uint32_t)v.len;
-            u.off = v.off;
-            u.table = (uint32_t)((v.len + (1ll << b.shift) - 1) >> b.shift);
-            u.pos0 = (int32_t)v.pos0;
-            u.flags = kUnitCausal | (pages ? kUnitParts : 0);
-            if (tile_rows((uint64_t)u.ntok * a.ratio) == kWide)
-                u.flags |= kUnitWide;
-            if (u.ntok)
-                cost += weight_of((uint64_t)u.ntok * a.ratio) * (u.key1 - u.key0);
-            pv.unit[b.groups + s] = u;
-        }
+            return sequence_unit(a, v, attempt || g >= b.groups ? 0 : pages[g]);
+        };
+        auto cost_of = [&](const Unit& u) -> uint64_t {
+            return u.ntok ? weight_of((uint64_t)u.ntok * a.ratio) * (u.key1 - u.key0) : 0;
+        };
+        Unit mine{};
+        if (tid < units)
+            mine = make(tid);
+        uint64_t cost = cost_of(mine);
+        for (uint32_t i = tid + kPlanThreads; i < units; i += kPlanThreads)
+            cost += cost_of(make(i));
         cost = block_sum64(cost, lds) * a.kv_heads;
         uint64_t chunk = (cost / a.target + kChunk) / kChunk * kChunk;
+        if (chunk < kLeastChunk)
+            chunk = kLeastChunk;
         if (attempt || chunk > 0x80000000ull)
             chunk = 0x80000000ull;
         // items and rows of parts before each unit
-        if (threadIdx.x == 0)
+        if (tid == 0)
             most = 1;
         uint64_t items = 0, rows = 0;
         for (uint32_t u0 = 0; u0 < units; u0 += kPlanThreads) {
-            const uint32_t i = u0 + threadIdx.x;
+            const uint32_t i = u0 + tid;
             uint64_t it = 0, rw = 0;
-            Unit u{};
-            if (i < units) {
-                u = pv.unit[i];
-                if (u.ntok) {
-                    const uint64_t r = (uint64_t)u.ntok * a.ratio;
-                    u.chunks = (uint32_t)((u.key1 - u.key0 + chunk - 1) / chunk);
-                    if (u.chunks == 0)
-                        u.chunks = 1;
-                    if (u.chunks > 1)
-                        u.flags |= kUnitParts;
-                    it = tiles_of(r) * u.chunks * a.kv_heads;
-                    if (u.flags & kUnitParts) {
-                        rw = r * u.chunks * a.kv_heads;
-                        atomicMax(&most, u.chunks);
-                    }
+            Unit u = mine;
+            if (u0 && i < units)
+                u = make(i);
+            __syncthreads();
+            if (i < units && u.ntok) {
+                const uint64_t r = (uint64_t)u.ntok * a.ratio;
+                u.chunks = (uint32_t)((u.key1 - u.key0 + chunk - 1) / chunk);
+                if (u.chunks == 0)
+                    u.chunks = 1;
+                if (u.chunks > 1)
+                    u.flags |= kUnitParts;
+                it = tiles_of(r) * u.chunks * a.kv_heads;
+                if (u.flags & kUnitParts) {
+                    rw = r * u.chunks * a.kv_heads;
+                    atomicMax(&most, u.chunks);
                 }
             }
             const uint64_t i1 = wave_incl_sum_u64(it, 0), r1 = wave_incl_sum_u64(rw, 0);
-            __syncthreads();
             if (lane_id() == kWave - 1) {
-                lds[threadIdx.x / kWave] = i1;
-                lds[kPlanThreads / kWave + threadIdx.x / kWave] = r1;
+                lds[tid / kWave] = i1;
+                lds[kPlanThreads / kWave + tid / kWave] = r1;
             }
             __syncthreads();
             uint64_t ib = items, rb = rows;
             for (uint32_t w = 0; w < kPlanThreads / kWave; w++) {
                 const uint64_t x = lds[w], y = lds[kPlanThreads / kWave + w];
-                if (w < threadIdx.x / kWave) {
+                if (w < tid / kWave) {
                     ib += x;
                     rb += y;
                 }
@@ -305,27 +352,30 @@ __global__ __launch_bounds__(kPlanThreads) void attn_plan_kernel(PlanIn a, PlanV
                 u.item0 = (uint32_t)(ib + i1 - it);
                 u.part0 = (uint32_t)(rb + r1 - rw);
                 pv.unit[i] = u;
+                if (i < b.groups)
+                    pv.shared[i] = u.table;
             }
         }
-        __syncthreads();
-        if (threadIdx.x == 0) {
-            PlanHead h{};
-            h.n = b.n;
-            h.groups = b.groups;
-            h.q_tokens = b.q_tokens;
-            h.q_heads = a.q_heads;
-            h.kv_heads = a.kv_heads;
-            h.shift = b.shift;
-            h.entries = b.entries;
-            h.items = (uint32_t)items;
-            h.units = units;
-            h.chunk = (uint32_t)chunk;
-            h.part_rows = (uint32_t)rows;
-            h.most_parts = most;
-            *pv.head = h;
-        }
-        if (rows <= a.part_rows && items < (1ull << 32))
+        if (rows <= a.part_rows && items < (1ull << 32)) {
+            if (tid == 0) {
+                PlanHead h{};
+                h.n = b.n;
+                h.groups = b.groups;
+                h.q_tokens = b.q_tokens;
+                h.q_heads = a.q_heads;
+                h.kv_heads = a.kv_heads;
+                h.shift = b.shift;
+                h.entries = b.entries;
+                h.items = (uint32_t)items;
+                h.units = units;
+                h.chunk = (uint32_t)chunk;
+                h.part_rows = (uint32_t)rows;
+                h.most_parts = most;
+                *pv.head = h;
+            }
             break;
+        }
+        __syncthreads();
     }
     if (bad)
         atomicOr(status, kErrInval);
@@ -618,7 +668,7 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attn_kernel(AttnIn
     if (item >= items)
         return;
     {
-        const uint32_t ui = wave_find(&pv.unit[0].item0, ph.units, sizeof(Unit) / 4, item);
+        const uint32_t ui = wave_find(&pv.unit[0].item0, a.b.groups + a.b.n, sizeof(Unit) / 4, item);
         const Unit u = pv.unit[ui];
         const uint32_t rows = u.ntok * a.ratio;
         const bool wide = u.flags & kUnitWide;
@@ -925,30 +975,43 @@ __global__ __launch_bounds__(kThreads) void attn_join_kernel(AttnIn a, const Pla
         }
         const uint32_t n = n0 + n1;
         auto place = [&](uint32_t i) { return i < n0 ? at0 + i : at1 + (i - n0); };
+        // the parts' weights, a lane each; then their rows, whose loads need not
+        // wait for one another
         float m = -INFINITY;
-        bool nan = false;
-        for (uint32_t i = lane; i < n; i += kWave) {
-            const float e = a.part_lse[place(i)];
-            nan |= e != e;
-            m = fmaxf(m, e);
-        }
+        for (uint32_t i = lane; i < n; i += kWave)
+            m = fmaxf(m, a.part_lse[place(i)]);
+#pragma unroll
         for (int o = 1; o < kWave; o *= 2)
             m = fmaxf(m, __shfl_xor(m, o));
-        nan = __any(nan);
         float v[kPer] = {}, total = 0;
-        const uint32_t from = together ? wave : 0, by = together ? kWaves : 1;
-        if (m != -INFINITY || nan)
-            for (uint32_t i = from; i < n; i += by) {
-                const uint64_t p = place(i);
-                const float e = a.part_lse[p];
-                if (e == -INFINITY)
-                    continue;  // a part that the row sees nothing of
-                const float w = __builtin_amdgcn_exp2f((e - m) * 1.44269504088896341f);
-                total += w;
+        const uint32_t from = together ? wave * kWave : 0, by = together ? kWaves * kWave : kWave;
+        for (uint32_t i0 = from; i0 < n; i0 += by) {
+            const uint32_t i = i0 + lane;
+            const float e = i < n ? a.part_lse[place(i)] : -INFINITY;
+            // a part that the row sees nothing of has no weight; NaN stays NaN
+            const float w = e == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f((e - m) * 1.44269504088896341f);
+            total += w;
+            const uint32_t k1 = n - i0 < kWave ? n - i0 : kWave;
+            for (uint32_t k = 0; k < k1; k += 4) {
+                float x[4], y[4][kPer];
 #pragma unroll
-                for (int k = 0; k < kPer; k++)
-                    v[k] += w * a.part[p * D + lane * kPer + k];
+                for (int j = 0; j < 4; j++) {
+                    x[j] = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, w), k + j));
+                    const float* at = a.part + place(i0 + (k + j < k1 ? k + j : k1 - 1)) * D + lane * kPer;
+#pragma unroll
+                    for (int c = 0; c < kPer; c++)
+                        y[j][c] = at[c];
+                }
+#pragma unroll
+                for (int j = 0; j < 4; j++)
+#pragma unroll
+                    for (int c = 0; c < kPer; c++)
+                        v[c] = x[j] == 0 ? v[c] : __builtin_fmaf(x[j], y[j][c], v[c]);
             }
+        }
+#pragma unroll
+        for (int o = 1; o < kWave; o *= 2)
+            total += __shfl_xor(total, o);
         if (together) {
             __shared__ float tot[kWaves];
             __syncthreads();
@@ -1023,8 +1086,7 @@ uint64_t part_rows_of(const dm_ctx* c, uint64_t q_tokens, uint32_t q_heads)
 
 uint64_t attn_plan_bytes(uint64_t n, uint64_t groups)
 {
-    return sizeof(PlanHead) + up16(sizeof(Unit) * (n + groups)) + 2 * up16(4 * n) + up16(4 * groups) +
-           up16(8 * groups) + 16;
+    return sizeof(PlanHead) + up16(sizeof(Unit) * (n + groups)) + 2 * up16(4 * n) + 2 * up16(4 * groups);
 }
 
 hipError_t attn_plan(dm_ctx* c, const dm_token_batch& b, const dm_kv_pages& kv, uint32_t q_heads,
@@ -1038,9 +1100,9 @@ hipError_t attn_plan(dm_ctx* c, const dm_token_batch& b, const dm_kv_pages& kv, 
     a.target = item_target(c);
     a.part_rows = part_rows_of(c, b.q_tokens, q_heads);
     const PlanView pv = plan_view(plan, b.tables.n, b.groups);
-    if (b.groups)
-        attn_common_kernel<<<grid_for(b.tables.n, 1), kThreads, 0, c->stream>>>(a.b, pv);
-    attn_plan_kernel<<<1, kPlanThreads, 0, c->stream>>>(a, pv, c->d_status);
+    a.arrived = c->d_status + 48;  // a line of its own
+    attn_plan_kernel<<<b.groups ? grid_for(b.tables.n, 1, 2u * c->n_cu) : 1, kPlanThreads, 0, c->stream>>>(
+        a, pv, c->d_status);
     return hipGetLastError();
 }
 

@@ -104,9 +104,12 @@ __device__ __forceinline__ uint32_t wave_find(const I* at, uint32_t n, uint32_t 
     return lo;
 }
 
-// The sequence whose new tokens t is among (if q_off is in order).
+// The sequence whose new tokens t is among (if q_off is in order).  In a decode
+// step token t is sequence t's, which one look confirms.
 __device__ __forceinline__ uint32_t sequence_of(const TokenBatch& b, uint32_t t)
 {
+    if (t < b.n && b.q_off[t] == (int64_t)t && b.q_off[t + 1] == (int64_t)t + 1)
+        return t;
     return b.n ? wave_find(b.q_off, b.n, 1, (int64_t)t) : 0;
 }
 

@@ -8,7 +8,9 @@
 //
 // The tables' calls are chains of short passes over the pages, the sequences
 // and the table entries; each pass needs the whole of the one before it, so
-// launches bound small calls and the scan by one workgroup large ones.
+// launches and waits bound them.  Small calls are one workgroup with everything
+// that the passes share in LDS; in large ones passes over entries take equal
+// shares of them, however long the tables are.
 #include "dm_internal.h"
 #include "dm_pages.h"
 
@@ -23,18 +25,21 @@ constexpr uint32_t kBadBlock = 1u << 31;   // of a page block's count: a negativ
 constexpr int64_t kMaxLen = 1ll << 31;     // sequences are shorter
 
 // ctl words: what a call has found wrong, then what its scan has found.
-enum : int { kCtlErr = 0, kCtlNeed = 1, kCtlMoves = 2, kCtlLive = 3, kCtlBelow = 4, kCtlWords = 8 };
+enum : int { kCtlErr = 0, kCtlNeed = 1, kCtlMoves = 2, kCtlLive = 3, kCtlBelow = 4, kCtlTurn = 5,
+             kCtlWords = 8 };
 
 // Work arrays of a call.
 struct Work {
     uint32_t* ctl;     // [kCtlWords]
-    uint32_t* blk;     // [blocks + 1] free (compact: live) pages per page block, then before it
+    uint32_t* blk;     // [blocks] free (compact: live) pages per page block, then before it
     int32_t* delta;    // [n_pages] change of the count by the tables
     uint32_t* writers; // [n_pages] sequences about to write into the page
     uint32_t* first;   // [n_pages] the first of them
+    uint32_t* list;    // [n_pages] free pages in order
     uint32_t* heir;    // [n] first sequence of the result that continues s
     uint32_t* base;    // [m] new pages before j's
     uint32_t* place;   // [m] j's move, kNone: none
+    int64_t* at;       // [m + 1] the result's entries before j's
 };
 
 struct ForkIn {
@@ -99,6 +104,97 @@ __device__ __forceinline__ void block_scan(uint64_t (&v)[K], uint64_t (&tot)[K],
     }
 }
 
+// Entries [e0, e1) of a CSR with bounds at[0 .. n] (row r begins at at[r]), by a
+// workgroup of kThreads, kEach entries a thread at once so that their reads
+// overlap.  make(r): what is to be known of a row, gathered once for all of its
+// entries (LDS holds it where the segment has few rows); use(entries, their
+// places in their rows, rows, number of entries that exist).
+constexpr int kEach = 4;
+constexpr uint32_t kSegment = kThreads * kEach, kHeldRows = kThreads;
+
+template <typename Row>
+struct SegmentLds {
+    int64_t at[kHeldRows];
+    Row row[kHeldRows];
+};
+
+template <typename Row, typename Make, typename Use>
+__device__ __forceinline__ void for_entries(const int64_t* at, uint32_t n, int64_t e0, int64_t e1,
+                                            SegmentLds<Row>& lds, Make&& make, Use&& use)
+{
+    const uint32_t r0 = wave_find(at, n, 1, e0), rows = wave_find(at, n, 1, e1 - 1) - r0 + 1;
+    const bool held = rows <= kHeldRows;
+    __syncthreads();
+    if (held && threadIdx.x < rows) {
+        lds.at[threadIdx.x] = at[r0 + threadIdx.x];
+        lds.row[threadIdx.x] = make(r0 + threadIdx.x);
+    }
+    __syncthreads();
+    const int64_t* b = held ? lds.at : at + r0;
+    int64_t e[kEach], i[kEach];
+    Row row[kEach];
+    int there = 0;
+#pragma unroll
+    for (int k = 0; k < kEach; k++) {
+        e[k] = e0 + threadIdx.x + k * kThreads;
+        if (e[k] >= e1)
+            continue;
+        there = k + 1;
+        uint32_t lo = 0, hi = rows;
+        while (hi - lo > 1) {
+            const uint32_t mid = (lo + hi) / 2;
+            if (b[mid] <= e[k])
+                lo = mid;
+            else
+                hi = mid;
+        }
+        i[k] = e[k] - b[lo];
+        row[k] = held ? lds.row[lo] : make(r0 + lo);
+    }
+    use(e, i, row, there);
+}
+
+// Is sequence s's table well formed?
+__device__ __forceinline__ bool table_ok(const ForkIn& a, uint32_t s)
+{
+    const int64_t o0 = a.off[s], o1 = a.off[s + 1], len = a.len[s];
+    return o0 >= 0 && o1 >= o0 && o1 <= a.entries && len >= 0 && len < kMaxLen &&
+           pages_of(len, a.shift) <= o1 - o0;
+}
+
+// Is what sequence j of the result takes well formed?
+__device__ __forceinline__ bool next_ok(const ForkIn& a, uint32_t j)
+{
+    const int64_t keep = a.keep[j], grow = a.grow[j];
+    if (keep < 0 || grow < 0 || keep >= kMaxLen || grow >= kMaxLen || keep + grow >= kMaxLen)
+        return false;
+    const uint32_t s = keep ? (uint32_t)a.src[j] : 0;
+    return !keep || (s < a.n && table_ok(a, s) && keep <= a.len[s]);
+}
+
+__device__ __forceinline__ bool writes(const ForkIn& a, int64_t keep, int64_t grow)
+{
+    return (keep & ((1ll << a.shift) - 1)) && grow;
+}
+
+// Rank of each thread's page among those of its kind (mine), in order over the
+// workgroup's pages; rank0 moves on by their number.
+__device__ __forceinline__ uint32_t rank_of(bool mine, uint32_t& rank0, uint32_t* lds)
+{
+    const uint64_t mask = ballot(mine);
+    __syncthreads();
+    if (lane_id() == 0)
+        lds[threadIdx.x / kWave] = __popcll(mask);
+    __syncthreads();
+    uint32_t rank = rank0 + __popcll(mask & ((1ull << lane_id()) - 1));
+    for (uint32_t k = 0; k < blockDim.x / kWave; k++) {
+        if (k < threadIdx.x / kWave)
+            rank += lds[k];
+        rank0 += lds[k];
+    }
+    return rank;
+}
+
 // Pass 1: work arrays cleared; free pages counted per block of pages.
 __global__ __launch_bounds__(kThreads) void fork_init_kernel(ForkIn a, Work w)
 {
@@ -128,81 +224,113 @@ __global__ __launch_bounds__(kThreads) void fork_init_kernel(ForkIn a, Work w)
         w.ctl[threadIdx.x] = 0;
 }
 
-// Is sequence s's table well formed?
-__device__ __forceinline__ bool table_ok(const ForkIn& a, uint32_t s)
-{
-    const int64_t o0 = a.off[s], o1 = a.off[s + 1], len = a.len[s];
-    return o0 >= 0 && o1 >= o0 && o1 <= a.entries && len >= 0 && len < kMaxLen &&
-           pages_of(len, a.shift) <= o1 - o0;
-}
-
-// Pass 2: sequences checked; the first continuation of each found.
+// Pass 2: sequences checked, the first continuation of each found; beside it,
+// the last workgroup sums the page blocks' counts.
 __global__ __launch_bounds__(kThreads) void fork_check_kernel(ForkIn a, Work w)
 {
-    const uint64_t stride = (uint64_t)gridDim.x * kThreads;
-    const uint64_t t0 = (uint64_t)blockIdx.x * kThreads + threadIdx.x;
+    __shared__ uint64_t lds[kThreads / kWave];
     bool bad = false;
-    for (uint64_t s = t0; s < a.n; s += stride)
-        bad |= !table_ok(a, (uint32_t)s);
-    for (uint64_t j = t0; j < a.m; j += stride) {
-        const int64_t keep = a.keep[j], grow = a.grow[j];
-        if (keep < 0 || grow < 0 || keep >= kMaxLen || grow >= kMaxLen || keep + grow >= kMaxLen) {
-            bad = true;
-            continue;
+    if (blockIdx.x == gridDim.x - 1) {
+        uint64_t carry = 0;
+        for (uint32_t b0 = 0; b0 < a.blocks; b0 += kThreads) {
+            const uint32_t b = b0 + threadIdx.x;
+            const uint32_t x = b < a.blocks ? w.blk[b] : 0;
+            uint64_t v[1] = {x & ~kBadBlock}, tot[1];
+            bad |= (x & kBadBlock) != 0;
+            block_scan<1>(v, tot, lds);
+            if (b < a.blocks)
+                w.blk[b] = (uint32_t)(carry + v[0]);
+            carry += tot[0];
         }
-        if (!keep)
-            continue;
-        const uint32_t s = (uint32_t)a.src[j];
-        if (s >= a.n || !table_ok(a, s) || keep > a.len[s]) {
-            bad = true;
-            continue;
+        if (threadIdx.x == 0)
+            w.ctl[kCtlLive] = (uint32_t)carry;  // free pages
+    } else {
+        const uint64_t stride = (uint64_t)(gridDim.x - 1) * kThreads;
+        const uint64_t t0 = (uint64_t)blockIdx.x * kThreads + threadIdx.x;
+        for (uint64_t s = t0; s < a.n; s += stride)
+            bad |= !table_ok(a, (uint32_t)s);
+        for (uint64_t j = t0; j < a.m; j += stride) {
+            if (!next_ok(a, (uint32_t)j))
+                bad = true;
+            else if (a.keep[j])
+                atomicMin(&w.heir[a.src[j]], (uint32_t)j);
         }
-        atomicMin(&w.heir[s], (uint32_t)j);
     }
     if (bad)
         atomicOr(&w.ctl[kCtlErr], kErrInval);
 }
 
-// Pass 3, a workgroup for a sequence: the counts' changes.  The first
+// Pass 3: the counts' changes, and the free pages listed.  The first
 // continuation of s takes s's references over, so that a sequence that just
-// goes on changes nothing: what it does not keep is released, and every other
-// continuation's pages get a reference more.
-__global__ __launch_bounds__(kThreads) void fork_count_kernel(ForkIn a, Work w)
+// goes on changes nothing: what it does not keep is released (equal shares of
+// the entries), and every other continuation's pages get a reference more (a
+// wave each).
+__global__ __launch_bounds__(kThreads) void fork_count_kernel(ForkIn a, Work w, uint32_t segments)
 {
+    __shared__ SegmentLds<int64_t> rows;
+    __shared__ uint32_t lds[kThreads / kWave];
     if (w.ctl[kCtlErr])
         return;
     bool bad = false;
-    for (uint64_t u = blockIdx.x; u < (uint64_t)a.n + a.m; u += gridDim.x) {
-        if (u < a.n) {
-            const uint32_t h = w.heir[u];
-            const int64_t o0 = a.off[u], o1 = a.off[u + 1];
-            const int64_t kept = h == kNone ? 0 : pages_of(a.keep[h], a.shift);
-            for (int64_t e = o0 + threadIdx.x; e < o1; e += kThreads) {
-                const uint32_t p = (uint32_t)a.page[e];
-                if (p >= a.n_pages || a.ref[p] <= 0)
-                    bad = true;
-                else if (e - o0 >= kept)
-                    atomicAdd(&w.delta[p], -1);
+    const uint64_t all = (uint64_t)a.blocks + segments + (a.m + kThreads / kWave - 1) / (kThreads / kWave);
+    for (uint64_t u = blockIdx.x; u < all; u += gridDim.x) {
+        if (u < segments) {
+            const int64_t first = a.n ? a.off[0] : 0, last = a.n ? a.off[a.n] : 0;
+            const int64_t e0 = first + (int64_t)u * kSegment;
+            if (e0 >= last)
+                continue;
+            for_entries<int64_t>(
+                a.off, a.n, e0, e0 + kSegment < last ? e0 + kSegment : last, rows,
+                [&](uint32_t s) -> int64_t {
+                    const uint32_t h = w.heir[s];
+                    return h == kNone ? 0 : pages_of(a.keep[h], a.shift);
+                },
+                [&](const int64_t* e, const int64_t* i, const int64_t* kept, int there) {
+                    uint32_t p[kEach];
+                    int32_t r[kEach];
+#pragma unroll
+                    for (int k = 0; k < kEach; k++)
+                        p[k] = k < there ? (uint32_t)a.page[e[k]] : 0;
+#pragma unroll
+                    for (int k = 0; k < kEach; k++)
+                        r[k] = p[k] < a.n_pages ? a.ref[p[k]] : 0;
+#pragma unroll
+                    for (int k = 0; k < kEach; k++)
+                        if (k < there) {
+                            bad |= r[k] <= 0;
+                            if (r[k] > 0 && i[k] >= kept[k])
+                                atomicAdd(&w.delta[p[k]], -1);
+                        }
+                });
+        } else if (u < (uint64_t)a.blocks + segments) {
+            const uint64_t b = u - segments;
+            uint32_t rank0 = w.blk[b];
+            for (uint32_t i0 = 0; i0 < kPageBlock; i0 += kThreads) {
+                const uint64_t p = b * kPageBlock + i0 + threadIdx.x;
+                const bool mine = p < a.n_pages && a.ref[p] == 0;
+                const uint32_t rank = rank_of(mine, rank0, lds);
+                if (mine)
+                    w.list[rank] = (uint32_t)p;
             }
-            continue;
-        }
-        const uint32_t j = (uint32_t)(u - a.n);
-        const int64_t keep = a.keep[j];
-        if (!keep)
-            continue;
-        const uint32_t s = (uint32_t)a.src[j];
-        const int64_t o0 = a.off[s], kept = pages_of(keep, a.shift);
-        if (w.heir[s] != j)
-            for (int64_t i = threadIdx.x; i < kept; i += kThreads) {
-                const uint32_t p = (uint32_t)a.page[o0 + i];
-                if (p < a.n_pages)
-                    atomicAdd(&w.delta[p], 1);
-            }
-        if (threadIdx.x == 0 && (keep & ((1ll << a.shift) - 1)) && a.grow[j]) {
-            const uint32_t p = (uint32_t)a.page[o0 + kept - 1];
-            if (p < a.n_pages) {
-                atomicAdd(&w.writers[p], 1u);
-                atomicMin(&w.first[p], j);
+        } else {
+            const uint64_t j = (u - a.blocks - segments) * (kThreads / kWave) + threadIdx.x / kWave;
+            const int64_t keep = j < a.m ? a.keep[j] : 0;
+            if (!keep)
+                continue;
+            const uint32_t s = (uint32_t)a.src[j];
+            const int64_t o0 = a.off[s], kept = pages_of(keep, a.shift);
+            if (w.heir[s] != (uint32_t)j)
+                for (int64_t i = lane_id(); i < kept; i += kWave) {
+                    const uint32_t p = (uint32_t)a.page[o0 + i];
+                    if (p < a.n_pages)
+                        atomicAdd(&w.delta[p], 1);
+                }
+            if (lane_id() == 0 && writes(a, keep, a.grow[j])) {
+                const uint32_t p = (uint32_t)a.page[o0 + kept - 1];
+                if (p < a.n_pages) {
+                    atomicAdd(&w.writers[p], 1u);
+                    atomicMin(&w.first[p], (uint32_t)j);
+                }
             }
         }
     }
@@ -210,156 +338,322 @@ __global__ __launch_bounds__(kThreads) void fork_count_kernel(ForkIn a, Work w)
         atomicOr(&w.ctl[kCtlErr], kErrInval);
 }
 
-// Does writer j of page p get a page of its own?
-__device__ __forceinline__ bool copies(const ForkIn& a, const Work& w, uint32_t p, uint32_t j)
+__device__ __forceinline__ void agent_store(uint32_t* p, uint32_t x)
 {
-    const bool alone = a.ref[p] + w.delta[p] == (int32_t)w.writers[p];
-    return !(alone && w.first[p] == j);
+    __hip_atomic_store(p, x, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ uint32_t agent_load(const uint32_t* p)
+{
+    return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }
 
-// Pass 4, one workgroup: free pages before each block, new pages, entries and
-// moves before each sequence; whether all of them have room.
+// Pass 4: new pages, entries and moves before each sequence, and whether all of
+// them have room.  Whether a sequence copies a page takes a chain of scattered
+// reads, a thread a sequence over the chip (by one workgroup 18 us for 4,096);
+// the last workgroup to finish sums.
 __global__ __launch_bounds__(kPlanThreads) void fork_scan_kernel(ForkIn a, Work w, dm_pages_out out,
                                                                  uint32_t* status)
 {
     __shared__ uint64_t lds[3 * kPlanThreads / kWave];
-    __shared__ uint32_t err;
-    if (threadIdx.x == 0) {
-        err = w.ctl[kCtlErr];
-        out.moves[0] = 0;
-    }
-    __syncthreads();
-    uint64_t carry = 0;
-    bool bad = false;
-    for (uint32_t b0 = 0; b0 < a.blocks; b0 += kPlanThreads) {
-        const uint32_t b = b0 + threadIdx.x;
-        const uint32_t x = b < a.blocks ? w.blk[b] : 0;
-        uint64_t v[1] = {x & ~kBadBlock}, tot[1];
-        bad |= (x & kBadBlock) != 0;
-        block_scan<1>(v, tot, lds);
-        if (b < a.blocks)
-            w.blk[b] = (uint32_t)(carry + v[0]);
-        carry += tot[0];
-    }
-    if (bad)
-        atomicOr(&err, kErrInval);
-    __syncthreads();
-    const bool ok = err == 0;
-    uint64_t at[3] = {0, 0, 0};
-    for (uint32_t j0 = 0; ok && j0 < a.m; j0 += kPlanThreads) {
-        const uint32_t j = j0 + threadIdx.x;
-        uint64_t v[3] = {0, 0, 0}, tot[3];
+    __shared__ uint32_t turn;
+    const uint32_t err = w.ctl[kCtlErr], free_pages = w.ctl[kCtlLive];
+    constexpr uint32_t kCopies = 1u << 31;  // of base: the sequence copies a page
+    for (uint64_t x = (uint64_t)blockIdx.x * kPlanThreads + threadIdx.x; err == 0 && x < a.m;
+         x += (uint64_t)gridDim.x * kPlanThreads) {
+        const uint32_t j = (uint32_t)x;
+        const int64_t keep = a.keep[j], grow = a.grow[j], kept = pages_of(keep, a.shift);
+        const uint32_t all = (uint32_t)pages_of(keep + grow, a.shift);
         bool copy = false;
-        if (j < a.m) {
-            const int64_t keep = a.keep[j], grow = a.grow[j];
-            const int64_t kept = pages_of(keep, a.shift), all = pages_of(keep + grow, a.shift);
-            if ((keep & ((1ll << a.shift) - 1)) && grow)
-                copy = copies(a, w, (uint32_t)a.page[a.off[a.src[j]] + kept - 1], j);
-            v[0] = all - kept + copy;
-            v[1] = all;
-            v[2] = copy;
+        if (writes(a, keep, grow)) {
+            // a writer alone with its page keeps it, of several the first
+            const uint32_t p = (uint32_t)a.page[a.off[a.src[j]] + kept - 1];
+            copy = !(a.ref[p] + w.delta[p] == (int32_t)w.writers[p] && w.first[p] == j);
+        }
+        agent_store(&w.base[j], (all - (uint32_t)kept + copy) | (copy ? kCopies : 0));
+        agent_store(&w.place[j], all);
+    }
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "agent");
+        turn = atomicAdd(&w.ctl[kCtlTurn], 1u);
+    }
+    __syncthreads();
+    if (turn != gridDim.x - 1)
+        return;
+    constexpr int kItems = 4;
+    uint64_t at[3] = {0, 0, 0};
+    for (uint32_t j0 = 0; err == 0 && j0 < a.m; j0 += kPlanThreads * kItems) {
+        uint64_t v[3] = {0, 0, 0}, tot[3];
+        uint32_t fresh[kItems], all[kItems];
+#pragma unroll
+        for (int k = 0; k < kItems; k++) {
+            const uint32_t j = j0 + threadIdx.x * kItems + k;
+            fresh[k] = j < a.m ? agent_load(&w.base[j]) : 0;
+            all[k] = j < a.m ? agent_load(&w.place[j]) : 0;
+            v[0] += fresh[k] & ~kCopies;
+            v[1] += all[k];
+            v[2] += fresh[k] >> 31;
         }
         block_scan<3>(v, tot, lds);
-        if (j < a.m) {
-            w.base[j] = (uint32_t)(at[0] + v[0]);
-            w.place[j] = copy ? (uint32_t)(at[2] + v[2]) : kNone;
+#pragma unroll
+        for (int k = 0; k < kItems; k++) {
+            const uint32_t j = j0 + threadIdx.x * kItems + k;
+            if (j < a.m) {
+                w.base[j] = (uint32_t)(at[0] + v[0]);
+                w.at[j] = (int64_t)(at[1] + v[1]);
+                w.place[j] = fresh[k] & kCopies ? (uint32_t)(at[2] + v[2]) : kNone;
+            }
+            v[0] += fresh[k] & ~kCopies;
+            v[1] += all[k];
+            v[2] += fresh[k] >> 31;
         }
         for (int k = 0; k < 3; k++)
             at[k] += tot[k];
     }
-    // free pages, entries, moves, and entries of the reference counts
-    uint32_t full = ok && (at[0] > carry || at[1] > out.cap || at[2] > out.move_cap) ? kErrFull : 0;
-    if (threadIdx.x == 0) {
-        w.ctl[kCtlErr] = err | full;
-        w.ctl[kCtlNeed] = (uint32_t)at[0];
-        if (err | full)
-            atomicOr(status, err | full);
-        else
-            out.moves[0] = (int64_t)at[2];
-    }
-    if (!ok || full)
+    if (threadIdx.x)
         return;
-    uint64_t o = 0;
-    for (uint32_t j0 = 0; j0 < a.m; j0 += kPlanThreads) {
-        const uint32_t j = j0 + threadIdx.x;
-        const int64_t len = j < a.m ? a.keep[j] + a.grow[j] : 0;
-        uint64_t v[1] = {(uint64_t)pages_of(len, a.shift)}, tot[1];
-        block_scan<1>(v, tot, lds);
-        if (j < a.m) {
-            out.off[j] = (int64_t)(o + v[0]);
-            out.len[j] = len;
-        }
-        o += tot[0];
-    }
-    if (threadIdx.x == 0)
-        out.off[a.m] = (int64_t)o;
+    const uint32_t e = err ? err : at[0] > free_pages || at[1] > out.cap || at[2] > out.move_cap ? kErrFull : 0;
+    w.at[a.m] = (int64_t)at[1];
+    w.ctl[kCtlErr] = e;
+    w.ctl[kCtlNeed] = (uint32_t)at[0];
+    out.moves[0] = e ? 0 : (int64_t)at[2];
+    if (e)
+        atomicOr(status, e);
 }
 
-// Pass 5: page blocks give their free pages away and write the counts; then
-// a workgroup for a sequence copies the entries that it keeps.
-__global__ __launch_bounds__(kThreads) void fork_write_kernel(ForkIn a, Work w, dm_pages_out out)
+// The count of page p after the call (r: before; not free).
+__device__ __forceinline__ int32_t count_after(int32_t r, int32_t delta, uint32_t writers)
 {
+    const int32_t total = r + delta;
+    return total - (int32_t)(writers && total == (int32_t)writers ? writers - 1 : writers);
+}
+
+// What the entries of a sequence of the result are made of.
+struct NextRow {
+    int64_t from;           // the kept pages' first entry
+    uint32_t own;           // entries that stay as they are
+    uint32_t base, place;   // first new page's rank, move
+};
+
+// Pass 5: counts, bounds and lengths, and equal shares of the result's entries.
+__global__ __launch_bounds__(kThreads) void fork_write_kernel(ForkIn a, Work w, dm_pages_out out,
+                                                              uint32_t segments)
+{
+    __shared__ SegmentLds<NextRow> rows;
+    __shared__ uint32_t lds[kThreads / kWave];
     if (w.ctl[kCtlErr])
         return;
     const uint32_t need = w.ctl[kCtlNeed];
-    for (uint64_t u = blockIdx.x; u < (uint64_t)a.blocks + a.m; u += gridDim.x) {
-        if (u < a.blocks) {
-            __shared__ uint32_t lds[kThreads / kWave];
-            uint32_t rank0 = w.blk[u];
-            for (uint32_t i0 = 0; i0 < kPageBlock; i0 += kThreads) {
-                const uint64_t p = u * kPageBlock + i0 + threadIdx.x;
-                const int32_t r = p < a.n_pages ? a.ref[p] : 1;
-                const uint64_t mask = ballot(r == 0);
-                __syncthreads();
-                if (lane_id() == 0)
-                    lds[threadIdx.x / kWave] = __popcll(mask);
-                __syncthreads();
-                uint32_t rank = rank0;
-                for (uint32_t k = 0; k < kThreads / kWave; k++) {
-                    if (k < threadIdx.x / kWave)
-                        rank += lds[k];
-                    rank0 += lds[k];
-                }
-                rank += __popcll(mask & ((1ull << lane_id()) - 1));
-                if (p >= a.n_pages)
-                    continue;
-                if (r > 0) {
-                    const uint32_t wr = w.writers[p];
-                    const int32_t total = r + w.delta[p];
-                    out.ref[p] = total - (int32_t)(wr && total == (int32_t)wr ? wr - 1 : wr);
-                } else if (rank >= need) {
-                    out.ref[p] = 0;
-                } else {
-                    // the sequence whose new pages the rank falls among
-                    uint32_t lo = 0, hi = a.m;
-                    while (hi - lo > 1) {
-                        const uint32_t mid = (lo + hi) / 2;
-                        if (w.base[mid] <= rank)
-                            lo = mid;
-                        else
-                            hi = mid;
-                    }
-                    const uint32_t k = rank - w.base[lo], place = w.place[lo];
-                    const bool copy = place != kNone;
-                    const int64_t kept = pages_of(a.keep[lo], a.shift);
-                    out.page[out.off[lo] + kept - copy + k] = (int32_t)p;
-                    if (copy && k == 0)
-                        out.move_dst[place] = (int32_t)p;
-                    out.ref[p] = 1;
-                }
-            }
+    for (uint64_t u = blockIdx.x; u < (uint64_t)a.blocks + segments; u += gridDim.x) {
+        if (u < segments) {
+            const int64_t last = w.at[a.m], e0 = (int64_t)u * kSegment;
+            if (e0 >= last)
+                continue;
+            for_entries<NextRow>(
+                w.at, a.m, e0, e0 + kSegment < last ? e0 + kSegment : last, rows,
+                [&](uint32_t j) -> NextRow {
+                    const int64_t keep = a.keep[j];
+                    const uint32_t place = w.place[j];
+                    return NextRow{keep ? a.off[a.src[j]] : 0,
+                                   (uint32_t)pages_of(keep, a.shift) - (place != kNone), w.base[j], place};
+                },
+                [&](const int64_t* e, const int64_t* i, const NextRow* r, int there) {
+                    int32_t p[kEach];
+#pragma unroll
+                    for (int k = 0; k < kEach; k++)
+                        if (k < there)
+                            p[k] = i[k] < r[k].own ? a.page[r[k].from + i[k]]
+                                                   : (int32_t)w.list[r[k].base + (i[k] - r[k].own)];
+#pragma unroll
+                    for (int k = 0; k < kEach; k++)
+                        if (k < there) {
+                            out.page[e[k]] = p[k];
+                            if (r[k].place != kNone && i[k] == r[k].own) {
+                                out.move_src[r[k].place] = a.page[r[k].from + i[k]];
+                                out.move_dst[r[k].place] = p[k];
+                            }
+                        }
+                });
             continue;
         }
-        const uint32_t j = (uint32_t)(u - a.blocks);
-        const int64_t keep = a.keep[j];
-        if (!keep)
+        const uint64_t b = u - segments;
+        uint32_t rank0 = w.blk[b];
+        for (uint32_t i0 = 0; i0 < kPageBlock; i0 += kThreads) {
+            const uint64_t p = b * kPageBlock + i0 + threadIdx.x;
+            const int32_t r = p < a.n_pages ? a.ref[p] : 1;
+            const uint32_t rank = rank_of(r == 0, rank0, lds);
+            if (p < a.n_pages)
+                out.ref[p] = r ? count_after(r, w.delta[p], w.writers[p]) : rank < need;
+        }
+    }
+    const uint64_t stride = (uint64_t)gridDim.x * kThreads;
+    for (uint64_t j = (uint64_t)blockIdx.x * kThreads + threadIdx.x; j <= a.m; j += stride) {
+        out.off[j] = w.at[j];
+        if (j < a.m)
+            out.len[j] = a.keep[j] + a.grow[j];
+    }
+}
+
+// ---------------------------------------------------------------------------
+// A small call in one workgroup: the same passes, what they share in LDS.  (24
+// sequences over 900 pages: 9 us, the passes above 24.)
+// ---------------------------------------------------------------------------
+
+constexpr uint32_t kSmallPages = 8192, kSmallRows = 1024;
+constexpr uint64_t kSmallEntries = 32768;
+
+__global__ __launch_bounds__(kPlanThreads) void fork_small_kernel(ForkIn a, dm_pages_out out, uint32_t* status)
+{
+    __shared__ int32_t delta[kSmallPages];
+    __shared__ uint32_t first[kSmallPages];
+    __shared__ __attribute__((aligned(4))) uint16_t writers[kSmallPages];
+    __shared__ uint16_t list[kSmallPages];
+    __shared__ uint64_t lds[3 * kPlanThreads / kWave];
+    __shared__ uint32_t heir[kSmallRows];
+    __shared__ int64_t in_at[kSmallRows + 1], out_at[kSmallRows + 1];
+    __shared__ uint32_t base[kSmallRows], place[kSmallRows], held[kSmallRows];
+    __shared__ int64_t from[kSmallRows];
+    __shared__ uint32_t err;
+    uint32_t* words = reinterpret_cast<uint32_t*>(lds);
+    const uint32_t tid = threadIdx.x, j = tid;
+    if (tid == 0)
+        err = 0;
+    heir[tid] = kNone;
+    if (tid < a.n)
+        in_at[tid] = a.off[tid];
+    if (tid == 0 && a.n)
+        in_at[a.n] = a.off[a.n];
+    __syncthreads();
+    // free pages listed, arrays cleared
+    bool bad = false;
+    uint32_t free_pages = 0;
+    for (uint32_t p0 = 0; p0 < a.n_pages; p0 += kPlanThreads) {
+        const uint32_t p = p0 + tid;
+        const int32_t r = p < a.n_pages ? a.ref[p] : 1;
+        const uint32_t rank = rank_of(r == 0, free_pages, words);
+        bad |= r < 0;
+        if (r == 0)
+            list[rank] = (uint16_t)p;
+        if (p < a.n_pages) {
+            delta[p] = 0;
+            first[p] = kNone;
+            writers[p] = 0;
+        }
+    }
+    if (tid < a.n)
+        bad |= !table_ok(a, tid);
+    const bool mine = j < a.m;
+    int64_t keep = 0, grow = 0, src_at = 0;
+    uint32_t s = 0;
+    if (mine) {
+        if (next_ok(a, j)) {
+            keep = a.keep[j];
+            grow = a.grow[j];
+            if (keep) {
+                s = (uint32_t)a.src[j];
+                src_at = in_at[s];
+                atomicMin(&heir[s], j);
+            }
+        } else {
+            bad = true;
+        }
+        held[j] = (uint32_t)pages_of(keep, a.shift);
+        from[j] = src_at;
+    }
+    if (bad)
+        atomicOr(&err, kErrInval);
+    __syncthreads();
+    if (err == 0) {
+        // what the first continuations do not keep is released
+        const int64_t e1 = a.n ? in_at[a.n] : 0;
+        for (int64_t e = (a.n ? in_at[0] : 0) + tid; e < e1; e += kPlanThreads) {
+            uint32_t lo = 0, hi = a.n;
+            while (hi - lo > 1) {
+                const uint32_t mid = (lo + hi) / 2;
+                if (in_at[mid] <= e)
+                    lo = mid;
+                else
+                    hi = mid;
+            }
+            const uint32_t p = (uint32_t)a.page[e], h = heir[lo];
+            if (p >= a.n_pages || a.ref[p] <= 0)
+                atomicOr(&err, kErrInval);
+            else if (e - in_at[lo] >= (h == kNone ? 0 : held[h]))
+                atomicAdd(&delta[p], -1);
+        }
+    }
+    __syncthreads();
+    const bool ok = err == 0;
+    // the other continuations' pages, a wave for one
+    for (uint32_t k = tid / kWave; ok && k < a.m; k += kPlanThreads / kWave)
+        if (held[k] && heir[a.src[k]] != k)
+            for (uint32_t i = lane_id(); i < held[k]; i += kWave)
+                atomicAdd(&delta[a.page[from[k] + i]], 1);
+    const bool writer = mine && writes(a, keep, grow);
+    uint32_t p = kNone;
+    if (ok && writer) {
+        p = (uint32_t)a.page[src_at + held[j] - 1];
+        atomicMin(&first[p], j);
+        // 16-bit counts in pairs
+        atomicAdd(reinterpret_cast<uint32_t*>(writers) + p / 2, p % 2 ? 1u << 16 : 1u);
+    }
+    __syncthreads();
+    uint64_t v[3] = {0, 0, 0}, tot[3];
+    bool copy = false;
+    if (ok && mine) {
+        copy = writer && !(a.ref[p] + delta[p] == (int32_t)writers[p] && first[p] == j);
+        v[1] = (uint64_t)pages_of(keep + grow, a.shift);
+        v[0] = v[1] - held[j] + copy;
+        v[2] = copy;
+    }
+    block_scan<3>(v, tot, lds);
+    const uint32_t full = ok && (tot[0] > free_pages || tot[1] > out.cap || tot[2] > out.move_cap) ? kErrFull : 0;
+    if (tid == 0) {
+        out.moves[0] = ok && !full ? (int64_t)tot[2] : 0;
+        if (err | full)
+            atomicOr(status, err | full);
+    }
+    if (!ok || full)
+        return;
+    if (mine) {
+        base[j] = (uint32_t)v[0];
+        place[j] = copy ? (uint32_t)v[2] : kNone;
+        out_at[j] = (int64_t)v[1];
+        out.off[j] = (int64_t)v[1];
+        out.len[j] = keep + grow;
+    }
+    if (tid == 0)
+        out.off[a.m] = (int64_t)tot[1];
+    __syncthreads();
+    for (int64_t e = tid; e < (int64_t)tot[1]; e += kPlanThreads) {
+        uint32_t lo = 0, hi = a.m;
+        while (hi - lo > 1) {
+            const uint32_t mid = (lo + hi) / 2;
+            if (out_at[mid] <= e)
+                lo = mid;
+            else
+                hi = mid;
+        }
+        const uint32_t i = (uint32_t)(e - out_at[lo]), pl = place[lo];
+        const uint32_t own = held[lo] - (pl != kNone);
+        if (i < own) {
+            out.page[e] = a.page[from[lo] + i];
             continue;
-        const uint32_t place = w.place[j];
-        const int64_t from = a.off[a.src[j]], to = out.off[j], kept = pages_of(keep, a.shift);
-        for (int64_t i = threadIdx.x; i < kept - (place != kNone); i += kThreads)
-            out.page[to + i] = a.page[from + i];
-        if (threadIdx.x == 0 && place != kNone)
-            out.move_src[place] = a.page[from + kept - 1];
+        }
+        const int32_t to = list[base[lo] + (i - own)];
+        out.page[e] = to;
+        if (pl != kNone && i == own) {
+            out.move_src[pl] = a.page[from[lo] + i];
+            out.move_dst[pl] = to;
+        }
+    }
+    uint32_t rank0 = 0;
+    for (uint32_t p0 = 0; p0 < a.n_pages; p0 += kPlanThreads) {
+        const uint32_t q = p0 + tid;
+        const int32_t r = q < a.n_pages ? a.ref[q] : 1;
+        const uint32_t rank = rank_of(r == 0, rank0, words);
+        if (q < a.n_pages)
+            out.ref[q] = r ? count_after(r, delta[q], writers[q]) : rank < tot[0];
     }
 }
 
@@ -469,18 +763,7 @@ __global__ __launch_bounds__(kThreads) void compact_list_kernel(CompactIn a, Wor
     for (uint32_t i0 = 0; i0 < kPageBlock; i0 += kThreads) {
         const uint64_t p = (uint64_t)blockIdx.x * kPageBlock + i0 + threadIdx.x;
         const int32_t r = p < a.n_pages ? a.ref[p] : 0;
-        const uint64_t mask = ballot(r > 0);
-        __syncthreads();
-        if (lane_id() == 0)
-            lds[threadIdx.x / kWave] = __popcll(mask);
-        __syncthreads();
-        uint32_t rank = rank0;
-        for (uint32_t k = 0; k < kThreads / kWave; k++) {
-            if (k < threadIdx.x / kWave)
-                rank += lds[k];
-            rank0 += lds[k];
-        }
-        rank += __popcll(mask & ((1ull << lane_id()) - 1));
+        const uint32_t rank = rank_of(r > 0, rank0, lds);
         if (p >= a.n_pages)
             continue;
         if (p < live) {
@@ -513,6 +796,74 @@ __global__ __launch_bounds__(kThreads) void compact_write_kernel(CompactIn a, Wo
             const int32_t p = a.page[e];
             out.page[e] = (uint32_t)p < live ? p : out.move_dst[w.first[p]];
         }
+}
+
+// A small call in one workgroup.
+__global__ __launch_bounds__(kPlanThreads) void compact_small_kernel(CompactIn a, dm_pages_out out,
+                                                                     uint32_t* status)
+{
+    __shared__ uint16_t rank_at[kSmallPages], hole[kSmallPages];
+    __shared__ uint32_t words[kPlanThreads / kWave], err;
+    const uint32_t tid = threadIdx.x;
+    if (tid == 0)
+        err = 0;
+    uint32_t live = 0;
+    bool bad = false;
+    for (uint32_t p0 = 0; p0 < a.n_pages; p0 += kPlanThreads) {
+        const uint32_t p = p0 + tid;
+        const int32_t r = p < a.n_pages ? a.ref[p] : 0;
+        const uint32_t rank = rank_of(r > 0, live, words);
+        bad |= r < 0;
+        if (p < a.n_pages)
+            rank_at[p] = (uint16_t)rank;
+    }
+    for (uint32_t s = tid; s < a.n; s += kPlanThreads) {
+        const int64_t o0 = a.off[s], o1 = a.off[s + 1];
+        bad |= o0 < 0 || o1 < o0 || o1 > a.entries;
+    }
+    if (bad)
+        atomicOr(&err, kErrInval);
+    __syncthreads();
+    const bool ordered = err == 0;
+    __syncthreads();
+    const int64_t e0 = ordered && a.n ? a.off[0] : 0, e1 = ordered && a.n ? a.off[a.n] : 0;
+    for (int64_t e = e0 + tid; e < e1; e += kPlanThreads) {
+        const uint32_t p = (uint32_t)a.page[e];
+        if (p >= a.n_pages || a.ref[p] <= 0)
+            atomicOr(&err, kErrInval);
+    }
+    __syncthreads();
+    const uint32_t below = live < a.n_pages ? rank_at[live] : live, moves = live - below;
+    const uint32_t wrong = err ? err : moves > out.move_cap ? kErrFull : 0;
+    if (tid == 0) {
+        out.moves[0] = wrong ? 0 : (int64_t)moves;
+        if (wrong)
+            atomicOr(status, wrong);
+        else
+            out.live[0] = live;
+    }
+    if (wrong)
+        return;
+    for (uint32_t p = tid; p < live; p += kPlanThreads)
+        if (a.ref[p] == 0) {
+            hole[p - rank_at[p]] = (uint16_t)p;
+            out.move_dst[p - rank_at[p]] = (int32_t)p;
+        } else {
+            out.ref[p] = a.ref[p];
+        }
+    __syncthreads();
+    for (uint32_t p = live + tid; p < a.n_pages; p += kPlanThreads) {
+        const int32_t r = a.ref[p];
+        out.ref[p] = 0;
+        if (r > 0) {
+            out.move_src[rank_at[p] - below] = (int32_t)p;
+            out.ref[hole[rank_at[p] - below]] = r;
+        }
+    }
+    for (int64_t e = e0 + tid; e < e1; e += kPlanThreads) {
+        const uint32_t p = (uint32_t)a.page[e];
+        out.page[e] = p < live ? (int32_t)p : (int32_t)hole[rank_at[p] - below];
+    }
 }
 
 // ---------------------------------------------------------------------------
@@ -602,32 +953,42 @@ hipError_t pages_fork(dm_ctx* c, const dm_page_tables& in, const int32_t* ref, u
                       const dm_pages_out& out)
 {
     const uint32_t blocks = (n_pages + kPageBlock - 1) / kPageBlock;
+    const ForkIn a{in.off, in.page, in.len, (uint32_t)in.n, (int64_t)in.entries, ref, n_pages,
+                   blocks, src, keep, grow, (uint32_t)m, log2_of(c->cfg.block_size)};
+    hipStream_t st = c->stream;
+    if (n_pages <= kSmallPages && in.n <= kSmallRows && m <= kSmallRows && in.entries <= kSmallEntries &&
+        out.cap <= kSmallEntries) {
+        fork_small_kernel<<<1, kPlanThreads, 0, st>>>(a, out, c->d_status);
+        return hipGetLastError();
+    }
     hipError_t e;
     uint8_t* p = static_cast<uint8_t*>(scratch_get(
         c, kSlotPages,
-        up256(4 * kCtlWords) + up256(4 * (uint64_t)(blocks + 1)) + 3 * up256(4 * (uint64_t)n_pages) +
-            up256(4 * in.n) + 2 * up256(4 * m),
+        up256(4 * kCtlWords) + up256(4 * (uint64_t)blocks) + 4 * up256(4 * (uint64_t)n_pages) +
+            up256(4 * in.n) + 2 * up256(4 * m) + up256(8 * (m + 1)),
         &e));
     if (!p)
         return e;
     Work w;
     w.ctl = carve<uint32_t>(p, kCtlWords);
-    w.blk = carve<uint32_t>(p, blocks + 1);
+    w.blk = carve<uint32_t>(p, blocks);
     w.delta = carve<int32_t>(p, n_pages);
     w.writers = carve<uint32_t>(p, n_pages);
     w.first = carve<uint32_t>(p, n_pages);
+    w.list = carve<uint32_t>(p, n_pages);
     w.heir = carve<uint32_t>(p, in.n);
     w.base = carve<uint32_t>(p, m);
     w.place = carve<uint32_t>(p, m);
-    const ForkIn a{in.off, in.page, in.len, (uint32_t)in.n, (int64_t)in.entries, ref, n_pages,
-                   blocks, src, keep, grow, (uint32_t)m, log2_of(c->cfg.block_size)};
-    hipStream_t st = c->stream;
+    w.at = carve<int64_t>(p, m + 1);
     const uint32_t over = grid_for(in.n > m ? in.n : m, kThreads, 4096);
+    const uint32_t in_segments = (uint32_t)((in.entries + kSegment - 1) / kSegment);
+    const uint32_t out_segments = (uint32_t)((out.cap + kSegment - 1) / kSegment);
     fork_init_kernel<<<blocks > over ? blocks : over, kThreads, 0, st>>>(a, w);
-    fork_check_kernel<<<over, kThreads, 0, st>>>(a, w);
-    fork_count_kernel<<<grid_for(in.n + m, 1), kThreads, 0, st>>>(a, w);
-    fork_scan_kernel<<<1, kPlanThreads, 0, st>>>(a, w, out, c->d_status);
-    fork_write_kernel<<<grid_for(blocks + m, 1), kThreads, 0, st>>>(a, w, out);
+    fork_check_kernel<<<over + 1, kThreads, 0, st>>>(a, w);
+    fork_count_kernel<<<grid_for((uint64_t)blocks + in_segments + (m + 3) / 4, 1), kThreads, 0, st>>>(
+        a, w, in_segments);
+    fork_scan_kernel<<<grid_for(m, kPlanThreads, 256), kPlanThreads, 0, st>>>(a, w, out, c->d_status);
+    fork_write_kernel<<<grid_for((uint64_t)blocks + out_segments, 1), kThreads, 0, st>>>(a, w, out, out_segments);
     return hipGetLastError();
 }
 
@@ -635,22 +996,26 @@ hipError_t pages_compact(dm_ctx* c, const dm_page_tables& in, const int32_t* ref
                          uint32_t n_pages, const dm_pages_out& out)
 {
     const uint32_t blocks = (n_pages + kPageBlock - 1) / kPageBlock;
+    const CompactIn a{in.off, in.page, (uint32_t)in.n, (int64_t)in.entries, ref, n_pages, blocks};
+    hipStream_t st = c->stream;
+    if (n_pages <= kSmallPages && in.entries <= kSmallEntries) {
+        compact_small_kernel<<<1, kPlanThreads, 0, st>>>(a, out, c->d_status);
+        return hipGetLastError();
+    }
     const uint32_t grid = grid_for(blocks + in.n, 1);
     hipError_t e;
     uint8_t* p = static_cast<uint8_t*>(scratch_get(
         c, kSlotPages,
-        up256(4 * kCtlWords) + up256(4 * (uint64_t)(blocks + 1)) + up256(4 * (uint64_t)n_pages) +
+        up256(4 * kCtlWords) + up256(4 * (uint64_t)blocks) + up256(4 * (uint64_t)n_pages) +
             up256(4 * (uint64_t)grid),
         &e));
     if (!p)
         return e;
     Work w{};
     w.ctl = carve<uint32_t>(p, kCtlWords);
-    w.blk = carve<uint32_t>(p, blocks + 1);
+    w.blk = carve<uint32_t>(p, blocks);
     w.first = carve<uint32_t>(p, n_pages);
     uint32_t* flag = carve<uint32_t>(p, grid);
-    const CompactIn a{in.off, in.page, (uint32_t)in.n, (int64_t)in.entries, ref, n_pages, blocks};
-    hipStream_t st = c->stream;
     compact_count_kernel<<<grid, kThreads, 0, st>>>(a, w, flag);
     compact_scan_kernel<<<1, kPlanThreads, 0, st>>>(a, w, flag, grid, out, c->d_status);
     compact_list_kernel<<<blocks, kThreads, 0, st>>>(a, w, out);
