@@ -18,9 +18,9 @@
 // order, which V's transposing LDS reads follow), so weights never leave their
 // lane.
 //
-//   narrow tiles: 32 rows; the four waves take every fourth 32 keys, each
-//     through its own part of LDS, and are joined at the end.  For rows that
-//     are few: bound by reading the pages.
+//   narrow tiles: 16 rows, on 16x16x32 instructions; the four waves take every
+//     fourth 32 keys, each through its own part of LDS, and are joined at the
+//     end.  For rows that are few: bound by reading the pages.
 //   wide tiles: 128 rows, 32 a wave, on a shared tile of 64 keys (two in LDS).
 //     Bound by the matrix and vector units.
 #include "dm_internal.h"
@@ -30,7 +30,8 @@ namespace dm {
 namespace {
 
 constexpr int kThreads = 256, kWaves = 4;
-constexpr uint32_t kNarrow = 32, kWide = 128;  // rows of a tile
+constexpr uint32_t kNarrow = 16, kWide = 128;  // rows of a tile
+constexpr uint32_t kNarrowRows = 64;           // rows of a unit, at most, that has narrow tiles
 constexpr uint32_t kNarrowKeys = 32, kWideKeys = 64;
 constexpr uint32_t kChunk = 128;               // chunks are multiples of this many keys
 constexpr uint32_t kLeastChunk = 128;          // and no shorter than this
@@ -43,10 +44,11 @@ constexpr uint64_t kPartRows = 1ull << 20;     // rows of parts kept beyond thos
 struct PlanHead {
     uint32_t n, groups, q_tokens, q_heads, kv_heads, shift;  // what it was made for
     int64_t entries;
-    uint32_t items, units;
+    uint32_t items;
     uint32_t chunk;       // keys of a chunk
     uint32_t part_rows;   // rows of parts
     uint32_t most_parts;  // of a row
+    uint32_t head_dim;
     uint32_t pad[3];
 };
 struct Unit {
@@ -91,9 +93,10 @@ __host__ __device__ inline PlanView plan_view(void* p, uint64_t n, uint64_t grou
     return v;
 }
 
-// A tile's cost a key: a wide one reads as much as a narrow one and takes
-// about twice its time.
-__device__ __forceinline__ uint32_t tile_rows(uint64_t rows) { return rows > 2 * kNarrow ? kWide : kNarrow; }
+// The tiles of a unit, by its rows, and their cost a key: a wide one reads as
+// much as a narrow one and takes about twice its time.
+__device__ __forceinline__ uint32_t tile_rows(uint64_t rows) { return rows <= kNarrowRows ? kNarrow : kWide; }
+__device__ __forceinline__ uint32_t tile_flags(uint64_t rows) { return tile_rows(rows) == kWide ? kUnitWide : 0; }
 __device__ __forceinline__ uint64_t tiles_of(uint64_t rows)
 {
     return (rows + tile_rows(rows) - 1) / tile_rows(rows);
@@ -125,7 +128,7 @@ __device__ __forceinline__ uint64_t block_sum64(uint64_t v, uint64_t* lds)
 
 struct PlanIn {
     TokenBatch b;
-    uint32_t q_heads, kv_heads, ratio;
+    uint32_t q_heads, kv_heads, ratio, head_dim;
     uint64_t target;     // items wanted
     uint64_t part_rows;  // rows of parts there is room for
     uint32_t* arrived;   // workgroups that are done with their sequences; zero between calls
@@ -194,7 +197,7 @@ __device__ __forceinline__ Unit run_unit(const PlanIn& a, uint32_t g, uint32_t p
     u.key1 = pages << a.b.shift;
     u.off = a.b.off[s0];
     u.table = pages;
-    u.flags = kUnitParts | (tile_rows((uint64_t)u.ntok * a.ratio) == kWide ? kUnitWide : 0);
+    u.flags = kUnitParts | tile_flags((uint64_t)u.ntok * a.ratio);
     return u;
 }
 
@@ -208,8 +211,7 @@ __device__ __forceinline__ Unit sequence_unit(const PlanIn& a, const SeqView& v,
     u.off = v.off;
     u.table = (uint32_t)((v.len + (1ll << a.b.shift) - 1) >> a.b.shift);
     u.pos0 = (int32_t)v.pos0;
-    u.flags = kUnitCausal | (pages ? kUnitParts : 0) |
-              (tile_rows((uint64_t)u.ntok * a.ratio) == kWide ? kUnitWide : 0);
+    u.flags = kUnitCausal | (pages ? kUnitParts : 0) | tile_flags((uint64_t)u.ntok * a.ratio);
     return u;
 }
 
@@ -226,9 +228,8 @@ __device__ __forceinline__ bool worth_sharing(const PlanIn& a, uint32_t g, uint3
 
 // Which runs share their prefixes, the chunk, and the units' items.  With
 // runs, a workgroup for a sequence first, and the last one to finish goes on
-// alone (a launch less; 10 us with two launches and every step through memory, at
-// 256 sequences).  A thread keeps its unit in registers from step to step;
-// beyond 1024 units the others are made again for each step.
+// alone (a launch less).  A thread keeps its first unit in registers from step to
+// step, and those past the first 1024 in the plan.
 __global__ __launch_bounds__(kPlanThreads) void attn_plan_kernel(PlanIn a, PlanView pv, uint32_t* status)
 {
     __shared__ uint64_t lds[2 * kPlanThreads / kWave];
@@ -297,11 +298,15 @@ __global__ __launch_bounds__(kPlanThreads) void attn_plan_kernel(PlanIn a, PlanV
             return u.ntok ? weight_of((uint64_t)u.ntok * a.ratio) * (u.key1 - u.key0) : 0;
         };
         Unit mine{};
-        if (tid < units)
-            mine = make(tid);
-        uint64_t cost = cost_of(mine);
-        for (uint32_t i = tid + kPlanThreads; i < units; i += kPlanThreads)
-            cost += cost_of(make(i));
+        uint64_t cost = 0;
+        for (uint32_t i = tid; i < units; i += kPlanThreads) {
+            const Unit u = make(i);
+            cost += cost_of(u);
+            if (i == tid)
+                mine = u;
+            else
+                pv.unit[i] = u;
+        }
         cost = block_sum64(cost, lds) * a.kv_heads;
         uint64_t chunk = (cost / a.target + kChunk) / kChunk * kChunk;
         if (chunk < kLeastChunk)
@@ -317,7 +322,7 @@ __global__ __launch_bounds__(kPlanThreads) void attn_plan_kernel(PlanIn a, PlanV
             uint64_t it = 0, rw = 0;
             Unit u = mine;
             if (u0 && i < units)
-                u = make(i);
+                u = pv.unit[i];
             __syncthreads();
             if (i < units && u.ntok) {
                 const uint64_t r = (uint64_t)u.ntok * a.ratio;
@@ -333,14 +338,15 @@ __global__ __launch_bounds__(kPlanThreads) void attn_plan_kernel(PlanIn a, PlanV
                 }
             }
             const uint64_t i1 = wave_incl_sum_u64(it, 0), r1 = wave_incl_sum_u64(rw, 0);
+            constexpr uint32_t kPlanWaves = kPlanThreads / kWave;
             if (lane_id() == kWave - 1) {
                 lds[tid / kWave] = i1;
-                lds[kPlanThreads / kWave + tid / kWave] = r1;
+                lds[kPlanWaves + tid / kWave] = r1;
             }
             __syncthreads();
             uint64_t ib = items, rb = rows;
-            for (uint32_t w = 0; w < kPlanThreads / kWave; w++) {
-                const uint64_t x = lds[w], y = lds[kPlanThreads / kWave + w];
+            for (uint32_t w = 0; w < kPlanWaves; w++) {
+                const uint64_t x = lds[w], y = lds[kPlanWaves + w];
                 if (w < tid / kWave) {
                     ib += x;
                     rb += y;
@@ -356,7 +362,7 @@ __global__ __launch_bounds__(kPlanThreads) void attn_plan_kernel(PlanIn a, PlanV
                     pv.shared[i] = u.table;
             }
         }
-        if (rows <= a.part_rows && items < (1ull << 32)) {
+        if (attempt || (rows <= a.part_rows && items < (1ull << 32))) {
             if (tid == 0) {
                 PlanHead h{};
                 h.n = b.n;
@@ -367,7 +373,7 @@ __global__ __launch_bounds__(kPlanThreads) void attn_plan_kernel(PlanIn a, PlanV
                 h.shift = b.shift;
                 h.entries = b.entries;
                 h.items = (uint32_t)items;
-                h.units = units;
+                h.head_dim = a.head_dim;
                 h.chunk = (uint32_t)chunk;
                 h.part_rows = (uint32_t)rows;
                 h.most_parts = most;
@@ -385,6 +391,7 @@ __global__ __launch_bounds__(kPlanThreads) void attn_plan_kernel(PlanIn a, PlanV
 // The pass over the keys.
 // ---------------------------------------------------------------------------
 
+typedef float v4f __attribute__((ext_vector_type(4)));
 typedef float v16f __attribute__((ext_vector_type(16)));
 typedef short v4s __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) v4s lds_v4s;
@@ -398,18 +405,29 @@ __device__ __forceinline__ v16f mfma(v8hf a, v8hf b, v16f c)
     return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0);
 }
 
+__device__ __forceinline__ v4f mfma(v8bf a, v8bf b, v4f c)
+{
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
+}
+__device__ __forceinline__ v4f mfma(v8hf a, v8hf b, v4f c)
+{
+    return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
+}
+
 // Tiles of keys in LDS: rows of D elements in 16-byte chunks, a row's chunks in
 // an order of its own, so that the 16 rows that neighbouring lanes read a
-// chunk of (K), or the four rows that they read 64 bytes of (V), lie in different
-// banks.
+// chunk of (K), the four rows that they read 64 bytes of (V of wide tiles) or the
+// eight that they read 32 bytes of (V of narrow ones) lie in different banks.
 template <int D>
 __device__ __forceinline__ uint32_t k_swizzle(uint32_t row)
 {
     return D == 64 ? (row >> 1) & 7 : row & 15;
 }
-template <int D>
+template <int D, bool WIDE = true>
 __device__ __forceinline__ uint32_t v_swizzle(uint32_t row)
 {
+    if (!WIDE)
+        return D == 64 ? ((row >> 1) & 3) << 1 : (row & 7) << 1;
     return D == 64 ? ((row >> 1) & 1) << 2 : (row & 3) << 2;
 }
 
@@ -478,6 +496,17 @@ __device__ __forceinline__ bool not_finite(v4u32 x)
     return f;
 }
 
+// The larger of a lane's value and that of the same row in the other half: the
+// upper half of one register exchanged with the lower half of another (the
+// compiler takes the two results of the instruction's builtin for one).  The
+// waits cover what the instruction needs of the vector instructions around it.
+__device__ __forceinline__ float halves_max(float x)
+{
+    float y = x;
+    asm("s_nop 1\n\tv_permlane32_swap_b32 %0, %1\n\ts_nop 1" : "+v"(x), "+v"(y));
+    return fmaxf(x, y);
+}
+
 // The running softmax of NB tiles of 32 keys: the tiles' weights in T.  limit:
 // the keys that the lane's row sees (absolute), key0: the tiles' first; masked:
 // some row does not see all of them.
@@ -487,11 +516,15 @@ __device__ __forceinline__ void weights(Row<D>& r, v16f (&s)[NB], typename Vec8<
 {
     const uint32_t half = lane_id() / 32;
     if (masked) {
+        // behind the branch: hoisted before it, as the compiler likes to, the selects
+        // of every tile were a third of the vector work
+        uint32_t first = key0 + half * 4;
+        asm volatile("" : "+v"(first));
 #pragma unroll
         for (int b = 0; b < NB; b++)
 #pragma unroll
             for (int i = 0; i < 16; i++)
-                if (key0 + b * 32 + (i / 4) * 8 + half * 4 + i % 4 >= limit)
+                if (first + b * 32 + (i / 4) * 8 + i % 4 >= limit)
                     s[b][i] = -INFINITY;
     }
     float mx = s[0][0];
@@ -500,7 +533,7 @@ __device__ __forceinline__ void weights(Row<D>& r, v16f (&s)[NB], typename Vec8<
 #pragma unroll
         for (int i = 0; i < 16; i++)
             mx = fmaxf(mx, s[b][i]);
-    mx = fmaxf(mx, __shfl_xor(mx, 32));
+    mx = halves_max(mx);
     // The maximum moves only when some row's has grown by more than 2^8 in weight:
     // weights up to 2^8 lose nothing in 32-bit sums nor, rounded, in T.
     const float grow = (mx - r.m) * scale2;
@@ -578,13 +611,15 @@ __device__ __forceinline__ void add_odd_values(Row<D>& r, const typename Vec8<T>
 }
 
 // The result of a row (o: O^T as in Row): divided by the sum, written to the
-// output or to its row of parts.
+// output or to its row of parts (rows: of the unit; rows from `end` on are not
+// the tile's).
 template <typename T, int D>
 __device__ __forceinline__ void write_row(const AttnIn& a, const Unit& u, uint32_t h, uint32_t row,
-                                          uint32_t rows, uint32_t chunk, const Row<D>& r, float l)
+                                          uint32_t end, uint32_t chunk, const Row<D>& r, float l,
+                                          uint32_t rows)
 {
     const uint32_t half = lane_id() / 32;
-    if (row >= rows)
+    if (row >= end)
         return;
     const float inv = l > 0 || l != l ? 1.0f / l : 0.0f;
     const bool seen = l > 0 || l != l;
@@ -596,7 +631,6 @@ __device__ __forceinline__ void write_row(const AttnIn& a, const Unit& u, uint32
         for (int d = 0; d < D / 32; d++)
 #pragma unroll
             for (int i = 0; i < 16; i += 4) {
-                typedef float v4f __attribute__((ext_vector_type(4)));
                 v4f x;
                 for (int k = 0; k < 4; k++)
                     x[k] = seen ? r.o[d][i + k] * inv : 0.0f;
@@ -622,313 +656,484 @@ __device__ __forceinline__ void write_row(const AttnIn& a, const Unit& u, uint32
         a.lse[(uint64_t)t * a.q_heads + x] = lse;
 }
 
-// An item's place: its unit, tile, chunk and KV head.
-struct Item {
+// Is the plan this call's?
+__device__ __forceinline__ bool plan_fits(const PlanHead& h, const AttnIn& a, uint64_t part_rows,
+                                          uint32_t head_dim)
+{
+    return h.n == a.b.n && h.groups == a.b.groups && h.q_tokens == a.b.q_tokens &&
+           h.q_heads == a.q_heads && h.kv_heads == a.kv_heads && h.shift == a.b.shift &&
+           h.entries == a.b.entries && h.head_dim == head_dim && h.part_rows <= part_rows;
+}
+
+// An item: a tile of a unit's rows, a chunk of its keys, a KV head.
+struct Tile {
     Unit u;
-    uint32_t tile, chunk, h, rows;
-    uint32_t key0, key1;  // keys of the chunk
+    uint32_t h, chunk, rows;    // rows of the unit
+    uint32_t first, last;       // the tile's rows
+    uint32_t key0, key1;        // keys that the chunk has and some row of the tile sees
+    uint32_t see_first;         // keys that the tile's first row sees, of the unit's
 };
 
-// 16 bytes of a page's row; zeros where there is no such key or page.
-struct KeyRows {
+// Keys of the unit that a row sees.
+__device__ __forceinline__ uint32_t sees(const Unit& u, uint32_t ratio, uint32_t row)
+{
+    if (!(u.flags & kUnitCausal))
+        return u.key1;
+    const int64_t n = (int64_t)u.pos0 + row / ratio + 1;
+    return n < 0 ? 0 : n > u.key1 ? u.key1 : (uint32_t)n;
+}
+
+__device__ __forceinline__ void tile_rows_are(Tile& t, uint32_t ratio, uint32_t chunk_keys, uint32_t first,
+                                              uint32_t count)
+{
+    t.first = first;
+    t.last = first + count < t.rows ? first + count - 1 : t.rows - 1;
+    t.key1 = t.u.key1 - t.key0 > chunk_keys ? t.key0 + chunk_keys : t.u.key1;
+    t.see_first = sees(t.u, ratio, t.first);
+    const uint32_t see_last = sees(t.u, ratio, t.last);
+    if (t.key1 > see_last)
+        t.key1 = see_last;
+}
+
+__device__ __forceinline__ Tile make_tile(const AttnIn& a, const Unit& u, uint32_t x, uint32_t chunk_keys,
+                                          uint32_t count)
+{
+    Tile t;
+    t.u = u;
+    t.rows = u.ntok * a.ratio;
+    const uint32_t tiles = (t.rows + count - 1) / count;
+    t.h = x % a.kv_heads;  // neighbouring workgroups, on different dies, take different heads
+    x /= a.kv_heads;
+    t.chunk = x / tiles;
+    t.key0 = u.key0 + t.chunk * chunk_keys;
+    // a sequence's last tiles see the most keys: they go first
+    tile_rows_are(t, a.ratio, chunk_keys, (tiles - 1 - x % tiles) * count, count);
+    return t;
+}
+
+// A row's query, as the right operand of K Q^T (rows past the tile's last: the
+// last one's again, not written).
+template <typename T, int D>
+__device__ __forceinline__ void load_query(const AttnIn& a, const Tile& t, uint32_t row,
+                                           typename Vec8<T>::type (&q)[D / 16])
+{
+    const uint32_t r = row < t.last ? row : t.last;
+    const uint16_t* at = a.q + (uint64_t)(t.u.tok0 + r / a.ratio) * a.q_stride +
+                         (uint64_t)(t.h * a.ratio + r % a.ratio) * D + lane_id() / 32 * 8;
+#pragma unroll
+    for (int k = 0; k < D / 16; k++)
+        q[k] = *reinterpret_cast<const typename Vec8<T>::type*>(at + k * 16);
+}
+
+template <int D>
+__device__ __forceinline__ void clear(Row<D>& r)
+{
+    r.m = -INFINITY;
+    r.l = 0;
+#pragma unroll
+    for (int d = 0; d < D / 32; d++)
+        r.o[d] = v16f{};
+}
+
+// A thread's share of the tiles of TILE keys and values that an item goes through:
+// 16-byte chunk `ch` of rows r0, r0 + STEP, ...  A tile's pages are looked up two tiles
+// ahead and its rows read one ahead; none of the reads is conditional: rows past
+// the last key read the last key's page, and their values become zeros on the
+// way to LDS.
+template <typename T, int D, int LOADS, int STEP, uint32_t TILE>
+struct Share {
+    // LANES: the waves look at tiles of their own, of which lane r knows row r's page
+    // (a register instead of one for each row that a thread reads)
+    static constexpr bool LANES = TILE < kWave;
+    v4u32 k[LOADS], v[LOADS];
+    uint32_t page[LANES ? 1 : LOADS];
     const int32_t* table;
-    uint32_t pages, key1, n_pages, shift;
-    uint64_t head_at;   // elements from a page's start to the KV head's rows
-    uint64_t page_size; // elements of a page
-    __device__ __forceinline__ int32_t page(uint32_t key) const
+    uint32_t key1, n_pages, shift, r0, ch, head_at, page_size;
+
+    __device__ __forceinline__ Share(const AttnIn& a, const Tile& t, uint32_t thread)
+        : table(a.b.page + t.u.off), key1(t.key1), n_pages(a.n_pages), shift(a.b.shift),
+          r0(thread / (D / 8)), ch(thread % (D / 8)), head_at((t.h * D << a.b.shift) + ch * 8),
+          page_size(a.kv_heads * D << a.b.shift)
     {
-        const uint32_t i = key >> shift;
-        if (key >= key1 || i >= pages)
-            return -1;
-        return table[i];
+    }
+    // r0, each time anew: what follows from it is worked out again for each tile
+    // instead of being kept in registers, of which there are none to spare
+    __device__ __forceinline__ uint32_t here() const
+    {
+        uint32_t r = r0;
+        asm volatile("" : "+v"(r));
+        return r;
+    }
+    // pages of the tile at `key` (uniform, < key1)
+    __device__ __forceinline__ void find(uint32_t key, bool& bad)
+    {
+        const uint32_t last = key1 - 1;
+        const uint32_t row = LANES ? key + lane_id() % TILE : key + here();
+#pragma unroll
+        for (int i = 0; i < (LANES ? 1 : LOADS); i++) {
+            uint32_t x = row + i * STEP;
+            if (key + TILE > key1)
+                x = x < last ? x : last;
+            const uint32_t p = (uint32_t)table[x >> shift];
+            bad |= p >= n_pages;
+            page[i] = p < n_pages ? p : 0;
+        }
+    }
+    __device__ __forceinline__ void fetch(const AttnIn& a, uint32_t key)
+    {
+        const uint32_t mask = (1u << shift) - 1;
+        const uint32_t row = key + here();
+#pragma unroll
+        for (int i = 0; i < LOADS; i++) {
+            const uint32_t p = LANES ? __shfl(page[0], r0 + i * STEP) : page[LANES ? 0 : i];
+            const uint64_t at = (uint64_t)p * page_size + (head_at + ((row + i * STEP) & mask) * D);
+            k[i] = *reinterpret_cast<const v4u32*>(a.k + at);
+            v[i] = *reinterpret_cast<const v4u32*>(a.v + at);
+            if (LANES)
+                __builtin_amdgcn_sched_barrier(0);  // an address at a time
+        }
+    }
+    // into LDS; true: values that are not finite among them (asked for where some
+    // row does not see all of the tile)
+    __device__ __forceinline__ bool stage(uint16_t* kt, uint16_t* vt, uint32_t key, bool ask)
+    {
+        bool odd = false;
+        if (ask) {
+            const uint32_t have = key1 - key;
+#pragma unroll
+            for (int i = 0; i < LOADS; i++) {
+                if (r0 + i * STEP >= have)
+                    v[i] = v4u32{};
+                odd |= not_finite<T>(v[i]);
+            }
+        }
+        const uint32_t row = LANES ? here() : r0;
+#pragma unroll
+        for (int i = 0; i < LOADS; i++) {
+            const uint32_t r = row + i * STEP;
+            *reinterpret_cast<v4u32*>(kt + r * D + (ch ^ k_swizzle<D>(r)) * 8) = k[i];
+            *reinterpret_cast<v4u32*>(vt + r * D + (ch ^ v_swizzle<D, !LANES>(r)) * 8) = v[i];
+        }
+        return odd;
     }
 };
+
+// What the waves of a narrow tile leave for one another.
+struct Joined {
+    float m[kWaves][kNarrow], l[kWaves][kNarrow];
+};
+
+// The largest of the values of a row's four lanes (16 apart), in each of them.
+__device__ __forceinline__ float quarters_max(float x)
+{
+    float y = x;
+    asm("s_nop 1\n\tv_permlane16_swap_b32 %0, %1\n\ts_nop 1" : "+v"(x), "+v"(y));
+    return halves_max(fmaxf(x, y));
+}
+
+// Four elements of a row's result, d on: to the output or to its row of parts.
+template <typename T, int D>
+__device__ __forceinline__ void write_four(const AttnIn& a, const Tile& t, uint32_t row, uint32_t d, v4f x)
+{
+    const Unit& u = t.u;
+    if (u.flags & kUnitParts) {
+        const uint64_t at = u.part0 + ((uint64_t)t.h * t.rows + row) * u.chunks + t.chunk;
+        *reinterpret_cast<v4f*>(a.part + at * D + d) = x;
+        return;
+    }
+    typedef T v4t __attribute__((ext_vector_type(4)));
+    v4t y;
+    for (int k = 0; k < 4; k++)
+        y[k] = (T)x[k];
+    *reinterpret_cast<v4t*>(a.out + (u.tok0 + row / a.ratio) * a.out_stride +
+                            (uint64_t)(t.h * a.ratio + row % a.ratio) * D + d) = y;
+}
+
+// A lane holds its row's (lane % 16) scores of 4 of 16 keys, key = h * 16 + (lane /
+// 16) * 4 + i, and of O^T the elements d = block * 16 + (lane / 16) * 4 + i.
+template <typename T, int D>
+__device__ __forceinline__ void narrow_tile(const AttnIn& a, const Tile& t, uint16_t* lds, Joined& joined,
+                                            bool& bad)
+{
+    using V = typename Vec8<T>::type;
+    constexpr int kLoads = kNarrowKeys * D / 8 / kWave;
+    constexpr uint32_t kRowChunks = D / 8, kStep = kWave / kRowChunks, kTurn = kWaves * kNarrowKeys;
+    constexpr int kBlocks = D / 16;
+    const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+    const uint32_t lane = lane_id(), row16 = lane % 16, g = lane / 16;
+    const uint32_t row = t.first + row16, in_tile = row < t.last ? row : t.last;
+    V q[D / 32];
+    {
+        const uint16_t* at = a.q + (uint64_t)(t.u.tok0 + in_tile / a.ratio) * a.q_stride +
+                             (uint64_t)(t.h * a.ratio + in_tile % a.ratio) * D + g * 8;
+#pragma unroll
+        for (int k = 0; k < D / 32; k++)
+            q[k] = *reinterpret_cast<const V*>(at + k * 32);
+    }
+    const uint32_t limit = sees(t.u, a.ratio, in_tile), end = limit < t.key1 ? limit : t.key1;
+    v4f o[kBlocks];
+    float m = -INFINITY, l = 0;
+#pragma unroll
+    for (int d = 0; d < kBlocks; d++)
+        o[d] = v4f{};
+    uint16_t* kt = lds + wave * 2 * kNarrowKeys * D;
+    uint16_t* vt = kt + kNarrowKeys * D;
+    V p;
+    // scores and weights of the tile in LDS
+    auto weigh = [&](uint32_t key, bool masked) {
+        v4f s[2];
+#pragma unroll
+        for (int h = 0; h < 2; h++) {
+            s[h] = v4f{};
+            const uint32_t r = h * 16 + row16;
+#pragma unroll
+            for (int k = 0; k < D / 32; k++)
+                s[h] = mfma(*reinterpret_cast<const V*>(kt + r * D + ((k * 4 + g) ^ k_swizzle<D>(r)) * 8), q[k],
+                            s[h]);
+        }
+        if (masked) {
+            uint32_t first = key + g * 4;
+            asm volatile("" : "+v"(first));  // as in weights()
+#pragma unroll
+            for (int i = 0; i < 8; i++)
+                if (first + (i / 4) * 16 + i % 4 >= end)
+                    s[i / 4][i % 4] = -INFINITY;
+        }
+        float mx = s[0][0];
+#pragma unroll
+        for (int i = 1; i < 8; i++)
+            mx = fmaxf(mx, s[i / 4][i % 4]);
+        mx = quarters_max(mx);
+        // as in weights()
+        if (__any(!((mx - m) * a.scale2 <= 8.0f))) {
+            const float now = fmaxf(m, mx);
+            const float keep = now == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f((m - now) * a.scale2);
+            m = now;
+            l *= keep;
+#pragma unroll
+            for (int d = 0; d < kBlocks; d++)
+                o[d] *= keep;
+        }
+        const float base = m == -INFINITY ? 0.0f : m * a.scale2;
+#pragma unroll
+        for (int i = 0; i < 8; i++) {
+            const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i / 4][i % 4], a.scale2, -base));
+            l += w;
+            p[i] = (T)w;
+        }
+    };
+    uint32_t key = t.key0 + wave * kNarrowKeys;
+    if (key < t.key1) {
+        Share<T, D, kLoads, kStep, kNarrowKeys> x(a, t, lane);
+        bool masked = false, odd = false;
+        // a wave's own part of LDS: its lanes' writes and reads in order
+        auto stage = [&](uint32_t key) {
+            masked = key + kNarrowKeys > t.see_first || key + kNarrowKeys > t.key1;
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            __builtin_amdgcn_wave_barrier();
+            odd |= x.stage(kt, vt, key, masked);
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            __builtin_amdgcn_wave_barrier();
+        };
+        x.find(key, bad);
+        x.fetch(a, key);
+        if (key + kTurn < t.key1)
+            x.find(key + kTurn, bad);
+        for (; key < t.key1; key += kTurn) {
+            stage(key);
+            if (masked && __any(odd))
+                break;
+            if (key + kTurn < t.key1)
+                x.fetch(a, key + kTurn);
+            if (key + 2 * kTurn < t.key1)
+                x.find(key + 2 * kTurn, bad);
+            weigh(key, masked);
+            // O^T += V^T P^T, keys in the order of the lane's weights
+            const uint32_t r = g * 4 + row16 / 4;
+#pragma unroll
+            for (int d = 0; d < kBlocks; d++) {
+                const uint32_t c = d * 2 + (lane % 4) / 2, e = (lane % 2) * 4;
+                const v4s v0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                    (lds_v4s*)(vt + r * D + (c ^ v_swizzle<D, false>(r)) * 8 + e));
+                const v4s v1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                    (lds_v4s*)(vt + (r + 16) * D + (c ^ v_swizzle<D, false>(r + 16)) * 8 + e));
+                typedef short v8s __attribute__((ext_vector_type(8)));
+                const v8s f = __builtin_shufflevector(v0, v1, 0, 1, 2, 3, 4, 5, 6, 7);
+                o[d] = mfma(__builtin_bit_cast(V, f), p, o[d]);
+            }
+        }
+        while (key < t.key1) {
+            // as add_odd_values()
+            weigh(key, true);
+#pragma unroll 1
+            for (uint32_t k = 0; k < kNarrowKeys; k++) {
+                float w = 0;
+#pragma unroll
+                for (int i = 0; i < 8; i++)
+                    if (k / 16 * 4 + k % 4 == (uint32_t)i)
+                        w = (float)p[i];
+                w = __shfl(w, (k % 16) / 4 * 16 + row16);
+                const bool seen = key + k < end;
+#pragma unroll
+                for (int d = 0; d < kBlocks; d++) {
+                    const uint32_t e = d * 16 + g * 4;
+                    typedef T v4t __attribute__((ext_vector_type(4)));
+                    const v4t x = *reinterpret_cast<const v4t*>(
+                        vt + k * D + ((e / 8) ^ v_swizzle<D, false>(k)) * 8 + e % 8);
+                    for (int i = 0; i < 4; i++)
+                        if (seen)
+                            o[d][i] = __builtin_fmaf(w, (float)x[i], o[d][i]);
+                }
+            }
+            key += kTurn;
+            if (key < t.key1) {
+                x.find(key, bad);
+                x.fetch(a, key);
+                stage(key);
+            }
+        }
+    }
+    // the four waves' parts joined, a quarter of the blocks by each wave
+    l += __shfl_xor(l, 16);
+    l += __shfl_xor(l, 32);
+    if (g == 0) {
+        joined.m[wave][row16] = m;
+        joined.l[wave][row16] = l;
+    }
+    v4f* sum = reinterpret_cast<v4f*>(lds);  // [wave][block][lane]
+    __syncthreads();
+    float all = -INFINITY, total = 0;
+    for (int w = 0; w < kWaves; w++)
+        all = fmaxf(all, joined.m[w][row16]);
+    for (int w = 0; w < kWaves; w++) {
+        const float mw = joined.m[w][row16], lw = joined.l[w][row16];
+        // a wave that saw nothing adds nothing, one that saw only NaN adds it
+        total += mw == -INFINITY ? (lw != lw ? lw : 0.0f) : lw * __builtin_amdgcn_exp2f((mw - all) * a.scale2);
+    }
+    const float keep = m == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f((m - all) * a.scale2);
+#pragma unroll
+    for (int d = 0; d < kBlocks; d++)
+        sum[(wave * kBlocks + d) * kWave + lane] = o[d] * keep;
+    __syncthreads();
+    const bool seen = total > 0 || total != total;
+    const float inv = seen ? 1.0f / total : 0.0f;
+#pragma unroll
+    for (int b = 0; b < kBlocks / kWaves; b++) {
+        const uint32_t d = wave * (kBlocks / kWaves) + b;
+        v4f x = {};
+        for (int w = 0; w < kWaves; w++)
+            x += sum[(w * kBlocks + d) * kWave + lane];
+        for (int k = 0; k < 4; k++)
+            x[k] = seen ? x[k] * inv : 0.0f;
+        if (row <= t.last)
+            write_four<T, D>(a, t, row, d * 16 + g * 4, x);
+    }
+    if (wave == 0 && g == 0 && row <= t.last) {
+        const float lse = seen ? (all * a.scale2 + __builtin_log2f(total)) * 0.69314718055994531f : -INFINITY;
+        if (t.u.flags & kUnitParts)
+            a.part_lse[t.u.part0 + ((uint64_t)t.h * t.rows + row) * t.u.chunks + t.chunk] = lse;
+        else if (a.lse)
+            a.lse[(uint64_t)(t.u.tok0 + row / a.ratio) * a.q_heads + t.h * a.ratio + row % a.ratio] = lse;
+    }
+}
+
+template <typename T, int D>
+__device__ __forceinline__ void wide_tile(const AttnIn& a, const Tile& t, uint16_t* lds, uint32_t* odd_tile,
+                                          bool& bad)
+{
+    constexpr int kLoads = kWideKeys * D / 8 / kThreads;
+    constexpr uint32_t kRowChunks = D / 8, kStep = kThreads / kRowChunks;
+    const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+    const uint32_t row = t.first + wave * 32 + lane_id() % 32;
+    typename Vec8<T>::type q[D / 16];
+    load_query<T, D>(a, t, row, q);
+    const uint32_t limit = sees(t.u, a.ratio, row < t.last ? row : t.last);
+    const uint32_t end = limit < t.key1 ? limit : t.key1;
+    Row<D> r;
+    clear<D>(r);
+    // keys that the wave's first and last rows see
+    const uint32_t w0 = t.first + wave * 32, w1 = w0 + 31 < t.last ? w0 + 31 : t.last;
+    const uint32_t wave_first = w0 <= t.last ? sees(t.u, a.ratio, w0) : 0;
+    const uint32_t wave_last = w0 <= t.last ? sees(t.u, a.ratio, w1) : 0;
+    auto masked = [&](uint32_t key, uint32_t first) { return key + kWideKeys > first || key + kWideKeys > t.key1; };
+    if (threadIdx.x < 2)
+        odd_tile[threadIdx.x] = 0;
+    __syncthreads();
+    uint32_t key = t.key0, buf = 0;
+    if (key < t.key1) {
+        Share<T, D, kLoads, kStep, kWideKeys> x(a, t, threadIdx.x);
+        x.find(key, bad);
+        x.fetch(a, key);
+        if (key + kWideKeys < t.key1)
+            x.find(key + kWideKeys, bad);
+        typename Vec8<T>::type p[2][2];
+        for (; key < t.key1; key += kWideKeys, buf ^= 1) {
+            uint16_t* kt = lds + buf * 2 * kWideKeys * D;
+            uint16_t* vt = kt + kWideKeys * D;
+            const bool ask = masked(key, t.see_first);
+            if (x.stage(kt, vt, key, ask))
+                odd_tile[buf] = 1;
+            __syncthreads();
+            if (ask && odd_tile[buf])
+                break;
+            if (key + kWideKeys < t.key1)
+                x.fetch(a, key + kWideKeys);
+            if (key + 2 * kWideKeys < t.key1)
+                x.find(key + 2 * kWideKeys, bad);
+            if (key < wave_last) {
+                v16f s[2] = {scores<T, D>(kt, q), scores<T, D>(kt + 32 * D, q)};
+                weights<T, D, 2>(r, s, p, key, end, masked(key, wave_first), a.scale2);
+                add_values<T, D, 2>(r, p, vt);
+            }
+        }
+        while (key < t.key1) {
+            uint16_t* kt = lds + buf * 2 * kWideKeys * D;
+            uint16_t* vt = kt + kWideKeys * D;
+            if (key < wave_last) {
+                v16f s[2] = {scores<T, D>(kt, q), scores<T, D>(kt + 32 * D, q)};
+                weights<T, D, 2>(r, s, p, key, end, true, a.scale2);
+                add_odd_values<T, D, 2>(r, p, vt, key, end);
+            }
+            key += kWideKeys;
+            if (key < t.key1) {
+                x.find(key, bad);
+                x.fetch(a, key);
+                __syncthreads();
+                x.stage(kt, vt, key, true);
+                __syncthreads();
+            }
+        }
+    }
+    write_row<T, D>(a, t.u, t.h, row, t.last + 1, t.chunk, r, r.l + __shfl_xor(r.l, 32), t.rows);
+}
 
 template <typename T, int D>
 __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attn_kernel(AttnIn a, const PlanView pv,
                                                                           uint64_t part_rows,
                                                                           uint32_t* status)
 {
-    using V = typename Vec8<T>::type;
     // two tiles of 64 keys and values, or four waves' 32 keys and values
     __shared__ __attribute__((aligned(16))) uint16_t lds[4 * kWideKeys * D];
     __shared__ uint32_t odd_tile[2];
-    __shared__ float joined[2][kWaves][kNarrow];
+    __shared__ Joined joined;
     const PlanHead& ph = *pv.head;
-    if (ph.n != a.b.n || ph.groups != a.b.groups || ph.q_tokens != a.b.q_tokens ||
-        ph.q_heads != a.q_heads || ph.kv_heads != a.kv_heads || ph.shift != a.b.shift ||
-        ph.entries != a.b.entries || ph.part_rows > part_rows || ph.items > gridDim.x) {
+    if (!plan_fits(ph, a, part_rows, D) || ph.items > gridDim.x) {
         if (blockIdx.x == 0 && threadIdx.x == 0)
             atomicOr(status, kErrInval);  // the plan of another batch
         return;
     }
-    const uint32_t items = ph.items, wave = threadIdx.x / kWave, lane = lane_id();
-    const uint32_t row32 = lane % 32, half = lane / 32;
-    const uint32_t item = blockIdx.x;
-    if (item >= items)
+    if (blockIdx.x >= ph.items)
         return;
-    {
-        const uint32_t ui = wave_find(&pv.unit[0].item0, a.b.groups + a.b.n, sizeof(Unit) / 4, item);
-        const Unit u = pv.unit[ui];
-        const uint32_t rows = u.ntok * a.ratio;
-        const bool wide = u.flags & kUnitWide;
-        const uint32_t per_tile = wide ? kWide : kNarrow, tiles = (rows + per_tile - 1) / per_tile;
-        uint32_t x = item - u.item0;
-        const uint32_t h = x % a.kv_heads;
-        x /= a.kv_heads;
-        // a sequence's last tiles see the most keys: they go first
-        const uint32_t tile = tiles - 1 - x % tiles, chunk = x / tiles;
-        const uint32_t first_row = tile * per_tile;
-        const uint32_t last_row = first_row + per_tile < rows ? first_row + per_tile - 1 : rows - 1;
-        const uint32_t key0 = u.key0 + chunk * ph.chunk;
-        uint32_t key1 = u.key1 - key0 > ph.chunk ? key0 + ph.chunk : u.key1;
-        // keys that a row sees, of the unit's
-        auto sees = [&](uint32_t row) -> uint32_t {
-            if (!(u.flags & kUnitCausal))
-                return u.key1;
-            const int64_t n = (int64_t)u.pos0 + row / a.ratio + 1;
-            return n < 0 ? 0 : n > u.key1 ? u.key1 : (uint32_t)n;
-        };
-        const uint32_t see_first = sees(first_row), see_last = sees(last_row);
-        if (key1 > see_last)
-            key1 = see_last;
-
-        const uint32_t row = first_row + (wide ? wave * 32 : 0) + row32;
-        const uint32_t limit = sees(row < rows ? row : last_row);
-        V q[D / 16];
-        {
-            const uint32_t rq = row < rows ? row : last_row;
-            const uint16_t* at = a.q + (uint64_t)(u.tok0 + rq / a.ratio) * a.q_stride +
-                                 (uint64_t)(h * a.ratio + rq % a.ratio) * D;
-#pragma unroll
-            for (int k = 0; k < D / 16; k++)
-                q[k] = *reinterpret_cast<const V*>(at + k * 16 + half * 8);
-        }
-        Row<D> r;
-        r.m = -INFINITY;
-        r.l = 0;
-#pragma unroll
-        for (int d = 0; d < D / 32; d++)
-            r.o[d] = v16f{};
-
-        KeyRows kr{a.b.page + u.off, u.table, key1, a.n_pages, a.b.shift,
-                   (uint64_t)h * D << a.b.shift, (uint64_t)a.kv_heads * D << a.b.shift};
-        const uint32_t slot_mask = (1u << a.b.shift) - 1;
-        bool bad_page = false;
-        // loads of a thread: rows r0, r0 + step, ... of a tile, chunk `ch`
-        constexpr uint32_t kRowChunks = D / 8;
-
-        if (!wide) {
-            constexpr int kLoads = kNarrowKeys * D / 8 / kWave;
-            constexpr uint32_t kStep = kWave / kRowChunks;  // rows a load of the wave covers
-            uint16_t* kt = lds + wave * 2 * kNarrowKeys * D;
-            uint16_t* vt = kt + kNarrowKeys * D;
-            const uint32_t ch = lane % kRowChunks, r0 = lane / kRowChunks;
-            v4u32 kx[kLoads], vx[kLoads];
-            auto fetch = [&](uint32_t key, int32_t page) {  // page: of row `lane`
-#pragma unroll
-                for (int i = 0; i < kLoads; i++) {
-                    const uint32_t rr = r0 + i * kStep;
-                    const int32_t p = __shfl(page, rr);
-                    kx[i] = v4u32{};
-                    vx[i] = v4u32{};
-                    if (p >= 0) {
-                        const uint64_t at = (uint64_t)p * kr.page_size + kr.head_at +
-                                            (uint64_t)((key + rr) & slot_mask) * D + ch * 8;
-                        kx[i] = *reinterpret_cast<const v4u32*>(a.k + at);
-                        vx[i] = *reinterpret_cast<const v4u32*>(a.v + at);
-                    }
-                }
-            };
-            auto page_of = [&](uint32_t key) -> int32_t {
-                int32_t p = lane < kNarrowKeys ? kr.page(key + lane) : -1;
-                if (p >= 0 && (uint32_t)p >= kr.n_pages)
-                    p = -1;
-                if (p < 0 && lane < kNarrowKeys && key + lane < key1)
-                    bad_page = true;
-                return p;
-            };
-            bool masked = false, odd = false;
-            auto stage = [&](uint32_t key) {
-                masked = key + kNarrowKeys > see_first || key + kNarrowKeys > key1;
-                __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-                __builtin_amdgcn_wave_barrier();
-#pragma unroll
-                for (int i = 0; i < kLoads; i++) {
-                    const uint32_t rr = r0 + i * kStep;
-                    *reinterpret_cast<v4u32*>(kt + rr * D + (ch ^ k_swizzle<D>(rr)) * 8) = kx[i];
-                    *reinterpret_cast<v4u32*>(vt + rr * D + (ch ^ v_swizzle<D>(rr)) * 8) = vx[i];
-                    if (masked)
-                        odd |= not_finite<T>(vx[i]);
-                }
-                __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-                __builtin_amdgcn_wave_barrier();
-            };
-            uint32_t key = key0 + wave * kNarrowKeys;
-            const uint32_t step = kWaves * kNarrowKeys, end = limit < key1 ? limit : key1;
-            V p[1][2];
-            int32_t page = page_of(key);
-            if (key < key1)
-                fetch(key, page);
-            page = page_of(key + step);
-            for (; key < key1; key += step) {
-                stage(key);
-                if (__any(odd))
-                    break;
-                if (key + step < key1)
-                    fetch(key + step, page);
-                page = page_of(key + 2 * step);
-                v16f s[1] = {scores<T, D>(kt, q)};
-                weights<T, D, 1>(r, s, p, key, end, masked, a.scale2);
-                add_values<T, D, 1>(r, p, vt);
-            }
-            while (key < key1) {
-                v16f s[1] = {scores<T, D>(kt, q)};
-                weights<T, D, 1>(r, s, p, key, end, true, a.scale2);
-                add_odd_values<T, D, 1>(r, p, vt, key, end);
-                key += step;
-                if (key < key1) {
-                    fetch(key, page_of(key));
-                    stage(key);
-                }
-            }
-            // the four waves' parts joined
-            float l = r.l + __shfl_xor(r.l, 32);
-            if (half == 0) {
-                joined[0][wave][row32] = r.m;
-                joined[1][wave][row32] = l;
-            }
-            __syncthreads();
-            float m = -INFINITY;
-            for (int w = 0; w < kWaves; w++)
-                m = fmaxf(m, joined[0][w][row32]);
-            float total = 0;
-            for (int w = 0; w < kWaves; w++) {
-                const float mw = joined[0][w][row32];
-                total += mw == -INFINITY ? (joined[1][w][row32] != joined[1][w][row32] ? joined[1][w][row32] : 0.0f)
-                                         : joined[1][w][row32] * __builtin_amdgcn_exp2f((mw - m) * a.scale2);
-            }
-            const float keep = r.m == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f((r.m - m) * a.scale2);
-            float* sum = reinterpret_cast<float*>(lds);  // [D / 4][32 rows][4] of a wave's share
-            // wave w adds the waves' parts in order, a quarter of d each turn:
-            // in turn each wave adds its own into LDS
-            for (int w = 0; w < kWaves; w++) {
-                __syncthreads();
-                if ((int)wave == w)
-#pragma unroll
-                    for (int d = 0; d < D / 32; d++)
-#pragma unroll
-                        for (int i = 0; i < 16; i++) {
-                            float* at = sum + (d * 16 + i) * kWave + lane;
-                            const float x = r.o[d][i] * keep;
-                            *at = w ? *at + x : x;
-                        }
-            }
-            __syncthreads();
-            if (wave == 0) {
-#pragma unroll
-                for (int d = 0; d < D / 32; d++)
-#pragma unroll
-                    for (int i = 0; i < 16; i++)
-                        r.o[d][i] = sum[(d * 16 + i) * kWave + lane];
-                r.m = m;
-                write_row<T, D>(a, u, h, row, rows, chunk, r, total);
-            }
-        } else {
-            constexpr int kLoads = kWideKeys * D / 8 / kThreads;
-            constexpr uint32_t kStep = kThreads / kRowChunks;
-            const uint32_t ch = threadIdx.x % kRowChunks, r0 = threadIdx.x / kRowChunks;
-            v4u32 kx[kLoads], vx[kLoads];
-            int32_t page[kLoads];
-            auto find = [&](uint32_t key) {
-#pragma unroll
-                for (int i = 0; i < kLoads; i++) {
-                    page[i] = kr.page(key + r0 + i * kStep);
-                    if (page[i] >= 0 && (uint32_t)page[i] >= kr.n_pages)
-                        page[i] = -1;
-                    if (page[i] < 0 && key + r0 + i * kStep < key1)
-                        bad_page = true;
-                }
-            };
-            auto fetch = [&](uint32_t key) {
-#pragma unroll
-                for (int i = 0; i < kLoads; i++) {
-                    kx[i] = v4u32{};
-                    vx[i] = v4u32{};
-                    if (page[i] >= 0) {
-                        const uint64_t at = (uint64_t)page[i] * kr.page_size + kr.head_at +
-                                            (uint64_t)((key + r0 + i * kStep) & slot_mask) * D + ch * 8;
-                        kx[i] = *reinterpret_cast<const v4u32*>(a.k + at);
-                        vx[i] = *reinterpret_cast<const v4u32*>(a.v + at);
-                    }
-                }
-            };
-            // keys that the wave's first and last rows see
-            const uint32_t w0 = first_row + wave * 32, w1 = w0 + 31 < last_row ? w0 + 31 : last_row;
-            const bool has_rows = w0 < rows;
-            const uint32_t wave_first = has_rows ? sees(w0) : 0, wave_last = has_rows ? sees(w1) : 0;
-            if (threadIdx.x < 2)
-                odd_tile[threadIdx.x] = 0;
-            __syncthreads();
-            find(key0);
-            fetch(key0);
-            find(key0 + kWideKeys);
-            bool odd = false;
-            auto stage = [&](uint32_t key, uint16_t* kt) {
-                uint16_t* vt = kt + kWideKeys * D;
-                const bool masked = key + kWideKeys > see_first || key + kWideKeys > key1;
-#pragma unroll
-                for (int i = 0; i < kLoads; i++) {
-                    const uint32_t rr = r0 + i * kStep;
-                    *reinterpret_cast<v4u32*>(kt + rr * D + (ch ^ k_swizzle<D>(rr)) * 8) = kx[i];
-                    *reinterpret_cast<v4u32*>(vt + rr * D + (ch ^ v_swizzle<D>(rr)) * 8) = vx[i];
-                    if (masked)
-                        odd |= not_finite<T>(vx[i]);
-                }
-            };
-            const uint32_t end = limit < key1 ? limit : key1;
-            V p[2][2];
-            uint32_t key = key0, buf = 0;
-            for (; key < key1; key += kWideKeys, buf ^= 1) {
-                uint16_t* kt = lds + buf * 2 * kWideKeys * D;
-                stage(key, kt);
-                if (odd)
-                    odd_tile[buf] = 1;
-                __syncthreads();
-                if (odd_tile[buf])
-                    break;
-                if (key + kWideKeys < key1)
-                    fetch(key + kWideKeys);
-                find(key + 2 * kWideKeys);
-                if (key < wave_last) {
-                    v16f s[2] = {scores<T, D>(kt, q), scores<T, D>(kt + 32 * D, q)};
-                    weights<T, D, 2>(r, s, p, key, end, key + kWideKeys > wave_first || key + kWideKeys > key1,
-                                     a.scale2);
-                    add_values<T, D, 2>(r, p, kt + kWideKeys * D);
-                }
-            }
-            while (key < key1) {
-                uint16_t* kt = lds + buf * 2 * kWideKeys * D;
-                if (key < wave_last) {
-                    v16f s[2] = {scores<T, D>(kt, q), scores<T, D>(kt + 32 * D, q)};
-                    weights<T, D, 2>(r, s, p, key, end, true, a.scale2);
-                    add_odd_values<T, D, 2>(r, p, kt + kWideKeys * D, key, end);
-                }
-                key += kWideKeys;
-                if (key < key1) {
-                    find(key);
-                    fetch(key);
-                    __syncthreads();
-                    stage(key, kt);
-                    __syncthreads();
-                }
-            }
-            const float l = r.l + __shfl_xor(r.l, 32);
-            write_row<T, D>(a, u, h, row, rows, chunk, r, l);
-        }
-        if (bad_page)
-            atomicOr(status, kErrInval);
-    }
+    const uint32_t ui = wave_find(&pv.unit[0].item0, a.b.groups + a.b.n, sizeof(Unit) / 4, blockIdx.x);
+    const Unit u = pv.unit[ui];
+    bool bad = false;
+    const uint32_t x = blockIdx.x - u.item0;
+    if (u.flags & kUnitWide)
+        wide_tile<T, D>(a, make_tile(a, u, x, ph.chunk, kWide), lds, odd_tile, bad);
+    else
+        narrow_tile<T, D>(a, make_tile(a, u, x, ph.chunk, kNarrow), lds, joined, bad);
+    if (bad)
+        atomicOr(status, kErrInval);
 }
 
 // ---------------------------------------------------------------------------
@@ -943,9 +1148,7 @@ __global__ __launch_bounds__(kThreads) void attn_join_kernel(AttnIn a, const Pla
     constexpr int kPer = D / kWave;  // elements a lane
     __shared__ float acc[kWaves][D];
     const PlanHead& ph = *pv.head;
-    if (ph.part_rows == 0 || ph.n != a.b.n || ph.groups != a.b.groups || ph.q_tokens != a.b.q_tokens ||
-        ph.q_heads != a.q_heads || ph.kv_heads != a.kv_heads || ph.shift != a.b.shift ||
-        ph.entries != a.b.entries || ph.part_rows > part_rows)
+    if (ph.part_rows == 0 || !plan_fits(ph, a, part_rows, D))
         return;
     const uint32_t wave = threadIdx.x / kWave, lane = lane_id();
     const bool together = ph.most_parts > 16;
@@ -1063,7 +1266,7 @@ uint64_t most_items(const dm_ctx* c, const dm_token_batch& b, uint32_t ratio, ui
 {
     const uint64_t rows = b.q_tokens * ratio;
     auto tiles = [&](uint64_t units) {
-        const uint64_t some = rows / kWide + 2 * units, few = rows / kNarrow + units;
+        const uint64_t some = rows / kWide + kNarrowRows / kNarrow * units, few = rows / kNarrow + units;
         return some < few ? some : few;
     };
     const uint64_t uncut = tiles(b.tables.n) + (b.groups ? tiles(b.groups) : 0);
@@ -1097,6 +1300,7 @@ hipError_t attn_plan(dm_ctx* c, const dm_token_batch& b, const dm_kv_pages& kv, 
     a.q_heads = q_heads;
     a.kv_heads = kv.kv_heads;
     a.ratio = q_heads / kv.kv_heads;
+    a.head_dim = kv.head_dim;
     a.target = item_target(c);
     a.part_rows = part_rows_of(c, b.q_tokens, q_heads);
     const PlanView pv = plan_view(plan, b.tables.n, b.groups);
@@ -1135,11 +1339,10 @@ hipError_t attn(dm_ctx* c, const dm_token_batch& b, const dm_kv_pages& kv, uint3
     const uint64_t most = most_items(c, b, a.ratio, kv.kv_heads);
     if (most > 0x7FFFFFFFull)
         return hipErrorInvalidValue;
-    const uint32_t grid = (uint32_t)most;
     by_type(kv.dtype, kv.head_dim, [&](auto t, auto d) {
         using T = decltype(t);
         constexpr int D = decltype(d)::value;
-        attn_kernel<T, D><<<grid, kThreads, 0, c->stream>>>(a, pv, rows, c->d_status);
+        attn_kernel<T, D><<<(uint32_t)most, kThreads, 0, c->stream>>>(a, pv, rows, c->d_status);
         attn_join_kernel<T, D><<<grid_for(b.q_tokens * q_heads, 1, 8u * c->n_cu), kThreads, 0, c->stream>>>(
             a, pv, rows);
     });
