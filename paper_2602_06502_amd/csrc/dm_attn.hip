@@ -34,8 +34,7 @@ constexpr uint32_t kNarrow = 16, kWide = 128;  // rows of a tile
 constexpr uint32_t kNarrowRows = 64;           // rows of a unit, at most, that has narrow tiles
 constexpr uint32_t kNarrowKeys = 32, kWideKeys = 64;
 constexpr uint32_t kChunk = 128;               // chunks are multiples of this many keys
-constexpr uint32_t kLeastChunk = 128;          // and no shorter than this
-constexpr int kPlanThreads = 1024;
+constexpr int kPlanThreads = 512;
 constexpr uint64_t kPartRows = 1ull << 20;     // rows of parts kept beyond those of cut items
 
 // The plan in memory: a head, then a unit for each run and each sequence
@@ -61,16 +60,22 @@ struct Unit {
     int64_t off;
     int32_t pos0;         // a sequence: position of its first new token
     uint32_t flags;
+    // of a sequence: its run's parts (chunks; 0: none), its first row among the
+    // run's, and the run's rows
+    uint32_t run_part0, run_chunks, run_row0, run_rows;
 };
 enum : uint32_t { kUnitWide = 1, kUnitCausal = 2, kUnitParts = 4 };
 
 struct PlanView {
     PlanHead* head;
     Unit* unit;
+    uint32_t* item0;   // [n + groups] the units' again, next to each other
     uint32_t* limit;   // [n] pages that s has in common with its run's first, at most
     uint32_t* run;     // [n] its run
-    uint32_t* shared;  // [groups] pages shared
-    uint32_t* gain;    // [groups] tiles of its sequences, each on its own
+    // of the runs, where they are too many for LDS: pages shared, cost of its
+    // sequences on their own (then its first row of parts)
+    uint32_t* shared;
+    uint32_t* gain;
 };
 
 __host__ __device__ inline uint64_t up16(uint64_t x) { return (x + 15) & ~15ull; }
@@ -83,6 +88,8 @@ __host__ __device__ inline PlanView plan_view(void* p, uint64_t n, uint64_t grou
     b += sizeof(PlanHead);
     v.unit = reinterpret_cast<Unit*>(b);
     b += up16(sizeof(Unit) * (n + groups));
+    v.item0 = reinterpret_cast<uint32_t*>(b);
+    b += up16(4 * (n + groups));
     v.limit = reinterpret_cast<uint32_t*>(b);
     b += up16(4 * n);
     v.run = reinterpret_cast<uint32_t*>(b);
@@ -147,55 +154,122 @@ __device__ __forceinline__ uint32_t agent_load(const uint32_t* p)
 constexpr uint32_t kNoSay = 0xFFFFFFFFu;
 constexpr uint32_t kLdsRuns = 1024;
 
-// How many leading pages sequence s could share with its run's first one, by
-// the whole workgroup (kNoSay: it has no row that sees a key).  A shared prefix
-// ends before the first new token of every sequence that has any.
-__device__ void common_pages(const PlanIn& a, const PlanView& pv, uint32_t s, uint32_t* least)
+// The run that sequence s is in, [g0, g1), and whether there is one.
+struct RunOf {
+    uint32_t g;
+    int64_t g0, g1;
+    bool ok;
+};
+__device__ __forceinline__ RunOf run_of(const TokenBatch& b, uint32_t s)
+{
+    RunOf r;
+    if (b.groups < kWave) {  // all bounds by one read
+        const int64_t at = b.group_off[lane_id() < b.groups ? lane_id() : b.groups];
+        const uint32_t k = __popcll(ballot(lane_id() < b.groups && at <= (int64_t)s));
+        r.g = k ? k - 1 : 0;
+        r.g0 = (int64_t)shfl_u64((uint64_t)at, r.g);
+        r.g1 = (int64_t)shfl_u64((uint64_t)at, r.g + 1);
+    } else {
+        r.g = wave_find(b.group_off, b.groups, 1, (int64_t)s);
+        r.g0 = b.group_off[r.g];
+        r.g1 = b.group_off[r.g + 1];
+    }
+    r.ok = r.g0 >= 0 && r.g1 <= (int64_t)b.n && r.g0 <= (int64_t)s && (int64_t)s < r.g1;
+    return r;
+}
+
+// How many leading pages sequence s could share with its run's first one (kNoSay:
+// it has no row that sees a key).  A shared prefix ends before the first new
+// token of every sequence that has any.  By the whole workgroup (least: a word
+// of LDS), or by a wave (least null).
+__device__ __forceinline__ void common_pages(const PlanIn& a, const PlanView& pv, uint32_t s, uint32_t* least)
 {
     const TokenBatch& b = a.b;
-    const uint32_t g = wave_find(b.group_off, b.groups, 1, (int64_t)s);
-    const int64_t g0 = b.group_off[g];
-    const bool mine = run_ok(b, g) && g0 <= (int64_t)s && (int64_t)s < b.group_off[g + 1];
     const SeqView v = sequence_view(b, s);
+    const RunOf r = run_of(b, s);
     uint32_t limit = 0;
-    if (mine && (v.ntok == 0 || (!v.bad && v.len == 0))) {
+    if (r.ok && (v.ntok == 0 || (!v.bad && v.len == 0))) {
         limit = kNoSay;
-    } else if (mine && !v.bad && v.pos0 > 0) {
-        const SeqView f = sequence_view(b, (uint32_t)g0);
-        int64_t m = v.pos0 >> b.shift;
-        const int64_t have = f.bad ? 0 : b.off[g0 + 1] - f.off;
-        if (have < m)
-            m = have;
-        limit = (uint32_t)m;
-        __syncthreads();
-        if (threadIdx.x == 0)
-            *least = limit;
-        __syncthreads();
-        for (uint32_t i = threadIdx.x; i < limit; i += kPlanThreads)
-            if (b.page[v.off + i] != b.page[f.off + i]) {
-                atomicMin(least, i);
-                break;
+    } else if (r.ok && !v.bad && v.pos0 > 0) {
+        // the first one's entries, and that they are there, are what is needed
+        const int64_t f0 = b.off[r.g0], f1 = b.off[r.g0 + 1];
+        const int64_t have = f0 < 0 || f1 < f0 || f1 > b.entries ? 0 : f1 - f0, own = v.pos0 >> b.shift;
+        limit = (uint32_t)(have < own ? have : own);
+        const int32_t *mine = b.page + v.off, *theirs = b.page + f0;
+        if (least) {
+            __syncthreads();
+            if (threadIdx.x == 0)
+                *least = limit;
+            __syncthreads();
+            for (uint32_t i = threadIdx.x; i < limit; i += kPlanThreads)
+                if (mine[i] != theirs[i]) {
+                    atomicMin(least, i);
+                    break;
+                }
+            __syncthreads();
+            limit = *least;
+        } else {
+            constexpr uint32_t kAt = 4;  // reads of a lane at once
+            for (uint32_t i0 = 0; i0 < limit; i0 += kAt * kWave) {
+                uint32_t x[kAt], y[kAt], first = limit;
+#pragma unroll
+                for (uint32_t k = 0; k < kAt; k++) {
+                    const uint32_t i = i0 + k * kWave + lane_id();
+                    x[k] = i < limit ? mine[i] : 0;
+                    y[k] = i < limit ? theirs[i] : 0;
+                }
+#pragma unroll
+                for (uint32_t k = 0; k < kAt; k++) {
+                    const uint64_t differ = ballot(x[k] != y[k]);
+                    if (differ) {
+                        const uint32_t at = i0 + k * kWave + (uint32_t)__builtin_ctzll(differ);
+                        first = at < first ? at : first;
+                    }
+                }
+                limit = first;
             }
-        __syncthreads();
-        limit = *least;
+        }
     }
-    if (threadIdx.x == 0) {
+    if (least ? threadIdx.x == 0 : lane_id() == 0) {
         agent_store(&pv.limit[s], limit);
-        agent_store(&pv.run[s], mine ? g : kNoSay);
+        agent_store(&pv.run[s], r.ok ? r.g : kNoSay);
     }
 }
 
-// The units of run g over its shared pages, and of sequence s.
-__device__ __forceinline__ Unit run_unit(const PlanIn& a, uint32_t g, uint32_t pages)
+// Sequences up to this many have a workgroup each, more a wave each: workgroups
+// that arrive at one counter take 11 ns each.
+constexpr uint32_t kPlanWorkgroups = 64;
+
+// What the plan's last workgroup reads of a run, and of a sequence.
+struct RunView {
+    uint32_t tok0, ntok;
+    int64_t off;
+    bool ok;
+};
+__device__ __forceinline__ RunView run_view(const TokenBatch& b, uint32_t g)
+{
+    RunView r{0, 0, 0, false};
+    const int64_t g0 = b.group_off[g], g1 = b.group_off[g + 1];
+    if (g0 < 0 || g1 < g0 || g1 > (int64_t)b.n || g0 >= (int64_t)b.n)
+        return r;
+    const int64_t t0 = b.q_off[g0], t1 = b.q_off[g1];
+    r.off = b.off[g0];
+    r.ok = t0 >= 0 && t1 >= t0 && t1 <= (int64_t)b.q_tokens;
+    r.tok0 = r.ok ? (uint32_t)t0 : 0;
+    r.ntok = r.ok ? (uint32_t)(t1 - t0) : 0;
+    return r;
+}
+
+// The units of a run over its shared pages, and of a sequence.
+__device__ __forceinline__ Unit run_unit(const PlanIn& a, const RunView& r, uint32_t pages)
 {
     Unit u{};
     if (pages == 0)
         return u;
-    const int64_t s0 = a.b.group_off[g], s1 = a.b.group_off[g + 1];
-    u.tok0 = (uint32_t)a.b.q_off[s0];
-    u.ntok = (uint32_t)a.b.q_off[s1] - u.tok0;
+    u.tok0 = r.tok0;
+    u.ntok = r.ntok;
     u.key1 = pages << a.b.shift;
-    u.off = a.b.off[s0];
+    u.off = r.off;
     u.table = pages;
     u.flags = kUnitParts | tile_flags((uint64_t)u.ntok * a.ratio);
     return u;
@@ -215,33 +289,38 @@ __device__ __forceinline__ Unit sequence_unit(const PlanIn& a, const SeqView& v,
     return u;
 }
 
-// Is a pass of its own over `pages` common pages worth it for run g?  Where the
+// Is a pass of its own over `pages` common pages worth it for a run?  Where the
 // run's rows together make clearly fewer tiles, over more than a chunk of keys.
-__device__ __forceinline__ bool worth_sharing(const PlanIn& a, uint32_t g, uint32_t pages, uint64_t gain)
+__device__ __forceinline__ bool worth_sharing(const PlanIn& a, const RunView& r, uint32_t pages, uint32_t gain)
 {
-    if (pages == 0 || pages == kNoSay || !run_ok(a.b, g) || ((uint64_t)pages << a.b.shift) < kChunk)
-        return false;
-    const int64_t t0 = a.b.q_off[a.b.group_off[g]], t1 = a.b.q_off[a.b.group_off[g + 1]];
-    return t0 >= 0 && t1 >= t0 && t1 <= (int64_t)a.b.q_tokens &&
-           2 * gain >= 3 * weight_of((uint64_t)(t1 - t0) * a.ratio);
+    return pages != 0 && pages != kNoSay && r.ok && ((uint64_t)pages << a.b.shift) >= kChunk &&
+           2 * (uint64_t)gain >= 3 * weight_of((uint64_t)r.ntok * a.ratio);
 }
 
 // Which runs share their prefixes, the chunk, and the units' items.  With
 // runs, a workgroup for a sequence first, and the last one to finish goes on
-// alone (a launch less).  A thread keeps its first unit in registers from step to
-// step, and those past the first 1024 in the plan.
+// alone (a launch less).  Its threads read what they need of their first unit
+// once and keep it; beyond 512 units the others are read again, and kept in the
+// plan between the steps.
 __global__ __launch_bounds__(kPlanThreads) void attn_plan_kernel(PlanIn a, PlanView pv, uint32_t* status)
 {
     __shared__ uint64_t lds[2 * kPlanThreads / kWave];
-    __shared__ uint32_t run_pages[kLdsRuns], run_gain[kLdsRuns];
+    __shared__ uint32_t run_pages[kLdsRuns], run_gain[kLdsRuns], run_tok0[kLdsRuns], run_ntok[kLdsRuns];
     __shared__ uint32_t most, least;
     const TokenBatch& b = a.b;
     const uint32_t units = b.groups + b.n, tid = threadIdx.x;
     if (b.groups) {
-        for (uint32_t s = blockIdx.x; s < b.n; s += gridDim.x)
-            common_pages(a, pv, s, &least);
-        // thread 0 wrote the workgroup's words: its fence alone orders them (one by
+        constexpr uint32_t kPlanWaves = kPlanThreads / kWave;
+        if (b.n <= kPlanWorkgroups)
+            for (uint32_t s = blockIdx.x; s < b.n; s += gridDim.x)
+                common_pages(a, pv, s, &least);
+        else
+            for (uint32_t s = blockIdx.x * kPlanWaves + tid / kWave; s < b.n; s += gridDim.x * kPlanWaves)
+                common_pages(a, pv, s, nullptr);
+        // the words are written through and have arrived when the barrier lets the
+        // waves go; one fence orders them for what thread 0 does next (one by
         // every wave of 256 workgroups took 60 us)
+        __syncthreads();
         if (tid == 0) {
             __builtin_amdgcn_fence(__ATOMIC_RELEASE, "agent");
             least = atomicAdd(a.arrived, 1u);
@@ -261,6 +340,21 @@ __global__ __launch_bounds__(kPlanThreads) void attn_plan_kernel(PlanIn a, PlanV
             __threadfence();
         __syncthreads();
     };
+    // the thread's first unit: a run, or a sequence with its run and common pages
+    const bool is_run = tid < b.groups;
+    const uint32_t s0 = tid - b.groups;
+    RunView rv{0, 0, 0, false};
+    SeqView sv{0, 0, 0, 0, 0, false};
+    uint32_t run = kNoSay, limit = kNoSay;
+    if (is_run) {
+        rv = run_view(b, tid);
+    } else if (tid < units) {
+        sv = sequence_view(b, s0);
+        if (b.groups) {
+            run = agent_load(&pv.run[s0]);
+            limit = agent_load(&pv.limit[s0]);
+        }
+    }
     if (b.groups) {
         for (uint32_t g = tid; g < b.groups; g += kPlanThreads) {
             pages[g] = kNoSay;
@@ -269,38 +363,48 @@ __global__ __launch_bounds__(kPlanThreads) void attn_plan_kernel(PlanIn a, PlanV
                    (g + 1 == b.groups && b.group_off[b.groups] != (int64_t)b.n);
         }
         settle();
-        for (uint32_t s = tid; s < b.n; s += kPlanThreads) {
-            const uint32_t g = agent_load(&pv.run[s]), limit = agent_load(&pv.limit[s]);
-            const SeqView v = sequence_view(b, s);
+        for (uint32_t i = tid; i < units; i += kPlanThreads) {
+            if (i < b.groups)
+                continue;
+            const uint32_t s = i - b.groups;
+            const uint32_t g = i == tid ? run : agent_load(&pv.run[s]);
+            const SeqView v = i == tid ? sv : sequence_view(b, s);
             if (g >= b.groups)
                 continue;
-            atomicMin(&pages[g], limit);
+            atomicMin(&pages[g], i == tid ? limit : agent_load(&pv.limit[s]));
             if (v.len)
                 atomicAdd(&gain[g], (uint32_t)weight_of((uint64_t)v.ntok * a.ratio));
         }
         settle();
-        for (uint32_t g = tid; g < b.groups; g += kPlanThreads)
-            pages[g] = worth_sharing(a, g, pages[g], gain[g]) ? pages[g] : 0;
+        for (uint32_t g = tid; g < b.groups; g += kPlanThreads) {
+            const RunView r = g == tid ? rv : run_view(b, g);
+            pages[g] = worth_sharing(a, r, pages[g], gain[g]) ? pages[g] : 0;
+            if (b.groups <= kLdsRuns) {
+                run_tok0[g] = r.tok0;
+                run_ntok[g] = r.ntok;
+            }
+        }
         settle();
     }
     // 0: as wanted; 1: without sharing and without cuts, if the parts of the
     // first try have no room
     for (int attempt = 0; attempt < 2; attempt++) {
-        auto make = [&](uint32_t i) -> Unit {
-            if (i < b.groups)
-                return run_unit(a, i, attempt ? 0 : pages[i]);
-            const uint32_t s = i - b.groups, g = b.groups ? agent_load(&pv.run[s]) : kNoSay;
-            const SeqView v = sequence_view(b, s);
-            bad |= v.bad;
-            return sequence_unit(a, v, attempt || g >= b.groups ? 0 : pages[g]);
-        };
         auto cost_of = [&](const Unit& u) -> uint64_t {
             return u.ntok ? weight_of((uint64_t)u.ntok * a.ratio) * (u.key1 - u.key0) : 0;
         };
         Unit mine{};
         uint64_t cost = 0;
         for (uint32_t i = tid; i < units; i += kPlanThreads) {
-            const Unit u = make(i);
+            Unit u{};
+            if (i < b.groups) {
+                u = run_unit(a, i == tid ? rv : run_view(b, i), attempt ? 0 : pages[i]);
+            } else {
+                const uint32_t s = i - b.groups;
+                const uint32_t g = i == tid || !b.groups ? run : agent_load(&pv.run[s]);
+                const SeqView v = i == tid ? sv : sequence_view(b, s);
+                bad |= v.bad;
+                u = sequence_unit(a, v, attempt || g >= b.groups ? 0 : pages[g]);
+            }
             cost += cost_of(u);
             if (i == tid)
                 mine = u;
@@ -309,8 +413,6 @@ __global__ __launch_bounds__(kPlanThreads) void attn_plan_kernel(PlanIn a, PlanV
         }
         cost = block_sum64(cost, lds) * a.kv_heads;
         uint64_t chunk = (cost / a.target + kChunk) / kChunk * kChunk;
-        if (chunk < kLeastChunk)
-            chunk = kLeastChunk;
         if (attempt || chunk > 0x80000000ull)
             chunk = 0x80000000ull;
         // items and rows of parts before each unit
@@ -354,12 +456,35 @@ __global__ __launch_bounds__(kPlanThreads) void attn_plan_kernel(PlanIn a, PlanV
                 items += x;
                 rows += y;
             }
+            u.item0 = (uint32_t)(ib + i1 - it);
+            u.part0 = (uint32_t)(rb + r1 - rw);
+            if (i < b.groups)
+                gain[i] = u.part0;  // for the run's sequences, which come later
+            if (b.groups)
+                settle();
+            if (i < units && i >= b.groups) {
+                const uint32_t s = i - b.groups;
+                const uint32_t g = u0 == 0 || !b.groups ? run : agent_load(&pv.run[s]);
+                if (!attempt && g < b.groups && pages[g]) {
+                    RunView r{0, 0, 0, true};
+                    if (b.groups <= kLdsRuns) {
+                        r.tok0 = run_tok0[g];
+                        r.ntok = run_ntok[g];
+                    } else {
+                        r = run_view(b, g);
+                    }
+                    // sequences that are not among their run's tokens: q_off is out of order
+                    const bool in = u.tok0 >= r.tok0 && u.tok0 - r.tok0 <= r.ntok && u.ntok <= r.ntok - (u.tok0 - r.tok0);
+                    bad |= !in;
+                    u.run_part0 = gain[g];
+                    u.run_chunks = in ? (uint32_t)((((uint64_t)pages[g] << b.shift) + chunk - 1) / chunk) : 0;
+                    u.run_row0 = (u.tok0 - r.tok0) * a.ratio;
+                    u.run_rows = r.ntok * a.ratio;
+                }
+            }
             if (i < units) {
-                u.item0 = (uint32_t)(ib + i1 - it);
-                u.part0 = (uint32_t)(rb + r1 - rw);
                 pv.unit[i] = u;
-                if (i < b.groups)
-                    pv.shared[i] = u.table;
+                pv.item0[i] = u.item0;
             }
         }
         if (attempt || (rows <= a.part_rows && items < (1ull << 32))) {
@@ -654,6 +779,23 @@ __device__ __forceinline__ void write_row(const AttnIn& a, const Unit& u, uint32
         }
     if (half == 0 && a.lse)
         a.lse[(uint64_t)t * a.q_heads + x] = lse;
+}
+
+// The last unit with item0 <= item, up to 512 units by one wait.
+__device__ __forceinline__ uint32_t find_unit(const uint32_t* item0, uint32_t units, uint32_t item)
+{
+    if (units > 8 * kWave)
+        return wave_find(item0, units, 1, item);
+    uint32_t x[8], k = 0;
+#pragma unroll
+    for (uint32_t i = 0; i < 8; i++) {
+        const uint32_t u = i * kWave + lane_id();
+        x[i] = u < units ? item0[u] : 0xFFFFFFFFu;
+    }
+#pragma unroll
+    for (uint32_t i = 0; i < 8; i++)
+        k += __popcll(ballot(x[i] <= item));
+    return k ? k - 1 : 0;
 }
 
 // Is the plan this call's?
@@ -1117,6 +1259,7 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attn_kernel(AttnIn
     __shared__ uint32_t odd_tile[2];
     __shared__ Joined joined;
     const PlanHead& ph = *pv.head;
+    const uint32_t ui = find_unit(pv.item0, a.b.groups + a.b.n, blockIdx.x);  // beside the head's reads
     if (!plan_fits(ph, a, part_rows, D) || ph.items > gridDim.x) {
         if (blockIdx.x == 0 && threadIdx.x == 0)
             atomicOr(status, kErrInval);  // the plan of another batch
@@ -1124,7 +1267,6 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attn_kernel(AttnIn
     }
     if (blockIdx.x >= ph.items)
         return;
-    const uint32_t ui = wave_find(&pv.unit[0].item0, a.b.groups + a.b.n, sizeof(Unit) / 4, blockIdx.x);
     const Unit u = pv.unit[ui];
     bool bad = false;
     const uint32_t x = blockIdx.x - u.item0;
@@ -1161,7 +1303,6 @@ __global__ __launch_bounds__(kThreads) void attn_join_kernel(AttnIn a, const Pla
         const uint32_t s = sequence_of(a.b, t), h = x / a.ratio;
         const Unit u = pv.unit[a.b.groups + s];
         const bool live = mine && t - u.tok0 < u.ntok && (u.flags & kUnitParts);
-        const uint32_t run = a.b.groups && live ? pv.run[s] : 0xFFFFFFFFu;
         // the row's parts: its run's chunks, then its own
         uint32_t n0 = 0, n1 = 0;
         uint64_t at0 = 0, at1 = 0;
@@ -1170,10 +1311,9 @@ __global__ __launch_bounds__(kThreads) void attn_join_kernel(AttnIn a, const Pla
             n1 = u.chunks;
             at1 = u.part0 + ((uint64_t)h * u.ntok * a.ratio + row) * n1;
             // a token before its sequence's first key sees no prefix either
-            if (run < a.b.groups && pv.shared[run] && (int64_t)u.pos0 + (t - u.tok0) >= 0) {
-                const Unit g = pv.unit[run];
-                n0 = g.chunks;
-                at0 = g.part0 + ((uint64_t)h * g.ntok * a.ratio + (t - g.tok0) * a.ratio + x % a.ratio) * n0;
+            if ((int64_t)u.pos0 + (t - u.tok0) >= 0) {
+                n0 = u.run_chunks;
+                at0 = u.run_part0 + ((uint64_t)h * u.run_rows + u.run_row0 + row) * n0;
             }
         }
         const uint32_t n = n0 + n1;
@@ -1289,7 +1429,8 @@ uint64_t part_rows_of(const dm_ctx* c, uint64_t q_tokens, uint32_t q_heads)
 
 uint64_t attn_plan_bytes(uint64_t n, uint64_t groups)
 {
-    return sizeof(PlanHead) + up16(sizeof(Unit) * (n + groups)) + 2 * up16(4 * n) + 2 * up16(4 * groups);
+    return sizeof(PlanHead) + up16(sizeof(Unit) * (n + groups)) + up16(4 * (n + groups)) + 2 * up16(4 * n) +
+           2 * up16(4 * groups);
 }
 
 hipError_t attn_plan(dm_ctx* c, const dm_token_batch& b, const dm_kv_pages& kv, uint32_t q_heads,
@@ -1305,8 +1446,10 @@ hipError_t attn_plan(dm_ctx* c, const dm_token_batch& b, const dm_kv_pages& kv, 
     a.part_rows = part_rows_of(c, b.q_tokens, q_heads);
     const PlanView pv = plan_view(plan, b.tables.n, b.groups);
     a.arrived = c->d_status + 48;  // a line of its own
-    attn_plan_kernel<<<b.groups ? grid_for(b.tables.n, 1, 2u * c->n_cu) : 1, kPlanThreads, 0, c->stream>>>(
-        a, pv, c->d_status);
+    const uint32_t grid = !b.groups                        ? 1
+                          : b.tables.n <= kPlanWorkgroups ? (uint32_t)b.tables.n
+                                                          : grid_for(b.tables.n, kPlanThreads / kWave, c->n_cu);
+    attn_plan_kernel<<<grid, kPlanThreads, 0, c->stream>>>(a, pv, c->d_status);
     return hipGetLastError();
 }
 
