@@ -634,10 +634,12 @@ __device__ __forceinline__ float halves_max(float x)
 
 // The running softmax of NB tiles of 32 keys: the tiles' weights in T.  limit:
 // the keys that the lane's row sees (absolute), key0: the tiles' first; masked:
-// some row does not see all of them.
-template <typename T, int D, int NB>
+// some row does not see all of them; beside(): what can be done meanwhile, when
+// s has been read (it may be written anew).
+template <typename T, int D, int NB, typename Beside>
 __device__ __forceinline__ void weights(Row<D>& r, v16f (&s)[NB], typename Vec8<T>::type (&p)[NB][2],
-                                        uint32_t key0, uint32_t limit, bool masked, float scale2)
+                                        uint32_t key0, uint32_t limit, bool masked, float scale2,
+                                        Beside&& beside)
 {
     const uint32_t half = lane_id() / 32;
     if (masked) {
@@ -674,12 +676,14 @@ __device__ __forceinline__ void weights(Row<D>& r, v16f (&s)[NB], typename Vec8<
                 r.o[d][i] *= keep;
     }
     const float base = r.m == -INFINITY ? 0.0f : r.m * scale2;
+    const v16f now[NB] = {s[0], s[NB - 1]};
+    beside();
     float sum = 0;
 #pragma unroll
     for (int b = 0; b < NB; b++)
 #pragma unroll
         for (int i = 0; i < 16; i++) {
-            const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(s[b][i], scale2, -base));
+            const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(now[b][i], scale2, -base));
             sum += w;
             p[b][i / 8][i % 8] = (T)w;
         }
@@ -1179,15 +1183,96 @@ __device__ __forceinline__ void narrow_tile(const AttnIn& a, const Tile& t, uint
     }
 }
 
+// A wide tile's keys and values go from memory to LDS without registers: 16 bytes a
+// lane, a wave's 1024 bytes next to each other in LDS, each lane reading the chunk
+// that belongs there.  The compiler does not know of these writes: wait_sent()
+// and a barrier come between them and their readers.
+__device__ __forceinline__ void send16(const uint16_t* from, uint32_t lds_at)
+{
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off"
+                 :
+                 : "s"(lds_at), "v"(from)
+                 : "memory");
+}
+__device__ __forceinline__ void wait_sent() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+
+// Byte address of a place in LDS.
+__device__ __forceinline__ uint32_t lds_address(const uint16_t* p)
+{
+    return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const uint16_t*)p;
+}
+
+// A thread's share of wide tiles: LDS chunk threadIdx.x + i * 256, that is row r0 +
+// i * kStep, place `ch` of the row.
+template <typename T, int D>
+struct Sender {
+    static constexpr int kLoads = kWideKeys * D / 8 / kThreads;
+    static constexpr uint32_t kRowChunks = D / 8, kStep = kThreads / kRowChunks;
+    const uint16_t *k, *v;  // the layer's pages, at the KV head
+    const int32_t* table;
+    uint32_t key1, n_pages, shift, page_size, r0, ch, wave_at;
+
+    __device__ __forceinline__ Sender(const AttnIn& a, const Tile& t, uint32_t wave)
+        : k(a.k + ((uint64_t)t.h * D << a.b.shift)), v(a.v + ((uint64_t)t.h * D << a.b.shift)),
+          table(a.b.page + t.u.off), key1(t.key1), n_pages(a.n_pages), shift(a.b.shift),
+          page_size(a.kv_heads * D << a.b.shift), r0(threadIdx.x / kRowChunks), ch(threadIdx.x % kRowChunks),
+          wave_at(wave * kWave * 16)
+    {
+    }
+    // pages of the tile at `key` (uniform, < key1); rows past the last key: the
+    // last key's
+    __device__ __forceinline__ void find(uint32_t key, uint32_t (&page)[kLoads], bool& bad) const
+    {
+        const uint32_t last = key + kWideKeys > key1 ? key1 - 1 : 0xFFFFFFFFu;
+#pragma unroll
+        for (int i = 0; i < kLoads; i++) {
+            const uint32_t x = key + r0 + i * kStep;
+            const uint32_t p = *reinterpret_cast<const uint32_t*>(reinterpret_cast<const uint8_t*>(table) +
+                                                                  (((x < last ? x : last) >> shift) << 2));
+            bad |= p >= n_pages;
+            page[i] = p < n_pages ? p : 0;
+        }
+    }
+    __device__ __forceinline__ void send(const uint16_t* base, bool values, uint32_t key,
+                                         const uint32_t (&page)[kLoads], const uint16_t* to) const
+    {
+        const uint32_t mask = (1u << shift) - 1, at = lds_address(to) + wave_at;
+#pragma unroll
+        for (int i = 0; i < kLoads; i++) {
+            const uint32_t r = r0 + i * kStep;
+            const uint32_t c = ch ^ (values ? v_swizzle<D>(r) : k_swizzle<D>(r));
+            send16(base + (uint64_t)page[i] * page_size + (((key + r) & mask) * D + c * 8),
+                   __builtin_amdgcn_readfirstlane(at + i * kThreads * 16));
+        }
+    }
+    // A tile of values of which some row does not see all: zeros for the places past
+    // the last key; true: values that are not finite among the others.
+    __device__ __forceinline__ bool clean(uint16_t* vt, uint32_t key) const
+    {
+        bool odd = false;
+#pragma unroll
+        for (int i = 0; i < kLoads; i++) {
+            v4u32* at = reinterpret_cast<v4u32*>(vt + (r0 + i * kStep) * D + ch * 8);
+            if (key + r0 + i * kStep >= key1)
+                *at = v4u32{};
+            else
+                odd |= not_finite<T>(*at);
+        }
+        return odd;
+    }
+};
+
+// Tile by tile, the next one's scores are taken beside this one's weights: the
+// matrix unit has work that does not wait for them.  K of tile t + 2 and V of
+// tile t + 1 are on their way meanwhile, to where K of tile t and V of tile t - 1
+// were.
 template <typename T, int D>
 __device__ __forceinline__ void wide_tile(const AttnIn& a, const Tile& t, uint16_t* lds, uint32_t* odd_tile,
                                           bool& bad)
 {
-    constexpr int kLoads = kWideKeys * D / 8 / kThreads;
-    constexpr uint32_t kRowChunks = D / 8, kStep = kThreads / kRowChunks;
     const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
     const uint32_t row = t.first + wave * 32 + lane_id() % 32;
-    typename Vec8<T>::type q[D / 16];
+    typename Vec8<T>::type q[D / 16], p[2][2];
     load_query<T, D>(a, t, row, q);
     const uint32_t limit = sees(t.u, a.ratio, row < t.last ? row : t.last);
     const uint32_t end = limit < t.key1 ? limit : t.key1;
@@ -1198,52 +1283,82 @@ __device__ __forceinline__ void wide_tile(const AttnIn& a, const Tile& t, uint16
     const uint32_t wave_first = w0 <= t.last ? sees(t.u, a.ratio, w0) : 0;
     const uint32_t wave_last = w0 <= t.last ? sees(t.u, a.ratio, w1) : 0;
     auto masked = [&](uint32_t key, uint32_t first) { return key + kWideKeys > first || key + kWideKeys > t.key1; };
-    if (threadIdx.x < 2)
-        odd_tile[threadIdx.x] = 0;
-    __syncthreads();
-    uint32_t key = t.key0, buf = 0;
-    if (key < t.key1) {
-        Share<T, D, kLoads, kStep, kWideKeys> x(a, t, threadIdx.x);
-        x.find(key, bad);
-        x.fetch(a, key);
-        if (key + kWideKeys < t.key1)
-            x.find(key + kWideKeys, bad);
-        typename Vec8<T>::type p[2][2];
-        for (; key < t.key1; key += kWideKeys, buf ^= 1) {
-            uint16_t* kt = lds + buf * 2 * kWideKeys * D;
-            uint16_t* vt = kt + kWideKeys * D;
-            const bool ask = masked(key, t.see_first);
-            if (x.stage(kt, vt, key, ask))
-                odd_tile[buf] = 1;
-            __syncthreads();
-            if (ask && odd_tile[buf])
-                break;
-            if (key + kWideKeys < t.key1)
-                x.fetch(a, key + kWideKeys);
-            if (key + 2 * kWideKeys < t.key1)
-                x.find(key + 2 * kWideKeys, bad);
-            if (key < wave_last) {
-                v16f s[2] = {scores<T, D>(kt, q), scores<T, D>(kt + 32 * D, q)};
-                weights<T, D, 2>(r, s, p, key, end, masked(key, wave_first), a.scale2);
-                add_values<T, D, 2>(r, p, vt);
-            }
+    constexpr uint32_t kTile = kWideKeys * D;
+    uint16_t* vts = lds + 2 * kTile;  // two tiles of keys, then two of values
+    if (t.key0 < t.key1) {
+        const Sender<T, D> x(a, t, wave);
+        uint32_t p1[Sender<T, D>::kLoads], p2[Sender<T, D>::kLoads];  // pages of the next tile, and the one after
+        if (threadIdx.x == 0)
+            *odd_tile = 0;
+        x.find(t.key0, p2, bad);
+        x.send(x.k, false, t.key0, p2, lds);
+        x.send(x.v, true, t.key0, p2, vts);
+        if (t.key0 + kWideKeys < t.key1) {
+            x.find(t.key0 + kWideKeys, p1, bad);
+            x.send(x.k, false, t.key0 + kWideKeys, p1, lds + kTile);
         }
-        while (key < t.key1) {
-            uint16_t* kt = lds + buf * 2 * kWideKeys * D;
-            uint16_t* vt = kt + kWideKeys * D;
+        if (t.key0 + 2 * kWideKeys < t.key1)
+            x.find(t.key0 + 2 * kWideKeys, p2, bad);
+        wait_sent();
+        __syncthreads();
+        v16f s[2] = {scores<T, D>(lds, q), scores<T, D>(lds + 32 * D, q)};
+        uint32_t key = t.key0, buf = 0;
+        bool odd = false;
+        while (true) {
+            // K of the next tile and V of this one are there; everyone is done with
+            // K of this tile and V of the one before
+            if (masked(key, t.see_first)) {
+                if (x.clean(vts + buf * kTile, key))
+                    *odd_tile = 1;
+                __syncthreads();
+                odd = *odd_tile;
+                if (odd)
+                    break;
+            }
+            const uint32_t key1 = key + kWideKeys, key2 = key1 + kWideKeys;
+            if (key2 < t.key1)
+                x.send(x.k, false, key2, p2, lds + buf * kTile);
+            if (key1 < t.key1) {
+                x.send(x.v, true, key1, p1, vts + (buf ^ 1) * kTile);
+#pragma unroll
+                for (int i = 0; i < Sender<T, D>::kLoads; i++)
+                    p1[i] = p2[i];
+            }
+            if (key2 + kWideKeys < t.key1)
+                x.find(key2 + kWideKeys, p2, bad);
             if (key < wave_last) {
-                v16f s[2] = {scores<T, D>(kt, q), scores<T, D>(kt + 32 * D, q)};
-                weights<T, D, 2>(r, s, p, key, end, true, a.scale2);
-                add_odd_values<T, D, 2>(r, p, vt, key, end);
+                weights<T, D, 2>(r, s, p, key, end, masked(key, wave_first), a.scale2, [&] {
+                    // (of the last tile: of what is there, and not used)
+                    s[0] = scores<T, D>(lds + (buf ^ 1) * kTile, q);
+                    s[1] = scores<T, D>(lds + (buf ^ 1) * kTile + 32 * D, q);
+                });
+                add_values<T, D, 2>(r, p, vts + buf * kTile);
+            }
+            key = key1;
+            buf ^= 1;
+            if (key >= t.key1)
+                break;
+            wait_sent();
+            __syncthreads();
+        }
+        while (key < t.key1) {  // rare: values that are not finite
+            if (key < wave_last) {
+                weights<T, D, 2>(r, s, p, key, end, true, a.scale2, [] {});
+                add_odd_values<T, D, 2>(r, p, vts + buf * kTile, key, end);
             }
             key += kWideKeys;
-            if (key < t.key1) {
-                x.find(key, bad);
-                x.fetch(a, key);
-                __syncthreads();
-                x.stage(kt, vt, key, true);
-                __syncthreads();
-            }
+            if (key >= t.key1)
+                break;
+            __syncthreads();
+            x.find(key, p1, bad);
+            x.send(x.k, false, key, p1, lds + buf * kTile);
+            x.send(x.v, true, key, p1, vts + buf * kTile);
+            wait_sent();
+            __syncthreads();
+            x.clean(vts + buf * kTile, key);
+            __syncthreads();
+            s[0] = scores<T, D>(lds + buf * kTile, q);
+            s[1] = scores<T, D>(lds + buf * kTile + 32 * D, q);
         }
     }
     write_row<T, D>(a, t.u, t.h, row, t.last + 1, t.chunk, r, r.l + __shfl_xor(r.l, 32), t.rows);
@@ -1256,7 +1371,7 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attn_kernel(AttnIn
 {
     // two tiles of 64 keys and values, or four waves' 32 keys and values
     __shared__ __attribute__((aligned(16))) uint16_t lds[4 * kWideKeys * D];
-    __shared__ uint32_t odd_tile[2];
+    __shared__ uint32_t odd_tile;
     __shared__ Joined joined;
     const PlanHead& ph = *pv.head;
     const uint32_t ui = find_unit(pv.item0, a.b.groups + a.b.n, blockIdx.x);  // beside the head's reads
@@ -1271,7 +1386,7 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attn_kernel(AttnIn
     bool bad = false;
     const uint32_t x = blockIdx.x - u.item0;
     if (u.flags & kUnitWide)
-        wide_tile<T, D>(a, make_tile(a, u, x, ph.chunk, kWide), lds, odd_tile, bad);
+        wide_tile<T, D>(a, make_tile(a, u, x, ph.chunk, kWide), lds, &odd_tile, bad);
     else
         narrow_tile<T, D>(a, make_tile(a, u, x, ph.chunk, kNarrow), lds, joined, bad);
     if (bad)
