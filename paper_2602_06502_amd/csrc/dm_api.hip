@@ -984,6 +984,8 @@ dm_status dm_attn_plan(dm_ctx* c, const dm_token_batch* batch, const dm_kv_pages
         return s;
     if (dm_status s = heads_check(c, kv, q_heads, "dm_attn_plan"); s != DM_OK)
         return s;
+    if (batch->q_tokens * q_heads >= (1ull << 31))
+        return fail(c, DM_EINVAL, "dm_attn_plan: q_tokens * q_heads must be below 2^31");
     if (!plan || !aligned16(plan) || plan_bytes < attn_plan_bytes(batch->tables.n, batch->groups))
         return fail(c, DM_EINVAL, "dm_attn_plan: plan is null, misaligned or smaller than "
                                   "dm_attn_plan_bytes");

@@ -1511,8 +1511,10 @@ __global__ __launch_bounds__(kThreads) void attn_join_kernel(AttnIn a, const Pla
     }
 }
 
-// Items wanted: four for each place of a workgroup (two a compute unit).
-uint64_t item_target(const dm_ctx* c) { return 8ull * c->n_cu; }
+// Items wanted: two for each place of a workgroup (two a compute unit).  (Half as
+// many: 64 decode rows of up to 8,192 keys 236 us instead of 219; twice as many:
+// 256 rows on 8 shared prefixes 205 instead of 194.)
+uint64_t item_target(const dm_ctx* c) { return 4ull * c->n_cu; }
 
 // Items that a plan can have: the tiles of its units (a unit of more than 64
 // rows has wide ones), and what cuts add: at most the items wanted, and no more

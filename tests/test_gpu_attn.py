@@ -209,6 +209,82 @@ def test_runs_that_have_nothing_in_common():
     b.check()
 
 
+@pytest.mark.parametrize("n,runs", [(70, 3), (200, 100), (600, 5), (1300, 1100)])
+def test_many_sequences_and_runs(n, runs):
+    """More sequences than have a workgroup each in the plan, more units than it has threads, more runs than fit its LDS."""
+    _say("many", n, runs)
+    r = np.random.default_rng(n)
+    run = np.sort(np.concatenate([np.arange(runs), r.integers(0, runs, size=n - runs)]))
+    seqs = [(int(r.integers(1, 3)), int(r.integers(2, 40)), int(g)) for g in run]
+    Batch(8, seqs, prefixes=[int(8 * r.integers(0, 30)) for _ in range(runs)], heads=(2, 1), dim=64, seed=n).check()
+
+
+def test_rows_around_tiles():
+    """Rows of a unit around a narrow tile, the last narrow unit and a wide tile."""
+    for ratio in (1, 3, 8):
+        rows = sorted({x // ratio for x in (15, 16, 17, 32, 47, 48, 63, 64, 65, 66, 127, 128, 129, 256, 257)} - {0})
+        _say("rows", ratio, rows)
+        Batch(16, [(t, t + 90) for t in rows], heads=(ratio, 1), dim=64, seed=ratio).check()
+
+
+def test_plan_and_attention_in_a_graph():
+    """Captured, replayed with other lengths, tables and queries, each replay equal to the eager result's bits."""
+    pk, _ = engine(16)
+    st = torch.cuda.Stream()
+    e = pk.DualMap(dict(block=16, key_blocks=1, seeds=(1, 2), vnodes=1, max_slots=1, index_log2_slots=4), stream=st)
+    sets = [Batch(16, [(1, 30 + 7 * i, 0), (1, 50, 0), (2, 9 + i, 0), (40, 60, 0), (1, 200 + i, 1), (1, 1, 1)],
+                  prefixes=(256, 320), seed=30 + i, spare=9 - i) for i in range(3)]
+    T = int(sets[0].q_off[-1])
+    most = max(len(b.page) for b in sets)
+    pages = max(b.k.shape[1] for b in sets)
+    k = torch.zeros((1, pages) + tuple(sets[0].k.shape[2:]), dtype=torch.bfloat16, device="cuda")
+    v = torch.zeros_like(k)
+    kv = pk.KVPages(k, v)
+    i64 = dict(dtype=torch.int64, device="cuda")
+    off, page, length = torch.zeros(7, **i64), torch.zeros(most, dtype=torch.int32, device="cuda"), torch.zeros(6, **i64)
+    q_off, grp = torch.zeros(7, **i64), torch.zeros(3, **i64)
+    q = torch.zeros((T, 8, 128), dtype=torch.bfloat16, device="cuda")
+    out, lse = torch.zeros_like(q), torch.zeros((T, 8), device="cuda")
+
+    def fill(b):
+        off.copy_(torch.from_numpy(b.off))
+        page[:len(b.page)].copy_(torch.from_numpy(b.page))
+        length.copy_(torch.from_numpy(b.len))
+        q_off.copy_(torch.from_numpy(b.q_off))
+        grp.copy_(torch.from_numpy(b.groups))
+        q.copy_(b.qrows.unflatten(1, (8, 128)))
+        k[:, :b.k.shape[1]].copy_(b.k)
+        v[:, :b.v.shape[1]].copy_(b.v)
+        torch.cuda.synchronize()
+
+    def call():
+        e.attn(e.attn_plan(kv, (off, page, length), q_off, T, 8, groups=grp), 0, q, 128 ** -0.5, out, lse)
+
+    fill(sets[0])
+    with torch.cuda.stream(st):
+        call()
+    st.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=st):
+        call()
+    for i in (1, 2, 0, 1):
+        fill(sets[i])
+        out.fill_(5)
+        lse.fill_(5)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        got = out.clone(), lse.clone()
+        with torch.cuda.stream(st):
+            call()
+        st.synchronize()
+        assert torch.equal(got[0].view(torch.int16), out.view(torch.int16)) and torch.equal(got[1], lse)
+        ref, rl, tol, ltol = sets[i].reference()
+        assert bool(((out.cpu().double() - ref).abs() <= tol).all())
+    e.sync()
+    e.close()
+
+
 def test_idle_places_and_empty_rows():
     """Length 0 with a new token (an idle place), no new token, fewer keys than new tokens: empty rows are zeros
     and -infinity, with and without runs."""
