@@ -1302,6 +1302,7 @@ __device__ __forceinline__ void wide_tile(const AttnIn& a, const Tile& t, uint16
         wait_sent();
         __syncthreads();
         v16f s[2] = {scores<T, D>(lds, q), scores<T, D>(lds + 32 * D, q)};
+        __syncthreads();  // the third tile's keys go where the first's are
         uint32_t key = t.key0, buf = 0;
         bool odd = false;
         while (true) {

@@ -219,6 +219,26 @@ def test_many_sequences_and_runs(n, runs):
     Batch(8, seqs, prefixes=[int(8 * r.integers(0, 30)) for _ in range(runs)], heads=(2, 1), dim=64, seed=n).check()
 
 
+@pytest.mark.parametrize("tokens,keys,dim", [(96, 1500, 128), (200, 700, 64), (1, 3000, 128), (130, 900, 256)])
+def test_same_bits_with_a_full_gpu(tokens, keys, dim):
+    """A full GPU's worth of items, twelve times: nothing in a result goes by which wave or workgroup comes first."""
+    _say("again", tokens, keys, dim)
+    b = Batch(16, [(tokens, keys + 37 * i) for i in range(64)], heads=(16, 4), dim=dim, seed=3)
+    pk, e = engine(16)
+    kv = pk.KVPages(b.k.cuda(), b.v.cuda())
+    t = tuple(torch.from_numpy(x).cuda() for x in (b.off, b.page, b.len))
+    q_off, T = torch.from_numpy(b.q_off).cuda(), int(b.q_off[-1])
+    q = b.qrows.unflatten(1, (16, dim)).contiguous().cuda()
+    first = None
+    for _ in range(12):
+        out, lse = torch.full_like(q, 7), torch.full((T, 16), 7.0, device="cuda")
+        e.attn(e.attn_plan(kv, t, q_off, T, 16), 0, q, dim ** -0.5, out, lse)
+        e.sync()
+        if first is None:
+            first = out, lse
+        assert torch.equal(out.view(torch.int16), first[0].view(torch.int16)) and torch.equal(lse, first[1])
+
+
 def test_rows_around_tiles():
     """Rows of a unit around a narrow tile, the last narrow unit and a wide tile."""
     for ratio in (1, 3, 8):
