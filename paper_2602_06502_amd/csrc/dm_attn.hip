@@ -31,9 +31,13 @@ namespace {
 
 constexpr int kThreads = 256, kWaves = 4;
 constexpr uint32_t kNarrow = 16, kWide = 128;  // rows of a tile
-constexpr uint32_t kNarrowRows = 64;           // rows of a unit, at most, that has narrow tiles
+// Rows of a unit, at most, that has narrow tiles.  (32 sequences of 4,096 keys, 32
+// query and 8 key heads of 128: 24 rows 104 us in a wide tile, 119 in two narrow
+// ones; 64 rows 110 and 170.  64 sequences of up to 8,192 keys, 4 rows: 219 narrow,
+// 244 wide.)
+constexpr uint32_t kNarrowRows = 16;
 constexpr uint32_t kNarrowKeys = 32, kWideKeys = 64;
-constexpr uint32_t kChunk = 128;               // chunks are multiples of this many keys
+constexpr uint32_t kChunk = 128;               // keys of a chunk, at least (of the longest: a multiple)
 constexpr int kPlanThreads = 512;
 constexpr uint64_t kPartRows = 1ull << 20;     // rows of parts kept beyond those of cut items
 
@@ -44,11 +48,10 @@ struct PlanHead {
     uint32_t n, groups, q_tokens, q_heads, kv_heads, shift;  // what it was made for
     int64_t entries;
     uint32_t items;
-    uint32_t chunk;       // keys of a chunk
     uint32_t part_rows;   // rows of parts
     uint32_t most_parts;  // of a row
     uint32_t head_dim;
-    uint32_t pad[3];
+    uint32_t pad[4];
 };
 struct Unit {
     uint32_t item0;       // items before this unit
@@ -100,8 +103,8 @@ __host__ __device__ inline PlanView plan_view(void* p, uint64_t n, uint64_t grou
     return v;
 }
 
-// The tiles of a unit, by its rows, and their cost a key: a wide one reads as
-// much as a narrow one and takes about twice its time.
+// The tiles of a unit, by its rows, and their cost a key: a wide one takes up to
+// twice a narrow one's time.
 __device__ __forceinline__ uint32_t tile_rows(uint64_t rows) { return rows <= kNarrowRows ? kNarrow : kWide; }
 __device__ __forceinline__ uint32_t tile_flags(uint64_t rows) { return tile_rows(rows) == kWide ? kUnitWide : 0; }
 __device__ __forceinline__ uint64_t tiles_of(uint64_t rows)
@@ -499,7 +502,6 @@ __global__ __launch_bounds__(kPlanThreads) void attn_plan_kernel(PlanIn a, PlanV
                 h.entries = b.entries;
                 h.items = (uint32_t)items;
                 h.head_dim = a.head_dim;
-                h.chunk = (uint32_t)chunk;
                 h.part_rows = (uint32_t)rows;
                 h.most_parts = most;
                 *pv.head = h;
@@ -841,8 +843,7 @@ __device__ __forceinline__ void tile_rows_are(Tile& t, uint32_t ratio, uint32_t 
         t.key1 = see_last;
 }
 
-__device__ __forceinline__ Tile make_tile(const AttnIn& a, const Unit& u, uint32_t x, uint32_t chunk_keys,
-                                          uint32_t count)
+__device__ __forceinline__ Tile make_tile(const AttnIn& a, const Unit& u, uint32_t x, uint32_t count)
 {
     Tile t;
     t.u = u;
@@ -851,6 +852,9 @@ __device__ __forceinline__ Tile make_tile(const AttnIn& a, const Unit& u, uint32
     t.h = x % a.kv_heads;  // neighbouring workgroups, on different dies, take different heads
     x /= a.kv_heads;
     t.chunk = x / tiles;
+    // chunks of one length, none empty: the last of a unit ends no sooner than the others
+    const uint32_t chunk_keys =
+        ((u.key1 - u.key0 + u.chunks - 1) / u.chunks + kWideKeys - 1) / kWideKeys * kWideKeys;
     t.key0 = u.key0 + t.chunk * chunk_keys;
     // a sequence's last tiles see the most keys: they go first
     tile_rows_are(t, a.ratio, chunk_keys, (tiles - 1 - x % tiles) * count, count);
@@ -1387,9 +1391,9 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attn_kernel(AttnIn
     bool bad = false;
     const uint32_t x = blockIdx.x - u.item0;
     if (u.flags & kUnitWide)
-        wide_tile<T, D>(a, make_tile(a, u, x, ph.chunk, kWide), lds, &odd_tile, bad);
+        wide_tile<T, D>(a, make_tile(a, u, x, kWide), lds, &odd_tile, bad);
     else
-        narrow_tile<T, D>(a, make_tile(a, u, x, ph.chunk, kNarrow), lds, joined, bad);
+        narrow_tile<T, D>(a, make_tile(a, u, x, kNarrow), lds, joined, bad);
     if (bad)
         atomicOr(status, kErrInval);
 }
@@ -1436,36 +1440,51 @@ __global__ __launch_bounds__(kThreads) void attn_join_kernel(AttnIn a, const Pla
         auto place = [&](uint32_t i) { return i < n0 ? at0 + i : at1 + (i - n0); };
         // the parts' weights, a lane each; then their rows, whose loads need not
         // wait for one another
-        float m = -INFINITY;
-        for (uint32_t i = lane; i < n; i += kWave)
-            m = fmaxf(m, a.part_lse[place(i)]);
+        const uint32_t from = together ? wave * kWave : 0, by = together ? kWaves * kWave : kWave;
+        float four[4][kPer];
+        auto read_four = [&](uint32_t i) {
+#pragma unroll
+            for (uint32_t j = 0; j < 4; j++) {
+                const float* at = a.part + place(i + j < n ? i + j : n - 1) * D + lane * kPer;
+#pragma unroll
+                for (int c = 0; c < kPer; c++)
+                    four[j][c] = at[c];
+            }
+        };
+        float m = -INFINITY, e0 = -INFINITY;
+        if (n) {
+            if (from + lane < n)
+                e0 = a.part_lse[place(from + lane)];
+            read_four(from);  // beside the weights' reads
+        }
+        if (together)
+            for (uint32_t i = lane; i < n; i += kWave)
+                m = fmaxf(m, a.part_lse[place(i)]);
+        else
+            m = e0;
 #pragma unroll
         for (int o = 1; o < kWave; o *= 2)
             m = fmaxf(m, __shfl_xor(m, o));
         float v[kPer] = {}, total = 0;
-        const uint32_t from = together ? wave * kWave : 0, by = together ? kWaves * kWave : kWave;
         for (uint32_t i0 = from; i0 < n; i0 += by) {
             const uint32_t i = i0 + lane;
-            const float e = i < n ? a.part_lse[place(i)] : -INFINITY;
+            const float e = i0 == from ? e0 : i < n ? a.part_lse[place(i)] : -INFINITY;
             // a part that the row sees nothing of has no weight; NaN stays NaN
             const float w = e == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f((e - m) * 1.44269504088896341f);
             total += w;
             const uint32_t k1 = n - i0 < kWave ? n - i0 : kWave;
             for (uint32_t k = 0; k < k1; k += 4) {
-                float x[4], y[4][kPer];
+                float x[4];
+                if (i0 != from || k)
+                    read_four(i0 + k);
 #pragma unroll
-                for (int j = 0; j < 4; j++) {
+                for (int j = 0; j < 4; j++)
                     x[j] = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, w), k + j));
-                    const float* at = a.part + place(i0 + (k + j < k1 ? k + j : k1 - 1)) * D + lane * kPer;
-#pragma unroll
-                    for (int c = 0; c < kPer; c++)
-                        y[j][c] = at[c];
-                }
 #pragma unroll
                 for (int j = 0; j < 4; j++)
 #pragma unroll
                     for (int c = 0; c < kPer; c++)
-                        v[c] = x[j] == 0 ? v[c] : __builtin_fmaf(x[j], y[j][c], v[c]);
+                        v[c] = x[j] == 0 ? v[c] : __builtin_fmaf(x[j], four[j][c], v[c]);
             }
         }
 #pragma unroll
@@ -1512,10 +1531,10 @@ __global__ __launch_bounds__(kThreads) void attn_join_kernel(AttnIn a, const Pla
     }
 }
 
-// Items wanted: two for each place of a workgroup (two a compute unit).  (Half as
-// many: 64 decode rows of up to 8,192 keys 236 us instead of 219; twice as many:
-// 256 rows on 8 shared prefixes 205 instead of 194.)
-uint64_t item_target(const dm_ctx* c) { return 4ull * c->n_cu; }
+// Items wanted: three for every two places of a workgroup (two a compute unit).
+// (64 decode rows of up to 8,192 keys, 256 rows on 8 shared prefixes: 218 and 190
+// us; with one for each place 229 and 196, with three 217 and 196.)
+uint64_t item_target(const dm_ctx* c) { return 3ull * c->n_cu; }
 
 // Items that a plan can have: the tiles of its units (a unit of more than 64
 // rows has wide ones), and what cuts add: at most the items wanted, and no more
