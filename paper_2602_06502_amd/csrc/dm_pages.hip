@@ -496,7 +496,7 @@ __global__ __launch_bounds__(kThreads) void fork_write_kernel(ForkIn a, Work w, 
 
 // ---------------------------------------------------------------------------
 // A small call in one workgroup: the same passes, what they share in LDS.  (24
-// sequences over 900 pages: 9 us, the passes above 24.)
+// sequences over 767 pages: 10 us, the passes above 24.)
 // ---------------------------------------------------------------------------
 
 constexpr uint32_t kSmallPages = 8192, kSmallRows = 1024;
