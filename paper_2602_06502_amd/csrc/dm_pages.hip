@@ -24,9 +24,12 @@ constexpr uint32_t kNone = 0xFFFFFFFFu;
 constexpr uint32_t kBadBlock = 1u << 31;   // of a page block's count: a negative reference count
 constexpr int64_t kMaxLen = 1ll << 31;     // sequences are shorter
 
-// ctl words: what a call has found wrong, then what its scan has found.
+// ctl words: what a call has found wrong, then what its scan has found.  What the
+// count pass finds has a word of its own: waves of one workgroup that read a word
+// while others set it could go different ways, past barriers and each other's
+// counts.
 enum : int { kCtlErr = 0, kCtlNeed = 1, kCtlMoves = 2, kCtlLive = 3, kCtlBelow = 4, kCtlTurn = 5,
-             kCtlWords = 8 };
+             kCtlCountErr = 6, kCtlWords = 8 };
 
 // Work arrays of a call.
 struct Work {
@@ -335,7 +338,7 @@ __global__ __launch_bounds__(kThreads) void fork_count_kernel(ForkIn a, Work w, 
         }
     }
     if (bad)
-        atomicOr(&w.ctl[kCtlErr], kErrInval);
+        atomicOr(&w.ctl[kCtlCountErr], kErrInval);
 }
 
 __device__ __forceinline__ void agent_store(uint32_t* p, uint32_t x)
@@ -356,7 +359,7 @@ __global__ __launch_bounds__(kPlanThreads) void fork_scan_kernel(ForkIn a, Work 
 {
     __shared__ uint64_t lds[3 * kPlanThreads / kWave];
     __shared__ uint32_t turn;
-    const uint32_t err = w.ctl[kCtlErr], free_pages = w.ctl[kCtlLive];
+    const uint32_t err = w.ctl[kCtlErr] | w.ctl[kCtlCountErr], free_pages = w.ctl[kCtlLive];
     constexpr uint32_t kCopies = 1u << 31;  // of base: the sequence copies a page
     for (uint64_t x = (uint64_t)blockIdx.x * kPlanThreads + threadIdx.x; err == 0 && x < a.m;
          x += (uint64_t)gridDim.x * kPlanThreads) {

@@ -273,6 +273,44 @@ def test_compact_errors_write_nothing():
     attempt(pk.DM_EFULL, [0, 2], [2, 3], [0, 0, 1, 1], moves=1)
 
 
+@pytest.mark.parametrize("where", [0, 0.5, 1])
+@pytest.mark.parametrize("what", ["page past the pool", "negative page", "page without a reference", "negative count"])
+def test_errors_in_large_calls_write_nothing(what, where):
+    """One fault among many pages and entries, in the first, a middle or the last of them."""
+    print("[case] large errors", what, where, flush=True)
+    pk, e = engine(16)
+    r = np.random.default_rng(41)
+    n, pages = 1200, 40_000
+    tables, lens, ref = make(r, 16, n, pages - 3000, 24)
+    ref = np.concatenate([ref, np.zeros(3000, np.int64)])
+    off, page = csr(tables)
+    entry = int(where * (len(page) - 1))
+    if what == "page past the pool":
+        page[entry] = pages
+    elif what == "negative page":
+        page[entry] = -1
+    elif what == "page without a reference":
+        ref[page[entry]] = 0
+    else:
+        ref[int(where * (pages - 1))] = -1
+    t = (dev(off, np.int64), dev(page, np.int32), dev(lens, np.int64))
+    src = np.arange(n)
+    for compact in (False, True):
+        out = e.alloc_pages_out(pages, n, len(page) + 2 * n)
+        for x in out.values():
+            x.fill_(-7)
+        if compact:
+            e.pages_compact_into(t, dev(ref, np.int32), out)
+        else:
+            e.pages_fork_into(t, dev(ref, np.int32), dev(src, np.int32), dev(np.array(lens) // 2, np.int64),
+                              dev(np.full(n, 9), np.int64), out)
+        with pytest.raises(pk.DMError) as x:
+            e.sync()
+        assert x.value.status == pk.DM_EINVAL
+        assert out.pop("moves").item() == 0
+        assert all(bool((v == -7).all()) for v in out.values())
+
+
 @pytest.mark.parametrize("B,heads,dim,layers,dtype", [(4, 1, 64, 1, "f16"), (16, 2, 64, 3, "bf16"), (32, 8, 128, 2, "bf16"),
                                                       (64, 3, 256, 2, "f16"), (16, 5, 128, 1, "bf16")])
 def test_copy(B, heads, dim, layers, dtype):
