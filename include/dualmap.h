@@ -446,8 +446,8 @@ typedef enum { DM_BF16 = 0, DM_F16 = 1 } dm_dtype;
 /* A store of pages: keys at k and values at v, each [layers][n_pages]
  * [kv_heads][B][head_dim] elements of dtype with layer_stride elements from a
  * layer to the next; 16-byte aligned, head_dim 64, 128 or 256, layer_stride a
- * multiple of 8 and at least n_pages * kv_heads * B * head_dim, n_pages <
- * 2^31. */
+ * multiple of 8 and at least n_pages * kv_heads * B * head_dim, 1 <= n_pages
+ * < 2^31. */
 typedef struct {
     void* k;
     void* v;

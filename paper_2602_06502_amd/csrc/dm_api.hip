@@ -811,9 +811,9 @@ static dm_status kv_pages_check(dm_ctx* c, const dm_kv_pages* kv, uint32_t layer
         return fail(c, DM_EINVAL, what + ": null pages");
     if (kv->reserved || (kv->dtype != DM_BF16 && kv->dtype != DM_F16) ||
         (kv->head_dim != 64 && kv->head_dim != 128 && kv->head_dim != 256) || kv->kv_heads < 1 ||
-        kv->kv_heads > 4096 || kv->n_pages >= (1u << 31))
+        kv->kv_heads > 4096 || kv->n_pages < 1 || kv->n_pages >= (1u << 31))
         return fail(c, DM_EINVAL, what + ": unsupported pages (bf16 or f16, head_dim 64, 128 or 256, "
-                                         "1 to 4096 KV heads, n_pages < 2^31)");
+                                         "1 to 4096 KV heads, 1 <= n_pages < 2^31)");
     if (!data)
         return DM_OK;
     const uint64_t size = (uint64_t)kv->n_pages * kv->kv_heads * c->cfg.block_size * kv->head_dim;

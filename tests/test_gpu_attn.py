@@ -505,3 +505,18 @@ def test_pages_past_32_bits():
     assert bool(((out.cpu().double() - ref).abs() <= tol).all())
     del k, v, kv
     torch.cuda.empty_cache()
+
+
+def test_store_without_pages_is_refused():
+    """Through the C entry: a store of no pages has no place that a row could be read from."""
+    pk, e = engine(16)
+    b = Batch(16, [(1, 40), (2, 30)], seed=19)
+    kv = pk.KVPages(b.k.cuda(), b.v.cuda())
+    q = torch.zeros((3, 8, 128), dtype=torch.bfloat16, device="cuda")
+    plan = e.attn_plan(kv, b.tables(), b.dev(b.q_off), 3, 8)
+    kv.struct.n_pages = 0
+    with pytest.raises(pk.DMError, match="n_pages"):
+        e.attn(plan, 0, q, 0.1, torch.empty_like(q))
+    kv.struct.n_pages = kv.pages
+    e.attn(plan, 0, q, 0.1, torch.empty_like(q))
+    e.sync()
