@@ -649,7 +649,8 @@ class DualMap:
             raise ValueError("q_off needs one entry more than len")
         if groups is None:
             return tb + (q_off.data_ptr(), q_tokens, 0, 0)
-        self._dev(groups, i64, "groups")
+        if self._dev(groups, i64, "groups").numel() < 1:
+            raise ValueError("groups needs one entry more than there are runs")
         return tb + (q_off.data_ptr(), q_tokens, groups.data_ptr(), groups.numel() - 1)
 
     def _rows(self, x, name, heads, dim, tokens, dtype):

@@ -520,3 +520,12 @@ def test_store_without_pages_is_refused():
     kv.struct.n_pages = kv.pages
     e.attn(plan, 0, q, 0.1, torch.empty_like(q))
     e.sync()
+
+
+def test_runs_without_bounds_are_refused():
+    pk, e = engine(16)
+    b = Batch(16, [(1, 40), (2, 30)], seed=19)
+    kv = pk.KVPages(b.k.cuda(), b.v.cuda())
+    with pytest.raises(ValueError, match="groups"):
+        e.attn_plan(kv, b.tables(), b.dev(b.q_off), 3, 8, groups=torch.zeros(0, dtype=torch.int64, device="cuda"))
+    e.sync()
