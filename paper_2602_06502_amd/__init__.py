@@ -700,7 +700,13 @@ class DualMap:
         self._kv(kv)
         b = self._batch(tables, q_off, q_tokens, groups)
         need = self.lib.dm_attn_plan_bytes(b[3], b[8])
-        buf = self.torch.empty(need, dtype=self.torch.uint8, device=self.device)
+        # of the context's stream, whose work is all that the memory has to outlive
+        torch = self.torch
+        if torch.cuda.current_stream(self._index) == self.stream:
+            buf = torch.empty(need, dtype=torch.uint8, device=self.device)
+        else:
+            with torch.cuda.stream(self.stream):
+                buf = torch.empty(need, dtype=torch.uint8, device=self.device)
         batch = _PACK_BATCH(*b)
         self._check(self.lib.dm_attn_plan(self._h, batch, kv._ref, q_heads, buf.data_ptr(), need),
                     "dm_attn_plan")

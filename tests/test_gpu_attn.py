@@ -388,6 +388,24 @@ def test_another_stream():
     e.close()
 
 
+def test_plan_memory_goes_by_the_contexts_stream():
+    """A plan that is dropped while its context's stream may still read it does not become another stream's tensor."""
+    pk, _ = engine(16)
+    st = torch.cuda.Stream()
+    e = pk.DualMap(dict(block=16, key_blocks=1, seeds=(1, 2), vnodes=1, max_slots=1, index_log2_slots=4), stream=st)
+    b = Batch(16, [(1, 300), (70, 128)], seed=17)
+    kv = pk.KVPages(b.k.cuda(), b.v.cuda())
+    tb, qo = b.tables(), b.dev(b.q_off)
+    torch.cuda.synchronize()
+    plan = e.attn_plan(kv, tb, qo, 71, 8)
+    at, size = plan.buf.data_ptr(), plan.buf.numel()
+    del plan
+    others = [torch.empty(size, dtype=torch.uint8, device="cuda") for _ in range(64)]
+    assert all(x.data_ptr() != at for x in others)
+    e.sync()
+    e.close()
+
+
 def test_same_bits_every_time():
     """No order of atomics changes a result."""
     b = Batch(16, [(1, 3000, 0), (1, 200, 0), (2, 100, 0), (1, 1, 0), (1, 50, 0)], prefixes=(2048,), seed=18)
