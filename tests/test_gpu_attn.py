@@ -547,3 +547,14 @@ def test_runs_without_bounds_are_refused():
     with pytest.raises(ValueError, match="groups"):
         e.attn_plan(kv, b.tables(), b.dev(b.q_off), 3, 8, groups=torch.zeros(0, dtype=torch.int64, device="cuda"))
     e.sync()
+
+
+@pytest.mark.parametrize("prefix", [0, 768])
+@pytest.mark.parametrize("dtype,dim,heads", [("bf16", 64, (96, 96)), ("f16", 128, (96, 48)), ("bf16", 256, (64, 64))])
+def test_many_rows_in_parts(dtype, dim, heads, prefix):
+    """More rows in parts than the join has waves: of a run and of cut sequences, some that see nothing, some in one part."""
+    seqs = [(9, 3400, 0), (3, 1, 0), (90, 300, 0), (33, 96, 1), (14, 0, 1), (20, 3100, 1), (1, 33, 1)]
+    b = Batch(16, seqs if prefix else [s[:2] for s in seqs], prefixes=(prefix, prefix) if prefix else (), heads=heads, dim=dim,
+              dtype=dtype, seed=43)
+    _say("many rows", dtype, dim, heads, prefix)
+    b.check()
