@@ -224,6 +224,13 @@ class AttnPlan:
         self._keep = keep  # the batch's tensors
 
 
+def _current_stream(index):
+    """The current stream's handle, by torch's short way where it has one."""
+    import torch
+    raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+    return raw(index) if raw else torch.cuda.current_stream(index).cuda_stream
+
+
 class DualMap:
     """A routing engine context on one GPU (torch tensors in and out)."""
 
@@ -239,6 +246,7 @@ class DualMap:
         self.block = cfg["block"]
         with torch.cuda.device(self.device):
             self.stream = stream if stream is not None else torch.cuda.current_stream(self.device)
+            self._raw_stream = self.stream.cuda_stream
             h = C.c_void_p()
             st = self.lib.dm_create(C.byref(make_config(cfg)), C.c_void_p(self.stream.cuda_stream),
                                     C.byref(h))
@@ -702,7 +710,7 @@ class DualMap:
         need = self.lib.dm_attn_plan_bytes(b[3], b[8])
         # of the context's stream, whose work is all that the memory has to outlive
         torch = self.torch
-        if torch.cuda.current_stream(self._index) == self.stream:
+        if _current_stream(self._index) == self._raw_stream:
             buf = torch.empty(need, dtype=torch.uint8, device=self.device)
         else:
             with torch.cuda.stream(self.stream):
