@@ -140,7 +140,7 @@ struct PlanIn {
     TokenBatch b;
     uint32_t q_heads, kv_heads, ratio, head_dim;
     uint64_t target;     // items wanted
-    uint64_t part_rows;  // rows of parts there is room for
+    uint64_t part_rows;  // rows of parts there is room for (0: no unit is cut)
     uint32_t* arrived;   // workgroups that are done with their sequences; zero between calls
 };
 
@@ -416,7 +416,7 @@ __global__ __launch_bounds__(kPlanThreads) void attn_plan_kernel(PlanIn a, PlanV
         }
         cost = block_sum64(cost, lds) * a.kv_heads;
         uint64_t chunk = (cost / a.target + kChunk) / kChunk * kChunk;
-        if (attempt || chunk > 0x80000000ull)
+        if (attempt || a.part_rows == 0 || chunk > 0x80000000ull)
             chunk = 0x80000000ull;
         // items and rows of parts before each unit
         if (tid == 0)
@@ -969,8 +969,9 @@ struct Share {
 };
 
 // What the waves of a narrow tile leave for one another.
+template <int WAVES>
 struct Joined {
-    float m[kWaves][kNarrow], l[kWaves][kNarrow];
+    float m[WAVES][kNarrow], l[WAVES][kNarrow];
 };
 
 // The largest of the values of a row's four lanes (16 apart), in each of them.
@@ -1001,13 +1002,13 @@ __device__ __forceinline__ void write_four(const AttnIn& a, const Tile& t, uint3
 
 // A lane holds its row's (lane % 16) scores of 4 of 16 keys, key = h * 16 + (lane /
 // 16) * 4 + i, and of O^T the elements d = block * 16 + (lane / 16) * 4 + i.
-template <typename T, int D>
-__device__ __forceinline__ void narrow_tile(const AttnIn& a, const Tile& t, uint16_t* lds, Joined& joined,
+template <typename T, int D, int WAVES>
+__device__ __forceinline__ void narrow_tile(const AttnIn& a, const Tile& t, uint16_t* lds, Joined<WAVES>& joined,
                                             bool& bad)
 {
     using V = typename Vec8<T>::type;
     constexpr int kLoads = kNarrowKeys * D / 8 / kWave;
-    constexpr uint32_t kRowChunks = D / 8, kStep = kWave / kRowChunks, kTurn = kWaves * kNarrowKeys;
+    constexpr uint32_t kRowChunks = D / 8, kStep = kWave / kRowChunks, kTurn = WAVES * kNarrowKeys;
     constexpr int kBlocks = D / 16;
     const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
     const uint32_t lane = lane_id(), row16 = lane % 16, g = lane / 16;
@@ -1143,7 +1144,7 @@ __device__ __forceinline__ void narrow_tile(const AttnIn& a, const Tile& t, uint
             }
         }
     }
-    // the four waves' parts joined, a quarter of the blocks by each wave
+    // the waves' parts joined, each wave a share of the blocks
     l += __shfl_xor(l, 16);
     l += __shfl_xor(l, 32);
     if (g == 0) {
@@ -1153,9 +1154,9 @@ __device__ __forceinline__ void narrow_tile(const AttnIn& a, const Tile& t, uint
     v4f* sum = reinterpret_cast<v4f*>(lds);  // [wave][block][lane]
     __syncthreads();
     float all = -INFINITY, total = 0;
-    for (int w = 0; w < kWaves; w++)
+    for (int w = 0; w < WAVES; w++)
         all = fmaxf(all, joined.m[w][row16]);
-    for (int w = 0; w < kWaves; w++) {
+    for (int w = 0; w < WAVES; w++) {
         const float mw = joined.m[w][row16], lw = joined.l[w][row16];
         // a wave that saw nothing adds nothing, one that saw only NaN adds it
         total += mw == -INFINITY ? (lw != lw ? lw : 0.0f) : lw * __builtin_amdgcn_exp2f((mw - all) * a.scale2);
@@ -1167,11 +1168,9 @@ __device__ __forceinline__ void narrow_tile(const AttnIn& a, const Tile& t, uint
     __syncthreads();
     const bool seen = total > 0 || total != total;
     const float inv = seen ? 1.0f / total : 0.0f;
-#pragma unroll
-    for (int b = 0; b < kBlocks / kWaves; b++) {
-        const uint32_t d = wave * (kBlocks / kWaves) + b;
+    for (uint32_t d = wave; d < kBlocks; d += WAVES) {
         v4f x = {};
-        for (int w = 0; w < kWaves; w++)
+        for (int w = 0; w < WAVES; w++)
             x += sum[(w * kBlocks + d) * kWave + lane];
         for (int k = 0; k < 4; k++)
             x[k] = seen ? x[k] * inv : 0.0f;
@@ -1377,7 +1376,7 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attn_kernel(AttnIn
     // two tiles of 64 keys and values, or four waves' 32 keys and values
     __shared__ __attribute__((aligned(16))) uint16_t lds[4 * kWideKeys * D];
     __shared__ uint32_t odd_tile;
-    __shared__ Joined joined;
+    __shared__ Joined<kWaves> joined;
     const PlanHead& ph = *pv.head;
     const uint32_t ui = find_unit(pv.item0, a.b.groups + a.b.n, blockIdx.x);  // beside the head's reads
     if (!plan_fits(ph, a, part_rows, D) || ph.items > gridDim.x) {
@@ -1393,7 +1392,37 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attn_kernel(AttnIn
     if (u.flags & kUnitWide)
         wide_tile<T, D>(a, make_tile(a, u, x, kWide), lds, &odd_tile, bad);
     else
-        narrow_tile<T, D>(a, make_tile(a, u, x, kNarrow), lds, joined, bad);
+        narrow_tile<T, D, kWaves>(a, make_tile(a, u, x, kNarrow), lds, joined, bad);
+    if (bad)
+        atomicOr(status, kErrInval);
+}
+
+// A few rows on a few keys: narrow tiles, uncut, of as many waves as have room in LDS,
+// where a second kernel that joins parts costs more than cutting gains.  A token of
+// 32 query and 8 key heads of 128 on 100, 300, 500, 700 and 1,000 keys: 6.9, 8.4, 9.6,
+// 11.2 and 13.2 us, in parts 8.6, 11.1, 11.1, 11.3 and 11.1; heads of 64 on 1,000 keys
+// 9.4 and 9.9, of 256 on 300 keys 16.4 and 14.4.
+template <int D>
+constexpr int kSmallWaves = D == 256 ? 4 : 8;
+template <typename T, int D>
+__global__ __launch_bounds__(kSmallWaves<D>* kWave, 1) void attn_small_kernel(AttnIn a, const PlanView pv,
+                                                                              uint32_t* status)
+{
+    constexpr int kW = kSmallWaves<D>;
+    __shared__ __attribute__((aligned(16))) uint16_t lds[kW * 2 * kNarrowKeys * D];
+    __shared__ Joined<kW> joined;
+    const PlanHead& ph = *pv.head;
+    const uint32_t ui = find_unit(pv.item0, a.b.n, blockIdx.x);
+    if (!plan_fits(ph, a, 0, D) || ph.items > gridDim.x) {
+        if (blockIdx.x == 0 && threadIdx.x == 0)
+            atomicOr(status, kErrInval);  // the plan of another batch
+        return;
+    }
+    if (blockIdx.x >= ph.items)
+        return;
+    const Unit u = pv.unit[ui];
+    bool bad = false;
+    narrow_tile<T, D, kW>(a, make_tile(a, u, blockIdx.x - u.item0, kNarrow), lds, joined, bad);
     if (bad)
         atomicOr(status, kErrInval);
 }
@@ -1632,6 +1661,14 @@ __global__ __launch_bounds__(kThreads) void attn_join_kernel(AttnIn a, const Pla
     }
 }
 
+// Is a batch small: no unit has more rows than a narrow tile, and no more keys than
+// attn_small_kernel is the faster on?
+bool small(const dm_ctx* c, const dm_token_batch& b, const dm_kv_pages& kv, uint32_t ratio)
+{
+    const uint64_t keys = kv.head_dim == 64 ? 1024 : kv.head_dim == 128 ? 768 : 256;
+    return b.groups == 0 && b.q_tokens * ratio <= kNarrowRows && b.tables.entries * c->cfg.block_size <= keys;
+}
+
 // Items wanted: three for every two places of a workgroup (two a compute unit).
 // (64 decode rows of up to 8,192 keys, 256 rows on 8 shared prefixes: 218 and 190
 // us; with one for each place 229 and 196, with three 217 and 196.)
@@ -1678,7 +1715,7 @@ hipError_t attn_plan(dm_ctx* c, const dm_token_batch& b, const dm_kv_pages& kv, 
     a.ratio = q_heads / kv.kv_heads;
     a.head_dim = kv.head_dim;
     a.target = item_target(c);
-    a.part_rows = part_rows_of(c, b.q_tokens, q_heads);
+    a.part_rows = small(c, b, kv, a.ratio) ? 0 : part_rows_of(c, b.q_tokens, q_heads);
     const PlanView pv = plan_view(plan, b.tables.n, b.groups);
     a.arrived = c->d_status + 48;  // a line of its own
     const uint32_t grid = !b.groups                        ? 1
@@ -1692,10 +1729,12 @@ hipError_t attn(dm_ctx* c, const dm_token_batch& b, const dm_kv_pages& kv, uint3
                 const void* plan, uint32_t layer, const void* q, int64_t q_stride, float scale,
                 void* out, int64_t out_stride, float* lse)
 {
-    const uint64_t rows = part_rows_of(c, b.q_tokens, q_heads);
+    const bool is_small = small(c, b, kv, q_heads / kv.kv_heads);
+    const uint64_t rows = is_small ? 0 : part_rows_of(c, b.q_tokens, q_heads);
     hipError_t e;
-    float* part = static_cast<float*>(scratch_get(c, kSlotPages, rows * (kv.head_dim + 1) * 4, &e));
-    if (!part)
+    float* part =
+        is_small ? nullptr : static_cast<float*>(scratch_get(c, kSlotPages, rows * (kv.head_dim + 1) * 4, &e));
+    if (!part && !is_small)
         return e;
     AttnIn a;
     a.b = token_batch(c, b);
@@ -1705,7 +1744,7 @@ hipError_t attn(dm_ctx* c, const dm_token_batch& b, const dm_kv_pages& kv, uint3
     a.out = static_cast<uint16_t*>(out);
     a.lse = lse;
     a.part = part;
-    a.part_lse = part + rows * kv.head_dim;
+    a.part_lse = is_small ? nullptr : part + rows * kv.head_dim;
     a.q_stride = q_stride;
     a.out_stride = out_stride;
     a.n_pages = kv.n_pages;
@@ -1714,12 +1753,16 @@ hipError_t attn(dm_ctx* c, const dm_token_batch& b, const dm_kv_pages& kv, uint3
     a.ratio = q_heads / kv.kv_heads;
     a.scale2 = scale * kLog2e;
     const PlanView pv = plan_view(const_cast<void*>(plan), b.tables.n, b.groups);
-    const uint64_t most = most_items(c, b, a.ratio, kv.kv_heads);
+    const uint64_t most = is_small ? (uint64_t)b.tables.n * kv.kv_heads : most_items(c, b, a.ratio, kv.kv_heads);
     if (most > 0x7FFFFFFFull)
         return hipErrorInvalidValue;
     by_type(kv.dtype, kv.head_dim, [&](auto t, auto d) {
         using T = decltype(t);
         constexpr int D = decltype(d)::value;
+        if (is_small) {
+            attn_small_kernel<T, D><<<(uint32_t)most, kSmallWaves<D> * kWave, 0, c->stream>>>(a, pv, c->d_status);
+            return;
+        }
         attn_kernel<T, D><<<(uint32_t)most, kThreads, 0, c->stream>>>(a, pv, rows, c->d_status);
         const uint64_t outs = b.q_tokens * q_heads;
         if (outs > 8ull * c->n_cu * kWaves)

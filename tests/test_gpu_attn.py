@@ -558,3 +558,37 @@ def test_many_rows_in_parts(dtype, dim, heads, prefix):
               dtype=dtype, seed=43)
     _say("many rows", dtype, dim, heads, prefix)
     b.check()
+
+
+@pytest.mark.parametrize("dtype,dim,heads", [("bf16", 64, (4, 2)), ("f16", 128, (14, 2)), ("bf16", 128, (16, 1)), ("f16", 256, (3, 3))])
+def test_few_rows_on_few_keys(dtype, dim, heads):
+    """Batches around the limits of the form without parts: rows, keys, sequences; idle places; a fault's report."""
+    ratio = heads[0] // heads[1]
+    most = {64: 1024, 128: 768, 256: 256}[dim]
+    for keys in (1, 31, 32, 33, 127, 129, 255, 256, 257, 500, 752, 767, 768, 769, 1023, 1024, 1025):
+        if keys <= most + 100:
+            Batch(16, [(1, keys)], heads=heads, dim=dim, dtype=dtype, seed=keys).check()
+    rows = 16 // ratio
+    for seqs in ([(rows, most - 5)], [(rows + 1, most - 5)], [(rows, 2)], [(1, 100), (0, 40), (1, 3)][:rows + 1],
+                 [(1, 0), (1, 77), (0, 0), (1, 1)][:rows + 1]):
+        _say("few", dtype, dim, heads, seqs)
+        Batch(16, seqs, heads=heads, dim=dim, dtype=dtype, seed=len(seqs) + 60).check()
+    b = Batch(16, [(rows, 200)], heads=heads, dim=dim, dtype=dtype, seed=61)
+    b.page = b.page.copy()
+    b.page[3] = 10 ** 6
+    pk, _ = engine(16)
+    with pytest.raises(pk.DMError) as x:
+        b.run()
+    assert x.value.status == pk.DM_EINVAL
+
+
+@pytest.mark.parametrize("what", [float("inf"), float("nan")])
+def test_few_rows_and_unseen_values(what):
+    """Infinities and NaN that some of a tile's rows do not see."""
+    b = Batch(16, [(4, 300)], heads=(8, 2), dim=128, seed=62)
+    out, lse = b.run()
+    at = int(b.page[b.off[0] + 299 // 16])
+    b.v[0, at, :, 299 % 16] = what
+    b.k[0, at, :, 299 % 16] = what
+    again, lse2 = b.run()
+    assert torch.equal(out[:3].view(torch.int16), again[:3].view(torch.int16)) and torch.equal(lse[:3], lse2[:3])
