@@ -885,25 +885,30 @@ __device__ __forceinline__ void clear(Row<D>& r)
         r.o[d] = v16f{};
 }
 
-// A thread's share of the tiles of TILE keys and values that an item goes through:
-// 16-byte chunk `ch` of rows r0, r0 + STEP, ...  A tile's pages are looked up two tiles
-// ahead and its rows read one ahead; none of the reads is conditional: rows past
-// the last key read the last key's page, and their values become zeros on the
-// way to LDS.
-template <typename T, int D, int LOADS, int STEP, uint32_t TILE>
-struct Share {
-    // LANES: the waves look at tiles of their own, of which lane r knows row r's page
-    // (a register instead of one for each row that a thread reads)
-    static constexpr bool LANES = TILE < kWave;
-    v4u32 k[LOADS], v[LOADS];
-    uint32_t page[LANES ? 1 : LOADS];
-    const int32_t* table;
-    uint32_t key1, n_pages, shift, r0, ch, head_at, page_size;
+// Pages are looked up by scalar loads: a send's or a load's rows
+// lie four to a page (tiles begin at multiples of four tokens), and vector loads would
+// wait for everything that was asked for before them.
+typedef const __attribute__((address_space(4))) uint32_t ScalarTable;
 
-    __device__ __forceinline__ Share(const AttnIn& a, const Tile& t, uint32_t thread)
-        : table(a.b.page + t.u.off), key1(t.key1), n_pages(a.n_pages), shift(a.b.shift),
-          r0(thread / (D / 8)), ch(thread % (D / 8)), head_at((t.h * D << a.b.shift) + ch * 8),
-          page_size(a.kv_heads * D << a.b.shift)
+// A lane's share of a wave's narrow tiles: 16-byte chunk `ch` of rows r0, r0 + kStep,
+// ...  A tile's pages are looked up two tiles ahead and its rows read one ahead; none
+// of the reads is conditional: rows past the last key read the last key's page, and
+// their values become zeros on the way to LDS.
+template <typename T, int D>
+struct Share {
+    static constexpr int kLoads = kNarrowKeys * D / 8 / kWave;
+    static constexpr uint32_t kRowChunks = D / 8, kStep = kWave / kRowChunks;
+    static constexpr int kGroups = kStep > 4 ? 2 : 1, kPages = kLoads * kGroups;
+    v4u32 k[kLoads], v[kLoads];
+    uint32_t page[kPages];
+    ScalarTable* table;
+    uint32_t key1, n_pages, shift, r0, ch, lane_at;
+    uint64_t head_at, page_size;
+
+    __device__ __forceinline__ Share(const AttnIn& a, const Tile& t)
+        : table((ScalarTable*)(a.b.page + t.u.off)), key1(t.key1), n_pages(a.n_pages), shift(a.b.shift),
+          r0(lane_id() / kRowChunks), ch(lane_id() % kRowChunks), lane_at(r0 % 4 * D + ch * 8),
+          head_at((uint64_t)t.h * D << a.b.shift), page_size((uint64_t)a.kv_heads * D << a.b.shift)
     {
     }
     // r0, each time anew: what follows from it is worked out again for each tile
@@ -914,33 +919,30 @@ struct Share {
         asm volatile("" : "+v"(r));
         return r;
     }
-    // pages of the tile at `key` (uniform, < key1)
-    __device__ __forceinline__ void find(uint32_t key, bool& bad)
+    // pages of the tile at `key` (uniform, < key1), as they are in the table
+    __device__ __forceinline__ void find(uint32_t key)
     {
-        const uint32_t last = key1 - 1;
-        const uint32_t row = LANES ? key + lane_id() % TILE : key + here();
 #pragma unroll
-        for (int i = 0; i < (LANES ? 1 : LOADS); i++) {
-            uint32_t x = row + i * STEP;
-            if (key + TILE > key1)
-                x = x < last ? x : last;
-            const uint32_t p = (uint32_t)table[x >> shift];
-            bad |= p >= n_pages;
-            page[i] = p < n_pages ? p : 0;
+        for (int i = 0; i < kPages; i++) {
+            const uint32_t x = key + i / kGroups * kStep + i % kGroups * 4;
+            page[i] = table[(x < key1 ? x : key1 - 1) >> shift];
         }
     }
-    __device__ __forceinline__ void fetch(const AttnIn& a, uint32_t key)
+    __device__ __forceinline__ void fetch(const AttnIn& a, uint32_t key, bool& bad)
     {
         const uint32_t mask = (1u << shift) - 1;
-        const uint32_t row = key + here();
 #pragma unroll
-        for (int i = 0; i < LOADS; i++) {
-            const uint32_t p = LANES ? __shfl(page[0], r0 + i * STEP) : page[LANES ? 0 : i];
-            const uint64_t at = (uint64_t)p * page_size + (head_at + ((row + i * STEP) & mask) * D);
-            k[i] = *reinterpret_cast<const v4u32*>(a.k + at);
-            v[i] = *reinterpret_cast<const v4u32*>(a.v + at);
-            if (LANES)
-                __builtin_amdgcn_sched_barrier(0);  // an address at a time
+        for (int i = 0; i < kLoads; i++) {
+            uint64_t at[kGroups];
+#pragma unroll
+            for (int g = 0; g < kGroups; g++) {
+                const uint32_t p = page[i * kGroups + g];
+                bad |= p >= n_pages;
+                at[g] = (p < n_pages ? p : 0) * page_size + head_at + ((key + i * kStep + g * 4) & mask) * D;
+            }
+            const uint64_t from = kGroups == 1 || lane_id() < kWave / 2 ? at[0] : at[kGroups - 1];
+            k[i] = *reinterpret_cast<const v4u32*>(a.k + from + lane_at);
+            v[i] = *reinterpret_cast<const v4u32*>(a.v + from + lane_at);
         }
     }
     // into LDS; true: values that are not finite among them (asked for where some
@@ -951,18 +953,18 @@ struct Share {
         if (ask) {
             const uint32_t have = key1 - key;
 #pragma unroll
-            for (int i = 0; i < LOADS; i++) {
-                if (r0 + i * STEP >= have)
+            for (int i = 0; i < kLoads; i++) {
+                if (r0 + i * kStep >= have)
                     v[i] = v4u32{};
                 odd |= not_finite<T>(v[i]);
             }
         }
-        const uint32_t row = LANES ? here() : r0;
+        const uint32_t row = here();
 #pragma unroll
-        for (int i = 0; i < LOADS; i++) {
-            const uint32_t r = row + i * STEP;
+        for (int i = 0; i < kLoads; i++) {
+            const uint32_t r = row + i * kStep;
             *reinterpret_cast<v4u32*>(kt + r * D + (ch ^ k_swizzle<D>(r)) * 8) = k[i];
-            *reinterpret_cast<v4u32*>(vt + r * D + (ch ^ v_swizzle<D, !LANES>(r)) * 8) = v[i];
+            *reinterpret_cast<v4u32*>(vt + r * D + (ch ^ v_swizzle<D, false>(r)) * 8) = v[i];
         }
         return odd;
     }
@@ -1007,8 +1009,7 @@ __device__ __forceinline__ void narrow_tile(const AttnIn& a, const Tile& t, uint
                                             bool& bad)
 {
     using V = typename Vec8<T>::type;
-    constexpr int kLoads = kNarrowKeys * D / 8 / kWave;
-    constexpr uint32_t kRowChunks = D / 8, kStep = kWave / kRowChunks, kTurn = WAVES * kNarrowKeys;
+    constexpr uint32_t kTurn = WAVES * kNarrowKeys;
     constexpr int kBlocks = D / 16;
     const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
     const uint32_t lane = lane_id(), row16 = lane % 16, g = lane / 16;
@@ -1075,7 +1076,7 @@ __device__ __forceinline__ void narrow_tile(const AttnIn& a, const Tile& t, uint
     };
     uint32_t key = t.key0 + wave * kNarrowKeys;
     if (key < t.key1) {
-        Share<T, D, kLoads, kStep, kNarrowKeys> x(a, t, lane);
+        Share<T, D> x(a, t);
         bool masked = false, odd = false;
         // a wave's own part of LDS: its lanes' writes and reads in order
         auto stage = [&](uint32_t key) {
@@ -1086,18 +1087,18 @@ __device__ __forceinline__ void narrow_tile(const AttnIn& a, const Tile& t, uint
             __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
             __builtin_amdgcn_wave_barrier();
         };
-        x.find(key, bad);
-        x.fetch(a, key);
+        x.find(key);
+        x.fetch(a, key, bad);
         if (key + kTurn < t.key1)
-            x.find(key + kTurn, bad);
+            x.find(key + kTurn);
         for (; key < t.key1; key += kTurn) {
             stage(key);
             if (masked && __any(odd))
                 break;
             if (key + kTurn < t.key1)
-                x.fetch(a, key + kTurn);
+                x.fetch(a, key + kTurn, bad);
             if (key + 2 * kTurn < t.key1)
-                x.find(key + 2 * kTurn, bad);
+                x.find(key + 2 * kTurn);
             weigh(key, masked);
             // O^T += V^T P^T, keys in the order of the lane's weights
             const uint32_t r = g * 4 + row16 / 4;
@@ -1138,8 +1139,8 @@ __device__ __forceinline__ void narrow_tile(const AttnIn& a, const Tile& t, uint
             }
             key += kTurn;
             if (key < t.key1) {
-                x.find(key, bad);
-                x.fetch(a, key);
+                x.find(key);
+                x.fetch(a, key, bad);
                 stage(key);
             }
         }
@@ -1197,6 +1198,16 @@ __device__ __forceinline__ void send16(const uint16_t* from, uint32_t lds_at)
                  : "s"(lds_at), "v"(from)
                  : "memory");
 }
+// The same from a uniform address and a lane's bytes on from it.  (Five wait states
+// between a vector instruction that may have written the address, such as the reload
+// of a spilled scalar, and its use; the compiler does not see into this.)
+__device__ __forceinline__ void send16(const uint16_t* from, uint32_t lane_at, uint32_t lds_at)
+{
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tglobal_load_lds_dwordx4 %1, %2"
+                 :
+                 : "s"(lds_at), "v"(lane_at), "s"(from)
+                 : "memory");
+}
 __device__ __forceinline__ void wait_sent() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
 
 // Byte address of a place in LDS.
@@ -1206,46 +1217,56 @@ __device__ __forceinline__ uint32_t lds_address(const uint16_t* p)
 }
 
 // A thread's share of wide tiles: LDS chunk threadIdx.x + i * 256, that is row r0 +
-// i * kStep, place `ch` of the row.
+// i * kStep, place `ch` of the row.  What a lane adds to its rows' address does not
+// change from tile to tile.
 template <typename T, int D>
 struct Sender {
     static constexpr int kLoads = kWideKeys * D / 8 / kThreads;
     static constexpr uint32_t kRowChunks = D / 8, kStep = kThreads / kRowChunks;
+    static constexpr uint32_t kWaveRows = kWave / kRowChunks;
+    static constexpr int kGroups = kWaveRows > 4 ? 2 : 1, kPages = kLoads * kGroups;
     const uint16_t *k, *v;  // the layer's pages, at the KV head
-    const int32_t* table;
-    uint32_t key1, n_pages, shift, page_size, r0, ch, wave_at;
+    ScalarTable* table;
+    uint32_t key1, n_pages, shift, page_size, r0, ch, wave, lane_row;
 
-    __device__ __forceinline__ Sender(const AttnIn& a, const Tile& t, uint32_t wave)
+    __device__ __forceinline__ Sender(const AttnIn& a, const Tile& t, uint32_t wave_)
         : k(a.k + ((uint64_t)t.h * D << a.b.shift)), v(a.v + ((uint64_t)t.h * D << a.b.shift)),
-          table(a.b.page + t.u.off), key1(t.key1), n_pages(a.n_pages), shift(a.b.shift),
+          table((ScalarTable*)(a.b.page + t.u.off)), key1(t.key1), n_pages(a.n_pages), shift(a.b.shift),
           page_size(a.kv_heads * D << a.b.shift), r0(threadIdx.x / kRowChunks), ch(threadIdx.x % kRowChunks),
-          wave_at(wave * kWave * 16)
+          wave(wave_), lane_row(r0 % kWaveRows % 4 * D)
     {
     }
-    // pages of the tile at `key` (uniform, < key1); rows past the last key: the
-    // last key's
-    __device__ __forceinline__ void find(uint32_t key, uint32_t (&page)[kLoads], bool& bad) const
+    // pages of the wave's rows of the tile at `key` (uniform, < key1), as they are in the
+    // table; rows past the last key: the last key's
+    __device__ __forceinline__ void find(uint32_t key, uint32_t (&page)[kPages]) const
     {
-        const uint32_t last = key + kWideKeys > key1 ? key1 - 1 : 0xFFFFFFFFu;
 #pragma unroll
-        for (int i = 0; i < kLoads; i++) {
-            const uint32_t x = key + r0 + i * kStep;
-            const uint32_t p = *reinterpret_cast<const uint32_t*>(reinterpret_cast<const uint8_t*>(table) +
-                                                                  (((x < last ? x : last) >> shift) << 2));
-            bad |= p >= n_pages;
-            page[i] = p < n_pages ? p : 0;
+        for (int i = 0; i < kPages; i++) {
+            const uint32_t x = key + wave * kWaveRows + i / kGroups * kStep + i % kGroups * 4;
+            page[i] = table[(x < key1 ? x : key1 - 1) >> shift];
         }
     }
     __device__ __forceinline__ void send(const uint16_t* base, bool values, uint32_t key,
-                                         const uint32_t (&page)[kLoads], const uint16_t* to) const
+                                         const uint32_t (&page)[kPages], const uint16_t* to, bool& bad) const
     {
-        const uint32_t mask = (1u << shift) - 1, at = lds_address(to) + wave_at;
+        const uint32_t mask = (1u << shift) - 1, at = lds_address(to) + wave * kWave * 16;
 #pragma unroll
         for (int i = 0; i < kLoads; i++) {
+            const uint16_t* from[kGroups];
+#pragma unroll
+            for (int g = 0; g < kGroups; g++) {
+                const uint32_t p = page[i * kGroups + g];
+                bad |= p >= n_pages;
+                from[g] = base + (uint64_t)(p < n_pages ? p : 0) * page_size +
+                          ((key + wave * kWaveRows + i * kStep + g * 4) & mask) * D;
+            }
             const uint32_t r = r0 + i * kStep;
             const uint32_t c = ch ^ (values ? v_swizzle<D>(r) : k_swizzle<D>(r));
-            send16(base + (uint64_t)page[i] * page_size + (((key + r) & mask) * D + c * 8),
-                   __builtin_amdgcn_readfirstlane(at + i * kThreads * 16));
+            const uint32_t lane_at = (lane_row + c * 8) * 2, lds_at = at + i * kThreads * 16;
+            if (kGroups == 1)
+                send16(from[0], lane_at, lds_at);
+            else
+                send16((lane_id() < kWave / 2 ? from[0] : from[kGroups - 1]) + lane_at / 2, lds_at);
         }
     }
     // A tile of values of which some row does not see all: zeros for the places past
@@ -1290,18 +1311,18 @@ __device__ __forceinline__ void wide_tile(const AttnIn& a, const Tile& t, uint16
     uint16_t* vts = lds + 2 * kTile;  // two tiles of keys, then two of values
     if (t.key0 < t.key1) {
         const Sender<T, D> x(a, t, wave);
-        uint32_t p1[Sender<T, D>::kLoads], p2[Sender<T, D>::kLoads];  // pages of the next tile, and the one after
+        uint32_t p1[Sender<T, D>::kPages], p2[Sender<T, D>::kPages];  // pages of the next tile, and the one after
         if (threadIdx.x == 0)
             *odd_tile = 0;
-        x.find(t.key0, p2, bad);
-        x.send(x.k, false, t.key0, p2, lds);
-        x.send(x.v, true, t.key0, p2, vts);
+        x.find(t.key0, p2);
+        x.send(x.k, false, t.key0, p2, lds, bad);
+        x.send(x.v, true, t.key0, p2, vts, bad);
         if (t.key0 + kWideKeys < t.key1) {
-            x.find(t.key0 + kWideKeys, p1, bad);
-            x.send(x.k, false, t.key0 + kWideKeys, p1, lds + kTile);
+            x.find(t.key0 + kWideKeys, p1);
+            x.send(x.k, false, t.key0 + kWideKeys, p1, lds + kTile, bad);
         }
         if (t.key0 + 2 * kWideKeys < t.key1)
-            x.find(t.key0 + 2 * kWideKeys, p2, bad);
+            x.find(t.key0 + 2 * kWideKeys, p2);
         wait_sent();
         __syncthreads();
         v16f s[2] = {scores<T, D>(lds, q), scores<T, D>(lds + 32 * D, q)};
@@ -1321,15 +1342,15 @@ __device__ __forceinline__ void wide_tile(const AttnIn& a, const Tile& t, uint16
             }
             const uint32_t key1 = key + kWideKeys, key2 = key1 + kWideKeys;
             if (key2 < t.key1)
-                x.send(x.k, false, key2, p2, lds + buf * kTile);
+                x.send(x.k, false, key2, p2, lds + buf * kTile, bad);
             if (key1 < t.key1) {
-                x.send(x.v, true, key1, p1, vts + (buf ^ 1) * kTile);
+                x.send(x.v, true, key1, p1, vts + (buf ^ 1) * kTile, bad);
 #pragma unroll
-                for (int i = 0; i < Sender<T, D>::kLoads; i++)
+                for (int i = 0; i < Sender<T, D>::kPages; i++)
                     p1[i] = p2[i];
             }
             if (key2 + kWideKeys < t.key1)
-                x.find(key2 + kWideKeys, p2, bad);
+                x.find(key2 + kWideKeys, p2);
             if (key < wave_last) {
                 weights<T, D, 2>(r, s, p, key, end, masked(key, wave_first), a.scale2, [&] {
                     // (of the last tile: of what is there, and not used)
@@ -1354,9 +1375,9 @@ __device__ __forceinline__ void wide_tile(const AttnIn& a, const Tile& t, uint16
             if (key >= t.key1)
                 break;
             __syncthreads();
-            x.find(key, p1, bad);
-            x.send(x.k, false, key, p1, lds + buf * kTile);
-            x.send(x.v, true, key, p1, vts + buf * kTile);
+            x.find(key, p1);
+            x.send(x.k, false, key, p1, lds + buf * kTile, bad);
+            x.send(x.v, true, key, p1, vts + buf * kTile, bad);
             wait_sent();
             __syncthreads();
             x.clean(vts + buf * kTile, key);

@@ -592,3 +592,13 @@ def test_few_rows_and_unseen_values(what):
     b.k[0, at, :, 299 % 16] = what
     again, lse2 = b.run()
     assert torch.equal(out[:3].view(torch.int16), again[:3].view(torch.int16)) and torch.equal(lse[:3], lse2[:3])
+
+
+@pytest.mark.parametrize("block", [4, 8, 64])
+@pytest.mark.parametrize("dtype,dim", [("bf16", 64), ("f16", 256), ("bf16", 128)])
+def test_small_pages_and_heads(block, dtype, dim):
+    """Pages smaller than the rows that a wave reads at once, in every form: few rows, narrow and wide tiles, a run."""
+    _say("pages", block, dtype, dim)
+    Batch(block, [(2, 150)], heads=(4, 2), dim=dim, dtype=dtype, seed=71).check()
+    Batch(block, [(1, 900), (3, 70), (40, 333), (1, 2)], heads=(8, 2), dim=dim, dtype=dtype, seed=72).check()
+    Batch(block, [(1, 30, 0), (2, 200, 0), (50, 77, 0), (9, 9, 0)], prefixes=(640,), heads=(8, 2), dim=dim, dtype=dtype, seed=73).check()
