@@ -902,12 +902,15 @@ struct Share {
     v4u32 k[kLoads], v[kLoads];
     uint32_t page[kPages];
     ScalarTable* table;
-    uint32_t key1, n_pages, shift, r0, ch, lane_at;
+    uint32_t key1, n_pages, shift, r0, ch;
+    bool halves;  // eight rows of a load are in two pages of four
+    uint32_t lane_at;
     uint64_t head_at, page_size;
 
     __device__ __forceinline__ Share(const AttnIn& a, const Tile& t)
         : table((ScalarTable*)(a.b.page + t.u.off)), key1(t.key1), n_pages(a.n_pages), shift(a.b.shift),
-          r0(lane_id() / kRowChunks), ch(lane_id() % kRowChunks), lane_at(r0 % 4 * D + ch * 8),
+          r0(lane_id() / kRowChunks), ch(lane_id() % kRowChunks), halves(kGroups == 2 && a.b.shift == 2),
+          lane_at(r0 % (halves ? 4 : 8) * D + ch * 8),
           head_at((uint64_t)t.h * D << a.b.shift), page_size((uint64_t)a.kv_heads * D << a.b.shift)
     {
     }
@@ -925,24 +928,32 @@ struct Share {
 #pragma unroll
         for (int i = 0; i < kPages; i++) {
             const uint32_t x = key + i / kGroups * kStep + i % kGroups * 4;
-            page[i] = table[(x < key1 ? x : key1 - 1) >> shift];
+            if (i % kGroups == 0 || halves)
+                page[i] = table[(x < key1 ? x : key1 - 1) >> shift];
         }
     }
     __device__ __forceinline__ void fetch(const AttnIn& a, uint32_t key, bool& bad)
     {
         const uint32_t mask = (1u << shift) - 1;
+        auto from = [&](int i, int g) {
+            const uint32_t p = page[i * kGroups + g];
+            bad |= p >= n_pages;
+            return (p < n_pages ? p : 0) * page_size + head_at + ((key + i * kStep + g * 4) & mask) * D;
+        };
+        auto load = [&](int i, uint64_t at) {
+            k[i] = *reinterpret_cast<const v4u32*>(a.k + at + lane_at);
+            v[i] = *reinterpret_cast<const v4u32*>(a.v + at + lane_at);
+        };
+        if (kGroups == 1 || !halves) {
 #pragma unroll
-        for (int i = 0; i < kLoads; i++) {
-            uint64_t at[kGroups];
+            for (int i = 0; i < kLoads; i++)
+                load(i, from(i, 0));
+        } else {
 #pragma unroll
-            for (int g = 0; g < kGroups; g++) {
-                const uint32_t p = page[i * kGroups + g];
-                bad |= p >= n_pages;
-                at[g] = (p < n_pages ? p : 0) * page_size + head_at + ((key + i * kStep + g * 4) & mask) * D;
+            for (int i = 0; i < kLoads; i++) {
+                const uint64_t low = from(i, 0), high = from(i, kGroups - 1);
+                load(i, lane_id() < kWave / 2 ? low : high);
             }
-            const uint64_t from = kGroups == 1 || lane_id() < kWave / 2 ? at[0] : at[kGroups - 1];
-            k[i] = *reinterpret_cast<const v4u32*>(a.k + from + lane_at);
-            v[i] = *reinterpret_cast<const v4u32*>(a.v + from + lane_at);
         }
     }
     // into LDS; true: values that are not finite among them (asked for where some
@@ -1227,13 +1238,15 @@ struct Sender {
     static constexpr int kGroups = kWaveRows > 4 ? 2 : 1, kPages = kLoads * kGroups;
     const uint16_t *k, *v;  // the layer's pages, at the KV head
     ScalarTable* table;
-    uint32_t key1, n_pages, shift, page_size, r0, ch, wave, lane_row;
+    uint32_t key1, n_pages, shift, page_size, r0, ch, wave;
+    bool halves;  // the wave's eight rows are in two pages of four
+    uint32_t lane_row;
 
     __device__ __forceinline__ Sender(const AttnIn& a, const Tile& t, uint32_t wave_)
         : k(a.k + ((uint64_t)t.h * D << a.b.shift)), v(a.v + ((uint64_t)t.h * D << a.b.shift)),
           table((ScalarTable*)(a.b.page + t.u.off)), key1(t.key1), n_pages(a.n_pages), shift(a.b.shift),
           page_size(a.kv_heads * D << a.b.shift), r0(threadIdx.x / kRowChunks), ch(threadIdx.x % kRowChunks),
-          wave(wave_), lane_row(r0 % kWaveRows % 4 * D)
+          wave(wave_), halves(kGroups == 2 && a.b.shift == 2), lane_row(r0 % kWaveRows % (halves ? 4 : 8) * D)
     {
     }
     // pages of the wave's rows of the tile at `key` (uniform, < key1), as they are in the
@@ -1243,7 +1256,8 @@ struct Sender {
 #pragma unroll
         for (int i = 0; i < kPages; i++) {
             const uint32_t x = key + wave * kWaveRows + i / kGroups * kStep + i % kGroups * 4;
-            page[i] = table[(x < key1 ? x : key1 - 1) >> shift];
+            if (i % kGroups == 0 || halves)
+                page[i] = table[(x < key1 ? x : key1 - 1) >> shift];
         }
     }
     __device__ __forceinline__ void send(const uint16_t* base, bool values, uint32_t key,
@@ -1252,21 +1266,21 @@ struct Sender {
         const uint32_t mask = (1u << shift) - 1, at = lds_address(to) + wave * kWave * 16;
 #pragma unroll
         for (int i = 0; i < kLoads; i++) {
-            const uint16_t* from[kGroups];
-#pragma unroll
-            for (int g = 0; g < kGroups; g++) {
+            auto from = [&](int g) {
                 const uint32_t p = page[i * kGroups + g];
                 bad |= p >= n_pages;
-                from[g] = base + (uint64_t)(p < n_pages ? p : 0) * page_size +
-                          ((key + wave * kWaveRows + i * kStep + g * 4) & mask) * D;
-            }
+                return base + (uint64_t)(p < n_pages ? p : 0) * page_size +
+                       ((key + wave * kWaveRows + i * kStep + g * 4) & mask) * D;
+            };
             const uint32_t r = r0 + i * kStep;
             const uint32_t c = ch ^ (values ? v_swizzle<D>(r) : k_swizzle<D>(r));
             const uint32_t lane_at = (lane_row + c * 8) * 2, lds_at = at + i * kThreads * 16;
-            if (kGroups == 1)
-                send16(from[0], lane_at, lds_at);
-            else
-                send16((lane_id() < kWave / 2 ? from[0] : from[kGroups - 1]) + lane_at / 2, lds_at);
+            if (kGroups == 1 || !halves) {
+                send16(from(0), lane_at, lds_at);
+            } else {
+                const uint16_t *low = from(0), *high = from(kGroups - 1);
+                send16((lane_id() < kWave / 2 ? low : high) + lane_at / 2, lds_at);
+            }
         }
     }
     // A tile of values of which some row does not see all: zeros for the places past
