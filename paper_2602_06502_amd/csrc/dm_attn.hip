@@ -147,16 +147,6 @@ struct PlanIn {
     uint32_t* arrived;   // workgroups that are done with their sequences; zero between calls
 };
 
-// Words that workgroups on other dies write or read within the launch.
-__device__ __forceinline__ void agent_store(uint32_t* p, uint32_t x)
-{
-    __hip_atomic_store(p, x, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-}
-__device__ __forceinline__ uint32_t agent_load(const uint32_t* p)
-{
-    return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-}
-
 constexpr uint32_t kNoSay = 0xFFFFFFFFu;
 constexpr uint32_t kLdsRuns = 1024;
 
@@ -323,16 +313,7 @@ __global__ __launch_bounds__(kPlanThreads) void attn_plan_kernel(PlanIn a, PlanV
         else
             for (uint32_t s = blockIdx.x * kPlanWaves + tid / kWave; s < b.n; s += gridDim.x * kPlanWaves)
                 common_pages(a, pv, s, nullptr);
-        // the words are written through and have arrived when the barrier lets the
-        // waves go; one fence orders them for what thread 0 does next (one by
-        // every wave of 256 workgroups took 60 us)
-        __syncthreads();
-        if (tid == 0) {
-            __builtin_amdgcn_fence(__ATOMIC_RELEASE, "agent");
-            least = atomicAdd(a.arrived, 1u);
-        }
-        __syncthreads();
-        if (least != gridDim.x - 1)
+        if (!last_to_arrive(a.arrived, &least))
             return;
         if (tid == 0)
             agent_store(a.arrived, 0);

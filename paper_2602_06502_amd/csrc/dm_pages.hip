@@ -341,15 +341,6 @@ __global__ __launch_bounds__(kThreads) void fork_count_kernel(ForkIn a, Work w, 
         atomicOr(&w.ctl[kCtlCountErr], kErrInval);
 }
 
-__device__ __forceinline__ void agent_store(uint32_t* p, uint32_t x)
-{
-    __hip_atomic_store(p, x, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-}
-__device__ __forceinline__ uint32_t agent_load(const uint32_t* p)
-{
-    return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-}
-
 // Pass 4: new pages, entries and moves before each sequence, and whether all of
 // them have room.  Whether a sequence copies a page takes a chain of scattered
 // reads, a thread a sequence over the chip (by one workgroup 18 us for 4,096);
@@ -375,13 +366,7 @@ __global__ __launch_bounds__(kPlanThreads) void fork_scan_kernel(ForkIn a, Work 
         agent_store(&w.base[j], (all - (uint32_t)kept + copy) | (copy ? kCopies : 0));
         agent_store(&w.place[j], all);
     }
-    __syncthreads();
-    if (threadIdx.x == 0) {
-        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "agent");
-        turn = atomicAdd(&w.ctl[kCtlTurn], 1u);
-    }
-    __syncthreads();
-    if (turn != gridDim.x - 1)
+    if (!last_to_arrive(&w.ctl[kCtlTurn], &turn))
         return;
     constexpr int kItems = 4;
     uint64_t at[3] = {0, 0, 0};
