@@ -439,6 +439,14 @@ dm_status dm_set_policy(dm_ctx* ctx, int policy);
  * tables.  The calls below do not wait for the device.  Malformed tables,
  * page ids out of range and full outputs are found on the device and reported
  * by dm_sync; no call reads or writes outside the arrays it was given.
+ *
+ * The calls can be captured in a graph.  dm_attn and the two calls that change
+ * tables use a work area of the context, which grows with the calls: make each
+ * call once before the capture, at its largest sizes (one that would have to
+ * grow the area under capture fails with DM_EDEVICE and leaves the capture
+ * whole).  An area that a captured call uses stays until dm_destroy, also when
+ * later calls outgrow it; replays belong on the context's stream, in turn with
+ * its other calls, and before dm_destroy.
  * ------------------------------------------------------------------------- */
 
 typedef enum { DM_BF16 = 0, DM_F16 = 1 } dm_dtype;

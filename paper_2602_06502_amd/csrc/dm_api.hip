@@ -23,7 +23,10 @@ dm_status hip_fail(dm_ctx* c, hipError_t e, const char* what)
 {
     if (e == hipErrorOutOfMemory || e == hipErrorMemoryAllocation)
         return fail(c, DM_ENOMEM, std::string(what) + ": out of device memory");
-    return fail(c, DM_EDEVICE, std::string(what) + ": " + hipGetErrorString(e));
+    std::string msg = std::string(what) + ": " + hipGetErrorString(e);
+    if (e == hipErrorStreamCaptureUnsupported)
+        msg += " (under stream capture a call cannot wait, nor need a larger work area than the calls before it)";
+    return fail(c, DM_EDEVICE, msg);
 }
 
 hipError_t sync_streams(dm_ctx* c)
@@ -50,8 +53,15 @@ void* scratch_get(dm_ctx* c, int slot, size_t bytes, hipError_t* e)
         *e = hipErrorOutOfMemory;
         return nullptr;
     }
-    if (s.bytes >= bytes)
+    if (s.bytes >= bytes) {
+        s.captured = s.captured || stream_capturing(c);
         return s.p;
+    }
+    // (the wait below would end the capture)
+    if (stream_capturing(c)) {
+        *e = hipErrorStreamCaptureUnsupported;
+        return nullptr;
+    }
     // Work already queued (on any of the context's streams) may still use
     // the old buffer.
     if ((*e = sync_streams(c)) != hipSuccess)
@@ -60,10 +70,11 @@ void* scratch_get(dm_ctx* c, int slot, size_t bytes, hipError_t* e)
     // where on the runtime maps an allocation on its own (35 to 60 us, not 1 to 10)
     size_t nb = std::max(bytes, s.bytes + s.bytes / 2);
     nb = (nb + 4095) & ~size_t(4095);
-    if (s.p)
+    if (s.captured)
+        c->outgrown.push_back(s.p);  // a graph's replays go on using it
+    else if (s.p)
         (void)hipFree(s.p);
-    s.p = nullptr;
-    s.bytes = 0;
+    s = Scratch{};
     *e = hipMalloc(&s.p, nb);
     if (*e != hipSuccess) {
         s.p = nullptr;
@@ -296,6 +307,8 @@ void dm_destroy(dm_ctx* c)
             free_ring(r);
     for (auto& s : c->scratch)
         (void)hipFree(s.p);
+    for (void* p : c->outgrown)
+        (void)hipFree(p);
     keylen_free(c);
     kv_free(c);
     for (auto& ev : c->tev)

@@ -73,6 +73,7 @@ struct RingView {
 struct Scratch {
     void* p = nullptr;
     size_t bytes = 0;
+    bool captured = false;  // a graph may hold the address
 };
 
 // Fixed work area for calls that must not allocate: every scratch slot is a
@@ -157,6 +158,7 @@ struct dm_ctx {
     std::vector<uint64_t> occ_bound;
 
     dm::Scratch scratch[dm::kScratchSlots];
+    std::vector<void*> outgrown;      // work areas that graphs may still use
     dm::Arena arena;                  // set only for the duration of an allocation-free call
     uint8_t* noalloc_area = nullptr;  // this device's static work area (dm_noalloc.hip)
     uint32_t shift_div = 0;        // log2(queue_div)
