@@ -44,9 +44,11 @@ constexpr uint32_t kChunk = 128;               // keys of a chunk, at least (of 
 constexpr int kPlanThreads = 512;
 constexpr uint64_t kPartRows = 1ull << 20;     // rows of parts kept beyond those of cut items
 
-// The plan in memory: a head, then a unit for each run and each sequence
-// (runs first), each with the number of items before it, then words of the
-// sequences.
+// The plan in memory: a head, the numbers of items before the units, room for
+// kEarlyUnits of them at least (so that a kernel may read as many beside the head,
+// before it knows whose plan it is), then a unit for each run and each sequence
+// (runs first), then words of the sequences.
+constexpr uint32_t kEarlyUnits = 8 * kWave;
 struct PlanHead {
     uint32_t n, groups, q_tokens, q_heads, kv_heads, shift;  // what it was made for
     int64_t entries;
@@ -86,16 +88,21 @@ struct PlanView {
 
 __host__ __device__ inline uint64_t up16(uint64_t x) { return (x + 15) & ~15ull; }
 
+__host__ __device__ inline uint64_t item0_bytes(uint64_t units)
+{
+    return up16(4 * (units < kEarlyUnits ? kEarlyUnits : units));
+}
+
 __host__ __device__ inline PlanView plan_view(void* p, uint64_t n, uint64_t groups)
 {
     PlanView v;
     uint8_t* b = static_cast<uint8_t*>(p);
     v.head = reinterpret_cast<PlanHead*>(b);
     b += sizeof(PlanHead);
-    v.unit = reinterpret_cast<Unit*>(b);
-    b += up16(sizeof(Unit) * (n + groups));
     v.item0 = reinterpret_cast<uint32_t*>(b);
-    b += up16(4 * (n + groups));
+    b += item0_bytes(n + groups);
+    v.unit = reinterpret_cast<Unit*>(b);
+    b += sizeof(Unit) * (n + groups);
     v.limit = reinterpret_cast<uint32_t*>(b);
     b += up16(4 * n);
     v.run = reinterpret_cast<uint32_t*>(b);
@@ -771,19 +778,17 @@ __device__ __forceinline__ void write_row(const AttnIn& a, const Unit& u, uint32
         a.lse[(uint64_t)t * a.q_heads + x] = lse;
 }
 
-// The last unit with item0 <= item, up to 512 units by one wait.
+// The last of up to kEarlyUnits units with item0 <= item, by one wait.
 __device__ __forceinline__ uint32_t find_unit(const uint32_t* item0, uint32_t units, uint32_t item)
 {
-    if (units > 8 * kWave)
-        return wave_find(item0, units, 1, item);
-    uint32_t x[8], k = 0;
+    uint32_t x[kEarlyUnits / kWave], k = 0;
 #pragma unroll
-    for (uint32_t i = 0; i < 8; i++) {
+    for (uint32_t i = 0; i < kEarlyUnits / kWave; i++) {
         const uint32_t u = i * kWave + lane_id();
         x[i] = u < units ? item0[u] : 0xFFFFFFFFu;
     }
 #pragma unroll
-    for (uint32_t i = 0; i < 8; i++)
+    for (uint32_t i = 0; i < kEarlyUnits / kWave; i++)
         k += __popcll(ballot(x[i] <= item));
     return k ? k - 1 : 0;
 }
@@ -795,6 +800,29 @@ __device__ __forceinline__ bool plan_fits(const PlanHead& h, const AttnIn& a, ui
     return h.n == a.b.n && h.groups == a.b.groups && h.q_tokens == a.b.q_tokens &&
            h.q_heads == a.q_heads && h.kv_heads == a.kv_heads && h.shift == a.b.shift &&
            h.entries == a.b.entries && h.head_dim == head_dim && h.part_rows <= part_rows;
+}
+
+// The unit of this workgroup's item; false: none, or the plan is another batch's
+// (reported).  What the plan holds is read beside its head as far as any plan
+// reaches, and beyond that only once the head has been looked at: the plan of a
+// batch of fewer sequences is a smaller one.
+__device__ __forceinline__ bool item_unit(const AttnIn& a, const PlanView& pv, uint32_t units,
+                                          uint64_t part_rows, uint32_t head_dim, uint32_t* status, Unit& u)
+{
+    const PlanHead& ph = *pv.head;
+    const bool early = units <= kEarlyUnits;
+    uint32_t ui = early ? find_unit(pv.item0, units, blockIdx.x) : 0;
+    if (!plan_fits(ph, a, part_rows, head_dim) || ph.items > gridDim.x) {
+        if (blockIdx.x == 0 && threadIdx.x == 0)
+            atomicOr(status, kErrInval);
+        return false;
+    }
+    if (blockIdx.x >= ph.items)
+        return false;
+    if (!early)
+        ui = wave_find(pv.item0, units, 1, blockIdx.x);
+    u = pv.unit[ui];
+    return true;
 }
 
 // An item: a tile of a unit's rows, a chunk of its keys, a KV head.
@@ -1396,16 +1424,9 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attn_kernel(AttnIn
     __shared__ __attribute__((aligned(16))) uint16_t lds[4 * kWideKeys * D];
     __shared__ uint32_t odd_tile;
     __shared__ Joined<kWaves> joined;
-    const PlanHead& ph = *pv.head;
-    const uint32_t ui = find_unit(pv.item0, a.b.groups + a.b.n, blockIdx.x);  // beside the head's reads
-    if (!plan_fits(ph, a, part_rows, D) || ph.items > gridDim.x) {
-        if (blockIdx.x == 0 && threadIdx.x == 0)
-            atomicOr(status, kErrInval);  // the plan of another batch
+    Unit u;
+    if (!item_unit(a, pv, a.b.groups + a.b.n, part_rows, D, status, u))
         return;
-    }
-    if (blockIdx.x >= ph.items)
-        return;
-    const Unit u = pv.unit[ui];
     bool bad = false;
     const uint32_t x = blockIdx.x - u.item0;
     if (u.flags & kUnitWide)
@@ -1430,16 +1451,9 @@ __global__ __launch_bounds__(kSmallWaves<D>* kWave, 1) void attn_small_kernel(At
     constexpr int kW = kSmallWaves<D>;
     __shared__ __attribute__((aligned(16))) uint16_t lds[kW * 2 * kNarrowKeys * D];
     __shared__ Joined<kW> joined;
-    const PlanHead& ph = *pv.head;
-    const uint32_t ui = find_unit(pv.item0, a.b.n, blockIdx.x);
-    if (!plan_fits(ph, a, 0, D) || ph.items > gridDim.x) {
-        if (blockIdx.x == 0 && threadIdx.x == 0)
-            atomicOr(status, kErrInval);  // the plan of another batch
+    Unit u;
+    if (!item_unit(a, pv, a.b.n, 0, D, status, u))
         return;
-    }
-    if (blockIdx.x >= ph.items)
-        return;
-    const Unit u = pv.unit[ui];
     bool bad = false;
     narrow_tile<T, D, kW>(a, make_tile(a, u, blockIdx.x - u.item0, kNarrow), lds, joined, bad);
     if (bad)
@@ -1720,7 +1734,7 @@ uint64_t part_rows_of(const dm_ctx* c, uint64_t q_tokens, uint32_t q_heads)
 
 uint64_t attn_plan_bytes(uint64_t n, uint64_t groups)
 {
-    return sizeof(PlanHead) + up16(sizeof(Unit) * (n + groups)) + up16(4 * (n + groups)) + 2 * up16(4 * n) +
+    return sizeof(PlanHead) + item0_bytes(n + groups) + sizeof(Unit) * (n + groups) + 2 * up16(4 * n) +
            2 * up16(4 * groups);
 }
 
