@@ -613,8 +613,8 @@ dm_status dm_kv_append(dm_ctx* ctx, const dm_kv_pages* kv, uint32_t layer,
  * [q_heads].  scale > 0.  q_heads a multiple of kv_heads. Rows past
  * q_off[n] are not written.  A sequence whose table is malformed counts as
  * length 0; one with a page out of range gets no defined result; both are
- * reported (DM_EINVAL), and so is a plan of another batch, whatever its size
- * (nothing written).
+ * reported (DM_EINVAL), and so is a plan of another batch, whatever its size,
+ * or of more work than q_tokens can be (q_off out of order): nothing written.
  * dm_attn's work area is the context's: its size goes by q_tokens, q_heads and
  * head_dim (it grows, synchronising once, only when a call needs more than
  * any before it). */

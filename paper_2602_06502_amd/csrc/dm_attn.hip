@@ -793,13 +793,15 @@ __device__ __forceinline__ uint32_t find_unit(const uint32_t* item0, uint32_t un
     return k ? k - 1 : 0;
 }
 
-// Is the plan this call's?
+// Is the plan this call's, of at most `items` items?  (A batch whose q_off is out of
+// order can have more than the call has workgroups.)
 __device__ __forceinline__ bool plan_fits(const PlanHead& h, const AttnIn& a, uint64_t part_rows,
-                                          uint32_t head_dim)
+                                          uint32_t head_dim, uint32_t items)
 {
     return h.n == a.b.n && h.groups == a.b.groups && h.q_tokens == a.b.q_tokens &&
            h.q_heads == a.q_heads && h.kv_heads == a.kv_heads && h.shift == a.b.shift &&
-           h.entries == a.b.entries && h.head_dim == head_dim && h.part_rows <= part_rows;
+           h.entries == a.b.entries && h.head_dim == head_dim && h.part_rows <= part_rows &&
+           h.items <= items;
 }
 
 // The unit of this workgroup's item; false: none, or the plan is another batch's
@@ -812,7 +814,7 @@ __device__ __forceinline__ bool item_unit(const AttnIn& a, const PlanView& pv, u
     const PlanHead& ph = *pv.head;
     const bool early = units <= kEarlyUnits;
     uint32_t ui = early ? find_unit(pv.item0, units, blockIdx.x) : 0;
-    if (!plan_fits(ph, a, part_rows, head_dim) || ph.items > gridDim.x) {
+    if (!plan_fits(ph, a, part_rows, head_dim, gridDim.x)) {
         if (blockIdx.x == 0 && threadIdx.x == 0)
             atomicOr(status, kErrInval);
         return false;
@@ -1575,13 +1577,13 @@ __device__ __forceinline__ void join_quarters(const AttnIn& a, const PlanView& p
 // waves of the other).
 template <typename T, int D, bool MANY>
 __global__ __launch_bounds__(kThreads) void attn_join_kernel(AttnIn a, const PlanView pv,
-                                                             uint64_t part_rows)
+                                                             uint64_t part_rows, uint32_t items)
 {
     constexpr int kPer = D / kWave;  // elements a lane
     __shared__ float acc[kWaves][D];
     const PlanHead& ph = *pv.head;
-    if (ph.part_rows == 0 || !plan_fits(ph, a, part_rows, D))
-        return;
+    if (ph.part_rows == 0 || !plan_fits(ph, a, part_rows, D, items))
+        return;  // the pass has left nothing (and reported it)
     const uint32_t wave = threadIdx.x / kWave, lane = lane_id();
     const bool together = ph.most_parts > 16;
     const uint64_t all = (uint64_t)a.b.q_tokens * a.q_heads;
@@ -1799,9 +1801,10 @@ hipError_t attn(dm_ctx* c, const dm_token_batch& b, const dm_kv_pages& kv, uint3
         attn_kernel<T, D><<<(uint32_t)most, kThreads, 0, c->stream>>>(a, pv, rows, c->d_status);
         const uint64_t outs = b.q_tokens * q_heads;
         if (outs > 8ull * c->n_cu * kWaves)
-            attn_join_kernel<T, D, true><<<4u * c->n_cu, kThreads, 0, c->stream>>>(a, pv, rows);
+            attn_join_kernel<T, D, true><<<4u * c->n_cu, kThreads, 0, c->stream>>>(a, pv, rows, (uint32_t)most);
         else
-            attn_join_kernel<T, D, false><<<grid_for(outs, 1, 8u * c->n_cu), kThreads, 0, c->stream>>>(a, pv, rows);
+            attn_join_kernel<T, D, false>
+                <<<grid_for(outs, 1, 8u * c->n_cu), kThreads, 0, c->stream>>>(a, pv, rows, (uint32_t)most);
     });
     return hipGetLastError();
 }
