@@ -1092,12 +1092,15 @@ __device__ __forceinline__ void narrow_tile(const AttnIn& a, const Tile& t, uint
                 o[d] *= keep;
         }
         const float base = m == -INFINITY ? 0.0f : m * a.scale2;
+        // light weights are summed before they meet a sum that a heavy one may be in
+        float sum = 0;
 #pragma unroll
         for (int i = 0; i < 8; i++) {
             const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i / 4][i % 4], a.scale2, -base));
-            l += w;
+            sum += w;
             p[i] = (T)w;
         }
+        l += sum;
     };
     uint32_t key = t.key0 + wave * kNarrowKeys;
     if (key < t.key1) {

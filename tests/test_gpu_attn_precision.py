@@ -1,0 +1,50 @@
+"""How exactly attention's weights meet the values, against the definition in 64 bits.
+
+Bounds, per element (u: half a unit in the last place of the type, 2^-8 for bfloat16, 2^-11 for float16): the output is
+rounded once, u |out|; a weight that is rounded once before it meets the values is off by u of itself, u sum w|v| / sum
+w; sums in 32 bits add some 2^-20 of sum w|v| / sum w.  The log-sum-exp is in 32 bits: 2^-18 of the largest |score|, and
+of itself.
+"""
+import pytest
+
+pytestmark = pytest.mark.gpu
+
+torch = pytest.importorskip("torch")
+
+from test_gpu_attn import DT, engine  # noqa: E402
+
+
+def light_weights(dtype, heads, dim, where):
+    """One key 17 above 131,072 others, which together have 0.0054 of the weight, 2^-24.5 of the largest each, for `heads`
+    rows a KV head, of as many sequences as leave the keys uncut.  (out, lse, weights and values in 64 bits, lse in 64 bits)"""
+    pk, e = engine(32)
+    n, S, H = 131_073, 200, 4
+    pages = -(-n // 32)
+    one = {"first": 0, "middle": 70_001, "last": n - 1}[where]
+    g = torch.Generator().manual_seed(dim + heads)
+    k = torch.zeros((1, pages, H, 32, dim), dtype=DT[dtype])
+    k[0, one // 32, :, one % 32] = 17 / (0.125 * dim)  # 17 at q = 1 and a scale of 1/8; a value of either type
+    v = (1 + 0.25 * torch.randn((1, pages, 1, 32, dim), generator=g)).to(DT[dtype]).expand(1, pages, H, 32, dim).contiguous()
+    v[0, one // 32, :, one % 32] = 0
+    kd, vd = k.cuda(), v.cuda()
+    i64 = dict(dtype=torch.int64, device="cuda")
+    tables = (pages * torch.arange(S + 1, **i64), torch.arange(pages, dtype=torch.int32, device="cuda").repeat(S),
+              torch.full((S,), n, **i64))
+    q = torch.ones((S, H * heads, dim), dtype=DT[dtype], device="cuda")
+    out, lse = torch.empty_like(q), torch.empty((S, H * heads), device="cuda")
+    print("[case] light weights", dtype, heads, dim, where, flush=True)
+    kv = pk.KVPages(kd, vd)
+    e.attn(e.attn_plan(kv, tables, torch.arange(S + 1, **i64), S, H * heads), 0, q, 0.125, out, lse)
+    e.sync()
+    scores = (kd[0, :, 0].reshape(-1, dim)[:n].double() @ q[0, 0].double()) * 0.125
+    assert float(scores.max()) == 17.0
+    return out, lse, torch.softmax(scores, 0), vd[0, :, 0].reshape(-1, dim)[:n].double(), torch.logsumexp(scores, 0)
+
+
+@pytest.mark.parametrize("where", ["first", "middle", "last"])
+@pytest.mark.parametrize("dtype,dim", [("bf16", 64), ("f16", 128), ("bf16", 256)])
+@pytest.mark.parametrize("heads", [1, 32])
+def test_many_light_weights_are_summed(heads, dtype, dim, where):
+    """In a narrow tile (one row) and in a wide one (32)."""
+    _, lse, _, _, far = light_weights(dtype, heads, dim, where)
+    assert bool(((lse.double() - far).abs() <= 2.0 ** -18 * 36).all()), float((lse.double() - far).abs().max())
