@@ -600,7 +600,8 @@ dm_status dm_kv_append(dm_ctx* ctx, const dm_kv_pages* kv, uint32_t layer,
  * lse = log sum_j w_j.  A token that sees nothing gets zeros and lse
  * = -infinity.  Keys and values that a token does not see have no part in its
  * result, whatever they hold.  Weights are kept in 32 bits and multiplied with
- * the values in dtype; sums, maxima and results of parts are in 32 bits.
+ * the values in dtype (a float16 weight below 2^-21 of its row's largest is off
+ * by up to 2^-32 of that); sums, maxima and results of parts are in 32 bits.
  *
  * dm_attn_plan looks at the batch's tables and cuts the work into items: the
  * prefix pages that a run's sequences have in common are read once for all

@@ -562,6 +562,14 @@ struct AttnIn {
     float scale2;      // scale * log2(e)
 };
 
+// Weights are raised by a power of two: a float16 one loses bits below 2^-14 and is
+// nothing below 2^-25, while the sum, in 32 bits, counts it.  They reach 2^8 (see
+// weights()) and float16 ends at 2^16, so 2^7 fits: a weight below 2^-21 of the
+// row's largest is off by up to 2^-32 of that.  The division takes the factor out
+// again, the log-sum-exp subtracts it.
+template <typename T>
+constexpr float kRaise = std::is_same<T, _Float16>::value ? 7.0f : 0.0f;
+
 // What a lane keeps of its row.
 template <int D>
 struct Row {
@@ -668,7 +676,7 @@ __device__ __forceinline__ void weights(Row<D>& r, v16f (&s)[NB], typename Vec8<
             for (int i = 0; i < 16; i++)
                 r.o[d][i] *= keep;
     }
-    const float base = r.m == -INFINITY ? 0.0f : r.m * scale2;
+    const float base = r.m == -INFINITY ? 0.0f : r.m * scale2 - kRaise<T>;
     const v16f now[NB] = {s[0], s[NB - 1]};
     beside();
     float sum = 0;
@@ -745,7 +753,8 @@ __device__ __forceinline__ void write_row(const AttnIn& a, const Unit& u, uint32
         return;
     const float inv = l > 0 || l != l ? 1.0f / l : 0.0f;
     const bool seen = l > 0 || l != l;
-    const float lse = seen ? (r.m * a.scale2 + __builtin_log2f(l)) * 0.69314718055994531f : -INFINITY;
+    const float lse =
+        seen ? (r.m * a.scale2 + (__builtin_log2f(l) - kRaise<T>)) * 0.69314718055994531f : -INFINITY;
     if (u.flags & kUnitParts) {
         const uint64_t at = u.part0 + ((uint64_t)h * rows + row) * u.chunks + chunk;
         float* o = a.part + at * D;
@@ -1091,7 +1100,7 @@ __device__ __forceinline__ void narrow_tile(const AttnIn& a, const Tile& t, uint
             for (int d = 0; d < kBlocks; d++)
                 o[d] *= keep;
         }
-        const float base = m == -INFINITY ? 0.0f : m * a.scale2;
+        const float base = m == -INFINITY ? 0.0f : m * a.scale2 - kRaise<T>;
         // light weights are summed before they meet a sum that a heavy one may be in
         float sum = 0;
 #pragma unroll
@@ -1207,7 +1216,8 @@ __device__ __forceinline__ void narrow_tile(const AttnIn& a, const Tile& t, uint
             write_four<T, D>(a, t, row, d * 16 + g * 4, x);
     }
     if (wave == 0 && g == 0 && row <= t.last) {
-        const float lse = seen ? (all * a.scale2 + __builtin_log2f(total)) * 0.69314718055994531f : -INFINITY;
+        const float lse =
+            seen ? (all * a.scale2 + (__builtin_log2f(total) - kRaise<T>)) * 0.69314718055994531f : -INFINITY;
         if (t.u.flags & kUnitParts)
             a.part_lse[t.u.part0 + ((uint64_t)t.h * t.rows + row) * t.u.chunks + t.chunk] = lse;
         else if (a.lse)

@@ -2,7 +2,8 @@
 
 Bounds, per element (u: half a unit in the last place of the type, 2^-8 for bfloat16, 2^-11 for float16): the output is
 rounded once, u |out|; a weight that is rounded once before it meets the values is off by u of itself, u sum w|v| / sum
-w; sums in 32 bits add some 2^-20 of sum w|v| / sum w.  The log-sum-exp is in 32 bits: 2^-18 of the largest |score|, and
+w; a float16 weight is raised by 2^7, so that one below 2^-21 of the row's largest is off by up to 2^-32 of that, n
+2^-32 max|v| over n keys; sums in 32 bits add some 2^-20 of sum w|v| / sum w.  The log-sum-exp is in 32 bits: 2^-18 of the largest |score|, and
 of itself.
 """
 import pytest
@@ -11,7 +12,7 @@ pytestmark = pytest.mark.gpu
 
 torch = pytest.importorskip("torch")
 
-from test_gpu_attn import DT, engine  # noqa: E402
+from test_gpu_attn import DT, ULP, engine  # noqa: E402
 
 
 def light_weights(dtype, heads, dim, where):
@@ -48,3 +49,16 @@ def test_many_light_weights_are_summed(heads, dtype, dim, where):
     """In a narrow tile (one row) and in a wide one (32)."""
     _, lse, _, _, far = light_weights(dtype, heads, dim, where)
     assert bool(((lse.double() - far).abs() <= 2.0 ** -18 * 36).all()), float((lse.double() - far).abs().max())
+
+
+@pytest.mark.parametrize("where", ["first", "middle", "last"])
+@pytest.mark.parametrize("dim", [64, 128, 256])
+@pytest.mark.parametrize("heads", [1, 32])
+def test_many_light_float16_weights(heads, dim, where):
+    """Weights of 2^-24.5 of the largest keep most of their bits."""
+    out, _, w, vals, _ = light_weights("f16", heads, dim, where)
+    want, mean = w @ vals, w @ vals.abs()
+    tol = ULP["f16"] * (want.abs() + mean) * 1.02 + 2.0 ** -20 * mean + len(w) * 2.0 ** -32 * vals.abs().max() + 2.0 ** -25
+    assert 0.005 < float(want.mean()) < 0.006 and float(tol.max()) < 1e-4
+    err = (out.double() - want).abs()
+    assert bool((err <= tol).all()), float((err / tol).max())
