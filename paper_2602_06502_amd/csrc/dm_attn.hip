@@ -20,7 +20,8 @@
 //
 //   narrow tiles: 16 rows, on 16x16x32 instructions; the four waves take every
 //     fourth 32 keys, each through its own part of LDS, and are joined at the
-//     end.  For rows that are few: bound by reading the pages.
+//     end.  Weights meet the values in two parts, as exactly as 32 bits nearly.
+//     For rows that are few: bound by reading the pages.
 //   wide tiles: 128 rows, 32 a wave, on a shared tile of 64 keys (two in LDS).
 //     Bound by the matrix and vector units: two prompts of 7,000 to 8,192 tokens, 32
 //     query and 8 key heads of 128, 895 us, 970 TFLOP/s.
@@ -1064,7 +1065,9 @@ __device__ __forceinline__ void narrow_tile(const AttnIn& a, const Tile& t, uint
         o[d] = v4f{};
     uint16_t* kt = lds + wave * 2 * kNarrowKeys * D;
     uint16_t* vt = kt + kNarrowKeys * D;
-    V p;
+    // weights, and what their rounding has left out: the matrix unit has time for both
+    // (4% busy with the weights alone, in 64 rows on up to 8,192 keys)
+    V p, rest;
     // scores and weights of the tile in LDS
     auto weigh = [&](uint32_t key, bool masked) {
         v4f s[2];
@@ -1108,6 +1111,7 @@ __device__ __forceinline__ void narrow_tile(const AttnIn& a, const Tile& t, uint
             const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i / 4][i % 4], a.scale2, -base));
             sum += w;
             p[i] = (T)w;
+            rest[i] = (T)(w - (float)p[i]);
         }
         l += sum;
     };
@@ -1149,6 +1153,7 @@ __device__ __forceinline__ void narrow_tile(const AttnIn& a, const Tile& t, uint
                 typedef short v8s __attribute__((ext_vector_type(8)));
                 const v8s f = __builtin_shufflevector(v0, v1, 0, 1, 2, 3, 4, 5, 6, 7);
                 o[d] = mfma(__builtin_bit_cast(V, f), p, o[d]);
+                o[d] = mfma(__builtin_bit_cast(V, f), rest, o[d]);
             }
         }
         while (key < t.key1) {
@@ -1160,7 +1165,7 @@ __device__ __forceinline__ void narrow_tile(const AttnIn& a, const Tile& t, uint
 #pragma unroll
                 for (int i = 0; i < 8; i++)
                     if (k / 16 * 4 + k % 4 == (uint32_t)i)
-                        w = (float)p[i];
+                        w = (float)p[i] + (float)rest[i];
                 w = __shfl(w, (k % 16) / 4 * 16 + row16);
                 const bool seen = key + k < end;
 #pragma unroll

@@ -3,7 +3,8 @@
 Bounds, per element (u: half a unit in the last place of the type, 2^-8 for bfloat16, 2^-11 for float16): the output is
 rounded once, u |out|; a weight that is rounded once before it meets the values is off by u of itself, u sum w|v| / sum
 w; a float16 weight is raised by 2^7, so that one below 2^-21 of the row's largest is off by up to 2^-32 of that, n
-2^-32 max|v| over n keys; sums in 32 bits add some 2^-20 of sum w|v| / sum w.  The log-sum-exp is in 32 bits: 2^-18 of the largest |score|, and
+2^-32 max|v| over n keys; sums in 32 bits add some 2^-20 of sum w|v| / sum w.  In narrow tiles (up to 16 rows a KV head) a weight
+meets the values in two parts, the second what the first's rounding has left out: off by u^2 of itself.  The log-sum-exp is in 32 bits: 2^-18 of the largest |score|, and
 of itself.
 """
 import pytest
@@ -12,7 +13,7 @@ pytestmark = pytest.mark.gpu
 
 torch = pytest.importorskip("torch")
 
-from test_gpu_attn import DT, ULP, engine  # noqa: E402
+from test_gpu_attn import DT, ULP, Batch, engine  # noqa: E402
 
 
 def light_weights(dtype, heads, dim, where):
@@ -62,3 +63,40 @@ def test_many_light_float16_weights(heads, dim, where):
     assert 0.005 < float(want.mean()) < 0.006 and float(tol.max()) < 1e-4
     err = (out.double() - want).abs()
     assert bool((err <= tol).all()), float((err / tol).max())
+
+
+def magnitudes(b):
+    """sum w|v| / sum w of each row, and the keys that each token sees."""
+    T = int(b.q_off[-1])
+    mean, keys = torch.zeros((T, b.hq, b.dim), dtype=torch.float64), torch.zeros((T, 1, 1), dtype=torch.float64)
+    q = b.qrows.unflatten(1, (b.hq, b.dim)).double()
+    ratio = b.hq // b.hkv
+    for s in range(len(b.len)):
+        L, t0, t1 = int(b.len[s]), int(b.q_off[s]), int(b.q_off[s + 1])
+        at = torch.from_numpy(b.page[b.off[s]:b.off[s + 1]].astype("int64"))
+        for t in range(t0, t1):
+            n = L - t1 + t + 1
+            keys[t] = n
+            for h in range(b.hkv):
+                K, V = (x[0][at, h].reshape(-1, b.dim)[:n].double() for x in (b.k, b.v))
+                w = torch.softmax(q[t, h * ratio:(h + 1) * ratio] @ K.T * b.scale(), -1)
+                mean[t, h * ratio:(h + 1) * ratio] = w @ V.abs()
+    return mean, keys
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("dim,heads", [(64, (14, 2)), (128, (32, 8)), (256, (4, 4))])
+def test_few_rows_are_rounded_once(dtype, dim, heads):
+    """Single tokens and drafts have the output's own rounding, and next to nothing of the weights'."""
+    u = ULP[dtype]
+    for seqs in ([(1, 300)], [(1, 100 + 331 * i) for i in range(17)] + [(2, 5), (2, 1400), (1, 9000)]):
+        print("[case] rounded once", dtype, dim, heads, len(seqs), flush=True)
+        b = Batch(16, seqs, heads=heads, dim=dim, dtype=dtype, seed=dim)
+        out, _ = b.run()
+        ref = b.reference()[0]
+        mean, keys = magnitudes(b)
+        tol = 1.02 * u * ref.abs() + (1.02 * u * u + 2.0 ** -20) * mean
+        if dtype == "f16":
+            tol = tol + keys * 2.0 ** -32 * float(b.v[~b.v.isnan()].abs().max()) + 2.0 ** -25
+        err = (out.double() - ref).abs()
+        assert bool((err <= tol).all()), float((err / tol).max())
