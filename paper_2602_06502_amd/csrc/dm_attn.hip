@@ -510,6 +510,7 @@ __global__ __launch_bounds__(kPlanThreads) void attn_plan_kernel(PlanIn a, PlanV
 // The pass over the keys.
 // ---------------------------------------------------------------------------
 
+typedef float v2f __attribute__((ext_vector_type(2)));
 typedef float v4f __attribute__((ext_vector_type(4)));
 typedef float v16f __attribute__((ext_vector_type(16)));
 typedef short v4s __attribute__((ext_vector_type(4)));
@@ -556,8 +557,8 @@ struct AttnIn {
     const uint16_t* q;
     uint16_t* out;
     float* lse;
-    float* part;       // [part rows][D] parts of rows, then their lse
-    float* part_lse;
+    float* part;       // [part rows][D] parts of rows
+    v2f* part_stat;    // [part rows] their maxima (of raw scores) and sums
     int64_t q_stride, out_stride;
     uint32_t n_pages, q_heads, kv_heads, ratio;
     float scale2;      // scale * log2(e)
@@ -741,6 +742,13 @@ __device__ __forceinline__ void add_odd_values(Row<D>& r, const typename Vec8<T>
     }
 }
 
+// log sum exp(scale score), from the maximum and the raised weights' sum.
+template <typename T>
+__device__ __forceinline__ float lse_of(float m, float l, float scale2)
+{
+    return (m * scale2 + (__builtin_log2f(l) - kRaise<T>)) * 0.69314718055994531f;
+}
+
 // The result of a row (o: O^T as in Row): divided by the sum, written to the
 // output or to its row of parts (rows: of the unit; rows from `end` on are not
 // the tile's).
@@ -754,8 +762,6 @@ __device__ __forceinline__ void write_row(const AttnIn& a, const Unit& u, uint32
         return;
     const float inv = l > 0 || l != l ? 1.0f / l : 0.0f;
     const bool seen = l > 0 || l != l;
-    const float lse =
-        seen ? (r.m * a.scale2 + (__builtin_log2f(l) - kRaise<T>)) * 0.69314718055994531f : -INFINITY;
     if (u.flags & kUnitParts) {
         const uint64_t at = u.part0 + ((uint64_t)h * rows + row) * u.chunks + chunk;
         float* o = a.part + at * D;
@@ -769,7 +775,7 @@ __device__ __forceinline__ void write_row(const AttnIn& a, const Unit& u, uint32
                 *reinterpret_cast<v4f*>(o + d * 32 + i * 2 + half * 4) = x;
             }
         if (half == 0)
-            a.part_lse[at] = lse;
+            a.part_stat[at] = v2f{r.m, l};
         return;
     }
     const uint32_t t = u.tok0 + row / a.ratio, x = h * a.ratio + row % a.ratio;
@@ -785,7 +791,7 @@ __device__ __forceinline__ void write_row(const AttnIn& a, const Unit& u, uint32
             *reinterpret_cast<v4t*>(o + d * 32 + i * 2 + half * 4) = y;
         }
     if (half == 0 && a.lse)
-        a.lse[(uint64_t)t * a.q_heads + x] = lse;
+        a.lse[(uint64_t)t * a.q_heads + x] = seen ? lse_of<T>(r.m, l, a.scale2) : -INFINITY;
 }
 
 // The last of up to kEarlyUnits units with item0 <= item, by one wait.
@@ -1221,12 +1227,11 @@ __device__ __forceinline__ void narrow_tile(const AttnIn& a, const Tile& t, uint
             write_four<T, D>(a, t, row, d * 16 + g * 4, x);
     }
     if (wave == 0 && g == 0 && row <= t.last) {
-        const float lse =
-            seen ? (all * a.scale2 + (__builtin_log2f(total) - kRaise<T>)) * 0.69314718055994531f : -INFINITY;
         if (t.u.flags & kUnitParts)
-            a.part_lse[t.u.part0 + ((uint64_t)t.h * t.rows + row) * t.u.chunks + t.chunk] = lse;
+            a.part_stat[t.u.part0 + ((uint64_t)t.h * t.rows + row) * t.u.chunks + t.chunk] = v2f{all, total};
         else if (a.lse)
-            a.lse[(uint64_t)(t.u.tok0 + row / a.ratio) * a.q_heads + t.h * a.ratio + row % a.ratio] = lse;
+            a.lse[(uint64_t)(t.u.tok0 + row / a.ratio) * a.q_heads + t.h * a.ratio + row % a.ratio] =
+                seen ? lse_of<T>(all, total, a.scale2) : -INFINITY;
     }
 }
 
@@ -1510,6 +1515,15 @@ __device__ __forceinline__ Parts parts_of(const Unit& u, uint32_t t, uint32_t x,
 
 constexpr float kLog2e = 1.44269504088896341f;
 
+// The weight of a part among parts whose largest maximum is m.  (Their maxima and sums
+// are kept apart: in one number, the log-sum-exp, scores of 2^14 would leave the sum
+// eleven bits.)  A part that the row sees nothing of has none; NaN stays NaN.
+__device__ __forceinline__ float part_weight(v2f stat, float m, float scale2)
+{
+    const float w = stat[1] * __builtin_amdgcn_exp2f((stat[0] - m) * scale2);
+    return stat[1] == 0 ? 0.0f : stat[0] == -INFINITY ? stat[1] : w;
+}
+
 // Neighbouring rows of the output by a wave, four at a time (16 lanes a row, D / 16
 // elements a lane); a row's sequence is looked for only where it is not the last
 // one's.  Bound by reading the parts: 95,488 rows of 64 in two parts 16.6 us, 105,600
@@ -1539,12 +1553,12 @@ __device__ __forceinline__ void join_quarters(const AttnIn& a, const PlanView& p
         for (uint32_t i0 = 0; __any(live && i0 < p.n); i0 += kAtOnce) {
             if (!live || i0 >= p.n)
                 continue;
-            float e[kAtOnce];
+            v2f e[kAtOnce];
             v4f r[kAtOnce][kPer / 4];
 #pragma unroll
             for (int j = 0; j < kAtOnce; j++) {
                 const uint64_t at = p.at(i0 + j < p.n ? i0 + j : p.n - 1);
-                e[j] = a.part_lse[at];
+                e[j] = a.part_stat[at];
 #pragma unroll
                 for (int c = 0; c < kPer / 4; c++)
                     r[j][c] = *reinterpret_cast<const v4f*>(a.part + at * D + d + c * 4);
@@ -1553,10 +1567,10 @@ __device__ __forceinline__ void join_quarters(const AttnIn& a, const PlanView& p
 #pragma unroll
             for (int j = 0; j < kAtOnce; j++) {
                 if (i0 + j >= p.n)
-                    e[j] = -INFINITY;
-                now = fmaxf(now, e[j]);
+                    e[j] = v2f{-INFINITY, 0};
+                now = fmaxf(now, e[j][0]);
             }
-            const float keep = m == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f((m - now) * kLog2e);
+            const float keep = m == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f((m - now) * a.scale2);
             m = now;
             total *= keep;
 #pragma unroll
@@ -1564,8 +1578,7 @@ __device__ __forceinline__ void join_quarters(const AttnIn& a, const PlanView& p
                 v[c] *= keep;
 #pragma unroll
             for (int j = 0; j < kAtOnce; j++) {
-                // a part that the row sees nothing of has no weight; NaN stays NaN
-                const float w = e[j] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f((e[j] - m) * kLog2e);
+                const float w = part_weight(e[j], m, a.scale2);
                 total += w;
 #pragma unroll
                 for (int c = 0; c < kPer; c++)
@@ -1587,15 +1600,19 @@ __device__ __forceinline__ void join_quarters(const AttnIn& a, const PlanView& p
             *reinterpret_cast<v4t*>(out + c * 4) = z;
         }
         if (d == 0 && a.lse)
-            a.lse[(uint64_t)t * a.q_heads + x] = seen ? m + __builtin_log2f(total) * 0.69314718055994531f : -INFINITY;
+            a.lse[(uint64_t)t * a.q_heads + x] = seen ? lse_of<T>(m, total, a.scale2) : -INFINITY;
     }
 }
 
 // MANY: more rows than waves (a kernel of its own: its registers would halve the
-// waves of the other).
+// waves of the other).  Waves a SIMD: all eight of the other up to heads of 128 (seven:
+// 1.2 us more for 8,192 rows), seven of this one for heads of 64 (six: 2 us more for
+// 95,488 rows).
 template <typename T, int D, bool MANY>
-__global__ __launch_bounds__(kThreads) void attn_join_kernel(AttnIn a, const PlanView pv,
-                                                             uint64_t part_rows, uint32_t items)
+__global__ __launch_bounds__(kThreads, D == 64 && MANY ? 7 : MANY || D == 256 ? 1 : 8) void attn_join_kernel(AttnIn a,
+                                                                                       const PlanView pv,
+                                                                                       uint64_t part_rows,
+                                                                                       uint32_t items)
 {
     constexpr int kPer = D / kWave;  // elements a lane
     __shared__ float acc[kWaves][D];
@@ -1634,26 +1651,27 @@ __global__ __launch_bounds__(kThreads) void attn_join_kernel(AttnIn a, const Pla
                     four[j][c] = at[c];
             }
         };
-        float m = -INFINITY, e0 = -INFINITY;
+        const v2f none = {-INFINITY, 0};
+        float m = -INFINITY;
+        v2f e0 = none;
         if (n) {
             if (from + lane < n)
-                e0 = a.part_lse[place(from + lane)];
+                e0 = a.part_stat[place(from + lane)];
             read_four(from);  // beside the weights' reads
         }
         if (together)
             for (uint32_t i = lane; i < n; i += kWave)
-                m = fmaxf(m, a.part_lse[place(i)]);
+                m = fmaxf(m, a.part_stat[place(i)][0]);
         else
-            m = e0;
+            m = e0[0];
 #pragma unroll
         for (int o = 1; o < kWave; o *= 2)
             m = fmaxf(m, __shfl_xor(m, o));
         float v[kPer] = {}, total = 0;
         for (uint32_t i0 = from; i0 < n; i0 += by) {
             const uint32_t i = i0 + lane;
-            const float e = i0 == from ? e0 : i < n ? a.part_lse[place(i)] : -INFINITY;
-            // a part that the row sees nothing of has no weight; NaN stays NaN
-            const float w = e == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f((e - m) * kLog2e);
+            const v2f e = i0 == from ? e0 : i < n ? a.part_stat[place(i)] : none;
+            const float w = part_weight(e, m, a.scale2);
             total += w;
             const uint32_t k1 = n - i0 < kWave ? n - i0 : kWave;
             for (uint32_t k = 0; k < k1; k += 4) {
@@ -1710,7 +1728,7 @@ __global__ __launch_bounds__(kThreads) void attn_join_kernel(AttnIn a, const Pla
         *reinterpret_cast<vt*>(a.out + t * a.out_stride + (uint64_t)x * D + lane * kPer) = z;
         if (lane == 0 && a.lse)
             a.lse[(uint64_t)t * a.q_heads + x] =
-                seen ? m + __builtin_log2f(total) * 0.69314718055994531f : -INFINITY;
+                seen ? lse_of<T>(m, total, a.scale2) : -INFINITY;
     }
 }
 
@@ -1786,7 +1804,7 @@ hipError_t attn(dm_ctx* c, const dm_token_batch& b, const dm_kv_pages& kv, uint3
     const uint64_t rows = is_small ? 0 : part_rows_of(c, b.q_tokens, q_heads);
     hipError_t e;
     float* part =
-        is_small ? nullptr : static_cast<float*>(scratch_get(c, kSlotPages, rows * (kv.head_dim + 1) * 4, &e));
+        is_small ? nullptr : static_cast<float*>(scratch_get(c, kSlotPages, rows * (kv.head_dim + 2) * 4, &e));
     if (!part && !is_small)
         return e;
     AttnIn a;
@@ -1797,7 +1815,7 @@ hipError_t attn(dm_ctx* c, const dm_token_batch& b, const dm_kv_pages& kv, uint3
     a.out = static_cast<uint16_t*>(out);
     a.lse = lse;
     a.part = part;
-    a.part_lse = is_small ? nullptr : part + rows * kv.head_dim;
+    a.part_stat = is_small ? nullptr : reinterpret_cast<v2f*>(part + rows * kv.head_dim);
     a.q_stride = q_stride;
     a.out_stride = out_stride;
     a.n_pages = kv.n_pages;

@@ -7,6 +7,9 @@ w; a float16 weight is raised by 2^7, so that one below 2^-21 of the row's large
 meets the values in two parts, the second what the first's rounding has left out: off by u^2 of itself.  The log-sum-exp is in 32 bits: 2^-18 of the largest |score|, and
 of itself.
 """
+import math
+
+import numpy as np
 import pytest
 
 pytestmark = pytest.mark.gpu
@@ -100,3 +103,26 @@ def test_few_rows_are_rounded_once(dtype, dim, heads):
             tol = tol + keys * 2.0 ** -32 * float(b.v[~b.v.isnan()].abs().max()) + 2.0 ** -25
         err = (out.double() - ref).abs()
         assert bool((err <= tol).all()), float((err / tol).max())
+
+
+def exact_scores(dtype, dim, heads, seqs, power, r):
+    """A batch whose scores are 2^power times whole numbers from -3 to 3, so that they are exact in 32 bits: the keys of the
+    largest share the weight (at 2^10 and above, whatever a row's largest is)."""
+    b = Batch(16, seqs, heads=heads, dim=dim, dtype=dtype, seed=dim)
+    b.qrows.zero_()
+    b.qrows.unflatten(1, (b.hq, dim))[:, :, 0] = 2.0 ** (power // 2)
+    b.k[~b.k.isnan()] = 0
+    small = torch.from_numpy(r.integers(-3, 4, size=tuple(b.k.shape[:4]))).double()
+    b.k[..., 0] = torch.where(b.k[..., 0].isnan(), math.nan, small * 2.0 ** (power - power // 2)).to(DT[dtype])
+    return b
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("dim,heads", [(64, (4, 2)), (128, (16, 1)), (256, (6, 3))])
+def test_rows_in_parts_with_large_scores(dtype, dim, heads):
+    """Parts of a row whose largest scores are equal count by their sums, however large the scores are."""
+    r = np.random.default_rng(dim)
+    for seqs in ([(3, 200), (1, 33), (40, 130), (70, 70)], [(1, 2500), (2, 4000), (1, 16)]):
+        for power in (10, 14, 18):
+            print("[case] parts, scores of 2 to the", power, dtype, dim, heads, len(seqs), flush=True)
+            exact_scores(dtype, dim, heads, seqs, power, r).check(scale=1.0)
