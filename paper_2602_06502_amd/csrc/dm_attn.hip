@@ -577,7 +577,16 @@ template <int D>
 struct Row {
     v16f o[D / 32];  // O^T: element (d = db * 32 + (i / 4) * 8 + half * 4 + i % 4, row)
     float m, l;      // maximum (of raw scores), this half's sum
+    bool far;        // scores_are_far(), of some row of the wave
 };
+
+// Scores are scaled and the base taken off in one rounding, which leaves every weight
+// of a row the same factor: 2 to half a unit in the base's last place.  From 2^20 on,
+// before that factor could overflow or lose the weights, the maximum is taken off first.
+__device__ __forceinline__ bool scores_are_far(float m, float scale2)
+{
+    return __any(m != -INFINITY && !(fabsf(m * scale2) < 0x1p20f));
+}
 
 // A tile of 32 keys for a wave's 32 rows: s holds S^T (key = (i / 4) * 8 + half
 // * 4 + i % 4).
@@ -671,6 +680,7 @@ __device__ __forceinline__ void weights(Row<D>& r, v16f (&s)[NB], typename Vec8<
         const float m = fmaxf(r.m, mx);
         const float keep = m == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f((r.m - m) * scale2);
         r.m = m;
+        r.far = scores_are_far(m, scale2);
         r.l *= keep;
 #pragma unroll
         for (int d = 0; d < D / 32; d++)
@@ -678,7 +688,16 @@ __device__ __forceinline__ void weights(Row<D>& r, v16f (&s)[NB], typename Vec8<
             for (int i = 0; i < 16; i++)
                 r.o[d][i] *= keep;
     }
-    const float base = r.m == -INFINITY ? 0.0f : r.m * scale2 - kRaise<T>;
+    if (r.far) {
+        float m = r.m == -INFINITY ? 0.0f : r.m;
+        asm volatile("" : "+v"(m));  // as above
+#pragma unroll
+        for (int b = 0; b < NB; b++)
+#pragma unroll
+            for (int i = 0; i < 16; i++)
+                s[b][i] -= m;
+    }
+    const float base = r.m == -INFINITY ? 0.0f : r.m * (r.far ? 0.0f : scale2) - kRaise<T>;
     const v16f now[NB] = {s[0], s[NB - 1]};
     beside();
     float sum = 0;
@@ -910,6 +929,7 @@ __device__ __forceinline__ void clear(Row<D>& r)
 {
     r.m = -INFINITY;
     r.l = 0;
+    r.far = false;
 #pragma unroll
     for (int d = 0; d < D / 32; d++)
         r.o[d] = v16f{};
@@ -1066,6 +1086,7 @@ __device__ __forceinline__ void narrow_tile(const AttnIn& a, const Tile& t, uint
     const uint32_t limit = sees(t.u, a.ratio, in_tile), end = limit < t.key1 ? limit : t.key1;
     v4f o[kBlocks];
     float m = -INFINITY, l = 0;
+    bool far = false;
 #pragma unroll
     for (int d = 0; d < kBlocks; d++)
         o[d] = v4f{};
@@ -1104,12 +1125,19 @@ __device__ __forceinline__ void narrow_tile(const AttnIn& a, const Tile& t, uint
             const float now = fmaxf(m, mx);
             const float keep = now == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f((m - now) * a.scale2);
             m = now;
+            far = scores_are_far(m, a.scale2);
             l *= keep;
 #pragma unroll
             for (int d = 0; d < kBlocks; d++)
                 o[d] *= keep;
         }
-        const float base = m == -INFINITY ? 0.0f : m * a.scale2 - kRaise<T>;
+        float base = m == -INFINITY ? 0.0f : m * a.scale2 - kRaise<T>;
+        if (far) {
+            const float top = m == -INFINITY ? 0.0f : m;
+            s[0] -= top;
+            s[1] -= top;
+            base = -kRaise<T>;
+        }
         // light weights are summed before they meet a sum that a heavy one may be in
         float sum = 0;
 #pragma unroll

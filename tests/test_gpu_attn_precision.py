@@ -126,3 +126,14 @@ def test_rows_in_parts_with_large_scores(dtype, dim, heads):
         for power in (10, 14, 18):
             print("[case] parts, scores of 2 to the", power, dtype, dim, heads, len(seqs), flush=True)
             exact_scores(dtype, dim, heads, seqs, power, r).check(scale=1.0)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("dim,heads", [(64, (4, 2)), (128, (16, 1)), (256, (6, 3))])
+def test_scores_of_any_size(dtype, dim, heads):
+    """Finite scores from 2^10 to 2^60 (bfloat16) or 2^26 (float16): drafts in narrow tiles, a prompt in wide ones, few rows."""
+    r = np.random.default_rng(dim)
+    for seqs in ([(2, 90)], [(3, 200), (1, 33), (40, 130), (70, 70)]):
+        for power in range(10, (26 if dtype == "f16" else 60) + 1, 4):
+            print("[case] scores of 2 to the", power, dtype, dim, heads, len(seqs), flush=True)
+            exact_scores(dtype, dim, heads, seqs, power, r).check(scale=1.0)
