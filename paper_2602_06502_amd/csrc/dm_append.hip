@@ -165,8 +165,9 @@ __global__ __launch_bounds__(kThreads, 6) void append_kernel(AppendIn a, uint32_
 #pragma unroll
                 for (int i = 0; i < 8; i += 2) {
                     const float u = x[i], v = x[i + 1];
-                    x[i] = u * cs[i / 2] - v * sn[i / 2];
-                    x[i + 1] = v * cs[i / 2] + u * sn[i / 2];
+                    // (a pair past the rotation is left as it is: 0 times infinity is NaN)
+                    x[i] = turns ? u * cs[i / 2] - v * sn[i / 2] : u;
+                    x[i + 1] = turns ? v * cs[i / 2] + u * sn[i / 2] : v;
                 }
             } else if (a.rot) {
                 const v4u32 mine = __builtin_bit_cast(v4u32, row);
