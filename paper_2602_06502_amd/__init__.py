@@ -689,7 +689,7 @@ class DualMap:
             wq = self._dev(q_norm, dt, "q_norm").data_ptr()
         if k_norm is not None:
             wk = self._dev(k_norm, dt, "k_norm").data_ptr()
-        if (wq and q_norm.numel() != D) or (wk and k_norm.numel() != D):
+        if (q_norm is not None and q_norm.numel() != D) or (k_norm is not None and k_norm.numel() != D):
             raise ValueError("q_norm and k_norm need head_dim weights")
         if cos is not None or sin is not None:
             f32 = self.torch.float32

@@ -1,4 +1,4 @@
-"""What appending does to values that are not finite."""
+"""What appending does to values that are not finite, and arguments that it refuses."""
 import pytest
 
 pytestmark = pytest.mark.gpu
@@ -39,3 +39,18 @@ def test_elements_past_the_rotation_pass_as_they_are(interleaved, dim, rot, dtyp
         assert torch.equal(got[..., rot:].isnan(), given[..., rot:].isnan())
         assert torch.equal(got[..., rot:].nan_to_num(7, 8, 9), given[..., rot:].nan_to_num(7, 8, 9))
         assert bool(got[..., :rot].isfinite().all())
+
+
+def test_norms_without_weights_are_refused():
+    """Weights of no elements are not the absence of a norm."""
+    pk, e = engine(16)
+    kp, vp = (torch.zeros((1, 1, 1, 16, 64), dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    i64 = dict(dtype=torch.int64, device="cuda")
+    tables = (torch.tensor([0, 1], **i64), torch.zeros(1, dtype=torch.int32, device="cuda"), torch.tensor([1], **i64))
+    q = torch.zeros((1, 1, 64), dtype=torch.bfloat16, device="cuda")
+    for name in ("q_norm", "k_norm"):
+        for size in (0, 63, 128):
+            with pytest.raises(ValueError, match="head_dim"):
+                e.kv_append(pk.KVPages(kp, vp), 0, tables, torch.tensor([0, 1], **i64), q, q, q, q,
+                            **{name: torch.ones(size, dtype=torch.bfloat16, device="cuda")})
+    e.sync()
