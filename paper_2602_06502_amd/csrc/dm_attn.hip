@@ -1272,7 +1272,7 @@ __device__ __forceinline__ void send16(const uint16_t* from, uint32_t lds_at)
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off"
                  :
                  : "s"(lds_at), "v"(from)
-                 : "memory");
+                 : "m0", "memory");
 }
 // The same from a uniform address and a lane's bytes on from it.  (Five wait states
 // between a vector instruction that may have written the address, such as the reload
@@ -1282,7 +1282,7 @@ __device__ __forceinline__ void send16(const uint16_t* from, uint32_t lane_at, u
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tglobal_load_lds_dwordx4 %1, %2"
                  :
                  : "s"(lds_at), "v"(lane_at), "s"(from)
-                 : "memory");
+                 : "m0", "memory");
 }
 __device__ __forceinline__ void wait_sent() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
 
