@@ -24,16 +24,6 @@ struct Vec8<_Float16> {
     using type = v8hf;
 };
 
-template <typename T>
-__device__ __forceinline__ void load8(const uint16_t* p, float (&x)[8])
-{
-    using V = typename Vec8<T>::type;
-    const V v = *reinterpret_cast<const V*>(p);
-#pragma unroll
-    for (int i = 0; i < 8; i++)
-        x[i] = (float)v[i];
-}
-
 // Rounds to nearest, ties to even.
 template <typename T>
 __device__ __forceinline__ void store8(uint16_t* p, const float (&x)[8])
