@@ -616,9 +616,11 @@ dm_status dm_kv_append(dm_ctx* ctx, const dm_kv_pages* kv, uint32_t layer,
  * length 0; one with a page out of range gets no defined result; both are
  * reported (DM_EINVAL), and so is a plan of another batch, whatever its size,
  * or of more work than q_tokens can be (q_off out of order): nothing written.
- * dm_attn's work area is the context's: its size goes by q_tokens, q_heads and
- * head_dim (it grows, synchronising once, only when a call needs more than
- * any before it). */
+ * dm_attn's work area is the context's (it grows, synchronising once, only when
+ * a call needs more than any before it): head_dim + 2 floats for each of 384
+ * rows a compute unit (51 MB at head_dim 128), and with groups for 2 * q_tokens *
+ * q_heads more, 2^20 at most (0.55 GB); a batch that would need more shares no
+ * prefix and is not cut. */
 uint64_t dm_attn_plan_bytes(uint64_t n, uint64_t groups);
 dm_status dm_attn_plan(dm_ctx* ctx, const dm_token_batch* batch, const dm_kv_pages* kv,
                        uint32_t q_heads, void* plan, uint64_t plan_bytes);

@@ -1788,11 +1788,14 @@ uint64_t most_items(const dm_ctx* c, const dm_token_batch& b, uint32_t ratio, ui
     return uncut * kv_heads + cuts;
 }
 
-// Rows of parts that a batch can need: twice its rows (a shared prefix and the
-// rest), up to a bound, and those of cut items.
-uint64_t part_rows_of(const dm_ctx* c, uint64_t q_tokens, uint32_t q_heads)
+// Rows of parts that a batch can need: those of cut units, and with runs twice its
+// rows (a shared prefix and the rest), up to a bound past which the plan neither
+// shares nor cuts.  Cut units: a chunk is longer than an item's share of the cost,
+// weight * keys over all units, and c chunks >= 2 take fewer than 2 keys / chunk, so
+// that they have fewer than 2 rows / weight <= 128 rows for each item wanted.
+uint64_t part_rows_of(const dm_ctx* c, const dm_token_batch& b, uint32_t q_heads)
 {
-    const uint64_t rows = 2 * q_tokens * q_heads;
+    const uint64_t rows = b.groups ? 2 * b.q_tokens * q_heads : 0;
     return (rows < kPartRows ? rows : kPartRows) + kWide * item_target(c);
 }
 
@@ -1814,7 +1817,7 @@ hipError_t attn_plan(dm_ctx* c, const dm_token_batch& b, const dm_kv_pages& kv, 
     a.ratio = q_heads / kv.kv_heads;
     a.head_dim = kv.head_dim;
     a.target = item_target(c);
-    a.part_rows = small(c, b, kv, a.ratio) ? 0 : part_rows_of(c, b.q_tokens, q_heads);
+    a.part_rows = small(c, b, kv, a.ratio) ? 0 : part_rows_of(c, b, q_heads);
     const PlanView pv = plan_view(plan, b.tables.n, b.groups);
     a.arrived = c->d_status + 48;  // a line of its own
     const uint32_t grid = !b.groups                        ? 1
@@ -1829,7 +1832,7 @@ hipError_t attn(dm_ctx* c, const dm_token_batch& b, const dm_kv_pages& kv, uint3
                 void* out, int64_t out_stride, float* lse)
 {
     const bool is_small = small(c, b, kv, q_heads / kv.kv_heads);
-    const uint64_t rows = is_small ? 0 : part_rows_of(c, b.q_tokens, q_heads);
+    const uint64_t rows = is_small ? 0 : part_rows_of(c, b, q_heads);
     hipError_t e;
     float* part =
         is_small ? nullptr : static_cast<float*>(scratch_get(c, kSlotPages, rows * (kv.head_dim + 2) * 4, &e));

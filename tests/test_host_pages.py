@@ -101,6 +101,26 @@ def scenario_growth_under_capture(x):
             x.L.dm_destroy(h)
 
 
+def scenario_attention_area(x):
+    """What attention's work area holds: 384 rows of parts a compute unit (256 of them here), and the batch's rows twice, up
+    to 2^20, only if it has runs."""
+    held = x.word("fake_bytes")
+    for tokens in (300, 4096, 16_384):
+        for dim in (64, 128, 256):
+            for groups in (0, 1):
+                h = x.create()
+                s = Pages(x, h)
+                before = held.value
+                assert s.attn(tokens, heads=(32, 8), dim=dim, groups=groups) == x.pk.DM_OK
+                rows = 384 * 256 + (min(2 * tokens * 32, 1 << 20) if groups else 0)
+                assert rows * (dim + 2) * 4 <= held.value - before <= rows * (dim + 2) * 4 + 4096, (tokens, dim, groups)
+                x.L.dm_destroy(h)
+
+
+def test_attention_work_area(fake):  # noqa: F811
+    _child(fake, "attention_area")
+
+
 def test_captured_work_areas_are_kept(fake):  # noqa: F811
     _child(fake, "captured_areas")
 
