@@ -11,6 +11,8 @@
 // launches and waits bound them.  Small calls are one workgroup with everything
 // that the passes share in LDS; in large ones passes over entries take equal
 // shares of them, however long the tables are.
+#include <algorithm>
+
 #include "dm_internal.h"
 #include "dm_pages.h"
 
@@ -483,12 +485,32 @@ __global__ __launch_bounds__(kThreads) void fork_write_kernel(ForkIn a, Work w, 
 }
 
 // ---------------------------------------------------------------------------
-// A small call in one workgroup: the same passes, what they share in LDS.  (24
-// sequences over 767 pages: 10 us, the passes above 24.)
+// A small call in one workgroup: the same passes, what they share in LDS.
 // ---------------------------------------------------------------------------
 
-constexpr uint32_t kSmallPages = 8192, kSmallRows = 1024;
+constexpr uint32_t kSmallPages = 8192, kSmallRows = 1024;  // what LDS holds
 constexpr uint64_t kSmallEntries = 32768;
+
+// Entries of tables, by the room for them: a caller that does not wait for their number
+// gives the most there can be; where that is many times the pages there are, pages
+// would have to be shared by as many sequences.
+uint64_t entries_about(uint64_t room, uint32_t n_pages) { return room < 4ull * n_pages ? room : 4ull * n_pages; }
+
+// Is a call the faster in one workgroup?  us of fork there and in passes, by pages,
+// sequences and entries: 767, 24, 600: 9.1 and 21.9; 2,048, 256, 4,096: 19.5 and 25.5;
+// 4,096, 256, 4,096: 22.5 and 26.0; 4,096, 256, 8,192: 30.2 and 25.5; 8,192, 64, 8,192:
+// 31.9 and 23.7; 8,192, 1,024, 32,768: 101 and 29.  Of compact: 2,048, 256, 4,096: 6.8
+// and 15.2; 8,192, 256, 8,192: 14.8 and 15.3; 8,192, 256, 16,384: 19.0 and 15.3; with
+// 65,536 sequences of 4,096 entries 20.7 and 75.8.
+bool fork_is_small(uint32_t n_pages, uint64_t rows, uint64_t room)
+{
+    return n_pages <= kSmallPages && rows <= kSmallRows && room <= kSmallEntries &&
+           n_pages + entries_about(room, n_pages) + 8 * rows < 12288;
+}
+bool compact_is_small(uint32_t n_pages, uint64_t room)
+{
+    return n_pages <= kSmallPages && room <= kSmallEntries && n_pages + entries_about(room, n_pages) / 2 <= 12288;
+}
 
 __global__ __launch_bounds__(kPlanThreads) void fork_small_kernel(ForkIn a, dm_pages_out out, uint32_t* status)
 {
@@ -944,8 +966,7 @@ hipError_t pages_fork(dm_ctx* c, const dm_page_tables& in, const int32_t* ref, u
     const ForkIn a{in.off, in.page, in.len, (uint32_t)in.n, (int64_t)in.entries, ref, n_pages,
                    blocks, src, keep, grow, (uint32_t)m, log2_of(c->cfg.block_size)};
     hipStream_t st = c->stream;
-    if (n_pages <= kSmallPages && in.n <= kSmallRows && m <= kSmallRows && in.entries <= kSmallEntries &&
-        out.cap <= kSmallEntries) {
+    if (fork_is_small(n_pages, std::max(in.n, m), std::max(in.entries, out.cap))) {
         fork_small_kernel<<<1, kPlanThreads, 0, st>>>(a, out, c->d_status);
         return hipGetLastError();
     }
@@ -986,7 +1007,7 @@ hipError_t pages_compact(dm_ctx* c, const dm_page_tables& in, const int32_t* ref
     const uint32_t blocks = (n_pages + kPageBlock - 1) / kPageBlock;
     const CompactIn a{in.off, in.page, (uint32_t)in.n, (int64_t)in.entries, ref, n_pages, blocks};
     hipStream_t st = c->stream;
-    if (n_pages <= kSmallPages && in.entries <= kSmallEntries) {
+    if (compact_is_small(n_pages, in.entries)) {
         compact_small_kernel<<<1, kPlanThreads, 0, st>>>(a, out, c->d_status);
         return hipGetLastError();
     }

@@ -121,6 +121,34 @@ def test_attention_work_area(fake):  # noqa: F811
     _child(fake, "attention_area")
 
 
+def scenario_small_calls(x):
+    """Calls on page tables go in one workgroup where that is the faster, by pages, sequences and room for entries."""
+    h, runs = x.create(), x.word("fake_launches")
+    s = Pages(x, h)
+
+    def launches(call, *a, **k):
+        before = runs.value
+        assert call(*a, **k) == x.pk.DM_OK
+        return runs.value - before
+
+    for pages, n, entries, one in ((767, 24, 600, True), (767, 24, 32_768, True), (2048, 256, 4096, True),
+                                   (4096, 256, 4096, True), (4096, 256, 8192, False), (8192, 64, 8192, False),
+                                   (8192, 1024, 8192, False), (8192, 256, 32_768, False), (8192, 1024, 32_768, False),
+                                   (1000, 1025, 1000, False), (8193, 1, 1, False), (1, 1, 32_769, False), (1, 1, 0, True)):
+        for rows, room in (((n, n), (entries, entries)), ((n, 1), (entries, 1)), ((1, n), (1, entries))):
+            got = launches(s.fork, rows[0], rows[1], pages, entries=room[0], cap=room[1])
+            assert got == (1 if one else 5), (pages, n, entries, got)
+    for pages, n, entries, one in ((767, 24, 600, True), (767, 24, 32_768, True), (2048, 256, 4096, True), (8192, 256, 8192, True),
+                                   (4096, 256, 16_384, True), (8192, 256, 16_384, False), (8192, 65_536, 4096, True),
+                                   (8192, 256, 32_768, False), (8193, 1, 1, False), (1, 1, 32_769, False)):
+        got = launches(s.compact, n, pages, entries=entries)
+        assert got == (1 if one else 4), (pages, n, entries, got)
+
+
+def test_page_table_calls_in_one_workgroup(fake):  # noqa: F811
+    _child(fake, "small_calls")
+
+
 def test_captured_work_areas_are_kept(fake):  # noqa: F811
     _child(fake, "captured_areas")
 
