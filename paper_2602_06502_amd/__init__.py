@@ -655,6 +655,8 @@ class DualMap:
         tb = self._tables(tables)
         if self._dev(q_off, i64, "q_off").numel() != tb[3] + 1:
             raise ValueError("q_off needs one entry more than len")
+        if not 0 <= q_tokens < 1 << 31:
+            raise ValueError("q_tokens must be at least 0 and below 2^31")
         if groups is None:
             return tb + (q_off.data_ptr(), q_tokens, 0, 0)
         if self._dev(groups, i64, "groups").numel() < 1:

@@ -32,3 +32,14 @@ def test_tokens_out_of_order_write_nothing():
         e.sync()
     assert x.value.status == pk.DM_EINVAL
     assert bool((out == 7).all()) and bool((lse == 7).all())
+
+
+@pytest.mark.parametrize("tokens", [-1, 2 ** 31, 2 ** 64])
+def test_token_counts_out_of_range_are_refused(tokens):
+    pk, e = engine(16)
+    k = torch.zeros((1, 1, 1, 16, 64), device="cuda").bfloat16()
+    i64 = dict(dtype=torch.int64, device="cuda")
+    tables = (torch.tensor([0, 1], **i64), torch.zeros(1, dtype=torch.int32, device="cuda"), torch.tensor([1], **i64))
+    with pytest.raises(ValueError, match="q_tokens"):
+        e.attn_plan(pk.KVPages(k, k.clone()), tables, torch.tensor([0, 1], **i64), tokens, 1)
+    e.sync()
