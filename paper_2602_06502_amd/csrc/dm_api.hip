@@ -4,6 +4,7 @@
 // allocates and launches.
 #include <algorithm>
 #include <cstring>
+#include <new>
 #include <string>
 
 #include "dm_internal.h"
@@ -70,10 +71,16 @@ void* scratch_get(dm_ctx* c, int slot, size_t bytes, hipError_t* e)
     // where on the runtime maps an allocation on its own (35 to 60 us, not 1 to 10)
     size_t nb = std::max(bytes, s.bytes + s.bytes / 2);
     nb = (nb + 4095) & ~size_t(4095);
-    if (s.captured)
-        c->outgrown.push_back(s.p);  // a graph's replays go on using it
-    else if (s.p)
+    if (s.captured) {
+        // a graph's replays go on using it (without host memory for its address, it is
+        // never freed)
+        try {
+            c->outgrown.push_back(s.p);
+        } catch (const std::bad_alloc&) {
+        }
+    } else if (s.p) {
         (void)hipFree(s.p);
+    }
     s = Scratch{};
     *e = hipMalloc(&s.p, nb);
     if (*e != hipSuccess) {
