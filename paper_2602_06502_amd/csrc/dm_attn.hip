@@ -24,7 +24,11 @@
 //     For rows that are few: bound by reading the pages.
 //   wide tiles: 128 rows, 32 a wave, on a shared tile of 64 keys (two in LDS).
 //     Bound by the matrix and vector units: two prompts of 7,000 to 8,192 tokens, 32
-//     query and 8 key heads of 128, 895 us, 970 TFLOP/s.
+//     query and 8 key heads of 128, 897 to 985 us by the card, 880 to 968 TFLOP/s.
+//     Weights are rounded to the pages' type: outputs are within 0.0023 relative of 64
+//     bits, where one rounding makes 0.0017.  In two parts, as in narrow tiles, the same
+//     prompts took 1,265 us on a card where they take 980; with the maximum moved
+//     whenever it grows, so that the heaviest weight is 1 exactly, 1,028 (0.0019).
 //   a few rows on a few keys: narrow tiles of more waves, nothing cut or joined.
 //     Bound by launches and the chain of reads.
 #include "dm_internal.h"
@@ -36,9 +40,9 @@ namespace {
 constexpr int kThreads = 256, kWaves = 4;
 constexpr uint32_t kNarrow = 16, kWide = 128;  // rows of a tile
 // Rows of a unit, at most, that has narrow tiles.  (32 sequences of 4,096 keys, 32
-// query and 8 key heads of 128: 24 rows 104 us in a wide tile, 119 in two narrow
-// ones; 64 rows 110 and 170.  64 sequences of up to 8,192 keys, 4 rows: 219 narrow,
-// 244 wide.)
+// query and 8 key heads of 128: 24 rows 104 us in a wide tile, 114 in two narrow
+// ones; 64 rows 112 and 158; 16 rows 103 and 106, 4 rows 100 and 102.  64 sequences of
+// 64 to 8,192 keys, 4 rows: 216 narrow, 262 wide.)
 constexpr uint32_t kNarrowRows = 16;
 constexpr uint32_t kNarrowKeys = 32, kWideKeys = 64;
 constexpr uint32_t kChunk = 128;               // keys of a chunk, at least (of the longest: a multiple)
@@ -1492,9 +1496,12 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attn_kernel(AttnIn
 
 // A few rows on a few keys: narrow tiles, uncut, of as many waves as have room in LDS,
 // where a second kernel that joins parts costs more than cutting gains.  A token of
-// 32 query and 8 key heads of 128 on 100, 300, 500, 700 and 1,000 keys: 6.9, 8.4, 9.6,
-// 11.2 and 13.2 us, in parts 8.6, 11.1, 11.1, 11.3 and 11.1; heads of 64 on 1,000 keys
-// 9.4 and 9.9, of 256 on 300 keys 16.4 and 14.4.
+// 32 query and 8 key heads of 128 on 128, 256, 512, 768 and 1,024 keys: 6.4, 7.2, 9.1,
+// 11.1 and 13.5 us, in parts 8.0, 10.5, 10.5, 10.9 and 10.7 (with the plan 15.5 and 15.9
+// on 768); heads of 64 on 768 and 1,024 keys 8.7 and 10.0, in parts 10.1 and 9.8; heads
+// of 256 on 256 and 384 keys 12.5 and 16.0, in parts 13.8 and 13.9.  1 to 64 KV heads
+// are within 0.4 us of these in this form.  Of several sequences the keys count together:
+// four tokens on 768 keys 7.2, in parts 10.6.
 template <int D>
 constexpr int kSmallWaves = D == 256 ? 4 : 8;
 template <typename T, int D>
@@ -1769,8 +1776,9 @@ bool small(const dm_ctx* c, const dm_token_batch& b, const dm_kv_pages& kv, uint
 }
 
 // Items wanted: three for every two places of a workgroup (two a compute unit).
-// (64 decode rows of up to 8,192 keys, 256 rows on 8 shared prefixes: 218 and 190
-// us; with one for each place 229 and 196, with three 217 and 196.)
+// (us with one for each place, three for two, two and three: 64 decode rows of up to
+// 8,192 keys 227, 217, 216 and 216; 256 rows on 8 shared prefixes 179, 178, 181 and 185; 8
+// tails on 2 prefixes 753, 774, 764 and 755.)
 uint64_t item_target(const dm_ctx* c) { return 3ull * c->n_cu; }
 
 // Items that a plan can have: the tiles of its units, and what cuts add: at most
