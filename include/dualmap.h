@@ -632,6 +632,41 @@ dm_status dm_attn(dm_ctx* ctx, const dm_token_batch* batch, const dm_kv_pages* k
                   uint32_t q_heads, const void* plan, uint32_t layer, const void* q,
                   int64_t q_stride, float scale, void* out, int64_t out_stride, float* lse);
 
+/* Inputs and parameters of dm_diff_attn.  q: token t's heads at q + t *
+ * q_stride, out alike (strides in elements, multiples of 8; out must not
+ * overlap q), lse NULL or float [q_tokens][q_heads].  lambda: [q_heads / 2].
+ * norm: weights [2 * head_dim] of the pages' type, or NULL for no norm.
+ * scale > 0, eps >= 0, gain finite. */
+typedef struct {
+    const void* q;
+    void* out;
+    int64_t q_stride, out_stride;
+    float* lse;
+    const float* lambda;
+    const void* norm;
+    float scale, eps, gain;
+    uint32_t reserved; /* must be 0 */
+} dm_diff_args;
+
+/* Differential attention of a batch's new tokens over the pages.  Query heads
+ * and KV heads are pairs of neighbours, (2j, 2j + 1) and (2g, 2g + 1): pair j
+ * reads pair g = j / (q_heads / kv_heads), its first head the first one's keys,
+ * its second the second one's, and both the values of the pair side by side, V
+ * = [v_2g | v_2g+1] (as dm_kv_append writes rows of 2 * head_dim elements):
+ *   o = softmax(scale q_2j K_2g) V - lambda[j] softmax(scale q_2j+1 K_2g+1) V,
+ * out = gain o, or, with norm, gain o / sqrt(mean(o^2) + eps) * norm, over the
+ * pair's 2 * head_dim elements, which are heads 2j and 2j + 1 of out.  lse is
+ * that of each query head.  Who sees what, empty rows (zeros), groups, errors,
+ * the work area and the roundings are dm_attn's for heads of 2 * head_dim; the
+ * difference and the norm are in 32 bits.  kv_heads even, head_dim 64 or 128.
+ * dm_diff_plan makes the plan, of dm_attn_plan_bytes(n, groups) bytes; it holds
+ * for dm_diff_attn as one of dm_attn_plan does for dm_attn. */
+dm_status dm_diff_plan(dm_ctx* ctx, const dm_token_batch* batch, const dm_kv_pages* kv,
+                       uint32_t q_heads, void* plan, uint64_t plan_bytes);
+dm_status dm_diff_attn(dm_ctx* ctx, const dm_token_batch* batch, const dm_kv_pages* kv,
+                       uint32_t q_heads, const void* plan, uint32_t layer,
+                       const dm_diff_args* args);
+
 /* Wait for all work on the context's stream (and, with pipelining, on its
  * work, selection and epilogue streams); return and clear the first
  * device-side error since the last dm_sync. */

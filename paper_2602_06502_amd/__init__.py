@@ -32,7 +32,8 @@ EXPORTS = ("dm_create", "dm_destroy", "dm_build_rings", "dm_ring_export", "dm_in
            "dm_set_pipelining", "dm_set_policy", "dm_keylen_enable",
            "dm_keylen_window",
            "dm_keylen_export", "dm_pages_fork", "dm_pages_compact", "dm_pages_copy", "dm_kv_append",
-           "dm_attn_plan_bytes", "dm_attn_plan", "dm_attn", "dm_sync", "dm_last_error")
+           "dm_attn_plan_bytes", "dm_attn_plan", "dm_attn", "dm_diff_plan", "dm_diff_attn", "dm_sync",
+           "dm_last_error")
 
 
 class DMError(RuntimeError):
@@ -103,6 +104,12 @@ class dm_append_args(C.Structure):
                 ("eps", C.c_float)]
 
 
+class dm_diff_args(C.Structure):
+    _fields_ = [("q", C.c_void_p), ("out", C.c_void_p), ("q_stride", C.c_int64), ("out_stride", C.c_int64),
+                ("lse", C.c_void_p), ("lambda_", C.c_void_p), ("norm", C.c_void_p), ("scale", C.c_float),
+                ("eps", C.c_float), ("gain", C.c_float), ("reserved", C.c_uint32)]
+
+
 _lib = None
 
 
@@ -147,6 +154,8 @@ def load_library(path: str = LIB_PATH):
         "dm_attn_plan_bytes": (u64, [u64, u64]),
         "dm_attn_plan": (i32, [P, P, P, u32, P, u64]),
         "dm_attn": (i32, [P, P, P, u32, P, u32, P, C.c_int64, C.c_float, P, C.c_int64, P]),
+        "dm_diff_plan": (i32, [P, P, P, u32, P, u64]),
+        "dm_diff_attn": (i32, [P, P, P, u32, P, u32, P]),
         "dm_sync": (i32, [P]),
         "dm_last_error": (C.c_char_p, [P]),
     }
@@ -185,12 +194,13 @@ def _ptr(t) -> Optional[int]:
     return None if t is None else t.data_ptr()
 
 
-# dm_page_tables, dm_token_batch, dm_pages_out and dm_append_args as bytes: a decode step makes these calls for every
+# dm_page_tables, dm_token_batch, dm_pages_out, dm_append_args and dm_diff_args as bytes: a decode step makes these calls for every
 # layer, and packing takes a fraction of the time of filling a ctypes structure
 _PACK_TABLES = struct.Struct("=5Q").pack
 _PACK_BATCH = struct.Struct("=9Q").pack
 _PACK_OUT = struct.Struct("=10Q").pack
 _PACK_APPEND = struct.Struct("=3Q3qQq5Q3If").pack
+_PACK_DIFF = struct.Struct("=2Q2q3Q3fI").pack
 
 
 class KVPages:
@@ -217,10 +227,11 @@ class KVPages:
 
 
 class AttnPlan:
-    """A plan of DualMap.attn_plan: the batch that it was made for."""
+    """A plan of DualMap.attn_plan or, with pairs, diff_plan: the batch that it was made for."""
 
-    def __init__(self, batch, q_tokens, kv, q_heads, buf, keep):
+    def __init__(self, batch, q_tokens, kv, q_heads, buf, keep, pairs=False):
         self.batch, self.q_tokens, self.kv, self.q_heads, self.buf = batch, q_tokens, kv, q_heads, buf
+        self.pairs = pairs
         self._keep = keep  # the batch's tensors
 
 
@@ -707,6 +718,13 @@ class DualMap:
     def attn_plan(self, kv: KVPages, tables, q_off, q_tokens: int, q_heads: int, groups=None) -> AttnPlan:
         """The work of attn for a batch (see dm_attn_plan), once for all layers.
         groups: int64 [runs + 1], the runs of sequences that may share a prefix."""
+        return self._plan("dm_attn_plan", kv, tables, q_off, q_tokens, q_heads, groups, False)
+
+    def diff_plan(self, kv: KVPages, tables, q_off, q_tokens: int, q_heads: int, groups=None) -> AttnPlan:
+        """The work of diff_attn for a batch (see dm_diff_plan), as attn_plan."""
+        return self._plan("dm_diff_plan", kv, tables, q_off, q_tokens, q_heads, groups, True)
+
+    def _plan(self, name, kv, tables, q_off, q_tokens, q_heads, groups, pairs):
         self._kv(kv)
         b = self._batch(tables, q_off, q_tokens, groups)
         need = self.lib.dm_attn_plan_bytes(b[3], b[8])
@@ -718,20 +736,45 @@ class DualMap:
             with torch.cuda.stream(self.stream):
                 buf = torch.empty(need, dtype=torch.uint8, device=self.device)
         batch = _PACK_BATCH(*b)
-        self._check(self.lib.dm_attn_plan(self._h, batch, kv._ref, q_heads, buf.data_ptr(), need),
-                    "dm_attn_plan")
-        return AttnPlan(batch, q_tokens, kv, q_heads, buf, (tables, q_off, groups))
+        self._check(getattr(self.lib, name)(self._h, batch, kv._ref, q_heads, buf.data_ptr(), need), name)
+        return AttnPlan(batch, q_tokens, kv, q_heads, buf, (tables, q_off, groups), pairs)
 
     def attn(self, plan: AttnPlan, layer: int, q, scale: float, out, lse=None) -> None:
         """Attention of a batch's new tokens over layer's pages (see dm_attn): q
         and out [tokens, q_heads, head_dim], lse float32 [tokens, q_heads]."""
         kv, T, heads = plan.kv, plan.q_tokens, plan.q_heads
+        if plan.pairs:
+            raise ValueError("the plan is diff_plan's")
         qp, qs = self._rows(q, "q", heads, kv.head_dim, T, kv.dtype)
         op, os_ = self._rows(out, "out", heads, kv.head_dim, T, kv.dtype)
-        lp = None
-        if lse is not None:
-            lp = self._dev(lse, self.torch.float32, "lse").data_ptr()
-            if lse.shape != (T, heads):
-                raise ValueError("lse must be [tokens, q_heads]")
+        lp = self._lse(lse, T, heads)
         self._check(self.lib.dm_attn(self._h, plan.batch, kv._ref, heads, plan.buf.data_ptr(), layer, qp,
                                      qs, scale, op, os_, lp), "dm_attn")
+
+    def _lse(self, lse, tokens, heads):
+        if lse is None:
+            return None
+        if self._dev(lse, self.torch.float32, "lse").shape != (tokens, heads):
+            raise ValueError("lse must be [tokens, q_heads]")
+        return lse.data_ptr()
+
+    def diff_attn(self, plan: AttnPlan, layer: int, q, scale: float, lam, out, lse=None, norm=None,
+                  eps: float = 1e-5, gain: float = 1.0) -> None:
+        """Differential attention of a batch's new tokens over layer's pages (see dm_diff_attn):
+        q and out [tokens, q_heads, head_dim], lam float32 [q_heads / 2], lse float32 [tokens,
+        q_heads], norm [2 * head_dim] of the pages' type.  plan: diff_plan's."""
+        kv, T, heads = plan.kv, plan.q_tokens, plan.q_heads
+        if not plan.pairs:
+            raise ValueError("the plan is attn_plan's")
+        qp, qs = self._rows(q, "q", heads, kv.head_dim, T, kv.dtype)
+        op, os_ = self._rows(out, "out", heads, kv.head_dim, T, kv.dtype)
+        if self._dev(lam, self.torch.float32, "lam").numel() != heads // 2:
+            raise ValueError("lam needs a number for each pair of query heads")
+        w = 0
+        if norm is not None:
+            if self._dev(norm, kv.dtype, "norm").numel() != 2 * kv.head_dim:
+                raise ValueError("norm needs 2 * head_dim weights")
+            w = norm.data_ptr()
+        a = _PACK_DIFF(qp, op, qs, os_, self._lse(lse, T, heads) or 0, lam.data_ptr(), w, scale, eps, gain, 0)
+        self._check(self.lib.dm_diff_attn(self._h, plan.batch, kv._ref, heads, plan.buf.data_ptr(), layer, a),
+                    "dm_diff_attn")

@@ -993,27 +993,49 @@ uint64_t dm_attn_plan_bytes(uint64_t n, uint64_t groups)
     return n < (1ull << 31) && groups <= n ? attn_plan_bytes(n, groups) : 0;
 }
 
-dm_status dm_attn_plan(dm_ctx* c, const dm_token_batch* batch, const dm_kv_pages* kv,
-                       uint32_t q_heads, void* plan, uint64_t plan_bytes)
+// KV heads in pairs: an even number of them, and 2 head_dim elements have their kernels.
+static dm_status pairs_check(dm_ctx* c, const dm_kv_pages* kv, const std::string& what)
+{
+    if (kv->kv_heads % 2 || kv->head_dim > 128)
+        return fail(c, DM_EINVAL, what + ": pairs need an even number of KV heads and head_dim 64 or 128");
+    return DM_OK;
+}
+
+static dm_status plan_checked(dm_ctx* c, const dm_token_batch* batch, const dm_kv_pages* kv, bool pairs,
+                              uint32_t q_heads, void* plan, uint64_t plan_bytes, const std::string& what)
 {
     if (!c)
         return DM_EINVAL;
-    if (dm_status s = kv_pages_check(c, kv, 0, false, "dm_attn_plan"); s != DM_OK)
+    if (dm_status s = kv_pages_check(c, kv, 0, false, what); s != DM_OK)
         return s;
-    if (dm_status s = token_batch_check(c, batch, "dm_attn_plan"); s != DM_OK)
+    if (dm_status s = pairs ? pairs_check(c, kv, what) : DM_OK; s != DM_OK)
         return s;
-    if (dm_status s = heads_check(c, kv, q_heads, "dm_attn_plan"); s != DM_OK)
+    if (dm_status s = token_batch_check(c, batch, what); s != DM_OK)
+        return s;
+    if (dm_status s = heads_check(c, kv, q_heads, what); s != DM_OK)
         return s;
     if (batch->q_tokens * q_heads >= (1ull << 31))
-        return fail(c, DM_EINVAL, "dm_attn_plan: q_tokens * q_heads must be below 2^31");
+        return fail(c, DM_EINVAL, what + ": q_tokens * q_heads must be below 2^31");
     if (!plan || !aligned16(plan) || plan_bytes < attn_plan_bytes(batch->tables.n, batch->groups))
-        return fail(c, DM_EINVAL, "dm_attn_plan: plan is null, misaligned or smaller than "
-                                  "dm_attn_plan_bytes");
+        return fail(c, DM_EINVAL, what + ": plan is null, misaligned or smaller than "
+                                         "dm_attn_plan_bytes");
     DeviceGuard g(c->device);
     hipError_t e = join_selection(c);
     if (e == hipSuccess)
-        e = attn_plan(c, *batch, *kv, q_heads, plan);
-    return e == hipSuccess ? DM_OK : hip_fail(c, e, "dm_attn_plan");
+        e = attn_plan(c, *batch, pairs ? pairs_of(*kv) : *kv, q_heads, plan);
+    return e == hipSuccess ? DM_OK : hip_fail(c, e, what.c_str());
+}
+
+dm_status dm_attn_plan(dm_ctx* c, const dm_token_batch* batch, const dm_kv_pages* kv,
+                       uint32_t q_heads, void* plan, uint64_t plan_bytes)
+{
+    return plan_checked(c, batch, kv, false, q_heads, plan, plan_bytes, "dm_attn_plan");
+}
+
+dm_status dm_diff_plan(dm_ctx* c, const dm_token_batch* batch, const dm_kv_pages* kv,
+                       uint32_t q_heads, void* plan, uint64_t plan_bytes)
+{
+    return plan_checked(c, batch, kv, true, q_heads, plan, plan_bytes, "dm_diff_plan");
 }
 
 dm_status dm_attn(dm_ctx* c, const dm_token_batch* batch, const dm_kv_pages* kv, uint32_t q_heads,
@@ -1044,6 +1066,41 @@ dm_status dm_attn(dm_ctx* c, const dm_token_batch* batch, const dm_kv_pages* kv,
     if (e == hipSuccess)
         e = attn(c, *batch, *kv, q_heads, plan, layer, q, q_stride, scale, out, out_stride, lse);
     return e == hipSuccess ? DM_OK : hip_fail(c, e, "dm_attn");
+}
+
+dm_status dm_diff_attn(dm_ctx* c, const dm_token_batch* batch, const dm_kv_pages* kv, uint32_t q_heads,
+                       const void* plan, uint32_t layer, const dm_diff_args* a)
+{
+    if (!c)
+        return DM_EINVAL;
+    if (dm_status s = kv_pages_check(c, kv, layer, true, "dm_diff_attn"); s != DM_OK)
+        return s;
+    if (dm_status s = pairs_check(c, kv, "dm_diff_attn"); s != DM_OK)
+        return s;
+    if (dm_status s = token_batch_check(c, batch, "dm_diff_attn"); s != DM_OK)
+        return s;
+    if (dm_status s = heads_check(c, kv, q_heads, "dm_diff_attn"); s != DM_OK)
+        return s;
+    if (!a || a->reserved)
+        return fail(c, DM_EINVAL, "dm_diff_attn: null arguments or reserved not 0");
+    if (!plan || !aligned16(plan) || !aligned(a->lse) || !aligned(a->lambda) || !aligned16(a->norm))
+        return fail(c, DM_EINVAL, "dm_diff_attn: null plan or misaligned pointer");
+    if (!(a->scale > 0) || a->scale > 1e30f || !(a->eps >= 0) || !(a->gain - a->gain == 0))
+        return fail(c, DM_EINVAL, "dm_diff_attn: scale must be positive and finite, eps not negative, gain finite");
+    if (batch->tables.n == 0 || batch->q_tokens == 0)
+        return DM_OK;
+    if (!a->lambda)
+        return fail(c, DM_EINVAL, "dm_diff_attn: null lambda");
+    if (!rows_ok(a->q, a->q_stride, q_heads, kv->head_dim) || !rows_ok(a->out, a->out_stride, q_heads, kv->head_dim))
+        return fail(c, DM_EINVAL, "dm_diff_attn: rows must be 16-byte aligned, their strides multiples of 8 "
+                                  "and at least heads * head_dim");
+    if (batch->q_tokens * q_heads >= (1ull << 31))
+        return fail(c, DM_EINVAL, "dm_diff_attn: q_tokens * q_heads must be below 2^31");
+    DeviceGuard g(c->device);
+    hipError_t e = join_selection(c);
+    if (e == hipSuccess)
+        e = diff_attn(c, *batch, *kv, q_heads, plan, layer, *a);
+    return e == hipSuccess ? DM_OK : hip_fail(c, e, "dm_diff_attn");
 }
 
 dm_status dm_sync(dm_ctx* c)

@@ -169,6 +169,28 @@ struct AttnIn {
     float scale2;      // scale * log2(e)
 };
 
+// Differential attention: KV heads are pairs, their values side by side one value of D
+// elements, their keys D / 2 elements each.  A row is a query head and reads the keys
+// of its own map, row % 2, of the pair; ratio, kv_heads: of pairs.
+struct DiffIn : AttnIn {
+    const float* lambda;   // [q_heads / 2]
+    const uint16_t* norm;  // [D], or null
+    float eps, gain;
+};
+template <bool PAIR>
+using InOf = std::conditional_t<PAIR, DiffIn, AttnIn>;
+
+// Elements of a key's row of one map, and in a page: a page holds a pair's heads one
+// after the other, so that place `chunk` (16 bytes) of a joint row is there.
+template <int D, bool PAIR>
+constexpr int kKeyElems = PAIR ? D / 2 : D;
+template <int D, bool PAIR>
+__device__ __forceinline__ uint32_t chunk_at(uint32_t chunk, uint32_t shift)
+{
+    constexpr uint32_t kOne = D / 16;  // chunks of a map's row
+    return PAIR ? ((chunk / kOne) * (D / 2) << shift) + chunk % kOne * 8 : chunk * 8;
+}
+
 // Weights are raised by a power of two: a float16 one loses bits below 2^-14 and is
 // nothing below 2^-25, while the sum, in 32 bits, counts it.  They reach 2^8 (see
 // weights()) and float16 ends at 2^16, so 2^7 fits: a weight below 2^-21 of the
@@ -194,16 +216,18 @@ __device__ __forceinline__ bool scores_are_far(float m, float scale2)
 }
 
 // A tile of 32 keys for a wave's 32 rows: s holds S^T (key = (i / 4) * 8 + half
-// * 4 + i % 4).
-template <typename T, int D>
-__device__ __forceinline__ v16f scores(const uint16_t* kt, const typename Vec8<T>::type (&q)[D / 16])
+// * 4 + i % 4).  map: of a pair.
+template <typename T, int D, bool PAIR = false>
+__device__ __forceinline__ v16f scores(const uint16_t* kt,
+                                       const typename Vec8<T>::type (&q)[kKeyElems<D, PAIR> / 16],
+                                       uint32_t map = 0)
 {
     using V = typename Vec8<T>::type;
     const uint32_t row = lane_id() % 32, half = lane_id() / 32;
     v16f s = {};
 #pragma unroll
-    for (int x = 0; x < D / 16; x++) {
-        const uint32_t chunk = (x * 2 + half) ^ k_swizzle<D>(row);
+    for (int x = 0; x < kKeyElems<D, PAIR> / 16; x++) {
+        const uint32_t chunk = ((PAIR ? map * (D / 16) : 0) + x * 2 + half) ^ k_swizzle<D>(row);
         s = mfma(*reinterpret_cast<const V*>(kt + row * D + chunk * 8), q[x], s);
     }
     return s;
@@ -517,15 +541,16 @@ __device__ __forceinline__ Tile make_tile(const AttnIn& a, const Unit& u, uint32
 
 // A row's query, as the right operand of K Q^T (rows past the tile's last: the
 // last one's again, not written).
-template <typename T, int D>
+template <typename T, int D, bool PAIR = false>
 __device__ __forceinline__ void load_query(const AttnIn& a, const Tile& t, uint32_t row,
-                                           typename Vec8<T>::type (&q)[D / 16])
+                                           typename Vec8<T>::type (&q)[kKeyElems<D, PAIR> / 16])
 {
+    constexpr int kElems = kKeyElems<D, PAIR>;
     const uint32_t r = row < t.last ? row : t.last;
     const uint16_t* at = a.q + (uint64_t)(t.u.tok0 + r / a.ratio) * a.q_stride +
-                         (uint64_t)(t.h * a.ratio + r % a.ratio) * D + lane_id() / 32 * 8;
+                         (uint64_t)(t.h * a.ratio + r % a.ratio) * kElems + lane_id() / 32 * 8;
 #pragma unroll
-    for (int k = 0; k < D / 16; k++)
+    for (int k = 0; k < kElems / 16; k++)
         q[k] = *reinterpret_cast<const typename Vec8<T>::type*>(at + k * 16);
 }
 
@@ -549,8 +574,9 @@ typedef const __attribute__((address_space(4))) uint32_t ScalarTable;
 // ...  A tile's pages are looked up two tiles ahead and its rows read one ahead; none
 // of the reads is conditional: rows past the last key read the last key's page, and
 // their values become zeros on the way to LDS.
-template <typename T, int D>
+template <typename T, int D, bool PAIR = false>
 struct Share {
+    static constexpr int kElems = kKeyElems<D, PAIR>;
     static constexpr int kLoads = kNarrowKeys * D / 8 / kWave;
     static constexpr uint32_t kRowChunks = D / 8, kStep = kWave / kRowChunks;
     static constexpr int kGroups = kStep > 4 ? 2 : 1, kPages = kLoads * kGroups;
@@ -565,7 +591,7 @@ struct Share {
     __device__ __forceinline__ Share(const AttnIn& a, const Tile& t)
         : table((ScalarTable*)(a.b.page + t.u.off)), key1(t.key1), n_pages(a.n_pages), shift(a.b.shift),
           r0(lane_id() / kRowChunks), ch(lane_id() % kRowChunks), halves(kGroups == 2 && a.b.shift == 2),
-          lane_at(r0 % (halves ? 4 : 8) * D + ch * 8),
+          lane_at(r0 % (halves ? 4 : 8) * kElems + chunk_at<D, PAIR>(ch, a.b.shift)),
           head_at((uint64_t)t.h * D << a.b.shift), page_size((uint64_t)a.kv_heads * D << a.b.shift)
     {
     }
@@ -593,7 +619,7 @@ struct Share {
         auto from = [&](int i, int g) {
             const uint32_t p = page[i * kGroups + g];
             bad |= p >= n_pages;
-            return (p < n_pages ? p : 0) * page_size + head_at + ((key + i * kStep + g * 4) & mask) * D;
+            return (p < n_pages ? p : 0) * page_size + head_at + ((key + i * kStep + g * 4) & mask) * kElems;
         };
         auto load = [&](int i, uint64_t at) {
             k[i] = *reinterpret_cast<const v4u32*>(a.k + at + lane_at);
@@ -636,6 +662,30 @@ struct Share {
     }
 };
 
+// 1 / sqrt(mean square + eps) of a differential row, from the sum of its D squares;
+// nothing has a norm of nothing, also where eps is 0.
+template <int D>
+__device__ __forceinline__ float norm_of(float ss, float eps)
+{
+    return ss == 0 ? 0.0f : rsqrtf(ss * (1.0f / D) + eps);
+}
+
+// Four elements of a differential row, d on, times `by` and the norm's weights.  x: the
+// first of the pair's query heads.
+template <typename T>
+__device__ __forceinline__ void write_normed(const DiffIn& a, uint32_t token, uint32_t x, int elems, uint32_t d, v4f y,
+                                             float by)
+{
+    typedef T v4t __attribute__((ext_vector_type(4)));
+    v4t w = {1, 1, 1, 1}, z;
+    if (a.norm)
+        w = *reinterpret_cast<const v4t*>(a.norm + d);
+#pragma unroll
+    for (int i = 0; i < 4; i++)
+        z[i] = (T)(y[i] * by * (float)w[i]);
+    *reinterpret_cast<v4t*>(a.out + token * a.out_stride + (uint64_t)x * elems + d) = z;
+}
+
 // What the waves of a narrow tile leave for one another.
 template <int WAVES>
 struct Joined {
@@ -669,23 +719,26 @@ __device__ __forceinline__ void write_four(const AttnIn& a, const Tile& t, uint3
 }
 
 // A lane holds its row's (lane % 16) scores of 4 of 16 keys, key = h * 16 + (lane /
-// 16) * 4 + i, and of O^T the elements d = block * 16 + (lane / 16) * 4 + i.
-template <typename T, int D, int WAVES>
-__device__ __forceinline__ void narrow_tile(const AttnIn& a, const Tile& t, uint16_t* lds, Joined<WAVES>& joined,
+// 16) * 4 + i, and of O^T the elements d = block * 16 + (lane / 16) * 4 + i.  PAIR: the
+// rows of a tile are of both maps in turn, so each takes the products with both maps'
+// keys and keeps its own: no more instructions than one product over D.
+template <typename T, int D, int WAVES, bool PAIR = false>
+__device__ __forceinline__ void narrow_tile(const InOf<PAIR>& a, const Tile& t, uint16_t* lds, Joined<WAVES>& joined,
                                             bool& bad)
 {
+    constexpr int kElems = kKeyElems<D, PAIR>;
     using V = typename Vec8<T>::type;
     constexpr uint32_t kTurn = WAVES * kNarrowKeys;
     constexpr int kBlocks = D / 16;
     const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
     const uint32_t lane = lane_id(), row16 = lane % 16, g = lane / 16;
     const uint32_t row = t.first + row16, in_tile = row < t.last ? row : t.last;
-    V q[D / 32];
+    V q[kElems / 32];
     {
         const uint16_t* at = a.q + (uint64_t)(t.u.tok0 + in_tile / a.ratio) * a.q_stride +
-                             (uint64_t)(t.h * a.ratio + in_tile % a.ratio) * D + g * 8;
+                             (uint64_t)(t.h * a.ratio + in_tile % a.ratio) * kElems + g * 8;
 #pragma unroll
-        for (int k = 0; k < D / 32; k++)
+        for (int k = 0; k < kElems / 32; k++)
             q[k] = *reinterpret_cast<const V*>(at + k * 32);
     }
     const uint32_t limit = sees(t.u, a.ratio, in_tile), end = limit < t.key1 ? limit : t.key1;
@@ -708,9 +761,20 @@ __device__ __forceinline__ void narrow_tile(const AttnIn& a, const Tile& t, uint
             s[h] = v4f{};
             const uint32_t r = h * 16 + row16;
 #pragma unroll
-            for (int k = 0; k < D / 32; k++)
+            for (int k = 0; k < kElems / 32; k++)
                 s[h] = mfma(*reinterpret_cast<const V*>(kt + r * D + ((k * 4 + g) ^ k_swizzle<D>(r)) * 8), q[k],
                             s[h]);
+            if constexpr (PAIR) {
+                v4f other = {};
+#pragma unroll
+                for (int k = 0; k < kElems / 32; k++)
+                    other = mfma(*reinterpret_cast<const V*>(
+                                     kt + r * D + ((D / 16 + k * 4 + g) ^ k_swizzle<D>(r)) * 8),
+                                 q[k], other);
+#pragma unroll
+                for (int i = 0; i < 4; i++)
+                    s[h][i] = row16 % 2 ? other[i] : s[h][i];
+            }
         }
         if (masked) {
             uint32_t first = key + g * 4;
@@ -756,7 +820,7 @@ __device__ __forceinline__ void narrow_tile(const AttnIn& a, const Tile& t, uint
     };
     uint32_t key = t.key0 + wave * kNarrowKeys;
     if (key < t.key1) {
-        Share<T, D> x(a, t);
+        Share<T, D, PAIR> x(a, t);
         bool masked = false, odd = false;
         // a wave's own part of LDS: its lanes' writes and reads in order
         auto stage = [&](uint32_t key) {
@@ -850,14 +914,58 @@ __device__ __forceinline__ void narrow_tile(const AttnIn& a, const Tile& t, uint
     __syncthreads();
     const bool seen = total > 0 || total != total;
     const float inv = seen ? 1.0f / total : 0.0f;
-    for (uint32_t d = wave; d < kBlocks; d += WAVES) {
+    auto block = [&](uint32_t d) {
         v4f x = {};
         for (int w = 0; w < WAVES; w++)
             x += sum[(w * kBlocks + d) * kWave + lane];
         for (int k = 0; k < 4; k++)
             x[k] = seen ? x[k] * inv : 0.0f;
-        if (row <= t.last)
-            write_four<T, D>(a, t, row, d * 16 + g * 4, x);
+        return x;
+    };
+    if (!PAIR || (t.u.flags & kUnitParts)) {
+        for (uint32_t d = wave; d < kBlocks; d += WAVES) {
+            const v4f x = block(d);
+            if (row <= t.last)
+                write_four<T, D>(a, t, row, d * 16 + g * 4, x);
+        }
+    }
+    if constexpr (PAIR) {
+        if (!(t.u.flags & kUnitParts)) {
+            // the maps' rows are in neighbouring lanes
+            constexpr int kMine = kBlocks / WAVES;
+            const uint32_t x = t.h * a.ratio + in_tile % a.ratio;
+            const float lambda = a.lambda[x / 2];
+            v4f y[kMine];
+            float ss = 0;
+#pragma unroll
+            for (int k = 0; k < kMine; k++) {
+                y[k] = block(wave + k * WAVES);
+#pragma unroll
+                for (int i = 0; i < 4; i++) {
+                    y[k][i] = __builtin_fmaf(-lambda, __shfl_xor(y[k][i], 1), y[k][i]);
+                    ss = __builtin_fmaf(y[k][i], y[k][i], ss);
+                }
+            }
+            float by = a.gain;
+            if (a.norm) {
+                ss += __shfl_xor(ss, 16);
+                ss += __shfl_xor(ss, 32);
+                __syncthreads();  // (the first use of joined.m is over)
+                if (g == 0)
+                    joined.m[wave][row16] = ss;
+                __syncthreads();
+                ss = 0;
+                for (int w = 0; w < WAVES; w++)
+                    ss += joined.m[w][row16];
+                by *= norm_of<D>(ss, a.eps);
+            }
+            if (row16 % 2 == 0 && row <= t.last)
+#pragma unroll
+                for (int k = 0; k < kMine; k++) {
+                    const uint32_t d = (wave + k * WAVES) * 16 + g * 4;
+                    write_normed<T>(a, t.u.tok0 + row / a.ratio, x, kElems, d, y[k], by);
+                }
+        }
     }
     if (wave == 0 && g == 0 && row <= t.last) {
         if (t.u.flags & kUnitParts)
@@ -900,8 +1008,9 @@ __device__ __forceinline__ uint32_t lds_address(const uint16_t* p)
 // A thread's share of wide tiles: LDS chunk threadIdx.x + i * 256, that is row r0 +
 // i * kStep, place `ch` of the row.  What a lane adds to its rows' address does not
 // change from tile to tile.
-template <typename T, int D>
+template <typename T, int D, bool PAIR = false>
 struct Sender {
+    static constexpr int kElems = kKeyElems<D, PAIR>;
     static constexpr int kLoads = kWideKeys * D / 8 / kThreads;
     static constexpr uint32_t kRowChunks = D / 8, kStep = kThreads / kRowChunks;
     static constexpr uint32_t kWaveRows = kWave / kRowChunks;
@@ -916,7 +1025,7 @@ struct Sender {
         : k(a.k + ((uint64_t)t.h * D << a.b.shift)), v(a.v + ((uint64_t)t.h * D << a.b.shift)),
           table((ScalarTable*)(a.b.page + t.u.off)), key1(t.key1), n_pages(a.n_pages), shift(a.b.shift),
           page_size(a.kv_heads * D << a.b.shift), r0(threadIdx.x / kRowChunks), ch(threadIdx.x % kRowChunks),
-          wave(wave_), halves(kGroups == 2 && a.b.shift == 2), lane_row(r0 % kWaveRows % (halves ? 4 : 8) * D)
+          wave(wave_), halves(kGroups == 2 && a.b.shift == 2), lane_row(r0 % kWaveRows % (halves ? 4 : 8) * kElems)
     {
     }
     // pages of the wave's rows of the tile at `key` (uniform, < key1), as they are in the
@@ -940,11 +1049,11 @@ struct Sender {
                 const uint32_t p = page[i * kGroups + g];
                 bad |= p >= n_pages;
                 return base + (uint64_t)(p < n_pages ? p : 0) * page_size +
-                       ((key + wave * kWaveRows + i * kStep + g * 4) & mask) * D;
+                       ((key + wave * kWaveRows + i * kStep + g * 4) & mask) * kElems;
             };
             const uint32_t r = r0 + i * kStep;
             const uint32_t c = ch ^ (values ? v_swizzle<D>(r) : k_swizzle<D>(r));
-            const uint32_t lane_at = (lane_row + c * 8) * 2, lds_at = at + i * kThreads * 16;
+            const uint32_t lane_at = (lane_row + chunk_at<D, PAIR>(c, shift)) * 2, lds_at = at + i * kThreads * 16;
             if (kGroups == 1 || !halves) {
                 send16(from(0), lane_at, lds_at);
             } else {
@@ -974,28 +1083,33 @@ struct Sender {
 // matrix unit has work that does not wait for them.  K of tile t + 2 and V of
 // tile t + 1 are on their way meanwhile, to where K of tile t and V of tile t - 1
 // were.
-template <typename T, int D>
-__device__ __forceinline__ void wide_tile(const AttnIn& a, const Tile& t, uint16_t* lds, uint32_t* odd_tile,
+// PAIR: a wave's rows are of one map, two waves take the maps of the same 32 pairs of
+// rows; each has products with its own map's keys only, both with all values.
+template <typename T, int D, bool PAIR = false>
+__device__ __forceinline__ void wide_tile(const InOf<PAIR>& a, const Tile& t, uint16_t* lds, uint32_t* odd_tile,
                                           bool& bad)
 {
     const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
-    const uint32_t row = t.first + wave * 32 + lane_id() % 32;
-    typename Vec8<T>::type q[D / 16], p[2][2];
-    load_query<T, D>(a, t, row, q);
+    const uint32_t map = PAIR ? wave % 2 : 0;
+    // the wave's first row, and from one to the next
+    const uint32_t w0 = t.first + (PAIR ? wave / 2 * 64 + map : wave * 32), step = PAIR ? 2 : 1;
+    const uint32_t row = w0 + lane_id() % 32 * step;
+    typename Vec8<T>::type q[kKeyElems<D, PAIR> / 16], p[2][2];
+    load_query<T, D, PAIR>(a, t, row, q);
     const uint32_t limit = sees(t.u, a.ratio, row < t.last ? row : t.last);
     const uint32_t end = limit < t.key1 ? limit : t.key1;
     Row<D> r;
     clear<D>(r);
     // keys that the wave's first and last rows see
-    const uint32_t w0 = t.first + wave * 32, w1 = w0 + 31 < t.last ? w0 + 31 : t.last;
+    const uint32_t w1 = w0 + 31 * step < t.last ? w0 + 31 * step : t.last;
     const uint32_t wave_first = w0 <= t.last ? sees(t.u, a.ratio, w0) : 0;
     const uint32_t wave_last = w0 <= t.last ? sees(t.u, a.ratio, w1) : 0;
     auto masked = [&](uint32_t key, uint32_t first) { return key + kWideKeys > first || key + kWideKeys > t.key1; };
     constexpr uint32_t kTile = kWideKeys * D;
     uint16_t* vts = lds + 2 * kTile;  // two tiles of keys, then two of values
     if (t.key0 < t.key1) {
-        const Sender<T, D> x(a, t, wave);
-        uint32_t p1[Sender<T, D>::kPages], p2[Sender<T, D>::kPages];  // pages of the next tile, and the one after
+        const Sender<T, D, PAIR> x(a, t, wave);
+        uint32_t p1[Sender<T, D, PAIR>::kPages], p2[Sender<T, D, PAIR>::kPages];  // pages of the next tile, and the one after
         if (threadIdx.x == 0)
             *odd_tile = 0;
         x.find(t.key0, p2);
@@ -1009,7 +1123,7 @@ __device__ __forceinline__ void wide_tile(const AttnIn& a, const Tile& t, uint16
             x.find(t.key0 + 2 * kWideKeys, p2);
         wait_sent();
         __syncthreads();
-        v16f s[2] = {scores<T, D>(lds, q), scores<T, D>(lds + 32 * D, q)};
+        v16f s[2] = {scores<T, D, PAIR>(lds, q, map), scores<T, D, PAIR>(lds + 32 * D, q, map)};
         __syncthreads();  // the third tile's keys go where the first's are
         uint32_t key = t.key0, buf = 0;
         bool odd = false;
@@ -1030,7 +1144,7 @@ __device__ __forceinline__ void wide_tile(const AttnIn& a, const Tile& t, uint16
             if (key1 < t.key1) {
                 x.send(x.v, true, key1, p1, vts + (buf ^ 1) * kTile, bad);
 #pragma unroll
-                for (int i = 0; i < Sender<T, D>::kPages; i++)
+                for (int i = 0; i < Sender<T, D, PAIR>::kPages; i++)
                     p1[i] = p2[i];
             }
             if (key2 + kWideKeys < t.key1)
@@ -1038,8 +1152,8 @@ __device__ __forceinline__ void wide_tile(const AttnIn& a, const Tile& t, uint16
             if (key < wave_last) {
                 weights<T, D, 2>(r, s, p, key, end, masked(key, wave_first), a.scale2, [&] {
                     // (of the last tile: of what is there, and not used)
-                    s[0] = scores<T, D>(lds + (buf ^ 1) * kTile, q);
-                    s[1] = scores<T, D>(lds + (buf ^ 1) * kTile + 32 * D, q);
+                    s[0] = scores<T, D, PAIR>(lds + (buf ^ 1) * kTile, q, map);
+                    s[1] = scores<T, D, PAIR>(lds + (buf ^ 1) * kTile + 32 * D, q, map);
                 });
                 add_values<T, D, 2>(r, p, vts + buf * kTile);
             }
@@ -1066,12 +1180,59 @@ __device__ __forceinline__ void wide_tile(const AttnIn& a, const Tile& t, uint16
             __syncthreads();
             x.clean(vts + buf * kTile, key);
             __syncthreads();
-            s[0] = scores<T, D>(lds + buf * kTile, q);
-            s[1] = scores<T, D>(lds + buf * kTile + 32 * D, q);
+            s[0] = scores<T, D, PAIR>(lds + buf * kTile, q, map);
+            s[1] = scores<T, D, PAIR>(lds + buf * kTile + 32 * D, q, map);
         }
     }
-    write_row<T, D>(a, t.u, t.h, row, t.last + 1, t.chunk, r, r.l + __shfl_xor(r.l, 32), t.rows);
+    const float l = r.l + __shfl_xor(r.l, 32);
+    if (!PAIR || (t.u.flags & kUnitParts))
+        write_row<T, D>(a, t.u, t.h, row, t.last + 1, t.chunk, r, l, t.rows);
+    if constexpr (PAIR) {
+        if (t.u.flags & kUnitParts)
+            return;
+        // the second map's rows by way of LDS to the first's wave
+        const uint32_t half = lane_id() / 32;
+        const uint32_t in_tile = row < t.last ? row : t.last, token = t.u.tok0 + in_tile / a.ratio;
+        const uint32_t x = t.h * a.ratio + in_tile % a.ratio;
+        const bool seen = l > 0 || l != l;
+        const float inv = seen ? 1.0f / l : 0.0f;
+        if (half == 0 && a.lse && row <= t.last)
+            a.lse[(uint64_t)token * a.q_heads + x] = seen ? lse_of<T>(r.m, l, a.scale2) : -INFINITY;
+        float* far = reinterpret_cast<float*>(lds) + wave / 2 * (D / 2 * kWave) + lane_id();
+        __syncthreads();
+        if (map)
+#pragma unroll
+            for (int d = 0; d < D / 32; d++)
+#pragma unroll
+                for (int i = 0; i < 16; i++)
+                    far[(d * 16 + i) * kWave] = seen ? r.o[d][i] * inv : 0.0f;
+        __syncthreads();
+        if (map)
+            return;
+        const float lambda = a.lambda[x / 2];
+        float ss = 0;
+#pragma unroll
+        for (int d = 0; d < D / 32; d++)
+#pragma unroll
+            for (int i = 0; i < 16; i++) {
+                const float y = __builtin_fmaf(-lambda, far[(d * 16 + i) * kWave], seen ? r.o[d][i] * inv : 0.0f);
+                ss = __builtin_fmaf(y, y, ss);
+                r.o[d][i] = y;
+            }
+        const float by = a.norm ? a.gain * norm_of<D>(ss + __shfl_xor(ss, 32), a.eps) : a.gain;
+        if (row <= t.last)
+#pragma unroll
+            for (int d = 0; d < D / 32; d++)
+#pragma unroll
+                for (int i = 0; i < 16; i += 4)
+                    write_normed<T>(a, token, x, D / 2, d * 32 + i * 2 + half * 4,
+                                    v4f{r.o[d][i], r.o[d][i + 1], r.o[d][i + 2], r.o[d][i + 3]}, by);
+    }
 }
+// Waves of a narrow tile that is not cut (as many as have room in LDS).
+template <int D>
+constexpr int kSmallWaves = D == 256 ? 4 : 8;
+
 // ---------------------------------------------------------------------------
 // Rows in parts joined: a wave for a row, or a workgroup where rows have many
 // parts, or, where there are more rows than waves, a quarter of a wave.
@@ -1115,8 +1276,8 @@ __device__ __forceinline__ float part_weight(v2f stat, float m, float scale2)
 // elements a lane); a row's sequence is looked for only where it is not the last
 // one's.  Bound by reading the parts: 95,488 rows of 64 in two parts 16.6 us, 105,600
 // of 128 29.7, where a wave for a row took 48 and 63.
-template <typename T, int D>
-__device__ __forceinline__ void join_quarters(const AttnIn& a, const PlanView& pv, uint64_t y0, uint64_t y1)
+template <typename T, int D, bool PAIR = false>
+__device__ __forceinline__ void join_quarters(const InOf<PAIR>& a, const PlanView& pv, uint64_t y0, uint64_t y1)
 {
     constexpr int kPer = D / 16, kAtOnce = 4;
     const uint32_t g = lane_id() / 16, d = lane_id() % 16 * kPer;
@@ -1176,15 +1337,38 @@ __device__ __forceinline__ void join_quarters(const AttnIn& a, const PlanView& p
             continue;
         const bool seen = total > 0 || total != total;
         const float inv = seen ? 1.0f / total : 0.0f;
-        typedef T v4t __attribute__((ext_vector_type(4)));
-        uint16_t* out = a.out + t * a.out_stride + (uint64_t)x * D + d;
+        if constexpr (PAIR) {
+            // the maps' rows are in neighbouring quarters, in the same loop or in none
+            const float lambda = a.lambda[x / 2];
+            float ss = 0;
 #pragma unroll
-        for (int c = 0; c < kPer / 4; c++) {
-            v4t z;
+            for (int c = 0; c < kPer; c++) {
+                v[c] *= inv;
+                v[c] = __builtin_fmaf(-lambda, __shfl_xor(v[c], 16), v[c]);
+                ss = __builtin_fmaf(v[c], v[c], ss);
+            }
+            float by = a.gain;
+            if (a.norm) {
 #pragma unroll
-            for (int k = 0; k < 4; k++)
-                z[k] = (T)(v[c * 4 + k] * inv);
-            *reinterpret_cast<v4t*>(out + c * 4) = z;
+                for (int o = 1; o < 16; o *= 2)
+                    ss += __shfl_xor(ss, o);
+                by *= norm_of<D>(ss, a.eps);
+            }
+            if (x % 2 == 0)
+#pragma unroll
+                for (int c = 0; c < kPer; c += 4)
+                    write_normed<T>(a, t, x, D / 2, d + c, v4f{v[c], v[c + 1], v[c + 2], v[c + 3]}, by);
+        } else {
+            typedef T v4t __attribute__((ext_vector_type(4)));
+            uint16_t* out = a.out + t * a.out_stride + (uint64_t)x * D + d;
+#pragma unroll
+            for (int c = 0; c < kPer / 4; c++) {
+                v4t z;
+#pragma unroll
+                for (int k = 0; k < 4; k++)
+                    z[k] = (T)(v[c * 4 + k] * inv);
+                *reinterpret_cast<v4t*>(out + c * 4) = z;
+            }
         }
         if (d == 0 && a.lse)
             a.lse[(uint64_t)t * a.q_heads + x] = seen ? lse_of<T>(m, total, a.scale2) : -INFINITY;

@@ -436,8 +436,6 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attn_kernel(AttnIn
 // of 256 on 256 and 384 keys 12.5 and 16.0, in parts 13.8 and 13.9.  1 to 64 KV heads
 // are within 0.4 us of these in this form.  Of several sequences the keys count together:
 // four tokens on 768 keys 7.2, in parts 10.6.
-template <int D>
-constexpr int kSmallWaves = D == 256 ? 4 : 8;
 template <typename T, int D>
 __global__ __launch_bounds__(kSmallWaves<D>* kWave, 1) void attn_small_kernel(AttnIn a, const PlanView pv,
                                                                               uint32_t* status)

@@ -439,7 +439,7 @@ hipError_t queue_ends(dm_ctx* c, const int64_t* qoff, int64_t* first, int64_t* l
 hipError_t rebalance(dm_ctx* c, const dm_queues* q, int64_t* loads_out, const dm_migrations* out,
                      uint64_t cap, uint64_t Q);
 
-// dm_pages.hip, dm_append.hip, dm_attn.hip: KV pages and attention over them,
+// dm_pages.hip, dm_append.hip, dm_attn.hip, dm_diff.hip: KV pages and attention over them,
 // asynchronous on c->stream; arguments checked by the entry points (dm_api.hip).
 hipError_t pages_fork(dm_ctx* c, const dm_page_tables& in, const int32_t* ref, uint32_t n_pages,
                       const int32_t* src, const int64_t* keep, const int64_t* grow, uint64_t m,
@@ -456,6 +456,11 @@ hipError_t attn_plan(dm_ctx* c, const dm_token_batch& b, const dm_kv_pages& kv, 
 hipError_t attn(dm_ctx* c, const dm_token_batch& b, const dm_kv_pages& kv, uint32_t q_heads,
                 const void* plan, uint32_t layer, const void* q, int64_t q_stride, float scale,
                 void* out, int64_t out_stride, float* lse);
+// dm_diff.hip: attention's view of a store whose KV heads are pairs; its plan is
+// attn_plan's of that view.
+dm_kv_pages pairs_of(const dm_kv_pages& kv);
+hipError_t diff_attn(dm_ctx* c, const dm_token_batch& b, const dm_kv_pages& kv, uint32_t q_heads,
+                     const void* plan, uint32_t layer, const dm_diff_args& a);
 
 }  // namespace dm
 
