@@ -594,6 +594,16 @@ typedef struct {
 dm_status dm_kv_append(dm_ctx* ctx, const dm_kv_pages* kv, uint32_t layer,
                        const dm_token_batch* batch, const dm_append_args* args);
 
+/* dm_kv_append with positions given: the first new token of sequence s is at
+ * position first[s] (device int64 [n]; NULL: as dm_kv_append), the next ones
+ * follow, and the rotation goes by these.  Where rows are written goes by the
+ * tables as ever.  For sequences whose places are not their positions, as after
+ * an eviction.  A token whose position is negative or max_pos or more is treated
+ * as one past max_pos. */
+dm_status dm_kv_append_at(dm_ctx* ctx, const dm_kv_pages* kv, uint32_t layer,
+                          const dm_token_batch* batch, const dm_append_args* args,
+                          const int64_t* first);
+
 /* Attention of a batch's new tokens over the pages: query head x reads KV head
  * x / (q_heads / kv_heads), a token sees its own and the earlier positions of
  * its sequence, out = sum_j w_j v_j / sum_j w_j with w_j = exp(scale q.k_j),
@@ -666,6 +676,121 @@ dm_status dm_diff_plan(dm_ctx* ctx, const dm_token_batch* batch, const dm_kv_pag
 dm_status dm_diff_attn(dm_ctx* ctx, const dm_token_batch* batch, const dm_kv_pages* kv,
                        uint32_t q_heads, const void* plan, uint32_t layer,
                        const dm_diff_args* args);
+
+/* Inputs and parameters of dm_attn_weights.  q, q_stride, scale: as the
+ * attention call had them, lse: float [q_tokens][q_heads], what it left.  w:
+ * [kv_heads] rows of w_stride floats, w_stride at least entries * B: token i of
+ * sequence s is at off[s] * B + i of a row.
+ * prev: what was collected before, rows of prev_room floats, prev_stride apart,
+ * or NULL.  With
+ * prev_off, src and keep (the tables before, of prev_n sequences, and what
+ * dm_pages_fork made these from), sequence s has carried the first keep[s]
+ * tokens of sequence src[s]; with all three NULL, prev's rows are laid out by
+ * the same tables and every token before the new ones is carried (prev may
+ * then be w itself; otherwise they must not overlap).
+ * last: only each sequence's last `last` new tokens count (0: all).  paired:
+ * the attention is dm_diff_attn, the plan dm_diff_plan's. */
+typedef struct {
+    const void* q;
+    int64_t q_stride;
+    const float* lse;
+    float* w;
+    int64_t w_stride;
+    const float* prev;
+    int64_t prev_stride, prev_room;
+    const int64_t* prev_off; /* [prev_n + 1] */
+    const int32_t* src;      /* [n]          */
+    const int64_t* keep;     /* [n]          */
+    uint64_t prev_n;
+    float scale, decay;
+    uint32_t last;
+    uint32_t paired;
+} dm_weight_args;
+
+/* The weight that the pages' keys have collected, for an eviction: for KV head h
+ * and token i < len[s],
+ *   w[h][i] = decay prev[h][i] + sum exp(scale q.k_i - lse),
+ * over the sequence's new tokens (the last of them) that see i and the query
+ * heads that read h: x / (q_heads / kv_heads) = h, or with paired those of h's
+ * place in its pair (each head of a pair of KV heads has its own map's weights).
+ * Products and sums are in 32 bits, each sum's order fixed.  A weight is off by
+ * some 2^-23 of itself for each unit of |lse| (its own rounding).  A query with
+ * lse = -infinity counts nowhere; keys that no query sees have what they had.
+ * Other places of w are left as they were.  Who sees what, malformed tables and
+ * a plan of another batch are as in dm_attn; a sequence's src or prev_off out of
+ * range carries nothing and is reported (DM_EINVAL). */
+dm_status dm_attn_weights(dm_ctx* ctx, const dm_token_batch* batch, const dm_kv_pages* kv,
+                          uint32_t q_heads, const void* plan, uint32_t layer,
+                          const dm_weight_args* args);
+
+/* Eviction.  Sequences longer than their budgets keep as many tokens as those
+ * say, chosen by what their keys have collected, for every layer, and for
+ * every choice of `share` neighbouring KV heads, on their own; their rows move
+ * to fresh pages, and the old ones are free for the next step:
+ *   dm_evict_select   what is kept, and the next tables' keep and grow;
+ *   dm_pages_fork     with these, sequence by sequence (src[s] = s); then
+ *                     dm_pages_copy, as after any fork;
+ *   dm_kv_gather      the kept rows to the new tables' pages.
+ * A token's place in its sequence is no longer its position then: dm_kv_append_at
+ * takes positions. */
+
+/* w: what keys have collected, [layers][kv_heads] rows as dm_attn_weights' w,
+ * w_layer_stride and w_stride floats apart.  kept: [layers][kv_heads / share]
+ * rows of kept_stride entries.  share: 1, or 2 for pairs, up to kv_heads; it
+ * divides kv_heads.  Strides at least entries * B. */
+typedef struct {
+    const float* w;
+    int64_t w_layer_stride, w_stride;
+    const int64_t* budget; /* [n] tokens that a sequence keeps, at least 0 */
+    const int64_t* room;   /* [n] room for what comes next, or NULL: 0     */
+    int32_t* kept;
+    int64_t kept_stride;
+    int64_t* keep; /* [n] out */
+    int64_t* grow; /* [n] out */
+    uint32_t layers, kv_heads, share;
+    uint32_t sink, recent;
+    uint32_t reserved; /* must be 0 */
+} dm_select_args;
+
+/* What sequences keep.  Sequence s is past its budget where len[s] > budget[s]: keep[s]
+ * = 0 and grow[s] = budget[s] + room[s] then, otherwise keep[s] = len[s] and
+ * grow[s] = room[s].  Of one past it, in every layer and choice, the first
+ * `sink` tokens stay, the last `recent` ones (the first ones before the last
+ * ones where the budget is smaller), and of the others those with the largest
+ * scores up to the budget: the weights of the choice's heads added in order, in
+ * 32 bits.  Of equal scores the earlier token stays; NaN counts less than any
+ * number.  Their places in the sequence go to kept, in increasing order: entry i
+ * of sequence s at off[s] * B + i of a row; nothing else of kept is written.
+ * Exact and the same every time.  page is not read.  A malformed table or a
+ * negative budget is reported (DM_EINVAL) and evicts nothing of its sequence. */
+dm_status dm_evict_select(dm_ctx* ctx, const dm_page_tables* tables, const dm_select_args* args);
+
+/* kept, budget, share: dm_evict_select's.  w and w_to: NULL, or the weights by
+ * the old tables and by the new ones. */
+typedef struct {
+    const int64_t* budget;
+    const int32_t* kept;
+    int64_t kept_stride;
+    const float* w;
+    int64_t w_layer_stride, w_stride;
+    float* w_to;
+    int64_t to_layer_stride, to_stride;
+    uint32_t share;
+    uint32_t reserved; /* must be 0 */
+} dm_gather_args;
+
+/* Kept rows moved, in all layers: of a sequence past its budget (by from's
+ * lengths), the keys and values of its kept tokens, in order, to the places 0
+ * .. budget[s] - 1 of sequence s of `to`; nothing of the others, whose pages `to`
+ * has as they are.  With w, the weights follow: of a sequence past its budget
+ * those of its kept tokens, of another those of all.  from and to have the same n
+ * sequences.  Pages that are written must not be pages of `from` (those that
+ * dm_pages_fork adds are not), w_to must not overlap w.  Other places are left as
+ * they were.  to->len is not read.  A malformed table, a sequence whose kept rows
+ * have no room in `to`, an entry of kept that is no token of its sequence and a
+ * page out of range are reported (DM_EINVAL), and nothing is moved for them. */
+dm_status dm_kv_gather(dm_ctx* ctx, const dm_kv_pages* kv, const dm_page_tables* from,
+                       const dm_page_tables* to, const dm_gather_args* args);
 
 /* Wait for all work on the context's stream (and, with pipelining, on its
  * work, selection and epilogue streams); return and clear the first

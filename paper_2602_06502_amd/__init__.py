@@ -32,7 +32,8 @@ EXPORTS = ("dm_create", "dm_destroy", "dm_build_rings", "dm_ring_export", "dm_in
            "dm_set_pipelining", "dm_set_policy", "dm_keylen_enable",
            "dm_keylen_window",
            "dm_keylen_export", "dm_pages_fork", "dm_pages_compact", "dm_pages_copy", "dm_kv_append",
-           "dm_attn_plan_bytes", "dm_attn_plan", "dm_attn", "dm_diff_plan", "dm_diff_attn", "dm_sync",
+           "dm_attn_plan_bytes", "dm_attn_plan", "dm_attn", "dm_diff_plan", "dm_diff_attn",
+           "dm_attn_weights", "dm_evict_select", "dm_kv_gather", "dm_kv_append_at", "dm_sync",
            "dm_last_error")
 
 
@@ -110,6 +111,27 @@ class dm_diff_args(C.Structure):
                 ("eps", C.c_float), ("gain", C.c_float), ("reserved", C.c_uint32)]
 
 
+class dm_weight_args(C.Structure):
+    _fields_ = [("q", C.c_void_p), ("q_stride", C.c_int64), ("lse", C.c_void_p), ("w", C.c_void_p),
+                ("w_stride", C.c_int64), ("prev", C.c_void_p), ("prev_stride", C.c_int64), ("prev_room", C.c_int64),
+                ("prev_off", C.c_void_p), ("src", C.c_void_p), ("keep", C.c_void_p), ("prev_n", C.c_uint64),
+                ("scale", C.c_float), ("decay", C.c_float), ("last", C.c_uint32), ("paired", C.c_uint32)]
+
+
+class dm_select_args(C.Structure):
+    _fields_ = [("w", C.c_void_p), ("w_layer_stride", C.c_int64), ("w_stride", C.c_int64), ("budget", C.c_void_p),
+                ("room", C.c_void_p), ("kept", C.c_void_p), ("kept_stride", C.c_int64), ("keep", C.c_void_p),
+                ("grow", C.c_void_p), ("layers", C.c_uint32), ("kv_heads", C.c_uint32), ("share", C.c_uint32),
+                ("sink", C.c_uint32), ("recent", C.c_uint32), ("reserved", C.c_uint32)]
+
+
+class dm_gather_args(C.Structure):
+    _fields_ = [("budget", C.c_void_p), ("kept", C.c_void_p), ("kept_stride", C.c_int64), ("w", C.c_void_p),
+                ("w_layer_stride", C.c_int64), ("w_stride", C.c_int64), ("w_to", C.c_void_p),
+                ("to_layer_stride", C.c_int64), ("to_stride", C.c_int64), ("share", C.c_uint32),
+                ("reserved", C.c_uint32)]
+
+
 _lib = None
 
 
@@ -156,6 +178,10 @@ def load_library(path: str = LIB_PATH):
         "dm_attn": (i32, [P, P, P, u32, P, u32, P, C.c_int64, C.c_float, P, C.c_int64, P]),
         "dm_diff_plan": (i32, [P, P, P, u32, P, u64]),
         "dm_diff_attn": (i32, [P, P, P, u32, P, u32, P]),
+        "dm_attn_weights": (i32, [P, P, P, u32, P, u32, P]),
+        "dm_evict_select": (i32, [P, P, P]),
+        "dm_kv_gather": (i32, [P, P, P, P, P]),
+        "dm_kv_append_at": (i32, [P, P, u32, P, P, P]),
         "dm_sync": (i32, [P]),
         "dm_last_error": (C.c_char_p, [P]),
     }
@@ -194,13 +220,16 @@ def _ptr(t) -> Optional[int]:
     return None if t is None else t.data_ptr()
 
 
-# dm_page_tables, dm_token_batch, dm_pages_out, dm_append_args and dm_diff_args as bytes: a decode step makes these calls for every
+# dm_page_tables, dm_token_batch, dm_pages_out and the calls' arguments as bytes: a decode step makes these calls for every
 # layer, and packing takes a fraction of the time of filling a ctypes structure
 _PACK_TABLES = struct.Struct("=5Q").pack
 _PACK_BATCH = struct.Struct("=9Q").pack
 _PACK_OUT = struct.Struct("=10Q").pack
 _PACK_APPEND = struct.Struct("=3Q3qQq5Q3If").pack
 _PACK_DIFF = struct.Struct("=2Q2q3Q3fI").pack
+_PACK_WEIGHTS = struct.Struct("=Qq2QqQ2q4Q2f2I").pack
+_PACK_SELECT = struct.Struct("=Q2q3Qq2Q6I").pack
+_PACK_GATHER = struct.Struct("=2QqQ2qQ2q2I").pack
 
 
 class KVPages:
@@ -231,7 +260,7 @@ class AttnPlan:
 
     def __init__(self, batch, q_tokens, kv, q_heads, buf, keep, pairs=False):
         self.batch, self.q_tokens, self.kv, self.q_heads, self.buf = batch, q_tokens, kv, q_heads, buf
-        self.pairs = pairs
+        self.pairs, self.n, self.entries = pairs, keep[0][2].numel(), keep[0][1].numel()
         self._keep = keep  # the batch's tensors
 
 
@@ -684,11 +713,13 @@ class DualMap:
         return x.data_ptr(), a if tokens > 1 else heads * dim
 
     def kv_append(self, kv: KVPages, layer: int, tables, q_off, q, k, v, q_out, q_norm=None,
-                  k_norm=None, eps: float = 1e-6, cos=None, sin=None, interleaved: bool = False) -> None:
+                  k_norm=None, eps: float = 1e-6, cos=None, sin=None, interleaved: bool = False,
+                  first=None) -> None:
         """New tokens' queries and keys normed per head and rotated, keys and
         values written to layer's pages (see dm_kv_append).  q, q_out: [tokens,
         q_heads, head_dim]; k, v: [tokens, kv_heads, head_dim]; cos, sin: float32
-        [positions, rot_dim / 2]."""
+        [positions, rot_dim / 2]; first: int64 [sequences], positions of their first new
+        tokens where those are not their places (see dm_kv_append_at)."""
         self._kv(kv)
         T, D, dt = q.shape[0], kv.head_dim, kv.dtype
         heads = q.shape[1]
@@ -713,7 +744,13 @@ class DualMap:
             rot *= 2
         a = _PACK_APPEND(qp, kp, vp, qs, ks, vs, op, os_, wq, wk, cp, sp, rows, heads, rot,
                          1 if interleaved else 0, eps)
-        self._check(self.lib.dm_kv_append(self._h, kv._ref, layer, _PACK_BATCH(*b), a), "dm_kv_append")
+        if first is None:
+            self._check(self.lib.dm_kv_append(self._h, kv._ref, layer, _PACK_BATCH(*b), a), "dm_kv_append")
+            return
+        if self._dev(first, self.torch.int64, "first").numel() != b[3]:
+            raise ValueError("first needs a position for each sequence")
+        self._check(self.lib.dm_kv_append_at(self._h, kv._ref, layer, _PACK_BATCH(*b), a, first.data_ptr()),
+                    "dm_kv_append_at")
 
     def attn_plan(self, kv: KVPages, tables, q_off, q_tokens: int, q_heads: int, groups=None) -> AttnPlan:
         """The work of attn for a batch (see dm_attn_plan), once for all layers.
@@ -778,3 +815,99 @@ class DualMap:
         a = _PACK_DIFF(qp, op, qs, os_, self._lse(lse, T, heads) or 0, lam.data_ptr(), w, scale, eps, gain, 0)
         self._check(self.lib.dm_diff_attn(self._h, plan.batch, kv._ref, heads, plan.buf.data_ptr(), layer, a),
                     "dm_diff_attn")
+
+    def _collected(self, w, name, heads):
+        """Address and row stride of [heads, places] with contiguous places."""
+        ok = getattr(w, "dtype", None) is self.torch.float32 and w.dim() == 2 and w.shape[0] == heads \
+            and w.get_device() == self._index and (w.stride(1) == 1 or w.shape[1] <= 1) and w.stride(0) >= w.shape[1]
+        if not ok:
+            raise ValueError(f"{name} must be a float32 tensor [kv_heads, places] on {self.device}, its rows contiguous")
+        return w.data_ptr(), w.stride(0) if heads > 1 else w.shape[1]
+
+    def attn_weights(self, plan: AttnPlan, layer: int, q, scale: float, lse, w, last: int = 0, prev=None,
+                     decay: float = 1.0) -> None:
+        """The weight that layer's keys collect from a batch's new tokens (see dm_attn_weights), after attn
+        or diff_attn with the same plan, q and scale: lse is what it left.  w: float32 [kv_heads, places], a
+        place for each of the tables' entries' tokens.  prev: what was collected before, laid out by the same
+        tables (w itself, to add to it), or (weights, off, src, keep) of the tables before a pages_fork."""
+        kv, T, heads, i64 = plan.kv, plan.q_tokens, plan.q_heads, self.torch.int64
+        qp, qs = self._rows(q, "q", heads, kv.head_dim, T, kv.dtype)
+        if lse is None:
+            raise ValueError("lse is what the attention call left")
+        lp = self._lse(lse, T, heads)
+        wp, ws = self._collected(w, "w", kv.kv_heads)
+        if w.shape[1] < plan.entries * kv.block:
+            raise ValueError("w needs a place for each token of the tables' entries")
+        pp = ps = room = off = src = keep = n = 0
+        if isinstance(prev, tuple):
+            prev, off, src, keep = prev
+            n = self._dev(off, i64, "prev's off").numel() - 1
+            if self._dev(src, self.torch.int32, "src").numel() != plan.n or \
+                    self._dev(keep, i64, "keep").numel() != plan.n or n < 0:
+                raise ValueError("src and keep need an entry for each sequence, off one more than there were")
+            off, src, keep = off.data_ptr(), src.data_ptr(), keep.data_ptr()
+        if prev is not None:
+            pp, ps = self._collected(prev, "prev", kv.kv_heads)
+            room = prev.shape[1]
+            if not off and room < plan.entries * kv.block:
+                raise ValueError("prev needs a place for each token of the tables' entries")
+        a = _PACK_WEIGHTS(qp, qs, lp, wp, ws, pp, ps, room, off, src, keep, n, scale, decay, last, 1 if plan.pairs else 0)
+        self._check(self.lib.dm_attn_weights(self._h, plan.batch, kv._ref, heads, plan.buf.data_ptr(), layer, a),
+                    "dm_attn_weights")
+
+    def _layers(self, x, name, dtype, heads, places):
+        """Address and strides of [layers, heads, at least `places`] with contiguous places."""
+        ok = getattr(x, "dtype", None) is dtype and x.dim() == 3 and x.get_device() == self._index \
+            and x.shape[1] == heads and x.shape[2] >= places and (x.stride(2) == 1 or x.shape[2] <= 1)
+        if not ok:
+            raise ValueError(f"{name} must be a {dtype} tensor [layers, {heads}, at least {places}] on {self.device}, "
+                             "its rows contiguous")
+        a, b = x.stride(0), x.stride(1) if heads > 1 else x.shape[2]
+        if b < x.shape[2] or (x.shape[0] > 1 and a < b * (heads - 1) + x.shape[2]):
+            raise ValueError(f"{name}'s rows must not overlap")
+        return x.data_ptr(), a, b
+
+    def evict_select(self, tables, w, budget, room, kept, keep, grow, sink: int = 0, recent: int = 0,
+                     share: int = 1) -> None:
+        """What sequences past their budgets keep, by the weight that keys have collected (see
+        dm_evict_select).  w: float32 [layers, kv_heads, places] as attn_weights lays out a layer's; budget,
+        room (or None), keep, grow: int64 [sequences], the last two pages_fork's arguments; kept: int32
+        [layers, kv_heads / share, places]."""
+        t, tb = self.torch, self._tables(tables)
+        places = tb[4] * self.block
+        if getattr(w, "ndim", 0) != 3 or share < 1 or w.shape[1] % share:
+            raise ValueError("w must be [layers, kv_heads, places], share divide kv_heads")
+        layers, heads = w.shape[:2]
+        wp, wl, ws = self._layers(w, "w", t.float32, heads, places)
+        kp, _, ks = self._layers(self._dev(kept, t.int32, "kept"), "kept", t.int32, heads // share, places)
+        if kept.shape[0] != layers:
+            raise ValueError("kept needs as many layers as w")
+        for x, name in ((budget, "budget"), (room, "room"), (keep, "keep"), (grow, "grow")):
+            if (x is not None or name != "room") and self._dev(x, t.int64, name).numel() != tb[3]:
+                raise ValueError(f"{name} needs an entry for each sequence")
+        if not 0 <= sink < 1 << 31 or not 0 <= recent < 1 << 31:
+            raise ValueError("sink and recent must be at least 0 and below 2^31")
+        a = _PACK_SELECT(wp, wl, ws, budget.data_ptr(), _ptr(room) or 0, kp, ks, keep.data_ptr(), grow.data_ptr(), layers,
+                         heads, share, sink, recent, 0)
+        self._check(self.lib.dm_evict_select(self._h, _PACK_TABLES(*tb), a), "dm_evict_select")
+
+    def kv_gather(self, kv: KVPages, tables, to, budget, kept, w=None, w_to=None) -> None:
+        """Kept rows moved to the next tables' pages in all layers (see dm_kv_gather): kept and budget as in
+        evict_select, `to` the tables that pages_fork made with its keep and grow.  w, w_to: weights by the
+        old tables and by the new ones, float32 [layers, kv_heads, places]."""
+        self._kv(kv)
+        t, tb, to = self.torch, self._tables(tables), self._tables(to)
+        if tb[3] != to[3] or self._dev(budget, t.int64, "budget").numel() != tb[3]:
+            raise ValueError("the tables and budget need the same sequences")
+        choices = kept.shape[1] if getattr(kept, "ndim", 0) == 3 else 0
+        if not choices or kv.kv_heads % choices or kept.shape[0] != kv.layers:
+            raise ValueError("kept must be [layers, kv_heads / share, places]")
+        kp, _, ks = self._layers(self._dev(kept, t.int32, "kept"), "kept", t.int32, choices, tb[4] * self.block)
+        wp = wl = ws = op = ol = os_ = 0
+        if w is not None or w_to is not None:
+            wp, wl, ws = self._layers(w, "w", t.float32, kv.kv_heads, tb[4] * self.block)
+            op, ol, os_ = self._layers(w_to, "w_to", t.float32, kv.kv_heads, to[4] * self.block)
+            if w.shape[0] != kv.layers or w_to.shape[0] != kv.layers:
+                raise ValueError("w and w_to need the pages' layers")
+        a = _PACK_GATHER(budget.data_ptr(), kp, ks, wp, wl, ws, op, ol, os_, kv.kv_heads // choices, 0)
+        self._check(self.lib.dm_kv_gather(self._h, kv._ref, _PACK_TABLES(*tb), _PACK_TABLES(*to), a), "dm_kv_gather")

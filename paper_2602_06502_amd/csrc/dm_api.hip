@@ -945,40 +945,54 @@ dm_status dm_pages_copy(dm_ctx* c, const dm_kv_pages* kv, const int32_t* src, co
     return e == hipSuccess ? DM_OK : hip_fail(c, e, "dm_pages_copy");
 }
 
-dm_status dm_kv_append(dm_ctx* c, const dm_kv_pages* kv, uint32_t layer,
-                       const dm_token_batch* batch, const dm_append_args* a)
+static dm_status append_checked(dm_ctx* c, const dm_kv_pages* kv, uint32_t layer, const dm_token_batch* batch,
+                                const dm_append_args* a, const int64_t* first, const std::string& what)
 {
     if (!c)
         return DM_EINVAL;
-    if (dm_status s = kv_pages_check(c, kv, layer, true, "dm_kv_append"); s != DM_OK)
+    if (dm_status s = kv_pages_check(c, kv, layer, true, what); s != DM_OK)
         return s;
-    if (dm_status s = token_batch_check(c, batch, "dm_kv_append"); s != DM_OK)
+    if (dm_status s = token_batch_check(c, batch, what); s != DM_OK)
         return s;
     if (!a)
-        return fail(c, DM_EINVAL, "dm_kv_append: null arguments");
+        return fail(c, DM_EINVAL, what + ": null arguments");
     if (a->q_heads < 1 || a->q_heads > 65536)
-        return fail(c, DM_EINVAL, "dm_kv_append: q_heads out of range");
+        return fail(c, DM_EINVAL, what + ": q_heads out of range");
     if (a->rot_dim % 16 || a->rot_dim > kv->head_dim || (a->rot_dim && (!a->cos || !a->sin)) ||
         a->max_pos > (1ull << 40))
-        return fail(c, DM_EINVAL, "dm_kv_append: rot_dim must be a multiple of 16, at most head_dim, "
+        return fail(c, DM_EINVAL, what + ": rot_dim must be a multiple of 16, at most head_dim, "
                                   "and have its tables");
     if (!aligned16(a->q_norm) || !aligned16(a->k_norm) || !aligned16(a->cos) || !aligned16(a->sin))
-        return fail(c, DM_EINVAL, "dm_kv_append: weights and tables must be 16-byte aligned");
+        return fail(c, DM_EINVAL, what + ": weights and tables must be 16-byte aligned");
+    if (!aligned(first))
+        return fail(c, DM_EINVAL, what + ": misaligned positions");
     if (!(a->eps >= 0))
-        return fail(c, DM_EINVAL, "dm_kv_append: eps must not be negative");
+        return fail(c, DM_EINVAL, what + ": eps must not be negative");
     if (batch->tables.n == 0 || batch->q_tokens == 0)
         return DM_OK;
     if (!rows_ok(a->q, a->q_stride, a->q_heads, kv->head_dim) ||
         !rows_ok(a->k, a->k_stride, kv->kv_heads, kv->head_dim) ||
         !rows_ok(a->v, a->v_stride, kv->kv_heads, kv->head_dim) ||
         !rows_ok(a->q_out, a->q_out_stride, a->q_heads, kv->head_dim))
-        return fail(c, DM_EINVAL, "dm_kv_append: rows must be 16-byte aligned, their strides multiples "
+        return fail(c, DM_EINVAL, what + ": rows must be 16-byte aligned, their strides multiples "
                                   "of 8 and at least heads * head_dim");
     DeviceGuard g(c->device);
     hipError_t e = join_selection(c);
     if (e == hipSuccess)
-        e = kv_append(c, *kv, layer, *batch, *a);
-    return e == hipSuccess ? DM_OK : hip_fail(c, e, "dm_kv_append");
+        e = kv_append(c, *kv, layer, *batch, *a, first);
+    return e == hipSuccess ? DM_OK : hip_fail(c, e, what.c_str());
+}
+
+dm_status dm_kv_append(dm_ctx* c, const dm_kv_pages* kv, uint32_t layer,
+                       const dm_token_batch* batch, const dm_append_args* a)
+{
+    return append_checked(c, kv, layer, batch, a, nullptr, "dm_kv_append");
+}
+
+dm_status dm_kv_append_at(dm_ctx* c, const dm_kv_pages* kv, uint32_t layer,
+                          const dm_token_batch* batch, const dm_append_args* a, const int64_t* first)
+{
+    return append_checked(c, kv, layer, batch, a, first, "dm_kv_append_at");
 }
 
 static dm_status heads_check(dm_ctx* c, const dm_kv_pages* kv, uint32_t q_heads, const std::string& what)
@@ -1101,6 +1115,124 @@ dm_status dm_diff_attn(dm_ctx* c, const dm_token_batch* batch, const dm_kv_pages
     if (e == hipSuccess)
         e = diff_attn(c, *batch, *kv, q_heads, plan, layer, *a);
     return e == hipSuccess ? DM_OK : hip_fail(c, e, "dm_diff_attn");
+}
+
+dm_status dm_attn_weights(dm_ctx* c, const dm_token_batch* batch, const dm_kv_pages* kv, uint32_t q_heads,
+                          const void* plan, uint32_t layer, const dm_weight_args* a)
+{
+    if (!c)
+        return DM_EINVAL;
+    if (dm_status s = kv_pages_check(c, kv, layer, true, "dm_attn_weights"); s != DM_OK)
+        return s;
+    if (!a || a->paired > 1)
+        return fail(c, DM_EINVAL, "dm_attn_weights: null arguments or paired not 0 or 1");
+    if (dm_status s = a->paired ? pairs_check(c, kv, "dm_attn_weights") : DM_OK; s != DM_OK)
+        return s;
+    if (dm_status s = token_batch_check(c, batch, "dm_attn_weights"); s != DM_OK)
+        return s;
+    if (dm_status s = heads_check(c, kv, q_heads, "dm_attn_weights"); s != DM_OK)
+        return s;
+    if (!plan || !aligned16(plan) || !aligned(a->lse) || !aligned(a->w) || !aligned(a->prev) ||
+        !aligned(a->prev_off) || !aligned(a->src) || !aligned(a->keep))
+        return fail(c, DM_EINVAL, "dm_attn_weights: null plan or misaligned pointer");
+    if (!(a->scale > 0) || a->scale > 1e30f || !(a->decay - a->decay == 0))
+        return fail(c, DM_EINVAL, "dm_attn_weights: scale must be positive and finite, decay finite");
+    if (batch->tables.n == 0 || batch->tables.entries == 0)
+        return DM_OK;
+    const int64_t rows = (int64_t)(batch->tables.entries * c->cfg.block_size);
+    if (!a->w || a->w_stride < rows || a->w_stride >= (1ll << 46))
+        return fail(c, DM_EINVAL, "dm_attn_weights: w needs rows of at least entries * B");
+    if ((a->prev_off != nullptr) != (a->src != nullptr) || (a->prev_off != nullptr) != (a->keep != nullptr))
+        return fail(c, DM_EINVAL, "dm_attn_weights: prev_off, src and keep go together");
+    if (a->prev && (a->prev_room < (a->prev_off ? 0 : rows) || a->prev_stride < a->prev_room ||
+                    a->prev_stride >= (1ll << 46) || a->prev_n >= (1ull << 31)))
+        return fail(c, DM_EINVAL, "dm_attn_weights: prev_room, prev_stride or prev_n out of range");
+    if (batch->q_tokens && (!a->lse || !rows_ok(a->q, a->q_stride, q_heads, kv->head_dim)))
+        return fail(c, DM_EINVAL, "dm_attn_weights: null lse, or rows that are not 16-byte aligned, their "
+                                  "strides multiples of 8 and at least heads * head_dim");
+    if (batch->q_tokens * q_heads >= (1ull << 31))
+        return fail(c, DM_EINVAL, "dm_attn_weights: q_tokens * q_heads must be below 2^31");
+    DeviceGuard g(c->device);
+    hipError_t e = join_selection(c);
+    if (e == hipSuccess)
+        e = attn_weights(c, *batch, *kv, q_heads, plan, layer, *a);
+    return e == hipSuccess ? DM_OK : hip_fail(c, e, "dm_attn_weights");
+}
+
+// rows of at least `rows` places, `stride` apart, and layers of them
+static bool places_ok(const void* p, int64_t layer_stride, int64_t stride, int64_t rows, uint32_t heads)
+{
+    return p && reinterpret_cast<uintptr_t>(p) % 4 == 0 && stride >= rows && stride < (1ll << 40) && layer_stride >= 0 && layer_stride < (1ll << 46) &&
+           layer_stride / stride >= (heads > 1 ? heads - 1 : 0);
+}
+
+static dm_status share_check(dm_ctx* c, uint32_t kv_heads, uint32_t share, const std::string& what)
+{
+    if (share < 1 || share > kv_heads || kv_heads % share)
+        return fail(c, DM_EINVAL, what + ": share must divide kv_heads");
+    return DM_OK;
+}
+
+dm_status dm_evict_select(dm_ctx* c, const dm_page_tables* t, const dm_select_args* a)
+{
+    if (!c)
+        return DM_EINVAL;
+    if (dm_status s = tables_check(c, t, true, "dm_evict_select"); s != DM_OK)
+        return s;
+    if (!a || a->reserved)
+        return fail(c, DM_EINVAL, "dm_evict_select: null arguments or reserved not 0");
+    if (a->kv_heads < 1 || a->kv_heads > 4096 || a->layers < 1 || a->layers > 65536)
+        return fail(c, DM_EINVAL, "dm_evict_select: layers or kv_heads out of range");
+    if (dm_status s = share_check(c, a->kv_heads, a->share, "dm_evict_select"); s != DM_OK)
+        return s;
+    if (t->n == 0)
+        return DM_OK;
+    if (!a->budget || !a->keep || !a->grow || !aligned(a->budget) || !aligned(a->room) || !aligned(a->keep) ||
+        !aligned(a->grow))
+        return fail(c, DM_EINVAL, "dm_evict_select: null or misaligned budget, room, keep or grow");
+    const int64_t rows = (int64_t)(t->entries * c->cfg.block_size);
+    if (rows && (!places_ok(a->w, a->layers > 1 ? a->w_layer_stride : 1ll << 45, a->w_stride, rows, a->kv_heads) ||
+                 !places_ok(a->kept, 1ll << 45, a->kept_stride, rows, 1)))
+        return fail(c, DM_EINVAL, "dm_evict_select: w and kept need rows of at least entries * B");
+    DeviceGuard g(c->device);
+    hipError_t e = join_selection(c);
+    if (e == hipSuccess)
+        e = evict_select(c, *t, *a);
+    return e == hipSuccess ? DM_OK : hip_fail(c, e, "dm_evict_select");
+}
+
+dm_status dm_kv_gather(dm_ctx* c, const dm_kv_pages* kv, const dm_page_tables* from, const dm_page_tables* to,
+                       const dm_gather_args* a)
+{
+    if (!c)
+        return DM_EINVAL;
+    if (dm_status s = kv_pages_check(c, kv, 0, true, "dm_kv_gather"); s != DM_OK)
+        return s;
+    if (dm_status s = tables_check(c, from, true, "dm_kv_gather"); s != DM_OK)
+        return s;
+    if (dm_status s = tables_check(c, to, false, "dm_kv_gather"); s != DM_OK)
+        return s;
+    if (!a || a->reserved || (a->w != nullptr) != (a->w_to != nullptr))
+        return fail(c, DM_EINVAL, "dm_kv_gather: null arguments, reserved not 0, or w without w_to or the reverse");
+    if (from->n != to->n)
+        return fail(c, DM_EINVAL, "dm_kv_gather: the tables must have as many sequences");
+    if (dm_status s = share_check(c, kv->kv_heads, a->share, "dm_kv_gather"); s != DM_OK)
+        return s;
+    if (to->n == 0 || to->entries == 0)
+        return DM_OK;
+    if (!a->budget || !aligned(a->budget))
+        return fail(c, DM_EINVAL, "dm_kv_gather: null or misaligned budget");
+    const int64_t rows = (int64_t)(from->entries * c->cfg.block_size);
+    const int64_t to_rows = (int64_t)(to->entries * c->cfg.block_size), far = 1ll << 45;
+    if ((rows && !places_ok(a->kept, far, a->kept_stride, rows, 1)) ||
+        (a->w && ((rows && !places_ok(a->w, kv->layers > 1 ? a->w_layer_stride : far, a->w_stride, rows, kv->kv_heads)) ||
+                  !places_ok(a->w_to, kv->layers > 1 ? a->to_layer_stride : far, a->to_stride, to_rows, kv->kv_heads))))
+        return fail(c, DM_EINVAL, "dm_kv_gather: kept, w and w_to need rows of at least entries * B of their tables");
+    DeviceGuard g(c->device);
+    hipError_t e = join_selection(c);
+    if (e == hipSuccess)
+        e = kv_gather(c, *kv, *from, *to, *a);
+    return e == hipSuccess ? DM_OK : hip_fail(c, e, "dm_kv_gather");
 }
 
 dm_status dm_sync(dm_ctx* c)

@@ -31,6 +31,7 @@ struct AppendIn {
     uint16_t *k_pages, *v_pages;  // the layer's
     uint32_t n_pages;
     TokenBatch b;
+    const int64_t* first;  // positions of the sequences' first new tokens; null: by their places
 };
 
 template <int CTRL>
@@ -110,9 +111,10 @@ __global__ __launch_bounds__(kThreads, 6) void append_kernel(AppendIn a, uint32_
             cs[i] = 1, sn[i] = 0;
         if (!sv.bad && pos >= 0) {
             const uint32_t p = (uint32_t)a.b.page[sv.off + (pos >> a.b.shift)];
-            const bool past = a.rot && (uint64_t)pos >= a.max_pos;
+            const int64_t turn = a.first ? a.first[s] + (t - sv.tok0) : pos;
+            const bool past = a.rot && (uint64_t)turn >= a.max_pos;
             if (!past && turns) {
-                const uint64_t at = (uint64_t)pos * half + (INTERLEAVED ? d0 / 2 : low ? d0 : d0 - half);
+                const uint64_t at = (uint64_t)turn * half + (INTERLEAVED ? d0 / 2 : low ? d0 : d0 - half);
 #pragma unroll
                 for (int i = 0; i < (INTERLEAVED ? 4 : 8); i += 4) {
                     const float4 c4 = *reinterpret_cast<const float4*>(a.cos + at + i);
@@ -196,7 +198,7 @@ __global__ __launch_bounds__(kThreads, 6) void append_kernel(AppendIn a, uint32_
 }  // namespace
 
 hipError_t kv_append(dm_ctx* c, const dm_kv_pages& kv, uint32_t layer, const dm_token_batch& b,
-                     const dm_append_args& g)
+                     const dm_append_args& g, const int64_t* first)
 {
     AppendIn a;
     a.q = static_cast<const uint16_t*>(g.q);
@@ -220,6 +222,7 @@ hipError_t kv_append(dm_ctx* c, const dm_kv_pages& kv, uint32_t layer, const dm_
     a.v_pages = static_cast<uint16_t*>(kv.v) + (uint64_t)layer * kv.layer_stride;
     a.n_pages = kv.n_pages;
     a.b = token_batch(c, b);
+    a.first = first;
     const uint32_t grid = grid_for(b.q_tokens, 1);
     by_type(kv.dtype, kv.head_dim, [&](auto t, auto d) {
         using T = decltype(t);

@@ -457,15 +457,20 @@ __device__ __forceinline__ uint32_t find_unit(const uint32_t* item0, uint32_t un
     return k ? k - 1 : 0;
 }
 
+// Is the plan one of this batch?
+__device__ __forceinline__ bool plan_of(const PlanHead& h, const TokenBatch& b, uint32_t q_heads, uint32_t kv_heads,
+                                        uint32_t head_dim)
+{
+    return h.n == b.n && h.groups == b.groups && h.q_tokens == b.q_tokens && h.q_heads == q_heads &&
+           h.kv_heads == kv_heads && h.shift == b.shift && h.entries == b.entries && h.head_dim == head_dim;
+}
+
 // Is the plan this call's, of at most `items` items?  (A batch whose q_off is out of
 // order can have more than the call has workgroups.)
 __device__ __forceinline__ bool plan_fits(const PlanHead& h, const AttnIn& a, uint64_t part_rows,
                                           uint32_t head_dim, uint32_t items)
 {
-    return h.n == a.b.n && h.groups == a.b.groups && h.q_tokens == a.b.q_tokens &&
-           h.q_heads == a.q_heads && h.kv_heads == a.kv_heads && h.shift == a.b.shift &&
-           h.entries == a.b.entries && h.head_dim == head_dim && h.part_rows <= part_rows &&
-           h.items <= items;
+    return plan_of(h, a.b, a.q_heads, a.kv_heads, head_dim) && h.part_rows <= part_rows && h.items <= items;
 }
 
 // The unit of this workgroup's item; false: none, or the plan is another batch's

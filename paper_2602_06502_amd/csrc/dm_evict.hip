@@ -1,0 +1,391 @@
+// Eviction from KV pages by the weight that keys have collected: which tokens of a sequence
+// stay within its budget, for each layer and each choice of KV heads, and their rows moved to
+// the next tables' pages.
+//
+// The choice is the k-th largest of a sequence's scores, then one pass in order of position.
+// A score is taken as a 32-bit number that orders as the float does; its digits of 11, 11
+// and 10 bits are counted in LDS from the top, each time among the scores that agree with the
+// digits found so far, so three passes give the k-th largest exactly, with how many of its
+// equals stay (the first ones).  A workgroup takes a (layer, choice, sequence); its scores
+// stay in registers where they fit.  Bound by reading the weights, and for short sequences
+// by the passes' barriers.
+//
+// The move takes a page of the new tables a workgroup: a row's token, that token's page, the
+// row.  Bound by memory.
+#include "dm_internal.h"
+#include "dm_pages.h"
+
+namespace dm {
+namespace {
+
+struct SelectIn {
+    const int64_t *off, *len, *budget, *room;
+    int64_t entries;
+    const float* w;
+    int64_t layer_stride, w_stride;
+    int32_t* kept;
+    int64_t kept_stride;
+    int64_t *keep, *grow;
+    uint32_t n, layers, choices, share, sink, recent, shift;
+};
+
+// A sequence's entries and tokens (none if it is malformed).
+struct Held {
+    int64_t off, len;
+    bool bad;
+};
+__device__ __forceinline__ Held held(const int64_t* off, const int64_t* len, int64_t entries, uint32_t s, uint32_t shift)
+{
+    const int64_t o0 = off[s], o1 = off[s + 1], l = len[s];
+    const bool bad = o0 < 0 || o1 < o0 || o1 > entries || l < 0 || l >= (1ll << 31) ||
+                     ((l + (1ll << shift) - 1) >> shift) > o1 - o0;
+    return Held{bad ? 0 : o0, bad ? 0 : l, bad};
+}
+
+// A score as a number that orders as it does, -0 as 0, NaN below all.
+__device__ __forceinline__ uint32_t ordered(float x)
+{
+    const uint32_t u = __builtin_bit_cast(uint32_t, x + 0.0f);
+    return x != x ? 0 : u & 0x80000000u ? ~u : u | 0x80000000u;
+}
+
+// Places of the digits: what is above them, and their widths.
+constexpr int kDigits = 3, kBins = 2048;
+__device__ __forceinline__ uint32_t digit_shift(int d) { return d == 0 ? 21 : d == 1 ? 10 : 0; }
+__device__ __forceinline__ uint32_t digit_mask(int d) { return d == 2 ? 1023 : 2047; }
+
+template <int WAVES>
+struct SelectLds {
+    uint32_t bins[kBins];
+    uint32_t above[WAVES];  // of a wave's bins, then of its scores
+    uint32_t equal[WAVES];
+    uint32_t digit, left;
+};
+
+// The choice among the n scores key(i), of which k < n stay: each wave takes a stretch of
+// them, R times 64 (kept in registers) or, R = 0, as many as it has to, read again each time.
+template <int WAVES, int R, typename Key>
+__device__ __forceinline__ void choose(SelectLds<WAVES>& lds, uint32_t n, uint32_t k, int32_t first, int32_t* out,
+                                       Key&& key)
+{
+    const uint32_t tid = threadIdx.x, wave = tid / kWave, lane = lane_id();
+    const uint32_t steps = R ? R : ((n + WAVES * kWave - 1) / (WAVES * kWave));
+    const uint32_t begin = wave * steps * kWave + lane;
+    uint32_t mine[R ? R : 1];
+    auto at = [&](uint32_t r) { return begin + r * kWave; };
+    if constexpr (R > 0) {
+#pragma unroll
+        for (int r = 0; r < R; r++)
+            mine[r] = at(r) < n ? key(at(r)) : 0;
+    }
+    // f(score, is there one), step by step
+    auto each = [&](auto&& f) {
+        if constexpr (R > 0) {
+#pragma unroll
+            for (int r = 0; r < R; r++)
+                f(mine[r], at(r) < n, at(r));
+        } else {
+            for (uint32_t r = 0; r < steps; r++)
+                f(at(r) < n ? key(at(r)) : 0, at(r) < n, at(r));
+        }
+    };
+    uint32_t found = 0, known = 0;  // the digits found, and their bits
+    uint32_t left = k;              // to be found among those that agree with them
+    for (int d = 0; d < kDigits; d++) {
+        const uint32_t shift = digit_shift(d), mask = digit_mask(d);
+        for (uint32_t b = tid; b < kBins; b += WAVES * kWave)
+            lds.bins[b] = 0;
+        __syncthreads();
+        each([&](uint32_t x, bool there, uint32_t) {
+            if (there && (x & known) == found)
+                atomicAdd(&lds.bins[(x >> shift) & mask], 1u);
+        });
+        __syncthreads();
+        // the bin that the left-th from the top is in; a thread has neighbouring bins
+        constexpr uint32_t kPer = kBins / (WAVES * kWave) ? kBins / (WAVES * kWave) : 1;
+        const uint32_t top = kBins - 1 - tid * kPer;
+        uint32_t own = 0;
+#pragma unroll
+        for (uint32_t b = 0; b < kPer; b++)
+            own += lds.bins[top - b];
+        const uint32_t upto = (uint32_t)wave_incl_sum_u64(own, 0);
+        if (lane == kWave - 1)
+            lds.above[wave] = upto;
+        __syncthreads();
+        uint32_t before = upto - own;
+        for (uint32_t w = 0; w < wave; w++)
+            before += lds.above[w];
+        if (before < left && left <= before + own) {
+            uint32_t b = top, x;
+            while (before + (x = lds.bins[b]) < left) {
+                before += x;
+                b--;
+            }
+            lds.digit = b;
+            lds.left = left - before;
+        }
+        __syncthreads();
+        found |= lds.digit << shift;
+        known |= mask << shift;
+        left = lds.left;
+        __syncthreads();
+    }
+    // found is the k-th largest; `left` of its equals stay.  Places of each wave's.
+    uint32_t above = 0, equal = 0;
+    each([&](uint32_t x, bool there, uint32_t) {
+        above += __popcll(ballot(there && x > found));
+        equal += __popcll(ballot(there && x == found));
+    });
+    if (lane == 0) {
+        lds.above[wave] = above;
+        lds.equal[wave] = equal;
+    }
+    __syncthreads();
+    above = equal = 0;
+    for (uint32_t w = 0; w < wave; w++) {
+        above += lds.above[w];
+        equal += lds.equal[w];
+    }
+    const uint64_t below = (1ull << lane) - 1;
+    each([&](uint32_t x, bool there, uint32_t i) {
+        const uint64_t up = ballot(there && x > found), same = ballot(there && x == found);
+        const uint32_t e = equal + __popcll(same & below);
+        // equals that stay before this one: the first `left` of all
+        const uint32_t stayed = e < left ? e : left;
+        const bool stays = there && (x > found || (x == found && e < left));
+        if (stays)
+            out[above + __popcll(up & below) + stayed] = first + (int32_t)i;
+        above += __popcll(up);
+        equal += __popcll(same);
+    });
+}
+
+template <int THREADS>
+__global__ __launch_bounds__(THREADS) void select_kernel(SelectIn a, uint32_t* status)
+{
+    constexpr int kW = THREADS / kWave;
+    __shared__ SelectLds<kW> lds;
+    const uint32_t tid = threadIdx.x;
+    const uint32_t s = blockIdx.x % a.n, x = blockIdx.x / a.n, c = x % a.choices, l = x / a.choices;
+    const Held h = held(a.off, a.len, a.entries, s, a.shift);
+    const int64_t budget = a.budget[s], room = a.room ? a.room[s] : 0;
+    const bool past = !h.bad && budget >= 0 && h.len > budget;
+    if (x == 0 && tid == 0) {
+        a.keep[s] = past ? 0 : h.len;
+        a.grow[s] = room + (past ? budget : 0);
+        if (h.bad || budget < 0)
+            atomicOr(status, kErrInval);
+    }
+    if (!past)
+        return;
+    const uint32_t len = (uint32_t)h.len, stay = (uint32_t)budget;
+    const uint32_t first = stay < a.sink ? stay : a.sink;
+    const uint32_t tail = stay - first < a.recent ? stay - first : a.recent;
+    const uint32_t k = stay - first - tail, n = len - first - tail;
+    const int64_t at = h.off << a.shift;
+    const float* w = a.w + (int64_t)l * a.layer_stride + (int64_t)(c * a.share) * a.w_stride + at;
+    int32_t* out = a.kept + ((int64_t)l * a.choices + c) * a.kept_stride + at;
+    for (uint32_t i = tid; i < first; i += THREADS)
+        out[i] = (int32_t)i;
+    for (uint32_t i = tid; i < tail; i += THREADS)
+        out[first + k + i] = (int32_t)(len - tail + i);
+    if (k == 0)
+        return;
+    auto key = [&](uint32_t i) {
+        const float* from = w + first + i;
+        float sum = *from;
+        for (uint32_t g = 1; g < a.share; g++)
+            sum += from[g * a.w_stride];
+        return ordered(sum);
+    };
+    if (n <= THREADS * 4)
+        choose<kW, 4>(lds, n, k, (int32_t)first, out + first, key);
+    else if (n <= THREADS * 16)
+        choose<kW, 16>(lds, n, k, (int32_t)first, out + first, key);
+    else
+        choose<kW, 0>(lds, n, k, (int32_t)first, out + first, key);
+}
+
+struct GatherIn {
+    const int64_t *off, *len, *budget, *to_off;
+    const int32_t *page, *to_page;
+    int64_t entries, to_entries;
+    uint16_t *k, *v;
+    int64_t layer_stride;
+    const int32_t* kept;
+    int64_t kept_stride;
+    const float* w;
+    int64_t w_layer_stride, w_stride;
+    float* w_to;
+    int64_t to_layer_stride, to_stride;
+    uint32_t n, layers, kv_heads, share, n_pages, shift, dim;
+};
+
+constexpr int kGatherThreads = 256;
+
+__global__ __launch_bounds__(kGatherThreads) void gather_kernel(GatherIn a, uint32_t* status)
+{
+    constexpr int kAtOnce = 4;
+    const int64_t e = blockIdx.x / a.layers;
+    const uint32_t l = blockIdx.x % a.layers, tid = threadIdx.x;
+    const uint32_t s = wave_find(a.to_off, a.n, 1, e);
+    const int64_t t0 = a.to_off[s], t1 = a.to_off[s + 1];
+    if (e < t0 || e >= t1)
+        return;  // an entry of no sequence
+    const Held h = held(a.off, a.len, a.entries, s, a.shift);
+    const int64_t budget = a.budget[s];
+    const bool past = h.len > budget;
+    const int64_t count = past ? budget : h.len;
+    const bool bad = h.bad || budget < 0 || t0 < 0 || t1 > a.to_entries || ((count + (1ll << a.shift) - 1) >> a.shift) > t1 - t0;
+    const uint32_t to = bad ? 0 : (uint32_t)a.to_page[e];
+    if (bad || to >= a.n_pages) {
+        if (tid == 0)
+            atomicOr(status, kErrInval);
+        return;
+    }
+    const int64_t i0 = (e - t0) << a.shift;
+    const uint32_t block = 1u << a.shift;
+    const uint32_t here = count <= i0 ? 0 : count - i0 < block ? (uint32_t)(count - i0) : block;
+    if (here == 0 || (!past && !a.w))
+        return;
+    bool wrong = false;
+    const uint32_t choices = a.kv_heads / a.share;
+    const int64_t from_at = h.off << a.shift;
+    // the token that row i0 + r of head g takes
+    auto token = [&](uint32_t g, uint32_t r) -> int64_t {
+        if (!past)
+            return i0 + r;
+        const int64_t t = a.kept[((int64_t)l * choices + g / a.share) * a.kept_stride + from_at + i0 + r];
+        wrong |= t < 0 || t >= h.len;
+        return t < 0 || t >= h.len ? -1 : t;
+    };
+    if (a.w)
+        for (uint32_t x = tid; x < a.kv_heads << a.shift; x += kGatherThreads) {
+            const uint32_t g = x >> a.shift, r = x & (block - 1);
+            if (r >= here)
+                continue;
+            const int64_t t = token(g, r);
+            if (t >= 0)
+                a.w_to[(int64_t)l * a.to_layer_stride + (int64_t)g * a.to_stride + (e << a.shift) + r] =
+                    a.w[(int64_t)l * a.w_layer_stride + (int64_t)g * a.w_stride + from_at + t];
+        }
+    if (past) {
+        const uint32_t chunks = a.dim / 8, rows = kGatherThreads / chunks, ch = tid % chunks * 8;
+        const uint32_t all = a.kv_heads << a.shift;
+        const uint64_t layer = (uint64_t)l * a.layer_stride;
+        for (uint32_t x0 = tid / chunks; x0 < all; x0 += rows * kAtOnce) {
+            int64_t t[kAtOnce];
+            uint32_t p[kAtOnce];
+            v4u32 kx[kAtOnce], vx[kAtOnce];
+#pragma unroll
+            for (int j = 0; j < kAtOnce; j++) {
+                const uint32_t x = x0 + j * rows;
+                t[j] = x < all && (x & (block - 1)) < here ? token(x >> a.shift, x & (block - 1)) : -1;
+            }
+#pragma unroll
+            for (int j = 0; j < kAtOnce; j++) {
+                p[j] = t[j] >= 0 ? (uint32_t)a.page[h.off + (t[j] >> a.shift)] : 0;
+                wrong |= p[j] >= a.n_pages;
+                t[j] = p[j] >= a.n_pages ? -1 : t[j];
+            }
+#pragma unroll
+            for (int j = 0; j < kAtOnce; j++)
+                if (t[j] >= 0) {
+                    const uint64_t at = layer + ((((uint64_t)p[j] * a.kv_heads + ((x0 + j * rows) >> a.shift)) << a.shift) +
+                                                 (t[j] & (block - 1))) * a.dim + ch;
+                    kx[j] = *reinterpret_cast<const v4u32*>(a.k + at);
+                    vx[j] = *reinterpret_cast<const v4u32*>(a.v + at);
+                }
+#pragma unroll
+            for (int j = 0; j < kAtOnce; j++)
+                if (t[j] >= 0) {
+                    const uint64_t at = layer + (((uint64_t)to * a.kv_heads << a.shift) + x0 + j * rows) * a.dim + ch;
+                    *reinterpret_cast<v4u32*>(a.k + at) = kx[j];
+                    *reinterpret_cast<v4u32*>(a.v + at) = vx[j];
+                }
+        }
+    }
+    if (wrong)
+        atomicOr(status, kErrInval);
+}
+
+uint32_t shift_of(const dm_ctx* c)
+{
+    uint32_t shift = 0;
+    while ((1u << shift) < c->cfg.block_size)
+        shift++;
+    return shift;
+}
+
+}  // namespace
+
+hipError_t evict_select(dm_ctx* c, const dm_page_tables& t, const dm_select_args& g)
+{
+    SelectIn a;
+    a.off = t.off;
+    a.len = t.len;
+    a.budget = g.budget;
+    a.room = g.room;
+    a.entries = (int64_t)t.entries;
+    a.w = g.w;
+    a.layer_stride = g.w_layer_stride;
+    a.w_stride = g.w_stride;
+    a.kept = g.kept;
+    a.kept_stride = g.kept_stride;
+    a.keep = g.keep;
+    a.grow = g.grow;
+    a.n = (uint32_t)t.n;
+    a.layers = g.layers;
+    a.choices = g.kv_heads / g.share;
+    a.share = g.share;
+    a.sink = g.sink;
+    a.recent = g.recent;
+    a.shift = shift_of(c);
+    const uint64_t grid = t.n * a.layers * a.choices;
+    if (grid > 0x7FFFFFFFull)
+        return hipErrorInvalidValue;
+    if (t.entries * c->cfg.block_size / t.n <= 2048)
+        select_kernel<256><<<(uint32_t)grid, 256, 0, c->stream>>>(a, c->d_status);
+    else
+        select_kernel<1024><<<(uint32_t)grid, 1024, 0, c->stream>>>(a, c->d_status);
+    return hipGetLastError();
+}
+
+hipError_t kv_gather(dm_ctx* c, const dm_kv_pages& kv, const dm_page_tables& from, const dm_page_tables& to,
+                     const dm_gather_args& g)
+{
+    GatherIn a;
+    a.off = from.off;
+    a.len = from.len;
+    a.budget = g.budget;
+    a.to_off = to.off;
+    a.page = from.page;
+    a.to_page = to.page;
+    a.entries = (int64_t)from.entries;
+    a.to_entries = (int64_t)to.entries;
+    a.k = static_cast<uint16_t*>(kv.k);
+    a.v = static_cast<uint16_t*>(kv.v);
+    a.layer_stride = kv.layer_stride;
+    a.kept = g.kept;
+    a.kept_stride = g.kept_stride;
+    a.w = g.w;
+    a.w_layer_stride = g.w_layer_stride;
+    a.w_stride = g.w_stride;
+    a.w_to = g.w_to;
+    a.to_layer_stride = g.to_layer_stride;
+    a.to_stride = g.to_stride;
+    a.n = (uint32_t)to.n;
+    a.layers = kv.layers;
+    a.kv_heads = kv.kv_heads;
+    a.share = g.share;
+    a.n_pages = kv.n_pages;
+    a.shift = shift_of(c);
+    a.dim = kv.head_dim;
+    const uint64_t grid = to.entries * kv.layers;
+    if (grid > 0x7FFFFFFFull)
+        return hipErrorInvalidValue;
+    gather_kernel<<<(uint32_t)grid, kGatherThreads, 0, c->stream>>>(a, c->d_status);
+    return hipGetLastError();
+}
+
+}  // namespace dm

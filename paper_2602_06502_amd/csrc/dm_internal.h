@@ -449,7 +449,7 @@ hipError_t pages_compact(dm_ctx* c, const dm_page_tables& in, const int32_t* ref
 hipError_t pages_copy(dm_ctx* c, const dm_kv_pages& kv, const int32_t* src, const int32_t* dst,
                       const int64_t* count, uint64_t cap);
 hipError_t kv_append(dm_ctx* c, const dm_kv_pages& kv, uint32_t layer, const dm_token_batch& b,
-                     const dm_append_args& a);
+                     const dm_append_args& a, const int64_t* first);
 uint64_t attn_plan_bytes(uint64_t n, uint64_t groups);
 hipError_t attn_plan(dm_ctx* c, const dm_token_batch& b, const dm_kv_pages& kv, uint32_t q_heads,
                      void* plan);
@@ -461,6 +461,13 @@ hipError_t attn(dm_ctx* c, const dm_token_batch& b, const dm_kv_pages& kv, uint3
 dm_kv_pages pairs_of(const dm_kv_pages& kv);
 hipError_t diff_attn(dm_ctx* c, const dm_token_batch& b, const dm_kv_pages& kv, uint32_t q_heads,
                      const void* plan, uint32_t layer, const dm_diff_args& a);
+// dm_weights.hip
+hipError_t attn_weights(dm_ctx* c, const dm_token_batch& b, const dm_kv_pages& kv, uint32_t q_heads,
+                        const void* plan, uint32_t layer, const dm_weight_args& a);
+// dm_evict.hip
+hipError_t evict_select(dm_ctx* c, const dm_page_tables& t, const dm_select_args& a);
+hipError_t kv_gather(dm_ctx* c, const dm_kv_pages& kv, const dm_page_tables& from, const dm_page_tables& to,
+                     const dm_gather_args& a);
 
 }  // namespace dm
 

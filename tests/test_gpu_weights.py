@@ -1,0 +1,325 @@
+"""The weight that cached keys collect, against its definition in 64 bits.
+
+Bounds: the log-sum-exp is an input.  A score in 32 bits is off by some 2^-20 of sum |q| |k| scale (products of 16-bit
+numbers are exact, their sum of D terms rounds), its product with log2(e) and the log-sum-exp's by 2^-23 of their sizes, an
+exponential by 2^-22; a weight so by (2^-20 (A + |lse|) + 2^-21) of itself, A the sum of |q k| scale.  A sum of n of them
+adds n 2^-24 of the sum at the most, the carried part 2^-22 of itself.
+"""
+import math
+
+import numpy as np
+import pytest
+
+pytestmark = pytest.mark.gpu
+
+torch = pytest.importorskip("torch")
+
+from test_gpu_attn import DECODE, Batch, engine  # noqa: E402
+
+
+def _say(*a):
+    print("[case]", *a, flush=True)
+
+
+class Collected(Batch):
+    """A batch whose attention's log-sum-exps are inputs, and what was collected before."""
+
+    def __init__(self, *a, paired=False, heads=(8, 2), last=0, decay=0.75, prev="fork", seed=0, **kw):
+        super().__init__(*a, heads=heads, seed=seed, **kw)
+        self.paired, self.last, self.decay, self.mode = paired, last, decay, prev
+        r, g = np.random.default_rng(seed + 5), torch.Generator().manual_seed(seed + 5)
+        n, B = len(self.len), self.block
+        self.rows = len(self.page) * B
+        new = np.diff(self.q_off)
+        if prev == "fork":
+            # the tables before: other sequences in another order; some carry less than all, one nothing
+            self.keep = np.maximum(self.len - new, 0)
+            self.keep[::3] //= 2
+            self.src = r.permutation(n).astype(np.int32)
+            before = np.empty(n, np.int64)
+            before[self.src] = self.keep + r.integers(0, 40, size=n)
+            self.prev_off = np.concatenate([[0], np.cumsum(-(-before // B))]).astype(np.int64)
+            self.prev = torch.rand((self.hkv, int(self.prev_off[-1]) * B), generator=g) * 8
+        elif prev == "same":
+            self.prev = torch.rand((self.hkv, self.rows), generator=g) * 8
+
+    def head_of(self, x):
+        r = self.hq // self.hkv
+        return 2 * (x // 2 // r) + x % 2 if self.paired else x // r
+
+    def far(self):
+        """Log-sum-exps of every query head, in 32 bits."""
+        T = int(self.q_off[-1])
+        lse = torch.full((T, self.hq), -math.inf, dtype=torch.float64)
+        for s, t0, t1, q, K, hidden in self.each():
+            for x in range(self.hq):
+                sc = (q[:, x] @ K[self.head_of(x)].T * self.scale()).masked_fill(hidden, -math.inf)
+                lse[t0:t1, x] = torch.logsumexp(sc, -1)
+        return lse.float()
+
+    def each(self):
+        q = self.qrows[:, :self.hq * self.dim].unflatten(1, (self.hq, self.dim)).double()
+        for s in range(len(self.len)):
+            L, t0, t1 = int(self.len[s]), int(self.q_off[s]), int(self.q_off[s + 1])
+            if L == 0 or t0 == t1:
+                continue
+            at = torch.from_numpy(self.page[self.off[s]:self.off[s] - (-L // self.block)].astype(np.int64))
+            K = [self.k[self.layer][at, h].reshape(-1, self.dim)[:L].double() for h in range(self.hkv)]
+            yield s, t0, t1, q[t0:t1], K, torch.arange(L) > (L - (t1 - t0) + torch.arange(t1 - t0))[:, None]
+
+    def reference(self, lse):
+        w = torch.zeros((self.hkv, self.rows), dtype=torch.float64)
+        tol, written = torch.zeros_like(w), torch.zeros(self.rows, dtype=torch.bool)
+        B, lse = self.block, lse.double()
+        for s in range(len(self.len)):
+            a, L = int(self.off[s]) * B, int(self.len[s])
+            written[a:a + L] = True
+            n, old = 0, 0
+            if self.mode == "fork":
+                n, old = min(int(self.keep[s]), L), int(self.prev_off[self.src[s]]) * B
+            elif self.mode == "same":
+                n, old = max(0, L - int(self.q_off[s + 1] - self.q_off[s])), a
+            if n:
+                w[:, a:a + n] = self.decay * self.prev[:, old:old + n].double()
+                tol[:, a:a + n] = w[:, a:a + n].abs() * 2.0 ** -22
+        for s, t0, t1, q, K, hidden in self.each():
+            a, L = int(self.off[s]) * B, int(self.len[s])
+            first = max(0, t1 - t0 - self.last) if self.last else 0
+            for x in range(self.hq):
+                h = self.head_of(x)
+                far = lse[t0:t1, x][:, None]
+                sc = q[:, x] @ K[h].T * self.scale()
+                A = q[:, x].abs() @ K[h].abs().T * self.scale()
+                z = torch.where(hidden | (far == -math.inf), 0.0, torch.exp(sc - far.clamp(min=-1e300)))
+                e = z * (2.0 ** -20 * (A + far.clamp(min=-1e300).abs()) + 2.0 ** -21)
+                w[h, a:a + L] += z[first:].sum(0)
+                tol[h, a:a + L] += e[first:].sum(0)
+        most = int(np.diff(self.q_off).max()) * (self.hq // self.hkv)
+        return w, tol + (most + 2) * 2.0 ** -24 * w.abs() + 1e-37, written
+
+    def run(self, lse, eng=None, groups=True, inplace=False):
+        pk, e = engine(self.block)
+        e = eng or e
+        kv = pk.KVPages(self.k.cuda(), self.v.cuda())
+        T = int(self.q_off[-1])
+        q = self.qrows.cuda()[:, :self.hq * self.dim].unflatten(1, (self.hq, self.dim))
+        plan = (e.diff_plan if self.paired else e.attn_plan)(kv, self.tables(), self.dev(self.q_off), T, self.hq,
+                                                            groups=self.dev(self.groups) if groups else None)
+        wide = torch.full((self.hkv, self.rows + 5), 7.0, device="cuda")
+        w = wide[:, :self.rows]
+        prev = None
+        if self.mode == "fork":
+            prev = (self.prev.cuda(), self.dev(self.prev_off), self.dev(self.src), self.dev(self.keep))
+        elif self.mode == "same":
+            prev = self.prev.cuda()
+            if inplace:
+                w.copy_(prev)
+                prev = w
+        e.attn_weights(plan, self.layer, q, self.scale(), lse.cuda(), w, last=self.last, prev=prev, decay=self.decay)
+        e.sync()
+        assert bool((wide[:, self.rows:] == 7).all())
+        return w.cpu()
+
+    def check(self, **kw):
+        lse = self.far()
+        w = self.run(lse, **kw)
+        ref, tol, written = self.reference(lse)
+        err = (w.double() - ref).abs()
+        bad = ~(err <= tol) & written
+        assert not bool(bad.any()), (int(bad.sum()), float((err / tol).nan_to_num(1e9)[:, written].max()))
+        left = self.prev[:, ~written] if kw.get("inplace") else 7
+        assert bool((w[:, ~written] == left).all())
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("dim", [64, 128, 256])
+@pytest.mark.parametrize("heads", [(4, 4), (8, 1), (14, 2), (33, 3)])
+def test_single_tokens(dtype, dim, heads):
+    _say("decode", dtype, dim, heads)
+    Collected(16, DECODE, heads=heads, dim=dim, dtype=dtype, seed=dim + heads[0]).check()
+
+
+@pytest.mark.parametrize("block", [4, 8, 16, 32, 64])
+@pytest.mark.parametrize("prev", ["fork", "same", None])
+def test_page_sizes(block, prev):
+    _say("block", block, prev)
+    b = Collected(block, [(1, 1), (3, 200), (40, 77), (1, 333), (0, 50), (90, 90), (7, 130)], prev=prev, seed=block)
+    b.check()
+    if prev == "same":
+        b.check(inplace=True)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("dim", [64, 128, 256])
+@pytest.mark.parametrize("last", [0, 1, 40])
+def test_prompts(dtype, dim, last):
+    _say("prompts", dtype, dim, last)
+    Collected(16, [(33, 33), (1, 1), (128, 300), (64, 64), (65, 129), (200, 200), (17, 500)], dim=dim, dtype=dtype,
+              last=last, seed=3).check()
+
+
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("heads", [(4, 4), (12, 2), (16, 4)])
+def test_pairs(dim, heads):
+    """After differential attention: each head of a pair has its own map's weights."""
+    _say("pairs", dim, heads)
+    Collected(16, [(1, 100), (50, 90), (3, 700), (1, 1)], heads=heads, dim=dim, paired=True, seed=dim).check()
+    Collected(32, [(1, 10, 0), (1, 45, 0), (2, 33, 0), (30, 40, 0)], prefixes=(256,), heads=heads, dim=dim, paired=True,
+              seed=dim + 1).check()
+
+
+@pytest.mark.parametrize("dim", [64, 128, 256])
+def test_shared_prefixes(dim):
+    """Runs that share, alone and not; one of them continues without new tokens."""
+    seqs = [(1, 1, 0), (1, 40, 0), (1, 17, 0), (3, 30, 1), (1, 1, 2), (1, 5, 2), (5, 5, 2), (0, 90, 2), (1, 2, 2),
+            (1, 1, 2), (2, 33, 2), (40, 50, 3), (60, 60, 3)]
+    b = Collected(16, seqs, prefixes=(256, 128, 640, 320), dim=dim, seed=5)
+    _say("shared", dim)
+    b.check()
+    b.check(groups=False)
+
+
+def test_many_sequences_share():
+    _say("many")
+    Collected(32, [(1, 1 + i % 70, 0) for i in range(45)] + [(1, 9, 1)], prefixes=(352, 160), heads=(14, 2), dim=64,
+              dtype="f16", seed=6).check()
+    r = np.random.default_rng(1)
+    run = np.sort(np.concatenate([np.arange(90), r.integers(0, 90, size=210)]))
+    Collected(8, [(int(r.integers(0, 3)), int(r.integers(2, 40)), int(g)) for g in run],
+              prefixes=[int(8 * r.integers(0, 30)) for _ in range(90)], heads=(2, 1), dim=64, seed=2).check()
+
+
+def test_long_rows():
+    _say("long")
+    Collected(16, [(1, 9000), (1, 4097), (3, 6001)], heads=(4, 2), dim=64, seed=11).check()
+    Collected(64, [(2, 12000)], heads=(4, 1), dim=128, seed=12).check()
+    Collected(16, [(900, 1300), (1000, 1000)], heads=(4, 1), dim=64, seed=13).check()
+
+
+def test_idle_places_and_empty_rows():
+    """Length 0 with a new token, no new token, fewer keys than new tokens."""
+    seqs = [(1, 0), (1, 40), (5, 3), (0, 20), (3, 0), (70, 30), (1, 1), (0, 0), (1, 200)]
+    _say("idle")
+    for prev in ("fork", "same", None):
+        Collected(16, seqs, prev=prev, seed=8).check()
+    b = Collected(16, [(1, 60, 0), (1, 20, 0), (0, 5, 0), (1, 30, 0), (2, 9, 0)], prefixes=(192,), prev="same", seed=9)
+    b.len[0] = 0  # the run's first: its pages are still the run's
+    b.check()
+    b.len[3] = 1  # shorter than the prefix
+    b.check()
+
+
+@pytest.mark.parametrize("what", [float("inf"), float("nan")])
+def test_unseen_places_have_no_part(what):
+    """Keys behind a sequence's end and of later tokens, whatever they hold; a key that is NaN spoils its own place
+    only."""
+    b = Collected(16, [(1, 50), (40, 90), (33, 40)], seed=4)
+    lse = b.far()
+    ref, tol, written = b.reference(lse)
+    seen = written.clone()
+    for s in range(3):
+        t = int(b.len[s]) - 1
+        b.k[:, int(b.page[b.off[s] + t // 16]), :, t % 16] = what
+        seen[int(b.off[s]) * 16 + t] = False
+    w = b.run(lse)
+    assert bool(((w.double() - ref).abs() <= tol)[:, seen].all())
+
+
+def test_same_bits():
+    """Results do not go by who comes first, with and without runs the same to rounding; a layer that is not the first, rows
+    of q with room between them."""
+    b = Collected(16, [(1 + 40 * (i % 3), 300 + 31 * i, 0) for i in range(24)], prefixes=(512,), layers=2, layer=1, pad_q=24,
+                  seed=3)
+    b.check()
+    lse = b.far()
+    first = b.run(lse)
+    for _ in range(3):
+        assert torch.equal(b.run(lse), first)
+
+
+def test_in_a_graph():
+    """Attention and the collecting of weights, captured and replayed, in place: a replay adds what an eager call adds."""
+    pk, _ = engine(16)
+    st = torch.cuda.Stream()
+    e = pk.DualMap(dict(block=16, key_blocks=1, seeds=(1, 2), vnodes=1, max_slots=1, index_log2_slots=4), stream=st)
+    b = Collected(16, [(1, 30, 0), (1, 50, 0), (2, 9, 0), (40, 60, 0), (1, 200, 1)], prefixes=(256, 320), prev="same", seed=30)
+    kv, t, q_off, grp = pk.KVPages(b.k.cuda(), b.v.cuda()), b.tables(), b.dev(b.q_off), b.dev(b.groups)
+    q = b.qrows.cuda().unflatten(1, (8, 128)).contiguous()
+    T = len(q)
+    out, lse = torch.zeros_like(q), torch.zeros((T, 8), device="cuda")
+    w = torch.zeros((2, b.rows), device="cuda")
+
+    def call():
+        plan = e.attn_plan(kv, t, q_off, T, 8, groups=grp)
+        e.attn(plan, 0, q, b.scale(), out, lse)
+        e.attn_weights(plan, 0, q, b.scale(), lse, w, prev=w, decay=0.5)
+
+    torch.cuda.synchronize()
+    with torch.cuda.stream(st):
+        call()
+    st.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=st):
+        call()
+    g = torch.Generator(device="cuda").manual_seed(1)
+    for _ in range(4):
+        q.normal_(generator=g)
+        start = torch.rand(w.shape, generator=g, device="cuda")
+        w.copy_(start)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        got = w.clone()
+        w.copy_(start)
+        torch.cuda.synchronize()
+        with torch.cuda.stream(st):
+            call()
+        st.synchronize()
+        assert torch.equal(got, w) and not torch.equal(got, start)
+        b.prev, b.decay, b.qrows = start.cpu(), 0.5, q.cpu().flatten(1)
+        ref, tol, written = b.reference(lse.cpu())
+        assert bool(((got.cpu().double() - ref).abs() <= tol)[:, written].all())
+    e.sync()
+    e.close()
+
+
+def test_refusals():
+    pk, e = engine(16)
+    b = Collected(16, [(1, 40), (2, 90)], seed=1)
+    kv = pk.KVPages(b.k.cuda(), b.v.cuda())
+    q = b.qrows.cuda().unflatten(1, (8, 128)).contiguous()
+    t, q_off, lse = b.tables(), b.dev(b.q_off), b.far().cuda()
+    w = torch.full((2, b.rows), 7.0, device="cuda")
+    plan = e.attn_plan(kv, t, q_off, 3, 8)
+    src, keep, off = b.dev(b.src), b.dev(b.keep), b.dev(b.prev_off)
+    old = b.prev.cuda()
+    for bad in (w[:1], w[:, :-1], w.double(), w.cpu(), w.t(), None):
+        with pytest.raises(ValueError, match="w "):
+            e.attn_weights(plan, 0, q, 0.1, lse, bad)
+    for bad in (lse[:2], None):
+        with pytest.raises(ValueError, match="lse"):
+            e.attn_weights(plan, 0, q, 0.1, bad, w)
+    with pytest.raises(ValueError, match="prev"):
+        e.attn_weights(plan, 0, q, 0.1, lse, w, prev=w[:, :-1])
+    with pytest.raises(ValueError, match="src and keep"):
+        e.attn_weights(plan, 0, q, 0.1, lse, w, prev=(old, off, src[:1], keep))
+    for kw in (dict(scale=0.0), dict(scale=math.nan), dict(decay=math.inf), dict(decay=math.nan)):
+        kw = dict(dict(scale=0.1), **kw)
+        with pytest.raises(pk.DMError, match="scale must be"):
+            e.attn_weights(plan, 0, q, kw.pop("scale"), lse, w, **kw)
+    with pytest.raises(pk.DMError, match="layer"):
+        e.attn_weights(plan, 1, q, 0.1, lse, w)
+    assert bool((w == 7).all())
+    # found on the device: sources out of range carry nothing
+    for bad in (torch.tensor([5, 0], dtype=torch.int32, device="cuda"), torch.tensor([-1, 0], dtype=torch.int32, device="cuda")):
+        e.attn_weights(plan, 0, q, b.scale(), lse, w, prev=(old, off, bad, keep))
+        with pytest.raises(pk.DMError):
+            e.sync()
+    # another batch's plan: reported, nothing written
+    w.fill_(7)
+    other = e.attn_plan(kv, (t[0][:2], t[1], t[2][:1]), q_off[:2], 3, 8)
+    other.batch, other.n = plan.batch, plan.n
+    e.attn_weights(other, 0, q, 0.1, lse, w)
+    with pytest.raises(pk.DMError):
+        e.sync()
+    assert bool((w == 7).all())
