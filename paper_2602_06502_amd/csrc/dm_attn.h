@@ -9,7 +9,7 @@ namespace dm {
 namespace {
 
 constexpr int kThreads = 256, kWaves = 4;
-constexpr uint32_t kNarrow = 16, kWide = 128;  // rows of a tile
+constexpr uint32_t kNarrow = 16, kWide = kAttnWide;  // rows of a tile
 // Rows of a unit, at most, that has narrow tiles.  (32 sequences of 4,096 keys, 32
 // query and 8 key heads of 128: 24 rows 104 us in a wide tile, 114 in two narrow
 // ones; 64 rows 112 and 158; 16 rows 103 and 106, 4 rows 100 and 102.  64 sequences of
@@ -31,7 +31,8 @@ struct PlanHead {
     uint32_t part_rows;   // rows of parts
     uint32_t most_parts;  // of a row
     uint32_t head_dim;
-    uint32_t pad[4];
+    uint32_t wide;  // rows of its wide tiles
+    uint32_t pad[3];
 };
 struct Unit {
     uint32_t item0;       // items before this unit
@@ -215,6 +216,12 @@ __device__ __forceinline__ bool scores_are_far(float m, float scale2)
     return __any(m != -INFINITY && !(fabsf(m * scale2) < 0x1p20f));
 }
 
+// Byte address of a place in LDS.
+__device__ __forceinline__ uint32_t lds_address(const uint16_t* p)
+{
+    return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const uint16_t*)p;
+}
+
 // A tile of 32 keys for a wave's 32 rows: s holds S^T (key = (i / 4) * 8 + half
 // * 4 + i % 4).  map: of a pair.
 template <typename T, int D, bool PAIR = false>
@@ -233,6 +240,42 @@ __device__ __forceinline__ v16f scores(const uint16_t* kt,
     return s;
 }
 
+// The same from one register of addresses: a row's chunks are x * 2 + half, exchanged by its
+// low bits, so chunk x is chunk 0's place with 32 x exchanged in (tiles begin at multiples of
+// 512 bytes).  at: of the lane's row and chunk 0 of its map, in bytes.
+template <int D, bool PAIR>
+__device__ __forceinline__ uint32_t score_place(uint32_t map)
+{
+    const uint32_t row = lane_id() % 32, half = lane_id() / 32;
+    return (row * D + (((PAIR ? map * (D / 16) : 0) + half) ^ k_swizzle<D>(row)) * 8) * 2;
+}
+// The scores of 64 keys so, a few reads ahead of the matrix instructions (left to itself the
+// compiler, short of registers, waits for every read where it is used).
+constexpr int kAhead = 2;
+template <typename T, int D, bool PAIR>
+__device__ __forceinline__ void scores_ahead(uint32_t at, const typename Vec8<T>::type (&q)[kKeyElems<D, PAIR> / 16],
+                                             v16f (&s)[2])
+{
+    using V = typename Vec8<T>::type;
+    constexpr int kSteps = kKeyElems<D, PAIR> / 8;
+    V f[kAhead + 1];
+    auto read = [&](int n) {
+        f[n % (kAhead + 1)] = *(const __attribute__((address_space(3))) V*)(uintptr_t)(
+            (at ^ (n / 2 * 32)) + n % 2 * (32 * D * 2));
+    };
+    s[0] = s[1] = v16f{};
+#pragma unroll
+    for (int n = 0; n < kAhead; n++)
+        read(n);
+#pragma unroll
+    for (int n = 0; n < kSteps; n++) {
+        if (n + kAhead < kSteps)
+            read(n + kAhead);
+        s[n % 2] = mfma(f[n % (kAhead + 1)], q[n / 2], s[n % 2]);
+        __builtin_amdgcn_sched_barrier(0);
+    }
+}
+
 // V^T of 16 keys (rows key0 ..) and 32 d (from db * 32 on), keys in the order
 // of the lane's weights.
 template <typename T, int D>
@@ -248,6 +291,24 @@ __device__ __forceinline__ typename Vec8<T>::type values(const uint16_t* vt, uin
     typedef short v8s __attribute__((ext_vector_type(8)));
     const v8s z = __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7);
     return __builtin_bit_cast(typename Vec8<T>::type, z);
+}
+
+// The same from one register of addresses (as score_place): block db's place is block 0's with
+// 64 db exchanged in.
+template <int D>
+__device__ __forceinline__ uint32_t value_place()
+{
+    const uint32_t l = lane_id(), row = l / 32 * 4 + l % 16 / 4, c = l / 16 % 2 * 2 + l % 4 / 2;
+    return (row * D + (c ^ v_swizzle<D>(row)) * 8 + l % 2 * 4) * 2;
+}
+template <typename T, int D>
+__device__ __forceinline__ typename Vec8<T>::type values_at(uint32_t at, uint32_t key0, uint32_t db)
+{
+    const uint32_t here = (at ^ (db * 64)) + key0 * D * 2;
+    const v4s x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s*)(uintptr_t)here);
+    const v4s y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s*)(uintptr_t)(here + 8 * D * 2));
+    typedef short v8s __attribute__((ext_vector_type(8)));
+    return __builtin_bit_cast(typename Vec8<T>::type, __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7));
 }
 
 // Is any of eight 16-bit values infinite or NaN?
@@ -273,14 +334,12 @@ __device__ __forceinline__ float halves_max(float x)
     return fmaxf(x, y);
 }
 
-// The running softmax of NB tiles of 32 keys: the tiles' weights in T.  limit:
-// the keys that the lane's row sees (absolute), key0: the tiles' first; masked:
-// some row does not see all of them; beside(): what can be done meanwhile, when
-// s has been read (it may be written anew).
-template <typename T, int D, int NB, typename Beside>
-__device__ __forceinline__ void weights(Row<D>& r, v16f (&s)[NB], typename Vec8<T>::type (&p)[NB][2],
-                                        uint32_t key0, uint32_t limit, bool masked, float scale2,
-                                        Beside&& beside)
+// The running maximum over NB tiles of 32 keys, in front of their weights: what is
+// taken off their scaled scores.  limit: the keys that the lane's row sees (absolute),
+// key0: the tiles' first; masked: some row does not see all of them.
+template <typename T, int D, int NB>
+__device__ __forceinline__ float settle(Row<D>& r, v16f (&s)[NB], uint32_t key0, uint32_t limit, bool masked,
+                                        float scale2)
 {
     const uint32_t half = lane_id() / 32;
     if (masked) {
@@ -326,7 +385,17 @@ __device__ __forceinline__ void weights(Row<D>& r, v16f (&s)[NB], typename Vec8<
             for (int i = 0; i < 16; i++)
                 s[b][i] -= m;
     }
-    const float base = r.m == -INFINITY ? 0.0f : r.m * (r.far ? 0.0f : scale2) - kRaise<T>;
+    return r.m == -INFINITY ? 0.0f : r.m * (r.far ? 0.0f : scale2) - kRaise<T>;
+}
+
+// The running softmax of NB tiles of 32 keys: the tiles' weights in T.  beside(): what
+// can be done meanwhile, when s has been read (it may be written anew).
+template <typename T, int D, int NB, typename Beside>
+__device__ __forceinline__ void weights(Row<D>& r, v16f (&s)[NB], typename Vec8<T>::type (&p)[NB][2],
+                                        uint32_t key0, uint32_t limit, bool masked, float scale2,
+                                        Beside&& beside)
+{
+    const float base = settle<T, D, NB>(r, s, key0, limit, masked, scale2);
     const v16f now[NB] = {s[0], s[NB - 1]};
     beside();
     float sum = 0;
@@ -353,6 +422,51 @@ __device__ __forceinline__ void add_values(Row<D>& r, const typename Vec8<T>::ty
 #pragma unroll
             for (int d = 0; d < D / 32; d++)
                 r.o[d] = mfma(values<T, D>(vt, b * 32 + t * 16, d), p[b][t], r.o[d]);
+}
+
+// Both for two tiles, the second one's weights taken beside the first one's products, a few
+// reads ahead of these.
+template <typename T, int D>
+__device__ __forceinline__ void weigh_and_add(Row<D>& r, v16f (&s)[2], uint32_t vt, uint32_t key0,
+                                              uint32_t limit, bool masked, float scale2)
+{
+    using V = typename Vec8<T>::type;
+    constexpr int kBlocks = D / 32, kSteps = 4 * kBlocks;
+    const float base = settle<T, D, 2>(r, s, key0, limit, masked, scale2);
+    V p[2][2], f[kAhead + 2];
+    float sum = 0;
+    auto weigh = [&](int b, int i) {
+        const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(s[b][i], scale2, -base));
+        sum += w;
+        p[b][i / 8][i % 8] = (T)w;
+    };
+    auto read = [&](int n) {
+        f[n % (kAhead + 2)] = values_at<T, D>(vt, n / kBlocks * 16, n % kBlocks);
+    };
+#pragma unroll
+    for (int n = 0; n < kAhead; n++)
+        read(n);
+#pragma unroll
+    for (int i = 0; i < 16; i++)
+        weigh(0, i);
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int n = 0; n < kSteps; n += 2) {
+#pragma unroll
+        for (int k = n; k < n + 2; k++) {
+            if (k + kAhead < kSteps)
+                read(k + kAhead);
+            r.o[k % kBlocks] = mfma(f[k % (kAhead + 2)], p[k / kBlocks / 2][k / kBlocks % 2], r.o[k % kBlocks]);
+        }
+        if (n < kSteps / 2) {
+            constexpr int kPer = 64 / kSteps;  // two steps' share of 16
+#pragma unroll
+            for (int i = 0; i < kPer; i++)
+                weigh(1, n / 2 * kPer + i);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+    }
+    r.l += sum;
 }
 
 // The same for values among which are infinities or NaN that some row does not
@@ -468,9 +582,10 @@ __device__ __forceinline__ bool plan_of(const PlanHead& h, const TokenBatch& b, 
 // Is the plan this call's, of at most `items` items?  (A batch whose q_off is out of
 // order can have more than the call has workgroups.)
 __device__ __forceinline__ bool plan_fits(const PlanHead& h, const AttnIn& a, uint64_t part_rows,
-                                          uint32_t head_dim, uint32_t items)
+                                          uint32_t head_dim, uint32_t wide, uint32_t items)
 {
-    return plan_of(h, a.b, a.q_heads, a.kv_heads, head_dim) && h.part_rows <= part_rows && h.items <= items;
+    return plan_of(h, a.b, a.q_heads, a.kv_heads, head_dim) && h.wide == wide && h.part_rows <= part_rows &&
+           h.items <= items;
 }
 
 // The unit of this workgroup's item; false: none, or the plan is another batch's
@@ -478,12 +593,13 @@ __device__ __forceinline__ bool plan_fits(const PlanHead& h, const AttnIn& a, ui
 // reaches, and beyond that only once the head has been looked at: the plan of a
 // batch of fewer sequences is a smaller one.
 __device__ __forceinline__ bool item_unit(const AttnIn& a, const PlanView& pv, uint32_t units,
-                                          uint64_t part_rows, uint32_t head_dim, uint32_t* status, Unit& u)
+                                          uint64_t part_rows, uint32_t head_dim, uint32_t wide, uint32_t* status,
+                                          Unit& u)
 {
     const PlanHead& ph = *pv.head;
     const bool early = units <= kEarlyUnits;
     uint32_t ui = early ? find_unit(pv.item0, units, blockIdx.x) : 0;
-    if (!plan_fits(ph, a, part_rows, head_dim, gridDim.x)) {
+    if (!plan_fits(ph, a, part_rows, head_dim, wide, gridDim.x)) {
         if (blockIdx.x == 0 && threadIdx.x == 0)
             atomicOr(status, kErrInval);
         return false;
@@ -642,6 +758,40 @@ struct Share {
             }
         }
     }
+    // keys or values alone, by way of k
+    __device__ __forceinline__ void fetch_one(const uint16_t* pages, uint32_t key, bool& bad)
+    {
+        static_assert(kGroups == 1, "a load's rows are in one page");
+        const uint32_t mask = (1u << shift) - 1;
+#pragma unroll
+        for (int i = 0; i < kLoads; i++) {
+            const uint32_t p = page[i];
+            bad |= p >= n_pages;
+            const uint64_t at = (p < n_pages ? p : 0) * page_size + head_at + ((key + i * kStep) & mask) * kElems;
+            k[i] = *reinterpret_cast<const v4u32*>(pages + at + lane_at);
+        }
+    }
+    template <bool VALUES>
+    __device__ __forceinline__ bool stage_one(uint16_t* to, uint32_t key, bool ask)
+    {
+        bool odd = false;
+        if (VALUES && ask) {
+            const uint32_t have = key1 - key;
+#pragma unroll
+            for (int i = 0; i < kLoads; i++) {
+                if (r0 + i * kStep >= have)
+                    k[i] = v4u32{};
+                odd |= not_finite<T>(k[i]);
+            }
+        }
+        const uint32_t row = here();
+#pragma unroll
+        for (int i = 0; i < kLoads; i++) {
+            const uint32_t r = row + i * kStep;
+            *reinterpret_cast<v4u32*>(to + r * D + (ch ^ (VALUES ? v_swizzle<D, false>(r) : k_swizzle<D>(r))) * 8) = k[i];
+        }
+        return odd;
+    }
     // into LDS; true: values that are not finite among them (asked for where some
     // row does not see all of the tile)
     __device__ __forceinline__ bool stage(uint16_t* kt, uint16_t* vt, uint32_t key, bool ask)
@@ -727,7 +877,9 @@ __device__ __forceinline__ void write_four(const AttnIn& a, const Tile& t, uint3
 // 16) * 4 + i, and of O^T the elements d = block * 16 + (lane / 16) * 4 + i.  PAIR: the
 // rows of a tile are of both maps in turn, so each takes the products with both maps'
 // keys and keeps its own: no more instructions than one product over D.
-template <typename T, int D, int WAVES, bool PAIR = false>
+// SPLIT: a wave's part of LDS holds a tile's keys, then its values, each on its way while
+// the other is worked on: half the LDS and half the registers a wave, for twice the waves.
+template <typename T, int D, int WAVES, bool PAIR = false, bool SPLIT = false>
 __device__ __forceinline__ void narrow_tile(const InOf<PAIR>& a, const Tile& t, uint16_t* lds, Joined<WAVES>& joined,
                                             bool& bad)
 {
@@ -753,18 +905,27 @@ __device__ __forceinline__ void narrow_tile(const InOf<PAIR>& a, const Tile& t, 
 #pragma unroll
     for (int d = 0; d < kBlocks; d++)
         o[d] = v4f{};
-    uint16_t* kt = lds + wave * 2 * kNarrowKeys * D;
-    uint16_t* vt = kt + kNarrowKeys * D;
+    uint16_t* kt = lds + wave * (SPLIT ? 1 : 2) * kNarrowKeys * D;
+    uint16_t* vt = SPLIT ? kt : kt + kNarrowKeys * D;
     // weights, and what their rounding has left out: the matrix unit has time for both
     // (4% busy with the weights alone, in 64 rows on up to 8,192 keys)
     V p, rest;
+    // a lane's number: SPLIT works places in LDS out anew for each tile, of which it has no
+    // registers to keep (kept, 15 of them were spilled, and their reloads waited for the
+    // pages: 297 us instead of 225 for 64 rows on up to 8,192 keys, heads of 128)
+    auto here = [](uint32_t x) {
+        if (SPLIT)
+            asm volatile("" : "+v"(x));
+        return x;
+    };
     // scores and weights of the tile in LDS
     auto weigh = [&](uint32_t key, bool masked) {
         v4f s[2];
+        const uint32_t at16 = here(row16);
 #pragma unroll
         for (int h = 0; h < 2; h++) {
             s[h] = v4f{};
-            const uint32_t r = h * 16 + row16;
+            const uint32_t r = h * 16 + at16;
 #pragma unroll
             for (int k = 0; k < kElems / 32; k++)
                 s[h] = mfma(*reinterpret_cast<const V*>(kt + r * D + ((k * 4 + g) ^ k_swizzle<D>(r)) * 8), q[k],
@@ -836,24 +997,12 @@ __device__ __forceinline__ void narrow_tile(const InOf<PAIR>& a, const Tile& t, 
             __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
             __builtin_amdgcn_wave_barrier();
         };
-        x.find(key);
-        x.fetch(a, key, bad);
-        if (key + kTurn < t.key1)
-            x.find(key + kTurn);
-        for (; key < t.key1; key += kTurn) {
-            stage(key);
-            if (masked && __any(odd))
-                break;
-            if (key + kTurn < t.key1)
-                x.fetch(a, key + kTurn, bad);
-            if (key + 2 * kTurn < t.key1)
-                x.find(key + 2 * kTurn);
-            weigh(key, masked);
-            // O^T += V^T P^T, keys in the order of the lane's weights
-            const uint32_t r = g * 4 + row16 / 4;
+        // O^T += V^T P^T, keys in the order of the lane's weights
+        auto add = [&] {
+            const uint32_t own = here(lane), r = own / 16 * 4 + own % 16 / 4;
 #pragma unroll
             for (int d = 0; d < kBlocks; d++) {
-                const uint32_t c = d * 2 + (lane % 4) / 2, e = (lane % 2) * 4;
+                const uint32_t c = d * 2 + (own % 4) / 2, e = (own % 2) * 4;
                 const v4s v0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
                     (lds_v4s*)(vt + r * D + (c ^ v_swizzle<D, false>(r)) * 8 + e));
                 const v4s v1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
@@ -863,10 +1012,9 @@ __device__ __forceinline__ void narrow_tile(const InOf<PAIR>& a, const Tile& t, 
                 o[d] = mfma(__builtin_bit_cast(V, f), p, o[d]);
                 o[d] = mfma(__builtin_bit_cast(V, f), rest, o[d]);
             }
-        }
-        while (key < t.key1) {
-            // as add_odd_values()
-            weigh(key, true);
+        };
+        // as add_odd_values()
+        auto add_odd = [&](uint32_t key) {
 #pragma unroll 1
             for (uint32_t k = 0; k < kNarrowKeys; k++) {
                 float w = 0;
@@ -887,11 +1035,57 @@ __device__ __forceinline__ void narrow_tile(const InOf<PAIR>& a, const Tile& t, 
                             o[d][i] = __builtin_fmaf(w, (float)x[i], o[d][i]);
                 }
             }
-            key += kTurn;
-            if (key < t.key1) {
-                x.find(key);
-                x.fetch(a, key, bad);
+        };
+        x.find(key);
+        if constexpr (SPLIT) {
+            auto in_order = [] {
+                __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+                __builtin_amdgcn_wave_barrier();
+            };
+            x.fetch_one(a.k, key, bad);
+            for (; key < t.key1; key += kTurn) {
+                const bool all = key + kNarrowKeys <= t.see_first && key + kNarrowKeys <= t.key1;
+                in_order();
+                x.template stage_one<false>(kt, key, false);
+                in_order();
+                x.fetch_one(a.v, key, bad);
+                if (key + kTurn < t.key1)
+                    x.find(key + kTurn);
+                weigh(key, !all);
+                in_order();
+                const bool strange = x.template stage_one<true>(vt, key, !all);
+                in_order();
+                if (key + kTurn < t.key1)
+                    x.fetch_one(a.k, key + kTurn, bad);
+                if (!all && __any(strange))
+                    add_odd(key);
+                else
+                    add();
+            }
+        } else {
+            x.fetch(a, key, bad);
+            if (key + kTurn < t.key1)
+                x.find(key + kTurn);
+            for (; key < t.key1; key += kTurn) {
                 stage(key);
+                if (masked && __any(odd))
+                    break;
+                if (key + kTurn < t.key1)
+                    x.fetch(a, key + kTurn, bad);
+                if (key + 2 * kTurn < t.key1)
+                    x.find(key + 2 * kTurn);
+                weigh(key, masked);
+                add();
+            }
+            while (key < t.key1) {
+                weigh(key, true);
+                add_odd(key);
+                key += kTurn;
+                if (key < t.key1) {
+                    x.find(key);
+                    x.fetch(a, key, bad);
+                    stage(key);
+                }
             }
         }
     }
@@ -1004,17 +1198,12 @@ __device__ __forceinline__ void send16(const uint16_t* from, uint32_t lane_at, u
 }
 __device__ __forceinline__ void wait_sent() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
 
-// Byte address of a place in LDS.
-__device__ __forceinline__ uint32_t lds_address(const uint16_t* p)
-{
-    return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const uint16_t*)p;
-}
-
 // A thread's share of wide tiles: LDS chunk threadIdx.x + i * 256, that is row r0 +
 // i * kStep, place `ch` of the row.  What a lane adds to its rows' address does not
 // change from tile to tile.
-template <typename T, int D, bool PAIR = false>
+template <typename T, int D, bool PAIR = false, int WAVES = kWaves>
 struct Sender {
+    static constexpr int kThreads = WAVES * kWave;
     static constexpr int kElems = kKeyElems<D, PAIR>;
     static constexpr int kLoads = kWideKeys * D / 8 / kThreads;
     static constexpr uint32_t kRowChunks = D / 8, kStep = kThreads / kRowChunks;
@@ -1090,7 +1279,9 @@ struct Sender {
 // were.
 // PAIR: a wave's rows are of one map, two waves take the maps of the same 32 pairs of
 // rows; each has products with its own map's keys only, both with all values.
-template <typename T, int D, bool PAIR = false>
+// BESIDE: the next tile's scores are taken beside this one's weights.  Without, a wave
+// has registers to spare, and another wave of its SIMD the matrix unit meanwhile.
+template <typename T, int D, bool PAIR = false, int WAVES = kWaves, bool BESIDE = true>
 __device__ __forceinline__ void wide_tile(const InOf<PAIR>& a, const Tile& t, uint16_t* lds, uint32_t* odd_tile,
                                           bool& bad)
 {
@@ -1113,8 +1304,10 @@ __device__ __forceinline__ void wide_tile(const InOf<PAIR>& a, const Tile& t, ui
     constexpr uint32_t kTile = kWideKeys * D;
     uint16_t* vts = lds + 2 * kTile;  // two tiles of keys, then two of values
     if (t.key0 < t.key1) {
-        const Sender<T, D, PAIR> x(a, t, wave);
-        uint32_t p1[Sender<T, D, PAIR>::kPages], p2[Sender<T, D, PAIR>::kPages];  // pages of the next tile, and the one after
+        using Send = Sender<T, D, PAIR, WAVES>;
+        const Send x(a, t, wave);
+        const uint32_t place = score_place<D, PAIR>(map), v_place = value_place<D>();
+        uint32_t p1[Send::kPages], p2[Send::kPages];  // pages of the next tile, and the one after
         if (threadIdx.x == 0)
             *odd_tile = 0;
         x.find(t.key0, p2);
@@ -1122,14 +1315,25 @@ __device__ __forceinline__ void wide_tile(const InOf<PAIR>& a, const Tile& t, ui
         x.send(x.v, true, t.key0, p2, vts, bad);
         if (t.key0 + kWideKeys < t.key1) {
             x.find(t.key0 + kWideKeys, p1);
-            x.send(x.k, false, t.key0 + kWideKeys, p1, lds + kTile, bad);
+            if (BESIDE)
+                x.send(x.k, false, t.key0 + kWideKeys, p1, lds + kTile, bad);
         }
-        if (t.key0 + 2 * kWideKeys < t.key1)
+        if (BESIDE && t.key0 + 2 * kWideKeys < t.key1)
             x.find(t.key0 + 2 * kWideKeys, p2);
         wait_sent();
         __syncthreads();
-        v16f s[2] = {scores<T, D, PAIR>(lds, q, map), scores<T, D, PAIR>(lds + 32 * D, q, map)};
-        __syncthreads();  // the third tile's keys go where the first's are
+        v16f s[2];
+        if (BESIDE) {
+            s[0] = scores<T, D, PAIR>(lds, q, map);
+            s[1] = scores<T, D, PAIR>(lds + 32 * D, q, map);
+            __syncthreads();  // the third tile's keys go where the first's are
+        } else {
+            // the query is here: the compiler, which does not count the sends, would wait for
+            // its reads in every tile and so for the sends
+#pragma unroll
+            for (int i = 0; i < kKeyElems<D, PAIR> / 16; i++)
+                asm volatile("" : "+v"(q[i]));
+        }
         uint32_t key = t.key0, buf = 0;
         bool odd = false;
         while (true) {
@@ -1144,12 +1348,33 @@ __device__ __forceinline__ void wide_tile(const InOf<PAIR>& a, const Tile& t, ui
                     break;
             }
             const uint32_t key1 = key + kWideKeys, key2 = key1 + kWideKeys;
+            if constexpr (!BESIDE) {
+                if (key1 < t.key1) {
+                    x.send(x.k, false, key1, p1, lds + (buf ^ 1) * kTile, bad);
+                    x.send(x.v, true, key1, p1, vts + (buf ^ 1) * kTile, bad);
+                }
+                if (key2 < t.key1)
+                    x.find(key2, p1);
+                if (key < wave_last) {
+                    const uint32_t at = lds_address(lds + buf * kTile) + place;
+                    v16f z[2];
+                    scores_ahead<T, D, PAIR>(at, q, z);
+                    weigh_and_add<T, D>(r, z, lds_address(vts + buf * kTile) + v_place, key, end, masked(key, wave_first), a.scale2);
+                }
+                key = key1;
+                buf ^= 1;
+                if (key >= t.key1)
+                    break;
+                wait_sent();
+                __syncthreads();
+                continue;
+            }
             if (key2 < t.key1)
                 x.send(x.k, false, key2, p2, lds + buf * kTile, bad);
             if (key1 < t.key1) {
                 x.send(x.v, true, key1, p1, vts + (buf ^ 1) * kTile, bad);
 #pragma unroll
-                for (int i = 0; i < Sender<T, D, PAIR>::kPages; i++)
+                for (int i = 0; i < Send::kPages; i++)
                     p1[i] = p2[i];
             }
             if (key2 + kWideKeys < t.key1)
@@ -1169,7 +1394,13 @@ __device__ __forceinline__ void wide_tile(const InOf<PAIR>& a, const Tile& t, ui
             wait_sent();
             __syncthreads();
         }
-        while (key < t.key1) {  // rare: values that are not finite
+        while ((BESIDE || odd) && key < t.key1) {  // rare: values that are not finite
+            if (!BESIDE) {  // (its own query, so that nothing is kept for this)
+                typename Vec8<T>::type own[kKeyElems<D, PAIR> / 16];
+                load_query<T, D, PAIR>(a, t, row, own);
+                s[0] = scores<T, D, PAIR>(lds + buf * kTile, own, map);
+                s[1] = scores<T, D, PAIR>(lds + buf * kTile + 32 * D, own, map);
+            }
             if (key < wave_last) {
                 weights<T, D, 2>(r, s, p, key, end, true, a.scale2, [] {});
                 add_odd_values<T, D, 2>(r, p, vts + buf * kTile, key, end);
@@ -1185,8 +1416,10 @@ __device__ __forceinline__ void wide_tile(const InOf<PAIR>& a, const Tile& t, ui
             __syncthreads();
             x.clean(vts + buf * kTile, key);
             __syncthreads();
-            s[0] = scores<T, D, PAIR>(lds + buf * kTile, q, map);
-            s[1] = scores<T, D, PAIR>(lds + buf * kTile + 32 * D, q, map);
+            if (BESIDE) {
+                s[0] = scores<T, D, PAIR>(lds + buf * kTile, q, map);
+                s[1] = scores<T, D, PAIR>(lds + buf * kTile + 32 * D, q, map);
+            }
         }
     }
     const float l = r.l + __shfl_xor(r.l, 32);
@@ -1397,10 +1630,10 @@ inline uint64_t item_target(const dm_ctx* c) { return 3ull * c->n_cu; }
 // Items that a plan can have: the tiles of its units, and what cuts add: at most
 // the items wanted, and no more than the table entries' keys are chunks for each
 // tile.
-inline uint64_t most_items(const dm_ctx* c, const dm_token_batch& b, uint32_t ratio, uint32_t kv_heads)
+inline uint64_t most_items(const dm_ctx* c, const dm_token_batch& b, uint32_t ratio, uint32_t kv_heads, uint32_t wide)
 {
     const uint64_t rows = b.q_tokens * ratio;
-    auto tiles = [&](uint64_t units) { return rows / kWide + units; };
+    auto tiles = [&](uint64_t units) { return rows / wide + units; };
     const uint64_t uncut = tiles(b.tables.n) + (b.groups ? tiles(b.groups) : 0);
     uint64_t cuts = item_target(c);
     const uint64_t chunks = b.tables.entries * c->cfg.block_size / kChunk + 1;

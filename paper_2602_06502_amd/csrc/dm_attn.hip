@@ -40,15 +40,15 @@ constexpr int kPlanThreads = 512;
 
 // The tiles of a unit, by its rows, and their cost a key: a wide one takes up to
 // twice a narrow one's time.
-__device__ __forceinline__ uint32_t tile_rows(uint64_t rows) { return rows <= kNarrowRows ? kNarrow : kWide; }
-__device__ __forceinline__ uint32_t tile_flags(uint64_t rows) { return tile_rows(rows) == kWide ? kUnitWide : 0; }
-__device__ __forceinline__ uint64_t tiles_of(uint64_t rows)
+__device__ __forceinline__ uint32_t tile_rows(uint64_t rows, uint32_t wide) { return rows <= kNarrowRows ? kNarrow : wide; }
+__device__ __forceinline__ uint32_t tile_flags(uint64_t rows) { return rows <= kNarrowRows ? 0 : kUnitWide; }
+__device__ __forceinline__ uint64_t tiles_of(uint64_t rows, uint32_t wide)
 {
-    return (rows + tile_rows(rows) - 1) / tile_rows(rows);
+    return (rows + tile_rows(rows, wide) - 1) / tile_rows(rows, wide);
 }
-__device__ __forceinline__ uint64_t weight_of(uint64_t rows)
+__device__ __forceinline__ uint64_t weight_of(uint64_t rows, uint32_t wide)
 {
-    return tiles_of(rows) * (tile_rows(rows) == kWide ? 2 : 1);
+    return tiles_of(rows, wide) * (rows <= kNarrowRows ? 1 : wide / (kWide / 2));
 }
 
 // Are the runs' bounds in order?
@@ -73,7 +73,7 @@ __device__ __forceinline__ uint64_t block_sum64(uint64_t v, uint64_t* lds)
 
 struct PlanIn {
     TokenBatch b;
-    uint32_t q_heads, kv_heads, ratio, head_dim;
+    uint32_t q_heads, kv_heads, ratio, head_dim, wide;
     uint64_t target;     // items wanted
     uint64_t part_rows;  // rows of parts there is room for (0: no unit is cut)
     uint32_t* arrived;   // workgroups that are done with their sequences; zero between calls
@@ -198,7 +198,7 @@ __device__ __forceinline__ Unit sequence_unit(const PlanIn& a, const SeqView& v,
 __device__ __forceinline__ bool worth_sharing(const PlanIn& a, const RunView& r, uint32_t pages, uint32_t gain)
 {
     return pages != 0 && pages != kNoSay && r.ok && ((uint64_t)pages << a.b.shift) >= kChunk &&
-           2 * (uint64_t)gain >= 3 * weight_of((uint64_t)r.ntok * a.ratio);
+           2 * (uint64_t)gain >= 3 * weight_of((uint64_t)r.ntok * a.ratio, a.wide);
 }
 
 // Which runs share their prefixes, the chunk, and the units' items.  With
@@ -268,7 +268,7 @@ __global__ __launch_bounds__(kPlanThreads) void attn_plan_kernel(PlanIn a, PlanV
                 continue;
             atomicMin(&pages[g], i == tid ? limit : agent_load(&pv.limit[s]));
             if (v.len)
-                atomicAdd(&gain[g], (uint32_t)weight_of((uint64_t)v.ntok * a.ratio));
+                atomicAdd(&gain[g], (uint32_t)weight_of((uint64_t)v.ntok * a.ratio, a.wide));
         }
         settle();
         for (uint32_t g = tid; g < b.groups; g += kPlanThreads) {
@@ -285,7 +285,7 @@ __global__ __launch_bounds__(kPlanThreads) void attn_plan_kernel(PlanIn a, PlanV
     // first try have no room
     for (int attempt = 0; attempt < 2; attempt++) {
         auto cost_of = [&](const Unit& u) -> uint64_t {
-            return u.ntok ? weight_of((uint64_t)u.ntok * a.ratio) * (u.key1 - u.key0) : 0;
+            return u.ntok ? weight_of((uint64_t)u.ntok * a.ratio, a.wide) * (u.key1 - u.key0) : 0;
         };
         Unit mine{};
         uint64_t cost = 0;
@@ -328,7 +328,7 @@ __global__ __launch_bounds__(kPlanThreads) void attn_plan_kernel(PlanIn a, PlanV
                     u.chunks = 1;
                 if (u.chunks > 1)
                     u.flags |= kUnitParts;
-                it = tiles_of(r) * u.chunks * a.kv_heads;
+                it = tiles_of(r, a.wide) * u.chunks * a.kv_heads;
                 if (u.flags & kUnitParts) {
                     rw = r * u.chunks * a.kv_heads;
                     atomicMax(&most, u.chunks);
@@ -394,6 +394,7 @@ __global__ __launch_bounds__(kPlanThreads) void attn_plan_kernel(PlanIn a, PlanV
                 h.entries = b.entries;
                 h.items = (uint32_t)items;
                 h.head_dim = a.head_dim;
+                h.wide = a.wide;
                 h.part_rows = (uint32_t)rows;
                 h.most_parts = most;
                 *pv.head = h;
@@ -416,7 +417,7 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attn_kernel(AttnIn
     __shared__ uint32_t odd_tile;
     __shared__ Joined<kWaves> joined;
     Unit u;
-    if (!item_unit(a, pv, a.b.groups + a.b.n, part_rows, D, status, u))
+    if (!item_unit(a, pv, a.b.groups + a.b.n, part_rows, D, kWide, status, u))
         return;
     bool bad = false;
     const uint32_t x = blockIdx.x - u.item0;
@@ -444,7 +445,7 @@ __global__ __launch_bounds__(kSmallWaves<D>* kWave, 1) void attn_small_kernel(At
     __shared__ __attribute__((aligned(16))) uint16_t lds[kW * 2 * kNarrowKeys * D];
     __shared__ Joined<kW> joined;
     Unit u;
-    if (!item_unit(a, pv, a.b.n, 0, D, status, u))
+    if (!item_unit(a, pv, a.b.n, 0, D, kWide, status, u))
         return;
     bool bad = false;
     narrow_tile<T, D, kW>(a, make_tile(a, u, blockIdx.x - u.item0, kNarrow), lds, joined, bad);
@@ -465,7 +466,7 @@ __global__ __launch_bounds__(kThreads, D == 64 && MANY ? 7 : MANY || D == 256 ? 
     constexpr int kPer = D / kWave;  // elements a lane
     __shared__ float acc[kWaves][D];
     const PlanHead& ph = *pv.head;
-    if (ph.part_rows == 0 || !plan_fits(ph, a, part_rows, D, items))
+    if (ph.part_rows == 0 || !plan_fits(ph, a, part_rows, D, kWide, items))
         return;  // the pass has left nothing (and reported it)
     const uint32_t wave = threadIdx.x / kWave, lane = lane_id();
     const bool together = ph.most_parts > 16;
@@ -589,7 +590,7 @@ uint64_t attn_plan_bytes(uint64_t n, uint64_t groups)
 }
 
 hipError_t attn_plan(dm_ctx* c, const dm_token_batch& b, const dm_kv_pages& kv, uint32_t q_heads,
-                     void* plan)
+                     uint32_t wide, void* plan)
 {
     PlanIn a;
     a.b = token_batch(c, b);
@@ -597,6 +598,7 @@ hipError_t attn_plan(dm_ctx* c, const dm_token_batch& b, const dm_kv_pages& kv, 
     a.kv_heads = kv.kv_heads;
     a.ratio = q_heads / kv.kv_heads;
     a.head_dim = kv.head_dim;
+    a.wide = wide;
     a.target = item_target(c);
     a.part_rows = small(c, b, kv, a.ratio) ? 0 : part_rows_of(c, b, q_heads);
     const PlanView pv = plan_view(plan, b.tables.n, b.groups);
@@ -636,7 +638,7 @@ hipError_t attn(dm_ctx* c, const dm_token_batch& b, const dm_kv_pages& kv, uint3
     a.ratio = q_heads / kv.kv_heads;
     a.scale2 = scale * kLog2e;
     const PlanView pv = plan_view(const_cast<void*>(plan), b.tables.n, b.groups);
-    const uint64_t most = is_small ? (uint64_t)b.tables.n * kv.kv_heads : most_items(c, b, a.ratio, kv.kv_heads);
+    const uint64_t most = is_small ? (uint64_t)b.tables.n * kv.kv_heads : most_items(c, b, a.ratio, kv.kv_heads, kWide);
     if (most > 0x7FFFFFFFull)
         return hipErrorInvalidValue;
     by_type(kv.dtype, kv.head_dim, [&](auto t, auto d) {

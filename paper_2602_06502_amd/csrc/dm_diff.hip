@@ -18,23 +18,31 @@
 namespace dm {
 namespace {
 
+// Rows of a wide tile and its waves, 32 rows a wave: where values have 256 elements LDS has
+// room for one workgroup a compute unit, so it has eight waves, two a SIMD.
+template <int D>
+constexpr uint32_t kDiffWide = D == 256 ? 2 * kWide : kWide;
+template <int D>
+constexpr int kDiffWaves = kDiffWide<D> / 32;
+
 template <typename T, int D>
-__global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void diff_kernel(DiffIn a, const PlanView pv,
-                                                                          uint64_t part_rows, uint32_t* status)
+__global__ __launch_bounds__(kDiffWaves<D>* kWave, D == 256 ? 1 : 2) void diff_kernel(DiffIn a, const PlanView pv,
+                                                                                    uint64_t part_rows,
+                                                                                    uint32_t* status)
 {
-    // as attn_kernel's; the second maps' rows at the end take half of it
-    __shared__ __attribute__((aligned(16))) uint16_t lds[4 * kWideKeys * D];
+    // as attn_kernel's; the second maps' rows at the end go through it
+    __shared__ __attribute__((aligned(512))) uint16_t lds[4 * kWideKeys * D];
     __shared__ uint32_t odd_tile;
-    __shared__ Joined<kWaves> joined;
+    __shared__ Joined<kDiffWaves<D>> joined;
     Unit u;
-    if (!item_unit(a, pv, a.b.groups + a.b.n, part_rows, D, status, u))
+    if (!item_unit(a, pv, a.b.groups + a.b.n, part_rows, D, kDiffWide<D>, status, u))
         return;
     bool bad = false;
     const uint32_t x = blockIdx.x - u.item0;
     if (u.flags & kUnitWide)
-        wide_tile<T, D, true>(a, make_tile(a, u, x, kWide), lds, &odd_tile, bad);
+        wide_tile<T, D, true, kDiffWaves<D>, false>(a, make_tile(a, u, x, kDiffWide<D>), lds, &odd_tile, bad);
     else
-        narrow_tile<T, D, kWaves, true>(a, make_tile(a, u, x, kNarrow), lds, joined, bad);
+        narrow_tile<T, D, kDiffWaves<D>, true, D == 256>(a, make_tile(a, u, x, kNarrow), lds, joined, bad);
     if (bad)
         atomicOr(status, kErrInval);
 }
@@ -48,7 +56,7 @@ __global__ __launch_bounds__(kSmallWaves<D>* kWave, 1) void diff_small_kernel(Di
     __shared__ __attribute__((aligned(16))) uint16_t lds[kW * 2 * kNarrowKeys * D];
     __shared__ Joined<kW> joined;
     Unit u;
-    if (!item_unit(a, pv, a.b.n, 0, D, status, u))
+    if (!item_unit(a, pv, a.b.n, 0, D, kDiffWide<D>, status, u))
         return;
     bool bad = false;
     narrow_tile<T, D, kW, true>(a, make_tile(a, u, blockIdx.x - u.item0, kNarrow), lds, joined, bad);
@@ -67,7 +75,7 @@ __global__ __launch_bounds__(kThreads) void diff_join_kernel(DiffIn a, const Pla
     __shared__ vper rows[kWaves][kWave];
     __shared__ v2f stats[kWaves];
     const PlanHead& ph = *pv.head;
-    if (ph.part_rows == 0 || !plan_fits(ph, a, part_rows, D, items))
+    if (ph.part_rows == 0 || !plan_fits(ph, a, part_rows, D, kDiffWide<D>, items))
         return;
     const uint32_t wave = threadIdx.x / kWave, lane = lane_id(), map = wave % 2;
     const uint32_t pairs = a.q_heads / 2, all = a.b.q_tokens * pairs;
@@ -163,7 +171,7 @@ __global__ __launch_bounds__(kThreads) void diff_join_many_kernel(DiffIn a, cons
                                                                   uint32_t items)
 {
     const PlanHead& ph = *pv.head;
-    if (ph.part_rows == 0 || !plan_fits(ph, a, part_rows, D, items))
+    if (ph.part_rows == 0 || !plan_fits(ph, a, part_rows, D, kDiffWide<D>, items))
         return;
     const uint64_t all = (uint64_t)a.b.q_tokens * a.q_heads, step = (uint64_t)gridDim.x * kWaves;
     const uint64_t per = ((all + step - 1) / step + 3) / 4 * 4;
@@ -181,6 +189,8 @@ dm_kv_pages pairs_of(const dm_kv_pages& kv)
     p.head_dim = kv.head_dim * 2;
     return p;
 }
+
+uint32_t diff_wide(const dm_kv_pages& kv) { return kv.head_dim == 128 ? kDiffWide<256> : kDiffWide<128>; }
 
 hipError_t diff_attn(dm_ctx* c, const dm_token_batch& b, const dm_kv_pages& store, uint32_t q_heads,
                      const void* plan, uint32_t layer, const dm_diff_args& g)
@@ -215,7 +225,7 @@ hipError_t diff_attn(dm_ctx* c, const dm_token_batch& b, const dm_kv_pages& stor
     a.eps = g.eps;
     a.gain = g.gain;
     const PlanView pv = plan_view(const_cast<void*>(plan), b.tables.n, b.groups);
-    const uint64_t most = is_small ? (uint64_t)b.tables.n * kv.kv_heads : most_items(c, b, ratio, kv.kv_heads);
+    const uint64_t most = is_small ? (uint64_t)b.tables.n * kv.kv_heads : most_items(c, b, ratio, kv.kv_heads, diff_wide(store));
     if (most > 0x7FFFFFFFull)
         return hipErrorInvalidValue;
     auto launch = [&](auto t, auto d) {
@@ -225,7 +235,7 @@ hipError_t diff_attn(dm_ctx* c, const dm_token_batch& b, const dm_kv_pages& stor
             diff_small_kernel<T, D><<<(uint32_t)most, kSmallWaves<D> * kWave, 0, c->stream>>>(a, pv, c->d_status);
             return;
         }
-        diff_kernel<T, D><<<(uint32_t)most, kThreads, 0, c->stream>>>(a, pv, rows, c->d_status);
+        diff_kernel<T, D><<<(uint32_t)most, kDiffWaves<D> * kWave, 0, c->stream>>>(a, pv, rows, c->d_status);
         const uint64_t outs = b.q_tokens * q_heads;
         if (outs > 8ull * c->n_cu * kWaves)
             diff_join_many_kernel<T, D><<<4u * c->n_cu, kThreads, 0, c->stream>>>(a, pv, rows, (uint32_t)most);

@@ -451,14 +451,17 @@ hipError_t pages_copy(dm_ctx* c, const dm_kv_pages& kv, const int32_t* src, cons
 hipError_t kv_append(dm_ctx* c, const dm_kv_pages& kv, uint32_t layer, const dm_token_batch& b,
                      const dm_append_args& a, const int64_t* first);
 uint64_t attn_plan_bytes(uint64_t n, uint64_t groups);
+// wide: rows of its wide tiles.
 hipError_t attn_plan(dm_ctx* c, const dm_token_batch& b, const dm_kv_pages& kv, uint32_t q_heads,
-                     void* plan);
+                     uint32_t wide, void* plan);
+constexpr uint32_t kAttnWide = 128;
 hipError_t attn(dm_ctx* c, const dm_token_batch& b, const dm_kv_pages& kv, uint32_t q_heads,
                 const void* plan, uint32_t layer, const void* q, int64_t q_stride, float scale,
                 void* out, int64_t out_stride, float* lse);
 // dm_diff.hip: attention's view of a store whose KV heads are pairs; its plan is
 // attn_plan's of that view.
 dm_kv_pages pairs_of(const dm_kv_pages& kv);
+uint32_t diff_wide(const dm_kv_pages& kv);
 hipError_t diff_attn(dm_ctx* c, const dm_token_batch& b, const dm_kv_pages& kv, uint32_t q_heads,
                      const void* plan, uint32_t layer, const dm_diff_args& a);
 // dm_weights.hip
