@@ -1036,7 +1036,7 @@ static dm_status plan_checked(dm_ctx* c, const dm_token_batch* batch, const dm_k
     DeviceGuard g(c->device);
     hipError_t e = join_selection(c);
     if (e == hipSuccess)
-        e = attn_plan(c, *batch, pairs ? pairs_of(*kv) : *kv, q_heads, pairs ? diff_wide(*kv) : kAttnWide, plan);
+        e = attn_plan(c, *batch, pairs ? pairs_of(*kv) : *kv, q_heads, pairs ? diff_wide(*kv, *batch, q_heads) : kAttnWide, plan);
     return e == hipSuccess ? DM_OK : hip_fail(c, e, what.c_str());
 }
 

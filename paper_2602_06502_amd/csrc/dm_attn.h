@@ -941,6 +941,8 @@ __device__ __forceinline__ void narrow_tile(const InOf<PAIR>& a, const Tile& t, 
                 for (int i = 0; i < 4; i++)
                     s[h][i] = row16 % 2 ? other[i] : s[h][i];
             }
+            if (SPLIT)
+                __builtin_amdgcn_sched_barrier(0);  // (not all of a tile's reads at once, for which there is no room)
         }
         if (masked) {
             uint32_t first = key + g * 4;
@@ -1055,11 +1057,12 @@ __device__ __forceinline__ void narrow_tile(const InOf<PAIR>& a, const Tile& t, 
                 in_order();
                 const bool strange = x.template stage_one<true>(vt, key, !all);
                 in_order();
+                const bool odd_ones = !all && __any(strange);
+                if (odd_ones)
+                    add_odd(key);  // (with nothing on its way: what this needs would push the query out)
                 if (key + kTurn < t.key1)
                     x.fetch_one(a.k, key + kTurn, bad);
-                if (!all && __any(strange))
-                    add_odd(key);
-                else
+                if (!odd_ones)
                     add();
             }
         } else {

@@ -38,17 +38,20 @@ namespace {
 
 constexpr int kPlanThreads = 512;
 
-// The tiles of a unit, by its rows, and their cost a key: a wide one takes up to
-// twice a narrow one's time.
+// The tiles of a unit, by its rows, and their cost a key: a wide one of 128 rows takes up
+// to twice a narrow one's time.  wide: rows of a wide tile; kNarrow: there are none.
 __device__ __forceinline__ uint32_t tile_rows(uint64_t rows, uint32_t wide) { return rows <= kNarrowRows ? kNarrow : wide; }
-__device__ __forceinline__ uint32_t tile_flags(uint64_t rows) { return rows <= kNarrowRows ? 0 : kUnitWide; }
+__device__ __forceinline__ uint32_t tile_flags(uint64_t rows, uint32_t wide) 
+{
+    return rows <= kNarrowRows || wide == kNarrow ? 0 : kUnitWide;
+}
 __device__ __forceinline__ uint64_t tiles_of(uint64_t rows, uint32_t wide)
 {
     return (rows + tile_rows(rows, wide) - 1) / tile_rows(rows, wide);
 }
 __device__ __forceinline__ uint64_t weight_of(uint64_t rows, uint32_t wide)
 {
-    return tiles_of(rows, wide) * (rows <= kNarrowRows ? 1 : wide / (kWide / 2));
+    return tiles_of(rows, wide) * (tile_flags(rows, wide) ? wide / (kWide / 2) : 1);
 }
 
 // Are the runs' bounds in order?
@@ -175,7 +178,7 @@ __device__ __forceinline__ Unit run_unit(const PlanIn& a, const RunView& r, uint
     u.key1 = pages << a.b.shift;
     u.off = r.off;
     u.table = pages;
-    u.flags = kUnitParts | tile_flags((uint64_t)u.ntok * a.ratio);
+    u.flags = kUnitParts | tile_flags((uint64_t)u.ntok * a.ratio, a.wide);
     return u;
 }
 
@@ -189,7 +192,7 @@ __device__ __forceinline__ Unit sequence_unit(const PlanIn& a, const SeqView& v,
     u.off = v.off;
     u.table = (uint32_t)((v.len + (1ll << a.b.shift) - 1) >> a.b.shift);
     u.pos0 = (int32_t)v.pos0;
-    u.flags = kUnitCausal | (pages ? kUnitParts : 0) | tile_flags((uint64_t)u.ntok * a.ratio);
+    u.flags = kUnitCausal | (pages ? kUnitParts : 0) | tile_flags((uint64_t)u.ntok * a.ratio, a.wide);
     return u;
 }
 

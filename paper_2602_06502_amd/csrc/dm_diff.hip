@@ -18,31 +18,62 @@
 namespace dm {
 namespace {
 
-// Rows of a wide tile and its waves, 32 rows a wave: where values have 256 elements LDS has
-// room for one workgroup a compute unit, so it has eight waves, two a SIMD.
-template <int D>
-constexpr uint32_t kDiffWide = D == 256 ? 2 * kWide : kWide;
-template <int D>
-constexpr int kDiffWaves = kDiffWide<D> / 32;
-
+// Values of 128 elements: both kinds of tiles in one kernel, two workgroups a compute unit.
 template <typename T, int D>
-__global__ __launch_bounds__(kDiffWaves<D>* kWave, D == 256 ? 1 : 2) void diff_kernel(DiffIn a, const PlanView pv,
-                                                                                    uint64_t part_rows,
-                                                                                    uint32_t* status)
+__global__ __launch_bounds__(kThreads, 2) void diff_kernel(DiffIn a, const PlanView pv, uint64_t part_rows,
+                                                           uint32_t* status)
 {
-    // as attn_kernel's; the second maps' rows at the end go through it
+    // as attn_kernel's; the second maps' rows at the end take half of it
     __shared__ __attribute__((aligned(512))) uint16_t lds[4 * kWideKeys * D];
     __shared__ uint32_t odd_tile;
-    __shared__ Joined<kDiffWaves<D>> joined;
+    __shared__ Joined<kWaves> joined;
     Unit u;
-    if (!item_unit(a, pv, a.b.groups + a.b.n, part_rows, D, kDiffWide<D>, status, u))
+    if (!item_unit(a, pv, a.b.groups + a.b.n, part_rows, D, kWide, status, u))
         return;
     bool bad = false;
     const uint32_t x = blockIdx.x - u.item0;
     if (u.flags & kUnitWide)
-        wide_tile<T, D, true, kDiffWaves<D>, false>(a, make_tile(a, u, x, kDiffWide<D>), lds, &odd_tile, bad);
+        wide_tile<T, D, true, kWaves, false>(a, make_tile(a, u, x, kWide), lds, &odd_tile, bad);
     else
-        narrow_tile<T, D, kDiffWaves<D>, true, D == 256>(a, make_tile(a, u, x, kNarrow), lds, joined, bad);
+        narrow_tile<T, D, kWaves, true>(a, make_tile(a, u, x, kNarrow), lds, joined, bad);
+    if (bad)
+        atomicOr(status, kErrInval);
+}
+
+// Values of 256: a wide tile's keys and values leave LDS room for one workgroup a compute
+// unit, which so has eight waves, two a SIMD, and 256 rows.  Narrow tiles, held apart, need
+// half of that a workgroup, so that two are on a compute unit and one reads while another
+// begins or ends: they have a kernel of their own.  (64 rows on up to 8,192 keys, 32 query and 8
+// key heads: 222 us; in one kernel of eight waves 246, of four, keys and values together, 225.)
+constexpr int kTallWaves = 8;
+constexpr uint32_t kTall = 32 * kTallWaves;
+
+template <typename T, int D>
+__global__ __launch_bounds__(kTallWaves* kWave, 1) void diff_tall_kernel(DiffIn a, const PlanView pv, uint64_t part_rows,
+                                                                         uint32_t* status)
+{
+    __shared__ __attribute__((aligned(512))) uint16_t lds[4 * kWideKeys * D];  // the second maps' rows too
+    __shared__ uint32_t odd_tile;
+    Unit u;
+    if (!item_unit(a, pv, a.b.groups + a.b.n, part_rows, D, kTall, status, u) || !(u.flags & kUnitWide))
+        return;
+    bool bad = false;
+    wide_tile<T, D, true, kTallWaves, false>(a, make_tile(a, u, blockIdx.x - u.item0, kTall), lds, &odd_tile, bad);
+    if (bad)
+        atomicOr(status, kErrInval);
+}
+
+template <typename T, int D>
+__global__ __launch_bounds__(kThreads, 2) void diff_narrow_kernel(DiffIn a, const PlanView pv, uint64_t part_rows,
+                                                                  uint32_t wide, uint32_t* status)
+{
+    __shared__ __attribute__((aligned(16))) uint16_t lds[kWaves * kNarrowKeys * D];
+    __shared__ Joined<kWaves> joined;
+    Unit u;
+    if (!item_unit(a, pv, a.b.groups + a.b.n, part_rows, D, wide, status, u) || (u.flags & kUnitWide))
+        return;
+    bool bad = false;
+    narrow_tile<T, D, kWaves, true, true>(a, make_tile(a, u, blockIdx.x - u.item0, kNarrow), lds, joined, bad);
     if (bad)
         atomicOr(status, kErrInval);
 }
@@ -50,13 +81,13 @@ __global__ __launch_bounds__(kDiffWaves<D>* kWave, D == 256 ? 1 : 2) void diff_k
 // A few rows on a few keys, as attn_small_kernel.
 template <typename T, int D>
 __global__ __launch_bounds__(kSmallWaves<D>* kWave, 1) void diff_small_kernel(DiffIn a, const PlanView pv,
-                                                                              uint32_t* status)
+                                                                              uint32_t wide, uint32_t* status)
 {
     constexpr int kW = kSmallWaves<D>;
     __shared__ __attribute__((aligned(16))) uint16_t lds[kW * 2 * kNarrowKeys * D];
     __shared__ Joined<kW> joined;
     Unit u;
-    if (!item_unit(a, pv, a.b.n, 0, D, kDiffWide<D>, status, u))
+    if (!item_unit(a, pv, a.b.n, 0, D, wide, status, u))
         return;
     bool bad = false;
     narrow_tile<T, D, kW, true>(a, make_tile(a, u, blockIdx.x - u.item0, kNarrow), lds, joined, bad);
@@ -68,14 +99,14 @@ __global__ __launch_bounds__(kSmallWaves<D>* kWave, 1) void diff_small_kernel(Di
 // with every second part; eight parts' rows are read at once.
 template <typename T, int D>
 __global__ __launch_bounds__(kThreads) void diff_join_kernel(DiffIn a, const PlanView pv, uint64_t part_rows,
-                                                             uint32_t items)
+                                                             uint32_t wide, uint32_t items)
 {
     constexpr int kPer = D / kWave, kAtOnce = 8;
     typedef float vper __attribute__((ext_vector_type(kPer)));
     __shared__ vper rows[kWaves][kWave];
     __shared__ v2f stats[kWaves];
     const PlanHead& ph = *pv.head;
-    if (ph.part_rows == 0 || !plan_fits(ph, a, part_rows, D, kDiffWide<D>, items))
+    if (ph.part_rows == 0 || !plan_fits(ph, a, part_rows, D, wide, items))
         return;
     const uint32_t wave = threadIdx.x / kWave, lane = lane_id(), map = wave % 2;
     const uint32_t pairs = a.q_heads / 2, all = a.b.q_tokens * pairs;
@@ -168,10 +199,10 @@ __global__ __launch_bounds__(kThreads) void diff_join_kernel(DiffIn a, const Pla
 // Where they are more than the places of waves: four rows a wave (as attn_join_kernel).
 template <typename T, int D>
 __global__ __launch_bounds__(kThreads) void diff_join_many_kernel(DiffIn a, const PlanView pv, uint64_t part_rows,
-                                                                  uint32_t items)
+                                                                  uint32_t wide, uint32_t items)
 {
     const PlanHead& ph = *pv.head;
-    if (ph.part_rows == 0 || !plan_fits(ph, a, part_rows, D, kDiffWide<D>, items))
+    if (ph.part_rows == 0 || !plan_fits(ph, a, part_rows, D, wide, items))
         return;
     const uint64_t all = (uint64_t)a.b.q_tokens * a.q_heads, step = (uint64_t)gridDim.x * kWaves;
     const uint64_t per = ((all + step - 1) / step + 3) / 4 * 4;
@@ -190,7 +221,15 @@ dm_kv_pages pairs_of(const dm_kv_pages& kv)
     return p;
 }
 
-uint32_t diff_wide(const dm_kv_pages& kv) { return kv.head_dim == 128 ? kDiffWide<256> : kDiffWide<128>; }
+// Heads of 128: where sequences have no more rows a pair than a narrow tile on average, and
+// no runs, every tile is narrow, and one kernel has them all.  (The other one's workgroups
+// would have been there only to see that they have nothing to do.)
+uint32_t diff_wide(const dm_kv_pages& kv, const dm_token_batch& b, uint32_t q_heads)
+{
+    if (kv.head_dim != 128)
+        return kWide;
+    return b.groups == 0 && b.q_tokens * (q_heads / (kv.kv_heads / 2)) <= kNarrowRows * b.tables.n ? kNarrow : kTall;
+}
 
 hipError_t diff_attn(dm_ctx* c, const dm_token_batch& b, const dm_kv_pages& store, uint32_t q_heads,
                      const void* plan, uint32_t layer, const dm_diff_args& g)
@@ -225,23 +264,30 @@ hipError_t diff_attn(dm_ctx* c, const dm_token_batch& b, const dm_kv_pages& stor
     a.eps = g.eps;
     a.gain = g.gain;
     const PlanView pv = plan_view(const_cast<void*>(plan), b.tables.n, b.groups);
-    const uint64_t most = is_small ? (uint64_t)b.tables.n * kv.kv_heads : most_items(c, b, ratio, kv.kv_heads, diff_wide(store));
+    const uint32_t wide = diff_wide(store, b, q_heads);
+    const uint64_t most = is_small ? (uint64_t)b.tables.n * kv.kv_heads : most_items(c, b, ratio, kv.kv_heads, wide);
     if (most > 0x7FFFFFFFull)
         return hipErrorInvalidValue;
     auto launch = [&](auto t, auto d) {
         using T = decltype(t);
         constexpr int D = decltype(d)::value;
         if (is_small) {
-            diff_small_kernel<T, D><<<(uint32_t)most, kSmallWaves<D> * kWave, 0, c->stream>>>(a, pv, c->d_status);
+            diff_small_kernel<T, D><<<(uint32_t)most, kSmallWaves<D> * kWave, 0, c->stream>>>(a, pv, wide, c->d_status);
             return;
         }
-        diff_kernel<T, D><<<(uint32_t)most, kDiffWaves<D> * kWave, 0, c->stream>>>(a, pv, rows, c->d_status);
+        if constexpr (D == 256) {
+            if (wide == kTall)
+                diff_tall_kernel<T, D><<<(uint32_t)most, kTallWaves * kWave, 0, c->stream>>>(a, pv, rows, c->d_status);
+            diff_narrow_kernel<T, D><<<(uint32_t)most, kThreads, 0, c->stream>>>(a, pv, rows, wide, c->d_status);
+        } else {
+            diff_kernel<T, D><<<(uint32_t)most, kThreads, 0, c->stream>>>(a, pv, rows, c->d_status);
+        }
         const uint64_t outs = b.q_tokens * q_heads;
         if (outs > 8ull * c->n_cu * kWaves)
-            diff_join_many_kernel<T, D><<<4u * c->n_cu, kThreads, 0, c->stream>>>(a, pv, rows, (uint32_t)most);
+            diff_join_many_kernel<T, D><<<4u * c->n_cu, kThreads, 0, c->stream>>>(a, pv, rows, wide, (uint32_t)most);
         else
             diff_join_kernel<T, D>
-                <<<grid_for(outs / 2, 1, 8u * c->n_cu), kThreads, 0, c->stream>>>(a, pv, rows, (uint32_t)most);
+                <<<grid_for(outs / 2, 1, 8u * c->n_cu), kThreads, 0, c->stream>>>(a, pv, rows, wide, (uint32_t)most);
     };
     auto dims = [&](auto t) {
         if (kv.head_dim == 128)

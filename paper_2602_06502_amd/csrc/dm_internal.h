@@ -461,7 +461,7 @@ hipError_t attn(dm_ctx* c, const dm_token_batch& b, const dm_kv_pages& kv, uint3
 // dm_diff.hip: attention's view of a store whose KV heads are pairs; its plan is
 // attn_plan's of that view.
 dm_kv_pages pairs_of(const dm_kv_pages& kv);
-uint32_t diff_wide(const dm_kv_pages& kv);
+uint32_t diff_wide(const dm_kv_pages& kv, const dm_token_batch& b, uint32_t q_heads);
 hipError_t diff_attn(dm_ctx* c, const dm_token_batch& b, const dm_kv_pages& kv, uint32_t q_heads,
                      const void* plan, uint32_t layer, const dm_diff_args& a);
 // dm_weights.hip
