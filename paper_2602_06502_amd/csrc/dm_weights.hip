@@ -10,6 +10,10 @@
 // lane's page is known without knowing whose it is, and a block may hold the end of one
 // sequence and the beginnings of others, which take their turns.
 //
+// Where sequences have many rows, a second kernel before the first has a workgroup for 256
+// keys of a head and a stretch of rows, which pass through LDS once for its four waves; it
+// leaves its sums, and the first kernel adds a key's up.
+//
 // The pages that a run shares (as its plan has found them) are read once, by the blocks of
 // its first sequence's entries, for all its sequences, each with its own sums.
 //
@@ -20,6 +24,10 @@ namespace dm {
 namespace {
 
 constexpr uint32_t kBlockKeys = 64;
+// Rows of a sequence, at most, that the blocks of 64 keys take themselves where there are
+// tall blocks too.
+constexpr uint32_t kFewRows = 64;
+constexpr uint32_t kTallKeys = kWaves * kBlockKeys, kTallRows = 64;  // keys of a tall block, rows in LDS
 
 struct WeightsIn {
     TokenBatch b;
@@ -35,7 +43,34 @@ struct WeightsIn {
     uint32_t prev_n, n_pages, q_heads, kv_heads, ratio, last, paired;
     uint32_t plan_heads, plan_dim;  // the plan's
     float scale2, decay;
+    // tall blocks: stretches of rows (0: there are none), their rows, and their sums
+    // [parts][kv_heads][slots]
+    uint32_t parts, part_rows;
+    float* part;
+    int64_t slots;
 };
+
+// The first row of a sequence that counts.
+__device__ __forceinline__ uint32_t first_row(const WeightsIn& a, const SeqView& v)
+{
+    return (a.last && a.last < v.ntok ? v.ntok - a.last : 0) * a.ratio;
+}
+__device__ __forceinline__ bool few(const WeightsIn& a, const SeqView& v)
+{
+    return v.ntok * a.ratio - first_row(a, v) <= kFewRows;
+}
+// Rows of stretch p that see something of a block whose first key is the sequence's i0-th.
+struct Stretch {
+    uint32_t row0, row1;
+};
+__device__ __forceinline__ Stretch stretch_of(const WeightsIn& a, const SeqView& v, int64_t i0, bool causal, uint32_t p)
+{
+    uint32_t row0 = first_row(a, v), row1 = v.ntok * a.ratio;
+    const uint64_t s0 = row0 + (uint64_t)p * a.part_rows, s1 = s0 + a.part_rows;
+    if (causal && i0 > v.pos0 + row0 / a.ratio)
+        row0 = (uint32_t)(i0 - v.pos0) * a.ratio;
+    return Stretch{row0 > s0 ? row0 : (uint32_t)s0, row1 < s1 ? row1 : (uint32_t)s1};
+}
 
 // The rows of a sequence for one KV head.
 struct Rows {
@@ -125,6 +160,37 @@ __device__ __forceinline__ void weights_of(const WeightsIn& a, const Rows& s, ui
     total[1] = sum[1].sum;
 }
 
+// collect(sequence, its view, the token that slot0 would be of it, tokens [from, to) that are
+// meant, whether later tokens do not see them) for the sequences that have tokens in the
+// slots from slot0 on; those that a run shares, for its first sequence's slots, for each of
+// its sequences.  By whole waves, slot0 uniform.
+template <typename F>
+__device__ __forceinline__ void each_sequence(const TokenBatch& b, const PlanView& pv, int64_t slot0, uint32_t keys,
+                                              bool& bad, F&& collect)
+{
+    const int64_t entry0 = slot0 >> b.shift, entry1 = (slot0 + keys - 1) >> b.shift;
+    for (uint32_t s = wave_find(b.off, b.n, 1, entry0); s < b.n && b.off[s] <= entry1; s++) {
+        const SeqView v = sequence_view(b, s);
+        bad |= v.bad;
+        const int64_t i0 = slot0 - (b.off[s] << b.shift);
+        int64_t shared = 0;  // tokens that the run's first sequence's blocks take
+        if (b.groups) {
+            const RunOf r = run_of(b, s);
+            shared = r.ok ? (int64_t)pv.unit[r.g].key1 : 0;
+            if (r.ok && s == (uint32_t)r.g0 && i0 < shared)
+                for (uint32_t m = (uint32_t)r.g0; m < (uint32_t)r.g1; m++) {
+                    const SeqView x = sequence_view(b, m);
+                    if (!x.bad && x.ntok && x.len && pv.unit[b.groups + m].key0)
+                        collect(m, x, i0, 0, shared, false);
+                }
+            // one that is not among those keeps its own
+            shared = v.ntok && v.len && pv.unit[b.groups + s].key0 ? shared : 0;
+        }
+        if (v.len > shared && i0 < v.len && i0 + (int64_t)keys > shared)
+            collect(s, v, i0, shared, v.len, true);
+    }
+}
+
 template <typename T, int D>
 __global__ __launch_bounds__(kThreads) void weights_kernel(WeightsIn a, const PlanView pv, uint64_t items, uint32_t* status)
 {
@@ -144,7 +210,6 @@ __global__ __launch_bounds__(kThreads) void weights_kernel(WeightsIn a, const Pl
     RowWords& words = all_words[wave];
     const uint32_t h = item % a.kv_heads;
     const int64_t slot0 = (int64_t)(item / a.kv_heads) * kBlockKeys;
-    const int64_t entry0 = slot0 >> b.shift, entry1 = (slot0 + kBlockKeys - 1) >> b.shift;
     const uint32_t x0 = a.paired ? h / 2 * 2 * a.ratio + h % 2 : h * a.ratio, xs = a.paired ? 2 : 1;
     V k[2][D / 16];
     bool bad_page[2] = {};
@@ -168,20 +233,28 @@ __global__ __launch_bounds__(kThreads) void weights_kernel(WeightsIn a, const Pl
     // sums of sequence s over tokens [from, to) that are in the block (token 0 is slot0 -
     // i0), whose keys are here, to where s has them
     auto collect = [&](uint32_t s, const SeqView& v, int64_t i0, int64_t from, int64_t to, bool causal) {
-        float sum[2] = {0, 0};
+        float sum[2] = {0, 0}, whole = 0;
         const int64_t i = i0 + lane;
         const bool mine = i >= from && i < to;
-        if (v.ntok) {
+        if (a.parts && v.ntok && !few(a, v)) {
+            // (the tall block begins before this one, in the same sequence's numbers)
+            const int64_t tall0 = i0 - (slot0 & (kTallKeys - 1)), at = (b.off[s] << b.shift) + i;
+            for (uint32_t p = 0; p < a.parts; p++) {
+                const Stretch r = stretch_of(a, v, tall0, causal, p);
+                if (mine && r.row0 < r.row1)
+                    whole += a.part[((uint64_t)p * a.kv_heads + h) * a.slots + at];
+            }
+        } else if (v.ntok) {
             load();
             const bool key[2] = {i0 + lane % 32 >= from && i0 + lane % 32 < to,
                                  i0 + 32 + lane % 32 >= from && i0 + 32 + lane % 32 < to};
             bad |= (key[0] && bad_page[0]) || (key[1] && bad_page[1]);
-            Rows r{v.tok0, v.ntok, (a.last && a.last < v.ntok ? v.ntok - a.last : 0) * a.ratio, v.pos0};
+            Rows r{v.tok0, v.ntok, first_row(a, v), v.pos0};
             weights_of<T, D>(a, r, x0, xs, i0, causal, k, words, sum);
         }
         sum[0] += __shfl_xor(sum[0], 32);
         sum[1] += __shfl_xor(sum[1], 32);
-        float w = half ? sum[1] : sum[0];
+        float w = (half ? sum[1] : sum[0]) + whole;
         if (!mine)
             return;
         const int64_t at = (v.off << b.shift) + i;
@@ -200,28 +273,211 @@ __global__ __launch_bounds__(kThreads) void weights_kernel(WeightsIn a, const Pl
         }
         a.w[(int64_t)h * a.w_stride + at] = w;
     };
-    for (uint32_t s = wave_find(b.off, b.n, 1, entry0); s < b.n && b.off[s] <= entry1; s++) {
-        const SeqView v = sequence_view(b, s);
-        bad |= v.bad;
-        const int64_t i0 = slot0 - (b.off[s] << b.shift);
-        int64_t shared = 0;  // tokens that the run's first sequence's blocks take
-        if (b.groups) {
-            const RunOf r = run_of(b, s);
-            shared = r.ok ? (int64_t)pv.unit[r.g].key1 : 0;
-            if (r.ok && s == (uint32_t)r.g0 && i0 < shared)
-                for (uint32_t m = (uint32_t)r.g0; m < (uint32_t)r.g1; m++) {
-                    const SeqView x = sequence_view(b, m);
-                    if (!x.bad && x.ntok && x.len && pv.unit[b.groups + m].key0)
-                        collect(m, x, i0, 0, shared, false);
-                }
-            // one that is not among those keeps its own
-            shared = v.ntok && v.len && pv.unit[b.groups + s].key0 ? shared : 0;
-        }
-        if (v.len > shared && i0 < v.len && i0 + (int64_t)kBlockKeys > shared)
-            collect(s, v, i0, shared, v.len, true);
-    }
+    each_sequence(b, pv, slot0, kBlockKeys, bad, collect);
     if (bad)
         atomicOr(status, kErrInval);
+}
+
+// ---------------------------------------------------------------------------
+// Many rows.
+// ---------------------------------------------------------------------------
+
+// A tile of rows in LDS: their queries, their log-sum-exps (in powers of two), the last key
+// that each sees.
+template <int D>
+struct RowTile {
+    uint16_t q[kTallRows * D];
+    float lse[kTallRows];
+    int32_t sees[kTallRows];
+};
+
+// Rows in the order that a thread sends them: token and head of its row, kept from tile to
+// tile without a division.
+struct RowAt {
+    uint32_t t, x;
+    __device__ __forceinline__ void begin(uint32_t row, uint32_t ratio)
+    {
+        t = row / ratio;
+        x = row - t * ratio;
+    }
+    __device__ __forceinline__ void on(uint32_t tokens, uint32_t heads, uint32_t ratio)
+    {
+        t += tokens;
+        x += heads;
+        if (x >= ratio) {
+            x -= ratio;
+            t++;
+        }
+    }
+};
+
+template <typename T, int D>
+__global__ __launch_bounds__(kThreads, D == 256 ? 1 : D == 128 ? 2 : 3) void weights_tall_kernel(WeightsIn a, const PlanView pv,
+                                                                                  uint32_t blocks, uint32_t* status)
+{
+    using V = typename Vec8<T>::type;
+    constexpr uint32_t kRowChunks = D / 8, kStep = kThreads / kRowChunks;
+    constexpr int kLoads = kTallRows * D / 8 / kThreads;
+    __shared__ __attribute__((aligned(512))) RowTile<D> tiles[2];
+    const TokenBatch& b = a.b;
+    if (!plan_of(*pv.head, b, a.q_heads, a.plan_heads, a.plan_dim))
+        return;  // (the other kernel reports it)
+    const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = lane_id(), half = lane / 32;
+    // the blocks that pass over the same rows at the same time are on the same die
+    const uint32_t h = blockIdx.x % a.kv_heads, block = blockIdx.x / a.kv_heads % blocks,
+                   p = blockIdx.x / a.kv_heads / blocks;
+    const int64_t slot0 = (int64_t)block * kTallKeys;
+    const uint32_t x0 = a.paired ? h / 2 * 2 * a.ratio + h % 2 : h * a.ratio, xs = a.paired ? 2 : 1;
+    V k[2][D / 16];
+    bool have = false, bad = false;
+    const uint32_t tokens = kTallRows / a.ratio, heads = kTallRows % a.ratio;
+    auto collect = [&](uint32_t s, const SeqView& v, int64_t i0, int64_t from, int64_t to, bool causal) {
+        if (v.ntok == 0 || few(a, v))
+            return;
+        const Stretch r = stretch_of(a, v, i0, causal, p);
+        if (r.row0 >= r.row1)
+            return;
+        if (!have) {
+            have = true;
+#pragma unroll
+            for (int c = 0; c < 2; c++) {
+                const int64_t slot = slot0 + wave * kBlockKeys + c * 32 + lane % 32, e = slot >> b.shift;
+                uint32_t page = e < b.entries ? (uint32_t)b.page[e] : 0;
+                page = page < a.n_pages ? page : 0;  // (the other kernel reports it)
+                const uint16_t* at = a.k + ((((uint64_t)page * a.kv_heads + h) << b.shift) + (slot & ((1 << b.shift) - 1))) * D +
+                                     half * 8;
+#pragma unroll
+                for (int d = 0; d < D / 16; d++)
+                    k[c][d] = *reinterpret_cast<const V*>(at + d * 16);
+            }
+        }
+        // what a thread sends of a tile, and whose words it writes
+        RowAt mine[kLoads], word;
+#pragma unroll
+        for (int i = 0; i < kLoads; i++)
+            mine[i].begin(r.row0 + threadIdx.x / kRowChunks + i * kStep, a.ratio);
+        word.begin(r.row0 + threadIdx.x % kTallRows, a.ratio);
+        float far = 0;
+        auto send = [&](uint32_t row0, RowTile<D>& to) {
+#pragma unroll
+            for (int i = 0; i < kLoads; i++) {
+                const uint32_t row = threadIdx.x / kRowChunks + i * kStep;
+                // rows past the last: the last token's first head's again
+                const bool there = row0 + row < r.row1;
+                const uint32_t t = there ? mine[i].t : v.ntok - 1, x = there ? mine[i].x : 0;
+                const uint32_t c = threadIdx.x % kRowChunks ^ k_swizzle<D>(row);
+                send16(a.q + (int64_t)(v.tok0 + t) * a.q_stride + (uint64_t)(x0 + x * xs) * D + c * 8,
+                       lds_address(to.q) + (i * kThreads + wave * kWave) * 16);
+                mine[i].on(tokens, heads, a.ratio);
+            }
+        };
+        // words of the tile at row0, read, and then written
+        auto read_words = [&](uint32_t row0) {
+            const uint32_t row = row0 + threadIdx.x;
+            far = INFINITY;
+            if (threadIdx.x < kTallRows && row < r.row1) {
+                const float l = a.lse[(uint64_t)(v.tok0 + word.t) * a.q_heads + x0 + word.x * xs] * kLog2e;
+                far = l != -INFINITY ? l : INFINITY;
+            }
+        };
+        auto write_words = [&](RowTile<D>& to) {
+            if (threadIdx.x < kTallRows) {
+                to.lse[threadIdx.x] = far;
+                to.sees[threadIdx.x] = (int32_t)(v.pos0 + word.t);
+            }
+            word.on(tokens, heads, a.ratio);
+        };
+        const int64_t i1 = i0 + wave * kBlockKeys;  // the wave's first key
+        const int32_t key = (int32_t)((uint32_t)i1 + lane % 32);
+        const bool any = i1 < to && i1 + (int64_t)kBlockKeys > from;
+        LongSum sum[2];
+        __syncthreads();  // (the tiles' last readers)
+        read_words(r.row0);
+        send(r.row0, tiles[0]);
+        write_words(tiles[0]);
+        uint32_t buf = 0;
+        for (uint32_t row0 = r.row0; row0 < r.row1; row0 += kTallRows, buf ^= 1) {
+            wait_sent();
+            __syncthreads();
+            const RowTile<D>& tile = tiles[buf];
+            const bool more = row0 + kTallRows < r.row1;
+            if (more) {
+                read_words(row0 + kTallRows);
+                send(row0 + kTallRows, tiles[buf ^ 1]);
+            }
+            const bool masked = causal && i1 + kBlockKeys - 1 > tile.sees[0];
+            if (any)
+#pragma unroll
+                for (uint32_t part = 0; part < kTallRows; part += 32) {
+                    v16f z[2] = {};
+#pragma unroll
+                    for (int d = 0; d < D / 16; d++) {
+                        const uint32_t chunk = (d * 2 + half) ^ k_swizzle<D>(lane % 32);
+                        const V q = *reinterpret_cast<const V*>(tile.q + (part + lane % 32) * D + chunk * 8);
+                        z[0] = mfma(q, k[0][d], z[0]);
+                        z[1] = mfma(q, k[1][d], z[1]);
+                    }
+                    float add[2] = {0, 0};
+#pragma unroll
+                    for (int g = 0; g < 16; g += 4) {
+                        const v4f l = *reinterpret_cast<const v4f*>(&tile.lse[part + g * 2 + half * 4]);
+                        float w[2][4];
+#pragma unroll
+                        for (int c = 0; c < 2; c++)
+#pragma unroll
+                            for (int j = 0; j < 4; j++)
+                                w[c][j] = __builtin_amdgcn_exp2f(__builtin_fmaf(z[c][g + j], a.scale2, -l[j]));
+                        if (masked) {
+                            const int4 sees = *reinterpret_cast<const int4*>(&tile.sees[part + g * 2 + half * 4]);
+                            const int32_t last[4] = {sees.x, sees.y, sees.z, sees.w};
+#pragma unroll
+                            for (int c = 0; c < 2; c++)
+#pragma unroll
+                                for (int j = 0; j < 4; j++)
+                                    w[c][j] = key + c * 32 <= last[j] ? w[c][j] : 0.0f;
+                        }
+#pragma unroll
+                        for (int j = 0; j < 4; j++) {
+                            add[0] += w[0][j];
+                            add[1] += w[1][j];
+                        }
+                    }
+                    sum[0].add(add[0]);
+                    sum[1].add(add[1]);
+                }
+            if (more)
+                write_words(tiles[buf ^ 1]);
+        }
+        const float s0 = sum[0].sum + __shfl_xor(sum[0].sum, 32), s1 = sum[1].sum + __shfl_xor(sum[1].sum, 32);
+        const int64_t i = i1 + lane;
+        if (i >= from && i < to)
+            a.part[((uint64_t)p * a.kv_heads + h) * a.slots + (b.off[s] << b.shift) + i] = half ? s1 : s0;
+    };
+    each_sequence(b, pv, slot0, kTallKeys, bad, collect);
+}
+
+// How many stretches of rows tall blocks are for (0: there are none), and their rows: some
+// six workgroups a compute unit if all sequences are alike.  A batch with hardly more
+// tokens than sequences has none: where one sequence has them all, those are a few rows yet.
+uint32_t parts_of_rows(const dm_ctx* c, const dm_token_batch& b, uint32_t ratio, uint32_t last, uint64_t blocks,
+                       uint32_t* part_rows)
+{
+    constexpr uint64_t kMany = 1024, kParts = 16;
+    *part_rows = 0;
+    const uint64_t n = b.tables.n, tokens = last && last < b.q_tokens ? last : b.q_tokens;  // of a sequence, at most
+    if (b.q_tokens <= n || (b.q_tokens - n) * ratio <= kMany || tokens * ratio <= kFewRows || blocks == 0)
+        return 0;
+    const uint64_t each = (last && last * n < b.q_tokens ? last * n : b.q_tokens) * ratio / n;  // rows of a sequence
+    uint64_t rows = blocks * each / (6 * c->n_cu);
+    rows = (rows / kTallRows + 1) * kTallRows;
+    rows = rows < 512 ? 512 : rows;
+    const uint64_t most = (tokens * ratio + kParts - 1) / kParts;  // no more stretches than kParts
+    rows = rows < most ? (most + kTallRows - 1) / kTallRows * kTallRows : rows;
+    const uint64_t parts = (tokens * ratio + rows - 1) / rows;
+    if (parts * blocks > 0x7FFFFFFFull)
+        return 0;
+    *part_rows = (uint32_t)rows;
+    return (uint32_t)parts;
 }
 
 }  // namespace
@@ -261,9 +517,22 @@ hipError_t attn_weights(dm_ctx* c, const dm_token_batch& b, const dm_kv_pages& k
         return hipErrorInvalidValue;
     if (grid == 0)
         return hipSuccess;
+    a.slots = (int64_t)slots;
+    const uint32_t blocks = (uint32_t)((slots + kTallKeys - 1) / kTallKeys);
+    a.parts = parts_of_rows(c, b, a.ratio, g.last, (uint64_t)blocks * kv.kv_heads, &a.part_rows);
+    a.part = nullptr;
+    if (a.parts) {
+        hipError_t e;
+        a.part = static_cast<float*>(scratch_get(c, kSlotPages, a.parts * kv.kv_heads * slots * 4, &e));
+        if (!a.part)
+            return e;
+    }
     by_type(kv.dtype, kv.head_dim, [&](auto t, auto d) {
         using T = decltype(t);
         constexpr int D = decltype(d)::value;
+        if (a.parts)
+            weights_tall_kernel<T, D>
+                <<<a.parts * blocks * kv.kv_heads, kThreads, 0, c->stream>>>(a, pv, blocks, c->d_status);
         weights_kernel<T, D><<<(uint32_t)grid, kThreads, 0, c->stream>>>(a, pv, items, c->d_status);
     });
     return hipGetLastError();
