@@ -78,11 +78,12 @@ struct Rows {
     int64_t pos0;
 };
 
-// What a wave leaves for itself of its 32 rows: their log-sum-exps (in powers of two), and
-// the last key that each sees.
-struct RowWords {
-    float lse[32];
-    int32_t sees[32];
+// What is in LDS of rows: their log-sum-exps (in powers of two), and the last key that each
+// sees.
+template <int ROWS>
+struct WordsOf {
+    float lse[ROWS];
+    int32_t sees[ROWS];
 };
 
 // A sum that keeps what its additions round away: tens of thousands of weights, most of
@@ -100,7 +101,7 @@ struct LongSum {
 
 template <typename T, int D>
 __device__ __forceinline__ void weights_of(const WeightsIn& a, const Rows& s, uint32_t x0, uint32_t xs, int64_t i0,
-                                           bool causal, const typename Vec8<T>::type (&k)[2][D / 16], RowWords& words,
+                                           bool causal, const typename Vec8<T>::type (&k)[2][D / 16], WordsOf<32>& words,
                                            float (&total)[2])
 {
     LongSum sum[2];
@@ -195,7 +196,7 @@ template <typename T, int D>
 __global__ __launch_bounds__(kThreads) void weights_kernel(WeightsIn a, const PlanView pv, uint64_t items, uint32_t* status)
 {
     using V = typename Vec8<T>::type;
-    __shared__ __attribute__((aligned(16))) RowWords all_words[kWaves];
+    __shared__ __attribute__((aligned(16))) WordsOf<32> all_words[kWaves];
     const TokenBatch& b = a.b;
     const PlanHead& ph = *pv.head;
     if (!plan_of(ph, b, a.q_heads, a.plan_heads, a.plan_dim)) {
@@ -207,7 +208,7 @@ __global__ __launch_bounds__(kThreads) void weights_kernel(WeightsIn a, const Pl
     const uint64_t item = (uint64_t)blockIdx.x * kWaves + wave;
     if (item >= items)
         return;
-    RowWords& words = all_words[wave];
+    WordsOf<32>& words = all_words[wave];
     const uint32_t h = item % a.kv_heads;
     const int64_t slot0 = (int64_t)(item / a.kv_heads) * kBlockKeys;
     const uint32_t x0 = a.paired ? h / 2 * 2 * a.ratio + h % 2 : h * a.ratio, xs = a.paired ? 2 : 1;
@@ -282,17 +283,7 @@ __global__ __launch_bounds__(kThreads) void weights_kernel(WeightsIn a, const Pl
 // Many rows.
 // ---------------------------------------------------------------------------
 
-// A tile of rows in LDS: their queries, their log-sum-exps (in powers of two), the last key
-// that each sees.
-template <int D>
-struct RowTile {
-    uint16_t q[kTallRows * D];
-    float lse[kTallRows];
-    int32_t sees[kTallRows];
-};
-
-// Rows in the order that a thread sends them: token and head of its row, kept from tile to
-// tile without a division.
+// Token and head of a thread's row, kept from tile to tile without a division.
 struct RowAt {
     uint32_t t, x;
     __device__ __forceinline__ void begin(uint32_t row, uint32_t ratio)
@@ -318,7 +309,9 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : D == 128 ? 2 : 3) void wei
     using V = typename Vec8<T>::type;
     constexpr uint32_t kRowChunks = D / 8, kStep = kThreads / kRowChunks;
     constexpr int kLoads = kTallRows * D / 8 / kThreads;
-    __shared__ __attribute__((aligned(512))) RowTile<D> tiles[2];
+    using RowWords = WordsOf<kTallRows>;
+    __shared__ __attribute__((aligned(512))) uint16_t tiles[2][kTallRows * D];
+    __shared__ __attribute__((aligned(16))) RowWords words[3];  // of the tile before too, whose weights come later
     const TokenBatch& b = a.b;
     if (!plan_of(*pv.head, b, a.q_heads, a.plan_heads, a.plan_dim))
         return;  // (the other kernel reports it)
@@ -351,24 +344,38 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : D == 128 ? 2 : 3) void wei
                     k[c][d] = *reinterpret_cast<const V*>(at + d * 16);
             }
         }
-        // what a thread sends of a tile, and whose words it writes
-        RowAt mine[kLoads], word;
-#pragma unroll
-        for (int i = 0; i < kLoads; i++)
-            mine[i].begin(r.row0 + threadIdx.x / kRowChunks + i * kStep, a.ratio);
+        RowAt word;  // whose words a thread writes
         word.begin(r.row0 + threadIdx.x % kTallRows, a.ratio);
         float far = 0;
-        auto send = [&](uint32_t row0, RowTile<D>& to) {
+        const uint32_t to_row = threadIdx.x / kRowChunks, to_chunk = threadIdx.x % kRowChunks;
+        // where a step of rows is whole tokens, a lane's place in one is the same in all of
+        // them, but for k_swizzle, which goes by the row's low four bits: a uniform address
+        // and the lane's bytes on from it
+        const bool even = kStep % a.ratio == 0 && r.row0 % a.ratio == 0 && a.q_stride < (1 << 24);
+        uint32_t lane_at[2];
+#pragma unroll
+        for (int i = 0; i < 2; i++)
+            lane_at[i] = even ? (uint32_t)(to_row / a.ratio * a.q_stride + (x0 + to_row % a.ratio * xs) * D +
+                                           (to_chunk ^ k_swizzle<D>(to_row + i * kStep)) * 8) * 2
+                              : 0;
+        auto send = [&](uint32_t row0, const uint16_t* to) {
+            const uint32_t at = lds_address(to) + wave * kWave * 16;
+            if (even && row0 + kTallRows <= r.row1) {
+                const uint16_t* from = a.q + (int64_t)(v.tok0 + row0 / a.ratio) * a.q_stride;
+#pragma unroll
+                for (int i = 0; i < kLoads; i++)
+                    send16(from + i * (int64_t)(kStep / a.ratio) * a.q_stride, lane_at[i % 2], at + i * kThreads * 16);
+                return;
+            }
 #pragma unroll
             for (int i = 0; i < kLoads; i++) {
-                const uint32_t row = threadIdx.x / kRowChunks + i * kStep;
+                const uint32_t row = to_row + i * kStep;
                 // rows past the last: the last token's first head's again
                 const bool there = row0 + row < r.row1;
-                const uint32_t t = there ? mine[i].t : v.ntok - 1, x = there ? mine[i].x : 0;
-                const uint32_t c = threadIdx.x % kRowChunks ^ k_swizzle<D>(row);
-                send16(a.q + (int64_t)(v.tok0 + t) * a.q_stride + (uint64_t)(x0 + x * xs) * D + c * 8,
-                       lds_address(to.q) + (i * kThreads + wave * kWave) * 16);
-                mine[i].on(tokens, heads, a.ratio);
+                const uint32_t t = there ? (row0 + row) / a.ratio : v.ntok - 1, x = there ? (row0 + row) % a.ratio : 0;
+                send16(a.q + (int64_t)(v.tok0 + t) * a.q_stride + (uint64_t)(x0 + x * xs) * D +
+                           (to_chunk ^ k_swizzle<D>(row)) * 8,
+                       at + i * kThreads * 16);
             }
         };
         // words of the tile at row0, read, and then written
@@ -380,7 +387,7 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : D == 128 ? 2 : 3) void wei
                 far = l != -INFINITY ? l : INFINITY;
             }
         };
-        auto write_words = [&](RowTile<D>& to) {
+        auto write_words = [&](RowWords& to) {
             if (threadIdx.x < kTallRows) {
                 to.lse[threadIdx.x] = far;
                 to.sees[threadIdx.x] = (int32_t)(v.pos0 + word.t);
@@ -389,65 +396,111 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : D == 128 ? 2 : 3) void wei
         };
         const int64_t i1 = i0 + wave * kBlockKeys;  // the wave's first key
         const int32_t key = (int32_t)((uint32_t)i1 + lane % 32);
-        const bool any = i1 < to && i1 + (int64_t)kBlockKeys > from;
+        const bool any = i1 < to && i1 + (int64_t)kBlockKeys > from;  // has the wave some of these keys?
         LongSum sum[2];
         __syncthreads();  // (the tiles' last readers)
         read_words(r.row0);
         send(r.row0, tiles[0]);
-        write_words(tiles[0]);
-        uint32_t buf = 0;
+        write_words(words[0]);
+        // the keys are here: the compiler, which does not count the sends, would wait for their
+        // reads in every tile and so for the sends
+#pragma unroll
+        for (int d = 0; d < D / 16; d++)
+            asm volatile("" : "+v"(k[0][d]), "+v"(k[1][d]));
+        // Scores of 32 rows (at q, in LDS).  With the weights of the 32 rows before them (old, at
+        // `part` of their tile) beside their products: the matrix unit has work that these do
+        // not wait for.
+        auto scores_of = [&](auto with, v16f (&z)[2], const uint16_t* q, const v16f (&old)[2], const RowWords& words,
+                             uint32_t part) {
+            constexpr int kSteps = D / 16, kPer = 32 / kSteps;
+            V f[2];
+            auto read = [&](int d) {
+                f[d % 2] = *reinterpret_cast<const V*>(q + lane % 32 * D + ((d * 2 + half) ^ k_swizzle<D>(lane % 32)) * 8);
+            };
+            float add[2] = {0, 0};
+            v4f l;
+            z[0] = z[1] = v16f{};
+            read(0);
+#pragma unroll
+            for (int d = 0; d < kSteps; d++) {
+                if (d + 1 < kSteps)
+                    read(d + 1);
+                z[0] = mfma(f[d % 2], k[0][d], z[0]);
+                z[1] = mfma(f[d % 2], k[1][d], z[1]);
+                if constexpr (decltype(with)::value) {
+#pragma unroll
+                    for (int i = d * kPer; i < (d + 1) * kPer; i++) {
+                        const int g = i / 8 * 4, c = i / 4 % 2, j = i % 4;
+                        if (i % 8 == 0)
+                            l = *reinterpret_cast<const v4f*>(&words.lse[part + g * 2 + half * 4]);
+                        add[c] += __builtin_amdgcn_exp2f(__builtin_fmaf(old[c][g + j], a.scale2, -l[j]));
+                    }
+                }
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            if constexpr (decltype(with)::value) {
+                sum[0].add(add[0]);
+                sum[1].add(add[1]);
+            }
+        };
+        // the weights of 32 rows by themselves; masked: some key is later than some row
+        auto finish = [&](const v16f (&z)[2], const RowWords& words, uint32_t part, bool masked) {
+            float add[2] = {0, 0};
+#pragma unroll
+            for (int g = 0; g < 16; g += 4) {
+                const v4f l = *reinterpret_cast<const v4f*>(&words.lse[part + g * 2 + half * 4]);
+                const int4 sees = *reinterpret_cast<const int4*>(&words.sees[part + g * 2 + half * 4]);
+                const int32_t last[4] = {sees.x, sees.y, sees.z, sees.w};
+#pragma unroll
+                for (int c = 0; c < 2; c++)
+#pragma unroll
+                    for (int j = 0; j < 4; j++) {
+                        const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(z[c][g + j], a.scale2, -l[j]));
+                        add[c] += !masked || key + c * 32 <= last[j] ? w : 0.0f;
+                    }
+            }
+            sum[0].add(add[0]);
+            sum[1].add(add[1]);
+        };
+        const std::true_type beside;
+        const std::false_type alone;
+        v16f za[2], zb[2];  // of a tile's first and second half
+        bool pending = false, was_masked = false;
+        uint32_t buf = 0, now = 0, before = 0;
         for (uint32_t row0 = r.row0; row0 < r.row1; row0 += kTallRows, buf ^= 1) {
             wait_sent();
             __syncthreads();
-            const RowTile<D>& tile = tiles[buf];
+            const uint16_t* q = tiles[buf];
             const bool more = row0 + kTallRows < r.row1;
             if (more) {
                 read_words(row0 + kTallRows);
                 send(row0 + kTallRows, tiles[buf ^ 1]);
             }
-            const bool masked = causal && i1 + kBlockKeys - 1 > tile.sees[0];
-            if (any)
-#pragma unroll
-                for (uint32_t part = 0; part < kTallRows; part += 32) {
-                    v16f z[2] = {};
-#pragma unroll
-                    for (int d = 0; d < D / 16; d++) {
-                        const uint32_t chunk = (d * 2 + half) ^ k_swizzle<D>(lane % 32);
-                        const V q = *reinterpret_cast<const V*>(tile.q + (part + lane % 32) * D + chunk * 8);
-                        z[0] = mfma(q, k[0][d], z[0]);
-                        z[1] = mfma(q, k[1][d], z[1]);
-                    }
-                    float add[2] = {0, 0};
-#pragma unroll
-                    for (int g = 0; g < 16; g += 4) {
-                        const v4f l = *reinterpret_cast<const v4f*>(&tile.lse[part + g * 2 + half * 4]);
-                        float w[2][4];
-#pragma unroll
-                        for (int c = 0; c < 2; c++)
-#pragma unroll
-                            for (int j = 0; j < 4; j++)
-                                w[c][j] = __builtin_amdgcn_exp2f(__builtin_fmaf(z[c][g + j], a.scale2, -l[j]));
-                        if (masked) {
-                            const int4 sees = *reinterpret_cast<const int4*>(&tile.sees[part + g * 2 + half * 4]);
-                            const int32_t last[4] = {sees.x, sees.y, sees.z, sees.w};
-#pragma unroll
-                            for (int c = 0; c < 2; c++)
-#pragma unroll
-                                for (int j = 0; j < 4; j++)
-                                    w[c][j] = key + c * 32 <= last[j] ? w[c][j] : 0.0f;
-                        }
-#pragma unroll
-                        for (int j = 0; j < 4; j++) {
-                            add[0] += w[0][j];
-                            add[1] += w[1][j];
-                        }
-                    }
-                    sum[0].add(add[0]);
-                    sum[1].add(add[1]);
+            if (any) {
+                const bool masked = causal && i1 + kBlockKeys - 1 > words[now].sees[0];
+                if (pending && !was_masked) {
+                    scores_of(beside, za, q, zb, words[before], 32);
+                } else {
+                    if (pending)
+                        finish(zb, words[before], 32, true);
+                    scores_of(alone, za, q, zb, words[before], 32);
                 }
+                if (!masked) {
+                    scores_of(beside, zb, q + 32 * D, za, words[now], 0);
+                } else {
+                    finish(za, words[now], 0, true);
+                    scores_of(alone, zb, q + 32 * D, za, words[now], 0);
+                }
+                pending = true;
+                was_masked = masked;
+            }
+            before = now;
+            now = now == 2 ? 0 : now + 1;
             if (more)
-                write_words(tiles[buf ^ 1]);
+                write_words(words[now]);
         }
+        if (any)
+            finish(zb, words[before], 32, was_masked);
         const float s0 = sum[0].sum + __shfl_xor(sum[0].sum, 32), s1 = sum[1].sum + __shfl_xor(sum[1].sum, 32);
         const int64_t i = i1 + lane;
         if (i >= from && i < to)
@@ -468,7 +521,7 @@ uint32_t parts_of_rows(const dm_ctx* c, const dm_token_batch& b, uint32_t ratio,
     if (b.q_tokens <= n || (b.q_tokens - n) * ratio <= kMany || tokens * ratio <= kFewRows || blocks == 0)
         return 0;
     const uint64_t each = (last && last * n < b.q_tokens ? last * n : b.q_tokens) * ratio / n;  // rows of a sequence
-    uint64_t rows = blocks * each / (6 * c->n_cu);
+    uint64_t rows = blocks * each / (32 * c->n_cu);
     rows = (rows / kTallRows + 1) * kTallRows;
     rows = rows < 512 ? 512 : rows;
     const uint64_t most = (tokens * ratio + kParts - 1) / kParts;  // no more stretches than kParts
