@@ -425,18 +425,26 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : D == 128 ? 2 : 3) void wei
             for (int d = 0; d < kSteps; d++) {
                 if (d + 1 < kSteps)
                     read(d + 1);
-                z[0] = mfma(f[d % 2], k[0][d], z[0]);
-                z[1] = mfma(f[d % 2], k[1][d], z[1]);
-                if constexpr (decltype(with)::value) {
 #pragma unroll
-                    for (int i = d * kPer; i < (d + 1) * kPer; i++) {
-                        const int g = i / 8 * 4, c = i / 4 % 2, j = i % 4;
-                        if (i % 8 == 0)
-                            l = *reinterpret_cast<const v4f*>(&words.lse[part + g * 2 + half * 4]);
-                        add[c] += __builtin_amdgcn_exp2f(__builtin_fmaf(old[c][g + j], a.scale2, -l[j]));
+                for (int c = 0; c < 2; c++) {
+                    z[c] = mfma(f[d % 2], k[c][d], z[c]);
+                    if constexpr (decltype(with)::value) {
+                        float w[kPer / 2];
+                        if ((d * kPer + c * kPer / 2) % 8 == 0)
+                            l = *reinterpret_cast<const v4f*>(&words.lse[part + (d * kPer + c * kPer / 2) / 8 * 8 + half * 4]);
+#pragma unroll
+                        for (int i = 0; i < kPer / 2; i++) {
+                            const int at = d * kPer + c * kPer / 2 + i;
+                            w[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(old[at / 4 % 2][at / 8 * 4 + at % 4], a.scale2, -l[at % 4]));
+                        }
+#pragma unroll
+                        for (int i = 0; i < kPer / 2; i++)
+                            add[(d * kPer + c * kPer / 2 + i) / 4 % 2] += w[i];
+                        // (they would sink to where the sums are wanted, behind all products)
+                        asm volatile("" : "+v"(add[0]), "+v"(add[1]));
                     }
+                    __builtin_amdgcn_sched_barrier(0);
                 }
-                __builtin_amdgcn_sched_barrier(0);
             }
             if constexpr (decltype(with)::value) {
                 sum[0].add(add[0]);
