@@ -3,9 +3,9 @@
 //             heads x that read h, of exp(scale q_x,t . k_h,i - lse_x,t).
 //
 // Keys stay, queries pass: a wave has 64 neighbouring keys of one head in registers, as the
-// right operand of S = Q K^T on 32x32x16 matrix instructions, and takes 32 rows (token,
+// right operand of S = Q K^T on 16x16x32 matrix instructions, and takes 16 rows (token,
 // query head) at a time; a lane then holds scores of one key, so that their weights' sum over
-// the rows is a sum over its own registers.  Nothing is added by two waves, so the order of
+// the rows is a sum over its own registers and one over four lanes at the end.  Nothing is added by two waves, so the order of
 // every sum is fixed.  Blocks of 64 keys follow the tables' entries, not the sequences: a
 // lane's page is known without knowing whose it is, and a block may hold the end of one
 // sequence and the beginnings of others, which take their turns.
@@ -14,8 +14,8 @@
 // keys of a head and a stretch of rows, which pass through LDS once for its four waves; it
 // leaves its sums, and the first kernel adds a key's up.
 //
-// The pages that a run shares (as its plan has found them) are read once, by the blocks of
-// its first sequence's entries, for all its sequences, each with its own sums.
+// The pages that a run shares (as its plan has found them) are read by the blocks of every
+// eighth of its sequences, for eight of them, each with its own sums.
 //
 // Bound by reading keys where rows are few, by the exponentials where they are many.
 #include "dm_attn.h"
@@ -72,12 +72,6 @@ __device__ __forceinline__ Stretch stretch_of(const WeightsIn& a, const SeqView&
     return Stretch{row0 > s0 ? row0 : (uint32_t)s0, row1 < s1 ? row1 : (uint32_t)s1};
 }
 
-// The rows of a sequence for one KV head.
-struct Rows {
-    uint32_t tok0, ntok, first;  // first row that counts
-    int64_t pos0;
-};
-
 // What is in LDS of rows: their log-sum-exps (in powers of two), and the last key that each
 // sees.
 template <int ROWS>
@@ -99,66 +93,125 @@ struct LongSum {
     }
 };
 
-template <typename T, int D>
-__device__ __forceinline__ void weights_of(const WeightsIn& a, const Rows& s, uint32_t x0, uint32_t xs, int64_t i0,
-                                           bool causal, const typename Vec8<T>::type (&k)[2][D / 16], WordsOf<32>& words,
-                                           float (&total)[2])
+// What is known of a sequence, a lane each for 64 neighbouring ones, and then of one by all
+// lanes: its new tokens, its tokens, where they are (`at`), where what it carries is (`old`,
+// of its first `keep` tokens), its tokens that are its run's, and its run's sequences.
+struct Known {
+    uint32_t tok0, ntok, len, keep, own0, g0, g1;
+    int64_t at, old;
+};
+__device__ __forceinline__ Known known_of(const WeightsIn& a, const PlanView& pv, uint32_t s, bool there, bool& bad)
 {
-    LongSum sum[2];
+    const TokenBatch& b = a.b;
+    Known x{};
+    if (!there)
+        return x;
+    const SeqView v = sequence_view(b, s);
+    bad |= v.bad;
+    x.tok0 = v.tok0;
+    x.ntok = v.bad ? 0 : v.ntok;
+    x.len = (uint32_t)v.len;
+    x.at = b.off[s] << b.shift;
+    if (b.groups) {
+        const uint32_t g = pv.run[s];
+        if (g < b.groups) {
+            x.g0 = (uint32_t)b.group_off[g];
+            x.g1 = (uint32_t)b.group_off[g + 1];
+            x.own0 = x.ntok && x.len ? pv.unit[b.groups + s].key0 : 0;
+        }
+    }
+    if (a.prev && !a.prev_off) {
+        x.old = x.at;
+        x.keep = v.pos0 > 0 ? (uint32_t)v.pos0 : 0;
+    } else if (a.prev) {
+        const int64_t keep = a.keep[s];
+        x.keep = keep < 0 ? 0 : keep < (int64_t)x.len ? (uint32_t)keep : x.len;
+        if (x.keep) {
+            const uint32_t src = (uint32_t)a.src[s];
+            x.old = src < a.prev_n ? a.prev_off[src] << b.shift : -1;
+            if (x.old < 0 || x.old + x.keep > a.prev_room) {
+                bad = true;
+                x.keep = 0;
+            }
+        }
+    }
+    return x;
+}
+__device__ __forceinline__ uint32_t from_lane(uint32_t x, uint32_t lane) { return __builtin_amdgcn_readlane(x, lane); }
+__device__ __forceinline__ int64_t from_lane(int64_t x, uint32_t lane)
+{
+    return (int64_t)((uint64_t)from_lane((uint32_t)((uint64_t)x >> 32), lane) << 32 | from_lane((uint32_t)x, lane));
+}
+__device__ __forceinline__ Known of_lane(const Known& x, uint32_t lane)
+{
+    Known y;
+    y.tok0 = from_lane(x.tok0, lane);
+    y.ntok = from_lane(x.ntok, lane);
+    y.len = from_lane(x.len, lane);
+    y.keep = from_lane(x.keep, lane);
+    y.own0 = from_lane(x.own0, lane);
+    y.g0 = from_lane(x.g0, lane);
+    y.g1 = from_lane(x.g1, lane);
+    y.at = from_lane(x.at, lane);
+    y.old = from_lane(x.old, lane);
+    return y;
+}
+
+// Sums over the rows [row0, end) of a sequence, for the keys in a wave's registers: of key c *
+// 16 + lane % 16, a quarter of the rows a lane.
+template <typename T, int D>
+__device__ __forceinline__ void weights_of(const WeightsIn& a, const Known& s, uint32_t row0, uint32_t x0, uint32_t xs,
+                                           int64_t i0, bool causal, const typename Vec8<T>::type (&k)[4][D / 32],
+                                           WordsOf<16>& words, float (&total)[4])
+{
     using V = typename Vec8<T>::type;
-    const uint32_t lane = lane_id(), half = lane / 32;
+    LongSum sum[4];
+    const uint32_t lane = lane_id(), quarter = lane / 16;
     const uint32_t end = s.ntok * a.ratio;
-    uint32_t row0 = s.first;
-    if (causal && i0 > s.pos0 + row0 / a.ratio)
-        row0 = (uint32_t)(i0 - s.pos0) * a.ratio;
-    for (; row0 < end; row0 += 32) {
-        const uint32_t mine = row0 + lane % 32, row = mine < end ? mine : end - 1;
+    const int64_t pos0 = (int64_t)s.len - s.ntok;
+    if (causal && i0 > pos0 + row0 / a.ratio)
+        row0 = (uint32_t)(i0 - pos0) * a.ratio;
+    for (; row0 < end; row0 += 16) {
+        const uint32_t mine = row0 + lane % 16, row = mine < end ? mine : end - 1;
         const uint32_t t = row / a.ratio, x = x0 + (row - t * a.ratio) * xs;
-        const uint16_t* at = a.q + (s.tok0 + t) * a.q_stride + (uint64_t)x * D + half * 8;
-        V q[D / 16];
+        const uint16_t* at = a.q + (int64_t)(s.tok0 + t) * a.q_stride + (uint64_t)x * D + quarter * 8;
+        V q[D / 32];
 #pragma unroll
-        for (int d = 0; d < D / 16; d++)
-            q[d] = *reinterpret_cast<const V*>(at + d * 16);
+        for (int d = 0; d < D / 32; d++)
+            q[d] = *reinterpret_cast<const V*>(at + d * 32);
         const float far = a.lse[(uint64_t)(s.tok0 + t) * a.q_heads + x] * kLog2e;
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         __builtin_amdgcn_wave_barrier();
-        if (half == 0) {
+        if (quarter == 0) {
             // rows past the last and rows that see nothing add nothing
             words.lse[lane] = mine < end && far != -INFINITY ? far : INFINITY;
-            words.sees[lane] = (int32_t)(s.pos0 + t);
+            words.sees[lane] = (int32_t)(pos0 + t);
         }
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         __builtin_amdgcn_wave_barrier();
-        v16f z[2] = {};
+        const v4f l = *reinterpret_cast<const v4f*>(&words.lse[quarter * 4]);
+        const int4 sees = *reinterpret_cast<const int4*>(&words.sees[quarter * 4]);
+        const int32_t last[4] = {sees.x, sees.y, sees.z, sees.w};
+        const bool masked = causal && i0 + kBlockKeys - 1 > pos0 + row0 / a.ratio;
+        const int32_t key = (int32_t)((uint32_t)i0 + lane % 16);
 #pragma unroll
-        for (int d = 0; d < D / 16; d++) {
-            z[0] = mfma(q[d], k[0][d], z[0]);
-            z[1] = mfma(q[d], k[1][d], z[1]);
-        }
-        const bool masked = causal && i0 + kBlockKeys - 1 > s.pos0 + row0 / a.ratio;
-        const int32_t key = (int32_t)((uint32_t)i0 + lane % 32);
-        float add[2] = {0, 0};
+        for (int c = 0; c < 4; c++) {
+            v4f z = {};
 #pragma unroll
-        for (int r = 0; r < 16; r += 4) {
-            const v4f l = *reinterpret_cast<const v4f*>(&words.lse[r * 2 + half * 4]);
+            for (int d = 0; d < D / 32; d++)
+                z = mfma(q[d], k[c][d], z);
+            float add = 0;
 #pragma unroll
             for (int j = 0; j < 4; j++) {
-                float w0 = __builtin_amdgcn_exp2f(__builtin_fmaf(z[0][r + j], a.scale2, -l[j]));
-                float w1 = __builtin_amdgcn_exp2f(__builtin_fmaf(z[1][r + j], a.scale2, -l[j]));
-                if (masked) {
-                    const int32_t last = words.sees[r * 2 + half * 4 + j];
-                    w0 = key <= last ? w0 : 0.0f;
-                    w1 = key + 32 <= last ? w1 : 0.0f;
-                }
-                add[0] += w0;
-                add[1] += w1;
+                const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(z[j], a.scale2, -l[j]));
+                add += !masked || key + c * 16 <= last[j] ? w : 0.0f;
             }
+            sum[c].add(add);
         }
-        sum[0].add(add[0]);
-        sum[1].add(add[1]);
     }
-    total[0] = sum[0].sum;
-    total[1] = sum[1].sum;
+#pragma unroll
+    for (int c = 0; c < 4; c++)
+        total[c] = sum[c].sum;
 }
 
 // collect(sequence, its view, the token that slot0 would be of it, tokens [from, to) that are
@@ -192,89 +245,139 @@ __device__ __forceinline__ void each_sequence(const TokenBatch& b, const PlanVie
     }
 }
 
+// How many of a run's sequences that see a prefix come before sequence s.  By a whole wave.
+__device__ __forceinline__ uint32_t rank_in_run(const PlanView& pv, uint32_t groups, uint32_t g0, uint32_t s)
+{
+    uint32_t rank = 0;
+    for (uint32_t m0 = g0; m0 < s; m0 += kWave) {
+        const uint32_t m = m0 + lane_id();
+        bool sees = false;
+        if (m < s) {
+            const Unit& u = pv.unit[groups + m];
+            sees = u.ntok && u.key0 && u.key1;
+        }
+        rank += __popcll(ballot(sees));
+    }
+    return rank;
+}
+
+// A wave has 64 slots and a few heads one after another.  Of a run's shared keys the blocks of
+// every kShared-th sequence that sees them have those of the next ones too.
+constexpr uint32_t kShared = 8;
+
 template <typename T, int D>
-__global__ __launch_bounds__(kThreads) void weights_kernel(WeightsIn a, const PlanView pv, uint64_t items, uint32_t* status)
+__global__ __launch_bounds__(kThreads, D == 256 ? 2 : 3) void weights_kernel(WeightsIn a, const PlanView pv,
+                                                                            uint32_t heads, uint64_t items,
+                                                                            uint32_t* status)
 {
     using V = typename Vec8<T>::type;
-    __shared__ __attribute__((aligned(16))) WordsOf<32> all_words[kWaves];
+    __shared__ __attribute__((aligned(16))) WordsOf<16> all_words[kWaves];
     const TokenBatch& b = a.b;
-    const PlanHead& ph = *pv.head;
-    if (!plan_of(ph, b, a.q_heads, a.plan_heads, a.plan_dim)) {
+    const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = lane_id();
+    const uint64_t item = (uint64_t)blockIdx.x * kWaves + wave;
+    const uint32_t sets = (a.kv_heads + heads - 1) / heads, h0 = item % sets * heads;
+    const uint32_t h1 = h0 + heads < a.kv_heads ? h0 + heads : a.kv_heads;
+    const int64_t slot0 = (int64_t)(item / sets) * kBlockKeys;
+    const int64_t entry0 = slot0 >> b.shift, entry1 = (slot0 + kBlockKeys - 1) >> b.shift;
+    // the pages of the block's keys, before it is known whose they are
+    uint32_t page[4];
+#pragma unroll
+    for (int c = 0; c < 4; c++) {
+        const int64_t e = (slot0 + c * 16 + lane % 16) >> b.shift;
+        page[c] = e < b.entries ? (uint32_t)b.page[e] : 0;
+    }
+    if (!plan_of(*pv.head, b, a.q_heads, a.plan_heads, a.plan_dim)) {
         if (blockIdx.x == 0 && threadIdx.x == 0)
             atomicOr(status, kErrInval);
         return;
     }
-    const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = lane_id(), half = lane / 32;
-    const uint64_t item = (uint64_t)blockIdx.x * kWaves + wave;
     if (item >= items)
         return;
-    WordsOf<32>& words = all_words[wave];
-    const uint32_t h = item % a.kv_heads;
-    const int64_t slot0 = (int64_t)(item / a.kv_heads) * kBlockKeys;
-    const uint32_t x0 = a.paired ? h / 2 * 2 * a.ratio + h % 2 : h * a.ratio, xs = a.paired ? 2 : 1;
-    V k[2][D / 16];
-    bool bad_page[2] = {};
-    bool have = false, bad = false;
-    auto load = [&] {
-        if (have)
+    WordsOf<16>& words = all_words[wave];
+    V k[4][D / 32];
+    uint32_t loaded = 0xFFFFFFFFu;  // the head whose keys k has
+    bool bad = false;
+    auto load = [&](uint32_t h) {
+        if (loaded == h)
             return;
-        have = true;
+        loaded = h;
 #pragma unroll
-        for (int c = 0; c < 2; c++) {
-            const int64_t slot = slot0 + c * 32 + lane % 32, e = slot >> b.shift;
-            const uint32_t p = e < b.entries ? (uint32_t)b.page[e] : 0;
-            bad_page[c] = p >= a.n_pages;
-            const uint16_t* at = a.k + ((((uint64_t)(p < a.n_pages ? p : 0) * a.kv_heads + h) << b.shift) +
-                                        (slot & ((1 << b.shift) - 1))) * D + half * 8;
+        for (int c = 0; c < 4; c++) {
+            const uint32_t p = page[c] < a.n_pages ? page[c] : 0;
+            const int64_t slot = slot0 + c * 16 + lane % 16;
+            const uint16_t* at =
+                a.k + ((((uint64_t)p * a.kv_heads + h) << b.shift) + (slot & ((1 << b.shift) - 1))) * D + lane / 16 * 8;
 #pragma unroll
-            for (int d = 0; d < D / 16; d++)
-                k[c][d] = *reinterpret_cast<const V*>(at + d * 16);
+            for (int d = 0; d < D / 32; d++)
+                k[c][d] = *reinterpret_cast<const V*>(at + d * 32);
         }
     };
-    // sums of sequence s over tokens [from, to) that are in the block (token 0 is slot0 -
-    // i0), whose keys are here, to where s has them
-    auto collect = [&](uint32_t s, const SeqView& v, int64_t i0, int64_t from, int64_t to, bool causal) {
-        float sum[2] = {0, 0}, whole = 0;
+    // sums of a sequence over its tokens [from, to) that are in the block (i0: the token that
+    // slot0 would be), whose keys are here, to where the sequence has them
+    auto collect = [&](const Known& s, uint32_t h, int64_t i0, int64_t from, int64_t to, bool causal) {
+        const uint32_t x0 = a.paired ? h / 2 * 2 * a.ratio + h % 2 : h * a.ratio, xs = a.paired ? 2 : 1;
         const int64_t i = i0 + lane;
         const bool mine = i >= from && i < to;
-        if (a.parts && v.ntok && !few(a, v)) {
+        float carried = 0;
+        if (mine && i < s.keep)
+            carried = a.decay * a.prev[(int64_t)h * a.prev_stride + s.old + i];
+        float sum = 0;
+        const uint32_t first = (a.last && a.last < s.ntok ? s.ntok - a.last : 0) * a.ratio;
+        if (a.parts && s.ntok * a.ratio - first > kFewRows) {
             // (the tall block begins before this one, in the same sequence's numbers)
-            const int64_t tall0 = i0 - (slot0 & (kTallKeys - 1)), at = (b.off[s] << b.shift) + i;
+            SeqView v{0, (int64_t)s.len, (int64_t)s.len - s.ntok, s.tok0, s.ntok, false};
+            const int64_t tall0 = i0 - (slot0 & (kTallKeys - 1));
             for (uint32_t p = 0; p < a.parts; p++) {
                 const Stretch r = stretch_of(a, v, tall0, causal, p);
                 if (mine && r.row0 < r.row1)
-                    whole += a.part[((uint64_t)p * a.kv_heads + h) * a.slots + at];
+                    sum += a.part[((uint64_t)p * a.kv_heads + h) * a.slots + s.at + i];
             }
-        } else if (v.ntok) {
-            load();
-            const bool key[2] = {i0 + lane % 32 >= from && i0 + lane % 32 < to,
-                                 i0 + 32 + lane % 32 >= from && i0 + 32 + lane % 32 < to};
-            bad |= (key[0] && bad_page[0]) || (key[1] && bad_page[1]);
-            Rows r{v.tok0, v.ntok, first_row(a, v), v.pos0};
-            weights_of<T, D>(a, r, x0, xs, i0, causal, k, words, sum);
-        }
-        sum[0] += __shfl_xor(sum[0], 32);
-        sum[1] += __shfl_xor(sum[1], 32);
-        float w = (half ? sum[1] : sum[0]) + whole;
-        if (!mine)
-            return;
-        const int64_t at = (v.off << b.shift) + i;
-        if (a.prev) {
-            if (!a.prev_off) {
-                if (i < v.pos0)
-                    w = __builtin_fmaf(a.decay, a.prev[(int64_t)h * a.prev_stride + at], w);
-            } else if (i < a.keep[s]) {
-                const uint32_t from_s = (uint32_t)a.src[s];
-                const int64_t old = from_s < a.prev_n ? (a.prev_off[from_s] << b.shift) + i : -1;
-                if (old >= 0 && old < a.prev_room)
-                    w = __builtin_fmaf(a.decay, a.prev[(int64_t)h * a.prev_stride + old], w);
-                else
-                    bad = true;
+        } else if (s.ntok) {
+            load(h);
+            float part[4];
+            weights_of<T, D>(a, s, first, x0, xs, i0, causal, k, words, part);
+#pragma unroll
+            for (int c = 0; c < 4; c++) {
+                part[c] += __shfl_xor(part[c], 16);
+                part[c] += __shfl_xor(part[c], 32);
+                sum = lane / 16 == (uint32_t)c ? part[c] : sum;
             }
         }
-        a.w[(int64_t)h * a.w_stride + at] = w;
+        if (s.ntok)
+#pragma unroll
+            for (int c = 0; c < 4; c++) {
+                const int64_t key = i0 + c * 16 + lane % 16;
+                bad |= key >= from && key < to && page[c] >= a.n_pages;
+            }
+        if (mine)
+            a.w[(int64_t)h * a.w_stride + s.at + i] = carried + sum;
     };
-    each_sequence(b, pv, slot0, kBlockKeys, bad, collect);
+    // the sequences in the block, 64 looked at a time
+    for (uint32_t s0 = wave_find(b.off, b.n, 1, entry0); s0 < b.n; s0 += kWave) {
+        const uint32_t s = s0 + lane;
+        const bool in = s < b.n && b.off[s] <= entry1;
+        const Known all = known_of(a, pv, s, in, bad);
+        for (uint64_t left = ballot(in); left; left &= left - 1) {
+            const uint32_t j = (uint32_t)__builtin_ctzll(left);
+            const Known x = of_lane(all, j);
+            const int64_t i0 = slot0 - x.at;
+            if (x.own0 && i0 < (int64_t)x.own0 && rank_in_run(pv, b.groups, x.g0, s0 + j) % kShared == 0) {
+                const uint32_t m = s0 + j + lane;
+                const Known of = known_of(a, pv, m, m < x.g1 && m < b.n, bad);
+                uint64_t those = ballot(of.own0 != 0);
+                for (uint32_t h = h0; h < h1; h++) {
+                    uint64_t next = those;
+                    for (uint32_t turn = 0; next && turn < kShared; turn++, next &= next - 1)
+                        collect(of_lane(of, (uint32_t)__builtin_ctzll(next)), h, i0, 0, x.own0, false);
+                }
+            }
+            if (x.len > x.own0 && i0 < (int64_t)x.len && i0 + (int64_t)kBlockKeys > (int64_t)x.own0)
+                for (uint32_t h = h0; h < h1; h++)
+                    collect(x, h, i0, x.own0, x.len, true);
+        }
+        if (!__all(in))
+            break;
+    }
     if (bad)
         atomicOr(status, kErrInval);
 }
@@ -573,12 +676,16 @@ hipError_t attn_weights(dm_ctx* c, const dm_token_batch& b, const dm_kv_pages& k
     a.decay = g.decay;
     const PlanView pv = plan_view(const_cast<void*>(plan), b.tables.n, b.groups);
     const uint64_t slots = b.tables.entries * c->cfg.block_size;
-    const uint64_t items = (slots + kBlockKeys - 1) / kBlockKeys * kv.kv_heads, grid = (items + kWaves - 1) / kWaves;
-    if (grid > 0x7FFFFFFFull)
-        return hipErrorInvalidValue;
-    if (grid == 0)
+    if (slots == 0)
         return hipSuccess;
     a.slots = (int64_t)slots;
+    // heads of a wave: one, or as many as leave some 16 waves a SIMD
+    uint64_t heads = slots / kBlockKeys * kv.kv_heads / (64 * c->n_cu);
+    heads = heads < 1 ? 1 : heads > kv.kv_heads ? kv.kv_heads : heads;
+    const uint64_t items = (slots + kBlockKeys - 1) / kBlockKeys * ((kv.kv_heads + heads - 1) / heads);
+    const uint64_t grid = (items + kWaves - 1) / kWaves;
+    if (grid > 0x7FFFFFFFull)
+        return hipErrorInvalidValue;
     const uint32_t blocks = (uint32_t)((slots + kTallKeys - 1) / kTallKeys);
     a.parts = parts_of_rows(c, b, a.ratio, g.last, (uint64_t)blocks * kv.kv_heads, &a.part_rows);
     a.part = nullptr;
@@ -594,7 +701,7 @@ hipError_t attn_weights(dm_ctx* c, const dm_token_batch& b, const dm_kv_pages& k
         if (a.parts)
             weights_tall_kernel<T, D>
                 <<<a.parts * blocks * kv.kv_heads, kThreads, 0, c->stream>>>(a, pv, blocks, c->d_status);
-        weights_kernel<T, D><<<(uint32_t)grid, kThreads, 0, c->stream>>>(a, pv, items, c->d_status);
+        weights_kernel<T, D><<<(uint32_t)grid, kThreads, 0, c->stream>>>(a, pv, (uint32_t)heads, items, c->d_status);
     });
     return hipGetLastError();
 }
