@@ -15,7 +15,8 @@
 // leaves its sums, and the first kernel adds a key's up.
 //
 // The pages that a run shares (as its plan has found them) are read by the blocks of every
-// eighth of its sequences, for eight of them, each with its own sums.
+// sixteenth of its sequences, for sixteen of them, each with its own sums; a few rows each,
+// several of them have one product.
 //
 // Bound by reading keys where rows are few, by the exponentials where they are many.
 #include "dm_attn.h"
@@ -100,9 +101,9 @@ struct Known {
     uint32_t tok0, ntok, len, keep, own0, g0, g1;
     int64_t at, old;
 };
-__device__ __forceinline__ Known known_of(const WeightsIn& a, const PlanView& pv, uint32_t s, bool there, bool& bad)
+template <bool RUNS>
+__device__ __forceinline__ Known known_of(const TokenBatch& b, const PlanView& pv, uint32_t s, bool there, bool& bad)
 {
-    const TokenBatch& b = a.b;
     Known x{};
     if (!there)
         return x;
@@ -112,7 +113,7 @@ __device__ __forceinline__ Known known_of(const WeightsIn& a, const PlanView& pv
     x.ntok = v.bad ? 0 : v.ntok;
     x.len = (uint32_t)v.len;
     x.at = b.off[s] << b.shift;
-    if (b.groups) {
+    if (RUNS) {
         const uint32_t g = pv.run[s];
         if (g < b.groups) {
             x.g0 = (uint32_t)b.group_off[g];
@@ -120,23 +121,75 @@ __device__ __forceinline__ Known known_of(const WeightsIn& a, const PlanView& pv
             x.own0 = x.ntok && x.len ? pv.unit[b.groups + s].key0 : 0;
         }
     }
-    if (a.prev && !a.prev_off) {
+    return x;
+}
+// What it carries.
+__device__ __forceinline__ void add_carried(const WeightsIn& a, uint32_t s, bool there, Known& x, bool& bad)
+{
+    if (!a.prev || !there)
+        return;
+    if (!a.prev_off) {
         x.old = x.at;
-        x.keep = v.pos0 > 0 ? (uint32_t)v.pos0 : 0;
-    } else if (a.prev) {
+        x.keep = x.len > x.ntok ? x.len - x.ntok : 0;
+    } else {
         const int64_t keep = a.keep[s];
         x.keep = keep < 0 ? 0 : keep < (int64_t)x.len ? (uint32_t)keep : x.len;
         if (x.keep) {
             const uint32_t src = (uint32_t)a.src[s];
-            x.old = src < a.prev_n ? a.prev_off[src] << b.shift : -1;
+            x.old = src < a.prev_n ? a.prev_off[src] << a.b.shift : -1;
             if (x.old < 0 || x.old + x.keep > a.prev_room) {
                 bad = true;
                 x.keep = 0;
             }
         }
     }
-    return x;
 }
+// Sums for sequences with up to ROWS rows each (4, 8 or 16), 16 / ROWS of them in one product:
+// a lane has in sum[c] key c * 16 + lane % 16's of the sequence that has its quarter of the
+// rows.  member(n): the lane of `of` that has the n-th sequence.
+template <typename T, int D, int ROWS, typename Member>
+__device__ __forceinline__ void packed_weights(const WeightsIn& a, const Known& of, uint32_t n0, uint32_t count,
+                                               Member&& member, uint32_t x0, uint32_t xs,
+                                               const typename Vec8<T>::type (&k)[4][D / 32], WordsOf<16>& words,
+                                               float (&sum)[4])
+{
+    using V = typename Vec8<T>::type;
+    const uint32_t lane = lane_id(), quarter = lane / 16, n = n0 + lane % 16 / ROWS, r = lane % ROWS;
+    const uint32_t from = member(n < count ? n : n0);
+    const uint32_t tok0 = __shfl(of.tok0, from), ntok = __shfl(of.ntok, from);
+    const uint32_t first = a.last && a.last < ntok ? ntok - a.last : 0, rows = (ntok - first) * a.ratio;
+    const bool there = n < count && r < rows;
+    const uint32_t row = there ? r : 0, t = first + row / a.ratio, x = x0 + row % a.ratio * xs;
+    const uint16_t* at = a.q + (int64_t)(tok0 + t) * a.q_stride + (uint64_t)x * D + quarter * 8;
+    V q[D / 32];
+#pragma unroll
+    for (int d = 0; d < D / 32; d++)
+        q[d] = *reinterpret_cast<const V*>(at + d * 32);
+    const float far = a.lse[(uint64_t)(tok0 + t) * a.q_heads + x] * kLog2e;
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    if (quarter == 0)
+        words.lse[lane] = there && far != -INFINITY ? far : INFINITY;
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    const v4f l = *reinterpret_cast<const v4f*>(&words.lse[quarter * 4]);
+#pragma unroll
+    for (int c = 0; c < 4; c++) {
+        v4f z = {};
+#pragma unroll
+        for (int d = 0; d < D / 32; d++)
+            z = mfma(q[d], k[c][d], z);
+        sum[c] = 0;
+#pragma unroll
+        for (int j = 0; j < 4; j++)
+            sum[c] += __builtin_amdgcn_exp2f(__builtin_fmaf(z[j], a.scale2, -l[j]));
+        if (ROWS > 4)
+            sum[c] += __shfl_xor(sum[c], 16);
+        if (ROWS > 8)
+            sum[c] += __shfl_xor(sum[c], 32);
+    }
+}
+
 __device__ __forceinline__ uint32_t from_lane(uint32_t x, uint32_t lane) { return __builtin_amdgcn_readlane(x, lane); }
 __device__ __forceinline__ int64_t from_lane(int64_t x, uint32_t lane)
 {
@@ -263,15 +316,17 @@ __device__ __forceinline__ uint32_t rank_in_run(const PlanView& pv, uint32_t gro
 
 // A wave has 64 slots and a few heads one after another.  Of a run's shared keys the blocks of
 // every kShared-th sequence that sees them have those of the next ones too.
-constexpr uint32_t kShared = 8;
+constexpr uint32_t kShared = 16;
 
-template <typename T, int D>
-__global__ __launch_bounds__(kThreads, D == 256 ? 2 : 3) void weights_kernel(WeightsIn a, const PlanView pv,
+// RUNS: the batch has runs (a kernel of its own: its registers would halve the other's waves).
+template <typename T, int D, bool RUNS>
+__global__ __launch_bounds__(kThreads, D == 256 ? (RUNS ? 1 : 2) : RUNS && D == 128 ? 2 : 3) void weights_kernel(WeightsIn a, const PlanView pv,
                                                                             uint32_t heads, uint64_t items,
                                                                             uint32_t* status)
 {
     using V = typename Vec8<T>::type;
     __shared__ __attribute__((aligned(16))) WordsOf<16> all_words[kWaves];
+    __shared__ uint32_t members[kWaves][kShared];  // lanes of a run's sequences
     const TokenBatch& b = a.b;
     const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = lane_id();
     const uint64_t item = (uint64_t)blockIdx.x * kWaves + wave;
@@ -352,28 +407,93 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 2 : 3) void weights_kernel(Wei
         if (mine)
             a.w[(int64_t)h * a.w_stride + s.at + i] = carried + sum;
     };
+    // The shared tokens in the block, those of sequence x, for kShared of its run's sequences
+    // that see them from s0 on; of 64 neighbouring sequences at a time, `taken` before.
+    auto share = [&](uint32_t s0, const Known& x, uint32_t taken) -> uint32_t {
+        const uint32_t m = s0 + lane;
+        Known of = known_of<RUNS>(b, pv, m, m < x.g1 && m < b.n, bad);
+        uint64_t those = ballot(of.own0 != 0);
+        const uint32_t rank = __popcll(those & ((1ull << lane) - 1));
+        const bool in = of.own0 && rank + taken < kShared;
+        those = ballot(in);
+        const uint32_t count = __popcll(those);
+        if (count == 0)
+            return 0;
+        add_carried(a, m, in, of, bad);
+        const uint32_t rows = (a.last && a.last < of.ntok ? a.last : of.ntok) * a.ratio;
+        const int64_t i0 = slot0 - x.at;
+        if (__any(in && rows > 16)) {
+            for (uint32_t h = h0; h < h1; h++)
+                for (uint64_t next = those; next; next &= next - 1)
+                    collect(of_lane(of, (uint32_t)__builtin_ctzll(next)), h, i0, 0, x.own0, false);
+            return count;
+        }
+        __builtin_amdgcn_wave_barrier();
+        if (in)
+            members[wave][rank] = lane;
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+        auto member = [&](uint32_t n) { return members[wave][n]; };
+        auto packed = [&](auto size) {
+            constexpr int kRows = decltype(size)::value;
+            for (uint32_t h = h0; h < h1; h++) {
+                const uint32_t x0 = a.paired ? h / 2 * 2 * a.ratio + h % 2 : h * a.ratio, xs = a.paired ? 2 : 1;
+                load(h);
+                for (uint32_t n0 = 0; n0 < count; n0 += 16 / kRows) {
+                    const uint32_t n = n0 + lane / 16 * 4 / kRows, from = member(n < count ? n : n0);
+                    const bool writes = n < count && lane / 16 * 4 % kRows == 0;
+                    const int64_t at = __shfl((long long)of.at, from), old = __shfl((long long)of.old, from);
+                    const uint32_t keep = __shfl(of.keep, from);
+                    float carried[4], sum[4];
+#pragma unroll
+                    for (int c = 0; c < 4; c++) {
+                        const int64_t i = i0 + c * 16 + lane % 16;
+                        carried[c] = writes && i >= 0 && i < keep ? a.decay * a.prev[(int64_t)h * a.prev_stride + old + i] : 0.0f;
+                    }
+                    packed_weights<T, D, kRows>(a, of, n0, count, member, x0, xs, k, words, sum);
+#pragma unroll
+                    for (int c = 0; c < 4; c++) {
+                        const int64_t i = i0 + c * 16 + lane % 16;
+                        if (writes && i >= 0 && i < x.own0)
+                            a.w[(int64_t)h * a.w_stride + at + i] = carried[c] + sum[c];
+                    }
+                }
+            }
+        };
+        if (!__any(in && rows > 4))
+            packed(std::integral_constant<int, 4>{});
+        else if (!__any(in && rows > 8))
+            packed(std::integral_constant<int, 8>{});
+        else
+            packed(std::integral_constant<int, 16>{});
+#pragma unroll
+        for (int c = 0; c < 4; c++) {
+            const int64_t key = i0 + c * 16 + lane % 16;
+            bad |= key >= 0 && key < x.own0 && page[c] >= a.n_pages;
+        }
+        return count;
+    };
     // the sequences in the block, 64 looked at a time
     for (uint32_t s0 = wave_find(b.off, b.n, 1, entry0); s0 < b.n; s0 += kWave) {
         const uint32_t s = s0 + lane;
         const bool in = s < b.n && b.off[s] <= entry1;
-        const Known all = known_of(a, pv, s, in, bad);
-        for (uint64_t left = ballot(in); left; left &= left - 1) {
+        Known all = known_of<RUNS>(b, pv, s, in, bad);
+        const bool own = in && all.len > all.own0 && slot0 - all.at < (int64_t)all.len &&
+                         slot0 - all.at + (int64_t)kBlockKeys > (int64_t)all.own0;
+        add_carried(a, s, own, all, bad);
+        for (uint64_t left = ballot(own); left; left &= left - 1) {
+            const Known x = of_lane(all, (uint32_t)__builtin_ctzll(left));
+            for (uint32_t h = h0; h < h1; h++)
+                collect(x, h, slot0 - x.at, x.own0, x.len, true);
+        }
+        // a run's shared tokens
+        for (uint64_t left = !RUNS ? 0 : ballot(in && all.own0 && slot0 - all.at < (int64_t)all.own0); left; left &= left - 1) {
             const uint32_t j = (uint32_t)__builtin_ctzll(left);
             const Known x = of_lane(all, j);
-            const int64_t i0 = slot0 - x.at;
-            if (x.own0 && i0 < (int64_t)x.own0 && rank_in_run(pv, b.groups, x.g0, s0 + j) % kShared == 0) {
-                const uint32_t m = s0 + j + lane;
-                const Known of = known_of(a, pv, m, m < x.g1 && m < b.n, bad);
-                uint64_t those = ballot(of.own0 != 0);
-                for (uint32_t h = h0; h < h1; h++) {
-                    uint64_t next = those;
-                    for (uint32_t turn = 0; next && turn < kShared; turn++, next &= next - 1)
-                        collect(of_lane(of, (uint32_t)__builtin_ctzll(next)), h, i0, 0, x.own0, false);
-                }
-            }
-            if (x.len > x.own0 && i0 < (int64_t)x.len && i0 + (int64_t)kBlockKeys > (int64_t)x.own0)
-                for (uint32_t h = h0; h < h1; h++)
-                    collect(x, h, i0, x.own0, x.len, true);
+            if constexpr (RUNS)
+                if (rank_in_run(pv, b.groups, x.g0, s0 + j) % kShared == 0)
+                    for (uint32_t m0 = s0 + j, taken = 0; m0 < x.g1 && taken < kShared; m0 += kWave)
+                        taken += share(m0, x, taken);
         }
         if (!__all(in))
             break;
@@ -680,7 +800,7 @@ hipError_t attn_weights(dm_ctx* c, const dm_token_batch& b, const dm_kv_pages& k
         return hipSuccess;
     a.slots = (int64_t)slots;
     // heads of a wave: one, or as many as leave some 16 waves a SIMD
-    uint64_t heads = slots / kBlockKeys * kv.kv_heads / (64 * c->n_cu);
+    uint64_t heads = slots / kBlockKeys * kv.kv_heads / (32 * c->n_cu);
     heads = heads < 1 ? 1 : heads > kv.kv_heads ? kv.kv_heads : heads;
     const uint64_t items = (slots + kBlockKeys - 1) / kBlockKeys * ((kv.kv_heads + heads - 1) / heads);
     const uint64_t grid = (items + kWaves - 1) / kWaves;
@@ -701,7 +821,10 @@ hipError_t attn_weights(dm_ctx* c, const dm_token_batch& b, const dm_kv_pages& k
         if (a.parts)
             weights_tall_kernel<T, D>
                 <<<a.parts * blocks * kv.kv_heads, kThreads, 0, c->stream>>>(a, pv, blocks, c->d_status);
-        weights_kernel<T, D><<<(uint32_t)grid, kThreads, 0, c->stream>>>(a, pv, (uint32_t)heads, items, c->d_status);
+        if (b.groups)
+            weights_kernel<T, D, true><<<(uint32_t)grid, kThreads, 0, c->stream>>>(a, pv, (uint32_t)heads, items, c->d_status);
+        else
+            weights_kernel<T, D, false><<<(uint32_t)grid, kThreads, 0, c->stream>>>(a, pv, (uint32_t)heads, items, c->d_status);
     });
     return hipGetLastError();
 }
