@@ -15,7 +15,7 @@
 // leaves its sums, and the first kernel adds a key's up.
 //
 // The pages that a run shares (as its plan has found them) are read by the blocks of every
-// sixteenth of its sequences, for sixteen of them, each with its own sums; a few rows each,
+// fourth of its sequences, for four of them, each with its own sums; a few rows each,
 // several of them have one product.
 //
 // Bound by reading keys where rows are few, by the exponentials where they are many.
@@ -316,7 +316,7 @@ __device__ __forceinline__ uint32_t rank_in_run(const PlanView& pv, uint32_t gro
 
 // A wave has 64 slots and a few heads one after another.  Of a run's shared keys the blocks of
 // every kShared-th sequence that sees them have those of the next ones too.
-constexpr uint32_t kShared = 16;
+constexpr uint32_t kShared = 4;
 
 // RUNS: the batch has runs (a kernel of its own: its registers would halve the other's waves).
 template <typename T, int D, bool RUNS>
