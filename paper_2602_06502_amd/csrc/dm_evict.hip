@@ -56,28 +56,26 @@ __device__ __forceinline__ uint32_t digit_mask(int d) { return d == 2 ? 1023 : 2
 
 template <int WAVES>
 struct SelectLds {
-    uint32_t bins[kBins];
+    uint32_t bins[2][kBins];  // one is cleared while the other is looked at
     uint32_t above[WAVES];  // of a wave's bins, then of its scores
     uint32_t equal[WAVES];
     uint32_t digit, left;
 };
 
-// The choice among the n scores key(i), of which k < n stay: each wave takes a stretch of
-// them, R times 64 (kept in registers) or, R = 0, as many as it has to, read again each time.
-template <int WAVES, int R, typename Key>
+// The choice among n scores, of which k < n stay: each wave takes a stretch of them, R times
+// 64 (kept in registers) or, R = 0, as many as it has to, read again each time.  keys(i, x):
+// x[r] = score i + 64 r, any number where there is none.
+template <int WAVES, int R, typename Keys>
 __device__ __forceinline__ void choose(SelectLds<WAVES>& lds, uint32_t n, uint32_t k, int32_t first, int32_t* out,
-                                       Key&& key)
+                                       Keys&& keys)
 {
     const uint32_t tid = threadIdx.x, wave = tid / kWave, lane = lane_id();
     const uint32_t steps = R ? R : ((n + WAVES * kWave - 1) / (WAVES * kWave));
     const uint32_t begin = wave * steps * kWave + lane;
     uint32_t mine[R ? R : 1];
     auto at = [&](uint32_t r) { return begin + r * kWave; };
-    if constexpr (R > 0) {
-#pragma unroll
-        for (int r = 0; r < R; r++)
-            mine[r] = at(r) < n ? key(at(r)) : 0;
-    }
+    if constexpr (R > 0)
+        keys(begin, mine);
     // f(score, is there one), step by step
     auto each = [&](auto&& f) {
         if constexpr (R > 0) {
@@ -85,20 +83,29 @@ __device__ __forceinline__ void choose(SelectLds<WAVES>& lds, uint32_t n, uint32
             for (int r = 0; r < R; r++)
                 f(mine[r], at(r) < n, at(r));
         } else {
-            for (uint32_t r = 0; r < steps; r++)
-                f(at(r) < n ? key(at(r)) : 0, at(r) < n, at(r));
+            // several reads at once: one at a time, 73,000 scores of two heads each took 54 us a pass
+            constexpr uint32_t kAtOnce = 16;
+            for (uint32_t r0 = 0; r0 < steps; r0 += kAtOnce) {
+                uint32_t x[kAtOnce];
+                keys(at(r0), x);
+#pragma unroll
+                for (uint32_t r = 0; r < kAtOnce; r++)
+                    if (r0 + r < steps)
+                        f(x[r], at(r0 + r) < n, at(r0 + r));
+            }
         }
     };
+    for (uint32_t b = tid; b < 2 * kBins; b += WAVES * kWave)
+        lds.bins[0][b] = 0;
+    __syncthreads();
     uint32_t found = 0, known = 0;  // the digits found, and their bits
     uint32_t left = k;              // to be found among those that agree with them
     for (int d = 0; d < kDigits; d++) {
         const uint32_t shift = digit_shift(d), mask = digit_mask(d);
-        for (uint32_t b = tid; b < kBins; b += WAVES * kWave)
-            lds.bins[b] = 0;
-        __syncthreads();
+        uint32_t* bins = lds.bins[d % 2];
         each([&](uint32_t x, bool there, uint32_t) {
             if (there && (x & known) == found)
-                atomicAdd(&lds.bins[(x >> shift) & mask], 1u);
+                atomicAdd(&bins[(x >> shift) & mask], 1u);
         });
         __syncthreads();
         // the bin that the left-th from the top is in; a thread has neighbouring bins
@@ -107,7 +114,7 @@ __device__ __forceinline__ void choose(SelectLds<WAVES>& lds, uint32_t n, uint32
         uint32_t own = 0;
 #pragma unroll
         for (uint32_t b = 0; b < kPer; b++)
-            own += lds.bins[top - b];
+            own += bins[top - b];
         const uint32_t upto = (uint32_t)wave_incl_sum_u64(own, 0);
         if (lane == kWave - 1)
             lds.above[wave] = upto;
@@ -117,7 +124,7 @@ __device__ __forceinline__ void choose(SelectLds<WAVES>& lds, uint32_t n, uint32
             before += lds.above[w];
         if (before < left && left <= before + own) {
             uint32_t b = top, x;
-            while (before + (x = lds.bins[b]) < left) {
+            while (before + (x = bins[b]) < left) {
                 before += x;
                 b--;
             }
@@ -128,7 +135,9 @@ __device__ __forceinline__ void choose(SelectLds<WAVES>& lds, uint32_t n, uint32
         found |= lds.digit << shift;
         known |= mask << shift;
         left = lds.left;
-        __syncthreads();
+        if (d == 0)  // for the third digit
+            for (uint32_t b = tid; b < kBins; b += WAVES * kWave)
+                bins[b] = 0;
     }
     // found is the k-th largest; `left` of its equals stay.  Places of each wave's.
     uint32_t above = 0, equal = 0;
@@ -191,19 +200,30 @@ __global__ __launch_bounds__(THREADS) void select_kernel(SelectIn a, uint32_t* s
         out[first + k + i] = (int32_t)(len - tail + i);
     if (k == 0)
         return;
-    auto key = [&](uint32_t i) {
-        const float* from = w + first + i;
-        float sum = *from;
-        for (uint32_t g = 1; g < a.share; g++)
-            sum += from[g * a.w_stride];
-        return ordered(sum);
+    // (head by head, so that reads need not wait for one another)
+    auto keys = [&](uint32_t i, auto& x) {
+        constexpr int kMany = sizeof(x) / sizeof(x[0]);
+        float sum[kMany];
+        for (uint32_t g = 0; g < a.share; g++) {
+            const float* from = w + first + g * a.w_stride;
+            float one[kMany];
+#pragma unroll
+            for (int r = 0; r < kMany; r++)
+                one[r] = i + r * kWave < n ? from[i + r * kWave] : 0.0f;
+#pragma unroll
+            for (int r = 0; r < kMany; r++)
+                sum[r] = g ? sum[r] + one[r] : one[r];
+        }
+#pragma unroll
+        for (int r = 0; r < kMany; r++)
+            x[r] = ordered(sum[r]);
     };
     if (n <= THREADS * 4)
-        choose<kW, 4>(lds, n, k, (int32_t)first, out + first, key);
+        choose<kW, 4>(lds, n, k, (int32_t)first, out + first, keys);
     else if (n <= THREADS * 16)
-        choose<kW, 16>(lds, n, k, (int32_t)first, out + first, key);
+        choose<kW, 16>(lds, n, k, (int32_t)first, out + first, keys);
     else
-        choose<kW, 0>(lds, n, k, (int32_t)first, out + first, key);
+        choose<kW, 0>(lds, n, k, (int32_t)first, out + first, keys);
 }
 
 struct GatherIn {
@@ -344,8 +364,11 @@ hipError_t evict_select(dm_ctx* c, const dm_page_tables& t, const dm_select_args
     const uint64_t grid = t.n * a.layers * a.choices;
     if (grid > 0x7FFFFFFFull)
         return hipErrorInvalidValue;
-    if (t.entries * c->cfg.block_size / t.n <= 2048)
+    const uint64_t mean = t.entries * c->cfg.block_size / t.n;
+    if (mean <= 2048)
         select_kernel<256><<<(uint32_t)grid, 256, 0, c->stream>>>(a, c->d_status);
+    else if (mean <= 6144)
+        select_kernel<512><<<(uint32_t)grid, 512, 0, c->stream>>>(a, c->d_status);
     else
         select_kernel<1024><<<(uint32_t)grid, 1024, 0, c->stream>>>(a, c->d_status);
     return hipGetLastError();
