@@ -58,42 +58,57 @@ template <int WAVES>
 struct SelectLds {
     uint32_t bins[2][kBins];  // one is cleared while the other is looked at
     uint32_t above[WAVES];  // of a wave's bins, then of its scores
-    uint32_t equal[WAVES];
-    uint32_t digit, left;
+    uint32_t equal[WAVES], up[WAVES];
+    uint32_t digit, left, held;
 };
 
+// The bin that the left-th score from the top is in, among those counted in bins: its number to
+// lds.digit, the scores to be found in it to lds.left.  A thread has neighbouring bins.
+template <int WAVES>
+__device__ __forceinline__ void find_bin(SelectLds<WAVES>& lds, const uint32_t* bins, uint32_t left)
+{
+    const uint32_t tid = threadIdx.x, wave = tid / kWave;
+    constexpr uint32_t kPer = kBins / (WAVES * kWave) ? kBins / (WAVES * kWave) : 1;
+    const uint32_t top = kBins - 1 - tid * kPer;
+    uint32_t own = 0;
+#pragma unroll
+    for (uint32_t b = 0; b < kPer; b++)
+        own += bins[top - b];
+    const uint32_t upto = (uint32_t)wave_incl_sum_u64(own, 0);
+    if (lane_id() == kWave - 1)
+        lds.above[wave] = upto;
+    __syncthreads();
+    uint32_t before = upto - own;
+    for (uint32_t w = 0; w < wave; w++)
+        before += lds.above[w];
+    if (before < left && left <= before + own) {
+        uint32_t b = top, x;
+        while (before + (x = bins[b]) < left) {
+            before += x;
+            b--;
+        }
+        lds.digit = b;
+        lds.left = left - before;
+    }
+    __syncthreads();
+}
+
 // The choice among n scores, of which k < n stay: each wave takes a stretch of them, R times
-// 64 (kept in registers) or, R = 0, as many as it has to, read again each time.  keys(i, x):
-// x[r] = score i + 64 r, any number where there is none.
+// 64, kept in registers.  keys(i, x): x[r] = score i + 64 r, any number where there is none.
 template <int WAVES, int R, typename Keys>
 __device__ __forceinline__ void choose(SelectLds<WAVES>& lds, uint32_t n, uint32_t k, int32_t first, int32_t* out,
                                        Keys&& keys)
 {
     const uint32_t tid = threadIdx.x, wave = tid / kWave, lane = lane_id();
-    const uint32_t steps = R ? R : ((n + WAVES * kWave - 1) / (WAVES * kWave));
-    const uint32_t begin = wave * steps * kWave + lane;
-    uint32_t mine[R ? R : 1];
+    const uint32_t begin = wave * R * kWave + lane;
+    uint32_t mine[R];
     auto at = [&](uint32_t r) { return begin + r * kWave; };
-    if constexpr (R > 0)
-        keys(begin, mine);
-    // f(score, is there one), step by step
+    keys(begin, mine);
+    // f(score, is there one, its place), step by step
     auto each = [&](auto&& f) {
-        if constexpr (R > 0) {
 #pragma unroll
-            for (int r = 0; r < R; r++)
-                f(mine[r], at(r) < n, at(r));
-        } else {
-            // several reads at once: one at a time, 73,000 scores of two heads each took 54 us a pass
-            constexpr uint32_t kAtOnce = 16;
-            for (uint32_t r0 = 0; r0 < steps; r0 += kAtOnce) {
-                uint32_t x[kAtOnce];
-                keys(at(r0), x);
-#pragma unroll
-                for (uint32_t r = 0; r < kAtOnce; r++)
-                    if (r0 + r < steps)
-                        f(x[r], at(r0 + r) < n, at(r0 + r));
-            }
-        }
+        for (int r = 0; r < R; r++)
+            f(mine[r], at(r) < n, at(r));
     };
     for (uint32_t b = tid; b < 2 * kBins; b += WAVES * kWave)
         lds.bins[0][b] = 0;
@@ -108,30 +123,7 @@ __device__ __forceinline__ void choose(SelectLds<WAVES>& lds, uint32_t n, uint32
                 atomicAdd(&bins[(x >> shift) & mask], 1u);
         });
         __syncthreads();
-        // the bin that the left-th from the top is in; a thread has neighbouring bins
-        constexpr uint32_t kPer = kBins / (WAVES * kWave) ? kBins / (WAVES * kWave) : 1;
-        const uint32_t top = kBins - 1 - tid * kPer;
-        uint32_t own = 0;
-#pragma unroll
-        for (uint32_t b = 0; b < kPer; b++)
-            own += bins[top - b];
-        const uint32_t upto = (uint32_t)wave_incl_sum_u64(own, 0);
-        if (lane == kWave - 1)
-            lds.above[wave] = upto;
-        __syncthreads();
-        uint32_t before = upto - own;
-        for (uint32_t w = 0; w < wave; w++)
-            before += lds.above[w];
-        if (before < left && left <= before + own) {
-            uint32_t b = top, x;
-            while (before + (x = bins[b]) < left) {
-                before += x;
-                b--;
-            }
-            lds.digit = b;
-            lds.left = left - before;
-        }
-        __syncthreads();
+        find_bin(lds, bins, left);
         found |= lds.digit << shift;
         known |= mask << shift;
         left = lds.left;
@@ -169,11 +161,159 @@ __device__ __forceinline__ void choose(SelectLds<WAVES>& lds, uint32_t n, uint32
     });
 }
 
+// More of them: read three times.  First for the highest digit; then for the scores that agree
+// with it, of which LDS has room for kCandidates (where they are more, the other digits take a
+// pass each) and how many are above them; then for the places.  A lane reads 16 bytes of
+// scores at a time, kAtOnce times before the first is looked at: the reads of one workgroup
+// are what bounds this (131,072 scores of two heads a choice, 128 choices: 160 us with 4 bytes
+// and five passes).  keys4(i, x): x[4 u + j] = score i + 256 u + j.
+template <int WAVES>
+constexpr uint32_t kCandidates = WAVES * 512;
+template <int WAVES, uint32_t kAtOnce, typename Keys4>
+__device__ __forceinline__ void choose_long(SelectLds<WAVES>& lds, uint32_t* candidate, uint8_t* whose, uint32_t n,
+                                            uint32_t k, int32_t first, int32_t* out, Keys4&& keys4)
+{
+    constexpr uint32_t kStep = 4 * kWave;
+    const uint32_t tid = threadIdx.x, wave = tid / kWave, lane = lane_id();
+    const uint32_t steps = (n + WAVES * kStep - 1) / (WAVES * kStep);
+    const uint32_t begin = wave * steps * kStep;
+    const uint64_t below = (1ull << lane) - 1;
+    // f(four scores, place of the first) for the wave's steps; places from n on are none
+    auto each = [&](auto&& f) {
+        for (uint32_t r0 = 0; r0 < steps; r0 += kAtOnce) {
+            uint32_t x[kAtOnce * 4];
+            keys4(begin + r0 * kStep + lane * 4, x);
+#pragma unroll
+            for (uint32_t r = 0; r < kAtOnce; r++)
+                if (r0 + r < steps)
+                    f(&x[r * 4], begin + (r0 + r) * kStep + lane * 4);
+        }
+    };
+    auto count = [&](int d, uint32_t x, uint32_t* bins) { atomicAdd(&bins[(x >> digit_shift(d)) & digit_mask(d)], 1u); };
+    for (uint32_t b = tid; b < 2 * kBins; b += WAVES * kWave)
+        lds.bins[0][b] = 0;
+    if (tid == 0)
+        lds.held = 0;
+    if (tid < WAVES)
+        lds.up[tid] = lds.equal[tid] = 0;
+    __syncthreads();
+    each([&](const uint32_t* x, uint32_t i) {
+#pragma unroll
+        for (uint32_t j = 0; j < 4; j++)
+            if (i + j < n)
+                count(0, x[j], lds.bins[0]);
+    });
+    __syncthreads();
+    find_bin(lds, lds.bins[0], k);
+    const uint32_t digit = lds.digit, many = lds.bins[0][digit];
+    uint32_t left = lds.left, found = digit << digit_shift(0), known = digit_mask(0) << digit_shift(0);
+    const bool fit = many <= kCandidates<WAVES>;
+    if (fit) {
+        uint32_t up = 0;
+        each([&](const uint32_t* x, uint32_t i) {
+#pragma unroll
+            for (uint32_t j = 0; j < 4; j++) {
+                const bool there = i + j < n;
+                up += __popcll(ballot(there && x[j] >> digit_shift(0) > digit));
+                const uint64_t those = ballot(there && x[j] >> digit_shift(0) == digit);
+                if (those == 0)
+                    continue;
+                uint32_t at = 0;
+                if (lane == 0)
+                    at = atomicAdd(&lds.held, (uint32_t)__popcll(those));
+                at = __builtin_amdgcn_readfirstlane(at) + __popcll(those & below);
+                if ((those >> lane) & 1) {
+                    candidate[at] = x[j];
+                    whose[at] = (uint8_t)wave;
+                }
+            }
+        });
+        if (lane == 0)
+            lds.up[wave] = up;
+    }
+    for (int d = 1; d < kDigits; d++) {
+        uint32_t* bins = lds.bins[d % 2];
+        if (d == 2)  // (the first digit's)
+            for (uint32_t b = tid; b < kBins; b += WAVES * kWave)
+                bins[b] = 0;
+        __syncthreads();
+        if (fit) {
+            for (uint32_t i = tid; i < many; i += WAVES * kWave)
+                if ((candidate[i] & known) == found)
+                    count(d, candidate[i], bins);
+        } else {
+            each([&](const uint32_t* x, uint32_t i) {
+#pragma unroll
+                for (uint32_t j = 0; j < 4; j++)
+                    if (i + j < n && (x[j] & known) == found)
+                        count(d, x[j], bins);
+            });
+        }
+        __syncthreads();
+        find_bin(lds, bins, left);
+        found |= lds.digit << digit_shift(d);
+        known |= digit_mask(d) << digit_shift(d);
+        left = lds.left;
+    }
+    // found is the k-th largest; `left` of its equals stay.  Each wave's, above it and equal.
+    if (fit) {
+        for (uint32_t i = tid; i < many; i += WAVES * kWave) {
+            if (candidate[i] > found)
+                atomicAdd(&lds.up[whose[i]], 1u);
+            else if (candidate[i] == found)
+                atomicAdd(&lds.equal[whose[i]], 1u);
+        }
+    } else {
+        uint32_t up = 0, equal = 0;
+        each([&](const uint32_t* x, uint32_t i) {
+#pragma unroll
+            for (uint32_t j = 0; j < 4; j++) {
+                up += __popcll(ballot(i + j < n && x[j] > found));
+                equal += __popcll(ballot(i + j < n && x[j] == found));
+            }
+        });
+        if (lane == 0) {
+            lds.up[wave] = up;
+            lds.equal[wave] = equal;
+        }
+    }
+    __syncthreads();
+    uint32_t above = 0, equal = 0;
+    for (uint32_t w = 0; w < wave; w++) {
+        above += lds.up[w];
+        equal += lds.equal[w];
+    }
+    each([&](const uint32_t* x, uint32_t i) {
+        // those before a lane's first, in the order of places: all of the lanes below it
+        uint32_t up = above, same = equal;
+#pragma unroll
+        for (uint32_t j = 0; j < 4; j++) {
+            const uint64_t more = ballot(i + j < n && x[j] > found), as = ballot(i + j < n && x[j] == found);
+            up += __popcll(more & below);
+            same += __popcll(as & below);
+            above += __popcll(more);
+            equal += __popcll(as);
+        }
+#pragma unroll
+        for (uint32_t j = 0; j < 4; j++) {
+            if (i + j >= n || x[j] < found)
+                continue;
+            const bool over = x[j] > found;
+            if (over || same < left)
+                out[up + (same < left ? same : left)] = first + (int32_t)(i + j);
+            up += over;
+            same += !over;
+        }
+    });
+}
+
 template <int THREADS>
 __global__ __launch_bounds__(THREADS) void select_kernel(SelectIn a, uint32_t* status)
 {
     constexpr int kW = THREADS / kWave;
     __shared__ SelectLds<kW> lds;
+    __shared__ uint32_t candidate[kCandidates<kW>];
+    __shared__ uint8_t whose[kCandidates<kW>];
     const uint32_t tid = threadIdx.x;
     const uint32_t s = blockIdx.x % a.n, x = blockIdx.x / a.n, c = x % a.choices, l = x / a.choices;
     const Held h = held(a.off, a.len, a.entries, s, a.shift);
@@ -223,7 +363,39 @@ __global__ __launch_bounds__(THREADS) void select_kernel(SelectIn a, uint32_t* s
     else if (n <= THREADS * 16)
         choose<kW, 16>(lds, n, k, (int32_t)first, out + first, keys);
     else
-        choose<kW, 0>(lds, n, k, (int32_t)first, out + first, keys);
+        choose_long<kW, THREADS == 1024 ? 4 : 1>(lds, candidate, whose, n, k, (int32_t)first, out + first, [&](uint32_t i, auto& x) {
+            constexpr uint32_t kMany = sizeof(x) / sizeof(x[0]);
+            typedef float v4 __attribute__((ext_vector_type(4), aligned(4)));
+            v4 sum[kMany / 4], more[kMany / 4];
+            auto read = [&](uint32_t g, v4 (&to)[kMany / 4]) {
+                const float* from = w + first + g * a.w_stride;
+#pragma unroll
+                for (uint32_t u = 0; u < kMany / 4; u++) {
+                    const uint32_t p = i + u * 4 * kWave;
+                    to[u] = v4{};
+                    if (p + 3 < n) {
+                        to[u] = *reinterpret_cast<const v4*>(from + p);
+                    } else {
+                        for (uint32_t j = 0; j < 4; j++)
+                            if (p + j < n)
+                                to[u][j] = from[p + j];
+                    }
+                }
+            };
+            read(0, sum);
+            if (a.share > 1)
+                read(1, more);  // (beside the first)
+            for (uint32_t g = 1; g < a.share; g++) {
+                if (g > 1)
+                    read(g, more);
+#pragma unroll
+                for (uint32_t u = 0; u < kMany / 4; u++)
+                    sum[u] = sum[u] + more[u];
+            }
+#pragma unroll
+            for (uint32_t u = 0; u < kMany; u++)
+                x[u] = ordered(sum[u / 4][u % 4]);
+        });
 }
 
 struct GatherIn {
