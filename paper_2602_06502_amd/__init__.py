@@ -817,12 +817,17 @@ class DualMap:
                     "dm_diff_attn")
 
     def _collected(self, w, name, heads):
-        """Address and row stride of [heads, places] with contiguous places."""
-        ok = getattr(w, "dtype", None) is self.torch.float32 and w.dim() == 2 and w.shape[0] == heads \
-            and w.get_device() == self._index and (w.stride(1) == 1 or w.shape[1] <= 1) and w.stride(0) >= w.shape[1]
+        """Address, row stride and places of [heads, places] with contiguous places."""
+        try:
+            h, room = w.shape
+            a, b = w.stride()
+            ok = w.dtype is self.torch.float32 and h == heads and w.get_device() == self._index and (b == 1 or room <= 1) \
+                and (a >= room or heads == 1)
+        except (AttributeError, ValueError, TypeError):
+            ok = False
         if not ok:
             raise ValueError(f"{name} must be a float32 tensor [kv_heads, places] on {self.device}, its rows contiguous")
-        return w.data_ptr(), w.stride(0) if heads > 1 else w.shape[1]
+        return w.data_ptr(), a if heads > 1 else room, room
 
     def attn_weights(self, plan: AttnPlan, layer: int, q, scale: float, lse, w, last: int = 0, prev=None,
                      decay: float = 1.0) -> None:
@@ -835,8 +840,8 @@ class DualMap:
         if lse is None:
             raise ValueError("lse is what the attention call left")
         lp = self._lse(lse, T, heads)
-        wp, ws = self._collected(w, "w", kv.kv_heads)
-        if w.shape[1] < plan.entries * kv.block:
+        wp, ws, have = self._collected(w, "w", kv.kv_heads)
+        if have < plan.entries * kv.block:
             raise ValueError("w needs a place for each token of the tables' entries")
         pp = ps = room = off = src = keep = n = 0
         if isinstance(prev, tuple):
@@ -847,8 +852,7 @@ class DualMap:
                 raise ValueError("src and keep need an entry for each sequence, off one more than there were")
             off, src, keep = off.data_ptr(), src.data_ptr(), keep.data_ptr()
         if prev is not None:
-            pp, ps = self._collected(prev, "prev", kv.kv_heads)
-            room = prev.shape[1]
+            pp, ps, room = self._collected(prev, "prev", kv.kv_heads)
             if not off and room < plan.entries * kv.block:
                 raise ValueError("prev needs a place for each token of the tables' entries")
         a = _PACK_WEIGHTS(qp, qs, lp, wp, ws, pp, ps, room, off, src, keep, n, scale, decay, last, 1 if plan.pairs else 0)
@@ -856,16 +860,29 @@ class DualMap:
                     "dm_attn_weights")
 
     def _layers(self, x, name, dtype, heads, places):
-        """Address and strides of [layers, heads, at least `places`] with contiguous places."""
-        ok = getattr(x, "dtype", None) is dtype and x.dim() == 3 and x.get_device() == self._index \
-            and x.shape[1] == heads and x.shape[2] >= places and (x.stride(2) == 1 or x.shape[2] <= 1)
+        """Address, strides and layers of [layers, heads, at least `places`] with contiguous places."""
+        try:
+            layers, h, room = x.shape
+            a, b, c = x.stride()
+            ok = x.dtype is dtype and x.get_device() == self._index and h == heads and room >= places \
+                and (c == 1 or room <= 1)
+        except (AttributeError, ValueError, TypeError):
+            ok = False
         if not ok:
             raise ValueError(f"{name} must be a {dtype} tensor [layers, {heads}, at least {places}] on {self.device}, "
                              "its rows contiguous")
-        a, b = x.stride(0), x.stride(1) if heads > 1 else x.shape[2]
-        if b < x.shape[2] or (x.shape[0] > 1 and a < b * (heads - 1) + x.shape[2]):
+        if heads == 1:
+            b = room
+        if b < room or (layers > 1 and a < b * (heads - 1) + room):
             raise ValueError(f"{name}'s rows must not overlap")
-        return x.data_ptr(), a, b
+        return x.data_ptr(), a, b, layers
+
+    def _kept(self, kept, choices, layers, places):
+        """Address and row stride of the choices' lists."""
+        kp, kl, ks, n = self._layers(kept, "kept", self.torch.int32, choices, places)
+        if n != layers or (layers > 1 and kl != choices * ks):
+            raise ValueError("kept needs as many layers as there are, one after another")
+        return kp, ks
 
     def evict_select(self, tables, w, budget, room, kept, keep, grow, sink: int = 0, recent: int = 0,
                      share: int = 1) -> None:
@@ -877,11 +894,9 @@ class DualMap:
         places = tb[4] * self.block
         if getattr(w, "ndim", 0) != 3 or share < 1 or w.shape[1] % share:
             raise ValueError("w must be [layers, kv_heads, places], share divide kv_heads")
-        layers, heads = w.shape[:2]
-        wp, wl, ws = self._layers(w, "w", t.float32, heads, places)
-        kp, _, ks = self._layers(self._dev(kept, t.int32, "kept"), "kept", t.int32, heads // share, places)
-        if kept.shape[0] != layers:
-            raise ValueError("kept needs as many layers as w")
+        heads = w.shape[1]
+        wp, wl, ws, layers = self._layers(w, "w", t.float32, heads, places)
+        kp, ks = self._kept(kept, heads // share, layers, places)
         for x, name in ((budget, "budget"), (room, "room"), (keep, "keep"), (grow, "grow")):
             if (x is not None or name != "room") and self._dev(x, t.int64, name).numel() != tb[3]:
                 raise ValueError(f"{name} needs an entry for each sequence")
@@ -900,14 +915,14 @@ class DualMap:
         if tb[3] != to[3] or self._dev(budget, t.int64, "budget").numel() != tb[3]:
             raise ValueError("the tables and budget need the same sequences")
         choices = kept.shape[1] if getattr(kept, "ndim", 0) == 3 else 0
-        if not choices or kv.kv_heads % choices or kept.shape[0] != kv.layers:
+        if not choices or kv.kv_heads % choices:
             raise ValueError("kept must be [layers, kv_heads / share, places]")
-        kp, _, ks = self._layers(self._dev(kept, t.int32, "kept"), "kept", t.int32, choices, tb[4] * self.block)
+        kp, ks = self._kept(kept, choices, kv.layers, tb[4] * self.block)
         wp = wl = ws = op = ol = os_ = 0
         if w is not None or w_to is not None:
-            wp, wl, ws = self._layers(w, "w", t.float32, kv.kv_heads, tb[4] * self.block)
-            op, ol, os_ = self._layers(w_to, "w_to", t.float32, kv.kv_heads, to[4] * self.block)
-            if w.shape[0] != kv.layers or w_to.shape[0] != kv.layers:
+            wp, wl, ws, n = self._layers(w, "w", t.float32, kv.kv_heads, tb[4] * self.block)
+            op, ol, os_, m = self._layers(w_to, "w_to", t.float32, kv.kv_heads, to[4] * self.block)
+            if n != kv.layers or m != kv.layers:
                 raise ValueError("w and w_to need the pages' layers")
         a = _PACK_GATHER(budget.data_ptr(), kp, ks, wp, wl, ws, op, ol, os_, kv.kv_heads // choices, 0)
         self._check(self.lib.dm_kv_gather(self._h, kv._ref, _PACK_TABLES(*tb), _PACK_TABLES(*to), a), "dm_kv_gather")
