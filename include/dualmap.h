@@ -713,8 +713,11 @@ typedef struct {
  * over the sequence's new tokens (the last of them) that see i and the query
  * heads that read h: x / (q_heads / kv_heads) = h, or with paired those of h's
  * place in its pair (each head of a pair of KV heads has its own map's weights).
- * Products and sums are in 32 bits, each sum's order fixed.  A weight is off by
- * some 2^-23 of itself for each unit of |lse| (its own rounding).  A query with
+ * Products and sums are in 32 bits, each sum's order fixed; the sums of many
+ * weights keep what their additions round away.  A weight is off by some 2^-23
+ * of itself for each unit of |lse| (its own rounding).  Where sequences have many
+ * rows the context's work area holds up to 16 sums for each of w's places, not
+ * more than 2^24 floats unless one each is more; it grows as dm_attn's.  A query with
  * lse = -infinity counts nowhere; keys that no query sees have what they had.
  * Other places of w are left as they were.  Who sees what, malformed tables and
  * a plan of another batch are as in dm_attn; a sequence's src or prev_off out of

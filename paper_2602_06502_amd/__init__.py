@@ -855,6 +855,8 @@ class DualMap:
             pp, ps, room = self._collected(prev, "prev", kv.kv_heads)
             if not off and room < plan.entries * kv.block:
                 raise ValueError("prev needs a place for each token of the tables' entries")
+        if not 0 <= last < 1 << 32:
+            raise ValueError("last must be at least 0 and below 2^32")
         a = _PACK_WEIGHTS(qp, qs, lp, wp, ws, pp, ps, room, off, src, keep, n, scale, decay, last, 1 if plan.pairs else 0)
         self._check(self.lib.dm_attn_weights(self._h, plan.batch, kv._ref, heads, plan.buf.data_ptr(), layer, a),
                     "dm_attn_weights")

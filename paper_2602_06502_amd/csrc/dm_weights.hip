@@ -372,7 +372,7 @@ __global__ __launch_bounds__(kThreads, D == 256 ? (RUNS ? 1 : 2) : RUNS && D == 
     auto collect = [&](const Known& s, uint32_t h, int64_t i0, int64_t from, int64_t to, bool causal) {
         const uint32_t x0 = a.paired ? h / 2 * 2 * a.ratio + h % 2 : h * a.ratio, xs = a.paired ? 2 : 1;
         const int64_t i = i0 + lane;
-        const bool mine = i >= from && i < to;
+        const bool mine = i >= from && i < to && i < (int64_t)s.len;  // (whatever the plan says)
         float carried = 0;
         if (mine && i < s.keep)
             carried = a.decay * a.prev[(int64_t)h * a.prev_stride + s.old + i];
@@ -443,7 +443,7 @@ __global__ __launch_bounds__(kThreads, D == 256 ? (RUNS ? 1 : 2) : RUNS && D == 
                     const uint32_t n = n0 + lane / 16 * 4 / kRows, from = member(n < count ? n : n0);
                     const bool writes = n < count && lane / 16 * 4 % kRows == 0;
                     const int64_t at = __shfl((long long)of.at, from), old = __shfl((long long)of.old, from);
-                    const uint32_t keep = __shfl(of.keep, from);
+                    const uint32_t keep = __shfl(of.keep, from), len = __shfl(of.len, from);
                     float carried[4], sum[4];
 #pragma unroll
                     for (int c = 0; c < 4; c++) {
@@ -454,7 +454,7 @@ __global__ __launch_bounds__(kThreads, D == 256 ? (RUNS ? 1 : 2) : RUNS && D == 
 #pragma unroll
                     for (int c = 0; c < 4; c++) {
                         const int64_t i = i0 + c * 16 + lane % 16;
-                        if (writes && i >= 0 && i < x.own0)
+                        if (writes && i >= 0 && i < x.own0 && i < len)
                             a.w[(int64_t)h * a.w_stride + at + i] = carried[c] + sum[c];
                     }
                 }
@@ -734,19 +734,20 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : D == 128 ? 2 : 3) void wei
             finish(zb, words[before], 32, was_masked);
         const float s0 = sum[0].sum + __shfl_xor(sum[0].sum, 32), s1 = sum[1].sum + __shfl_xor(sum[1].sum, 32);
         const int64_t i = i1 + lane;
-        if (i >= from && i < to)
+        if (i >= from && i < to && i < v.len)
             a.part[((uint64_t)p * a.kv_heads + h) * a.slots + (b.off[s] << b.shift) + i] = half ? s1 : s0;
     };
     each_sequence(b, pv, slot0, kTallKeys, bad, collect);
 }
 
-// How many stretches of rows tall blocks are for (0: there are none), and their rows: some
-// six workgroups a compute unit if all sequences are alike.  A batch with hardly more
+// How many stretches of rows tall blocks are for (0: there are none), and their rows: some 32
+// workgroups a compute unit if all sequences are alike (two prompts of 7,000 to 8,192 tokens: 6
+// 728 us, 16 or 32 665), not more than kParts, nor than kSums sums.  A batch with hardly more
 // tokens than sequences has none: where one sequence has them all, those are a few rows yet.
 uint32_t parts_of_rows(const dm_ctx* c, const dm_token_batch& b, uint32_t ratio, uint32_t last, uint64_t blocks,
                        uint32_t* part_rows)
 {
-    constexpr uint64_t kMany = 1024, kParts = 16;
+    constexpr uint64_t kMany = 1024, kParts = 16, kSums = 1 << 24;
     *part_rows = 0;
     const uint64_t n = b.tables.n, tokens = last && last < b.q_tokens ? last : b.q_tokens;  // of a sequence, at most
     if (b.q_tokens <= n || (b.q_tokens - n) * ratio <= kMany || tokens * ratio <= kFewRows || blocks == 0)
@@ -755,7 +756,9 @@ uint32_t parts_of_rows(const dm_ctx* c, const dm_token_batch& b, uint32_t ratio,
     uint64_t rows = blocks * each / (32 * c->n_cu);
     rows = (rows / kTallRows + 1) * kTallRows;
     rows = rows < 512 ? 512 : rows;
-    const uint64_t most = (tokens * ratio + kParts - 1) / kParts;  // no more stretches than kParts
+    const uint64_t room = kSums / (blocks * kTallKeys);
+    const uint64_t limit = room < 1 ? 1 : room < kParts ? room : kParts;
+    const uint64_t most = (tokens * ratio + limit - 1) / limit;
     rows = rows < most ? (most + kTallRows - 1) / kTallRows * kTallRows : rows;
     const uint64_t parts = (tokens * ratio + rows - 1) / rows;
     if (parts * blocks > 0x7FFFFFFFull)

@@ -143,6 +143,16 @@ def test_shared_prefixes(dim):
     b.check(groups=False)
 
 
+@pytest.mark.parametrize("dim", [64, 128])
+def test_batches_of_few_rows_a_sequence(dim):
+    """A few rows a sequence on average, and one with many among them; the same with runs."""
+    _say("few", dim)
+    b = Pairs(16, [(1, 30 + 11 * i) for i in range(20)] + [(19, 300), (2, 2)], heads=(8, 4), dim=dim, seed=4)
+    b.check()
+    b.groups = np.array([0, 9, 22], np.int64)
+    b.check()
+
+
 def test_many_rows_in_parts():
     """More rows than waves, on shared prefixes: four rows joined by a wave."""
     _say("many")

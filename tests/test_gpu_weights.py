@@ -179,6 +179,40 @@ def test_shared_prefixes(dim):
     b.check(groups=False)
 
 
+def test_members_of_a_run_far_apart():
+    """Between the sequences of a run that see its prefix, many that have no new token."""
+    _say("far apart")
+    seqs = [((1 if i % 37 == 5 else 0), 3 + i % 50, 0) for i in range(260)]
+    Collected(16, seqs, prefixes=(192,), heads=(4, 2), dim=64, seed=4).check()
+    Collected(16, [(n, 3 + i % 50, 0) for i, (n, _, _) in enumerate(seqs)], prefixes=(192,), heads=(16, 1), dim=64, prev="same",
+              seed=5).check()
+
+
+@pytest.mark.parametrize("heads", [(1, 1), (2, 1), (3, 1), (5, 1), (8, 1), (16, 1), (17, 1)])
+def test_rows_of_a_run(heads):
+    """One to seventeen rows a sequence, which share products by fours, eights and sixteens, or do not."""
+    _say("rows", heads)
+    Collected(16, [(1, 5 + 9 * i, 0) for i in range(21)], prefixes=(336,), heads=heads, dim=64, dtype="f16", seed=2).check()
+    Collected(16, [(1 + i % 2, 5 + 9 * i, 0) for i in range(9)], prefixes=(336,), heads=heads, last=1, seed=3).check()
+
+
+@pytest.mark.parametrize("heads", [(3, 1), (7, 1), (16, 1), (24, 1)])
+@pytest.mark.parametrize("dim", [64, 128, 256])
+def test_many_rows_of_odd_ratios(heads, dim):
+    """Rows that pass through LDS, where a step of them is not whole tokens, with room between rows of q."""
+    _say("ratios", heads, dim)
+    Collected(16, [(500, 700), (90, 90), (1, 300), (260, 900)], heads=heads, dim=dim, pad_q=40, last=0, seed=1).check()
+    Collected(16, [(500, 700, 0), (90, 90, 0), (1, 300, 0)], prefixes=(320,), heads=heads, dim=dim, last=333, seed=1).check()
+
+
+def test_no_new_tokens():
+    """A batch without any: what was carried, decayed."""
+    _say("none")
+    Collected(16, [(0, 30), (0, 0), (0, 77)], prev="fork", seed=1).check()
+    b = Collected(16, [(0, 30), (0, 77)], prev="same", seed=1)
+    b.check(inplace=True)
+
+
 def test_many_sequences_share():
     _say("many")
     Collected(32, [(1, 1 + i % 70, 0) for i in range(45)] + [(1, 9, 1)], prefixes=(352, 160), heads=(14, 2), dim=64,

@@ -134,6 +134,37 @@ def scenario_areas(x):
     assert rows * 130 * 4 <= held.value - before <= rows * 130 * 4 + 4096
 
 
+def scenario_weights_area(x):
+    """Sums of stretches of rows: none for a few rows a sequence, up to 16 for a place otherwise, 2^24 floats or one for each
+    place at the most; growth under capture is refused."""
+    held, capturing = x.word("fake_bytes"), x.word("fake_capturing", C.c_int)
+    for tokens, n, entries, last, parts in ((64, 64, 4000, 0, 0), (66, 64, 4000, 0, 0), (16_000, 2, 1000, 0, (2, 16)),
+                                            (16_000, 2, 1000, 16, 0), (16_000, 2, 1000, 200, (1, 16)),
+                                            (6400, 64, 32_768, 0, (1, 8)), (100_000, 4, 1 << 20, 0, (1, 1))):
+        c = Calls(x)
+        before = held.value
+        kw = dict(batch=dict(tokens=tokens, n=n, entries=entries), w_stride=entries * 16, last=last)
+        assert c.weights(**kw) == x.pk.DM_OK
+        one = entries * 16 * 4 * 4
+        got = held.value - before
+        if parts == 0:
+            assert got == 0, (tokens, n, got)
+        else:
+            assert one * parts[0] <= got <= one * parts[1] + 4096, (tokens, n, got / one)
+            assert got <= max(4 << 24, one) + 4096
+            capturing.value = 1
+            assert c.weights(**kw) == x.pk.DM_OK
+            kw["batch"]["entries"], kw["w_stride"] = 64 * entries, 64 * entries * 16
+            assert c.weights(**kw) == x.pk.DM_EDEVICE and b"capture" in x.L.dm_last_error(c.h)
+            capturing.value = 0
+            assert c.weights(**kw) == x.pk.DM_OK
+        x.L.dm_destroy(c.h)
+
+
+def test_weights_work_area(fake):  # noqa: F811
+    _child(fake, "weights_area")
+
+
 def test_refusals(fake):  # noqa: F811
     _child(fake, "refusals")
 
