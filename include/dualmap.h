@@ -716,7 +716,7 @@ typedef struct {
  * Products and sums are in 32 bits, each sum's order fixed; the sums of many
  * weights keep what their additions round away.  A weight is off by some 2^-23
  * of itself for each unit of |lse| (its own rounding).  Where sequences have many
- * rows the context's work area holds up to 16 sums for each of w's places, not
+ * rows the context's work area holds up to 32 sums for each of w's places, not
  * more than 2^24 floats unless one each is more; it grows as dm_attn's.  A query with
  * lse = -infinity counts nowhere; keys that no query sees have what they had.
  * Other places of w are left as they were.  Who sees what, malformed tables and

@@ -95,16 +95,18 @@ __global__ __launch_bounds__(kSmallWaves<D>* kWave, 1) void diff_small_kernel(Di
         atomicOr(status, kErrInval);
 }
 
-// Rows in parts where they are few: a workgroup for a pair of rows, two waves a map, each
-// with every second part; eight parts' rows are read at once.
-template <typename T, int D>
-__global__ __launch_bounds__(kThreads) void diff_join_kernel(DiffIn a, const PlanView pv, uint64_t part_rows,
+// Rows in parts where they are few: a workgroup for a pair of rows, half of its waves a map,
+// each with every second or fourth part; eight parts' rows are read at once.  Eight waves where
+// pairs are fewer than two a compute unit (18 pairs in up to 190 parts: 73 to 58 us with the
+// pass), four otherwise (1,024 pairs: 222 us, with eight 226).
+template <typename T, int D, int JOIN>
+__global__ __launch_bounds__(JOIN* kWave) void diff_join_kernel(DiffIn a, const PlanView pv, uint64_t part_rows,
                                                              uint32_t wide, uint32_t items)
 {
-    constexpr int kPer = D / kWave, kAtOnce = 8;
+    constexpr int kPer = D / kWave, kAtOnce = 8, kEach = JOIN / 2;
     typedef float vper __attribute__((ext_vector_type(kPer)));
-    __shared__ vper rows[kWaves][kWave];
-    __shared__ v2f stats[kWaves];
+    __shared__ vper rows[JOIN][kWave];
+    __shared__ v2f stats[JOIN];
     const PlanHead& ph = *pv.head;
     if (ph.part_rows == 0 || !plan_fits(ph, a, part_rows, D, wide, items))
         return;
@@ -117,19 +119,19 @@ __global__ __launch_bounds__(kThreads) void diff_join_kernel(DiffIn a, const Pla
             continue;
         float m = -INFINITY, total = 0;
         vper v = {};
-        for (uint32_t i0 = wave / 2; i0 < p.n; i0 += 2 * kAtOnce) {
+        for (uint32_t i0 = wave / 2; i0 < p.n; i0 += kEach * kAtOnce) {
             v2f e[kAtOnce];
             vper r[kAtOnce];
 #pragma unroll
             for (int j = 0; j < kAtOnce; j++) {
-                const uint64_t at = p.at(i0 + 2 * j < p.n ? i0 + 2 * j : p.n - 1);
+                const uint64_t at = p.at(i0 + kEach * j < p.n ? i0 + kEach * j : p.n - 1);
                 e[j] = a.part_stat[at];
                 r[j] = *reinterpret_cast<const vper*>(a.part + at * D + lane * kPer);
             }
             float now = m;
 #pragma unroll
             for (int j = 0; j < kAtOnce; j++) {
-                if (i0 + 2 * j >= p.n)
+                if (i0 + kEach * j >= p.n)
                     e[j] = v2f{-INFINITY, 0};
                 now = fmaxf(now, e[j][0]);
             }
@@ -151,32 +153,35 @@ __global__ __launch_bounds__(kThreads) void diff_join_kernel(DiffIn a, const Pla
         if (lane == 0)
             stats[wave] = v2f{m, total};
         __syncthreads();
-        if (wave > 1)
-            continue;
-        // waves 0 and 1: their maps, from two waves each
-        const v2f other = stats[wave + 2];
-        const float top = fmaxf(m, other[0]);
-        const float k0 = m == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f((m - top) * a.scale2);
-        const float k1 = other[0] == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f((other[0] - top) * a.scale2);
-        total = total * k0 + other[1] * k1;
-        const bool seen = total > 0 || total != total;
-        if (lane == 0 && a.lse)
-            a.lse[(uint64_t)t * a.q_heads + x + map] = seen ? lse_of<T>(top, total, a.scale2) : -INFINITY;
         if (wave)
             continue;
-        const v2f f1 = stats[1], f3 = stats[3];
-        const float top1 = fmaxf(f1[0], f3[0]);
-        const float k2 = f1[0] == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f((f1[0] - top1) * a.scale2);
-        const float k3 = f3[0] == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f((f3[0] - top1) * a.scale2);
-        const float total1 = f1[1] * k2 + f3[1] * k3, lambda = a.lambda[x / 2];
-        const float inv = seen ? 1.0f / total : 0.0f;
-        const float inv1 = total1 > 0 || total1 != total1 ? 1.0f / total1 : 0.0f;
-        const vper v1 = rows[1][lane], v2 = rows[2][lane], v3 = rows[3][lane];
+        // wave 0: both maps, from four waves each
+        vper o[2];
+        const float lambda = a.lambda[x / 2];
+#pragma unroll
+        for (uint32_t map1 = 0; map1 < 2; map1++) {
+            float top = -INFINITY, sum = 0;
+#pragma unroll
+            for (uint32_t k = 0; k < kEach; k++)
+                top = fmaxf(top, stats[map1 + 2 * k][0]);
+            o[map1] = vper{};
+#pragma unroll
+            for (uint32_t k = 0; k < kEach; k++) {
+                const v2f e = stats[map1 + 2 * k];
+                // (one that saw nothing has zeros, one that saw NaN only has a sum of NaN)
+                const float by = e[0] == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f((e[0] - top) * a.scale2);
+                sum += e[1] * by;
+                o[map1] += rows[map1 + 2 * k][lane] * by;
+            }
+            const bool seen = sum > 0 || sum != sum;
+            o[map1] *= seen ? 1.0f / sum : 0.0f;
+            if (lane == 0 && a.lse)
+                a.lse[(uint64_t)t * a.q_heads + x + map1] = seen ? lse_of<T>(top, sum, a.scale2) : -INFINITY;
+        }
         float ss = 0;
 #pragma unroll
         for (int c = 0; c < kPer; c++) {
-            v[c] = (v[c] * k0 + v2[c] * k1) * inv;
-            v[c] = __builtin_fmaf(-lambda, (v1[c] * k2 + v3[c] * k3) * inv1, v[c]);
+            v[c] = __builtin_fmaf(-lambda, o[1][c], o[0][c]);
             ss = __builtin_fmaf(v[c], v[c], ss);
         }
         float by = a.gain;
@@ -285,9 +290,12 @@ hipError_t diff_attn(dm_ctx* c, const dm_token_batch& b, const dm_kv_pages& stor
         const uint64_t outs = b.q_tokens * q_heads;
         if (outs > 8ull * c->n_cu * kWaves)
             diff_join_many_kernel<T, D><<<4u * c->n_cu, kThreads, 0, c->stream>>>(a, pv, rows, wide, (uint32_t)most);
+        else if (outs > 4ull * c->n_cu)
+            diff_join_kernel<T, D, 4>
+                <<<grid_for(outs / 2, 1, 8u * c->n_cu), 4 * kWave, 0, c->stream>>>(a, pv, rows, wide, (uint32_t)most);
         else
-            diff_join_kernel<T, D>
-                <<<grid_for(outs / 2, 1, 8u * c->n_cu), kThreads, 0, c->stream>>>(a, pv, rows, wide, (uint32_t)most);
+            diff_join_kernel<T, D, 8>
+                <<<(uint32_t)(outs / 2), 8 * kWave, 0, c->stream>>>(a, pv, rows, wide, (uint32_t)most);
     };
     auto dims = [&](auto t) {
         if (kv.head_dim == 128)

@@ -747,7 +747,7 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : D == 128 ? 2 : 3) void wei
 uint32_t parts_of_rows(const dm_ctx* c, const dm_token_batch& b, uint32_t ratio, uint32_t last, uint64_t blocks,
                        uint32_t* part_rows)
 {
-    constexpr uint64_t kMany = 1024, kParts = 16, kSums = 1 << 24;
+    constexpr uint64_t kMany = 1024, kParts = 32, kSums = 1 << 24;
     *part_rows = 0;
     const uint64_t n = b.tables.n, tokens = last && last < b.q_tokens ? last : b.q_tokens;  // of a sequence, at most
     if (b.q_tokens <= n || (b.q_tokens - n) * ratio <= kMany || tokens * ratio <= kFewRows || blocks == 0)
@@ -755,7 +755,7 @@ uint32_t parts_of_rows(const dm_ctx* c, const dm_token_batch& b, uint32_t ratio,
     const uint64_t each = (last && last * n < b.q_tokens ? last * n : b.q_tokens) * ratio / n;  // rows of a sequence
     uint64_t rows = blocks * each / (32 * c->n_cu);
     rows = (rows / kTallRows + 1) * kTallRows;
-    rows = rows < 512 ? 512 : rows;
+    rows = rows < 256 ? 256 : rows;
     const uint64_t room = kSums / (blocks * kTallKeys);
     const uint64_t limit = room < 1 ? 1 : room < kParts ? room : kParts;
     const uint64_t most = (tokens * ratio + limit - 1) / limit;

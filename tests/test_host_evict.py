@@ -135,11 +135,11 @@ def scenario_areas(x):
 
 
 def scenario_weights_area(x):
-    """Sums of stretches of rows: none for a few rows a sequence, up to 16 for a place otherwise, 2^24 floats or one for each
+    """Sums of stretches of rows: none for a few rows a sequence, up to 32 for a place otherwise, 2^24 floats or one for each
     place at the most; growth under capture is refused."""
     held, capturing = x.word("fake_bytes"), x.word("fake_capturing", C.c_int)
-    for tokens, n, entries, last, parts in ((64, 64, 4000, 0, 0), (66, 64, 4000, 0, 0), (16_000, 2, 1000, 0, (2, 16)),
-                                            (16_000, 2, 1000, 16, 0), (16_000, 2, 1000, 200, (1, 16)),
+    for tokens, n, entries, last, parts in ((64, 64, 4000, 0, 0), (66, 64, 4000, 0, 0), (16_000, 2, 1000, 0, (2, 32)),
+                                            (16_000, 2, 1000, 16, 0), (16_000, 2, 1000, 200, (1, 32)),
                                             (6400, 64, 32_768, 0, (1, 8)), (100_000, 4, 1 << 20, 0, (1, 1))):
         c = Calls(x)
         before = held.value
