@@ -584,7 +584,10 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : D == 128 ? 2 : 3) void wei
         auto send = [&](uint32_t row0, const uint16_t* to) {
             const uint32_t at = lds_address(to) + wave * kWave * 16;
             if (even && row0 + kTallRows <= r.row1) {
-                const uint16_t* from = a.q + (int64_t)(v.tok0 + row0 / a.ratio) * a.q_stride;
+                // (uniform, and said so: not every optimisation level sees it)
+                const uint64_t first = (uint64_t)(v.tok0 + row0 / a.ratio) * a.q_stride;
+                const uint16_t* from = a.q + ((uint64_t)__builtin_amdgcn_readfirstlane((uint32_t)(first >> 32)) << 32 |
+                                              (uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)first));
 #pragma unroll
                 for (int i = 0; i < kLoads; i++)
                     send16(from + i * (int64_t)(kStep / a.ratio) * a.q_stride, lane_at[i % 2], at + i * kThreads * 16);
