@@ -718,8 +718,8 @@ typedef struct {
  * of itself for each unit of |lse| (its own rounding).  Where sequences have many
  * rows the context's work area holds up to 32 sums for each of w's places, not
  * more than 2^24 floats unless one each is more; it grows as dm_attn's.  A query with
- * lse = -infinity counts nowhere; keys that no query sees have what they had.
- * Other places of w are left as they were.  Who sees what, malformed tables and
+ * lse = -infinity counts nowhere (its scores finite); keys that no query sees have
+ * what they had.  Other places of w are left as they were.  Who sees what, malformed tables and
  * a plan of another batch are as in dm_attn; a sequence's src or prev_off out of
  * range carries nothing and is reported (DM_EINVAL). */
 dm_status dm_attn_weights(dm_ctx* ctx, const dm_token_batch* batch, const dm_kv_pages* kv,
@@ -764,7 +764,11 @@ typedef struct {
  * 32 bits.  Of equal scores the earlier token stays; NaN counts less than any
  * number.  Their places in the sequence go to kept, in increasing order: entry i
  * of sequence s at off[s] * B + i of a row; nothing else of kept is written.
- * Exact and the same every time.  page is not read.  A malformed table or a
+ * Exact and the same every time.  The few choices of long histories (means of more
+ * than 24,576 tokens) are split over workgroups: the context's work area, which grows
+ * as dm_attn's, then holds a number for each of their scores and 8 KiB for each
+ * workgroup, not more than 2^29 bytes (choices that would need more are not split).
+ * page is not read.  A malformed table or a
  * negative budget is reported (DM_EINVAL) and evicts nothing of its sequence. */
 dm_status dm_evict_select(dm_ctx* ctx, const dm_page_tables* tables, const dm_select_args* args);
 

@@ -7,11 +7,15 @@
 // and 10 bits are counted in LDS from the top, each time among the scores that agree with the
 // digits found so far, so three passes give the k-th largest exactly, with how many of its
 // equals stay (the first ones).  A workgroup takes a (layer, choice, sequence); its scores
-// stay in registers where they fit.  Bound by reading the weights, and for short sequences
-// by the passes' barriers.
+// stay in registers where they fit; where choices are few and long, several take one.  Bound by
+// reading the weights, three times where they are long (four histories of 27,000 to 124,000
+// tokens, 8 layers, pairs of 8 heads: 82 us, 88 with a workgroup a choice; 86 MB a pass take 17),
+// and for short sequences by the passes' barriers (16 chats, 4 layers, 8 heads: 12 us).
 //
 // The move takes a page of the new tables a workgroup: a row's token, that token's page, the
 // row.  Bound by memory.
+#include <type_traits>
+
 #include "dm_internal.h"
 #include "dm_pages.h"
 
@@ -307,6 +311,101 @@ __device__ __forceinline__ void choose_long(SelectLds<WAVES>& lds, uint32_t* can
     });
 }
 
+// What a (layer, choice, sequence) is to choose: k of the n tokens from `first` on; none (k = 0)
+// where the sequence is within its budget.
+struct Pick {
+    uint32_t len, first, tail, k, n;
+    const float* w;  // of token `first`, of the choice's first head
+    int32_t* out;    // the choice's first entry
+    int64_t at;      // the sequence's first place
+    bool past;
+};
+__device__ __forceinline__ Pick pick_of(const SelectIn& a, uint32_t x, bool& bad)
+{
+    const uint32_t s = x % a.n, c = x / a.n % a.choices, l = x / a.n / a.choices;
+    const Held h = held(a.off, a.len, a.entries, s, a.shift);
+    const int64_t budget = a.budget[s];
+    Pick p{};
+    bad = h.bad || budget < 0;
+    p.len = (uint32_t)h.len;
+    p.past = !bad && h.len > budget;
+    if (!p.past)
+        return p;
+    const uint32_t stay = (uint32_t)budget;
+    p.first = stay < a.sink ? stay : a.sink;
+    p.tail = stay - p.first < a.recent ? stay - p.first : a.recent;
+    p.k = stay - p.first - p.tail;
+    p.n = p.len - p.first - p.tail;
+    p.at = h.off << a.shift;
+    p.w = a.w + (int64_t)l * a.layer_stride + (int64_t)(c * a.share) * a.w_stride + p.at + p.first;
+    p.out = a.kept + ((int64_t)l * a.choices + c) * a.kept_stride + p.at;
+    return p;
+}
+// What needs no choosing: the first and the last tokens, and, once a sequence, the next tables'
+// numbers.
+__device__ __forceinline__ void settle(const SelectIn& a, const Pick& p, uint32_t x, bool bad, uint32_t threads,
+                                       uint32_t* status)
+{
+    const uint32_t tid = threadIdx.x;
+    if (x < a.n && tid == 0) {
+        a.keep[x] = p.past ? 0 : p.len;
+        a.grow[x] = (a.room ? a.room[x] : 0) + (p.past ? p.first + p.tail + p.k : 0);
+        if (bad)
+            atomicOr(status, kErrInval);
+    }
+    if (!p.past)
+        return;
+    for (uint32_t i = tid; i < p.first; i += threads)
+        p.out[i] = (int32_t)i;
+    for (uint32_t i = tid; i < p.tail; i += threads)
+        p.out[p.first + p.k + i] = (int32_t)(p.len - p.tail + i);
+}
+
+// Scores i + 256 u + j, to x[4 u + j], of those below `end`: 16 bytes of each head at a time.
+template <bool WHOLE, uint32_t MANY>
+__device__ __forceinline__ void scores4(const SelectIn& a, const float* w, uint32_t end, uint32_t i, uint32_t (&x)[MANY])
+{
+    typedef float v4 __attribute__((ext_vector_type(4), aligned(4)));
+    v4 sum[MANY / 4], more[MANY / 4];
+    // (waves within `end` read without a branch between their reads: 78 us for the three kernels
+    // that split, 88 without; one kernel by itself has no registers for it, 88 and 100)
+    const bool whole = WHOLE && __builtin_amdgcn_readfirstlane(i) + MANY * kWave <= end;
+    auto read = [&](uint32_t g, v4 (&to)[MANY / 4]) {
+        const float* from = w + g * a.w_stride;
+        if (whole) {
+#pragma unroll
+            for (uint32_t u = 0; u < MANY / 4; u++)
+                to[u] = *reinterpret_cast<const v4*>(from + i + u * 4 * kWave);
+            return;
+        }
+#pragma unroll
+        for (uint32_t u = 0; u < MANY / 4; u++) {
+            const uint32_t p = i + u * 4 * kWave;
+            to[u] = v4{};
+            if (p + 3 < end) {
+                to[u] = *reinterpret_cast<const v4*>(from + p);
+            } else {
+                for (uint32_t j = 0; j < 4; j++)
+                    if (p + j < end)
+                        to[u][j] = from[p + j];
+            }
+        }
+    };
+    read(0, sum);
+    if (a.share > 1)
+        read(1, more);  // (beside the first)
+    for (uint32_t g = 1; g < a.share; g++) {
+        if (g > 1)
+            read(g, more);
+#pragma unroll
+        for (uint32_t u = 0; u < MANY / 4; u++)
+            sum[u] = sum[u] + more[u];
+    }
+#pragma unroll
+    for (uint32_t u = 0; u < MANY; u++)
+        x[u] = ordered(sum[u / 4][u % 4]);
+}
+
 template <int THREADS>
 __global__ __launch_bounds__(THREADS) void select_kernel(SelectIn a, uint32_t* status)
 {
@@ -314,38 +413,20 @@ __global__ __launch_bounds__(THREADS) void select_kernel(SelectIn a, uint32_t* s
     __shared__ SelectLds<kW> lds;
     __shared__ uint32_t candidate[kCandidates<kW>];
     __shared__ uint8_t whose[kCandidates<kW>];
-    const uint32_t tid = threadIdx.x;
-    const uint32_t s = blockIdx.x % a.n, x = blockIdx.x / a.n, c = x % a.choices, l = x / a.choices;
-    const Held h = held(a.off, a.len, a.entries, s, a.shift);
-    const int64_t budget = a.budget[s], room = a.room ? a.room[s] : 0;
-    const bool past = !h.bad && budget >= 0 && h.len > budget;
-    if (x == 0 && tid == 0) {
-        a.keep[s] = past ? 0 : h.len;
-        a.grow[s] = room + (past ? budget : 0);
-        if (h.bad || budget < 0)
-            atomicOr(status, kErrInval);
-    }
-    if (!past)
-        return;
-    const uint32_t len = (uint32_t)h.len, stay = (uint32_t)budget;
-    const uint32_t first = stay < a.sink ? stay : a.sink;
-    const uint32_t tail = stay - first < a.recent ? stay - first : a.recent;
-    const uint32_t k = stay - first - tail, n = len - first - tail;
-    const int64_t at = h.off << a.shift;
-    const float* w = a.w + (int64_t)l * a.layer_stride + (int64_t)(c * a.share) * a.w_stride + at;
-    int32_t* out = a.kept + ((int64_t)l * a.choices + c) * a.kept_stride + at;
-    for (uint32_t i = tid; i < first; i += THREADS)
-        out[i] = (int32_t)i;
-    for (uint32_t i = tid; i < tail; i += THREADS)
-        out[first + k + i] = (int32_t)(len - tail + i);
+    bool bad;
+    const Pick p = pick_of(a, blockIdx.x, bad);
+    settle(a, p, blockIdx.x, bad, THREADS, status);
+    const uint32_t k = p.k, n = p.n, first = p.first;
     if (k == 0)
         return;
+    const float* w = p.w;
+    int32_t* out = p.out;
     // (head by head, so that reads need not wait for one another)
     auto keys = [&](uint32_t i, auto& x) {
         constexpr int kMany = sizeof(x) / sizeof(x[0]);
         float sum[kMany];
         for (uint32_t g = 0; g < a.share; g++) {
-            const float* from = w + first + g * a.w_stride;
+            const float* from = w + g * a.w_stride;
             float one[kMany];
 #pragma unroll
             for (int r = 0; r < kMany; r++)
@@ -364,38 +445,317 @@ __global__ __launch_bounds__(THREADS) void select_kernel(SelectIn a, uint32_t* s
         choose<kW, 16>(lds, n, k, (int32_t)first, out + first, keys);
     else
         choose_long<kW, THREADS == 1024 ? 4 : 1>(lds, candidate, whose, n, k, (int32_t)first, out + first, [&](uint32_t i, auto& x) {
-            constexpr uint32_t kMany = sizeof(x) / sizeof(x[0]);
-            typedef float v4 __attribute__((ext_vector_type(4), aligned(4)));
-            v4 sum[kMany / 4], more[kMany / 4];
-            auto read = [&](uint32_t g, v4 (&to)[kMany / 4]) {
-                const float* from = w + first + g * a.w_stride;
-#pragma unroll
-                for (uint32_t u = 0; u < kMany / 4; u++) {
-                    const uint32_t p = i + u * 4 * kWave;
-                    to[u] = v4{};
-                    if (p + 3 < n) {
-                        to[u] = *reinterpret_cast<const v4*>(from + p);
-                    } else {
-                        for (uint32_t j = 0; j < 4; j++)
-                            if (p + j < n)
-                                to[u][j] = from[p + j];
-                    }
-                }
-            };
-            read(0, sum);
-            if (a.share > 1)
-                read(1, more);  // (beside the first)
-            for (uint32_t g = 1; g < a.share; g++) {
-                if (g > 1)
-                    read(g, more);
-#pragma unroll
-                for (uint32_t u = 0; u < kMany / 4; u++)
-                    sum[u] = sum[u] + more[u];
-            }
-#pragma unroll
-            for (uint32_t u = 0; u < kMany; u++)
-                x[u] = ordered(sum[u / 4][u % 4]);
+            scores4<false>(a, w, n, i, x);
         });
+}
+
+// Long histories where choices are too few to fill the chip: `parts` workgroups a choice, each
+// with a stretch of its scores, in three passes (the choice itself is the same):
+//   count   each part's scores by their highest digit;
+//   list    every part adds these up, so it knows the digit of the k-th largest, how many
+//           scores of the parts before it are above it and how many agree with it, and lists its
+//           own ones that agree at their place in the choice's list;
+//   place   every part finds the k-th largest among the list, and with it, as it reads its
+//           scores a last time, their places.
+constexpr int kPartThreads = 512, kPartWaves = kPartThreads / kWave;
+constexpr uint32_t kRound = kPartThreads * 16;  // scores that a workgroup has in registers
+
+struct Found {  // by the list pass, of a part
+    uint32_t digit, left, many;  // the choice's
+    uint32_t above, agree;       // of the parts before
+    uint32_t mine;               // that agree, of the part
+};
+struct Split {
+    uint32_t each;   // scores of a part, a multiple of 4
+    uint32_t row;    // workgroups of a (layer, choice)
+    uint32_t* bins;  // [workgroups][kBins]
+    Found* found;    // [workgroups]
+    uint32_t* list;  // [layers][choices], rows of `places`: where a sequence's scores are
+    int64_t places;
+};
+// What a workgroup has: a stretch of a choice's scores, its number among the choice's `parts`.
+struct Part {
+    uint32_t x, part, parts, begin, end;
+    Pick p;
+    bool bad, there;
+};
+// A sequence has one workgroup for `each` of its scores, at least one.  By whole waves.
+__device__ __forceinline__ Part part_of(const SelectIn& a, const Split& d)
+{
+    const uint32_t row = blockIdx.x / d.row;
+    uint32_t j = blockIdx.x % d.row;
+    Part t{};
+    for (uint32_t s0 = 0; s0 < a.n; s0 += kWave) {
+        const uint32_t s = s0 + lane_id();
+        uint32_t parts = 0;
+        if (s < a.n) {
+            bool bad;
+            const Pick p = pick_of(a, s, bad);
+            parts = p.k ? (p.n - 1) / d.each + 1 : 1;
+        }
+        const uint32_t upto = (uint32_t)wave_incl_sum_u64(parts, 0);
+        const uint32_t lane = __popcll(ballot(upto <= j));
+        if (lane < kWave) {
+            t.part = j - (uint32_t)__builtin_amdgcn_readlane(upto - parts, lane);
+            t.parts = (uint32_t)__builtin_amdgcn_readlane(parts, lane);
+            t.x = row * a.n + s0 + lane;
+            t.there = true;
+            break;
+        }
+        j -= (uint32_t)__builtin_amdgcn_readlane(upto, kWave - 1);
+    }
+    if (!t.there)
+        return t;
+    // (tables that overlap, which are malformed, can want more workgroups than there are)
+    const uint32_t room = d.row - (blockIdx.x % d.row - t.part);
+    t.parts = t.parts < room ? t.parts : room;
+    t.p = pick_of(a, t.x, t.bad);
+    const uint64_t begin = (uint64_t)t.part * d.each, end = begin + d.each;
+    t.begin = begin < t.p.n ? (uint32_t)begin : t.p.n;
+    t.end = end < t.p.n ? (uint32_t)end : t.p.n;
+    return t;
+}
+// f(16 scores of a lane, place of its first) by whole waves, kRound scores of the workgroup at a
+// time: x[j] is score i + 256 (j / 4) + j % 4.  Places from the stretch's end on are none.
+template <typename F>
+__device__ __forceinline__ void each_round(const SelectIn& a, const Part& s, F&& f)
+{
+    const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+    for (uint64_t r0 = s.begin; r0 < s.end; r0 += kRound) {
+        uint32_t x[16];
+        const uint32_t i = (uint32_t)r0 + wave * (kRound / kPartWaves) + lane_id() * 4;
+        scores4<true>(a, s.p.w, s.end, i, x);
+        f(x, i);
+    }
+}
+
+__global__ __launch_bounds__(kPartThreads, 4) void select_count_kernel(SelectIn a, Split d, uint32_t* status)
+{
+    __shared__ __attribute__((aligned(16))) uint32_t bins[kBins];
+    const uint32_t tid = threadIdx.x;
+    const Part s = part_of(a, d);
+    if (s.there && s.part == 0)
+        settle(a, s.p, s.x, s.bad, kPartThreads, status);
+    if (s.p.k == 0)
+        return;
+    for (uint32_t b = tid; b < kBins; b += kPartThreads)
+        bins[b] = 0;
+    __syncthreads();
+    each_round(a, s, [&](const uint32_t (&v)[16], uint32_t i) {
+#pragma unroll
+        for (uint32_t j = 0; j < 16; j++)
+            if (i + j / 4 * 4 * kWave + j % 4 < s.end)
+                atomicAdd(&bins[v[j] >> digit_shift(0)], 1u);
+    });
+    __syncthreads();
+    uint32_t* to = d.bins + (uint64_t)blockIdx.x * kBins;
+    for (uint32_t b = tid; b < kBins; b += kPartThreads)
+        to[b] = bins[b];
+}
+
+__global__ __launch_bounds__(kPartThreads, 4) void select_list_kernel(SelectIn a, Split d)
+{
+    constexpr uint32_t kPer = kBins / kPartThreads;
+    static_assert(kPer == 4);
+    __shared__ SelectLds<kPartWaves> lds;
+    const uint32_t tid = threadIdx.x;
+    const Part s = part_of(a, d);
+    if (s.p.k == 0)
+        return;
+    const Pick& p = s.p;
+    const uint4* from = reinterpret_cast<const uint4*>(d.bins + (uint64_t)(blockIdx.x - s.part) * kBins) + tid;
+    uint32_t all[4] = {}, before[4] = {};
+#pragma unroll 8
+    for (uint32_t q = 0; q < s.parts; q++) {
+        const uint4 v = from[q * (kBins / 4)];
+        const uint32_t one[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+        for (int j = 0; j < 4; j++) {
+            all[j] += one[j];
+            before[j] += q < s.part ? one[j] : 0;
+        }
+    }
+#pragma unroll
+    for (int j = 0; j < 4; j++)
+        lds.bins[0][tid * 4 + j] = all[j];
+    if (tid == 0)
+        lds.held = lds.up[0] = lds.equal[0] = lds.digit = lds.left = 0;
+    __syncthreads();
+    find_bin(lds, lds.bins[0], p.k);
+    const uint32_t digit = lds.digit, left = lds.left;
+    uint32_t above = 0;
+#pragma unroll
+    for (int j = 0; j < 4; j++) {
+        above += tid * 4 + j > digit ? before[j] : 0;
+        if (tid * 4 + j == digit)
+            lds.equal[0] = before[j];
+    }
+    above = (uint32_t)wave_incl_sum_u64(above, 0);
+    if (lane_id() == kWave - 1)
+        atomicAdd(&lds.up[0], above);
+    __syncthreads();
+    const uint32_t agree = lds.equal[0];
+    if (tid == 0)
+        d.found[blockIdx.x] = Found{digit, left, lds.bins[0][digit], lds.up[0], agree, d.bins[(uint64_t)blockIdx.x * kBins + digit]};
+    uint32_t* list = d.list + (int64_t)(s.x / a.n) * d.places + p.at;
+    const uint64_t below = (1ull << lane_id()) - 1;
+    each_round(a, s, [&](const uint32_t (&v)[16], uint32_t i) {
+#pragma unroll
+        for (uint32_t j = 0; j < 16; j++) {
+            const uint64_t those = ballot(i + j / 4 * 4 * kWave + j % 4 < s.end && v[j] >> digit_shift(0) == digit);
+            if (those == 0)
+                continue;
+            uint32_t at = 0;
+            if (lane_id() == 0)
+                at = atomicAdd(&lds.held, (uint32_t)__popcll(those));
+            at = agree + __builtin_amdgcn_readfirstlane(at) + __popcll(those & below);
+            if ((those >> lane_id()) & 1 && at < p.n)
+                list[at] = v[j];
+        }
+    });
+}
+
+__global__ __launch_bounds__(kPartThreads, 4) void select_place_kernel(SelectIn a, Split d)
+{
+    __shared__ SelectLds<kPartWaves> lds;
+    __shared__ uint32_t ups[2][kPartWaves], sames[2][kPartWaves];
+    const uint32_t tid = threadIdx.x;
+    const uint32_t wave = __builtin_amdgcn_readfirstlane(tid / kWave), lane = lane_id();
+    const Part s = part_of(a, d);
+    if (s.p.k == 0)
+        return;
+    const Pick& p = s.p;
+    const Found f = d.found[blockIdx.x];
+    const uint32_t* list = d.list + (int64_t)(s.x / a.n) * d.places + p.at;
+    const uint32_t many = f.many < p.n ? f.many : p.n;
+    uint32_t found = f.digit << digit_shift(0), known = digit_mask(0) << digit_shift(0), left = f.left;
+    for (uint32_t b = tid; b < 2 * kBins; b += kPartThreads)
+        lds.bins[0][b] = 0;
+    if (tid == 0)
+        lds.held = lds.up[0] = lds.equal[0] = lds.digit = lds.left = 0;
+    __syncthreads();
+    for (int e = 1; e < kDigits; e++) {
+        uint32_t* bins = lds.bins[e % 2];
+        for (uint32_t i = tid; i < many; i += kPartThreads) {
+            const uint32_t v = list[i];
+            if ((v & known) == found)
+                atomicAdd(&bins[(v >> digit_shift(e)) & digit_mask(e)], 1u);
+        }
+        __syncthreads();
+        find_bin(lds, bins, left);
+        found |= lds.digit << digit_shift(e);
+        known |= digit_mask(e) << digit_shift(e);
+        left = lds.left;
+    }
+    // those before the part: above it, and equal; and equal in the part
+    const uint32_t own = f.agree + f.mine < many ? f.agree + f.mine : many;
+    for (uint32_t i = tid; i < own; i += kPartThreads) {
+        const uint32_t v = list[i];
+        if (v == found)
+            atomicAdd(i < f.agree ? &lds.held : &lds.equal[0], 1u);
+        else if (v > found && i < f.agree)
+            atomicAdd(&lds.up[0], 1u);
+    }
+    __syncthreads();
+    const uint32_t equal = lds.held, stay = equal < left ? equal : left;
+    uint32_t above = f.above + lds.up[0] + stay, turn = 0;
+    // of the part's equals all stay, or none does, or the first ones do
+    const bool all = equal + lds.equal[0] <= left, some = !all && equal < left;
+    const uint32_t least = all ? found : found + 1;
+    uint32_t equals = left - stay;  // that stay yet, where some do
+    int32_t* out = p.out + p.first;
+    const uint64_t below = (1ull << lane) - 1;
+    auto place = [&](auto one_by_one) {
+        each_round(a, s, [&](uint32_t (&v)[16], uint32_t i) {
+            auto there = [&](uint32_t j) { return i + j / 4 * 4 * kWave + j % 4 < s.end; };
+            if constexpr (decltype(one_by_one)::value) {
+                // equals by their places: those that stay are raised, the workgroup's waves in turn
+                uint32_t same = 0;
+#pragma unroll
+                for (uint32_t j = 0; j < 16; j++)
+                    same += __popcll(ballot(there(j) && v[j] == found));
+                if (lane == 0)
+                    sames[turn][wave] = same;
+                __syncthreads();
+                uint32_t before = 0, sum = 0;
+                for (uint32_t w = 0; w < kPartWaves; w++) {
+                    before += w < wave ? sames[turn][w] : 0;
+                    sum += sames[turn][w];
+                }
+#pragma unroll
+                for (uint32_t u = 0; u < 16; u += 4) {
+                    uint32_t mine = before;
+#pragma unroll
+                    for (uint32_t j = u; j < u + 4; j++) {
+                        const uint64_t is = ballot(there(j) && v[j] == found);
+                        mine += __popcll(is & below);
+                        before += __popcll(is);
+                    }
+#pragma unroll
+                    for (uint32_t j = u; j < u + 4; j++)
+                        if (v[j] == found) {
+                            v[j] += mine < equals;
+                            mine += there(j);
+                        }
+                }
+                equals -= sum < equals ? sum : equals;
+            }
+            uint32_t up = 0;
+#pragma unroll
+            for (uint32_t j = 0; j < 16; j++)
+                up += __popcll(ballot(there(j) && v[j] >= least));
+            if (lane == 0)
+                ups[turn][wave] = up;
+            __syncthreads();
+            // what the workgroup had and the waves before have, then in the order of places: steps of
+            // 256, four neighbours a lane
+            up = above;
+            for (uint32_t w = 0; w < kPartWaves; w++) {
+                up += w < wave ? ups[turn][w] : 0;
+                above += ups[turn][w];
+            }
+            turn ^= 1;  // (the next round's words are others: one barrier for them)
+#pragma unroll
+            for (uint32_t u = 0; u < 16; u += 4) {
+                uint32_t at = up;
+#pragma unroll
+                for (uint32_t j = u; j < u + 4; j++) {
+                    const uint64_t those = ballot(there(j) && v[j] >= least);
+                    at += __popcll(those & below);
+                    up += __popcll(those);
+                }
+#pragma unroll
+                for (uint32_t j = u; j < u + 4; j++)
+                    if (there(j) && v[j] >= least) {
+                        if (at < p.k)
+                            out[at] = (int32_t)(p.first + i + u / 4 * 4 * kWave + j % 4);
+                        at++;
+                    }
+            }
+        });
+    };
+    if (some)
+        place(std::true_type{});
+    else
+        place(std::false_type{});
+}
+
+constexpr uint64_t kSplitArea = 1ull << 29;  // bytes of the work area, at most
+
+// Scores of a part where choices are split (0: one kernel has them).  By itself a choice takes a
+// time that goes by its length, split one that goes by all lengths, and two launches more.  us, by
+// itself and split, of choices of 9,000 scores (some kept in registers): 1 11 and 21, 128 12 and
+// 29; of 32,768: 16 31 and 24, 64 31 and 34, 128 36 and 48; of 65,536: 16 53 and 30, 128 61 and
+// 61, 192 64 and 74; of 131,072: 1 95 and 25, 64 109 and 53, 128 110 and 82, 224 114 and 105.
+uint32_t part_scores(const dm_ctx* c, uint64_t choices, uint64_t rows, uint64_t places, uint64_t n)
+{
+    constexpr uint64_t kMean = 24576, kLike = 512;
+    if (places <= kMean * n || choices * kLike * n > places || choices >= c->n_cu || rows * places >= (1ull << 40))
+        return 0;
+    // two workgroups a compute unit, with half a part more for every choice
+    const uint64_t wanted = 2 * c->n_cu - choices / 2;
+    const uint64_t each = rows * places / wanted;
+    return (uint32_t)(each < 4096 ? 4096 : each / 4 * 4 + 4);
 }
 
 struct GatherIn {
@@ -536,7 +896,28 @@ hipError_t evict_select(dm_ctx* c, const dm_page_tables& t, const dm_select_args
     const uint64_t grid = t.n * a.layers * a.choices;
     if (grid > 0x7FFFFFFFull)
         return hipErrorInvalidValue;
-    const uint64_t mean = t.entries * c->cfg.block_size / t.n;
+    const uint64_t places = t.entries * c->cfg.block_size, mean = places / t.n;
+    const uint64_t rows = (uint64_t)a.layers * a.choices;
+    const uint32_t each = part_scores(c, grid, rows, places, t.n);
+    const uint64_t row = each ? places / each + t.n : 0, all = row * rows;
+    const uint64_t bins = all * kBins * 4, found = (all * sizeof(Found) + 15) / 16 * 16;
+    if (each && bins + found + rows * places * 4 <= kSplitArea) {
+        hipError_t e;
+        char* at = static_cast<char*>(scratch_get(c, kSlotPages, bins + found + rows * places * 4, &e));
+        if (!at)
+            return e;
+        Split d;
+        d.each = each;
+        d.row = (uint32_t)row;
+        d.bins = reinterpret_cast<uint32_t*>(at);
+        d.found = reinterpret_cast<Found*>(at + bins);
+        d.list = reinterpret_cast<uint32_t*>(at + bins + found);
+        d.places = (int64_t)places;
+        select_count_kernel<<<(uint32_t)all, kPartThreads, 0, c->stream>>>(a, d, c->d_status);
+        select_list_kernel<<<(uint32_t)all, kPartThreads, 0, c->stream>>>(a, d);
+        select_place_kernel<<<(uint32_t)all, kPartThreads, 0, c->stream>>>(a, d);
+        return hipGetLastError();
+    }
     if (mean <= 2048)
         select_kernel<256><<<(uint32_t)grid, 256, 0, c->stream>>>(a, c->d_status);
     else if (mean <= 6144)

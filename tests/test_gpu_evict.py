@@ -131,6 +131,66 @@ def test_long_histories(lens):
     Histories(64, lens, layers=1, heads=2, seed=5, values=[0.5]).check([n // 2 for n in lens])
 
 
+@pytest.mark.parametrize("share", [1, 2])
+@pytest.mark.parametrize("lens", [[40_000], [24_577, 24_640, 30_001], [100_001, 12, 50_000, 0, 90_000], [150_000, 3]])
+def test_choices_of_several_workgroups(lens, share):
+    """Few and long choices: their parts' borders, equals that reach over them, short sequences between."""
+    _say("split", lens, share)
+    b = Histories(32, lens, layers=2, heads=2, seed=11)
+    for budget in ([n // 2 for n in lens], [min(n, 777) for n in lens], [max(0, n - 1) for n in lens], [0 for _ in lens]):
+        b.check(budget, sink=3, recent=65, share=share, room=list(range(len(lens))))
+    for values in ([0.5], [0.0, -0.0], [1.0, 2.0, math.nan, math.inf, -math.inf]):
+        Histories(32, lens, layers=1, heads=2, seed=12, values=values).check([n * 5 // 8 for n in lens], share=share)
+
+
+def test_long_choices_of_one_workgroup():
+    """Many of them, and one long among short ones."""
+    _say("one workgroup")
+    Histories(16, [26_000] * 4, layers=4, heads=16, seed=13).check([5000, 25_999, 1, 13_000], sink=1, recent=9)
+    lens = [70_000] + [200] * 30
+    for values in (None, [0.5]):
+        Histories(16, lens, layers=1, heads=2, seed=14, values=values).check([n // 3 for n in lens], recent=5)
+
+
+def test_a_split_choice_in_a_graph():
+    """Its work area is the context's: the same replays before and after a larger call has grown it."""
+    _say("split graph")
+    pk, _ = engine(64)
+    b = Histories(64, [60_000, 30_000], layers=2, heads=2, seed=15)
+    budget = [4000, 29_000]
+    want = b.expected(budget)
+    tables, w, bud = b.tables(), dev(b.w), dev(np.array(budget, np.int64))
+    kept = torch.full((2, 2, b.rows + 1), -7, dtype=torch.int32, device="cuda")
+    keep, grow = torch.zeros(2, dtype=torch.int64, device="cuda"), torch.zeros(2, dtype=torch.int64, device="cuda")
+
+    def run(eng):
+        eng.evict_select(tables, w, bud, None, kept, keep, grow)
+
+    st = torch.cuda.Stream()
+    own = pk.DualMap(dict(block=64, key_blocks=1, seeds=(1, 2), vnodes=1, max_slots=1, index_log2_slots=4), stream=st)
+    torch.cuda.synchronize()
+    with torch.cuda.stream(st):
+        run(own)
+    st.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=st):
+        run(own)
+    for turn in range(4):
+        kept.fill_(-7)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert np.array_equal(kept.cpu().numpy(), want), turn
+        if turn == 1:
+            more = Histories(64, [200_000, 100_000], layers=2, heads=2, seed=16)
+            with torch.cuda.stream(st):
+                got, _, _ = more.select([1000, 2000], eng=own)
+            assert np.array_equal(got, more.expected([1000, 2000]))
+            torch.cuda.synchronize()
+    own.sync()
+    own.close()
+
+
 def test_many_short_histories():
     r = np.random.default_rng(1)
     lens = r.integers(0, 200, size=700)

@@ -161,6 +161,35 @@ def scenario_weights_area(x):
         x.L.dm_destroy(c.h)
 
 
+def scenario_select_area(x):
+    """Few and long choices: counts and a list, 2^29 bytes at the most; none for others; growth under capture is refused."""
+    held, capturing = x.word("fake_bytes"), x.word("fake_capturing", C.c_int)
+    for n, entries, layers, heads, some in ((4, 400, 2, 4, False), (4, 8000, 2, 4, True), (1, 1537, 1, 1, True), (1, 1536, 1, 1, False),
+                                            (2, 65_536, 4, 8, True), (2, 65_536, 32, 8, False), (1, 1 << 22, 1, 2, False)):
+        c = Calls(x)
+        before = held.value
+        rows = entries * 16
+        kw = dict(tables=dict(n=n, entries=entries), w_stride=rows, w_layer_stride=rows * heads, kept_stride=rows, layers=layers,
+                  kv_heads=heads, share=1)
+        assert c.select(**kw) == x.pk.DM_OK
+        got = held.value - before
+        if some:
+            assert layers * heads * rows * 4 < got <= (1 << 29) + 4096, (n, entries, got)
+            capturing.value = 1
+            assert c.select(**kw) == x.pk.DM_OK
+            kw.update(tables=dict(n=n, entries=2 * entries), w_stride=2 * rows, w_layer_stride=2 * rows * heads, kept_stride=2 * rows)
+            grown = c.select(**kw)
+            capturing.value = 0
+            assert grown == x.pk.DM_EDEVICE and b"capture" in x.L.dm_last_error(c.h)
+        else:
+            assert got == 0, (n, entries, got)
+        x.L.dm_destroy(c.h)
+
+
+def test_select_work_area(fake):  # noqa: F811
+    _child(fake, "select_area")
+
+
 def test_weights_work_area(fake):  # noqa: F811
     _child(fake, "weights_area")
 
