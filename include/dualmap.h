@@ -766,10 +766,11 @@ typedef struct {
  * of sequence s at off[s] * B + i of a row; nothing else of kept is written.
  * Exact and the same every time.  The few choices of long histories (means of more
  * than 24,576 tokens) are split over workgroups: the context's work area, which grows
- * as dm_attn's, then holds a number for each of their scores and 8 KiB for each
- * workgroup, not more than 2^29 bytes (choices that would need more are not split).
- * page is not read.  A malformed table or a
- * negative budget is reported (DM_EINVAL) and evicts nothing of its sequence. */
+ * as dm_attn's, then holds a number (with share > 1 two) for each of their scores and
+ * 8 KiB for each workgroup, not more than 2^29 bytes (choices that would need more
+ * are not split).  page is not read.  A malformed table or a negative budget is
+ * reported (DM_EINVAL) and evicts nothing of its sequence; where off decreases, others
+ * than that sequence have no defined result either. */
 dm_status dm_evict_select(dm_ctx* ctx, const dm_page_tables* tables, const dm_select_args* args);
 
 /* kept, budget, share: dm_evict_select's.  w and w_to: NULL, or the weights by

@@ -853,6 +853,8 @@ class DualMap:
             off, src, keep = off.data_ptr(), src.data_ptr(), keep.data_ptr()
         if prev is not None:
             pp, ps, room = self._collected(prev, "prev", kv.kv_heads)
+            if off and pp == wp:
+                raise ValueError("prev may be w only where the tables are the same")
             if not off and room < plan.entries * kv.block:
                 raise ValueError("prev needs a place for each token of the tables' entries")
         if not 0 <= last < 1 << 32:

@@ -471,6 +471,7 @@ struct Split {
     uint32_t* bins;  // [workgroups][kBins]
     Found* found;    // [workgroups]
     uint32_t* list;  // [layers][choices], rows of `places`: where a sequence's scores are
+    uint32_t* sums;  // alike, or null: the scores of several heads, left by the first pass
     int64_t places;
 };
 // What a workgroup has: a stretch of a choice's scores, its number among the choice's `parts`.
@@ -517,14 +518,37 @@ __device__ __forceinline__ Part part_of(const SelectIn& a, const Split& d)
 }
 // f(16 scores of a lane, place of its first) by whole waves, kRound scores of the workgroup at a
 // time: x[j] is score i + 256 (j / 4) + j % 4.  Places from the stretch's end on are none.
-template <typename F>
-__device__ __forceinline__ void each_round(const SelectIn& a, const Part& s, F&& f)
+template <bool FIRST, typename F>
+__device__ __forceinline__ void each_round(const SelectIn& a, const Split& d, const Part& s, F&& f)
 {
     const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+    // (16 bytes at a time: a sequence's place and a part's begin are multiples of 4)
+    uint32_t* sums = d.sums ? d.sums + (int64_t)(s.x / a.n) * d.places + s.p.at : nullptr;
     for (uint64_t r0 = s.begin; r0 < s.end; r0 += kRound) {
         uint32_t x[16];
         const uint32_t i = (uint32_t)r0 + wave * (kRound / kPartWaves) + lane_id() * 4;
-        scores4<true>(a, s.p.w, s.end, i, x);
+        if (FIRST || !sums) {
+            scores4<true>(a, s.p.w, s.end, i, x);
+            if (FIRST && sums)
+#pragma unroll
+                for (uint32_t u = 0; u < 16; u += 4)
+                    if (i + u * kWave < s.end)
+                        *reinterpret_cast<uint4*>(sums + i + u * kWave) = uint4{x[u], x[u + 1], x[u + 2], x[u + 3]};
+        } else {
+            uint4 v[4];
+#pragma unroll
+            for (uint32_t u = 0; u < 4; u++) {
+                const uint32_t at = i + u * 4 * kWave;
+                v[u] = *reinterpret_cast<const uint4*>(sums + (at < s.end ? at : s.begin));
+            }
+#pragma unroll
+            for (uint32_t u = 0; u < 4; u++) {
+                x[u * 4] = v[u].x;
+                x[u * 4 + 1] = v[u].y;
+                x[u * 4 + 2] = v[u].z;
+                x[u * 4 + 3] = v[u].w;
+            }
+        }
         f(x, i);
     }
 }
@@ -541,7 +565,7 @@ __global__ __launch_bounds__(kPartThreads, 4) void select_count_kernel(SelectIn 
     for (uint32_t b = tid; b < kBins; b += kPartThreads)
         bins[b] = 0;
     __syncthreads();
-    each_round(a, s, [&](const uint32_t (&v)[16], uint32_t i) {
+    each_round<true>(a, d, s, [&](const uint32_t (&v)[16], uint32_t i) {
 #pragma unroll
         for (uint32_t j = 0; j < 16; j++)
             if (i + j / 4 * 4 * kWave + j % 4 < s.end)
@@ -599,7 +623,7 @@ __global__ __launch_bounds__(kPartThreads, 4) void select_list_kernel(SelectIn a
         d.found[blockIdx.x] = Found{digit, left, lds.bins[0][digit], lds.up[0], agree, d.bins[(uint64_t)blockIdx.x * kBins + digit]};
     uint32_t* list = d.list + (int64_t)(s.x / a.n) * d.places + p.at;
     const uint64_t below = (1ull << lane_id()) - 1;
-    each_round(a, s, [&](const uint32_t (&v)[16], uint32_t i) {
+    each_round<false>(a, d, s, [&](const uint32_t (&v)[16], uint32_t i) {
 #pragma unroll
         for (uint32_t j = 0; j < 16; j++) {
             const uint64_t those = ballot(i + j / 4 * 4 * kWave + j % 4 < s.end && v[j] >> digit_shift(0) == digit);
@@ -666,7 +690,7 @@ __global__ __launch_bounds__(kPartThreads, 4) void select_place_kernel(SelectIn 
     int32_t* out = p.out + p.first;
     const uint64_t below = (1ull << lane) - 1;
     auto place = [&](auto one_by_one) {
-        each_round(a, s, [&](uint32_t (&v)[16], uint32_t i) {
+        each_round<false>(a, d, s, [&](uint32_t (&v)[16], uint32_t i) {
             auto there = [&](uint32_t j) { return i + j / 4 * 4 * kWave + j % 4 < s.end; };
             if constexpr (decltype(one_by_one)::value) {
                 // equals by their places: those that stay are raised, the workgroup's waves in turn
@@ -901,9 +925,11 @@ hipError_t evict_select(dm_ctx* c, const dm_page_tables& t, const dm_select_args
     const uint32_t each = part_scores(c, grid, rows, places, t.n);
     const uint64_t row = each ? places / each + t.n : 0, all = row * rows;
     const uint64_t bins = all * kBins * 4, found = (all * sizeof(Found) + 15) / 16 * 16;
-    if (each && bins + found + rows * places * 4 <= kSplitArea) {
+    const uint64_t list = rows * places * 4, area = bins + found + list;
+    const uint64_t sums = a.share > 1 && area + list <= kSplitArea ? list : 0;
+    if (each && area <= kSplitArea) {
         hipError_t e;
-        char* at = static_cast<char*>(scratch_get(c, kSlotPages, bins + found + rows * places * 4, &e));
+        char* at = static_cast<char*>(scratch_get(c, kSlotPages, area + sums, &e));
         if (!at)
             return e;
         Split d;
@@ -912,6 +938,7 @@ hipError_t evict_select(dm_ctx* c, const dm_page_tables& t, const dm_select_args
         d.bins = reinterpret_cast<uint32_t*>(at);
         d.found = reinterpret_cast<Found*>(at + bins);
         d.list = reinterpret_cast<uint32_t*>(at + bins + found);
+        d.sums = sums ? reinterpret_cast<uint32_t*>(at + area) : nullptr;
         d.places = (int64_t)places;
         select_count_kernel<<<(uint32_t)all, kPartThreads, 0, c->stream>>>(a, d, c->d_status);
         select_list_kernel<<<(uint32_t)all, kPartThreads, 0, c->stream>>>(a, d);

@@ -357,3 +357,42 @@ def test_refusals():
     with pytest.raises(pk.DMError):
         e.sync()
     assert bool((w == 7).all())
+
+
+def test_carried_in_place_by_other_tables():
+    """w itself is what was carried by the same tables only: by others, places would be read after they are written."""
+    pk, e = engine(16)
+    b = Collected(16, [(1, 40), (2, 90)], seed=1)
+    kv = pk.KVPages(b.k.cuda(), b.v.cuda())
+    q = b.qrows.cuda().unflatten(1, (8, 128)).contiguous()
+    plan = e.attn_plan(kv, b.tables(), b.dev(b.q_off), 3, 8)
+    w = torch.full((2, b.rows), 7.0, device="cuda")
+    with pytest.raises(ValueError, match="same"):
+        e.attn_weights(plan, 0, q, 0.1, b.far().cuda(), w, prev=(w, b.dev(b.prev_off), b.dev(b.src), b.dev(b.keep)))
+    e.sync()
+    assert bool((w == 7).all())
+
+
+def test_one_plan_for_attention_weights_and_other_layers():
+    """Two layers' weights by one plan in turn, twice: the same bits, each its own layer's."""
+    pk, e = engine(16)
+    b = Collected(16, [(3, 70), (40, 90), (1, 200)], seed=6, layers=2)
+    kv = pk.KVPages(b.k.cuda(), b.v.cuda())
+    T = int(b.q_off[-1])
+    q = b.qrows.cuda().unflatten(1, (8, 128)).contiguous()
+    plan = e.attn_plan(kv, b.tables(), b.dev(b.q_off), T, 8)
+    out, lse = torch.zeros_like(q), [torch.zeros((T, 8), device="cuda") for _ in range(2)]
+    got = []
+    for turn in range(2):
+        for layer in (0, 1):
+            e.attn(plan, layer, q, b.scale(), out, lse[layer])
+            w = torch.zeros((2, b.rows), device="cuda")
+            e.attn_weights(plan, layer, q, b.scale(), lse[layer], w)
+            got.append(w)
+    e.sync()
+    assert torch.equal(got[0], got[2]) and torch.equal(got[1], got[3]) and not torch.equal(got[0], got[1])
+    # every query gives a weight of 1 to the keys that it sees, each off by 2^-20 of the sum of its absolute products and of
+    # its log-sum-exp, which are below 32 together
+    for w in got[:2]:
+        total = float(w.double().sum())
+        assert abs(total - 8 * T) <= 8 * T * 2.0 ** -15, total
