@@ -9,7 +9,7 @@
 // equals stay (the first ones).  A workgroup takes a (layer, choice, sequence); its scores
 // stay in registers where they fit; where choices are few and long, several take one.  Bound by
 // reading the weights, three times where they are long (four histories of 27,000 to 124,000
-// tokens, 8 layers, pairs of 8 heads: 82 us, 88 with a workgroup a choice; 86 MB a pass take 17),
+// tokens, 8 layers, pairs of 8 heads: 70 us, 88 with a workgroup a choice; 86 MB a pass take 17),
 // and for short sequences by the passes' barriers (16 chats, 4 layers, 8 heads: 12 us).
 //
 // The move takes a page of the new tables a workgroup: a row's token, that token's page, the
@@ -368,7 +368,7 @@ __device__ __forceinline__ void scores4(const SelectIn& a, const float* w, uint3
     typedef float v4 __attribute__((ext_vector_type(4), aligned(4)));
     v4 sum[MANY / 4], more[MANY / 4];
     // (waves within `end` read without a branch between their reads: 78 us for the three kernels
-    // that split, 88 without; one kernel by itself has no registers for it, 88 and 100)
+    // that split, 99 without; one kernel by itself has no registers for it, 88 without and 100)
     const bool whole = WHOLE && __builtin_amdgcn_readfirstlane(i) + MANY * kWave <= end;
     auto read = [&](uint32_t g, v4 (&to)[MANY / 4]) {
         const float* from = w + g * a.w_stride;
@@ -449,14 +449,16 @@ __global__ __launch_bounds__(THREADS) void select_kernel(SelectIn a, uint32_t* s
         });
 }
 
-// Long histories where choices are too few to fill the chip: `parts` workgroups a choice, each
+// Long histories where choices are too few to fill the chip: several workgroups a choice, each
 // with a stretch of its scores, in three passes (the choice itself is the same):
-//   count   each part's scores by their highest digit;
+//   count   each part's scores by their highest digit; sums of several heads are left for the
+//           other passes (82 to 73 us);
 //   list    every part adds these up, so it knows the digit of the k-th largest, how many
 //           scores of the parts before it are above it and how many agree with it, and lists its
 //           own ones that agree at their place in the choice's list;
 //   place   every part finds the k-th largest among the list, and with it, as it reads its
 //           scores a last time, their places.
+// The last two read a round ahead, the first one beside the counts and the list (73 to 70 us).
 constexpr int kPartThreads = 512, kPartWaves = kPartThreads / kWave;
 constexpr uint32_t kRound = kPartThreads * 16;  // scores that a workgroup has in registers
 
@@ -471,7 +473,7 @@ struct Split {
     uint32_t* bins;  // [workgroups][kBins]
     Found* found;    // [workgroups]
     uint32_t* list;  // [layers][choices], rows of `places`: where a sequence's scores are
-    uint32_t* sums;  // alike, or null: the scores of several heads, left by the first pass
+    uint32_t* sums;  // alike, or null (one head a choice): scores, left by the first pass
     int64_t places;
 };
 // What a workgroup has: a stretch of a choice's scores, its number among the choice's `parts`.
@@ -516,42 +518,60 @@ __device__ __forceinline__ Part part_of(const SelectIn& a, const Split& d)
     t.end = end < t.p.n ? (uint32_t)end : t.p.n;
     return t;
 }
-// f(16 scores of a lane, place of its first) by whole waves, kRound scores of the workgroup at a
-// time: x[j] is score i + 256 (j / 4) + j % 4.  Places from the stretch's end on are none.
-template <bool FIRST, typename F>
-__device__ __forceinline__ void each_round(const SelectIn& a, const Split& d, const Part& s, F&& f)
+// A lane's first place of a round, of the workgroup's kRound; x[j] is score i + 256 (j / 4) + j % 4.
+// Places from the stretch's end on are none.
+__device__ __forceinline__ uint32_t place_of(uint64_t r0)
 {
     const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
-    // (16 bytes at a time: a sequence's place and a part's begin are multiples of 4)
-    uint32_t* sums = d.sums ? d.sums + (int64_t)(s.x / a.n) * d.places + s.p.at : nullptr;
-    for (uint64_t r0 = s.begin; r0 < s.end; r0 += kRound) {
-        uint32_t x[16];
-        const uint32_t i = (uint32_t)r0 + wave * (kRound / kPartWaves) + lane_id() * 4;
-        if (FIRST || !sums) {
-            scores4<true>(a, s.p.w, s.end, i, x);
-            if (FIRST && sums)
-#pragma unroll
-                for (uint32_t u = 0; u < 16; u += 4)
-                    if (i + u * kWave < s.end)
-                        *reinterpret_cast<uint4*>(sums + i + u * kWave) = uint4{x[u], x[u + 1], x[u + 2], x[u + 3]};
-        } else {
-            uint4 v[4];
-#pragma unroll
-            for (uint32_t u = 0; u < 4; u++) {
-                const uint32_t at = i + u * 4 * kWave;
-                v[u] = *reinterpret_cast<const uint4*>(sums + (at < s.end ? at : s.begin));
-            }
-#pragma unroll
-            for (uint32_t u = 0; u < 4; u++) {
-                x[u * 4] = v[u].x;
-                x[u * 4 + 1] = v[u].y;
-                x[u * 4 + 2] = v[u].z;
-                x[u * 4 + 3] = v[u].w;
-            }
-        }
-        f(x, i);
-    }
+    return (uint32_t)r0 + wave * (kRound / kPartWaves) + lane_id() * 4;
 }
+
+// The second and third pass over a stretch: 16 bytes a lane at a time (a sequence's place and a
+// part's begin are multiples of 4), a round ahead.  start() asks for the first round.
+struct Rounds {
+    typedef uint32_t v4 __attribute__((ext_vector_type(4), aligned(4)));
+    const uint32_t* from;  // sums, or the one head's weights
+    uint32_t begin, end;
+    bool sums;
+    v4 next[4];
+
+    __device__ __forceinline__ Rounds(const SelectIn& a, const Split& d, const Part& s)
+        : from(d.sums ? d.sums + (int64_t)(s.x / a.n) * d.places + s.p.at : reinterpret_cast<const uint32_t*>(s.p.w)),
+          begin(s.begin), end(s.end), sums(d.sums)
+    {
+    }
+    __device__ __forceinline__ void read(uint64_t r0)
+    {
+        const uint32_t i = place_of(r0);
+        if (__builtin_amdgcn_readfirstlane(i) + 16 * kWave <= end) {
+#pragma unroll
+            for (uint32_t u = 0; u < 4; u++)
+                next[u] = *reinterpret_cast<const v4*>(from + i + u * 4 * kWave);
+            return;
+        }
+#pragma unroll
+        for (uint32_t u = 0; u < 4; u++)
+#pragma unroll
+            for (uint32_t j = 0; j < 4; j++) {
+                const uint32_t at = i + u * 4 * kWave + j;
+                next[u][j] = at < end ? from[at] : 0;
+            }
+    }
+    __device__ __forceinline__ void start() { read(begin); }
+    template <typename F>
+    __device__ __forceinline__ void each(F&& f)
+    {
+        for (uint64_t r0 = begin; r0 < end; r0 += kRound) {
+            uint32_t x[16];
+#pragma unroll
+            for (uint32_t j = 0; j < 16; j++)
+                x[j] = sums ? next[j / 4][j % 4] : ordered(__builtin_bit_cast(float, (uint32_t)next[j / 4][j % 4]));
+            if (r0 + kRound < end)
+                read(r0 + kRound);
+            f(x, place_of(r0));
+        }
+    }
+};
 
 __global__ __launch_bounds__(kPartThreads, 4) void select_count_kernel(SelectIn a, Split d, uint32_t* status)
 {
@@ -565,12 +585,21 @@ __global__ __launch_bounds__(kPartThreads, 4) void select_count_kernel(SelectIn 
     for (uint32_t b = tid; b < kBins; b += kPartThreads)
         bins[b] = 0;
     __syncthreads();
-    each_round<true>(a, d, s, [&](const uint32_t (&v)[16], uint32_t i) {
+    uint32_t* sums = d.sums ? d.sums + (int64_t)(s.x / a.n) * d.places + s.p.at : nullptr;
+    for (uint64_t r0 = s.begin; r0 < s.end; r0 += kRound) {
+        const uint32_t i = place_of(r0);
+        uint32_t v[16];
+        scores4<true>(a, s.p.w, s.end, i, v);
+        if (sums)  // (up to 3 places past the last score, in the sequence's last page)
+#pragma unroll
+            for (uint32_t u = 0; u < 16; u += 4)
+                if (i + u * kWave < s.end)
+                    *reinterpret_cast<uint4*>(sums + i + u * kWave) = uint4{v[u], v[u + 1], v[u + 2], v[u + 3]};
 #pragma unroll
         for (uint32_t j = 0; j < 16; j++)
             if (i + j / 4 * 4 * kWave + j % 4 < s.end)
                 atomicAdd(&bins[v[j] >> digit_shift(0)], 1u);
-    });
+    }
     __syncthreads();
     uint32_t* to = d.bins + (uint64_t)blockIdx.x * kBins;
     for (uint32_t b = tid; b < kBins; b += kPartThreads)
@@ -587,6 +616,8 @@ __global__ __launch_bounds__(kPartThreads, 4) void select_list_kernel(SelectIn a
     if (s.p.k == 0)
         return;
     const Pick& p = s.p;
+    Rounds rounds(a, d, s);
+    rounds.start();  // (beside the counts)
     const uint4* from = reinterpret_cast<const uint4*>(d.bins + (uint64_t)(blockIdx.x - s.part) * kBins) + tid;
     uint32_t all[4] = {}, before[4] = {};
 #pragma unroll 8
@@ -623,7 +654,7 @@ __global__ __launch_bounds__(kPartThreads, 4) void select_list_kernel(SelectIn a
         d.found[blockIdx.x] = Found{digit, left, lds.bins[0][digit], lds.up[0], agree, d.bins[(uint64_t)blockIdx.x * kBins + digit]};
     uint32_t* list = d.list + (int64_t)(s.x / a.n) * d.places + p.at;
     const uint64_t below = (1ull << lane_id()) - 1;
-    each_round<false>(a, d, s, [&](const uint32_t (&v)[16], uint32_t i) {
+    rounds.each([&](const uint32_t (&v)[16], uint32_t i) {
 #pragma unroll
         for (uint32_t j = 0; j < 16; j++) {
             const uint64_t those = ballot(i + j / 4 * 4 * kWave + j % 4 < s.end && v[j] >> digit_shift(0) == digit);
@@ -649,6 +680,8 @@ __global__ __launch_bounds__(kPartThreads, 4) void select_place_kernel(SelectIn 
     if (s.p.k == 0)
         return;
     const Pick& p = s.p;
+    Rounds rounds(a, d, s);
+    rounds.start();
     const Found f = d.found[blockIdx.x];
     const uint32_t* list = d.list + (int64_t)(s.x / a.n) * d.places + p.at;
     const uint32_t many = f.many < p.n ? f.many : p.n;
@@ -690,7 +723,7 @@ __global__ __launch_bounds__(kPartThreads, 4) void select_place_kernel(SelectIn 
     int32_t* out = p.out + p.first;
     const uint64_t below = (1ull << lane) - 1;
     auto place = [&](auto one_by_one) {
-        each_round<false>(a, d, s, [&](uint32_t (&v)[16], uint32_t i) {
+        rounds.each([&](uint32_t (&v)[16], uint32_t i) {
             auto there = [&](uint32_t j) { return i + j / 4 * 4 * kWave + j % 4 < s.end; };
             if constexpr (decltype(one_by_one)::value) {
                 // equals by their places: those that stay are raised, the workgroup's waves in turn
@@ -769,8 +802,8 @@ constexpr uint64_t kSplitArea = 1ull << 29;  // bytes of the work area, at most
 // Scores of a part where choices are split (0: one kernel has them).  By itself a choice takes a
 // time that goes by its length, split one that goes by all lengths, and two launches more.  us, by
 // itself and split, of choices of 9,000 scores (some kept in registers): 1 11 and 21, 128 12 and
-// 29; of 32,768: 16 31 and 24, 64 31 and 34, 128 36 and 48; of 65,536: 16 53 and 30, 128 61 and
-// 61, 192 64 and 74; of 131,072: 1 95 and 25, 64 109 and 53, 128 110 and 82, 224 114 and 105.
+// 29; of 32,768: 16 31 and 24, 64 31 and 33, 128 36 and 48; of 65,536: 16 53 and 30, 128 61 and
+// 56, 192 64 and 74; of 131,072: 1 95 and 25, 64 109 and 54, 128 110 and 83, 192 115 and 103.
 uint32_t part_scores(const dm_ctx* c, uint64_t choices, uint64_t rows, uint64_t places, uint64_t n)
 {
     constexpr uint64_t kMean = 24576, kLike = 512;
@@ -925,11 +958,10 @@ hipError_t evict_select(dm_ctx* c, const dm_page_tables& t, const dm_select_args
     const uint32_t each = part_scores(c, grid, rows, places, t.n);
     const uint64_t row = each ? places / each + t.n : 0, all = row * rows;
     const uint64_t bins = all * kBins * 4, found = (all * sizeof(Found) + 15) / 16 * 16;
-    const uint64_t list = rows * places * 4, area = bins + found + list;
-    const uint64_t sums = a.share > 1 && area + list <= kSplitArea ? list : 0;
+    const uint64_t list = rows * places * 4, area = bins + found + (a.share > 1 ? 2 : 1) * list;
     if (each && area <= kSplitArea) {
         hipError_t e;
-        char* at = static_cast<char*>(scratch_get(c, kSlotPages, area + sums, &e));
+        char* at = static_cast<char*>(scratch_get(c, kSlotPages, area, &e));
         if (!at)
             return e;
         Split d;
@@ -938,7 +970,7 @@ hipError_t evict_select(dm_ctx* c, const dm_page_tables& t, const dm_select_args
         d.bins = reinterpret_cast<uint32_t*>(at);
         d.found = reinterpret_cast<Found*>(at + bins);
         d.list = reinterpret_cast<uint32_t*>(at + bins + found);
-        d.sums = sums ? reinterpret_cast<uint32_t*>(at + area) : nullptr;
+        d.sums = a.share > 1 ? reinterpret_cast<uint32_t*>(at + bins + found + list) : nullptr;
         d.places = (int64_t)places;
         select_count_kernel<<<(uint32_t)all, kPartThreads, 0, c->stream>>>(a, d, c->d_status);
         select_list_kernel<<<(uint32_t)all, kPartThreads, 0, c->stream>>>(a, d);
