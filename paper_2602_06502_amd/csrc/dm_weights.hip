@@ -49,6 +49,8 @@ struct WeightsIn {
     uint32_t parts, part_rows;
     float* part;
     int64_t slots;
+    struct SeqRow* rows;  // with runs: of each sequence
+    uint32_t* order;   // [n] of each run, from its first sequence on: those that see its prefix
 };
 
 // The first row of a sequence that counts.
@@ -98,7 +100,7 @@ struct LongSum {
 // lanes: its new tokens, its tokens, where they are (`at`), where what it carries is (`old`,
 // of its first `keep` tokens), its tokens that are its run's, and its run's sequences.
 struct Known {
-    uint32_t tok0, ntok, len, keep, own0, g0, g1;
+    uint32_t tok0, ntok, len, keep, own0;
     int64_t at, old;
 };
 template <bool RUNS>
@@ -115,11 +117,8 @@ __device__ __forceinline__ Known known_of(const TokenBatch& b, const PlanView& p
     x.at = b.off[s] << b.shift;
     if (RUNS) {
         const uint32_t g = pv.run[s];
-        if (g < b.groups) {
-            x.g0 = (uint32_t)b.group_off[g];
-            x.g1 = (uint32_t)b.group_off[g + 1];
+        if (g < b.groups)
             x.own0 = x.ntok && x.len ? pv.unit[b.groups + s].key0 : 0;
-        }
     }
     return x;
 }
@@ -144,6 +143,78 @@ __device__ __forceinline__ void add_carried(const WeightsIn& a, uint32_t s, bool
         }
     }
 }
+// What a batch with runs has of each sequence, laid out by a kernel of its own: a wave of the
+// others then finds what it has to do in two reads, not in eight that wait for one another.
+constexpr uint32_t kShared = 4;  // sequences of a run that read its keys at once
+struct alignas(16) SeqRow {
+    Known x;
+    // if it sees its run's prefix and is every kShared-th of those that do: it and the next ones
+    uint32_t many, member[kShared];
+};
+static_assert(sizeof(SeqRow) == 64);
+
+// A workgroup for 256 sequences, then one for each run.
+__global__ __launch_bounds__(kThreads) void weights_rows_kernel(WeightsIn a, const PlanView pv, uint32_t chunks, uint32_t* status)
+{
+    const TokenBatch& b = a.b;
+    __shared__ uint32_t counts[kWaves];
+    const uint32_t tid = threadIdx.x, wave = tid / kWave, lane = lane_id();
+    if (!plan_of(*pv.head, b, a.q_heads, a.plan_heads, a.plan_dim))
+        return;  // (the other kernel reports it, and reads nothing of these)
+    if (blockIdx.x < chunks) {
+        const uint32_t s = blockIdx.x * kThreads + tid;
+        bool bad = false;
+        Known x = known_of<true>(b, pv, s, s < b.n, bad);
+        add_carried(a, s, s < b.n, x, bad);
+        if (s < b.n)
+            a.rows[s].x = x;
+        if (bad)
+            atomicOr(status, kErrInval);
+        return;
+    }
+    const uint32_t g = blockIdx.x - chunks;
+    const int64_t g0 = b.group_off[g], g1 = b.group_off[g + 1];
+    if (g0 < 0 || g1 < g0 || g1 > (int64_t)b.n)
+        return;
+    // (as known_of has it)
+    auto sees = [&](uint32_t m) {
+        const Unit& u = pv.unit[b.groups + m];
+        return u.ntok && u.key0 && u.key1 && pv.run[m] == g;
+    };
+    // ranks of those that see the prefix, twice: their order, then by it their neighbours
+    uint32_t total = 0;
+    for (uint32_t pass = 0; pass < 2; pass++) {
+        uint32_t seen = 0;
+        for (uint32_t m0 = (uint32_t)g0; m0 < (uint32_t)g1; m0 += kThreads) {
+            const uint32_t m = m0 + tid;
+            const bool in = m < (uint32_t)g1 && sees(m);
+            const uint64_t those = ballot(in);
+            __syncthreads();
+            if (lane == 0)
+                counts[wave] = __popcll(those);
+            __syncthreads();
+            uint32_t rank = seen + __popcll(those & ((1ull << lane) - 1));
+            for (uint32_t w = 0; w < kWaves; w++) {
+                rank += w < wave ? counts[w] : 0;
+                seen += counts[w];
+            }
+            if (m >= (uint32_t)g1)
+                continue;
+            if (pass == 0) {
+                if (in)
+                    a.order[g0 + rank] = m;
+                continue;
+            }
+            const uint32_t many = !in || rank % kShared ? 0 : total - rank < kShared ? total - rank : kShared;
+            a.rows[m].many = many;
+            for (uint32_t k = 0; k < many; k++)
+                a.rows[m].member[k] = a.order[g0 + rank + k];
+        }
+        total = seen;
+        __syncthreads();
+    }
+}
+
 // Sums for sequences with up to ROWS rows each (4, 8 or 16), 16 / ROWS of them in one product:
 // a lane has in sum[c] key c * 16 + lane % 16's of the sequence that has its quarter of the
 // rows.  member(n): the lane of `of` that has the n-th sequence.
@@ -203,8 +274,6 @@ __device__ __forceinline__ Known of_lane(const Known& x, uint32_t lane)
     y.len = from_lane(x.len, lane);
     y.keep = from_lane(x.keep, lane);
     y.own0 = from_lane(x.own0, lane);
-    y.g0 = from_lane(x.g0, lane);
-    y.g1 = from_lane(x.g1, lane);
     y.at = from_lane(x.at, lane);
     y.old = from_lane(x.old, lane);
     return y;
@@ -298,25 +367,8 @@ __device__ __forceinline__ void each_sequence(const TokenBatch& b, const PlanVie
     }
 }
 
-// How many of a run's sequences that see a prefix come before sequence s.  By a whole wave.
-__device__ __forceinline__ uint32_t rank_in_run(const PlanView& pv, uint32_t groups, uint32_t g0, uint32_t s)
-{
-    uint32_t rank = 0;
-    for (uint32_t m0 = g0; m0 < s; m0 += kWave) {
-        const uint32_t m = m0 + lane_id();
-        bool sees = false;
-        if (m < s) {
-            const Unit& u = pv.unit[groups + m];
-            sees = u.ntok && u.key0 && u.key1;
-        }
-        rank += __popcll(ballot(sees));
-    }
-    return rank;
-}
-
 // A wave has 64 slots and a few heads one after another.  Of a run's shared keys the blocks of
 // every kShared-th sequence that sees them have those of the next ones too.
-constexpr uint32_t kShared = 4;
 
 // RUNS: the batch has runs (a kernel of its own: its registers would halve the other's waves).
 template <typename T, int D, bool RUNS>
@@ -326,7 +378,6 @@ __global__ __launch_bounds__(kThreads, D == 256 ? (RUNS ? 1 : 2) : RUNS && D == 
 {
     using V = typename Vec8<T>::type;
     __shared__ __attribute__((aligned(16))) WordsOf<16> all_words[kWaves];
-    __shared__ uint32_t members[kWaves][kShared];  // lanes of a run's sequences
     const TokenBatch& b = a.b;
     const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = lane_id();
     const uint64_t item = (uint64_t)blockIdx.x * kWaves + wave;
@@ -407,33 +458,22 @@ __global__ __launch_bounds__(kThreads, D == 256 ? (RUNS ? 1 : 2) : RUNS && D == 
         if (mine)
             a.w[(int64_t)h * a.w_stride + s.at + i] = carried + sum;
     };
-    // The shared tokens in the block, those of sequence x, for kShared of its run's sequences
-    // that see them from s0 on; of 64 neighbouring sequences at a time, `taken` before.
-    auto share = [&](uint32_t s0, const Known& x, uint32_t taken) -> uint32_t {
-        const uint32_t m = s0 + lane;
-        Known of = known_of<RUNS>(b, pv, m, m < x.g1 && m < b.n, bad);
-        uint64_t those = ballot(of.own0 != 0);
-        const uint32_t rank = __popcll(those & ((1ull << lane) - 1));
-        const bool in = of.own0 && rank + taken < kShared;
-        those = ballot(in);
-        const uint32_t count = __popcll(those);
-        if (count == 0)
-            return 0;
-        add_carried(a, m, in, of, bad);
+    // The shared tokens in the block, those of sequence x, for the `count` sequences that its row names.
+    auto share = [&](const Known& x, uint32_t count, uint32_t m) {
+        const bool in = lane < count && m < b.n;
+        Known of{};
+        if (in)
+            of = a.rows[m].x;
+        const uint64_t those = ballot(in);
         const uint32_t rows = (a.last && a.last < of.ntok ? a.last : of.ntok) * a.ratio;
         const int64_t i0 = slot0 - x.at;
         if (__any(in && rows > 16)) {
             for (uint32_t h = h0; h < h1; h++)
                 for (uint64_t next = those; next; next &= next - 1)
                     collect(of_lane(of, (uint32_t)__builtin_ctzll(next)), h, i0, 0, x.own0, false);
-            return count;
+            return;
         }
-        __builtin_amdgcn_wave_barrier();
-        if (in)
-            members[wave][rank] = lane;
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-        __builtin_amdgcn_wave_barrier();
-        auto member = [&](uint32_t n) { return members[wave][n]; };
+        auto member = [&](uint32_t n) { return n; };
         auto packed = [&](auto size) {
             constexpr int kRows = decltype(size)::value;
             for (uint32_t h = h0; h < h1; h++) {
@@ -471,29 +511,35 @@ __global__ __launch_bounds__(kThreads, D == 256 ? (RUNS ? 1 : 2) : RUNS && D == 
             const int64_t key = i0 + c * 16 + lane % 16;
             bad |= key >= 0 && key < x.own0 && page[c] >= a.n_pages;
         }
-        return count;
     };
     // the sequences in the block, 64 looked at a time
     for (uint32_t s0 = wave_find(b.off, b.n, 1, entry0); s0 < b.n; s0 += kWave) {
         const uint32_t s = s0 + lane;
         const bool in = s < b.n && b.off[s] <= entry1;
-        Known all = known_of<RUNS>(b, pv, s, in, bad);
+        Known all{};
+        uint32_t many = 0;
+        if constexpr (RUNS) {
+            if (in) {
+                all = a.rows[s].x;
+                many = all.own0 ? a.rows[s].many : 0;
+            }
+        } else {
+            all = known_of<false>(b, pv, s, in, bad);
+        }
         const bool own = in && all.len > all.own0 && slot0 - all.at < (int64_t)all.len &&
                          slot0 - all.at + (int64_t)kBlockKeys > (int64_t)all.own0;
-        add_carried(a, s, own, all, bad);
+        if (!RUNS)
+            add_carried(a, s, own, all, bad);
         for (uint64_t left = ballot(own); left; left &= left - 1) {
             const Known x = of_lane(all, (uint32_t)__builtin_ctzll(left));
             for (uint32_t h = h0; h < h1; h++)
                 collect(x, h, slot0 - x.at, x.own0, x.len, true);
         }
         // a run's shared tokens
-        for (uint64_t left = !RUNS ? 0 : ballot(in && all.own0 && slot0 - all.at < (int64_t)all.own0); left; left &= left - 1) {
-            const uint32_t j = (uint32_t)__builtin_ctzll(left);
-            const Known x = of_lane(all, j);
+        for (uint64_t left = !RUNS ? 0 : ballot(many && slot0 - all.at < (int64_t)all.own0); left; left &= left - 1) {
+            const uint32_t j = (uint32_t)__builtin_ctzll(left), count = from_lane(many < kShared ? many : kShared, j);
             if constexpr (RUNS)
-                if (rank_in_run(pv, b.groups, x.g0, s0 + j) % kShared == 0)
-                    for (uint32_t m0 = s0 + j, taken = 0; m0 < x.g1 && taken < kShared; m0 += kWave)
-                        taken += share(m0, x, taken);
+                share(of_lane(all, j), count, lane < count ? a.rows[s0 + j].member[lane] : 0);
         }
         if (!__all(in))
             break;
@@ -815,12 +861,22 @@ hipError_t attn_weights(dm_ctx* c, const dm_token_batch& b, const dm_kv_pages& k
     const uint32_t blocks = (uint32_t)((slots + kTallKeys - 1) / kTallKeys);
     a.parts = parts_of_rows(c, b, a.ratio, g.last, (uint64_t)blocks * kv.kv_heads, &a.part_rows);
     a.part = nullptr;
-    if (a.parts) {
+    a.rows = nullptr;
+    a.order = nullptr;
+    const uint64_t n = b.tables.n, parts = (a.parts * kv.kv_heads * slots * 4 + 15) / 16 * 16;
+    const uint64_t area = parts + (b.groups ? n * (sizeof(SeqRow) + 4) : 0);
+    if (area) {
         hipError_t e;
-        a.part = static_cast<float*>(scratch_get(c, kSlotPages, a.parts * kv.kv_heads * slots * 4, &e));
-        if (!a.part)
+        char* at = static_cast<char*>(scratch_get(c, kSlotPages, area, &e));
+        if (!at)
             return e;
+        a.part = reinterpret_cast<float*>(at);
+        a.rows = reinterpret_cast<SeqRow*>(at + parts);
+        a.order = reinterpret_cast<uint32_t*>(a.rows + n);
     }
+    const uint32_t chunks = (uint32_t)((n + kThreads - 1) / kThreads);
+    if (b.groups)
+        weights_rows_kernel<<<chunks + (uint32_t)b.groups, kThreads, 0, c->stream>>>(a, pv, chunks, c->d_status);
     by_type(kv.dtype, kv.head_dim, [&](auto t, auto d) {
         using T = decltype(t);
         constexpr int D = decltype(d)::value;
