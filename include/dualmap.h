@@ -717,7 +717,8 @@ typedef struct {
  * weights keep what their additions round away.  A weight is off by some 2^-23
  * of itself for each unit of |lse| (its own rounding).  Where sequences have many
  * rows the context's work area holds up to 32 sums for each of w's places, not
- * more than 2^24 floats unless one each is more; it grows as dm_attn's.  A query with
+ * more than 2^24 floats unless one each is more, and with groups 68 bytes a sequence;
+ * it grows as dm_attn's.  A query with
  * lse = -infinity counts nowhere (its scores finite); keys that no query sees have
  * what they had.  Other places of w are left as they were.  Who sees what, malformed tables and
  * a plan of another batch are as in dm_attn; a sequence's src or prev_off out of

@@ -14,9 +14,8 @@
 // keys of a head and a stretch of rows, which pass through LDS once for its four waves; it
 // leaves its sums, and the first kernel adds a key's up.
 //
-// The pages that a run shares (as its plan has found them) are read by the blocks of every
-// fourth of its sequences, for four of them, each with its own sums; a few rows each,
-// several of them have one product.
+// The pages that a run shares (as its plan has found them) are read for four of its sequences
+// at once, each with its own sums; a few rows each, several of them have one product.
 //
 // Bound by reading keys where rows are few, by the exponentials where they are many.
 #include "dm_attn.h"
@@ -98,7 +97,7 @@ struct LongSum {
 
 // What is known of a sequence, a lane each for 64 neighbouring ones, and then of one by all
 // lanes: its new tokens, its tokens, where they are (`at`), where what it carries is (`old`,
-// of its first `keep` tokens), its tokens that are its run's, and its run's sequences.
+// of its first `keep` tokens), and its tokens that are its run's.
 struct Known {
     uint32_t tok0, ntok, len, keep, own0;
     int64_t at, old;
@@ -148,7 +147,8 @@ __device__ __forceinline__ void add_carried(const WeightsIn& a, uint32_t s, bool
 constexpr uint32_t kShared = 4;  // sequences of a run that read its keys at once
 struct alignas(16) SeqRow {
     Known x;
-    // if it sees its run's prefix and is every kShared-th of those that do: it and the next ones
+    // if it sees its run's prefix: the kShared neighbours among those that do, it among them; how
+    // many they are, and from bit 8 on which of them it is
     uint32_t many, member[kShared];
 };
 static_assert(sizeof(SeqRow) == 64);
@@ -205,10 +205,11 @@ __global__ __launch_bounds__(kThreads) void weights_rows_kernel(WeightsIn a, con
                     a.order[g0 + rank] = m;
                 continue;
             }
-            const uint32_t many = !in || rank % kShared ? 0 : total - rank < kShared ? total - rank : kShared;
-            a.rows[m].many = many;
+            const uint32_t mine = rank % kShared, first = rank - mine;
+            const uint32_t many = !in ? 0 : total - first < kShared ? total - first : kShared;
+            a.rows[m].many = many | mine << 8;
             for (uint32_t k = 0; k < many; k++)
-                a.rows[m].member[k] = a.order[g0 + rank + k];
+                a.rows[m].member[k] = a.order[g0 + first + k];
         }
         total = seen;
         __syncthreads();
@@ -367,8 +368,8 @@ __device__ __forceinline__ void each_sequence(const TokenBatch& b, const PlanVie
     }
 }
 
-// A wave has 64 slots and a few heads one after another.  Of a run's shared keys the blocks of
-// every kShared-th sequence that sees them have those of the next ones too.
+// A wave has 64 slots and a few heads one after another.  A run's shared keys are read for
+// kShared of its sequences at once, by the blocks of one of these, or of each for some heads.
 
 // RUNS: the batch has runs (a kernel of its own: its registers would halve the other's waves).
 template <typename T, int D, bool RUNS>
@@ -458,8 +459,16 @@ __global__ __launch_bounds__(kThreads, D == 256 ? (RUNS ? 1 : 2) : RUNS && D == 
         if (mine)
             a.w[(int64_t)h * a.w_stride + s.at + i] = carried + sum;
     };
-    // The shared tokens in the block, those of sequence x, for the `count` sequences that its row names.
-    auto share = [&](const Known& x, uint32_t count, uint32_t m) {
+    // The shared tokens in the block, those of sequence x, for the `count` sequences that its row
+    // names (m: a lane's), of which it is number `mine`.
+    auto share = [&](const Known& x, uint32_t count, uint32_t mine, uint32_t m) {
+        // Where a wave has many heads, the sequences' blocks have each its own of them (128 sequences
+        // on 8 prefixes 88 to 83 us); where it has few, the first sequence's have all (16 on 2: 20,
+        // dealt 21).
+        const bool dealt = heads >= kShared;
+        const uint32_t first = dealt ? h0 + (mine + count - h0 % count) % count : mine ? h1 : h0, step = dealt ? count : 1;
+        if (first >= h1)
+            return;
         const bool in = lane < count && m < b.n;
         Known of{};
         if (in)
@@ -468,7 +477,7 @@ __global__ __launch_bounds__(kThreads, D == 256 ? (RUNS ? 1 : 2) : RUNS && D == 
         const uint32_t rows = (a.last && a.last < of.ntok ? a.last : of.ntok) * a.ratio;
         const int64_t i0 = slot0 - x.at;
         if (__any(in && rows > 16)) {
-            for (uint32_t h = h0; h < h1; h++)
+            for (uint32_t h = first; h < h1; h += step)
                 for (uint64_t next = those; next; next &= next - 1)
                     collect(of_lane(of, (uint32_t)__builtin_ctzll(next)), h, i0, 0, x.own0, false);
             return;
@@ -476,7 +485,7 @@ __global__ __launch_bounds__(kThreads, D == 256 ? (RUNS ? 1 : 2) : RUNS && D == 
         auto member = [&](uint32_t n) { return n; };
         auto packed = [&](auto size) {
             constexpr int kRows = decltype(size)::value;
-            for (uint32_t h = h0; h < h1; h++) {
+            for (uint32_t h = first; h < h1; h += step) {
                 const uint32_t x0 = a.paired ? h / 2 * 2 * a.ratio + h % 2 : h * a.ratio, xs = a.paired ? 2 : 1;
                 load(h);
                 for (uint32_t n0 = 0; n0 < count; n0 += 16 / kRows) {
@@ -537,9 +546,11 @@ __global__ __launch_bounds__(kThreads, D == 256 ? (RUNS ? 1 : 2) : RUNS && D == 
         }
         // a run's shared tokens
         for (uint64_t left = !RUNS ? 0 : ballot(many && slot0 - all.at < (int64_t)all.own0); left; left &= left - 1) {
-            const uint32_t j = (uint32_t)__builtin_ctzll(left), count = from_lane(many < kShared ? many : kShared, j);
+            const uint32_t j = (uint32_t)__builtin_ctzll(left), word = from_lane(many, j);
+            const uint32_t count = (word & 255) < kShared ? word & 255 : kShared, mine = word >> 8;
             if constexpr (RUNS)
-                share(of_lane(all, j), count, lane < count ? a.rows[s0 + j].member[lane] : 0);
+                if (count)
+                    share(of_lane(all, j), count, mine, lane < count ? a.rows[s0 + j].member[lane] : 0);
         }
         if (!__all(in))
             break;

@@ -396,3 +396,17 @@ def test_one_plan_for_attention_weights_and_other_layers():
     for w in got[:2]:
         total = float(w.double().sum())
         assert abs(total - 8 * T) <= 8 * T * 2.0 ** -15, total
+
+
+@pytest.mark.parametrize("paired", [False, True])
+def test_runs_of_hundreds(paired):
+    """Runs longer than a workgroup looks at a time, some of their sequences with nothing to do; the last group of a run short."""
+    r = np.random.default_rng(4)
+    seqs = [(int(r.integers(1, 3)), int(r.integers(2, 40)), 0) for _ in range(301)]
+    seqs += [(1, 7, 1)] + [(1 if i % 5 else 0, 9 + i % 30, 2) for i in range(290)]
+    b = Collected(16, seqs, prefixes=(160, 144, 320), heads=(8, 4) if paired else (4, 2), dim=64, paired=paired, seed=21)
+    for i in (0, 3, 4, 260, 302, 303, 420):
+        b.len[i] = 0
+        b.keep[i] = 0
+    _say("hundreds", paired)
+    b.check()

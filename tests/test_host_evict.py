@@ -186,6 +186,21 @@ def scenario_select_area(x):
         x.L.dm_destroy(c.h)
 
 
+def scenario_weights_runs_area(x):
+    """With runs, 68 bytes a sequence, beside the sums of stretches where there are some."""
+    held = x.word("fake_bytes")
+    for tokens, n, groups, some in ((64, 64, 0, 0), (64, 64, 4, 68 * 64), (5000, 5000, 9, 68 * 5000)):
+        c = Calls(x)
+        before = held.value
+        assert c.weights(batch=dict(tokens=tokens, n=n, entries=4000, groups=groups), w_stride=64_000) == x.pk.DM_OK
+        assert some <= held.value - before <= (some + 4096 if some else 0), (n, groups, held.value - before)
+        x.L.dm_destroy(c.h)
+
+
+def test_weights_runs_work_area(fake):  # noqa: F811
+    _child(fake, "weights_runs_area")
+
+
 def test_select_work_area(fake):  # noqa: F811
     _child(fake, "select_area")
 
