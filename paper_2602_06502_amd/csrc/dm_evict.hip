@@ -445,9 +445,8 @@ __global__ __launch_bounds__(THREADS) void select_kernel(SelectIn a, uint32_t* s
     else if (n <= THREADS * 16)
         choose<kW, 16>(lds, n, k, (int32_t)first, out + first, keys);
     else
-        choose_long<kW, THREADS == 1024 ? 4 : 1>(lds, candidate, whose, n, k, (int32_t)first, out + first, [&](uint32_t i, auto& x) {
-            scores4<false>(a, w, n, i, x);
-        });
+        choose_long<kW, THREADS == 1024 ? 4 : 1>(lds, candidate, whose, n, k, (int32_t)first, out + first,
+                                                 [&](uint32_t i, auto& x) { scores4<false>(a, w, n, i, x); });
 }
 
 // Long histories where choices are too few to fill the chip: several workgroups a choice, each
@@ -652,7 +651,8 @@ __global__ __launch_bounds__(kPartThreads, 4) void select_list_kernel(SelectIn a
     __syncthreads();
     const uint32_t agree = lds.equal[0];
     if (tid == 0)
-        d.found[blockIdx.x] = Found{digit, left, lds.bins[0][digit], lds.up[0], agree, d.bins[(uint64_t)blockIdx.x * kBins + digit]};
+        d.found[blockIdx.x] =
+            Found{digit, left, lds.bins[0][digit], lds.up[0], agree, d.bins[(uint64_t)blockIdx.x * kBins + digit]};
     uint32_t* list = d.list + (int64_t)(s.x / a.n) * d.places + p.at;
     const uint64_t below = (1ull << lane_id()) - 1;
     rounds.each([&](const uint32_t (&v)[16], uint32_t i) {

@@ -152,6 +152,38 @@ def test_long_choices_of_one_workgroup():
         Histories(16, lens, layers=1, heads=2, seed=14, values=values).check([n // 3 for n in lens], recent=5)
 
 
+def test_malformed_tables_of_split_choices():
+    """A length that its table cannot hold, a negative budget, offsets that decrease: reported; the others of the first two are
+    chosen as ever, and so is a good call after them."""
+    _say("split, malformed")
+    pk, e = engine(32)
+    b = Histories(32, [60_000, 50_000, 40_000], layers=2, heads=2, seed=17)
+    budget = [7000, 800, 39_000]
+    want = b.expected(budget)
+
+    def run(off, length, budget):
+        kept = torch.full((2, 2, b.rows + 1), -7, dtype=torch.int32, device="cuda")
+        keep, grow = torch.full((3,), -7, device="cuda"), torch.full((3,), -7, device="cuda")
+        e.evict_select((dev(off), dev(b.page), dev(length)), dev(b.w), dev(np.array(budget, np.int64)), None, kept, keep, grow)
+        try:
+            e.sync()
+        except pk.DMError:
+            return kept.cpu().numpy(), keep.tolist(), True
+        return kept.cpu().numpy(), keep.tolist(), False
+
+    others = want.copy()
+    a = int(b.off[1]) * 32
+    others[..., a:a + budget[1]] = -7
+    for length, budgets, keep1 in ((np.array([60_000, 50_100, 40_000]), budget, 0), (b.len, [7000, -1, 39_000], 50_000)):
+        kept, keep, told = run(b.off, length.astype(np.int64), budgets)
+        assert told and np.array_equal(kept, others) and keep == [0, keep1, 0]
+    _say("decreasing offsets")
+    _, _, told = run(np.array([0, b.off[2], b.off[1], b.off[3]], np.int64), np.array([100_000, 9, 80_000], np.int64), budget)
+    assert told
+    kept, keep, told = run(b.off, b.len, budget)
+    assert not told and np.array_equal(kept, want) and keep == [0, 0, 0]
+
+
 def test_a_split_choice_in_a_graph():
     """Its work area is the context's: the same replays before and after a larger call has grown it."""
     _say("split graph")
