@@ -410,3 +410,56 @@ def test_runs_of_hundreds(paired):
         b.keep[i] = 0
     _say("hundreds", paired)
     b.check()
+
+
+def test_runs_with_malformed_arguments():
+    """With runs: a source out of range carries nothing, a length that a table cannot hold counts as 0, another batch's plan writes
+    nothing; each is reported, and the other sequences have theirs."""
+    pk, e = engine(16)
+    seqs = [(1, 30 + 7 * i, 0) for i in range(9)] + [(2, 20, 1), (1, 33, 1)]
+    b = Collected(16, seqs, prefixes=(256, 192), heads=(4, 2), dim=64, seed=8)
+    lse = b.far()
+    kv, T = pk.KVPages(b.k.cuda(), b.v.cuda()), int(b.q_off[-1])
+    q = b.qrows.cuda()[:, :4 * 64].unflatten(1, (4, 64)).contiguous()
+    groups, q_off, keep, off = b.dev(b.groups), b.dev(b.q_off), b.dev(b.keep), b.dev(b.prev_off)
+
+    def run(src, length=None, plan=None):
+        tables = b.tables() if length is None else (b.tables()[0], b.tables()[1], b.dev(length))
+        plan = plan or e.attn_plan(kv, tables, q_off, T, 4, groups=groups)
+        w = torch.full((2, b.rows), 7.0, device="cuda")
+        e.attn_weights(plan, 0, q, b.scale(), lse.cuda(), w, prev=(b.prev.cuda(), off, b.dev(src), keep), decay=b.decay)
+        try:
+            e.sync()
+        except pk.DMError:
+            return w.cpu(), True
+        return w.cpu(), False
+
+    good, told = run(b.src)
+    assert not told
+    ref, tol, written = b.reference(lse)
+    assert bool(((good.double() - ref).abs() <= tol)[:, written].all())
+    places = [slice(int(b.off[s]) * 16, int(b.off[s]) * 16 + int(b.len[s])) for s in range(len(seqs))]
+    for bad in (-1, 5000):
+        _say("source", bad)
+        src = b.src.copy()
+        src[4] = bad
+        w, told = run(src)
+        assert told
+        for s, at in enumerate(places):
+            if s != 4:
+                assert torch.equal(w[:, at], good[:, at]), s
+        n = int(b.keep[4])
+        at = slice(places[4].start, places[4].start + n)
+        old = b.decay * b.prev[:, int(b.prev_off[b.src[4]]) * 16:][:, :n].double()
+        assert bool(((w[:, at].double() - (ref[:, at] - old)).abs() <= tol[:, at]).all())
+    _say("length")
+    length = b.len.copy()
+    length[2] += 4000
+    w, told = run(b.src, length)
+    assert told and bool((w[:, places[2]] == 7).all())
+    _say("plan")
+    other = e.attn_plan(kv, b.tables(), q_off, T, 4, groups=b.dev(np.array([0, 11], np.int64)))
+    mine = e.attn_plan(kv, b.tables(), q_off, T, 4, groups=groups)
+    mine.buf = other.buf
+    w, told = run(b.src, plan=mine)
+    assert told and bool((w == 7).all())
