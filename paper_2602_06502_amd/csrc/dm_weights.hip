@@ -145,7 +145,7 @@ __device__ __forceinline__ void add_carried(const WeightsIn& a, uint32_t s, bool
         }
     }
 }
-// What a batch with runs has of each sequence, laid out by a kernel of its own (5 us): a wave of
+// What a batch with runs has of each sequence, laid out by a kernel of its own (4 us): a wave of
 // the others then finds what it has to do in two reads, not in eight that wait for one another
 // (128 sequences on 8 prefixes 99 to 88 us, 16 on 2 24 to 20, 4 on one 13 and 13).
 constexpr uint32_t kShared = 4;  // sequences of a run that read its keys at once
@@ -161,7 +161,7 @@ static_assert(sizeof(SeqRow) == 64);
 __global__ __launch_bounds__(kThreads) void weights_rows_kernel(WeightsIn a, const PlanView pv, uint32_t chunks, uint32_t* status)
 {
     const TokenBatch& b = a.b;
-    __shared__ uint32_t counts[kWaves];
+    __shared__ uint32_t counts[kWaves], order[kThreads];
     const uint32_t tid = threadIdx.x, wave = tid / kWave, lane = lane_id();
     if (!plan_of(*pv.head, b, a.q_heads, a.plan_heads, a.plan_dim))
         return;  // (the other kernel reports it, and reads nothing of these)
@@ -185,9 +185,12 @@ __global__ __launch_bounds__(kThreads) void weights_rows_kernel(WeightsIn a, con
         const Unit& u = pv.unit[b.groups + m];
         return u.ntok && u.key0 && u.key1 && pv.run[m] == g;
     };
-    // ranks of those that see the prefix, twice: their order, then by it their neighbours
+    // ranks of those that see the prefix, for their order, then by it their neighbours; of a run
+    // that the workgroup sees at once in one pass, the order in LDS
+    const bool at_once = g1 - g0 <= kThreads;
+    uint32_t* list = at_once ? order : a.order + g0;
     uint32_t total = 0;
-    for (uint32_t pass = 0; pass < 2; pass++) {
+    auto each = [&](auto&& f) {  // f(sequence, does it see the prefix, how many before it do)
         uint32_t seen = 0;
         for (uint32_t m0 = (uint32_t)g0; m0 < (uint32_t)g1; m0 += kThreads) {
             const uint32_t m = m0 + tid;
@@ -202,22 +205,35 @@ __global__ __launch_bounds__(kThreads) void weights_rows_kernel(WeightsIn a, con
                 rank += w < wave ? counts[w] : 0;
                 seen += counts[w];
             }
-            if (m >= (uint32_t)g1)
-                continue;
-            if (pass == 0) {
-                if (in)
-                    a.order[g0 + rank] = m;
-                continue;
-            }
-            const uint32_t mine = rank % kShared, first = rank - mine;
-            const uint32_t many = !in ? 0 : total - first < kShared ? total - first : kShared;
-            a.rows[m].many = many | mine << 8;
-            for (uint32_t k = 0; k < many; k++)
-                a.rows[m].member[k] = a.order[g0 + first + k];
+            total = seen;
+            f(m, in, rank);
         }
-        total = seen;
-        __syncthreads();
-    }
+    };
+    auto write = [&](uint32_t m, bool in, uint32_t rank) {
+        if (m >= (uint32_t)g1)
+            return;
+        const uint32_t mine = rank % kShared, first = rank - mine;
+        const uint32_t many = !in ? 0 : total - first < kShared ? total - first : kShared;
+        a.rows[m].many = many | mine << 8;
+        for (uint32_t k = 0; k < many; k++)
+            a.rows[m].member[k] = list[first + k];
+    };
+    each([&](uint32_t m, bool in, uint32_t rank) {
+        if (in)
+            list[rank] = m;
+        if (at_once) {
+            __syncthreads();
+            write(m, in, rank);
+        }
+    });
+    if (at_once)
+        return;
+    const uint32_t all = total;
+    __syncthreads();
+    each([&](uint32_t m, bool in, uint32_t rank) {
+        total = all;
+        write(m, in, rank);
+    });
 }
 
 // Sums for sequences with up to ROWS rows each (4, 8 or 16), 16 / ROWS of them in one product:
