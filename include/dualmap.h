@@ -769,9 +769,11 @@ typedef struct {
  * than 24,576 tokens) are split over workgroups: the context's work area, which grows
  * as dm_attn's, then holds a number (with share > 1 two) for each of their scores and
  * 8 KiB for each workgroup, not more than 2^29 bytes (choices that would need more
- * are not split).  page is not read.  A malformed table or a negative budget is
- * reported (DM_EINVAL) and evicts nothing of its sequence; where off decreases, others
- * than that sequence have no defined result either. */
+ * are not split).  page is not read.  A malformed table and a negative budget are reported
+ * (DM_EINVAL).  A negative budget evicts nothing of its sequence; a malformed table has nothing
+ * kept (keep 0) and a grow of -1, which dm_pages_fork refuses, so that no page is freed before
+ * the report is read.  Where off decreases, others than that sequence have no defined result
+ * either. */
 dm_status dm_evict_select(dm_ctx* ctx, const dm_page_tables* tables, const dm_select_args* args);
 
 /* kept, budget, share: dm_evict_select's.  w and w_to: NULL, or the weights by

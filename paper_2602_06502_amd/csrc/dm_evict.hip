@@ -319,7 +319,7 @@ struct Pick {
     const float* w;  // of token `first`, of the choice's first head
     int32_t* out;    // the choice's first entry
     int64_t at;      // the sequence's first place
-    bool past;
+    bool past, malformed;  // (malformed: its table)
 };
 __device__ __forceinline__ Pick pick_of(const SelectIn& a, uint32_t x, bool& bad)
 {
@@ -329,6 +329,7 @@ __device__ __forceinline__ Pick pick_of(const SelectIn& a, uint32_t x, bool& bad
     Pick p{};
     bad = h.bad || budget < 0;
     p.len = (uint32_t)h.len;
+    p.malformed = h.bad;
     p.past = !bad && h.len > budget;
     if (!p.past)
         return p;
@@ -343,14 +344,16 @@ __device__ __forceinline__ Pick pick_of(const SelectIn& a, uint32_t x, bool& bad
     return p;
 }
 // What needs no choosing: the first and the last tokens, and, once a sequence, the next tables'
-// numbers.
+// numbers.  Of a sequence whose table is malformed it is not known what it has: with a keep of 0
+// alone the fork of other tables would free all of it before dm_sync is asked, so its grow is one
+// that a fork refuses.
 __device__ __forceinline__ void settle(const SelectIn& a, const Pick& p, uint32_t x, bool bad, uint32_t threads,
                                        uint32_t* status)
 {
     const uint32_t tid = threadIdx.x;
     if (x < a.n && tid == 0) {
         a.keep[x] = p.past ? 0 : p.len;
-        a.grow[x] = (a.room ? a.room[x] : 0) + (p.past ? p.first + p.tail + p.k : 0);
+        a.grow[x] = p.malformed ? -1 : (a.room ? a.room[x] : 0) + (p.past ? p.first + p.tail + p.k : 0);
         if (bad)
             atomicOr(status, kErrInval);
     }

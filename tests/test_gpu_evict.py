@@ -598,3 +598,46 @@ def test_choice_and_move_in_a_graph():
         assert np.array_equal(got[want != -5], want[want != -5])
     e.sync()
     e.close()
+
+
+@pytest.mark.parametrize("lens,budget", [([100, 60, 200], [30, 30, 250]), ([60_000, 50_000, 40_000], [7000, 800, 41_000])])
+@pytest.mark.parametrize("what", ["length"])
+def test_a_malformed_sequence_frees_nothing(lens, budget, what):
+    """The fork that follows a choice at once, with these tables or with good ones, takes nothing of it: no page is freed, and
+    what dm_sync reports comes in time. Whole choices and split ones."""
+    pk, e = engine(32)
+    b = Histories(32, lens, seed=5)
+    n = len(lens)
+    length, room = b.len.copy(), np.array([3, 4, 5], np.int64)
+    if what == "length":
+        length[1] += 4000
+    else:
+        room[1] = -1
+    good, asked = b.tables(), (dev(b.off), dev(b.page), dev(length))
+    ref = torch.zeros(b.pages + 4000, dtype=torch.int32, device="cuda")
+    ref[torch.from_numpy(b.page.astype(np.int64)).cuda()] = 1
+    src = torch.arange(n, dtype=torch.int32, device="cuda")
+
+    def run(tables, room, then):
+        kept = torch.full((2, 4, b.rows), -7, dtype=torch.int32, device="cuda")
+        keep, grow = torch.full((n,), -7, device="cuda"), torch.full((n,), -7, device="cuda")
+        out = e.alloc_pages_out(ref.numel(), n, 6000)
+        for x in out.values():
+            if x is not None:
+                x.fill_(-5)
+        e.evict_select(tables, dev(b.w), dev(np.array(budget, np.int64)), dev(room), kept, keep, grow)
+        e.pages_fork_into(then, ref, src, keep, grow, out)
+        try:
+            e.sync()
+        except pk.DMError:
+            return keep.tolist(), grow.tolist(), out, True
+        return keep.tolist(), grow.tolist(), out, False
+
+    for then in (asked, good):
+        _say("malformed", what, lens, "good" if then is good else "same")
+        keep, grow, out, told = run(asked, room, then)
+        assert told and int(out["moves"][0]) == 0 and bool((out["ref"] == -5).all()) and bool((out["len"] == -5).all())
+        assert keep == [0, 0, lens[2]] and grow == [budget[0] + 3, -1, 5]
+    keep, grow, out, told = run(good, np.array([3, 4, 5], np.int64), good)
+    assert not told and keep == [0, 0, lens[2]] and grow == [budget[0] + 3, budget[1] + 4, 5]
+    assert out["len"].tolist() == [budget[0] + 3, budget[1] + 4, lens[2] + 5]
