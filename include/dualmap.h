@@ -746,7 +746,7 @@ typedef struct {
     const float* w;
     int64_t w_layer_stride, w_stride;
     const int64_t* budget; /* [n] tokens that a sequence keeps, at least 0 */
-    const int64_t* room;   /* [n] room for what comes next, or NULL: 0     */
+    const int64_t* room;   /* [n] room for what comes next, at least 0, or NULL: 0 */
     int32_t* kept;
     int64_t kept_stride;
     int64_t* keep; /* [n] out */
@@ -769,11 +769,11 @@ typedef struct {
  * than 24,576 tokens) are split over workgroups: the context's work area, which grows
  * as dm_attn's, then holds a number (with share > 1 two) for each of their scores and
  * 8 KiB for each workgroup, not more than 2^29 bytes (choices that would need more
- * are not split).  page is not read.  A malformed table and a negative budget are reported
- * (DM_EINVAL).  A negative budget evicts nothing of its sequence; a malformed table has nothing
- * kept (keep 0) and a grow of -1, which dm_pages_fork refuses, so that no page is freed before
- * the report is read.  Where off decreases, others than that sequence have no defined result
- * either. */
+ * are not split).  page is not read.  A malformed table, a negative budget and a negative
+ * room are reported (DM_EINVAL).  A negative budget evicts nothing of its sequence; a
+ * malformed table has nothing kept (keep 0), and it and a negative room have a grow of -1,
+ * which dm_pages_fork refuses, so that no page is freed before the report is read.  Where off
+ * decreases, others than that sequence have no defined result either. */
 dm_status dm_evict_select(dm_ctx* ctx, const dm_page_tables* tables, const dm_select_args* args);
 
 /* kept, budget, share: dm_evict_select's.  w and w_to: NULL, or the weights by

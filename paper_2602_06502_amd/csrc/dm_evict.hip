@@ -346,15 +346,16 @@ __device__ __forceinline__ Pick pick_of(const SelectIn& a, uint32_t x, bool& bad
 // What needs no choosing: the first and the last tokens, and, once a sequence, the next tables'
 // numbers.  Of a sequence whose table is malformed it is not known what it has: with a keep of 0
 // alone the fork of other tables would free all of it before dm_sync is asked, so its grow is one
-// that a fork refuses.
+// that a fork refuses.  Room below 0 is refused alike.
 __device__ __forceinline__ void settle(const SelectIn& a, const Pick& p, uint32_t x, bool bad, uint32_t threads,
                                        uint32_t* status)
 {
     const uint32_t tid = threadIdx.x;
     if (x < a.n && tid == 0) {
+        const int64_t room = a.room ? a.room[x] : 0;
         a.keep[x] = p.past ? 0 : p.len;
-        a.grow[x] = p.malformed ? -1 : (a.room ? a.room[x] : 0) + (p.past ? p.first + p.tail + p.k : 0);
-        if (bad)
+        a.grow[x] = p.malformed || room < 0 ? -1 : room + (p.past ? p.first + p.tail + p.k : 0);
+        if (bad || room < 0)
             atomicOr(status, kErrInval);
     }
     if (!p.past)

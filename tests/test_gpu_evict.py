@@ -601,7 +601,7 @@ def test_choice_and_move_in_a_graph():
 
 
 @pytest.mark.parametrize("lens,budget", [([100, 60, 200], [30, 30, 250]), ([60_000, 50_000, 40_000], [7000, 800, 41_000])])
-@pytest.mark.parametrize("what", ["length"])
+@pytest.mark.parametrize("what", ["length", "room"])
 def test_a_malformed_sequence_frees_nothing(lens, budget, what):
     """The fork that follows a choice at once, with these tables or with good ones, takes nothing of it: no page is freed, and
     what dm_sync reports comes in time. Whole choices and split ones."""
