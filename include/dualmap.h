@@ -741,7 +741,9 @@ dm_status dm_attn_weights(dm_ctx* ctx, const dm_token_batch* batch, const dm_kv_
 /* w: what keys have collected, [layers][kv_heads] rows as dm_attn_weights' w,
  * w_layer_stride and w_stride floats apart.  kept: [layers][kv_heads / share]
  * rows of kept_stride entries.  share: 1, or 2 for pairs, up to kv_heads; it
- * divides kv_heads.  Strides at least entries * B. */
+ * divides kv_heads.  Strides at least entries * B, from layer to layer at least
+ * the rows of one, (kv_heads - 1) * w_stride + entries * B (not looked at where
+ * there is one layer). */
 typedef struct {
     const float* w;
     int64_t w_layer_stride, w_stride;
@@ -777,7 +779,7 @@ typedef struct {
 dm_status dm_evict_select(dm_ctx* ctx, const dm_page_tables* tables, const dm_select_args* args);
 
 /* kept, budget, share: dm_evict_select's.  w and w_to: NULL, or the weights by
- * the old tables and by the new ones. */
+ * the old tables and by the new ones, strides as in dm_select_args. */
 typedef struct {
     const int64_t* budget;
     const int32_t* kept;

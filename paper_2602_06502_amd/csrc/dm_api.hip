@@ -1159,11 +1159,12 @@ dm_status dm_attn_weights(dm_ctx* c, const dm_token_batch* batch, const dm_kv_pa
     return e == hipSuccess ? DM_OK : hip_fail(c, e, "dm_attn_weights");
 }
 
-// rows of at least `rows` places, `stride` apart, and layers of them
-static bool places_ok(const void* p, int64_t layer_stride, int64_t stride, int64_t rows, uint32_t heads)
+// rows of at least `rows` places, `stride` apart, and layers of them, none of which begins in
+// another (where there is one layer its stride is not looked at)
+static bool places_ok(const void* p, uint32_t layers, int64_t layer_stride, int64_t stride, int64_t rows, uint32_t heads)
 {
-    return p && reinterpret_cast<uintptr_t>(p) % 4 == 0 && stride >= rows && stride < (1ll << 40) && layer_stride >= 0 && layer_stride < (1ll << 46) &&
-           layer_stride / stride >= (heads > 1 ? heads - 1 : 0);
+    return p && reinterpret_cast<uintptr_t>(p) % 4 == 0 && stride >= rows && stride < (1ll << 40) &&
+           (layers == 1 || (layer_stride < (1ll << 46) && layer_stride >= (heads - 1) * stride + rows));
 }
 
 static dm_status share_check(dm_ctx* c, uint32_t kv_heads, uint32_t share, const std::string& what)
@@ -1191,9 +1192,9 @@ dm_status dm_evict_select(dm_ctx* c, const dm_page_tables* t, const dm_select_ar
         !aligned(a->grow))
         return fail(c, DM_EINVAL, "dm_evict_select: null or misaligned budget, room, keep or grow");
     const int64_t rows = (int64_t)(t->entries * c->cfg.block_size);
-    if (rows && (!places_ok(a->w, a->layers > 1 ? a->w_layer_stride : 1ll << 45, a->w_stride, rows, a->kv_heads) ||
-                 !places_ok(a->kept, 1ll << 45, a->kept_stride, rows, 1)))
-        return fail(c, DM_EINVAL, "dm_evict_select: w and kept need rows of at least entries * B");
+    if (rows && (!places_ok(a->w, a->layers, a->w_layer_stride, a->w_stride, rows, a->kv_heads) ||
+                 !places_ok(a->kept, 1, 0, a->kept_stride, rows, 1)))
+        return fail(c, DM_EINVAL, "dm_evict_select: w and kept need rows of at least entries * B, layers apart");
     DeviceGuard g(c->device);
     hipError_t e = join_selection(c);
     if (e == hipSuccess)
@@ -1223,11 +1224,11 @@ dm_status dm_kv_gather(dm_ctx* c, const dm_kv_pages* kv, const dm_page_tables* f
     if (!a->budget || !aligned(a->budget))
         return fail(c, DM_EINVAL, "dm_kv_gather: null or misaligned budget");
     const int64_t rows = (int64_t)(from->entries * c->cfg.block_size);
-    const int64_t to_rows = (int64_t)(to->entries * c->cfg.block_size), far = 1ll << 45;
-    if ((rows && !places_ok(a->kept, far, a->kept_stride, rows, 1)) ||
-        (a->w && ((rows && !places_ok(a->w, kv->layers > 1 ? a->w_layer_stride : far, a->w_stride, rows, kv->kv_heads)) ||
-                  !places_ok(a->w_to, kv->layers > 1 ? a->to_layer_stride : far, a->to_stride, to_rows, kv->kv_heads))))
-        return fail(c, DM_EINVAL, "dm_kv_gather: kept, w and w_to need rows of at least entries * B of their tables");
+    const int64_t to_rows = (int64_t)(to->entries * c->cfg.block_size);
+    if ((rows && !places_ok(a->kept, 1, 0, a->kept_stride, rows, 1)) ||
+        (a->w && ((rows && !places_ok(a->w, kv->layers, a->w_layer_stride, a->w_stride, rows, kv->kv_heads)) ||
+                  !places_ok(a->w_to, kv->layers, a->to_layer_stride, a->to_stride, to_rows, kv->kv_heads))))
+        return fail(c, DM_EINVAL, "dm_kv_gather: kept, w and w_to need rows of at least entries * B of their tables, layers apart");
     DeviceGuard g(c->device);
     hipError_t e = join_selection(c);
     if (e == hipSuccess)

@@ -96,6 +96,30 @@ REFUSED = {
 }
 
 
+OVERLAP = {  # layers of which one's last head would be another's first; with one head each, the same places
+    "select": [dict(w_layer_stride=4800), dict(w_layer_stride=6399), dict(kv_heads=1, share=1, w_layer_stride=0),
+               dict(kv_heads=1, share=1, w_layer_stride=1599), dict(w_layer_stride=6500, w_stride=2000), dict(w_layer_stride=-6400)],
+    "gather": [dict(to_layer_stride=4800), dict(w_layer_stride=4800), dict(to_layer_stride=6399), dict(w_layer_stride=6399),
+               dict(kv=dict(kv_heads=1), share=1, to_layer_stride=0), dict(kv=dict(kv_heads=1), share=1, w_layer_stride=0)],
+}
+
+
+def scenario_overlap(x):
+    c = Calls(x)
+    launches = x.word("fake_launches")
+    for name, cases in OVERLAP.items():
+        call = getattr(c, name)
+        for bad in cases:
+            before = launches.value
+            assert call(**bad) == x.pk.DM_EINVAL, (name, bad)
+            assert launches.value == before and x.L.dm_last_error(c.h), (name, bad)
+    # one layer has no stride between layers; rows apart, the last one's end is what counts
+    assert c.select(layers=1, w_layer_stride=0) == x.pk.DM_OK
+    assert c.select(w_stride=2000, w_layer_stride=7600) == x.pk.DM_OK
+    assert c.gather(kv=dict(layers=1), w_layer_stride=0, to_layer_stride=0) == x.pk.DM_OK
+    assert c.gather(to_stride=(1 << 40) - 1, to_layer_stride=1 << 43) == x.pk.DM_OK
+
+
 def scenario_refusals(x):
     c = Calls(x)
     launches = x.word("fake_launches")
@@ -211,6 +235,10 @@ def test_weights_work_area(fake):  # noqa: F811
 
 def test_refusals(fake):  # noqa: F811
     _child(fake, "refusals")
+
+
+def test_layers_do_not_overlap(fake):  # noqa: F811
+    _child(fake, "overlap")
 
 
 def test_work_areas(fake):  # noqa: F811
