@@ -799,9 +799,10 @@ typedef struct {
  * those of its kept tokens, of another those of all.  from and to have the same n
  * sequences.  Pages that are written must not be pages of `from` (those that
  * dm_pages_fork adds are not), w_to must not overlap w.  Other places are left as
- * they were.  to->len is not read.  A malformed table, a sequence whose kept rows
- * have no room in `to`, an entry of kept that is no token of its sequence and a
- * page out of range are reported (DM_EINVAL), and nothing is moved for them. */
+ * they were.  to->len is not read.  A sequence without entries in `to` (freed by the fork)
+ * has nothing moved.  A malformed table, a negative budget, a sequence whose kept rows have
+ * too little room in `to`, an entry of kept that is no token of its sequence and a page out
+ * of range are reported (DM_EINVAL), and nothing is moved for them. */
 dm_status dm_kv_gather(dm_ctx* ctx, const dm_kv_pages* kv, const dm_page_tables* from,
                        const dm_page_tables* to, const dm_gather_args* args);
 

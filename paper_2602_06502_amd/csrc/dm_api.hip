@@ -1219,7 +1219,7 @@ dm_status dm_kv_gather(dm_ctx* c, const dm_kv_pages* kv, const dm_page_tables* f
         return fail(c, DM_EINVAL, "dm_kv_gather: the tables must have as many sequences");
     if (dm_status s = share_check(c, kv->kv_heads, a->share, "dm_kv_gather"); s != DM_OK)
         return s;
-    if (to->n == 0 || to->entries == 0)
+    if (to->n == 0)
         return DM_OK;
     if (!a->budget || !aligned(a->budget))
         return fail(c, DM_EINVAL, "dm_kv_gather: null or misaligned budget");
@@ -1227,7 +1227,7 @@ dm_status dm_kv_gather(dm_ctx* c, const dm_kv_pages* kv, const dm_page_tables* f
     const int64_t to_rows = (int64_t)(to->entries * c->cfg.block_size);
     if ((rows && !places_ok(a->kept, 1, 0, a->kept_stride, rows, 1)) ||
         (a->w && ((rows && !places_ok(a->w, kv->layers, a->w_layer_stride, a->w_stride, rows, kv->kv_heads)) ||
-                  !places_ok(a->w_to, kv->layers, a->to_layer_stride, a->to_stride, to_rows, kv->kv_heads))))
+                  (to_rows && !places_ok(a->w_to, kv->layers, a->to_layer_stride, a->to_stride, to_rows, kv->kv_heads)))))
         return fail(c, DM_EINVAL, "dm_kv_gather: kept, w and w_to need rows of at least entries * B of their tables, layers apart");
     DeviceGuard g(c->device);
     hipError_t e = join_selection(c);

@@ -840,8 +840,20 @@ constexpr int kGatherThreads = 256;
 __global__ __launch_bounds__(kGatherThreads) void gather_kernel(GatherIn a, uint32_t* status)
 {
     constexpr int kAtOnce = 4;
+    const uint32_t tid = threadIdx.x;
+    const uint64_t moves = (uint64_t)a.to_entries * a.layers;
+    if (blockIdx.x >= moves) {
+        // after the moves, a sequence a thread: no entry's workgroup sees the tables of one that has none
+        const uint64_t s = (blockIdx.x - moves) * kGatherThreads + tid;
+        if (s < a.n) {
+            const int64_t t0 = a.to_off[s], t1 = a.to_off[s + 1];
+            if (t0 < 0 || t1 < t0 || t1 > a.to_entries || a.budget[s] < 0 || held(a.off, a.len, a.entries, (uint32_t)s, a.shift).bad)
+                atomicOr(status, kErrInval);
+        }
+        return;
+    }
     const int64_t e = blockIdx.x / a.layers;
-    const uint32_t l = blockIdx.x % a.layers, tid = threadIdx.x;
+    const uint32_t l = blockIdx.x % a.layers;
     const uint32_t s = wave_find(a.to_off, a.n, 1, e);
     const int64_t t0 = a.to_off[s], t1 = a.to_off[s + 1];
     if (e < t0 || e >= t1)
@@ -1021,7 +1033,7 @@ hipError_t kv_gather(dm_ctx* c, const dm_kv_pages& kv, const dm_page_tables& fro
     a.n_pages = kv.n_pages;
     a.shift = shift_of(c);
     a.dim = kv.head_dim;
-    const uint64_t grid = to.entries * kv.layers;
+    const uint64_t grid = to.entries * kv.layers + (to.n + kGatherThreads - 1) / kGatherThreads;
     if (grid > 0x7FFFFFFFull)
         return hipErrorInvalidValue;
     gather_kernel<<<(uint32_t)grid, kGatherThreads, 0, c->stream>>>(a, c->d_status);

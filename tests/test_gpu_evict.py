@@ -641,3 +641,33 @@ def test_a_malformed_sequence_frees_nothing(lens, budget, what):
     keep, grow, out, told = run(good, np.array([3, 4, 5], np.int64), good)
     assert not told and keep == [0, 0, lens[2]] and grow == [budget[0] + 3, budget[1] + 4, 5]
     assert out["len"].tolist() == [budget[0] + 3, budget[1] + 4, lens[2] + 5]
+
+
+def test_malformed_tables_without_entries_are_reported():
+    """Sequences that the next tables have no entry of: freed ones have nothing moved, malformed ones are reported all the same."""
+    pk, e = engine(16)
+    h = Histories(16, [100, 60, 40], seed=2)
+    k = torch.randn((2, h.pages + 4, 4, 16, 64)).bfloat16().cuda()
+    kv, start = pk.KVPages(k, k.clone()), k.clone()
+    kept = dev(np.zeros((2, 4, h.rows), np.int32))
+    page = dev(np.array([h.pages, h.pages + 1], np.int32))
+
+    def run(length, to_off, budget, page=page):
+        to = (dev(np.array(to_off, np.int64)), page, dev(np.zeros(3, np.int64)))
+        e.kv_gather(kv, (dev(h.off), dev(h.page), dev(np.array(length, np.int64))), to, dev(np.array(budget, np.int64)), kept)
+        e.sync()
+
+    _say("freed")
+    run([100, 60, 40], [0, 0, 0, 0], [30, 30, 30])
+    run([100, 60, 40], [0, 0, 0, 0], [30, 30, 30], page=page[:0])
+    assert torch.equal(kv.k, start)
+    for length, to_off, budget in (([100, 600, 40], [0, 0, 0, 0], [30, 30, 30]), ([100, 60, -1], [0, 0, 0, 0], [30, 30, 30]),
+                                   ([100, 60, 40], [0, 0, 0, 0], [30, -1, 30]), ([100, 60, 40], [0, 0, -1, -1], [30, 30, 30]),
+                                   ([100, 60, 40], [2, 0, 0, 0], [30, 30, 30]), ([100, 60, 40], [0, 0, 0, 5], [30, 30, 30])):
+        for p in (page, page[:0]):
+            _say("reported", length, to_off, budget, p.numel())
+            with pytest.raises(pk.DMError):
+                run(length, to_off, budget, page=p)
+            # (a last sequence of more entries than there are is of this call's first ones: none of it is moved)
+            assert torch.equal(kv.k, start)
+    run([100, 60, 40], [0, 0, 0, 0], [30, 30, 30])
