@@ -463,3 +463,32 @@ def test_runs_with_malformed_arguments():
     mine.buf = other.buf
     w, told = run(b.src, plan=mine)
     assert told and bool((w == 7).all())
+
+
+@pytest.mark.parametrize("heads,dim,paired,new,dtype", [((8, 8), 64, False, [1], "bf16"), ((16, 8), 64, True, [1, 2], "f16"),
+                                                        ((48, 8), 64, False, [1, 3, 1], "bf16"), ((14, 7), 64, False, [1, 0, 4], "f16"),
+                                                        ((8, 8), 128, False, [2], "bf16"), ((8, 8), 256, False, [1], "f16")])
+def test_waves_of_several_heads(heads, dim, paired, new, dtype):
+    """So many places that a wave has several heads, the last set of them a short one: dealt to a run's sequences, which are
+    not a whole number of fours; the same batch without runs; a sequence with many rows among them."""
+    pages = 512 if dim < 256 else 256
+    n = 45 if pages == 512 else 87
+    seqs = [(new[i % len(new)], 5 + 3 * i % 47, 0) for i in range(n)]
+    b = Collected(16, seqs, prefixes=(16 * pages,), heads=heads, dim=dim, dtype=dtype, paired=paired, seed=heads[0] + dim)
+    a_wave = b.rows // 64 * heads[1] // (32 * torch.cuda.get_device_properties(0).multi_processor_count)
+    assert 4 <= a_wave < heads[1] and heads[1] % a_wave, a_wave
+    _say("several heads", heads, dim, paired, new, "a wave", a_wave)
+    b.check()
+    b.check(groups=False)
+
+
+@pytest.mark.parametrize("n,heads", [(13, (16, 8)), (26, (16, 8)), (35, (8, 8)), (22, (6, 6))])
+def test_waves_of_few_heads(n, heads):
+    """Two to four heads a wave, below and at the number from which on they are dealt; one sequence with many rows."""
+    seqs = [(1 if i != 2 else 300, 5 + 3 * i % 47 + (300 if i == 2 else 0), 0) for i in range(n)]
+    b = Collected(16, seqs, prefixes=(16 * (512 if n != 13 else 700),), heads=heads, dim=64, seed=n)
+    a_wave = b.rows // 64 * heads[1] // (32 * torch.cuda.get_device_properties(0).multi_processor_count)
+    assert 2 <= a_wave <= 4, a_wave
+    _say("few heads", n, heads, "a wave", a_wave)
+    b.check()
+    b.check(groups=False)
