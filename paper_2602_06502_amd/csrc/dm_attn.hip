@@ -39,15 +39,16 @@ namespace {
 constexpr int kPlanThreads = 512;
 
 // The tiles of a unit, by its rows, and their cost a key: a wide one of 128 rows takes up
-// to twice a narrow one's time.  wide: rows of a wide tile; kNarrow: there are none.
-__device__ __forceinline__ uint32_t tile_rows(uint64_t rows, uint32_t wide) { return rows <= kNarrowRows ? kNarrow : wide; }
-__device__ __forceinline__ uint32_t tile_flags(uint64_t rows, uint32_t wide) 
+// to twice a narrow one's time.  wide: rows of a wide tile, a power of two (the plan's
+// kernel divides by it where its chain of steps waits); kNarrow: there are none.
+__device__ __forceinline__ uint32_t tile_flags(uint64_t rows, uint32_t wide)
 {
     return rows <= kNarrowRows || wide == kNarrow ? 0 : kUnitWide;
 }
 __device__ __forceinline__ uint64_t tiles_of(uint64_t rows, uint32_t wide)
 {
-    return (rows + tile_rows(rows, wide) - 1) / tile_rows(rows, wide);
+    const uint32_t tile = rows <= kNarrowRows ? kNarrow : wide;
+    return (rows + tile - 1) >> __builtin_ctz(tile);
 }
 __device__ __forceinline__ uint64_t weight_of(uint64_t rows, uint32_t wide)
 {
