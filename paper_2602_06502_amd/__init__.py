@@ -258,9 +258,9 @@ class KVPages:
 class AttnPlan:
     """A plan of DualMap.attn_plan or, with pairs, diff_plan: the batch that it was made for."""
 
-    def __init__(self, batch, q_tokens, kv, q_heads, buf, keep, pairs=False):
+    def __init__(self, batch, q_tokens, kv, q_heads, buf, pairs, n, entries, keep):
         self.batch, self.q_tokens, self.kv, self.q_heads, self.buf = batch, q_tokens, kv, q_heads, buf
-        self.pairs, self.n, self.entries = pairs, keep[0][2].numel(), keep[0][1].numel()
+        self.pairs, self.n, self.entries = pairs, n, entries  # n sequences, their tables' entries
         self._keep = keep  # the batch's tensors
 
 
@@ -755,13 +755,13 @@ class DualMap:
     def attn_plan(self, kv: KVPages, tables, q_off, q_tokens: int, q_heads: int, groups=None) -> AttnPlan:
         """The work of attn for a batch (see dm_attn_plan), once for all layers.
         groups: int64 [runs + 1], the runs of sequences that may share a prefix."""
-        return self._plan("dm_attn_plan", kv, tables, q_off, q_tokens, q_heads, groups, False)
+        return self._plan(self.lib.dm_attn_plan, kv, tables, q_off, q_tokens, q_heads, groups, False)
 
     def diff_plan(self, kv: KVPages, tables, q_off, q_tokens: int, q_heads: int, groups=None) -> AttnPlan:
         """The work of diff_attn for a batch (see dm_diff_plan), as attn_plan."""
-        return self._plan("dm_diff_plan", kv, tables, q_off, q_tokens, q_heads, groups, True)
+        return self._plan(self.lib.dm_diff_plan, kv, tables, q_off, q_tokens, q_heads, groups, True)
 
-    def _plan(self, name, kv, tables, q_off, q_tokens, q_heads, groups, pairs):
+    def _plan(self, call, kv, tables, q_off, q_tokens, q_heads, groups, pairs):
         self._kv(kv)
         b = self._batch(tables, q_off, q_tokens, groups)
         need = self.lib.dm_attn_plan_bytes(b[3], b[8])
@@ -773,8 +773,8 @@ class DualMap:
             with torch.cuda.stream(self.stream):
                 buf = torch.empty(need, dtype=torch.uint8, device=self.device)
         batch = _PACK_BATCH(*b)
-        self._check(getattr(self.lib, name)(self._h, batch, kv._ref, q_heads, buf.data_ptr(), need), name)
-        return AttnPlan(batch, q_tokens, kv, q_heads, buf, (tables, q_off, groups), pairs)
+        self._check(call(self._h, batch, kv._ref, q_heads, buf.data_ptr(), need), "dm_diff_plan" if pairs else "dm_attn_plan")
+        return AttnPlan(batch, q_tokens, kv, q_heads, buf, pairs, b[3], b[4], (tables, q_off, groups))
 
     def attn(self, plan: AttnPlan, layer: int, q, scale: float, out, lse=None) -> None:
         """Attention of a batch's new tokens over layer's pages (see dm_attn): q
