@@ -571,12 +571,14 @@ __device__ __forceinline__ uint32_t find_unit(const uint32_t* item0, uint32_t un
     return k ? k - 1 : 0;
 }
 
-// Is the plan one of this batch?
+// Is the plan one of this batch?  (Without short cuts: the head's words by one wait, not one
+// after the other, which a single token's pass would notice.)
 __device__ __forceinline__ bool plan_of(const PlanHead& h, const TokenBatch& b, uint32_t q_heads, uint32_t kv_heads,
                                         uint32_t head_dim)
 {
-    return h.n == b.n && h.groups == b.groups && h.q_tokens == b.q_tokens && h.q_heads == q_heads &&
-           h.kv_heads == kv_heads && h.shift == b.shift && h.entries == b.entries && h.head_dim == head_dim;
+    const uint64_t entries = (uint64_t)(h.entries ^ b.entries);
+    return ((h.n ^ b.n) | (h.groups ^ b.groups) | (h.q_tokens ^ b.q_tokens) | (h.q_heads ^ q_heads) | (h.kv_heads ^ kv_heads) |
+            (h.shift ^ b.shift) | (h.head_dim ^ head_dim) | (uint32_t)entries | (uint32_t)(entries >> 32)) == 0;
 }
 
 // Is the plan this call's, of at most `items` items?  (A batch whose q_off is out of
@@ -584,8 +586,8 @@ __device__ __forceinline__ bool plan_of(const PlanHead& h, const TokenBatch& b, 
 __device__ __forceinline__ bool plan_fits(const PlanHead& h, const AttnIn& a, uint64_t part_rows,
                                           uint32_t head_dim, uint32_t wide, uint32_t items)
 {
-    return plan_of(h, a.b, a.q_heads, a.kv_heads, head_dim) && h.wide == wide && h.part_rows <= part_rows &&
-           h.items <= items;
+    return plan_of(h, a.b, a.q_heads, a.kv_heads, head_dim) & (h.wide == wide) & (h.part_rows <= part_rows) &
+           (h.items <= items);
 }
 
 // The unit of this workgroup's item; false: none, or the plan is another batch's
