@@ -667,8 +667,9 @@ typedef struct {
  * out = gain o, or, with norm, gain o / sqrt(mean(o^2) + eps) * norm, over the
  * pair's 2 * head_dim elements, which are heads 2j and 2j + 1 of out.  lse is
  * that of each query head.  Who sees what, empty rows (zeros), groups, errors,
- * the work area and the roundings are dm_attn's for heads of 2 * head_dim; the
- * difference and the norm are in 32 bits.  kv_heads even, head_dim 64 or 128.
+ * the work area and the roundings are dm_attn's for heads of 2 * head_dim, each map's
+ * of that map's size, also where the maps cancel; the difference and the norm are
+ * in 32 bits.  kv_heads even, head_dim 64 or 128.
  * dm_diff_plan makes the plan, of dm_attn_plan_bytes(n, groups) bytes; it holds
  * for dm_diff_attn as one of dm_attn_plan does for dm_attn. */
 dm_status dm_diff_plan(dm_ctx* ctx, const dm_token_batch* batch, const dm_kv_pages* kv,

@@ -10,6 +10,13 @@
 // them.  Rows that are whole are subtracted, normed and written where they end; those in
 // parts are joined by a second kernel, map by map, and subtracted there.
 //
+// Wide tiles round a row's weights to the pages' type before they meet the values, as in plain
+// attention, whose comment has the reasons; the difference, the sums and the norm are in 32 bits.
+// So an error of either map's size, not of the difference's, stays where the maps cancel.  With the
+// weights in two parts, as narrow tiles have them, the prompts below take 1,897 us instead of 1,196
+// and the tails 510 instead of 367, for errors of 0.0017 instead of 0.0022 of the output (rounding
+// it alone makes 0.0017) and of 0.00021 instead of 0.00029.
+//
 // Bound as attention is: narrow tiles by reading the pages, wide ones by the matrix and
 // vector units (each weight meets two head_dims of values, so the matrix unit has three
 // quarters of its work there, where it has half in plain attention).  32 query and 8 key heads: 64
@@ -158,7 +165,7 @@ __global__ __launch_bounds__(JOIN* kWave) void diff_join_kernel(DiffIn a, const 
         __syncthreads();
         if (wave)
             continue;
-        // wave 0: both maps, from four waves each
+        // wave 0: both maps, from half of the waves each
         vper o[2];
         const float lambda = a.lambda[x / 2];
 #pragma unroll
@@ -231,7 +238,9 @@ dm_kv_pages pairs_of(const dm_kv_pages& kv)
 
 // Heads of 128: where sequences have no more rows a pair than a narrow tile on average, and
 // no runs, every tile is narrow, and one kernel has them all.  (The other one's workgroups
-// would have been there only to see that they have nothing to do.)
+// would have been there only to see that they have nothing to do.)  By the mean: a chunk of 64
+// tokens beside 63 single ones, 32 query and 8 key heads, 8,192 keys each, is 32 narrow tiles for
+// a pair, each reading the chunk's keys: 473 us, the 63 alone 380.
 uint32_t diff_wide(const dm_kv_pages& kv, const dm_token_batch& b, uint32_t q_heads)
 {
     if (kv.head_dim != 128)

@@ -238,16 +238,16 @@ __global__ __launch_bounds__(kThreads) void weights_rows_kernel(WeightsIn a, con
 
 // Sums for sequences with up to ROWS rows each (4, 8 or 16), 16 / ROWS of them in one product:
 // a lane has in sum[c] key c * 16 + lane % 16's of the sequence that has its quarter of the
-// rows.  member(n): the lane of `of` that has the n-th sequence.
-template <typename T, int D, int ROWS, typename Member>
+// rows.  Lane n of `of` has the n-th sequence.
+template <typename T, int D, int ROWS>
 __device__ __forceinline__ void packed_weights(const WeightsIn& a, const Known& of, uint32_t n0, uint32_t count,
-                                               Member&& member, uint32_t x0, uint32_t xs,
+                                               uint32_t x0, uint32_t xs,
                                                const typename Vec8<T>::type (&k)[4][D / 32], WordsOf<16>& words,
                                                float (&sum)[4])
 {
     using V = typename Vec8<T>::type;
     const uint32_t lane = lane_id(), quarter = lane / 16, n = n0 + lane % 16 / ROWS, r = lane % ROWS;
-    const uint32_t from = member(n < count ? n : n0);
+    const uint32_t from = n < count ? n : n0;
     const uint32_t tok0 = __shfl(of.tok0, from), ntok = __shfl(of.ntok, from);
     const uint32_t first = a.last && a.last < ntok ? ntok - a.last : 0, rows = (ntok - first) * a.ratio;
     const bool there = n < count && r < rows;
@@ -390,7 +390,6 @@ __device__ __forceinline__ void each_sequence(const TokenBatch& b, const PlanVie
 
 // A wave has 64 slots and a few heads one after another.  A run's shared keys are read for
 // kShared of its sequences at once, by the blocks of one of these, or of each for some heads.
-
 // RUNS: the batch has runs (a kernel of its own: its registers would halve the other's waves).
 template <typename T, int D, bool RUNS>
 __global__ __launch_bounds__(kThreads, D == 256 ? (RUNS ? 1 : 2) : RUNS && D == 128 ? 2 : 3) void weights_kernel(WeightsIn a, const PlanView pv,
@@ -502,14 +501,13 @@ __global__ __launch_bounds__(kThreads, D == 256 ? (RUNS ? 1 : 2) : RUNS && D == 
                     collect(of_lane(of, (uint32_t)__builtin_ctzll(next)), h, i0, 0, x.own0, false);
             return;
         }
-        auto member = [&](uint32_t n) { return n; };
         auto packed = [&](auto size) {
             constexpr int kRows = decltype(size)::value;
             for (uint32_t h = first; h < h1; h += step) {
                 const uint32_t x0 = a.paired ? h / 2 * 2 * a.ratio + h % 2 : h * a.ratio, xs = a.paired ? 2 : 1;
                 load(h);
                 for (uint32_t n0 = 0; n0 < count; n0 += 16 / kRows) {
-                    const uint32_t n = n0 + lane / 16 * 4 / kRows, from = member(n < count ? n : n0);
+                    const uint32_t n = n0 + lane / 16 * 4 / kRows, from = n < count ? n : n0;
                     const bool writes = n < count && lane / 16 * 4 % kRows == 0;
                     const int64_t at = __shfl((long long)of.at, from), old = __shfl((long long)of.old, from);
                     const uint32_t keep = __shfl(of.keep, from), len = __shfl(of.len, from);
@@ -519,7 +517,7 @@ __global__ __launch_bounds__(kThreads, D == 256 ? (RUNS ? 1 : 2) : RUNS && D == 
                         const int64_t i = i0 + c * 16 + lane % 16;
                         carried[c] = writes && i >= 0 && i < keep ? a.decay * a.prev[(int64_t)h * a.prev_stride + old + i] : 0.0f;
                     }
-                    packed_weights<T, D, kRows>(a, of, n0, count, member, x0, xs, k, words, sum);
+                    packed_weights<T, D, kRows>(a, of, n0, count, x0, xs, k, words, sum);
 #pragma unroll
                     for (int c = 0; c < 4; c++) {
                         const int64_t i = i0 + c * 16 + lane % 16;
@@ -823,7 +821,11 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : D == 128 ? 2 : 3) void wei
 // How many stretches of rows tall blocks are for (0: there are none), and their rows: some 32
 // workgroups a compute unit if all sequences are alike (two prompts of 7,000 to 8,192 tokens: 6
 // 728 us, 16 or 32 665), not more than kParts, nor than kSums sums.  A batch with hardly more
-// tokens than sequences has none: where one sequence has them all, those are a few rows yet.
+// tokens than sequences (kMany rows) is taken for a decode step, whose blocks would find nothing
+// to do, and has none.  By these numbers alone it cannot be told from one where a few sequences
+// have all the new tokens among many that have none, which is slower for it: 512 tokens of one
+// sequence, 64 query and 8 key heads of 128, 4,096 keys, take 191 us among 64 places, 1,792 among
+// 512 or 1,024.
 uint32_t parts_of_rows(const dm_ctx* c, const dm_token_batch& b, uint32_t ratio, uint32_t last, uint64_t blocks,
                        uint32_t* part_rows)
 {
