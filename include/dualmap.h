@@ -744,7 +744,8 @@ dm_status dm_attn_weights(dm_ctx* ctx, const dm_token_batch* batch, const dm_kv_
  * rows of kept_stride entries.  share: 1, or 2 for pairs, up to kv_heads; it
  * divides kv_heads.  Strides at least entries * B, from layer to layer at least
  * the rows of one, (kv_heads - 1) * w_stride + entries * B (not looked at where
- * there is one layer). */
+ * there is one layer).  kept, keep and grow must not overlap an input: budgets and
+ * lengths are read for every layer. */
 typedef struct {
     const float* w;
     int64_t w_layer_stride, w_stride;

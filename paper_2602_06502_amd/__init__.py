@@ -892,8 +892,8 @@ class DualMap:
                      share: int = 1) -> None:
         """What sequences past their budgets keep, by the weight that keys have collected (see
         dm_evict_select).  w: float32 [layers, kv_heads, places] as attn_weights lays out a layer's; budget,
-        room (or None), keep, grow: int64 [sequences], the last two pages_fork's arguments; kept: int32
-        [layers, kv_heads / share, places]."""
+        room (or None), keep, grow: int64 [sequences], the last two pages_fork's arguments, in memory of their
+        own; kept: int32 [layers, kv_heads / share, places]."""
         t, tb = self.torch, self._tables(tables)
         places = tb[4] * self.block
         if getattr(w, "ndim", 0) != 3 or share < 1 or w.shape[1] % share:
